@@ -46,7 +46,7 @@ typedef enum {
     DVDQ_ERR_ARCH = 8,           /* current device is not sm_100 */
     DVDQ_ERR_CUDA = 9,           /* a CUDA runtime or driver call failed */
     DVDQ_ERR_DEVICE_TIMEOUT = 10,/* a kernel gave up on a bounded device-side wait */
-    DVDQ_ERR_UNSUPPORTED = 11    /* an option that is not built (scale_group other than 0, 128, 256, 1024; unknown activation function) */
+    DVDQ_ERR_UNSUPPORTED = 11    /* an option that is not built (scale_group other than 0, 128, 256, 1024; unknown activation function or element type) */
 } dvdq_status;
 
 /* Human-readable name of a status code (static storage, never NULL). */
@@ -314,6 +314,112 @@ int32_t dvdq_gbs_next_bits(dvdq_gbs_state* g /* host */);
 /* Adds L1(F, t) = l1_change / l1_prev of the step that just finished.  An all-zero F_{t-1}
  * counts as relative change 1 if F_t differs from it, else 0. */
 dvdq_status dvdq_gbs_observe(dvdq_gbs_state* g /* host */, double l1_change, double l1_prev);
+
+/* ==== around the quantized layers =====================================================
+ *
+ * What a video transformer and its latent decoder run next to the quantized linear layers, in the
+ * same manner (device pointers, caller's workspace, asynchronous on the stream): the linear layers
+ * that stay in 16-bit floating point (embedders, modulation, output projections), rotary positions
+ * of queries and keys between the fused projection and attention, and the decoder's group norm; each with
+ * its gradients.  Sums, statistics and activations are in fp32 (fp64 across partial sums); every
+ * output is rounded once.  Results do not depend on the order in which CTAs run: no atomics. */
+typedef enum { DVDQ_BF16 = 0, DVDQ_F16 = 1, DVDQ_F32 = 2 } dvdq_dtype;
+typedef enum {
+    DVDQ_ACT_NONE = 0,
+    DVDQ_ACT_GELU_TANH = 1,      /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+    DVDQ_ACT_SILU = 2            /* z / (1 + exp(-z)); the operators below only */
+} dvdq_act;
+
+/* ---- linear layer in 16-bit floating point: y = act(x W^T + bias) + residual -----------
+ *
+ *   X [M, K], W [N, K], Y [M, N]   dtype DVDQ_BF16 or DVDQ_F16, all the same; row pitches ldx, ldw, ldy
+ *   bias [N] or NULL, R [M, N] or NULL (the residual, pitch ldr; R may be Y itself), same type
+ *   Z [M, N] or NULL               the pre-activation z = x W^T + bias, for the backward pass (pitch ldz)
+ * fp32 accumulation on the tensor cores; bias, activation and residual in fp32, one rounding each for y and z.
+ * Matrices start on 16 bytes and pitches are multiples of 8 elements (DVDQ_ERR_ALIGN); M, N and K
+ * themselves are arbitrary, and what lies between a row's last element and the pitch is neither read nor
+ * written.  The pitch of a single row is not read.  M == 0 is a no-op.  Few tokens: the contraction is
+ * cut into pieces, whose fp32 sums live in the workspace (dvdq_linear_workspace_bytes, often 0; 256-byte aligned). */
+size_t dvdq_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, int64_t N, int64_t K, int64_t ldw,
+                        const void* bias, const void* R, int64_t ldr, int32_t act, void* Y, int64_t ldy,
+                        void* Z, int64_t ldz, int32_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Its gradients:  dz = dy act'(z),  dX = dz W,  dW = dz^T X,  dbias = sum over tokens of dz  (the residual's
+ * gradient is dy itself).  dY, Z, X, W, dX, dW as above in one dtype; dbias fp32 [N].  dX, dW and dbias may each be
+ * NULL: not computed.  Z is not read for DVDQ_ACT_NONE; X only for dW, W only for dX.  dz is rounded to dtype for
+ * the tensor cores; dbias sums it unrounded.  M == 0 writes zeros to dW and dbias.
+ * The outputs are written, not added to.  Workspace: 256-byte aligned. */
+size_t dvdq_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t act);
+dvdq_status dvdq_linear_backward(const void* dY, int64_t lddy, const void* Z, int64_t ldz, const void* X, int64_t ldx,
+                                 const void* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t act,
+                                 void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias, int32_t dtype,
+                                 void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---- rotary positions ----------------------------------------------------------------------
+ *
+ * Channels (a, b) of a head turn by the angle position * freq_i: (a cos - b sin, b cos + a sin), with
+ * (a, b) = (x[2i], x[2i+1]) (DVDQ_ROPE_PAIRS) or (x[i], x[i + rot_dim/2]) (DVDQ_ROPE_HALVES); channels from
+ * rot_dim on pass through.  Three steps: frequencies (host), a table of cosines and sines (once per
+ * set of positions), and the rotation of q and k (every layer).
+ *
+ * dvdq_rope_frequencies  freqs_out [rot_dim / 2] and *amplitude_out (host, fp64): freq_i = theta^(-2i/rot_dim), and
+ *   for contexts longer than the trained one
+ *     DVDQ_ROPE_LINEAR     every frequency / factor (positions interpolated)
+ *     DVDQ_ROPE_BASE       theta' = theta factor^(rot_dim/(rot_dim-2)): the highest frequency stays, the lowest is / factor
+ *     DVDQ_ROPE_BY_PARTS   pairs that turn more than beta_fast times over original_length stay, those that turn less than
+ *                          beta_slow times are / factor, in between a ramp over the pair index; amplitude
+ *                          0.1 ln(factor) + 1
+ *   rot_dim even, <= 512. */
+typedef enum { DVDQ_ROPE_PAIRS = 0, DVDQ_ROPE_HALVES = 1 } dvdq_rope_layout;
+typedef enum { DVDQ_ROPE_PLAIN = 0, DVDQ_ROPE_LINEAR = 1, DVDQ_ROPE_BASE = 2, DVDQ_ROPE_BY_PARTS = 3 } dvdq_rope_scaling;
+dvdq_status dvdq_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double original_length,
+                                  double beta_fast, double beta_slow, double* freqs_out /* host */,
+                                  double* amplitude_out /* host */);
+/* table_out [rows, pairs, 2] fp32 (16-byte aligned) = amplitude (cos, sin)(positions[row][axis_of_pair[i]] freqs[i]), angles in
+ * fp64.  positions (device) int32 [rows, axes], or NULL with axes == 1: position = row.  A video's positions have three
+ * axes (frame, row, column), each with its share of the pairs.  freqs [pairs] and axis_of_pair [pairs] (NULL: axis 0) are on the HOST. */
+dvdq_status dvdq_rope_table(const double* freqs /* host */, const int32_t* axis_of_pair /* host */, int32_t pairs,
+                            const int32_t* positions, int64_t rows, int32_t axes, double amplitude, float* table_out,
+                            void* cuda_stream);
+/* One of q and k: [B, S, heads, head_dim] with unit stride inside a head, strides in elements; x and y are the same
+ * memory with the same strides, or do not overlap.  They may be views of a fused projection's output. */
+typedef struct {
+    const void* x;
+    void* y;
+    int64_t heads;
+    int64_t x_batch, x_token, x_head;
+    int64_t y_batch, y_token, y_head;
+} dvdq_rope_tensor;
+/* Rotates q and (if not NULL) k.  Token (b, s) takes table row rows[b * rows_batch + s] (device, int32; rows_batch 0: the
+ * same for all sequences), or row s if rows is NULL.  A row outside [0, table_rows) gives NaN in the rotated channels and DVDQ_ERR_SHAPE
+ * in dvdq_last_device_status (detail 16).  inverse != 0 turns the other way: the gradient.  dtype: any.
+ * B == 0 or S == 0 is a no-op. */
+dvdq_status dvdq_rope(const dvdq_rope_tensor* q /* host */, const dvdq_rope_tensor* k /* host */, int64_t B, int64_t S,
+                      int32_t head_dim, int32_t rot_dim, const float* table, int64_t table_rows, const int32_t* rows,
+                      int64_t rows_batch, int32_t layout, int32_t inverse, int32_t dtype, void* cuda_stream);
+
+/* ---- group norm with an activation, channels last -----------------------------------------
+ *
+ * X [N, S, C] (samples, places, channels; pitches x_sample and x_place in elements, unit stride of channels), groups of
+ * C / G neighbouring channels:  h = (x - mean) rstd with mean and variance over the group's S * C / G values,
+ * rstd = 1 / sqrt(variance + eps);  y = act(gamma_c h + beta_c).
+ *   gamma, beta [C] or NULL (1 and 0), of type param_dtype: X's, or DVDQ_F32
+ *   mean_out, rstd_out [N, G] fp32 or NULL: what the backward pass reads
+ * Y may be X itself (same pitches).  N <= 65535, C <= 2^20.  S == 0: statistics (0, 1 / sqrt(eps)). */
+size_t dvdq_group_norm_workspace_bytes(int64_t N, int64_t S, int64_t C, int64_t G);
+dvdq_status dvdq_group_norm(const void* X, int64_t x_sample, int64_t x_place, int64_t N, int64_t S, int64_t C, int64_t G,
+                            const void* gamma, const void* beta, int32_t param_dtype, float eps, int32_t act,
+                            void* Y, int64_t y_sample, int64_t y_place, float* mean_out, float* rstd_out, int32_t dtype,
+                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* Its gradients, with dz = dy act'(z) and dh = gamma dz:  dX = rstd (dh - <dh> - h <dh h>), <.> the mean over the group;
+ * dgamma = sum dz h, dbeta = sum dz over samples and places (fp32 [C]).  dX, dgamma, dbeta may each be NULL.
+ * dX may be dY or X itself (same pitches).  Same workspace size as the forward call. */
+dvdq_status dvdq_group_norm_backward(const void* dY, int64_t dy_sample, int64_t dy_place, const void* X, int64_t x_sample,
+                                     int64_t x_place, const float* mean, const float* rstd, int64_t N, int64_t S, int64_t C,
+                                     int64_t G, const void* gamma, const void* beta, int32_t param_dtype, int32_t act,
+                                     void* dX, int64_t dx_sample, int64_t dx_place, float* dgamma, float* dbeta,
+                                     int32_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* ---- test / debug entry points (so that no caller depends on the packed layouts) ---- */
 

@@ -27,7 +27,17 @@ EXPORTS = [
     "dvdq_rotate_weights", "dvdq_quantize_weights_symmetric", "dvdq_int8_mma_ceiling", "dvdq_debug_wait_timeout",
     "dvdq_weight_operand_bytes", "dvdq_widen_weights",
     "dvdq_bgr_quantize", "dvdq_gbs_l1_terms", "dvdq_gbs_init", "dvdq_gbs_next_bits", "dvdq_gbs_observe",
+    "dvdq_linear_workspace_bytes", "dvdq_linear", "dvdq_linear_backward_workspace_bytes", "dvdq_linear_backward",
+    "dvdq_rope_frequencies", "dvdq_rope_table", "dvdq_rope",
+    "dvdq_group_norm_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_backward",
 ]
+
+# element types, activations and rotary options of include/dvdq.h
+BF16, F16, F32 = range(3)
+ACT_NONE, ACT_GELU_TANH, ACT_SILU = range(3)
+ROPE_PAIRS, ROPE_HALVES = range(2)
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = range(4)
+_DTYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 
 class DvdqError(RuntimeError):
@@ -48,6 +58,13 @@ class Weights(C.Structure):
     _fields_ = [("magic", C.c_uint32), ("version", C.c_uint32), ("N", C.c_int64), ("K", C.c_int64),
                 ("rot_block", C.c_int32), ("k_layout", C.c_int32), ("blob", C.c_void_p),
                 ("blob_bytes", C.c_uint64), ("operand", C.c_void_p), ("operand_bytes", C.c_uint64)]
+
+
+class RopeTensor(C.Structure):
+    """dvdq_rope_tensor: one of q and k, [B, S, heads, head_dim], strides in elements."""
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("heads", C.c_int64),
+                ("x_batch", C.c_int64), ("x_token", C.c_int64), ("x_head", C.c_int64),
+                ("y_batch", C.c_int64), ("y_token", C.c_int64), ("y_head", C.c_int64)]
 
 
 class GbsState(C.Structure):
@@ -108,6 +125,18 @@ def load():
         "dvdq_gbs_init": (C.c_int, [C.POINTER(GbsState), C.c_double, i32, i32]),
         "dvdq_gbs_next_bits": (i32, [C.POINTER(GbsState)]),
         "dvdq_gbs_observe": (C.c_int, [C.POINTER(GbsState), C.c_double, C.c_double]),
+        "dvdq_linear_workspace_bytes": (sz, [i64, i64, i64]),
+        "dvdq_linear": (C.c_int, [p, i64, i64, p, i64, i64, i64, p, p, i64, i32, p, i64, p, i64, i32, p, sz, p]),
+        "dvdq_linear_backward_workspace_bytes": (sz, [i64, i64, i64, i32]),
+        "dvdq_linear_backward": (C.c_int, [p, i64, p, i64, p, i64, p, i64, i64, i64, i64, i32, p, i64, p, i64, p, i32, p, sz, p]),
+        "dvdq_rope_frequencies": (C.c_int, [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                            C.POINTER(C.c_double), C.POINTER(C.c_double)]),
+        "dvdq_rope_table": (C.c_int, [C.POINTER(C.c_double), C.POINTER(i32), i32, p, i64, i32, C.c_double, p, p]),
+        "dvdq_rope": (C.c_int, [C.POINTER(RopeTensor), C.POINTER(RopeTensor), i64, i64, i32, i32, p, i64, p, i64, i32, i32, i32, p]),
+        "dvdq_group_norm_workspace_bytes": (sz, [i64, i64, i64, i64]),
+        "dvdq_group_norm": (C.c_int, [p, i64, i64, i64, i64, i64, i64, p, p, i32, C.c_float, i32, p, i64, i64, p, p, i32, p, sz, p]),
+        "dvdq_group_norm_backward": (C.c_int, [p, i64, i64, p, i64, i64, p, p, i64, i64, i64, i64, p, p, i32, i32, p, i64, i64, p, p,
+                                               i32, p, sz, p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -247,6 +276,243 @@ def dvdq_qlinear_static(X: torch.Tensor, q: ActQuant, w: Weights, bias: Optional
     _check(load().dvdq_qlinear_static(_ptr(X, torch.bfloat16, "X"), X.shape[0], ldx, C.byref(q), C.byref(w),
                                       _ptr(bias, torch.bfloat16, "bias"), act, _ptr(Y, torch.bfloat16, "Y"), ldy,
                                       _stream(stream)), "dvdq_qlinear_static")
+
+
+# ------------------------------------------------------------------ around the quantized layers
+
+def _address(t: Optional[torch.Tensor], dtype, name: str, shape=None) -> Optional[int]:
+    """Device address of a tensor whose dtype (and shape) are as required; None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise TypeError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _vector(t: Optional[torch.Tensor], dtype, n: int, name: str) -> Optional[int]:
+    if t is not None and (t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1)):
+        raise TypeError(f"{name} must be a dense vector of {n} values")
+    return _address(t, dtype, name)
+
+
+def _matrix(t: Optional[torch.Tensor], dtype, rows: int, cols: int, name: str):
+    """(address, row pitch) of a [rows, cols] matrix with unit inner stride."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise TypeError(f"{name} must have shape {(rows, cols)}, got {tuple(t.shape)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise TypeError(f"{name} must have unit inner stride")
+    return _address(t, dtype, name), t.stride(0)
+
+
+def _element_type(t: torch.Tensor, name: str, allowed) -> int:
+    code = _DTYPES.get(t.dtype, -1)
+    if code not in allowed:
+        raise TypeError(f"{name} must be one of {[str(k) for k, v in _DTYPES.items() if v in allowed]}, got {t.dtype}")
+    return code
+
+
+def _room(workspace: Optional[torch.Tensor]):
+    if workspace is None:
+        return None, 0
+    return _address(workspace, torch.uint8, "workspace"), workspace.numel()
+
+
+def _raw_stream(stream, t: torch.Tensor) -> int:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return stream.cuda_stream
+
+
+def dvdq_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().dvdq_linear_workspace_bytes(M, N, K))
+
+
+def dvdq_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], residual: Optional[torch.Tensor], act: int,
+                Y: torch.Tensor, Z: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Y = act(X W^T + bias) + residual for X [M, K], W [N, K] in bf16 or fp16; Z, if given, receives the
+    pre-activation for dvdq_linear_backward.  residual may be Y itself.  Rows start on 16 bytes (pitches
+    are multiples of 8 elements); workspace: dvdq_linear_workspace_bytes(M, N, K) bytes, None where that is 0."""
+    dt = X.dtype
+    code = _element_type(X, "X", (BF16, F16))
+    if X.dim() != 2 or W.dim() != 2:
+        raise TypeError("X and W must be 2-D")
+    (M, K), N = X.shape, W.shape[0]
+    x, ldx = _matrix(X, dt, M, K, "X")
+    w, ldw = _matrix(W, dt, N, K, "W")
+    r, ldr = _matrix(residual, dt, M, N, "residual")
+    y, ldy = _matrix(Y, dt, M, N, "Y")
+    z, ldz = _matrix(Z, dt, M, N, "Z")
+    ws, room = _room(workspace)
+    _check(load().dvdq_linear(x, M, ldx, w, N, K, ldw, _vector(bias, dt, N, "bias"), r, ldr, act, y, ldy, z, ldz, code, ws, room,
+                              _raw_stream(stream, X)), "dvdq_linear")
+
+
+def dvdq_linear_backward_workspace_bytes(M: int, N: int, K: int, act: int) -> int:
+    return int(load().dvdq_linear_backward_workspace_bytes(M, N, K, act))
+
+
+def dvdq_linear_backward(dY: torch.Tensor, Z: Optional[torch.Tensor], X: Optional[torch.Tensor], W: Optional[torch.Tensor], act: int,
+                         dX: Optional[torch.Tensor], dW: Optional[torch.Tensor], dbias: Optional[torch.Tensor],
+                         workspace: torch.Tensor, stream=None) -> None:
+    """Gradients of dvdq_linear: dX [M, K], dW [N, K] (dY's type), dbias fp32 [N], each written if given.  Z is
+    the pre-activation (not read without an activation); X is needed for dW, W for dX.  The residual's gradient is dY."""
+    dt = dY.dtype
+    code = _element_type(dY, "dY", (BF16, F16))
+    if dY.dim() != 2:
+        raise TypeError("dY must be 2-D")
+    M, N = dY.shape
+    given = next((t for t in (X, W, dX, dW) if t is not None), None)
+    K = given.shape[1] if given is not None and given.dim() == 2 else 8  # only dbias asked for: no K is read
+    dy, lddy = _matrix(dY, dt, M, N, "dY")
+    z, ldz = _matrix(Z, dt, M, N, "Z")
+    x, ldx = _matrix(X, dt, M, K, "X")
+    w, ldw = _matrix(W, dt, N, K, "W")
+    dx, lddx = _matrix(dX, dt, M, K, "dX")
+    dw, lddw = _matrix(dW, dt, N, K, "dW")
+    ws, room = _room(workspace)
+    _check(load().dvdq_linear_backward(dy, lddy, z, ldz, x, ldx, w, ldw, M, N, K, act, dx, lddx, dw, lddw,
+                                       _vector(dbias, torch.float32, N, "dbias"), code, ws, room, _raw_stream(stream, dY)),
+           "dvdq_linear_backward")
+
+
+def dvdq_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+                          original_length: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(list of rot_dim / 2 frequencies, amplitude) on the host, optionally stretched for long contexts."""
+    freqs, amplitude = (C.c_double * max(1, rot_dim // 2))(), C.c_double(0.0)
+    _check(load().dvdq_rope_frequencies(rot_dim, theta, scaling, factor, original_length, beta_fast, beta_slow, freqs,
+                                        C.byref(amplitude)), "dvdq_rope_frequencies")
+    return list(freqs), amplitude.value
+
+
+def dvdq_rope_table(freqs, positions: Optional[torch.Tensor], table: torch.Tensor, axis_of_pair=None, amplitude: float = 1.0,
+                    stream=None) -> None:
+    """table [rows, pairs, 2] fp32 = amplitude * (cos, sin)(position * frequency).  positions: int32 [rows] or
+    [rows, axes], or None (position = row); axis_of_pair: for each pair, which axis it turns with."""
+    pairs = len(freqs)
+    if table.dim() != 3 or table.shape[1:] != (pairs, 2) or not table.is_contiguous():
+        raise TypeError(f"table must be dense [rows, {pairs}, 2]")
+    rows, axes = table.shape[0], 1
+    if positions is not None:
+        axes = 1 if positions.dim() == 1 else positions.shape[-1]
+        if positions.dim() not in (1, 2) or positions.shape[0] != rows or not positions.is_contiguous():
+            raise TypeError("positions must be dense [rows] or [rows, axes]")
+    if axis_of_pair is not None and len(axis_of_pair) != pairs:
+        raise TypeError("axis_of_pair must name an axis for each pair")
+    axis = (C.c_int32 * pairs)(*axis_of_pair) if axis_of_pair is not None else None
+    _check(load().dvdq_rope_table((C.c_double * pairs)(*freqs), axis, pairs, _address(positions, torch.int32, "positions"), rows, axes,
+                                  amplitude, _address(table, torch.float32, "table"), _raw_stream(stream, table)), "dvdq_rope_table")
+
+
+def _rope_tensor(x: torch.Tensor, y: torch.Tensor, shape, dtype, name: str) -> RopeTensor:
+    if x.dim() != 4 or x.shape[0] != shape[0] or x.shape[1] != shape[1] or x.shape[3] != shape[3]:
+        raise TypeError(f"{name} must be [B, S, heads, head_dim] like q")
+    xs, ys = x.stride(), y.stride()
+    if shape[3] > 1 and (xs[3] != 1 or ys[3] != 1):
+        raise TypeError(f"{name} must have unit stride inside a head")
+    return RopeTensor(_address(x, dtype, name), _address(y, dtype, name + "_out", x.shape), x.shape[2], xs[0], xs[1], xs[2],
+                      ys[0], ys[1], ys[2])
+
+
+def dvdq_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: torch.Tensor, rows: Optional[torch.Tensor], layout: int,
+              inverse: bool, q_out: torch.Tensor, k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rotates q [B, S, Hq, D] and k [B, S, Hk, D] (any strides with unit stride inside a head) into q_out and k_out, which
+    may be q and k themselves.  table [rows, rot_dim / 2, 2] of dvdq_rope_table; rows: int32 [B, S] or [S], the table
+    row of each token (None: token s takes row s).  inverse=True: the gradient."""
+    dt = q.dtype
+    code = _element_type(q, "q", (BF16, F16, F32))
+    if q.dim() != 4:
+        raise TypeError("q must be [B, S, heads, head_dim]")
+    B, S, _, D = q.shape
+    if (k is None) != (k_out is None):
+        raise TypeError("k and k_out come together")
+    if table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise TypeError("table must be dense [rows, rot_dim / 2, 2]")
+    batch = 0
+    if rows is not None:
+        if rows.shape != (B, S) and rows.shape != (S,):
+            raise TypeError("rows must be [B, S] or [S]")
+        if S > 1 and rows.stride(-1) != 1:
+            raise TypeError("rows must have unit stride along the tokens")
+        batch = rows.stride(0) if rows.dim() == 2 else 0
+    qt = _rope_tensor(q, q_out, q.shape, dt, "q")
+    kt = _rope_tensor(k, k_out, q.shape, dt, "k") if k is not None else None
+    _check(load().dvdq_rope(qt, kt, B, S, D, 2 * table.shape[1], _address(table, torch.float32, "table"), table.shape[0],
+                            _address(rows, torch.int32, "rows"), batch, layout, 1 if inverse else 0, code, _raw_stream(stream, q)), "dvdq_rope")
+
+
+def dvdq_group_norm_workspace_bytes(N: int, S: int, C_: int, G: int) -> int:
+    return int(load().dvdq_group_norm_workspace_bytes(N, S, C_, G))
+
+
+def _places(t: Optional[torch.Tensor], dtype, shape, name: str):
+    """(address, sample pitch, place pitch) of an [N, S, C] tensor with unit stride of channels."""
+    if t is None:
+        return None, 0, 0
+    if t.shape != shape:
+        raise TypeError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    st = t.stride()
+    if shape[2] > 1 and st[2] != 1:
+        raise TypeError(f"{name} must have unit stride of channels (channels last)")
+    return _address(t, dtype, name), st[0], st[1]
+
+
+def _norm_params(gamma, beta, dt, code: int, channels: int):
+    given = gamma if gamma is not None else beta
+    pt = dt if given is None else given.dtype
+    if pt is not dt and pt is not torch.float32:
+        raise TypeError(f"gamma and beta must be {dt} or torch.float32, got {pt}")
+    return _vector(gamma, pt, channels, "gamma"), _vector(beta, pt, channels, "beta"), code if pt is dt else F32
+
+
+def _group_stats(t: Optional[torch.Tensor], N: int, G: int, name: str):
+    if t is not None and (t.shape != (N, G) or not t.is_contiguous()):
+        raise TypeError(f"{name} must be dense [{N}, {G}]")
+    return _address(t, torch.float32, name)
+
+
+def dvdq_group_norm(X: torch.Tensor, G: int, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, act: int,
+                    Y: torch.Tensor, mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], workspace: torch.Tensor,
+                    stream=None) -> None:
+    """Y = act(group norm of X [N, S, C]) over G groups of neighbouring channels, channels last (places of a feature map
+    flattened to S); mean and rstd, if given, receive fp32 [N, G] for dvdq_group_norm_backward."""
+    dt = X.dtype
+    code = _element_type(X, "X", (BF16, F16, F32))
+    if X.dim() != 3:
+        raise TypeError("X must be [N, S, C]")
+    N, S, channels = X.shape
+    x, xn, xs = _places(X, dt, X.shape, "X")
+    y, yn, ys = _places(Y, dt, X.shape, "Y")
+    ga, be, param_code = _norm_params(gamma, beta, dt, code, channels)
+    ws, room = _room(workspace)
+    _check(load().dvdq_group_norm(x, xn, xs, N, S, channels, G, ga, be, param_code, eps, act, y, yn, ys, _group_stats(mean, N, G, "mean"),
+                                  _group_stats(rstd, N, G, "rstd"), code, ws, room, _raw_stream(stream, X)), "dvdq_group_norm")
+
+
+def dvdq_group_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, G: int,
+                             gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], act: int, dX: Optional[torch.Tensor],
+                             dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor], workspace: torch.Tensor,
+                             stream=None) -> None:
+    """Gradients of dvdq_group_norm: dX (X's type), dgamma and dbeta (fp32 [C]), each written if given."""
+    dt = X.dtype
+    code = _element_type(X, "X", (BF16, F16, F32))
+    if X.dim() != 3:
+        raise TypeError("X must be [N, S, C]")
+    N, S, channels = X.shape
+    x, xn, xs = _places(X, dt, X.shape, "X")
+    d, dn, ds = _places(dY, dt, X.shape, "dY")
+    y, yn, ys = _places(dX, dt, X.shape, "dX")
+    ga, be, param_code = _norm_params(gamma, beta, dt, code, channels)
+    ws, room = _room(workspace)
+    _check(load().dvdq_group_norm_backward(d, dn, ds, x, xn, xs, _group_stats(mean, N, G, "mean"), _group_stats(rstd, N, G, "rstd"), N, S,
+                                           channels, G, ga, be, param_code, act, y, yn, ys, _vector(dgamma, torch.float32, channels, "dgamma"),
+                                           _vector(dbeta, torch.float32, channels, "dbeta"), code, ws, room, _raw_stream(stream, X)),
+           "dvdq_group_norm_backward")
 
 
 # ------------------------------------------------------------------ test / debug entry points

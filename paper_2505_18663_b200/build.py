@@ -8,9 +8,9 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libdvdq.so")
-SOURCES = ["dvdq_lib.cu"]
+SOURCES = ["dvdq_lib.cu", "dvdq_block.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC"]
 
 
 def _nvcc() -> str:
@@ -30,16 +30,25 @@ def is_stale() -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile ``csrc/dvdq_lib.cu`` into ``libdvdq.so`` (cross-compiles without a GPU)."""
+    """Compile the sources of ``csrc`` side by side and link ``libdvdq.so`` (cross-compiles without a GPU)."""
     if not force and not is_stale():
         return LIB_PATH
-    tmp = LIB_PATH + f".tmp{os.getpid()}"
-    cmd = [_nvcc(), *NVCC_FLAGS]
-    if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += ["-o", tmp, *[os.path.join(CSRC, s) for s in SOURCES], "-lcudart"]
-    subprocess.run(cmd, check=True, cwd=CSRC)
-    os.replace(tmp, LIB_PATH)
+    tag = f".tmp{os.getpid()}"
+    flags = NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else [])
+    objects = [os.path.join(_HERE, s + tag + ".o") for s in SOURCES]
+    try:
+        jobs = [subprocess.Popen([_nvcc(), *flags, "-c", "-o", o, os.path.join(CSRC, s)], cwd=CSRC)
+                for s, o in zip(SOURCES, objects)]
+        codes = [j.wait() for j in jobs]
+        for s, code in zip(SOURCES, codes):
+            if code != 0:
+                raise subprocess.CalledProcessError(code, f"nvcc -c {s}")
+        subprocess.run([_nvcc(), *flags, "-shared", "-o", LIB_PATH + tag, *objects, "-lcudart"], check=True, cwd=CSRC)
+        os.replace(LIB_PATH + tag, LIB_PATH)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     return LIB_PATH
 
 

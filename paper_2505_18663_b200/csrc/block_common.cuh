@@ -1,0 +1,134 @@
+// What the 16-bit-float and fp32 operators around the quantized layers share (linear.cuh, rope.cuh,
+// group_norm.cuh): element types, vector accesses, the activations and their slopes.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "dvdq_common.cuh"
+
+namespace dvdq {
+
+// ------------------------------------------------------------------ element types
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+// the one rounding of an output: to nearest, ties to even
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t w);
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+
+template <typename T> struct IsBf16 { static constexpr int value = 0; };
+template <> struct IsBf16<__nv_bfloat16> { static constexpr int value = 1; };
+
+// V elements moved by one access (V * sizeof(T) = 2, 4, 8 or 16 bytes, aligned to that).
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Vec {
+    T e[V];
+};
+template <typename T, int V>
+__device__ __forceinline__ void load_f32(const T* p, float (&f)[V]) {
+    const Vec<T, V> v = *reinterpret_cast<const Vec<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void widen(const Vec<T, V>& v, float (&f)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
+}
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> narrow(const float (&f)[V]) {
+    Vec<T, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v.e[i] = from_f32<T>(f[i]);
+    return v;
+}
+
+// ------------------------------------------------------------------ activations
+
+// 1 / (1 + exp(-u)): one ex2.approx and one rcp.approx, about 1e-6 relative for |u| < 10.
+__device__ __forceinline__ float logistic(float u) {
+    float t, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(-1.4426950408889634f * u));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + t));
+    return r;
+}
+
+// Both activations are z f(u) with f the logistic function: u = z (SiLU), or u = sqrt(8 / pi)
+// (z + 0.044715 z^3) (GELU in its tanh form, since (1 + tanh(a)) / 2 = f(2a)).
+constexpr float kGeluA = 1.5957691216057308f;              // sqrt(8 / pi)
+constexpr float kGeluB = kGeluA * 0.044715f;
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if (ACT == DVDQ_ACT_NONE) return z;
+    const float u = ACT == DVDQ_ACT_SILU ? z : z * fmaf(kGeluB, z * z, kGeluA);
+    return z * logistic(u);
+}
+// d/dz of it: f + z u'(z) f (1 - f).  Past |z| = 20 the second term is below the smallest float
+// (u > 30, and z u' f (1 - f) < 1e-9 for SiLU, 0 for GELU), so z is held there: no overflow of z^3.
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if (ACT == DVDQ_ACT_NONE) return 1.0f;
+    const float c = z != z ? z : fminf(fmaxf(z, -20.0f), 20.0f);
+    const float u = ACT == DVDQ_ACT_SILU ? c : c * fmaf(kGeluB, c * c, kGeluA);
+    const float du = ACT == DVDQ_ACT_SILU ? 1.0f : fmaf(3.0f * kGeluB, c * c, kGeluA);
+    const float f = logistic(u);
+    return fmaf(c * du * f, 1.0f - f, f);
+}
+__device__ __forceinline__ float act_value_rt(int act, float z) {
+    return act == DVDQ_ACT_GELU_TANH ? act_value<DVDQ_ACT_GELU_TANH>(z) : act == DVDQ_ACT_SILU ? act_value<DVDQ_ACT_SILU>(z) : z;
+}
+
+// ------------------------------------------------------------------ dependent launches
+
+// A kernel launched with launch_after may start while its predecessor on the stream drains; it
+// must not touch the predecessor's results before wait_predecessor.
+__device__ __forceinline__ void wait_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void release_successor() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... Par, typename... Arg>
+inline cudaError_t launch_after(void (*kern)(Par...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Arg... arg) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<Par>(arg)...);
+}
+
+// ------------------------------------------------------------------ host helpers
+
+inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline int dtype_bytes(int32_t dtype) { return dtype == DVDQ_F32 ? 4 : 2; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace dvdq

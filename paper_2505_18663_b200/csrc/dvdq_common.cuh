@@ -63,14 +63,15 @@ __host__ __device__ inline int hi_field_shift(int a, int i) { return 2 * (4 * (i
 
 // ------------------------------------------------------------------ device status word
 
-// [0] = status (0 ok, else dvdq_status), [1] = detail of the first failure.  The library is a
-// single translation unit, so this is the one copy.
-__device__ uint32_t g_device_status[2] = {0u, 0u};
+// [0] = status (0 ok, else dvdq_status), [1] = detail of the first failure.  One copy per translation
+// unit; dvdq_last_device_status reads them all.
+static __device__ uint32_t g_device_status[2] = {0u, 0u};
 
 enum WaitId : uint32_t {
     kWaitPackedEmpty = 1, kWaitPackedFull = 2, kWaitWideEmpty = 3, kWaitWideFull = 4,
     kWaitAccEmpty = 5, kWaitAccFull = 6, kWaitDrain = 7, kWaitDebug = 8
 };
+constexpr uint32_t kDetailRopeRow = 16;  // DVDQ_ERR_SHAPE: a position's row is outside the table
 
 __device__ __forceinline__ void report_timeout(uint32_t detail) {
     if (atomicCAS(&g_device_status[0], 0u, (uint32_t)DVDQ_ERR_DEVICE_TIMEOUT) == 0u) g_device_status[1] = detail;
@@ -427,5 +428,14 @@ dvdq_status check_device_arch();
 dvdq_status validate_act_quant(const dvdq_act_quant* q, int64_t K);
 dvdq_status validate_weights(const dvdq_weights* w);
 dvdq_status cuda_status(cudaError_t e);
+// Reads and clears one translation unit's status word, the device already synchronized.
+inline dvdq_status read_status_word(const void* symbol, uint32_t (&h)[2]) {
+    h[0] = h[1] = 0u;
+    if (cudaMemcpyFromSymbol(h, symbol, sizeof h) != cudaSuccess) return DVDQ_ERR_CUDA;
+    const uint32_t zero[2] = {0u, 0u};
+    if (h[0] != 0u && cudaMemcpyToSymbol(symbol, zero, sizeof zero) != cudaSuccess) return DVDQ_ERR_CUDA;
+    return DVDQ_OK;
+}
+dvdq_status read_block_status(uint32_t (&h)[2]);  // dvdq_block.cu
 
 }  // namespace dvdq

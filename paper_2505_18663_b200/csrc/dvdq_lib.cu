@@ -1,6 +1,6 @@
 // C ABI of the library (see include/dvdq.h): argument validation, size queries and the
 // launches of the kernels in rotate_quantize.cuh, pack.cuh, weights.cuh, qgemm.cuh and
-// qgemm_ss.cuh.  One translation unit, so that the device status word is a single symbol.
+// qgemm_ss.cuh.  The 16-bit and fp32 operators around the quantized layers are in dvdq_block.cu.
 #include "dvdq_common.cuh"
 
 #include "bgr.cuh"
@@ -539,15 +539,12 @@ dvdq_status dvdq_debug_wait_timeout(uint64_t limit_ns, void* stream) {
 }
 
 dvdq_status dvdq_last_device_status(uint32_t* detail) {
-    uint32_t h[2] = {0u, 0u};
+    uint32_t h[2], other[2];
     if (cudaDeviceSynchronize() != cudaSuccess) return DVDQ_ERR_CUDA;
-    if (cudaMemcpyFromSymbol(h, g_device_status, sizeof h) != cudaSuccess) return DVDQ_ERR_CUDA;
-    if (h[0] != 0u) {
-        const uint32_t zero[2] = {0u, 0u};
-        if (cudaMemcpyToSymbol(g_device_status, zero, sizeof zero) != cudaSuccess) return DVDQ_ERR_CUDA;
-    }
-    if (detail) *detail = h[1];
-    return (dvdq_status)h[0];
+    if (read_status_word(g_device_status, h) != DVDQ_OK || read_block_status(other) != DVDQ_OK) return DVDQ_ERR_CUDA;
+    const uint32_t* first = h[0] != 0u ? h : other;
+    if (detail) *detail = first[1];
+    return (dvdq_status)first[0];
 }
 
 }  // extern "C"

@@ -1,0 +1,639 @@
+// The linear layer in 16-bit floating point and its gradients, as one kernel of matrix products
+//
+//   D[m, n] = sum_k A[m, k] B[n, k]     forward   D = z = X W^T      A = X  [M, K],    B = W [N, K]
+//                                       dX = dZ W                    A = dZ [M, N],    B = W^T
+//                                       dW = dZ^T X                  A = dZ^T,         B = X^T
+//
+// A transposed operand is read where it lies: tcgen05 takes shared-memory tiles whose contiguous
+// axis is the contracted one ("K-major") or the other one ("MN-major"), so nothing is transposed in memory.
+//
+// A CTA pair owns a 256 x 256 tile of D: tcgen05.mma.cta_group::2.kind::f16 256x256x16, operands in
+// shared memory (128-byte swizzle) in a ring of TMA-filled stages of 64 along k, two 256-column fp32
+// accumulators in tensor memory, so that the epilogue of a tile runs under the next tile's products.
+// Roles per CTA: warp 0 TMA producer; warp 1 (leader CTA) issues the products; warps 4-11 epilogue, two
+// per tensor-memory lane quarter, 128 columns each: bias, activation, residual in fp32, ONE rounding, and
+// TMA stores of 32 x 32 blocks; the residual's blocks come by TMA one block ahead.
+//
+// What bounds it: the tensor pipe on layers of thousands of tokens; with few tokens, streaming W.
+// Products with fewer tiles than CTA pairs are cut along k (`splits`): each piece writes its fp32 sums,
+// and a second kernel adds the pieces in a fixed order and does the epilogue (no atomics).
+#pragma once
+
+#include "block_common.cuh"
+#include "host_setup.cuh"
+
+namespace dvdq {
+
+constexpr int kLinBK = 64;                    // elements of k per stage: one 128-byte swizzle row
+constexpr int kLinTile = 256;                 // rows and columns of a pair's tile
+constexpr int kLinEpiWarps = 8, kLinFirstEpi = 4;
+constexpr int kLinThreads = (kLinFirstEpi + kLinEpiWarps) * 32;
+constexpr int kLinPairs = 74;                 // CTA pairs of a B200 (148 SMs): what the split along k is planned for
+
+enum LinOut { kLinFinal = 0, kLinFinalZ = 1, kLinPartial = 2 };
+
+template <int OUT>
+struct LinSmem {
+    // storing z as well takes a third output block per epilogue warp, and a stage less
+    static constexpr int kStages = OUT == kLinFinalZ ? 5 : 6;
+    static constexpr int kBufs = OUT == kLinFinalZ ? 3 : 2;
+    static constexpr int kOperand = 128 * kLinBK * 2;       // one CTA's half of an operand's stage
+    static constexpr int kStage = 2 * kOperand;
+    static constexpr int kBuf = 32 * 32 * 2;                // 32 x 32 outputs; fp32 partials use two as one
+    static constexpr int kBufOff = kStages * kStage;
+    static constexpr int kBiasOff = kBufOff + kLinEpiWarps * kBufs * kBuf;
+    static constexpr int kBarOff = kBiasOff + kLinEpiWarps * 32 * 4;
+    static constexpr int kNumBars = 2 * kStages + 5 + 2 * kLinEpiWarps;
+    static constexpr int kMiscOff = kBarOff + kNumBars * 8;
+    static constexpr int kTotal = kMiscOff + 16 + 1024;
+    static_assert(kTotal <= 232448, "more than the 227 KB of shared memory a CTA can have");
+};
+
+struct LinArgs {
+    int Md, Nd;             // rows and columns of D
+    int num_m, num_n;       // tiles
+    int kblocks, splits;    // k-blocks of the contraction, pieces it is cut into
+    int panel;              // column tiles walked together
+    int part_rows;          // rows of one piece in the partial buffer
+    int act, has_residual, has_z;
+    const void* bias;
+};
+
+// Item -> tile and piece.  Tiles are walked in panels of `panel` column tiles, columns fastest, so that the
+// tiles in flight together share rows and columns of the operands in L2; the pieces of a tile are neighbours.
+__device__ __forceinline__ void lin_item(const LinArgs& A, int item, int& tm, int& tn, int& piece) {
+    const int tile = item / A.splits;
+    piece = item - tile * A.splits;
+    const int per_panel = A.num_m * A.panel;
+    const int p = tile / per_panel, r = tile - p * per_panel;
+    const int w = min(A.panel, A.num_n - p * A.panel);
+    tm = r / w;
+    tn = p * A.panel + (r - tm * w);
+}
+__device__ __forceinline__ int2 lin_range(const LinArgs& A, int piece) {  // k-blocks of a piece: never empty
+    const int q = A.kblocks / A.splits, rest = A.kblocks - q * A.splits;
+    const int b = piece * q + min(piece, rest);
+    return make_int2(b, b + q + (piece < rest ? 1 : 0));
+}
+
+// Descriptor of a 64-wide MN-major tile with the 128-byte swizzle: rows of k are 128 bytes, eight of
+// them (1024 bytes) a swizzle atom; the next 64 columns are kLinBK rows = 8192 bytes further on.
+__device__ __forceinline__ uint64_t umma_desc_sw128_mnmajor(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr >> 4) & 0x3FFFu);
+    d |= (uint64_t)((kLinBK * 128) >> 4) << 16;
+    d |= (uint64_t)(1024u >> 4) << 32;
+    d |= (uint64_t)1u << 46;
+    d |= (uint64_t)2u << 61;
+    return d;
+}
+// Instruction descriptor for kind::f16: fp32 accumulator, both operands bf16 (or both fp16), and which
+// of them are MN-major.
+__host__ __device__ constexpr uint32_t umma_idesc_f16(bool bf16, bool a_mn, bool b_mn, int m, int n) {
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void tc_mma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// This CTA's 128 rows (or columns) of an operand's stage: one box of 64 x 128 rows, or two boxes of 64
+// columns x 64 rows of k; both count their bytes on the leader's barrier.
+template <bool MN>
+__device__ __forceinline__ void lin_load(uint32_t dst, const CUtensorMap* m, uint32_t bar, int k0, int r0) {
+    if (!MN) {
+        tma_load_2d_pair(dst, m, bar, k0, r0);
+    } else {
+        tma_load_2d_pair(dst, m, bar, r0, k0);
+        tma_load_2d_pair(dst + kLinBK * 128, m, bar, r0 + 64, k0);
+    }
+}
+
+template <typename T, bool AMN, bool BMN, int OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
+linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
+              const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ LinArgs A) {
+    using S = LinSmem<OUT>;
+    constexpr int ST = S::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+    const int items = A.num_m * A.num_n * A.splits;
+
+    const uint32_t bar0 = sbase + S::kBarOff;
+    auto full = [&](int s) { return bar0 + 8u * s; };                    // leader's copy: both CTAs' operands are in place
+    auto empty = [&](int s) { return bar0 + 8u * (ST + s); };            // one per CTA
+    auto acc_full = [&](int s) { return bar0 + 8u * (2 * ST + s); };     // one per CTA
+    auto acc_empty = [&](int s) { return bar0 + 8u * (2 * ST + 2 + s); };  // leader's copy
+    const uint32_t drain_bar = bar0 + 8u * (2 * ST + 4);
+    auto res_full = [&](int w, int b) { return bar0 + 8u * (2 * ST + 5 + 2 * w + b); };  // a warp's residual block has landed
+    volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kMiscOff);  // [0] tmem base, [1] abort
+    volatile uint32_t* abort_flag = misc + 1;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), 2 * kLinEpiWarps); }
+        mbar_init(drain_bar, 1);
+        for (int w = 0; w < kLinEpiWarps; ++w) { mbar_init(res_full(w, 0), 1); mbar_init(res_full(w, 1), 1); }
+        misc[1] = 0u;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(sbase + S::kMiscOff, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = misc[0];
+    wait_predecessor();
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            tma_prefetch_desc(&tmA);
+            tma_prefetch_desc(&tmB);
+            uint32_t st = 0, ph = 0;
+            bool ok = true;
+            for (int item = pair; ok && item < items; item += num_pairs) {
+                int tm, tn, piece;
+                lin_item(A, item, tm, tn, piece);
+                const int2 kr = lin_range(A, piece);
+                const int m0 = tm * kLinTile + (int)rank * 128, n0 = tn * kLinTile + (int)rank * 128;
+                for (int kb = kr.x; kb < kr.y; ++kb) {
+                    if (!mbar_wait(empty(st), ph ^ 1u, abort_flag, kWaitWideEmpty)) { ok = false; break; }
+                    if (rank == 0) mbar_arrive_expect_tx(full(st), 2 * S::kStage);
+                    const uint32_t bar = map_to_cta(full(st), 0), dst = sbase + st * S::kStage;
+                    lin_load<AMN>(dst, &tmA, bar, kb * kLinBK, m0);
+                    lin_load<BMN>(dst + S::kOperand, &tmB, bar, kb * kLinBK, n0);
+                    if (++st == ST) { st = 0; ph ^= 1u; }
+                }
+            }
+            if (!ok)  // giving up after seconds of waiting: a bounded pause covers the last copies
+                for (int it = 0; it < 64; ++it) __nanosleep(1000);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ products (leader CTA only)
+        if (rank == 0) {
+            constexpr uint32_t idesc = umma_idesc_f16(IsBf16<T>::value, AMN, BMN, kLinTile, kLinTile);
+            // 16 elements along k: 32 bytes inside a K-major swizzle row, two atoms of an MN-major tile
+            constexpr uint32_t kStepA = AMN ? 2048 / 16 : 2, kStepB = BMN ? 2048 / 16 : 2;
+            uint32_t st = 0, ph = 0, lt = 0;
+            bool ok = true;
+            for (int item = pair; ok && item < items; item += num_pairs, ++lt) {
+                int tm, tn, piece;
+                lin_item(A, item, tm, tn, piece);
+                const int2 kr = lin_range(A, piece);
+                const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
+                if (!mbar_wait_warp(acc_empty(a), aph ^ 1u, abort_flag, kWaitAccEmpty)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + a * kLinTile;
+                for (int kb = kr.x; kb < kr.y; ++kb) {
+                    if (!mbar_wait_warp(full(st), ph, abort_flag, kWaitWideFull)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t at = sbase + st * S::kStage;
+                        const uint64_t ad = AMN ? umma_desc_sw128_mnmajor(at) : umma_desc_sw128_kmajor(at);
+                        const uint64_t bd = BMN ? umma_desc_sw128_mnmajor(at + S::kOperand) : umma_desc_sw128_kmajor(at + S::kOperand);
+#pragma unroll
+                        for (int k = 0; k < kLinBK / 16; ++k)
+                            tc_mma_f16_pair(d_tmem, ad + kStepA * k, bd + kStepB * k, idesc, (kb != kr.x || k != 0) ? 1u : 0u);
+                        tc_commit_pair(empty(st), 3);
+                        if (kb + 1 == kr.y) tc_commit_pair(acc_full(a), 3);
+                    }
+                    __syncwarp();
+                    if (++st == ST) { st = 0; ph ^= 1u; }
+                }
+            }
+            if (elect_one()) tc_commit_pair(drain_bar, 1);
+            __syncwarp();
+            mbar_wait(drain_bar, 0u, abort_flag, kWaitDrain);
+        }
+        __syncwarp();
+    } else if (warp >= kLinFirstEpi) {
+        // ------------------------------------------------------------ epilogue
+        const int ew = warp - kLinFirstEpi;
+        const int q = warp & 3, half = ew >> 2;  // tensor-memory lane quarter; which 128 of the 256 columns
+        const uint32_t buf0 = sbase + S::kBufOff + ew * (S::kBufs * S::kBuf);
+        const uint32_t c_bias = sbase + S::kBiasOff + ew * 128;
+        const bool residual = OUT != kLinPartial && A.has_residual;
+        const bool with_bias = OUT != kLinPartial && A.bias != nullptr;
+        const T* bias = static_cast<const T*>(A.bias);
+        if (lane == 0) tma_prefetch_desc(&tmY);
+        uint32_t lt = 0, blk = 0, rload = 0, rwait = 0;  // output blocks so far; residual blocks asked for / taken
+        bool ok = true;
+        // asks for the residual of the block at (row, col) into output buffer `rload & 1`
+        auto ask = [&](int row, int col) {
+            if (lane == 0) {
+                tma_store_wait_read<0>();
+                mbar_arrive_expect_tx(res_full(ew, rload & 1u), S::kBuf);
+                tma_load_2d(buf0 + (rload & 1u) * S::kBuf, &tmR, res_full(ew, rload & 1u), col, row);
+            }
+            ++rload;
+        };
+        for (int item = pair; ok && item < items; item += num_pairs, ++lt) {
+            int tm, tn, piece;
+            lin_item(A, item, tm, tn, piece);
+            const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
+            const int row0 = tm * kLinTile + (int)rank * 128 + q * 32, col0 = tn * kLinTile + half * 128;
+            // 32 x 32 blocks of this warp that lie in D
+            const int blocks = row0 < A.Md && col0 < A.Nd ? min(4, (A.Nd - col0 + 31) >> 5) : 0;
+            float b_next = 0.f;
+            if (with_bias && blocks > 0 && col0 + lane < A.Nd) b_next = to_f32(bias[col0 + lane]);
+            __syncwarp();
+            if (residual && blocks > 0) ask(row0, col0);
+            ok = mbar_wait_warp(acc_full(a), aph, abort_flag, kWaitAccFull);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < blocks; ++c) {
+                uint32_t r[32];
+                __syncwarp();
+                tmem_ld_32x32(tmem_base + a * kLinTile + half * 128 + c * 32 + ((uint32_t)(q * 32) << 16), r);
+                if (OUT == kLinPartial) {
+                    if (lane == 0) tma_store_wait_read<0>();
+                    __syncwarp();
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)  // rows of 128 bytes, 16-byte chunk index XORed with row % 8
+                        sts128(buf0 + lane * 128 + ((j ^ (lane & 7)) << 4), r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&tmY, buf0, col0 + c * 32, piece * A.part_rows + row0);
+                        tma_store_commit();
+                    }
+                    continue;
+                }
+                // the block's output buffer: free once all but the newest store have been read
+                // (with a residual, ask() has waited for it)
+                if (residual && c + 1 < blocks) ask(row0, col0 + (c + 1) * 32);
+                if (!residual && lane == 0) tma_store_wait_read<1>();
+                if (with_bias) sts32f(c_bias + 4 * lane, b_next);
+                __syncwarp();
+                if (with_bias && c + 1 < blocks) b_next = col0 + (c + 1) * 32 + lane < A.Nd ? to_f32(bias[col0 + (c + 1) * 32 + lane]) : 0.f;
+                const uint32_t buf = buf0 + ((residual ? rwait : blk) & 1u) * S::kBuf;
+                if (residual) {
+                    ok = mbar_wait_warp(res_full(ew, rwait & 1u), (rwait >> 1) & 1u, abort_flag, kWaitPackedFull);
+                    ++rwait;
+                    if (!ok) break;
+                }
+                ++blk;
+                tmem_ld_wait();
+                float v[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+                if (with_bias) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = lds128f(c_bias + 4 * j);
+                        v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+                    }
+                }
+                // rows of 64 bytes, 16-byte chunk index XORed with (row / 2) % 4: what the swizzled TMA copies use
+                auto at = [&](uint32_t base, int j) { return base + lane * 64 + (((j >> 3) ^ ((lane >> 1) & 3)) << 4); };
+                if (OUT == kLinFinalZ) {
+                    const uint32_t zb = buf0 + 2 * S::kBuf;
+                    if (residual && lane == 0) tma_store_wait_read<0>();  // z's own buffer
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8)
+                        sts128(at(zb, j), pack2<T>(v[j], v[j + 1]), pack2<T>(v[j + 2], v[j + 3]), pack2<T>(v[j + 4], v[j + 5]),
+                               pack2<T>(v[j + 6], v[j + 7]));
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&tmZ, zb, col0 + c * 32, row0);
+                        tma_store_commit();
+                    }
+                }
+                if (A.act == DVDQ_ACT_GELU_TANH) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = act_value<DVDQ_ACT_GELU_TANH>(v[j]);
+                } else if (A.act == DVDQ_ACT_SILU) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = act_value<DVDQ_ACT_SILU>(v[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    if (residual) {
+                        const uint4 w = lds128(at(buf, j));
+                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const float2 f = unpack2<T>(ws[t]);
+                            v[j + 2 * t] += f.x;
+                            v[j + 2 * t + 1] += f.y;
+                        }
+                    }
+                    sts128(at(buf, j), pack2<T>(v[j], v[j + 1]), pack2<T>(v[j + 2], v[j + 3]), pack2<T>(v[j + 4], v[j + 5]),
+                           pack2<T>(v[j + 6], v[j + 7]));
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d(&tmY, buf, col0 + c * 32, row0);
+                    tma_store_commit();
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(a), 0));
+        }
+        if (lane == 0) {
+            tma_store_wait_all();
+            // gave up with a residual block in flight: let it land (bounded) before the CTA exits
+            for (; rwait < rload; ++rwait)
+                for (int it = 0; it < (1 << 16) && !mbar_try_wait(res_full(ew, rwait & 1u), (rwait >> 1) & 1u); ++it) {}
+        }
+        __syncwarp();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    release_successor();
+    cluster_sync_all();
+    if (warp == 1) tmem_dealloc(tmem_base, 512);
+}
+
+// ------------------------------------------------------------------ joining the pieces
+
+// y = act(sum of the pieces + bias) + residual, four columns per thread; pieces are added in order.
+template <typename T>
+__global__ void __launch_bounds__(256)
+linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pitch, int splits, int64_t Md, int Nd, const T* __restrict__ bias,
+                   const T* residual, int64_t ldr, int act, T* y, int64_t ldy, T* z, int64_t ldz) {
+    wait_predecessor();
+    const int quads = (Nd + 3) >> 2;
+    const int64_t total = Md * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / quads;
+        const int n = (int)(i - m * quads) * 4;
+        const float* p = part + m * pitch + n;
+        float4 s = *reinterpret_cast<const float4*>(p);
+#pragma unroll 4
+        for (int k = 1; k < splits; ++k) {
+            const float4 t = *reinterpret_cast<const float4*>(p + k * piece_floats);
+            s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+        }
+        float v[4] = {s.x, s.y, s.z, s.w};
+        const int here = Nd - n < 4 ? Nd - n : 4;
+        if (bias) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < here) v[j] += to_f32(bias[n + j]);
+        }
+        if (here == 4) {  // rows start on 16 bytes and n is a multiple of 4: 8-byte accesses
+            if (z) *reinterpret_cast<uint2*>(z + m * ldz + n) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = act_value_rt(act, v[j]);
+            if (residual) {
+                const uint2 w = *reinterpret_cast<const uint2*>(residual + m * ldr + n);
+                const float2 f0 = unpack2<T>(w.x), f1 = unpack2<T>(w.y);
+                v[0] += f0.x; v[1] += f0.y; v[2] += f1.x; v[3] += f1.y;
+            }
+            *reinterpret_cast<uint2*>(y + m * ldy + n) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+        } else {
+            for (int j = 0; j < here; ++j) {
+                if (z) z[m * ldz + n + j] = from_f32<T>(v[j]);
+                float o = act_value_rt(act, v[j]);
+                if (residual) o += to_f32(residual[m * ldr + n + j]);
+                y[m * ldy + n + j] = from_f32<T>(o);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ backward: dz and its column sums
+
+// dz = dy act'(z) in fp32, rounded once to the operands' type for the tensor cores (an fp32 dz would cost
+// the two products half of their rate or more); the bias's gradient sums the unrounded values.
+// A CTA takes 256 columns (8 per thread, 32 threads side by side, 8 rows at a time) of one chunk of
+// rows and writes their sums; linear_colsum_kernel adds the chunks.  act = none: dz is dy itself, only sums.
+constexpr int kLinDzThreads = 256, kLinDzCols = 256;
+
+template <typename T, int ACT>
+__global__ void __launch_bounds__(kLinDzThreads)
+linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, int64_t M, int N, int64_t rows,
+                 T* __restrict__ dz, int64_t lddz, float* __restrict__ sums) {
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int n = blockIdx.x * kLinDzCols + tx * 8;
+    const int64_t m0 = (int64_t)blockIdx.y * rows, m1 = m0 + rows < M ? m0 + rows : M;
+    float s[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = 0.f;
+    const int here = N - n < 8 ? N - n : 8;
+    if (here > 0) {
+        // rows start on 16 bytes and have room for whole 16-byte groups up to the pitch, but only the
+        // first N values of a row are the caller's: the last group goes element by element
+        auto row = [&](int64_t m, const Vec<T, 8>& d, const Vec<T, 8>& zz) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = to_f32(d.e[j]);
+                if (ACT != DVDQ_ACT_NONE) v[j] *= act_slope<ACT>(to_f32(zz.e[j]));
+                s[j] += v[j];
+            }
+            if (ACT != DVDQ_ACT_NONE) *reinterpret_cast<Vec<T, 8>*>(dz + m * lddz + n) = narrow<T, 8>(v);
+        };
+        if (here == 8) {
+            constexpr int U = 4;
+            int64_t m = m0 + ty;
+            for (; m + (U - 1) * 8 < m1; m += U * 8) {
+                Vec<T, 8> d[U], zz[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    d[u] = *reinterpret_cast<const Vec<T, 8>*>(dy + (m + u * 8) * lddy + n);
+                    if (ACT != DVDQ_ACT_NONE) zz[u] = *reinterpret_cast<const Vec<T, 8>*>(z + (m + u * 8) * ldz + n);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) row(m + u * 8, d[u], zz[u]);
+            }
+            for (; m < m1; m += 8) {
+                Vec<T, 8> zz = {};
+                if (ACT != DVDQ_ACT_NONE) zz = *reinterpret_cast<const Vec<T, 8>*>(z + m * ldz + n);
+                row(m, *reinterpret_cast<const Vec<T, 8>*>(dy + m * lddy + n), zz);
+            }
+        } else {
+            for (int64_t m = m0 + ty; m < m1; m += 8) {
+                Vec<T, 8> d, zz;
+                for (int j = 0; j < 8; ++j) {
+                    d.e[j] = from_f32<T>(0.f);
+                    zz.e[j] = from_f32<T>(0.f);
+                    if (j < here) {
+                        d.e[j] = dy[m * lddy + n + j];
+                        if (ACT != DVDQ_ACT_NONE) zz.e[j] = z[m * ldz + n + j];
+                    }
+                }
+                row(m, d, zz);  // dz is the workspace's: whole groups may be written
+            }
+        }
+    }
+    if (sums) {
+        __shared__ float sh[8][kLinDzCols + 8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sh[ty][tx * 8 + j] = s[j];
+        __syncthreads();
+        const int c = blockIdx.x * kLinDzCols + threadIdx.x;
+        if (c < N) {
+            float t = 0.f;
+#pragma unroll
+            for (int y = 0; y < 8; ++y) t += sh[y][threadIdx.x];
+            sums[(int64_t)blockIdx.y * N + c] = t;
+        }
+    }
+    release_successor();
+}
+
+__global__ void __launch_bounds__(256) linear_colsum_kernel(const float* __restrict__ sums, int chunks, int N, float* __restrict__ out) {
+    wait_predecessor();
+    __shared__ double sh[8][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
+    double t = 0.0;
+    if (c < N)
+        for (int i = w; i < chunks; i += 8) t += sums[(int64_t)i * N + c];
+    sh[w][lane] = t;
+    __syncthreads();
+    if (w == 0 && c < N) {
+#pragma unroll
+        for (int y = 1; y < 8; ++y) t += sh[y][lane];
+        out[c] = (float)t;
+    }
+    release_successor();
+}
+
+// ------------------------------------------------------------------ host side
+
+struct LinPlan {
+    int splits;
+    int64_t part_rows, part_pitch, part_bytes;
+};
+
+// Pieces along k, from the sizes alone.  In units of one k-block's products (0.37 us per pair): a wave of
+// items costs its k-blocks plus about 8 for filling the ring and draining the last accumulator; cutting
+// costs writing and reading the fp32 pieces (about 6 TB/s of L2 traffic) and a launch (about 6 units).
+inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc) {
+    const int64_t tiles = ceil_div(Md, kLinTile) * ceil_div(Nd, kLinTile), kb = ceil_div(Kc, kLinBK);
+    LinPlan p;
+    p.splits = 1;
+    p.part_rows = align_up(Md, 32);
+    p.part_pitch = align_up(Nd, 4);
+    double best = 1e300;
+    for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
+        if (s > 1 && s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20)) break;
+        const double waves = (double)ceil_div(tiles * s, kLinPairs);
+        double cost = waves * ((double)ceil_div(kb, s) + 8.0);
+        if (s > 1) cost += 6.0 + (double)s * Md * Nd * 8.0 / 6.0e12 / 0.37e-6;
+        if (cost < best * 0.98) { best = cost; p.splits = (int)s; }
+    }
+    p.part_bytes = p.splits > 1 ? align_up(p.splits * p.part_rows * p.part_pitch * 4, 256) : 0;
+    return p;
+}
+
+// A 16-bit matrix [rows, cols] with row pitch ld elements, tiles of box_rows x box_cols.
+inline bool make_map16(CUtensorMap* tm, bool bf16, const void* base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
+                       uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+    PFN_encodeTiled enc = get_encode_tiled();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {box_cols, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(tm, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+           CUDA_SUCCESS;
+}
+inline bool make_map_f32(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld) {
+    PFN_encodeTiled enc = get_encode_tiled();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 4};
+    const cuuint32_t box[2] = {32, 32};
+    const cuuint32_t estr[2] = {1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct LinMatrix {
+    const void* p;
+    int64_t ld;
+};
+struct LinEpilogue {
+    const void* bias;
+    LinMatrix residual, z;
+    int act;
+};
+
+template <typename T, bool AMN, bool BMN, int OUT>
+static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
+                                     const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
+    constexpr bool bf = IsBf16<T>::value != 0;
+    using S = LinSmem<OUT>;
+    CUtensorMap tmA, tmB, tmY, tmR, tmZ;
+    auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows) {
+        return mn ? make_map16(m, bf, x.p, Kc, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
+                  : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, 128, CU_TENSOR_MAP_SWIZZLE_128B);
+    };
+    if (!operand(&tmA, AMN, a, Md) || !operand(&tmB, BMN, b, Nd)) return DVDQ_ERR_CUDA;
+    if (OUT == kLinPartial ? !make_map_f32(&tmY, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
+                           : !make_map16(&tmY, bf, y.p, Md, Nd, y.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+        return DVDQ_ERR_CUDA;
+    tmR = tmZ = tmY;  // where unused
+    const bool fin = OUT != kLinPartial;
+    if (fin && e.residual.p && !make_map16(&tmR, bf, e.residual.p, Md, Nd, e.residual.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
+    if (fin && e.z.p && !make_map16(&tmZ, bf, e.z.p, Md, Nd, e.z.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
+    LinArgs A;
+    A.Md = (int)Md;
+    A.Nd = (int)Nd;
+    A.num_m = (int)ceil_div(Md, kLinTile);
+    A.num_n = (int)ceil_div(Nd, kLinTile);
+    A.kblocks = (int)ceil_div(Kc, kLinBK);
+    A.splits = plan.splits;
+    A.panel = A.num_n < 8 ? A.num_n : 8;
+    A.part_rows = (int)plan.part_rows;
+    A.act = e.act;
+    A.has_residual = fin && e.residual.p != nullptr;
+    A.has_z = OUT == kLinFinalZ;
+    A.bias = fin ? e.bias : nullptr;
+    auto kern = linear_kernel<T, AMN, BMN, OUT>;
+    static PerDevice<int> cache;
+    const int max_pairs = resident_pairs(cache, kern, kLinThreads, S::kTotal);
+    if (max_pairs == 0) return DVDQ_ERR_CUDA;
+    const int64_t items = (int64_t)A.num_m * A.num_n * A.splits;
+    const unsigned pairs = (unsigned)(items < max_pairs ? items : max_pairs);
+    return cuda_status(launch_after(kern, dim3(2 * pairs), dim3(kLinThreads), S::kTotal, st, tmA, tmB, tmY, tmR, tmZ, A));
+}
+
+// D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.
+template <typename T, bool AMN, bool BMN>
+static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
+                                 const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
+    if (plan.splits == 1) {
+        // only the forward product stores its pre-activation
+        if constexpr (!AMN && !BMN) {
+            if (e.z.p) return launch_linear_out<T, AMN, BMN, kLinFinalZ>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+        }
+        return launch_linear_out<T, AMN, BMN, kLinFinal>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+    }
+    dvdq_status s = launch_linear_out<T, AMN, BMN, kLinPartial>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+    if (s != DVDQ_OK) return s;
+    const int64_t quads = Md * ((Nd + 3) / 4);
+    const int64_t ctas = ceil_div(quads, 256);
+    return cuda_status(launch_after(linear_join_kernel<T>, dim3((unsigned)(ctas < 148 * 8 ? ctas : 148 * 8)), dim3(256), 0, st, part,
+                                    plan.part_rows * plan.part_pitch, (int)plan.part_pitch, plan.splits, Md, (int)Nd,
+                                    static_cast<const T*>(e.bias), static_cast<const T*>(e.residual.p), e.residual.ld, e.act,
+                                    static_cast<T*>(const_cast<void*>(y.p)), y.ld, static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld));
+}
+
+}  // namespace dvdq

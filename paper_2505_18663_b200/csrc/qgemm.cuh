@@ -21,6 +21,7 @@
 #pragma once
 
 #include "dvdq_common.cuh"
+#include "host_setup.cuh"
 
 namespace dvdq {
 
@@ -42,22 +43,6 @@ __device__ __forceinline__ float gelu_tanh_f32(float y) {
 }
 
 // ------------------------------------------------------------------ host side
-
-typedef CUresult (*PFN_encodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-inline PFN_encodeTiled get_encode_tiled() {
-    static PFN_encodeTiled fn = nullptr;
-    if (!fn) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-            qres == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<PFN_encodeTiled>(p);
-    }
-    return fn;
-}
 
 // bf16 matrix [rows, cols] with row pitch ld elements, tiles of 32 rows x 64 columns, 128-byte
 // swizzle (the layout the epilogue stages its output in).
@@ -86,31 +71,6 @@ inline bool make_byte_map(CUtensorMap* tm, const void* base, uint64_t row_len, u
     return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
                CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// One-time set-up of a pair kernel on the current device: the opt-in to its dynamic shared memory and
-// the number of CTA pairs the device keeps resident at once (one CTA per SM).  0 on failure.
-template <typename Kern>
-static int resident_pairs(PerDevice<int>& cache, Kern kern, int threads, int smem_bytes) {
-    int* mp = cache.get([&](int& max_pairs, int dev) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes) != cudaSuccess) return false;
-        int sm_count = 0;
-        if (cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return false;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(sm_count & ~1), 1, 1);
-        cfg.blockDim = dim3((unsigned)threads, 1, 1);
-        cfg.dynamicSmemBytes = (size_t)smem_bytes;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        int clusters = 0;
-        if (cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg) != cudaSuccess || clusters < 1) return false;
-        max_pairs = clusters < sm_count / 2 ? clusters : sm_count / 2;
-        return true;
-    });
-    return mp ? *mp : 0;
 }
 
 // qgemm_ss.cuh: activation codes stored one int8 per code

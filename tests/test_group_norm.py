@@ -1,0 +1,275 @@
+"""dvdq_group_norm and dvdq_group_norm_backward against the formulas in 64 bits.
+
+Tolerances.  With n = S C / G values per group, sums of d = x - pivot are fp32 over at most S / 32 + 32 steps per thread, then
+trees, then fp64: relative error of mean - pivot and of the second moment below e = 2^-24 * 64, taken of the sums' magnitudes
+(mean |d|, mean d^2 about the pivot).  h = (x - mean) rstd in fp32: 2^-22 |h| more.  One rounding u |y| of the output."""
+import math
+
+import pytest
+import torch
+
+from paper_2505_18663_b200 import binding as B
+
+gpu = pytest.mark.gpu
+DEV = "cuda"
+DTYPES = [torch.bfloat16, torch.float16, torch.float32]
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+EPS = 1e-5
+E = 64 * 2.0 ** -24
+
+# (N, S, C, G): one place; one channel per group; groups inside a 16-byte access and across several; channel counts that
+# 16 bytes do not divide; wide rows (channel blocks); one group of many channels (cut into pieces); long samples
+SHAPES = [(1, 1, 32, 2), (2, 1, 24, 1), (1, 70, 8, 8), (3, 77, 180, 12), (2, 50, 64, 32), (1, 333, 30, 3), (2, 64, 7, 7), (1, 40, 2304, 32),
+          (1, 9, 4160, 1), (2, 17, 600, 2), (1, 33, 5000, 8), (1, 20000, 128, 32), (4, 1000, 96, 4), (1, 3000, 5, 1)]
+
+
+def act64(z, act):
+    if act == B.ACT_SILU:
+        return z * torch.sigmoid(z)
+    if act == B.ACT_GELU_TANH:
+        return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+    return z
+
+
+def norm64(x, G, gamma, beta, act, eps=EPS):
+    N, S, C = x.shape
+    v = x.view(N, S, G, C // G)
+    mean = v.mean((1, 3), keepdim=True)
+    rstd = ((v - mean).square().mean((1, 3), keepdim=True) + eps).rsqrt()
+    h = ((v - mean) * rstd).reshape(N, S, C)
+    z = h * (gamma if gamma is not None else 1.0) + (beta if beta is not None else 0.0)
+    return act64(z, act), mean.reshape(N, G), rstd.reshape(N, G), h, z
+
+
+def make(shape, dt, seed, offset=0.5):
+    N, S, C, G = shape
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = (torch.randn(N, S, C, generator=g, device=DEV) + offset * torch.randn(N, 1, C, generator=g, device=DEV) + offset).to(dt)
+    gamma, beta = (1 + 0.3 * torch.randn(C, generator=g, device=DEV)), 0.3 * torch.randn(C, generator=g, device=DEV)
+    return x, gamma, beta, g
+
+
+def workspace(N, S, C, G):
+    return torch.full((max(1, B.dvdq_group_norm_workspace_bytes(N, S, C, G)),), 255, dtype=torch.uint8, device=DEV)
+
+
+def spreads(x, G):
+    """mean |d| and mean d^2 about each group's pivot, the first place's first channel"""
+    N, S, C = x.shape
+    v = x.view(N, S, G, C // G)
+    d = v - v[:, :1, :, :1]
+    return d.abs().mean((1, 3)), d.square().mean((1, 3))
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("act,params", [(0, None), (1, "own"), (2, "fp32")])
+def test_forward(dt, shape, act, params):
+    N, S, C, G = shape
+    x, gamma, beta, _ = make(shape, dt, S + C)
+    if params is None:
+        gamma = beta = None
+    elif params == "own":
+        gamma, beta = gamma.to(dt), beta.to(dt)
+    y = torch.full_like(x, float("nan"))
+    mean, rstd = (torch.full((N, G), float("nan"), device=DEV) for _ in range(2))
+    B.dvdq_group_norm(x, G, gamma, beta, EPS, act, y, mean, rstd, workspace(*shape))
+    x6 = x.double()
+    ga, be = (None if t is None else t.double() for t in (gamma, beta))
+    y6, m6, r6, h6, z6 = norm64(x6, G, ga, be, act)
+    a1, a2 = spreads(x6, G)
+    em = E * a1 + 2.0 ** -23 * m6.abs()                          # of the mean
+    ev = E * (a2 + a1 * a1) * 2                                   # of the variance
+    er = 0.5 * ev * r6 ** 3 * 1.5 + 2.0 ** -23 * r6               # of rstd
+    assert ((mean - m6).abs() <= em).all()
+    assert ((rstd - r6).abs() <= er).all()
+    wide = lambda t: t[:, None, :, None].expand(N, S, G, C // G).reshape(N, S, C)  # noqa: E731
+    eh = wide(em * r6) + h6.abs() * wide(er / r6) + 2.0 ** -21 * (h6.abs() + wide(m6.abs() * r6))
+    g_abs = ga.abs() if ga is not None else 1.0
+    inner = 1.13 * (eh * g_abs + 2.0 ** -22 * z6.abs()) + (2.0 ** -18 * z6.abs() if act else 0.0)
+    bound = inner + U[dt] * (y6.abs() + inner) + (2.0 ** -25 if dt == torch.float16 else 0)
+    assert ((y.double() - y6).abs() <= bound).all(), float(((y.double() - y6).abs() - bound).max())
+    y2 = x.clone()                                                # in place, without statistics: the same bits
+    B.dvdq_group_norm(y2, G, gamma, beta, EPS, act, y2, None, None, workspace(*shape))
+    assert torch.equal(y2, y)
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s[1] * s[2] // s[3] >= 16])
+@pytest.mark.parametrize("act,params", [(0, None), (1, "own"), (2, "fp32")])
+def test_backward(dt, shape, act, params):
+    N, S, C, G = shape
+    x, gamma, beta, g = make(shape, dt, 2 * S + C)
+    if params is None:
+        gamma = beta = None
+    elif params == "own":
+        gamma, beta = gamma.to(dt), beta.to(dt)
+    dy = torch.randn(N, S, C, generator=g, device=DEV).to(dt)
+    x6, dy6 = x.double(), dy.double()
+    ga = gamma.double() if gamma is not None else torch.ones(C, dtype=torch.float64, device=DEV)
+    be = beta.double() if beta is not None else torch.zeros(C, dtype=torch.float64, device=DEV)
+    _, m6, r6, _, _ = norm64(x6, G, ga, be, act)
+    mean, rstd = m6.float(), r6.float()
+    dx = torch.full_like(x, float("nan"))
+    dgamma, dbeta = (torch.full((C,), float("nan"), device=DEV) for _ in range(2))
+    ws = workspace(*shape)
+    B.dvdq_group_norm_backward(dy, x, mean, rstd, G, gamma, beta, act, dx, dgamma, dbeta, ws)
+    wide = lambda t: t[:, None, :, None].expand(N, S, G, C // G).reshape(N, S, C)  # noqa: E731
+    r = wide(rstd.double())
+    h = (x6 - wide(mean.double())) * r                             # the statistics that were given
+    eh = 2.0 ** -22 * (h.abs() + wide(mean.double().abs()) * r)
+    z = (h * ga + be).requires_grad_(True)
+    act64(z, act).sum().backward()
+    slope, z = z.grad, z.detach()
+    dz = dy6 * slope
+    # the slope's own slope is at most 1.2; ex2 / rcp: 2^-18 (1 + |z|)
+    ez = dy6.abs() * ((1.2 * (eh * ga.abs() + 2.0 ** -22 * z.abs()) + 2.0 ** -18 * (1 + z.abs())) if act else 0.0) + 2.0 ** -23 * dz.abs()
+    assert (dbeta - dz.sum((0, 1))).abs().le(ez.sum((0, 1)) + E * dz.abs().sum((0, 1))).all()
+    ezh = ez * h.abs() + dz.abs() * eh
+    assert (dgamma - (dz * h).sum((0, 1))).abs().le(ezh.sum((0, 1)) + E * (dz * h).abs().sum((0, 1))).all()
+    group = lambda t: wide(t.view(N, S, G, C // G).mean((1, 3)))   # noqa: E731
+    dh, edh = dz * ga, (ez + 2.0 ** -23 * dz.abs()) * ga.abs()
+    m1, m2 = group(dh), group(dh * h)
+    e1 = group(edh) + 2 * E * group(dh.abs())
+    e2 = group(ezh * ga.abs()) + 2 * E * group((dh * h).abs())
+    want = r * (dh - m1 - h * m2)
+    inner = r * (edh + e1 + h.abs() * e2 + eh * m2.abs() + 2.0 ** -22 * (dh.abs() + m1.abs() + (h * m2).abs()))
+    bound = inner + U[dt] * (want.abs() + inner) + (2.0 ** -25 if dt == torch.float16 else 0)
+    assert ((dx.double() - want).abs() <= bound).all(), float(((dx.double() - want).abs() - bound).max())
+    # each alone, and dx over dy: the same bits
+    d2 = dy.clone()
+    B.dvdq_group_norm_backward(d2, x, mean, rstd, G, gamma, beta, act, d2, None, None, ws)
+    g2, b2 = torch.empty_like(dgamma), torch.empty_like(dbeta)
+    B.dvdq_group_norm_backward(dy, x, mean, rstd, G, gamma, beta, act, None, g2, None, ws)
+    B.dvdq_group_norm_backward(dy, x, mean, rstd, G, gamma, beta, act, None, None, b2, ws)
+    assert torch.equal(d2, dx) and torch.equal(g2, dgamma) and torch.equal(b2, dbeta)
+
+
+@gpu
+def test_gradient_against_differences():
+    """fp32; f = sum(c y).  Central differences along sign(dx) with step 1/64: the third-order term is below 1 % of the
+    first for h of order one and steps of 2^-6 (relative (2^-6)^2 times a third derivative of order 10)."""
+    shape = N, S, C, G = 2, 19, 24, 3
+    x, gamma, beta, g = make(shape, torch.float32, 9)
+    c = torch.randn(N, S, C, generator=g, device=DEV)
+    y, mean, rstd, ws = torch.empty_like(x), torch.empty(N, G, device=DEV), torch.empty(N, G, device=DEV), workspace(*shape)
+
+    def f(xx, ga):
+        B.dvdq_group_norm(xx, G, ga, beta, EPS, B.ACT_SILU, y, mean, rstd, ws)
+        return float((y.double() * c.double()).sum())
+
+    f(x, gamma)
+    dx, dgamma = torch.empty_like(x), torch.empty(C, device=DEV)
+    B.dvdq_group_norm_backward(c, x, mean.clone(), rstd.clone(), G, gamma, beta, B.ACT_SILU, dx, dgamma, None, ws)
+    for t, grad in ((x, dx), (gamma, dgamma)):
+        d = torch.sign(grad) * 2.0 ** -6
+        diff = f(x + d, gamma) - f(x - d, gamma) if t is x else f(x, gamma + d) - f(x, gamma - d)
+        want = 2 * float((grad.double() * d.double()).sum())
+        assert abs(diff - want) <= 0.02 * abs(want), (diff, want)
+
+
+@gpu
+@pytest.mark.parametrize("C,pad", [(64, 8), (64, 3), (30, 0)])
+def test_pitches(C, pad):
+    """Places further apart than their channels, samples further apart than their places; nothing between is written."""
+    N, S, G, dt = 2, 37, 2, torch.bfloat16
+    x, gamma, beta, _ = make((N, S, C, G), dt, 10)
+    big = torch.full((N, S + 2, C + pad), float("nan"), dtype=dt, device=DEV)
+    xv = big[:, :S, :C]
+    xv.copy_(x)
+    out = torch.full_like(big, float("nan"))
+    yv, y = out[:, 1:S + 1, pad:], torch.empty_like(x)
+    B.dvdq_group_norm(xv, G, gamma, beta, EPS, 2, yv, None, None, workspace(N, S, C, G))
+    B.dvdq_group_norm(x, G, gamma, beta, EPS, 2, y, None, None, workspace(N, S, C, G))
+    # other accesses, other order of the sums: equal up to one rounding of the output
+    assert ((yv.double() - y.double()).abs() <= 2.0 ** -7 * y.double().abs() + 1e-5).all()
+    assert out[:, 0].isnan().all() and out[:, S + 1].isnan().all() and (pad == 0 or out[:, :, :pad].isnan().all())
+
+
+@gpu
+def test_a_mean_far_from_zero_costs_no_digits():
+    x = (1000.0 + torch.randn(1, 5000, 16, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)))
+    y, ws = torch.empty_like(x), workspace(1, 5000, 16, 2)
+    B.dvdq_group_norm(x, 2, None, None, 0.0, 0, y, None, None, ws)
+    want, _, _, _, _ = norm64(x.double(), 2, None, None, 0, eps=0.0)
+    # the mean itself is an fp32 number: 2^-24 * 1000 = 6e-5 of a value's size
+    assert (y.double() - want).abs().max() <= 1.2e-4
+
+
+@gpu
+def test_a_constant_group_gives_beta():
+    x = torch.full((1, 50, 8), 3.0, device=DEV)
+    beta, y, ws = torch.arange(8.0, device=DEV), torch.empty_like(x), workspace(1, 50, 8, 2)
+    B.dvdq_group_norm(x, 2, None, beta, EPS, 0, y, None, None, ws)
+    assert torch.equal(y, beta.expand_as(x))
+
+
+@gpu
+def test_nan_and_infinity_stay_in_their_group():
+    x = torch.randn(2, 40, 16, device=DEV)
+    x[0, 3, 1], x[1, 7, 9] = float("nan"), float("inf")
+    y = torch.empty_like(x)
+    B.dvdq_group_norm(x, 4, None, None, EPS, 0, y, None, None, workspace(2, 40, 16, 4))
+    bad = torch.zeros(2, 40, 16, dtype=torch.bool, device=DEV)
+    bad[0, :, 0:4] = True
+    bad[1, :, 8:12] = True
+    assert y[~bad].isfinite().all() and y[0, :, 0:4].isnan().all() and not y[1, :, 8:12].isfinite().all()
+
+
+@gpu
+def test_empty_samples():
+    e = torch.empty(2, 0, 8, device=DEV)
+    mean, rstd = torch.ones(2, 2, device=DEV), torch.ones(2, 2, device=DEV)
+    B.dvdq_group_norm(e, 2, None, None, 4.0, 0, e, mean, rstd, None)
+    assert (mean == 0).all() and (rstd == 0.5).all()
+    dg, db = torch.ones(8, device=DEV), torch.ones(8, device=DEV)
+    B.dvdq_group_norm_backward(e, e, mean, rstd, 2, None, None, 0, None, dg, db, None)
+    assert (dg == 0).all() and (db == 0).all()
+    z = torch.empty(0, 5, 8, device=DEV)
+    B.dvdq_group_norm(z, 2, None, None, EPS, 0, z, None, None, None)
+
+
+# ------------------------------------------------------------------ refusals (no GPU needed)
+
+P = 4096
+
+
+def forward(**k):
+    a = dict(X=P, xn=320, xs=32, N=2, S=10, C=32, G=4, gamma=P, beta=P, pt=2, eps=1e-5, act=2, Y=P, yn=320, ys=32, mean=None, rstd=None, dtype=0,
+             ws=P, n=1 << 20, stream=None)
+    a.update(k)
+    return B.load().dvdq_group_norm(*a.values())
+
+
+def backward(**k):
+    a = dict(dY=P, dn=320, ds=32, X=P, xn=320, xs=32, mean=P, rstd=P, N=2, S=10, C=32, G=4, gamma=P, beta=P, pt=2, act=2, dX=P, en=320, es=32,
+             dg=P, db=P, dtype=0, ws=P, n=1 << 20, stream=None)
+    a.update(k)
+    return B.load().dvdq_group_norm_backward(*a.values())
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(N=-1), B.ERR_SHAPE), (dict(N=65536), B.ERR_SHAPE), (dict(S=-1), B.ERR_SHAPE), (dict(C=0), B.ERR_SHAPE), (dict(G=0), B.ERR_SHAPE),
+    (dict(G=5), B.ERR_SHAPE), (dict(eps=-1.0), B.ERR_SHAPE), (dict(eps=float("nan")), B.ERR_SHAPE), (dict(act=3), B.ERR_UNSUPPORTED),
+    (dict(dtype=3), B.ERR_UNSUPPORTED), (dict(pt=1), B.ERR_UNSUPPORTED), (dict(dtype=2, pt=0), B.ERR_UNSUPPORTED), (dict(X=None), B.ERR_NULL),
+    (dict(Y=None), B.ERR_NULL), (dict(ws=None), B.ERR_NULL), (dict(n=10), B.ERR_WORKSPACE), (dict(ws=P + 8), B.ERR_ALIGN),
+    (dict(X=P + 1), B.ERR_ALIGN), (dict(gamma=P + 2), B.ERR_ALIGN), (dict(mean=P + 2), B.ERR_ALIGN), (dict(ys=31), B.ERR_SHAPE),
+    (dict(xs=-32), B.ERR_SHAPE), (dict(yn=0), B.ERR_SHAPE), (dict(N=0), B.OK), (dict(S=0), B.OK)])
+def test_forward_refuses(change, status):
+    assert forward(**change) == status
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(G=3), B.ERR_SHAPE), (dict(act=-1), B.ERR_UNSUPPORTED), (dict(dY=None), B.ERR_NULL), (dict(X=None), B.ERR_NULL),
+    (dict(mean=None), B.ERR_NULL), (dict(rstd=None), B.ERR_NULL), (dict(ws=None), B.ERR_NULL), (dict(n=10), B.ERR_WORKSPACE),
+    (dict(es=16), B.ERR_SHAPE), (dict(dX=P + 1), B.ERR_ALIGN), (dict(dg=P + 2), B.ERR_ALIGN), (dict(N=0, dg=None, db=None), B.OK)])
+def test_backward_refuses(change, status):
+    assert backward(**change) == status
+
+
+def test_workspace_sizes():
+    assert B.dvdq_group_norm_workspace_bytes(0, 10, 8, 2) == 0 and B.dvdq_group_norm_workspace_bytes(1, 10, 8, 3) == 0
+    assert B.dvdq_group_norm_workspace_bytes(1, 10, 8, 2) > 0
+    assert B.dvdq_group_norm_workspace_bytes(1, 499200, 128, 32) < 8 << 20
