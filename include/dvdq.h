@@ -406,7 +406,7 @@ dvdq_status dvdq_rope(const dvdq_rope_tensor* q /* host */, const dvdq_rope_tens
  * rstd = 1 / sqrt(variance + eps);  y = act(gamma_c h + beta_c).
  *   gamma, beta [C] or NULL (1 and 0), of type param_dtype: X's, or DVDQ_F32
  *   mean_out, rstd_out [N, G] fp32 or NULL: what the backward pass reads
- * Y may be X itself (same pitches).  N <= 65535, C <= 2^20.  S == 0: statistics (0, 1 / sqrt(eps)). */
+ * Y may be X itself (same pitches).  N <= 65535, S < 2^31, C <= 2^20.  S == 0: statistics (0, 1 / sqrt(eps)). */
 size_t dvdq_group_norm_workspace_bytes(int64_t N, int64_t S, int64_t C, int64_t G);
 dvdq_status dvdq_group_norm(const void* X, int64_t x_sample, int64_t x_place, int64_t N, int64_t S, int64_t C, int64_t G,
                             const void* gamma, const void* beta, int32_t param_dtype, float eps, int32_t act,

@@ -103,6 +103,96 @@ __device__ __forceinline__ float act_value_rt(int act, float z) {
     return act == DVDQ_ACT_GELU_TANH ? act_value<DVDQ_ACT_GELU_TANH>(z) : act == DVDQ_ACT_SILU ? act_value<DVDQ_ACT_SILU>(z) : z;
 }
 
+// ------------------------------------------------------------------ the same on pairs of channels
+//
+// sm_100 issues add, multiply and fma on two fp32 values at a time; the streaming kernels are bound by
+// issue slots long before arithmetic, so they work on pairs.  One channel (V = 1) rides with a zero beside it.
+template <int V>
+struct Pairs {
+    static constexpr int N = (V + 1) / 2;
+    uint64_t p[N];
+    __device__ __forceinline__ float get(int i) const {
+        float a, b;
+        f2_unpack(p[i >> 1], a, b);
+        return i & 1 ? b : a;
+    }
+    __device__ __forceinline__ void set(const float (&f)[V]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = f2_pack(f[2 * i], 2 * i + 1 < V ? f[2 * i + 1] : 0.f);
+    }
+};
+template <typename T, int V>
+__device__ __forceinline__ Pairs<V> widen2(const Vec<T, V>& v) {
+    Pairs<V> r;
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 f = unpack2<T>(reinterpret_cast<const uint32_t*>(&v)[i]);
+            r.p[i] = f2_pack(f.x, f.y);
+        }
+    } else {
+        float f[V];
+        widen(v, f);
+        r.set(f);
+    }
+    return r;
+}
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> narrow2(const Pairs<V>& r) {
+    Vec<T, V> v;
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            float a, b;
+            f2_unpack(r.p[i], a, b);
+            reinterpret_cast<uint32_t*>(&v)[i] = pack2<T>(a, b);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v.e[i] = from_f32<T>(r.get(i));
+    }
+    return v;
+}
+__device__ __forceinline__ uint64_t f2_splat(float v) { return f2_pack(v, v); }
+// logistic(u) of a pair, given -log2(e) u
+__device__ __forceinline__ uint64_t logistic2_scaled(uint64_t e) {
+    float a, b;
+    f2_unpack(e, a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    f2_unpack(f2_add(f2_pack(a, b), f2_splat(1.0f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return f2_pack(a, b);
+}
+constexpr float kMinusLog2e = -1.4426950408889634f;
+template <int ACT>
+__device__ __forceinline__ uint64_t act_value2(uint64_t z) {
+    if (ACT == DVDQ_ACT_NONE) return z;
+    const uint64_t e = ACT == DVDQ_ACT_SILU ? f2_mul(z, f2_splat(kMinusLog2e))
+                                            : f2_mul(z, f2_fma(f2_splat(kGeluB * kMinusLog2e), f2_mul(z, z), f2_splat(kGeluA * kMinusLog2e)));
+    return f2_mul(z, logistic2_scaled(e));
+}
+// act_slope of a pair.  SiLU needs no bound on z: f (1 + z (1 - f)) has no power of z to overflow.
+template <int ACT>
+__device__ __forceinline__ uint64_t act_slope2(uint64_t z) {
+    if (ACT == DVDQ_ACT_SILU) {
+        const uint64_t f = logistic2_scaled(f2_mul(z, f2_splat(kMinusLog2e)));
+        return f2_fma(f, f2_sub(z, f2_mul(z, f)), f);
+    }
+    if (ACT == DVDQ_ACT_GELU_TANH) {
+        float a, b;
+        f2_unpack(z, a, b);  // NaN stays NaN
+        asm("{\n\tmax.NaN.f32 %0, %0, 0fC1A00000;\n\tmin.NaN.f32 %0, %0, 0f41A00000;\n\t}" : "+f"(a));
+        asm("{\n\tmax.NaN.f32 %0, %0, 0fC1A00000;\n\tmin.NaN.f32 %0, %0, 0f41A00000;\n\t}" : "+f"(b));
+        const uint64_t c = f2_pack(a, b), s = f2_mul(c, c);
+        const uint64_t f = logistic2_scaled(f2_mul(c, f2_fma(f2_splat(kGeluB * kMinusLog2e), s, f2_splat(kGeluA * kMinusLog2e))));
+        const uint64_t w = f2_mul(f2_mul(c, f2_fma(f2_splat(3.0f * kGeluB), s, f2_splat(kGeluA))), f);  // c u'(c) f
+        return f2_add(f, f2_sub(w, f2_mul(w, f)));
+    }
+    return f2_splat(1.0f);
+}
+
 // ------------------------------------------------------------------ dependent launches
 
 // A kernel launched with launch_after may start while its predecessor on the stream drains; it

@@ -283,7 +283,7 @@ dvdq_status dvdq_rope(const dvdq_rope_tensor* q, const dvdq_rope_tensor* k, int6
 // ---- group norm ---------------------------------------------------------------------------------
 
 static bool group_norm_sizes_ok(int64_t N, int64_t S, int64_t C, int64_t G) {
-    return N >= 0 && N <= 65535 && S >= 0 && S <= ((int64_t)1 << 40) && C > 0 && C <= (1 << 20) && G > 0 && C % G == 0 && G <= 65535 / gn_pieces(C / G);
+    return N >= 0 && N <= 65535 && S >= 0 && S <= 0x7FFFFFFFll && C > 0 && C <= (1 << 20) && G > 0 && C % G == 0 && G <= 65535 / gn_pieces(C / G);
 }
 
 size_t dvdq_group_norm_workspace_bytes(int64_t N, int64_t S, int64_t C, int64_t G) {
@@ -319,6 +319,7 @@ static dvdq_status group_norm_run(const GnArgs& A0, int64_t N, int64_t S, int32_
     A.params_bf16 = param_dtype == DVDQ_BF16;
     A.part = static_cast<float2*>(workspace);
     A.pivot = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + room.pivot_off);
+    A.stat = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + room.stat_off);
     A.part_c = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + room.part_c_off);
     const cudaError_t e = dtype == DVDQ_BF16  ? launch_gn_t<__nv_bfloat16>(A, backward, act, st)
                           : dtype == DVDQ_F16 ? launch_gn_t<__half>(A, backward, act, st)

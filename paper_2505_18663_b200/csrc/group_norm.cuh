@@ -8,12 +8,15 @@
 // before its first output, so a tensor larger than the chip's shared memory is read twice; the
 // second pass walks every chunk backwards, so that it begins with what the L2 cache still holds.
 //
-// Two launches.  Pass 1: a CTA sums one chunk of places of one sample over all channels (a thread keeps
-// its 16 bytes of channels, so its loads are whole sectors) and writes two numbers per group.
-// Pass 2: every CTA adds up its sample's chunks in a fixed order (no atomics: the same bits every
-// time), then streams its chunk.  It is launched while pass 1 drains.  Sums are of x minus a value
-// of the group itself (the first place's first channel), so that a mean far from zero costs no
-// digits, in fp32 within a chunk and in fp64 across chunks.
+// Large tensors, three launches.  Pass 1: a CTA sums one chunk of places of one sample over all channels (a
+// thread keeps its 16 bytes of channels, so its loads are whole sectors) and writes two numbers per
+// group.  Join: a warp per group adds up its chunks in a fixed order (no atomics: the same bits every
+// time); backward, the channels' sums over samples and chunks as well.  Pass 2 streams the chunks.
+// Join and pass 2 are launched while their predecessor drains.  Sums are of x minus a value of the
+// group itself (the first place's first channel), so that a mean far from zero costs no digits, in
+// fp32 within a chunk and in fp64 across chunks.
+// Small tensors, one launch: where a slice of whole groups of one sample fits a CTA's shared memory,
+// the CTA reads it once, and does both passes on it.
 #pragma once
 
 #include "block_common.cuh"
@@ -36,6 +39,7 @@ struct GnArgs {
     float2* part;            // [N, chunks, G]
     float* pivot;            // [N, G]: what pass 1 subtracted (y may be x: pass 2 cannot read it there)
     float2* part_c;          // backward: [N, chunks, C]
+    float2* stat;            // [N, G]: (mean, rstd) forward, (<dh>, <dh h>) backward
     int64_t xn, xs, dn, ds, yn, ys;  // pitches of samples and places, elements
     int64_t S;
     int N, C, G, per;        // per = C / G
@@ -84,16 +88,21 @@ struct GnPlace {
         s0 = (int64_t)blockIdx.x * A.rows;
         s1 = s0 + A.rows < A.S ? s0 + A.rows : A.S;
     }
+    // this thread's places: s0 + r, s0 + r + lanes, ...
+    __device__ __forceinline__ int count(int lanes) const {
+        const int64_t k = s1 - s0 - r;
+        return k > 0 ? (int)((k + lanes - 1) / lanes) : 0;
+    }
 };
 
 // Adds up [lanes][vecs * V] pairs in shared memory over the lanes, then over the channels of each group
 // in this block, and writes one pair per group (and per channel).
 template <int V, bool PER_CHANNEL>
-__device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V>& P, const float (&s1)[V], const float (&s2)[V], float2* sh) {
+__device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
     const int width = A.vecs * V;
     if (P.on) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) sh[P.r * width + P.v * V + i] = make_float2(s1[i], s2[i]);
+        for (int i = 0; i < V; ++i) sh[P.r * width + P.v * V + i] = make_float2(s1.get(i), s2.get(i));
     }
     __syncthreads();
     const int64_t slot = (int64_t)blockIdx.y * A.chunks + blockIdx.x;
@@ -141,14 +150,90 @@ __device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V
     }
 }
 
+template <typename T, int V> struct GnRing { static constexpr bool value = sizeof(T) * V == 16; };
+
+// A thread's own stream of 16-byte pieces, `count` of them from STREAMS tensors side by side, through a ring
+// of D slots of its own in shared memory (cp.async): D - 1 pieces per tensor are in flight while one is
+// worked on, without a register each, and no barrier is needed.  With whole batches of register loads
+// a warp waits for its slowest load with nothing in flight: 3.8 instead of 5 TB/s.
+// A slot is refilled only when what was read from it has been delivered: the copy's address
+// depends on the words read (ANDed with a zero that the compiler does not know).
+template <int D, int STREAMS, typename T, int V, typename Use>
+__device__ __forceinline__ void gn_stream(uint32_t ring, int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
+    constexpr uint32_t kSlot = kGnThreads * 16;
+    static_assert(sizeof(Vec<T, V>) == 16, "16-byte pieces");
+    uint32_t zero;
+    asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
+    zero -= 1u;
+    auto fill = [&](uint32_t slot, int k, uint32_t dep) {
+        if (k < count) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * STREAMS * kSlot + dep), "l"(from0) : "memory");
+            from0 += step0;
+            if constexpr (STREAMS == 2) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (slot * STREAMS + 1) * kSlot + dep), "l"(from1) : "memory");
+                from1 += step1;
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int k = 0; k < D - 1; ++k) fill((uint32_t)k, k, 0u);
+    uint32_t slot = 0, behind = D - 1, dep = 0u;  // `behind`: the slot that was read last (at first: the one not yet filled)
+    for (int k = 0; k < count; ++k) {
+        fill(behind, k + D - 1, dep);
+        asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory");
+        union { uint4 w; Vec<T, V> v; } in[STREAMS];
+        dep = 0u;
+#pragma unroll
+        for (int j = 0; j < STREAMS; ++j) {
+            in[j].w = lds128(ring + (slot * STREAMS + j) * kSlot);
+            dep ^= in[j].w.w;
+        }
+        dep &= zero;
+        if constexpr (STREAMS == 1) use(in[0].v);
+        else use(in[0].v, in[1].v);
+        behind = slot;
+        slot = slot + 1 == D ? 0u : slot + 1;
+    }
+}
+// The same sequence with plain loads, for accesses narrower than 16 bytes.
+template <int STREAMS, typename T, int V, typename Use>
+__device__ __forceinline__ void gn_plain_stream(int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
+#pragma unroll 4
+    for (int k = 0; k < count; ++k) {
+        const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(from0);
+        from0 += step0;
+        if constexpr (STREAMS == 1) {
+            use(a);
+        } else {
+            const Vec<T, V> b = *reinterpret_cast<const Vec<T, V>*>(from1);
+            from1 += step1;
+            use(a, b);
+        }
+    }
+}
+template <int D, int STREAMS, typename T, int V, typename Use>
+__device__ __forceinline__ void gn_walk(const uint8_t* raw, int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
+    if constexpr (GnRing<T, V>::value)
+        gn_stream<D, STREAMS, T, V>(smem_u32(raw) + threadIdx.x * 16, count, from0, step0, from1, step1, use);
+    else
+        gn_plain_stream<STREAMS, T, V>(count, from0, step0, from1, step1, use);
+}
 template <typename T, int V>
-__global__ void __launch_bounds__(kGnThreads) gn_stats_kernel(const __grid_constant__ GnArgs A) {
-    extern __shared__ float2 sh[];
+__device__ __forceinline__ void store_streaming(T* p, const Vec<T, V>& v) {  // written once, not read here again: first out of L2
+    if constexpr (sizeof(Vec<T, V>) == 16) __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
+    else *reinterpret_cast<Vec<T, V>*>(p) = v;
+}
+constexpr int kGnDepth = 8, kGnGradDepth = 5;  // slots: 32 KB a CTA, 40 KB for two tensors; four CTAs per SM
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_constant__ GnArgs A) {
+    extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
-    float s1[V], s2[V];
+    Pairs<V> s1, s2;
 #pragma unroll
-    for (int i = 0; i < V; ++i) s1[i] = s2[i] = 0.f;
+    for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
     if (P.on) {
         const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
         float pv[V];
@@ -158,137 +243,174 @@ __global__ void __launch_bounds__(kGnThreads) gn_stats_kernel(const __grid_const
             pv[i] = to_f32(base[g * A.per]);
             if (blockIdx.x == 0 && P.r == 0 && P.c0 + i == g * A.per) A.pivot[(int64_t)n * A.G + g] = pv[i];
         }
-        const T* p = base + P.c0;
-        constexpr int U = 4;
-        int64_t s = P.s0 + P.r;
-        for (; s + (U - 1) * A.lanes < P.s1; s += (int64_t)U * A.lanes) {
-            Vec<T, V> v[U];
+        Pairs<V> pivot;
+        pivot.set(pv);
+        gn_walk<kGnDepth, 1, T, V>(raw, P.count(A.lanes), base + P.c0 + (P.s0 + P.r) * A.xs, A.lanes * A.xs, nullptr, 0, [&](const Vec<T, V>& v) {
+            const Pairs<V> x = widen2<T, V>(v);
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec<T, V>*>(p + (s + (int64_t)u * A.lanes) * A.xs);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = to_f32(v[u].e[i]) - pv[i];
-                    s1[i] += d;
-                    s2[i] = fmaf(d, d, s2[i]);
-                }
-        }
-        for (; s < P.s1; s += A.lanes) {
-            const Vec<T, V> v = *reinterpret_cast<const Vec<T, V>*>(p + s * A.xs);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = to_f32(v.e[i]) - pv[i];
-                s1[i] += d;
-                s2[i] = fmaf(d, d, s2[i]);
+            for (int i = 0; i < Pairs<V>::N; ++i) {
+                const uint64_t d = f2_sub(x.p[i], pivot.p[i]);
+                s1.p[i] = f2_add(s1.p[i], d);
+                s2.p[i] = f2_fma(d, d, s2.p[i]);
             }
-        }
+        });
     }
-    gn_reduce_block<V, false>(A, P, s1, s2, sh);
+    __syncthreads();  // the ring's memory becomes the sums'
+    gn_reduce_block<V, false>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
     release_successor();
 }
 
-// The two numbers of each group of sample n, added over the chunks: a warp per group, fp64.
-// stat[g] = (mean, rstd) forward, (<dh>, <dh h>) backward.
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
 
+// mean and rstd from the group's mean and mean square about its pivot
+__device__ __forceinline__ float2 gn_mean_rstd(double pivot, double m1, double m2, float eps) {
+    const double var = m2 - m1 * m1;
+    return make_float2((float)(pivot + m1), (float)(1.0 / sqrt((var > 0.0 || var != var ? var : 0.0) + (double)eps)));
+}
+
+// Adds up the chunks: the first `group_ctas` CTAs a warp per group, the rest (backward) 32 channels each.
 template <bool BACKWARD>
-__device__ __forceinline__ void gn_group_stats(const GnArgs& A, int n, int g0, int g1, float2* stat) {
+__global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_constant__ GnArgs A, int group_ctas) {
+    constexpr int kWarps = kGnThreads / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const double count = (double)A.S * A.per;
-    for (int g = g0 + warp; g < g1; g += kGnThreads / 32) {
+    wait_predecessor();
+    if ((int)blockIdx.x < group_ctas) {
+        const int64_t ng = (int64_t)blockIdx.x * kWarps + warp;
+        if (ng >= (int64_t)A.N * A.G) return;
+        const int n = (int)(ng / A.G), g = (int)(ng - (int64_t)n * A.G);
+        const int entries = A.chunks * A.bpg, pitch = A.G * A.bpg;
+        const float2* base = A.part + (int64_t)n * A.chunks * pitch + (int64_t)g * A.bpg;
         double a = 0.0, b = 0.0;
-        // entry i of the group: chunk i / bpg, piece i % bpg
-        for (int i = lane; i < A.chunks * A.bpg; i += 32) {
-            const int c = A.bpg == 1 ? i : i / A.bpg;
-            const float2 t = A.part[((int64_t)n * A.chunks + c) * (A.G * A.bpg) + g * A.bpg + (i - c * A.bpg)];
+        auto entry = [&](int i) { return A.bpg == 1 ? base[(int64_t)i * pitch] : base[(int64_t)(i / A.bpg) * pitch + i % A.bpg]; };
+        int i = lane;
+        for (; i + 7 * 32 < entries; i += 8 * 32) {
+            float2 t[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) t[u] = entry(i + 32 * u);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) { a += t[u].x; b += t[u].y; }
+        }
+        for (; i < entries; i += 32) {
+            const float2 t = entry(i);
             a += t.x;
             b += t.y;
         }
+        const double count = (double)A.S * A.per;
         a = warp_sum(a) / count;
         b = warp_sum(b) / count;
         if (lane == 0) {
             if (BACKWARD) {
-                stat[g - g0] = make_float2((float)a, (float)b);
+                A.stat[ng] = make_float2((float)a, (float)b);
             } else {
-                const double pivot = (double)A.pivot[(int64_t)n * A.G + g];
-                const double var = b - a * a;
-                const float m = (float)(pivot + a), r = (float)(1.0 / sqrt((var > 0.0 || var != var ? var : 0.0) + (double)A.eps));
-                stat[g - g0] = make_float2(m, r);
-                if (A.mean && blockIdx.x == 0) A.mean[(int64_t)n * A.G + g] = m;
-                if (A.rstd && blockIdx.x == 0) A.rstd[(int64_t)n * A.G + g] = r;
+                const float2 t = gn_mean_rstd((double)A.pivot[ng], a, b, A.eps);
+                A.stat[ng] = t;
+                if (A.mean) A.mean[ng] = t.x;
+                if (A.rstd) A.rstd[ng] = t.y;
             }
+        }
+    } else if constexpr (BACKWARD) {
+        __shared__ double2 red[kWarps][32];
+        const int c = ((int)blockIdx.x - group_ctas) * 32 + lane;
+        double a = 0.0, b = 0.0;
+        if (c < A.C) {
+            const int64_t rows = (int64_t)A.N * A.chunks;
+            int64_t i = warp;
+            for (; i + 7 * kWarps < rows; i += 8 * kWarps) {
+                float2 t[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) t[u] = A.part_c[(i + u * kWarps) * A.C + c];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) { a += t[u].x; b += t[u].y; }
+            }
+            for (; i < rows; i += kWarps) {
+                const float2 t = A.part_c[i * A.C + c];
+                a += t.x;
+                b += t.y;
+            }
+        }
+        red[warp][lane] = make_double2(a, b);
+        __syncthreads();
+        if (warp == 0 && c < A.C) {
+            for (int w = 1; w < kWarps; ++w) {
+                a += red[w][lane].x;
+                b += red[w][lane].y;
+            }
+            if (A.dbeta) A.dbeta[c] = (float)a;
+            if (A.dgamma) A.dgamma[c] = (float)b;
         }
     }
 }
 
+// z = (x - mean) a + beta with a = gamma rstd.  For 16-bit x the mean goes into the constant (x a + (beta -
+// mean a): the constant's rounding, 2^-24 |mean| a, is far below x's own step); fp32 x subtracts first.
+template <typename T, int V>
+struct GnScale {
+    Pairs<V> mean, a, b;
+    __device__ __forceinline__ GnScale(const float (&mu)[V], const float (&sc)[V], const float (&sh)[V]) {
+        float t[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) t[i] = sizeof(T) == 2 ? fmaf(-mu[i], sc[i], sh[i]) : sh[i];
+        mean.set(mu);
+        a.set(sc);
+        b.set(t);
+    }
+    __device__ __forceinline__ uint64_t operator()(uint64_t x, int i) const {
+        return f2_fma(sizeof(T) == 2 ? x : f2_sub(x, mean.p[i]), a.p[i], b.p[i]);
+    }
+};
+
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads) gn_apply_kernel(const __grid_constant__ GnArgs A) {
-    extern __shared__ float2 sh[];
+__global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_constant__ GnArgs A) {
+    extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
-    float ga[V], be[V];
-    if (P.on) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            ga[i] = gn_param(A.gamma, A.params_f32, A.params_bf16, P.c0 + i, 1.0f);
-            be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, P.c0 + i, 0.0f);
-        }
-    }
     wait_predecessor();
-    gn_group_stats<false>(A, n, P.g0, P.g1, sh);
-    __syncthreads();
     if (!P.on) return;
-    float mu[V];
+    float mu[V], ga[V], be[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const float2 t = sh[(P.c0 + i) / A.per - P.g0];
+        const float2 t = A.stat[(int64_t)n * A.G + (P.c0 + i) / A.per];
         mu[i] = t.x;
-        ga[i] *= t.y;
+        ga[i] = t.y * gn_param(A.gamma, A.params_f32, A.params_bf16, P.c0 + i, 1.0f);
+        be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, P.c0 + i, 0.0f);
     }
-    const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0;
-    T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0;
-    constexpr int U = 4;
-    auto one = [&](const Vec<T, V>& v, int64_t s) {
-        float o[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = act_value<ACT>(fmaf(to_f32(v.e[i]) - mu[i], ga[i], be[i]));
-        *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow<T, V>(o);
-    };
+    const GnScale<T, V> scale(mu, ga, be);
     // backwards: from the place pass 1 read last
-    int64_t k = P.s1 - P.s0 - P.r;                      // places left for this thread: s0 + r, + lanes, ...
-    int64_t left = k > 0 ? (k + A.lanes - 1) / A.lanes : 0;
-    int64_t s = P.s0 + P.r + (left - 1) * A.lanes;
-    for (; left >= U; left -= U, s -= (int64_t)U * A.lanes) {
-        Vec<T, V> v[U];
+    const int count = P.count(A.lanes);
+    const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
+    T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0 + last * A.ys;
+    const int64_t back = -(int64_t)A.lanes * A.ys;
+    gn_walk<kGnDepth, 1, T, V>(raw, count, static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + last * A.xs, -(int64_t)A.lanes * A.xs, nullptr, 0,
+                               [&](const Vec<T, V>& v) {
+        const Pairs<V> x = widen2<T, V>(v);
+        Pairs<V> o;
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec<T, V>*>(p + (s - (int64_t)u * A.lanes) * A.xs);
-#pragma unroll
-        for (int u = 0; u < U; ++u) one(v[u], s - (int64_t)u * A.lanes);
-    }
-    for (; left > 0; --left, s -= A.lanes) one(*reinterpret_cast<const Vec<T, V>*>(p + s * A.xs), s);
+        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT>(scale(x.p[i], i));
+        store_streaming<T, V>(q, narrow2<T, V>(o));
+        q += back;
+    });
 }
 
 // ------------------------------------------------------------------ backward
 
-// dz and h of V channels at one place
-template <typename T, int V, int ACT>
-__device__ __forceinline__ void gn_dz(const Vec<T, V>& xv, const Vec<T, V>& dv, const float (&mu)[V], const float (&rs)[V],
-                                      const float (&ga)[V], const float (&be)[V], float (&dz)[V], float (&h)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        h[i] = (to_f32(xv.e[i]) - mu[i]) * rs[i];
-        dz[i] = to_f32(dv.e[i]);
-        if (ACT != DVDQ_ACT_NONE) dz[i] *= act_slope<ACT>(fmaf(ga[i], h[i], be[i]));
+// What the backward passes hold per channel: h = (x - mean) rstd, z = gamma h + beta.
+template <typename T, int V>
+struct GnGrad {
+    GnScale<T, V> h;
+    Pairs<V> gamma, beta;
+    template <int ACT>
+    __device__ __forceinline__ void dz(uint64_t x, uint64_t dy, int i, uint64_t& out_dz, uint64_t& out_h) const {
+        out_h = h(x, i);
+        out_dz = ACT == DVDQ_ACT_NONE ? dy : f2_mul(dy, act_slope2<ACT>(f2_fma(gamma.p[i], out_h, beta.p[i])));
     }
-}
-
-template <typename T, int V, int ACT>
-__device__ __forceinline__ void gn_constants(const GnArgs& A, int n, int c0, float (&mu)[V], float (&rs)[V], float (&ga)[V], float (&be)[V]) {
+};
+template <typename T, int V>
+__device__ __forceinline__ GnGrad<T, V> gn_constants(const GnArgs& A, int n, int c0, float (&rs)[V], float (&ga)[V]) {
+    float mu[V], be[V], none[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int64_t g = (int64_t)n * A.G + (c0 + i) / A.per;
@@ -296,121 +418,290 @@ __device__ __forceinline__ void gn_constants(const GnArgs& A, int n, int c0, flo
         rs[i] = A.rstd[g];
         ga[i] = gn_param(A.gamma, A.params_f32, A.params_bf16, c0 + i, 1.0f);
         be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, c0 + i, 0.0f);
+        none[i] = 0.f;
     }
+    GnGrad<T, V> r{GnScale<T, V>(mu, rs, none), {}, {}};
+    r.gamma.set(ga);
+    r.beta.set(be);
+    return r;
 }
 
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads) gn_grad_stats_kernel(const __grid_constant__ GnArgs A) {
-    extern __shared__ float2 sh[];
+__global__ void __launch_bounds__(kGnThreads, 4) gn_grad_stats_kernel(const __grid_constant__ GnArgs A) {
+    extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
-    float s1[V], s2[V];
+    Pairs<V> s1, s2;
 #pragma unroll
-    for (int i = 0; i < V; ++i) s1[i] = s2[i] = 0.f;
+    for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
     if (P.on) {
-        float mu[V], rs[V], ga[V], be[V];
-        gn_constants<T, V, ACT>(A, n, P.c0, mu, rs, ga, be);
-        const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0;
-        const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0;
-        auto one = [&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
-            float dz[V], h[V];
-            gn_dz<T, V, ACT>(xv, dv, mu, rs, ga, be, dz, h);
+        float rs[V], ga[V];
+        const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
+        const int64_t s0 = P.s0 + P.r;
+        gn_walk<kGnGradDepth, 2, T, V>(raw, P.count(A.lanes), static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + s0 * A.xs, A.lanes * A.xs,
+                                       static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0 + s0 * A.ds, A.lanes * A.ds,
+                                       [&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
+            const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                s1[i] += dz[i];
-                s2[i] = fmaf(dz[i], h[i], s2[i]);
+            for (int i = 0; i < Pairs<V>::N; ++i) {
+                uint64_t dz, h;
+                K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+                s1.p[i] = f2_add(s1.p[i], dz);
+                s2.p[i] = f2_fma(dz, h, s2.p[i]);
             }
-        };
-        constexpr int U = 2;
-        int64_t s = P.s0 + P.r;
-        for (; s + (U - 1) * A.lanes < P.s1; s += (int64_t)U * A.lanes) {
-            Vec<T, V> xv[U], dv[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                xv[u] = *reinterpret_cast<const Vec<T, V>*>(p + (s + (int64_t)u * A.lanes) * A.xs);
-                dv[u] = *reinterpret_cast<const Vec<T, V>*>(d + (s + (int64_t)u * A.lanes) * A.ds);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) one(xv[u], dv[u]);
-        }
-        for (; s < P.s1; s += A.lanes)
-            one(*reinterpret_cast<const Vec<T, V>*>(p + s * A.xs), *reinterpret_cast<const Vec<T, V>*>(d + s * A.ds));
+        });
     }
-    gn_reduce_block<V, true>(A, P, s1, s2, sh);
+    __syncthreads();  // the ring's memory becomes the sums'
+    gn_reduce_block<V, true>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
     release_successor();
 }
 
-template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads) gn_grad_apply_kernel(const __grid_constant__ GnArgs A) {
-    extern __shared__ float2 sh[];
-    const GnPlace<V> P(A);
-    const int n = blockIdx.y;
-    float mu[V], rs[V], ga[V], be[V];
-    if (P.on) gn_constants<T, V, ACT>(A, n, P.c0, mu, rs, ga, be);
-    wait_predecessor();
-    gn_group_stats<true>(A, n, P.g0, P.g1, sh);
-    __syncthreads();
-    if (P.on && A.y) {
-        float m1[V], m2[V];
+// dx = rstd (gamma dz - m1 - h m2) = dz (rstd gamma) + (h (-rstd m2) + (-rstd m1))
+template <int V>
+struct GnDx {
+    Pairs<V> c1, c2, c3;
+    __device__ __forceinline__ GnDx(const float (&rs)[V], const float (&ga)[V], const float (&m1)[V], const float (&m2)[V]) {
+        float a[V], b[V], c[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float2 t = sh[(P.c0 + i) / A.per - P.g0];
-            m1[i] = t.x;
-            m2[i] = t.y;
+            a[i] = rs[i] * ga[i];
+            b[i] = -rs[i] * m2[i];
+            c[i] = -rs[i] * m1[i];
         }
-        const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0;
-        const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0;
-        T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0;
-        auto one = [&](const Vec<T, V>& xv, const Vec<T, V>& dv, int64_t s) {
-            float dz[V], h[V], o[V];
-            gn_dz<T, V, ACT>(xv, dv, mu, rs, ga, be, dz, h);
-#pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = rs[i] * (fmaf(dz[i], ga[i], -m1[i]) - h[i] * m2[i]);
-            *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow<T, V>(o);
-        };
-        constexpr int U = 2;
-        int64_t k = P.s1 - P.s0 - P.r;
-        int64_t left = k > 0 ? (k + A.lanes - 1) / A.lanes : 0;
-        int64_t s = P.s0 + P.r + (left - 1) * A.lanes;
-        for (; left >= U; left -= U, s -= (int64_t)U * A.lanes) {
-            Vec<T, V> xv[U], dv[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                xv[u] = *reinterpret_cast<const Vec<T, V>*>(p + (s - (int64_t)u * A.lanes) * A.xs);
-                dv[u] = *reinterpret_cast<const Vec<T, V>*>(d + (s - (int64_t)u * A.lanes) * A.ds);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) one(xv[u], dv[u], s - (int64_t)u * A.lanes);
-        }
-        for (; left > 0; --left, s -= A.lanes)
-            one(*reinterpret_cast<const Vec<T, V>*>(p + s * A.xs), *reinterpret_cast<const Vec<T, V>*>(d + s * A.ds), s);
+        c1.set(a);
+        c2.set(b);
+        c3.set(c);
     }
-    // the parameters' gradients: the first CTAs take 32 channels each, 8 rows of chunks side by side, fp64
-    if (!A.dgamma && !A.dbeta) return;
-    const int ctas = gridDim.x * gridDim.y * gridDim.z;
-    const int cta = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    __shared__ double2 red[kGnThreads / 32][32];
-    for (int cb = cta; cb < (A.C + 31) / 32; cb += ctas) {
-        const int c = cb * 32 + lane;
-        double a = 0.0, b = 0.0;
-        if (c < A.C)
-            for (int64_t i = warp; i < (int64_t)A.N * A.chunks; i += kGnThreads / 32) {
-                const float2 t = A.part_c[i * A.C + c];
-                a += t.x;
-                b += t.y;
-            }
-        __syncthreads();
-        red[warp][lane] = make_double2(a, b);
-        __syncthreads();
-        if (warp == 0 && c < A.C) {
-            for (int w = 1; w < kGnThreads / 32; ++w) {
-                a += red[w][lane].x;
-                b += red[w][lane].y;
-            }
-            if (A.dbeta) A.dbeta[c] = (float)a;
-            if (A.dgamma) A.dgamma[c] = (float)b;
+    __device__ __forceinline__ uint64_t operator()(uint64_t dz, uint64_t h, int i) const { return f2_fma(dz, c1.p[i], f2_fma(h, c2.p[i], c3.p[i])); }
+};
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __grid_constant__ GnArgs A) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    const GnPlace<V> P(A);
+    const int n = blockIdx.y;
+    wait_predecessor();
+    if (!P.on) return;
+    float rs[V], ga[V], m1[V], m2[V];
+    const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float2 t = A.stat[(int64_t)n * A.G + (P.c0 + i) / A.per];
+        m1[i] = t.x;
+        m2[i] = t.y;
+    }
+    const GnDx<V> dx(rs, ga, m1, m2);
+    const int count = P.count(A.lanes);
+    const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
+    T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0 + last * A.ys;
+    const int64_t back = -(int64_t)A.lanes * A.ys;
+    gn_walk<kGnGradDepth, 2, T, V>(raw, count, static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + last * A.xs, -(int64_t)A.lanes * A.xs,
+                                   static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0 + last * A.ds, -(int64_t)A.lanes * A.ds,
+                                   [&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
+        const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
+        Pairs<V> o;
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            uint64_t dz, h;
+            K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+            o.p[i] = dx(dz, h, i);
         }
+        store_streaming<T, V>(q, narrow2<T, V>(o));
+        q += back;
+    });
+}
+
+// ------------------------------------------------------------------ small tensors: one launch
+
+// Sums of one float per (lane, channel) over the lanes and the channels of each group: out[g].
+__device__ __forceinline__ void gn_small_groups(const float* red, int lanes, int width, int per, int groups, float scale, float* out) {
+    __syncthreads();
+    for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
+        float t = 0.f;
+        for (int i = threadIdx.x & 31; i < lanes * per; i += 32) {
+            const int l = i / per;
+            t += red[l * width + g * per + (i - l * per)];
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+        if ((threadIdx.x & 31) == 0) out[g] = t * scale;
+    }
+    __syncthreads();
+}
+
+// A CTA: `vecs` vectors of whole groups, all places of sample blockIdx.y.  Every thread keeps to the places it
+// loaded itself, so only the sums go through barriers.  Mean first, then squares about it.
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_constant__ GnArgs A) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    const int width = A.vecs * V, v = threadIdx.x % A.vecs, r = threadIdx.x / A.vecs, n = blockIdx.y;
+    const int cbase = blockIdx.x * width, here = min(A.C - cbase, width), groups = here / A.per, c0 = cbase + v * V;
+    const bool on = r < A.lanes && v * V < here;
+    const int S = (int)A.S;
+    Vec<T, V>* data = reinterpret_cast<Vec<T, V>*>(raw);
+    float* red = reinterpret_cast<float*>(raw + align_up((int64_t)S * width * sizeof(T), 16));
+    float *mean = red + A.lanes * width, *rstd = mean + width;
+    const float inv = 1.0f / ((float)S * A.per);
+    const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
+    float s1[V], pv[V];
+    wait_predecessor();
+    if (on) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            pv[i] = to_f32(base[(c0 + i) / A.per * A.per]);
+            s1[i] = 0.f;
+        }
+#pragma unroll 4
+        for (int s = r; s < S; s += A.lanes) {
+            const Vec<T, V> x = *reinterpret_cast<const Vec<T, V>*>(base + s * A.xs + c0);
+            data[s * A.vecs + v] = x;
+#pragma unroll
+            for (int i = 0; i < V; ++i) s1[i] += to_f32(x.e[i]) - pv[i];
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[r * width + v * V + i] = s1[i];
+    }
+    gn_small_groups(red, A.lanes, width, A.per, groups, inv, mean);  // about the pivot
+    float mu[V];
+    if (on) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            mu[i] = pv[i] + mean[(c0 + i) / A.per - cbase / A.per];
+            s1[i] = 0.f;
+        }
+        for (int s = r; s < S; s += A.lanes) {
+            const Vec<T, V> x = data[s * A.vecs + v];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = to_f32(x.e[i]) - mu[i];
+                s1[i] = fmaf(d, d, s1[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[r * width + v * V + i] = s1[i];
+    }
+    gn_small_groups(red, A.lanes, width, A.per, groups, inv, rstd);
+    if (!on) return;
+    float ga[V], be[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int c = c0 + i, g = c / A.per;
+        const float rs = 1.0f / sqrtf(rstd[g - cbase / A.per] + A.eps);
+        ga[i] = rs * gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
+        be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, c, 0.0f);
+        if (r == 0 && c == g * A.per) {
+            if (A.mean) A.mean[(int64_t)n * A.G + g] = mu[i];
+            if (A.rstd) A.rstd[(int64_t)n * A.G + g] = rs;
+        }
+    }
+    T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + c0;
+    for (int s = r; s < S; s += A.lanes) {
+        const Vec<T, V> x = data[s * A.vecs + v];
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = act_value<ACT>(fmaf(to_f32(x.e[i]) - mu[i], ga[i], be[i]));
+        *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow<T, V>(o);
+    }
+}
+
+// Its gradients: the CTA takes its channels of every sample in turn, so that the parameters' gradients
+// need no second kernel.
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_constant__ GnArgs A) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    const int width = A.vecs * V, v = threadIdx.x % A.vecs, r = threadIdx.x / A.vecs;
+    const int cbase = blockIdx.x * width, here = min(A.C - cbase, width), groups = here / A.per, c0 = cbase + v * V;
+    const bool on = r < A.lanes && v * V < here;
+    const int S = (int)A.S;
+    const int64_t slice = align_up((int64_t)S * width * sizeof(T), 16);
+    Vec<T, V>* xd = reinterpret_cast<Vec<T, V>*>(raw);
+    Vec<T, V>* dd = reinterpret_cast<Vec<T, V>*>(raw + slice);
+    float2* red = reinterpret_cast<float2*>(raw + 2 * slice);
+    float2* sums = red + A.lanes * width;   // per channel
+    float2* gsum = sums + width;            // per group
+    double dgamma = 0.0, dbeta = 0.0;       // of channel cbase + threadIdx.x
+    const float inv = 1.0f / ((float)S * A.per);
+    wait_predecessor();
+    for (int n = 0; n < A.N; ++n) {
+        float rs[V], ga[V];
+        const GnGrad<T, V> K = gn_constants<T, V>(A, n, on ? c0 : cbase, rs, ga);
+        if (on) {
+            Pairs<V> s1, s2;
+            const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + c0;
+            const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + c0;
+#pragma unroll
+            for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
+#pragma unroll 2
+            for (int s = r; s < S; s += A.lanes) {
+                const Vec<T, V> xv = *reinterpret_cast<const Vec<T, V>*>(p + s * A.xs), dv = *reinterpret_cast<const Vec<T, V>*>(d + s * A.ds);
+                xd[s * A.vecs + v] = xv;
+                dd[s * A.vecs + v] = dv;
+                const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
+#pragma unroll
+                for (int i = 0; i < Pairs<V>::N; ++i) {
+                    uint64_t dz, h;
+                    K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+                    s1.p[i] = f2_add(s1.p[i], dz);
+                    s2.p[i] = f2_fma(dz, h, s2.p[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) red[r * width + v * V + i] = make_float2(s1.get(i), s2.get(i));
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < here; c += kGnThreads) {
+            float2 t = red[c];
+            for (int l = 1; l < A.lanes; ++l) {
+                t.x += red[l * width + c].x;
+                t.y += red[l * width + c].y;
+            }
+            // the host keeps a CTA's channels within its threads: one channel per thread
+            dbeta += t.x;
+            dgamma += t.y;
+            const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, cbase + c, 1.0f);
+            sums[c] = make_float2(t.x * g, t.y * g);
+        }
+        __syncthreads();
+        for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
+            float2 t = make_float2(0.f, 0.f);
+            for (int i = threadIdx.x & 31; i < A.per; i += 32) {
+                t.x += sums[g * A.per + i].x;
+                t.y += sums[g * A.per + i].y;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
+                t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
+            }
+            if ((threadIdx.x & 31) == 0) gsum[g] = make_float2(t.x * inv, t.y * inv);
+        }
+        __syncthreads();
+        if (on && A.y) {
+            T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + c0;
+            float m1[V], m2[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float2 t = gsum[(c0 + i) / A.per - cbase / A.per];
+                m1[i] = t.x;
+                m2[i] = t.y;
+            }
+            const GnDx<V> dx(rs, ga, m1, m2);
+            for (int s = r; s < S; s += A.lanes) {
+                const Pairs<V> x = widen2<T, V>(xd[s * A.vecs + v]), dy = widen2<T, V>(dd[s * A.vecs + v]);
+                Pairs<V> o;
+#pragma unroll
+                for (int i = 0; i < Pairs<V>::N; ++i) {
+                    uint64_t dz, h;
+                    K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+                    o.p[i] = dx(dz, h, i);
+                }
+                *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow2<T, V>(o);
+            }
+        }
+    }
+    if ((int)threadIdx.x < here) {
+        if (A.dbeta) A.dbeta[cbase + threadIdx.x] = (float)dbeta;
+        if (A.dgamma) A.dgamma[cbase + threadIdx.x] = (float)dgamma;
     }
 }
 
@@ -450,13 +741,14 @@ inline GnPlan gn_plan(int64_t N, int64_t S) {
 // Pieces that a group wider than a CTA's vectors is cut into, at most (single-element accesses).
 inline int64_t gn_pieces(int64_t per) { return ceil_div(per, kGnMaxVecs); }
 struct GnRoom {
-    int64_t pivot_off, part_c_off, total;
+    int64_t pivot_off, stat_off, part_c_off, total;
 };
 inline GnRoom gn_room(int64_t N, int64_t S, int64_t C, int64_t G) {
     const GnPlan p = gn_plan(N, S);
     GnRoom r;
     r.pivot_off = align_up(N * p.chunks * G * gn_pieces(C / G) * 8, 256);
-    r.part_c_off = r.pivot_off + align_up(N * G * 4, 256);
+    r.stat_off = r.pivot_off + align_up(N * G * 4, 256);
+    r.part_c_off = r.stat_off + align_up(N * G * 8, 256);
     r.total = r.part_c_off + N * p.chunks * C * 8;
     return r;
 }
@@ -485,27 +777,77 @@ inline bool gn_cut(GnArgs& A, int V) {
     return true;
 }
 
+// The one-launch kernels: the fewest whole groups that fill 64 bytes of a place (or all channels, if
+// those are fewer), so that a warp's loads are whole sectors; used where their places fit kGnSmallSmem, which
+// leaves room for three CTAs per SM.  A tensor of more than kGnSmallBytes is left to the three launches,
+// whose loads are whole rows.
+constexpr int64_t kGnSmallSmem = 64 << 10, kGnSmallBytes = 8 << 20;
 template <typename T, int V>
-static cudaError_t launch_gn_v(GnArgs A, bool backward, int act, cudaStream_t st) {
+static bool gn_small_cut(GnArgs& A, bool backward, size_t* smem) {
+    if (A.C % V != 0) return false;
+    int64_t width = A.per;
+    while (width % V != 0 || (width * (int64_t)sizeof(T) < 64 && width < A.C)) width += A.per;
+    if (width > A.C) width = A.C;
+    if (width % V != 0 || width > kGnThreads) return false;  // a channel per thread in the last sums
+    const int64_t bytes = A.S * width * (int64_t)sizeof(T);
+    if (bytes * (backward ? 2 : 1) > kGnSmallSmem || (int64_t)A.N * A.S * A.C * (int64_t)sizeof(T) > kGnSmallBytes) return false;
+    if (backward && A.N > 8) return false;                    // samples in turn
+    A.vecs = (int)(width / V);
+    A.lanes = kGnThreads / A.vecs;
+    if (A.lanes > A.S) A.lanes = (int)A.S;
+    A.blocks = (int)ceil_div(A.C, width);
+    const int64_t slice = align_up(bytes, 16), red = (int64_t)A.lanes * width;
+    *smem = (size_t)(backward ? 2 * slice + (red + 2 * width) * 8 : slice + (red + 2 * width) * 4);
+    return true;
+}
+
+template <typename Kern>
+static bool gn_small_ready(PerDevice<int>& cache, Kern kern) {
+    return cache.get([&](int&, int) {
+        // 64 KB of data, at most 256 x 8 sums of 8 bytes, statistics
+        return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnSmallSmem + 24 * 1024) == cudaSuccess;
+    }) != nullptr;
+}
+
+template <typename T, int V, int ACT>
+static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
+    size_t smem = 0;
+    if (gn_small_cut<T, V>(A, backward, &smem)) {
+        static PerDevice<int> ready, ready_grad;
+        if (!backward) {
+            if (!gn_small_ready(ready, gn_small_kernel<T, V, ACT>)) return cudaErrorInvalidValue;
+            return launch_after(gn_small_kernel<T, V, ACT>, dim3((unsigned)A.blocks, (unsigned)A.N), dim3(kGnThreads), smem, st, A);
+        }
+        if (!gn_small_ready(ready_grad, gn_small_grad_kernel<T, V, ACT>)) return cudaErrorInvalidValue;
+        return launch_after(gn_small_grad_kernel<T, V, ACT>, dim3((unsigned)A.blocks), dim3(kGnThreads), smem, st, A);
+    }
     const dim3 grid((unsigned)A.chunks, (unsigned)A.N, (unsigned)A.blocks);
-    const size_t smem = (size_t)kGnThreads * V * sizeof(float2);
+    const unsigned group_ctas = (unsigned)ceil_div((int64_t)A.N * A.G, kGnThreads / 32);
+    // the rings; the sums of pass 1 (V pairs per thread) take their place
+    constexpr bool ring = GnRing<T, V>::value;
+    constexpr size_t sums = (size_t)kGnThreads * V * sizeof(float2);
+    constexpr size_t one = ring ? (size_t)kGnThreads * 16 * kGnDepth : 0, two = ring ? (size_t)kGnThreads * 16 * 2 * kGnGradDepth : 0;
+    static_assert(one <= 48 * 1024 && two <= 48 * 1024 && sums <= 48 * 1024, "more than a kernel has without asking");
     cudaError_t e;
     if (!backward) {
-        gn_stats_kernel<T, V><<<grid, kGnThreads, smem, st>>>(A);
+        gn_stats_kernel<T, V><<<grid, kGnThreads, sums > one ? sums : one, st>>>(A);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        auto k = act == DVDQ_ACT_GELU_TANH ? gn_apply_kernel<T, V, DVDQ_ACT_GELU_TANH>
-                 : act == DVDQ_ACT_SILU    ? gn_apply_kernel<T, V, DVDQ_ACT_SILU>
-                                           : gn_apply_kernel<T, V, DVDQ_ACT_NONE>;
-        return launch_after(k, grid, dim3(kGnThreads), smem, st, A);
+        if ((e = launch_after(gn_join_kernel<false>, dim3(group_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess) return e;
+        return launch_after(gn_apply_kernel<T, V, ACT>, grid, dim3(kGnThreads), one, st, A);
     }
-    if (act == DVDQ_ACT_GELU_TANH) gn_grad_stats_kernel<T, V, DVDQ_ACT_GELU_TANH><<<grid, kGnThreads, smem, st>>>(A);
-    else if (act == DVDQ_ACT_SILU) gn_grad_stats_kernel<T, V, DVDQ_ACT_SILU><<<grid, kGnThreads, smem, st>>>(A);
-    else gn_grad_stats_kernel<T, V, DVDQ_ACT_NONE><<<grid, kGnThreads, smem, st>>>(A);
+    gn_grad_stats_kernel<T, V, ACT><<<grid, kGnThreads, sums > two ? sums : two, st>>>(A);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    auto k = act == DVDQ_ACT_GELU_TANH ? gn_grad_apply_kernel<T, V, DVDQ_ACT_GELU_TANH>
-             : act == DVDQ_ACT_SILU    ? gn_grad_apply_kernel<T, V, DVDQ_ACT_SILU>
-                                       : gn_grad_apply_kernel<T, V, DVDQ_ACT_NONE>;
-    return launch_after(k, grid, dim3(kGnThreads), smem, st, A);
+    const unsigned channel_ctas = A.dgamma || A.dbeta ? (unsigned)ceil_div(A.C, 32) : 0;
+    if ((e = launch_after(gn_join_kernel<true>, dim3(group_ctas + channel_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess)
+        return e;
+    return A.y ? launch_after(gn_grad_apply_kernel<T, V, ACT>, grid, dim3(kGnThreads), two, st, A) : cudaSuccess;
+}
+
+template <typename T, int V>
+static cudaError_t launch_gn_v(const GnArgs& A, bool backward, int act, cudaStream_t st) {
+    if (act == DVDQ_ACT_GELU_TANH) return launch_gn_act<T, V, DVDQ_ACT_GELU_TANH>(A, backward, st);
+    if (act == DVDQ_ACT_SILU) return launch_gn_act<T, V, DVDQ_ACT_SILU>(A, backward, st);
+    return launch_gn_act<T, V, DVDQ_ACT_NONE>(A, backward, st);
 }
 
 // Whole 16-byte accesses where channels, pitches and pointers allow it, single elements otherwise.
