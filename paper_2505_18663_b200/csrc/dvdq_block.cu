@@ -7,6 +7,7 @@
 
 #include "group_norm.cuh"
 #include "linear.cuh"
+#include "linear_few.cuh"
 #include "rope.cuh"
 
 namespace dvdq {
@@ -18,7 +19,7 @@ static bool valid_dtype(int32_t t) { return valid_dtype16(t) || t == DVDQ_F32; }
 static bool valid_act(int32_t a) { return a == DVDQ_ACT_NONE || a == DVDQ_ACT_GELU_TANH || a == DVDQ_ACT_SILU; }
 
 // A matrix operand of the linear layer: rows start on 16 bytes; the pitch of a single row is not read.
-constexpr int64_t kLinMaxDim = 0x7FFFFF00ll, kLinMaxPitch = (int64_t)1 << 38;
+constexpr int64_t kLinMaxTokens = 0x7FFFFF00ll, kLinMaxChannels = (int64_t)1 << 25, kLinMaxPitch = (int64_t)1 << 38;
 static dvdq_status check_matrix(const void* p, int64_t rows, int64_t cols, int64_t* ld, bool required) {
     if (!p) return required ? DVDQ_ERR_NULL : DVDQ_OK;
     if (rows <= 1) *ld = align_up(cols, 8);
@@ -27,7 +28,7 @@ static dvdq_status check_matrix(const void* p, int64_t rows, int64_t cols, int64
     return DVDQ_OK;
 }
 static bool linear_sizes_ok(int64_t M, int64_t N, int64_t K) {
-    if (M < 0 || N <= 0 || K <= 0 || M > kLinMaxDim || N > kLinMaxDim || K > kLinMaxDim) return false;
+    if (M < 0 || N <= 0 || K <= 0 || M > kLinMaxTokens || N > kLinMaxChannels || K > kLinMaxChannels) return false;
     const int64_t m = ceil_div(M, kLinTile), n = ceil_div(N, kLinTile), k = ceil_div(K, kLinTile), most = (int64_t)1 << 24;
     return m * n < most && m * k < most && n * k < most;  // tiles of y, dX and dW
 }
@@ -44,9 +45,13 @@ struct LinBackwardPlan {
     int64_t chunks, rows;
 };
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
-    LinBackwardPlan p;
-    p.dx = lin_plan(M, K, N);
-    p.dw = lin_plan(N, K, M);
+    LinBackwardPlan p = {};
+    if (M <= kFewTokens) {
+        p.total = few_dx_plan(M, N, K).bytes;
+        return p;
+    }
+    p.dx = lin_plan(M, K, N, 64);
+    p.dw = lin_plan(N, K, M, 64);
     p.lddz = align_up(N, 8);
     p.rows = ceil_div(M, dz_chunks(M, N));
     p.chunks = ceil_div(M, p.rows);
@@ -60,12 +65,19 @@ static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int
 template <typename T>
 static dvdq_status linear_t(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e, const LinMatrix& y,
                             void* ws, cudaStream_t st) {
-    return launch_linear<T, false, false>(x, w, M, N, K, lin_plan(M, N, K), e, y, static_cast<float*>(ws), st);
+    if (M <= kFewTokens) return launch_linear_few<T>(x, w, M, N, K, e, y, st);
+    return launch_linear<T, false, false>(x, w, M, N, K, lin_plan(M, N, K, 32), e, y, static_cast<float*>(ws), st);
 }
 
 template <typename T>
 static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N,
                                      int64_t K, int32_t act, const LinMatrix& dx, const LinMatrix& dw, float* db, uint8_t* ws, cudaStream_t st) {
+    if (M <= kFewTokens) {
+        float* few = reinterpret_cast<float*>(ws);
+        if (M == 1) return launch_linear_few_grad<T, 1>(dy, z, x, w, M, N, K, act, dx, dw, db, few, st);
+        if (M <= 4) return launch_linear_few_grad<T, 4>(dy, z, x, w, M, N, K, act, dx, dw, db, few, st);
+        return launch_linear_few_grad<T, 16>(dy, z, x, w, M, N, K, act, dx, dw, db, few, st);
+    }
     const LinBackwardPlan p = linear_backward_plan(M, N, K, act);
     float* sums = db ? reinterpret_cast<float*>(ws + p.sums_off) : nullptr;
     float* part = reinterpret_cast<float*>(ws + p.part_off);
@@ -77,7 +89,7 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
         auto k = act == DVDQ_ACT_GELU_TANH ? linear_dz_kernel<T, DVDQ_ACT_GELU_TANH>
                  : act == DVDQ_ACT_SILU    ? linear_dz_kernel<T, DVDQ_ACT_SILU>
                                            : linear_dz_kernel<T, DVDQ_ACT_NONE>;
-        k<<<grid, kLinDzThreads, 0, st>>>(static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p), z.ld, M, (int)N, p.rows,
+        k<<<grid, kStreamThreads, 0, st>>>(static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p), z.ld, M, (int)N, p.rows,
                                           static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, sums);
         if ((s = cuda_status(cudaGetLastError())) != DVDQ_OK) return s;
         if (db && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
@@ -99,8 +111,8 @@ extern "C" {
 // ---- the 16-bit linear layer ------------------------------------------------------------------
 
 size_t dvdq_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (!linear_sizes_ok(M, N, K) || M == 0) return 0;
-    return (size_t)lin_plan(M, N, K).part_bytes;
+    if (!linear_sizes_ok(M, N, K) || M <= kFewTokens) return 0;
+    return (size_t)lin_plan(M, N, K, 32).part_bytes;
 }
 
 dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, int64_t N, int64_t K, int64_t ldw, const void* bias,
@@ -265,7 +277,7 @@ dvdq_status dvdq_rope(const dvdq_rope_tensor* q, const dvdq_rope_tensor* k, int6
     A.rows = rows;
     A.rows_batch = rows_batch;
     A.table_rows = table_rows;
-    A.S = (int)S;
+    A.S = S;
     A.rot = rot_dim;
     A.head_dim = head_dim;
     A.inverse = inverse != 0;

@@ -23,7 +23,7 @@
 
 namespace dvdq {
 
-constexpr int kGnThreads = 256;
+constexpr int kGnThreads = kStreamThreads;
 constexpr int kGnMaxVecs = kGnThreads;  // channel vectors of one CTA; wider rows are cut into channel blocks
 
 struct GnArgs {
@@ -150,80 +150,6 @@ __device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V
     }
 }
 
-template <typename T, int V> struct GnRing { static constexpr bool value = sizeof(T) * V == 16; };
-
-// A thread's own stream of 16-byte pieces, `count` of them from STREAMS tensors side by side, through a ring
-// of D slots of its own in shared memory (cp.async): D - 1 pieces per tensor are in flight while one is
-// worked on, without a register each, and no barrier is needed.  With whole batches of register loads
-// a warp waits for its slowest load with nothing in flight: 3.8 instead of 5 TB/s.
-// A slot is refilled only when what was read from it has been delivered: the copy's address
-// depends on the words read (ANDed with a zero that the compiler does not know).
-template <int D, int STREAMS, typename T, int V, typename Use>
-__device__ __forceinline__ void gn_stream(uint32_t ring, int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
-    constexpr uint32_t kSlot = kGnThreads * 16;
-    static_assert(sizeof(Vec<T, V>) == 16, "16-byte pieces");
-    uint32_t zero;
-    asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
-    zero -= 1u;
-    auto fill = [&](uint32_t slot, int k, uint32_t dep) {
-        if (k < count) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * STREAMS * kSlot + dep), "l"(from0) : "memory");
-            from0 += step0;
-            if constexpr (STREAMS == 2) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (slot * STREAMS + 1) * kSlot + dep), "l"(from1) : "memory");
-                from1 += step1;
-            }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-#pragma unroll
-    for (int k = 0; k < D - 1; ++k) fill((uint32_t)k, k, 0u);
-    uint32_t slot = 0, behind = D - 1, dep = 0u;  // `behind`: the slot that was read last (at first: the one not yet filled)
-    for (int k = 0; k < count; ++k) {
-        fill(behind, k + D - 1, dep);
-        asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory");
-        union { uint4 w; Vec<T, V> v; } in[STREAMS];
-        dep = 0u;
-#pragma unroll
-        for (int j = 0; j < STREAMS; ++j) {
-            in[j].w = lds128(ring + (slot * STREAMS + j) * kSlot);
-            dep ^= in[j].w.w;
-        }
-        dep &= zero;
-        if constexpr (STREAMS == 1) use(in[0].v);
-        else use(in[0].v, in[1].v);
-        behind = slot;
-        slot = slot + 1 == D ? 0u : slot + 1;
-    }
-}
-// The same sequence with plain loads, for accesses narrower than 16 bytes.
-template <int STREAMS, typename T, int V, typename Use>
-__device__ __forceinline__ void gn_plain_stream(int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
-#pragma unroll 4
-    for (int k = 0; k < count; ++k) {
-        const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(from0);
-        from0 += step0;
-        if constexpr (STREAMS == 1) {
-            use(a);
-        } else {
-            const Vec<T, V> b = *reinterpret_cast<const Vec<T, V>*>(from1);
-            from1 += step1;
-            use(a, b);
-        }
-    }
-}
-template <int D, int STREAMS, typename T, int V, typename Use>
-__device__ __forceinline__ void gn_walk(const uint8_t* raw, int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
-    if constexpr (GnRing<T, V>::value)
-        gn_stream<D, STREAMS, T, V>(smem_u32(raw) + threadIdx.x * 16, count, from0, step0, from1, step1, use);
-    else
-        gn_plain_stream<STREAMS, T, V>(count, from0, step0, from1, step1, use);
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_streaming(T* p, const Vec<T, V>& v) {  // written once, not read here again: first out of L2
-    if constexpr (sizeof(Vec<T, V>) == 16) __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
-    else *reinterpret_cast<Vec<T, V>*>(p) = v;
-}
 constexpr int kGnDepth = 8, kGnGradDepth = 5;  // slots: 32 KB a CTA, 40 KB for two tensors; four CTAs per SM
 
 template <typename T, int V>
@@ -245,7 +171,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_co
         }
         Pairs<V> pivot;
         pivot.set(pv);
-        gn_walk<kGnDepth, 1, T, V>(raw, P.count(A.lanes), base + P.c0 + (P.s0 + P.r) * A.xs, A.lanes * A.xs, nullptr, 0, [&](const Vec<T, V>& v) {
+        walk<kGnDepth, 1, T, V>(raw, P.count(A.lanes), base + P.c0 + (P.s0 + P.r) * A.xs, A.lanes * A.xs, nullptr, 0, [&](const Vec<T, V>& v) {
             const Pairs<V> x = widen2<T, V>(v);
 #pragma unroll
             for (int i = 0; i < Pairs<V>::N; ++i) {
@@ -384,7 +310,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
     T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0 + last * A.ys;
     const int64_t back = -(int64_t)A.lanes * A.ys;
-    gn_walk<kGnDepth, 1, T, V>(raw, count, static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + last * A.xs, -(int64_t)A.lanes * A.xs, nullptr, 0,
+    walk<kGnDepth, 1, T, V>(raw, count, static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + last * A.xs, -(int64_t)A.lanes * A.xs, nullptr, 0,
                                [&](const Vec<T, V>& v) {
         const Pairs<V> x = widen2<T, V>(v);
         Pairs<V> o;
@@ -438,7 +364,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_grad_stats_kernel(const __gr
         float rs[V], ga[V];
         const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
         const int64_t s0 = P.s0 + P.r;
-        gn_walk<kGnGradDepth, 2, T, V>(raw, P.count(A.lanes), static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + s0 * A.xs, A.lanes * A.xs,
+        walk<kGnGradDepth, 2, T, V>(raw, P.count(A.lanes), static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + s0 * A.xs, A.lanes * A.xs,
                                        static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0 + s0 * A.ds, A.lanes * A.ds,
                                        [&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
             const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
@@ -495,7 +421,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __gr
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
     T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0 + last * A.ys;
     const int64_t back = -(int64_t)A.lanes * A.ys;
-    gn_walk<kGnGradDepth, 2, T, V>(raw, count, static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + last * A.xs, -(int64_t)A.lanes * A.xs,
+    walk<kGnGradDepth, 2, T, V>(raw, count, static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + last * A.xs, -(int64_t)A.lanes * A.xs,
                                    static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0 + last * A.ds, -(int64_t)A.lanes * A.ds,
                                    [&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
         const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
@@ -824,7 +750,7 @@ static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
     const dim3 grid((unsigned)A.chunks, (unsigned)A.N, (unsigned)A.blocks);
     const unsigned group_ctas = (unsigned)ceil_div((int64_t)A.N * A.G, kGnThreads / 32);
     // the rings; the sums of pass 1 (V pairs per thread) take their place
-    constexpr bool ring = GnRing<T, V>::value;
+    constexpr bool ring = WholePieces<T, V>::value;
     constexpr size_t sums = (size_t)kGnThreads * V * sizeof(float2);
     constexpr size_t one = ring ? (size_t)kGnThreads * 16 * kGnDepth : 0, two = ring ? (size_t)kGnThreads * 16 * 2 * kGnGradDepth : 0;
     static_assert(one <= 48 * 1024 && two <= 48 * 1024 && sums <= 48 * 1024, "more than a kernel has without asking");

@@ -7,12 +7,13 @@
 // A transposed operand is read where it lies: tcgen05 takes shared-memory tiles whose contiguous
 // axis is the contracted one ("K-major") or the other one ("MN-major"), so nothing is transposed in memory.
 //
-// A CTA pair owns a 256 x 256 tile of D: tcgen05.mma.cta_group::2.kind::f16 256x256x16, operands in
-// shared memory (128-byte swizzle) in a ring of TMA-filled stages of 64 along k, two 256-column fp32
+// A CTA pair owns a tile of 256 rows x `bn` columns of D (bn = 32 .. 256, chosen per call: the smaller
+// it is, the more tiles a small product has for the 74 pairs): tcgen05.mma.cta_group::2.kind::f16 256 x bn x 16,
+// operands in shared memory (128-byte swizzle) in a ring of TMA-filled stages of 64 along k, two fp32
 // accumulators in tensor memory, so that the epilogue of a tile runs under the next tile's products.
 // Roles per CTA: warp 0 TMA producer; warp 1 (leader CTA) issues the products; warps 4-11 epilogue, two
-// per tensor-memory lane quarter, 128 columns each: bias, activation, residual in fp32, ONE rounding, and
-// TMA stores of 32 x 32 blocks; the residual's blocks come by TMA one block ahead.
+// per tensor-memory lane quarter, every other 32 columns each: bias, activation, residual in fp32, ONE rounding,
+// and TMA stores of 32 x 32 blocks; the residual's blocks come by TMA one block ahead.
 //
 // What bounds it: the tensor pipe on layers of thousands of tokens; with few tokens, streaming W.
 // Products with fewer tiles than CTA pairs are cut along k (`splits`): each piece writes its fp32 sums,
@@ -25,7 +26,7 @@
 namespace dvdq {
 
 constexpr int kLinBK = 64;                    // elements of k per stage: one 128-byte swizzle row
-constexpr int kLinTile = 256;                 // rows and columns of a pair's tile
+constexpr int kLinTile = 256;                 // rows of a pair's tile, and most columns
 constexpr int kLinEpiWarps = 8, kLinFirstEpi = 4;
 constexpr int kLinThreads = (kLinFirstEpi + kLinEpiWarps) * 32;
 constexpr int kLinPairs = 74;                 // CTA pairs of a B200 (148 SMs): what the split along k is planned for
@@ -51,6 +52,7 @@ struct LinSmem {
 
 struct LinArgs {
     int Md, Nd;             // rows and columns of D
+    int bn;                 // columns of a tile: a multiple of 32 (of 64 where B is MN-major)
     int num_m, num_n;       // tiles
     int kblocks, splits;    // k-blocks of the contraction, pieces it is cut into
     int panel;              // column tiles walked together
@@ -87,11 +89,11 @@ __device__ __forceinline__ uint64_t umma_desc_sw128_mnmajor(uint32_t smem_addr) 
     d |= (uint64_t)2u << 61;
     return d;
 }
-// Instruction descriptor for kind::f16: fp32 accumulator, both operands bf16 (or both fp16), and which
-// of them are MN-major.
-__host__ __device__ constexpr uint32_t umma_idesc_f16(bool bf16, bool a_mn, bool b_mn, int m, int n) {
+// Instruction descriptor for kind::f16: fp32 accumulator, both operands bf16 (or both fp16), which of them
+// are MN-major, and the shape; n is added at run time.
+__host__ __device__ constexpr uint32_t umma_idesc_f16(bool bf16, bool a_mn, bool b_mn, int m) {
     return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+           ((uint32_t)(m >> 4) << 24);
 }
 __device__ __forceinline__ void tc_mma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -102,17 +104,19 @@ __device__ __forceinline__ void tc_mma_f16_pair(uint32_t d_tmem, uint64_t a_desc
         : "memory");
 }
 
-// This CTA's 128 rows (or columns) of an operand's stage: one box of 64 x 128 rows, or two boxes of 64
-// columns x 64 rows of k; both count their bytes on the leader's barrier.
+// This CTA's `width` rows (or columns) of an operand's stage: one box of 64 x width, or boxes of 64 columns x 64
+// rows of k (the last one may be wider than needed); all count their bytes on the leader's barrier.
 template <bool MN>
-__device__ __forceinline__ void lin_load(uint32_t dst, const CUtensorMap* m, uint32_t bar, int k0, int r0) {
+__device__ __forceinline__ void lin_load(uint32_t dst, const CUtensorMap* m, uint32_t bar, int k0, int r0, int width) {
     if (!MN) {
         tma_load_2d_pair(dst, m, bar, k0, r0);
     } else {
         tma_load_2d_pair(dst, m, bar, r0, k0);
-        tma_load_2d_pair(dst + kLinBK * 128, m, bar, r0 + 64, k0);
+        if (width > 64) tma_load_2d_pair(dst + kLinBK * 128, m, bar, r0 + 64, k0);
     }
 }
+template <bool MN>
+__device__ __forceinline__ uint32_t lin_bytes(int width) { return (uint32_t)(MN ? (width + 63) / 64 * (kLinBK * 128) : width * kLinBK * 2); }
 
 template <typename T, bool AMN, bool BMN, int OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
@@ -164,17 +168,19 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             tma_prefetch_desc(&tmB);
             uint32_t st = 0, ph = 0;
             bool ok = true;
+            const int bw = A.bn / 2;  // columns per CTA
+            const uint32_t bytes = 2 * (lin_bytes<AMN>(128) + lin_bytes<BMN>(bw));
             for (int item = pair; ok && item < items; item += num_pairs) {
                 int tm, tn, piece;
                 lin_item(A, item, tm, tn, piece);
                 const int2 kr = lin_range(A, piece);
-                const int m0 = tm * kLinTile + (int)rank * 128, n0 = tn * kLinTile + (int)rank * 128;
+                const int m0 = tm * kLinTile + (int)rank * 128, n0 = tn * A.bn + (int)rank * bw;
                 for (int kb = kr.x; kb < kr.y; ++kb) {
                     if (!mbar_wait(empty(st), ph ^ 1u, abort_flag, kWaitWideEmpty)) { ok = false; break; }
-                    if (rank == 0) mbar_arrive_expect_tx(full(st), 2 * S::kStage);
+                    if (rank == 0) mbar_arrive_expect_tx(full(st), bytes);
                     const uint32_t bar = map_to_cta(full(st), 0), dst = sbase + st * S::kStage;
-                    lin_load<AMN>(dst, &tmA, bar, kb * kLinBK, m0);
-                    lin_load<BMN>(dst + S::kOperand, &tmB, bar, kb * kLinBK, n0);
+                    lin_load<AMN>(dst, &tmA, bar, kb * kLinBK, m0, 128);
+                    lin_load<BMN>(dst + S::kOperand, &tmB, bar, kb * kLinBK, n0, bw);
                     if (++st == ST) { st = 0; ph ^= 1u; }
                 }
             }
@@ -185,7 +191,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     } else if (warp == 1) {
         // ------------------------------------------------------------ products (leader CTA only)
         if (rank == 0) {
-            constexpr uint32_t idesc = umma_idesc_f16(IsBf16<T>::value, AMN, BMN, kLinTile, kLinTile);
+            const uint32_t idesc = umma_idesc_f16(IsBf16<T>::value, AMN, BMN, kLinTile) | ((uint32_t)(A.bn >> 3) << 17);
             // 16 elements along k: 32 bytes inside a K-major swizzle row, two atoms of an MN-major tile
             constexpr uint32_t kStepA = AMN ? 2048 / 16 : 2, kStepB = BMN ? 2048 / 16 : 2;
             uint32_t st = 0, ph = 0, lt = 0;
@@ -223,7 +229,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     } else if (warp >= kLinFirstEpi) {
         // ------------------------------------------------------------ epilogue
         const int ew = warp - kLinFirstEpi;
-        const int q = warp & 3, half = ew >> 2;  // tensor-memory lane quarter; which 128 of the 256 columns
+        const int q = warp & 3, half = ew >> 2;  // tensor-memory lane quarter; which of every two 32-column blocks
         const uint32_t buf0 = sbase + S::kBufOff + ew * (S::kBufs * S::kBuf);
         const uint32_t c_bias = sbase + S::kBiasOff + ew * 128;
         const bool residual = OUT != kLinPartial && A.has_residual;
@@ -245,9 +251,10 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             int tm, tn, piece;
             lin_item(A, item, tm, tn, piece);
             const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
-            const int row0 = tm * kLinTile + (int)rank * 128 + q * 32, col0 = tn * kLinTile + half * 128;
-            // 32 x 32 blocks of this warp that lie in D
-            const int blocks = row0 < A.Md && col0 < A.Nd ? min(4, (A.Nd - col0 + 31) >> 5) : 0;
+            const int row0 = tm * kLinTile + (int)rank * 128 + q * 32, col0 = tn * A.bn + half * 32;
+            // 32 x 32 blocks of this warp that lie in D: columns col0, col0 + 64, ...
+            const int width = min(A.bn, A.Nd - tn * A.bn) - half * 32;
+            const int blocks = row0 < A.Md && width > 0 ? (width + 63) >> 6 : 0;
             float b_next = 0.f;
             if (with_bias && blocks > 0 && col0 + lane < A.Nd) b_next = to_f32(bias[col0 + lane]);
             __syncwarp();
@@ -259,7 +266,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             for (int c = 0; c < blocks; ++c) {
                 uint32_t r[32];
                 __syncwarp();
-                tmem_ld_32x32(tmem_base + a * kLinTile + half * 128 + c * 32 + ((uint32_t)(q * 32) << 16), r);
+                tmem_ld_32x32(tmem_base + a * kLinTile + half * 32 + c * 64 + ((uint32_t)(q * 32) << 16), r);
                 if (OUT == kLinPartial) {
                     if (lane == 0) tma_store_wait_read<0>();
                     __syncwarp();
@@ -270,18 +277,18 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(&tmY, buf0, col0 + c * 32, piece * A.part_rows + row0);
+                        tma_store_2d(&tmY, buf0, col0 + c * 64, piece * A.part_rows + row0);
                         tma_store_commit();
                     }
                     continue;
                 }
                 // the block's output buffer: free once all but the newest store have been read
                 // (with a residual, ask() has waited for it)
-                if (residual && c + 1 < blocks) ask(row0, col0 + (c + 1) * 32);
+                if (residual && c + 1 < blocks) ask(row0, col0 + (c + 1) * 64);
                 if (!residual && lane == 0) tma_store_wait_read<1>();
                 if (with_bias) sts32f(c_bias + 4 * lane, b_next);
                 __syncwarp();
-                if (with_bias && c + 1 < blocks) b_next = col0 + (c + 1) * 32 + lane < A.Nd ? to_f32(bias[col0 + (c + 1) * 32 + lane]) : 0.f;
+                if (with_bias && c + 1 < blocks) b_next = col0 + (c + 1) * 64 + lane < A.Nd ? to_f32(bias[col0 + (c + 1) * 64 + lane]) : 0.f;
                 const uint32_t buf = buf0 + ((residual ? rwait : blk) & 1u) * S::kBuf;
                 if (residual) {
                     ok = mbar_wait_warp(res_full(ew, rwait & 1u), (rwait >> 1) & 1u, abort_flag, kWaitPackedFull);
@@ -313,7 +320,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(&tmZ, zb, col0 + c * 32, row0);
+                        tma_store_2d(&tmZ, zb, col0 + c * 64, row0);
                         tma_store_commit();
                     }
                 }
@@ -342,7 +349,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    tma_store_2d(&tmY, buf, col0 + c * 32, row0);
+                    tma_store_2d(&tmY, buf, col0 + c * 64, row0);
                     tma_store_commit();
                 }
             }
@@ -420,75 +427,70 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
 // the two products half of their rate or more); the bias's gradient sums the unrounded values.
 // A CTA takes 256 columns (8 per thread, 32 threads side by side, 8 rows at a time) of one chunk of
 // rows and writes their sums; linear_colsum_kernel adds the chunks.  act = none: dz is dy itself, only sums.
-constexpr int kLinDzThreads = 256, kLinDzCols = 256;
+constexpr int kLinDzCols = 256, kLinDzDepth = 5;
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(kLinDzThreads)
+__global__ void __launch_bounds__(kStreamThreads, 4)
 linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, int64_t M, int N, int64_t rows,
                  T* __restrict__ dz, int64_t lddz, float* __restrict__ sums) {
+    constexpr bool kAct = ACT != DVDQ_ACT_NONE;
+    __shared__ __align__(16) uint8_t raw[kStreamThreads * 16 * kLinDzDepth * (kAct ? 2 : 1)];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
     const int n = blockIdx.x * kLinDzCols + tx * 8;
     const int64_t m0 = (int64_t)blockIdx.y * rows, m1 = m0 + rows < M ? m0 + rows : M;
-    float s[8];
+    Pairs<8> s;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = 0.f;
+    for (int i = 0; i < 4; ++i) s.p[i] = 0ull;
     const int here = N - n < 8 ? N - n : 8;
-    if (here > 0) {
-        // rows start on 16 bytes and have room for whole 16-byte groups up to the pitch, but only the
-        // first N values of a row are the caller's: the last group goes element by element
-        auto row = [&](int64_t m, const Vec<T, 8>& d, const Vec<T, 8>& zz) {
-            float v[8];
+    const int64_t mt = m0 + ty;
+    const int count = here > 0 && mt < m1 ? (int)((m1 - mt + 7) / 8) : 0;
+    if (count > 0) {
+        T* out = dz + mt * lddz + n;
+        auto row = [&](const Vec<T, 8>& dv, const Vec<T, 8>& zv) {
+            Pairs<8> d = widen2<T, 8>(dv);
+            const Pairs<8> zz = widen2<T, 8>(zv);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = to_f32(d.e[j]);
-                if (ACT != DVDQ_ACT_NONE) v[j] *= act_slope<ACT>(to_f32(zz.e[j]));
-                s[j] += v[j];
+            for (int i = 0; i < 4; ++i) {
+                if (kAct) d.p[i] = f2_mul(d.p[i], act_slope2<ACT>(zz.p[i]));
+                s.p[i] = f2_add(s.p[i], d.p[i]);
             }
-            if (ACT != DVDQ_ACT_NONE) *reinterpret_cast<Vec<T, 8>*>(dz + m * lddz + n) = narrow<T, 8>(v);
+            if (kAct) {
+                *reinterpret_cast<Vec<T, 8>*>(out) = narrow2<T, 8>(d);
+                out += 8 * lddz;
+            }
         };
         if (here == 8) {
-            constexpr int U = 4;
-            int64_t m = m0 + ty;
-            for (; m + (U - 1) * 8 < m1; m += U * 8) {
-                Vec<T, 8> d[U], zz[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    d[u] = *reinterpret_cast<const Vec<T, 8>*>(dy + (m + u * 8) * lddy + n);
-                    if (ACT != DVDQ_ACT_NONE) zz[u] = *reinterpret_cast<const Vec<T, 8>*>(z + (m + u * 8) * ldz + n);
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) row(m + u * 8, d[u], zz[u]);
-            }
-            for (; m < m1; m += 8) {
-                Vec<T, 8> zz = {};
-                if (ACT != DVDQ_ACT_NONE) zz = *reinterpret_cast<const Vec<T, 8>*>(z + m * ldz + n);
-                row(m, *reinterpret_cast<const Vec<T, 8>*>(dy + m * lddy + n), zz);
-            }
+            const T *pd = dy + mt * lddy + n, *pz = z + mt * ldz + n;
+            if constexpr (kAct) walk<kLinDzDepth, 2, T, 8>(raw, count, pd, 8 * lddy, pz, 8 * ldz, row);
+            else walk<kLinDzDepth, 1, T, 8>(raw, count, pd, 8 * lddy, pd, 0, [&](const Vec<T, 8>& dv) { row(dv, dv); });
         } else {
-            for (int64_t m = m0 + ty; m < m1; m += 8) {
+            // only the first N values of a row are the caller's: the last group goes element by element
+            // (dz is the workspace's: whole groups may be written)
+            for (int64_t m = mt; m < m1; m += 8) {
                 Vec<T, 8> d, zz;
                 for (int j = 0; j < 8; ++j) {
                     d.e[j] = from_f32<T>(0.f);
                     zz.e[j] = from_f32<T>(0.f);
                     if (j < here) {
                         d.e[j] = dy[m * lddy + n + j];
-                        if (ACT != DVDQ_ACT_NONE) zz.e[j] = z[m * ldz + n + j];
+                        if (kAct) zz.e[j] = z[m * ldz + n + j];
                     }
                 }
-                row(m, d, zz);  // dz is the workspace's: whole groups may be written
+                row(d, zz);
             }
         }
     }
     if (sums) {
-        __shared__ float sh[8][kLinDzCols + 8];
+        __syncthreads();  // the ring's memory becomes the sums'
+        float* sh = reinterpret_cast<float*>(raw);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sh[ty][tx * 8 + j] = s[j];
+        for (int j = 0; j < 8; ++j) sh[ty * kLinDzCols + tx * 8 + j] = s.get(j);
         __syncthreads();
         const int c = blockIdx.x * kLinDzCols + threadIdx.x;
         if (c < N) {
             float t = 0.f;
 #pragma unroll
-            for (int y = 0; y < 8; ++y) t += sh[y][threadIdx.x];
+            for (int y = 0; y < 8; ++y) t += sh[y * kLinDzCols + threadIdx.x];
             sums[(int64_t)blockIdx.y * N + c] = t;
         }
     }
@@ -516,26 +518,34 @@ __global__ void __launch_bounds__(256) linear_colsum_kernel(const float* __restr
 // ------------------------------------------------------------------ host side
 
 struct LinPlan {
-    int splits;
+    int bn, splits;
     int64_t part_rows, part_pitch, part_bytes;
 };
 
-// Pieces along k, from the sizes alone.  In units of one k-block's products (0.37 us per pair): a wave of
-// items costs its k-blocks plus about 8 for filling the ring and draining the last accumulator; cutting
-// costs writing and reading the fp32 pieces (about 6 TB/s of L2 traffic) and a launch (about 6 units).
-inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc) {
-    const int64_t tiles = ceil_div(Md, kLinTile) * ceil_div(Nd, kLinTile), kb = ceil_div(Kc, kLinBK);
+// Tile width and pieces along k, from the sizes alone, by an estimate in microseconds fitted to measurements: a k-block of a
+// 256-row tile takes a pair 0.37 us per 256 columns of products, but at least the time to bring its operands from L2 (about
+// 240 GB/s per pair); a tile's epilogue 0.5 + 2 us per 256 columns, hidden under the next tile's products if there is one; 2 us
+// to fill the ring.  Pieces cost a second launch (3.5 us) and writing and reading their fp32 sums (about 5 TB/s).
+// `step`: 32, or 64 where B is MN-major (its shared-memory tiles are 64 columns wide).
+inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
+    const int64_t kb = ceil_div(Kc, kLinBK), num_m = ceil_div(Md, kLinTile);
     LinPlan p;
+    p.bn = kLinTile;
     p.splits = 1;
     p.part_rows = align_up(Md, 32);
     p.part_pitch = align_up(Nd, 4);
     double best = 1e300;
-    for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
-        if (s > 1 && s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20)) break;
-        const double waves = (double)ceil_div(tiles * s, kLinPairs);
-        double cost = waves * ((double)ceil_div(kb, s) + 8.0);
-        if (s > 1) cost += 6.0 + (double)s * Md * Nd * 8.0 / 6.0e12 / 0.37e-6;
-        if (cost < best * 0.98) { best = cost; p.splits = (int)s; }
+    for (int bn = kLinTile; bn >= 32 && bn % step == 0; bn -= step) {
+        const int64_t tiles = num_m * ceil_div(Nd, bn);
+        const double products = 0.37 * bn / 256.0, feed = (256.0 + bn) * 128.0 / 240e3;
+        const double t_kb = products > feed ? products : feed, t_epi = 0.5 + 2.0 * bn / 256.0;
+        for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
+            if (s > 1 && (tiles * s > 4 * kLinPairs || s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20))) break;
+            const double item = (double)ceil_div(kb, s) * t_kb;
+            double cost = (double)ceil_div(tiles * s, kLinPairs) * (item > t_epi ? item : t_epi) + 2.0 + t_epi;
+            if (s > 1) cost += 3.5 + (double)s * Md * Nd * 8.0 / 5.0e6;
+            if (cost < best * 0.97) { best = cost; p.bn = bn; p.splits = (int)s; }  // a wider tile reads less: prefer it when near
+        }
     }
     p.part_bytes = p.splits > 1 ? align_up(p.splits * p.part_rows * p.part_pitch * 4, 256) : 0;
     return p;
@@ -581,11 +591,11 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
     constexpr bool bf = IsBf16<T>::value != 0;
     using S = LinSmem<OUT>;
     CUtensorMap tmA, tmB, tmY, tmR, tmZ;
-    auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows) {
+    auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows, int box) {
         return mn ? make_map16(m, bf, x.p, Kc, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
-                  : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, 128, CU_TENSOR_MAP_SWIZZLE_128B);
+                  : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, (uint32_t)box, CU_TENSOR_MAP_SWIZZLE_128B);
     };
-    if (!operand(&tmA, AMN, a, Md) || !operand(&tmB, BMN, b, Nd)) return DVDQ_ERR_CUDA;
+    if (!operand(&tmA, AMN, a, Md, 128) || !operand(&tmB, BMN, b, Nd, plan.bn / 2)) return DVDQ_ERR_CUDA;
     if (OUT == kLinPartial ? !make_map_f32(&tmY, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
                            : !make_map16(&tmY, bf, y.p, Md, Nd, y.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return DVDQ_ERR_CUDA;
@@ -597,10 +607,11 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
     A.Md = (int)Md;
     A.Nd = (int)Nd;
     A.num_m = (int)ceil_div(Md, kLinTile);
-    A.num_n = (int)ceil_div(Nd, kLinTile);
+    A.bn = plan.bn;
+    A.num_n = (int)ceil_div(Nd, plan.bn);
     A.kblocks = (int)ceil_div(Kc, kLinBK);
     A.splits = plan.splits;
-    A.panel = A.num_n < 8 ? A.num_n : 8;
+    A.panel = 2048 / plan.bn < A.num_n ? 2048 / plan.bn : A.num_n;
     A.part_rows = (int)plan.part_rows;
     A.act = e.act;
     A.has_residual = fin && e.residual.p != nullptr;

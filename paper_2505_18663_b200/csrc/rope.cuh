@@ -38,6 +38,18 @@ rope_table_kernel(const __grid_constant__ RopeAngles ang, const int32_t* __restr
     }
 }
 
+// n / d for 32-bit n by a multiplication: m = ceil(2^(32 + s) / d) with 2^s >= d, n < 2^31.
+struct FastDiv {
+    uint32_t d, m, s;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t div) : d(div), m(0), s(0) {
+        while ((1u << s) < div) ++s;
+        const uint64_t full = (((uint64_t)1 << (32 + s)) + div - 1) / div;  // in (2^32, 2^33]: keep the low word
+        m = (uint32_t)(full - ((uint64_t)1 << 32));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)__umulhi(n, m) + n) >> s); }
+};
+
 struct RopeSide {
     const void* x;
     void* y;
@@ -50,12 +62,14 @@ struct RopeArgs {
     const float2* table;
     const int32_t* rows;
     int64_t rows_batch, table_rows;
-    int64_t token0;       // first token (over batches) of this launch
-    int tokens, S;        // tokens of this launch; tokens of a sequence
+    int64_t token0;        // first token (over batches) of this launch
+    uint32_t threads;      // of this launch: tokens * groups * items
+    int64_t S;             // tokens of a sequence
     int rot, head_dim;
-    int groups;           // ceil((q.heads + k.heads) / heads per thread)
-    int items, rot_items; // accesses per head: those that rotate, then those that pass through
-    int inverse;
+    int q_groups;          // groups of heads, q's first; a group belongs to one of the two
+    FastDiv per_token, items, seq;
+    int rot_items;         // accesses per head: those that rotate, then those that pass through
+    int inverse, small;    // small: token indices fit 31 bits
 };
 
 // W elements per access; a rotating item covers W pairs of a "halves" head (two accesses) or W / 2
@@ -63,97 +77,97 @@ struct RopeArgs {
 template <typename T, bool HALVES, int W, int HEADS>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs A) {
     constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);
-    const uint32_t per_token = (uint32_t)A.groups * (uint32_t)A.items;
+    constexpr bool TWO = HALVES || W == 1;  // a rotating item is two accesses
     const uint32_t idx = blockIdx.x * (uint32_t)kRopeThreads + threadIdx.x;
-    const uint32_t lt = idx / per_token;
-    if (lt >= (uint32_t)A.tokens) return;
-    const uint32_t rem = idx - lt * per_token;
-    const int grp = (int)(rem / (uint32_t)A.items), item = (int)(rem - (uint32_t)grp * (uint32_t)A.items);
+    if (idx >= A.threads) return;
+    const uint32_t lt = A.per_token(idx), rem = idx - lt * A.per_token.d;
+    int grp = (int)A.items(rem);
+    const int item = (int)(rem - (uint32_t)grp * A.items.d);
     const int64_t token = A.token0 + lt;
-    const int64_t b = A.S == 1 ? token : token / A.S;
+    const int64_t b = A.small ? (int64_t)A.seq((uint32_t)token) : token / A.S;
     const int64_t s = token - b * A.S;
-    const int heads = A.q.heads + A.k.heads;
 
     const bool turns = item < A.rot_items;
     const int c0 = turns ? item * (HALVES ? P : 2 * P) : A.rot + (item - A.rot_items) * W;  // first channel
-    const int c1 = HALVES ? c0 + A.rot / 2 : c0 + W;                                          // the second access's
-
-    const T* src[HEADS];
-    T* dst[HEADS];
+    const int c1 = HALVES ? A.rot / 2 : W;                                                    // on to the second access's
+    float2 cs[P];
+    bool inside = true;
+    if (turns) {
+        const int64_t row = A.rows ? (int64_t)A.rows[b * A.rows_batch + s] : s;
+        inside = row >= 0 && row < A.table_rows;
+        const float2* t = A.table + (inside ? row : 0) * (A.rot / 2) + (HALVES ? c0 : c0 / 2);
+        if constexpr (P >= 2) {
+#pragma unroll
+            for (int p = 0; p < P; p += 2) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(t + p));
+                cs[p] = make_float2(v.x, v.y);
+                cs[p + 1] = make_float2(v.z, v.w);
+            }
+        } else {
+            cs[0] = __ldg(t);
+        }
+    }
+    const bool is_q = grp < A.q_groups;
+    if (!is_q) grp -= A.q_groups;
+    const RopeSide& side = is_q ? A.q : A.k;
+    const int h0 = grp * HEADS, left = side.heads - h0;  // this thread's heads: h0 .. h0 + min(HEADS, left)
+    const T* src = static_cast<const T*>(side.x) + b * side.xb + s * side.xs + h0 * side.xh + c0;
+    T* dst = static_cast<T*>(side.y) + b * side.yb + s * side.ys + h0 * side.yh + c0;
+    if (!turns && src == dst) return;  // in place: what passes through is there already
     Vec<T, W> lo[HEADS], hi[HEADS];
-    const bool two = turns && (HALVES || W == 1);
 #pragma unroll
     for (int j = 0; j < HEADS; ++j) {
-        const int h = grp + j * A.groups;
-        src[j] = nullptr;
-        if (h < heads) {
-            const bool is_q = h < A.q.heads;
-            const RopeSide& side = is_q ? A.q : A.k;
-            const int hh = is_q ? h : h - A.q.heads;
-            src[j] = static_cast<const T*>(side.x) + b * side.xb + s * side.xs + hh * side.xh;
-            dst[j] = static_cast<T*>(side.y) + b * side.yb + s * side.ys + hh * side.yh;
-            if (!turns && src[j] == dst[j]) src[j] = nullptr;  // in place: what passes through is there already
-        }
-        if (src[j]) {
-            lo[j] = *reinterpret_cast<const Vec<T, W>*>(src[j] + c0);
-            if (two) hi[j] = *reinterpret_cast<const Vec<T, W>*>(src[j] + c1);
+        if (j < left) {
+            lo[j] = *reinterpret_cast<const Vec<T, W>*>(src);
+            if (TWO && turns) hi[j] = *reinterpret_cast<const Vec<T, W>*>(src + c1);
+            src += side.xh;
         }
     }
     if (!turns) {
 #pragma unroll
-        for (int j = 0; j < HEADS; ++j)
-            if (src[j]) *reinterpret_cast<Vec<T, W>*>(dst[j] + c0) = lo[j];
+        for (int j = 0; j < HEADS; ++j) {
+            if (j < left) *reinterpret_cast<Vec<T, W>*>(dst) = lo[j];
+            dst += side.yh;
+        }
         return;
     }
-    float cs[P], sn[P];
-    {
-        const int64_t row = A.rows ? (int64_t)A.rows[b * A.rows_batch + s] : s;
-        if (row >= 0 && row < A.table_rows) {
-            const float2* t = A.table + row * (A.rot / 2) + (HALVES ? c0 : c0 / 2);
-            if constexpr (P >= 2) {
+    if (!inside) {  // a row outside the table: the outputs say so, and so does the device status
+        if (item == 0 && atomicCAS(&g_device_status[0], 0u, (uint32_t)DVDQ_ERR_SHAPE) == 0u) g_device_status[1] = kDetailRopeRow;
 #pragma unroll
-                for (int p = 0; p < P; p += 2) {
-                    const float4 v = __ldg(reinterpret_cast<const float4*>(t + p));
-                    cs[p] = v.x; sn[p] = v.y; cs[p + 1] = v.z; sn[p + 1] = v.w;
-                }
-            } else {
-                const float2 v = __ldg(t);
-                cs[0] = v.x; sn[0] = v.y;
-            }
-        } else {  // a row outside the table: the outputs say so, and so does the device status
-            if (item == 0 && grp == 0 && atomicCAS(&g_device_status[0], 0u, (uint32_t)DVDQ_ERR_SHAPE) == 0u)
-                g_device_status[1] = kDetailRopeRow;
+        for (int p = 0; p < P; ++p) cs[p] = make_float2(__int_as_float(0x7FC00000), __int_as_float(0x7FC00000));
+    }
+    if (A.inverse) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) cs[p] = sn[p] = __int_as_float(0x7FC00000);
-        }
-        if (A.inverse) {
-#pragma unroll
-            for (int p = 0; p < P; ++p) sn[p] = -sn[p];
-        }
+        for (int p = 0; p < P; ++p) cs[p].y = -cs[p].y;
     }
 #pragma unroll
     for (int j = 0; j < HEADS; ++j) {
-        if (!src[j]) continue;
-        if constexpr (HALVES || W == 1) {
-            float a[W], bb[W], ya[W], yb[W];
-            widen(lo[j], a);
-            widen(hi[j], bb);
+        if (j < left) {
+            if constexpr (TWO) {  // fp32 pairs: neighbouring channels of one half
+                const Pairs<W> a = widen2<T, W>(lo[j]), bb = widen2<T, W>(hi[j]);
+                Pairs<W> ya, yb;
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                ya[p] = fmaf(a[p], cs[p], -(bb[p] * sn[p]));
-                yb[p] = fmaf(bb[p], cs[p], a[p] * sn[p]);
-            }
-            *reinterpret_cast<Vec<T, W>*>(dst[j] + c0) = narrow<T, W>(ya);
-            *reinterpret_cast<Vec<T, W>*>(dst[j] + c1) = narrow<T, W>(yb);
-        } else {
-            float a[W], y[W];
-            widen(lo[j], a);
+                for (int i = 0; i < Pairs<W>::N; ++i) {
+                    const int p1 = 2 * i + 1 < P ? 2 * i + 1 : 2 * i;
+                    const uint64_t c = f2_pack(cs[2 * i].x, cs[p1].x), sn = f2_pack(cs[2 * i].y, cs[p1].y);
+                    const uint64_t ns = f2_pack(-cs[2 * i].y, -cs[p1].y);
+                    ya.p[i] = f2_fma(a.p[i], c, f2_mul(bb.p[i], ns));
+                    yb.p[i] = f2_fma(bb.p[i], c, f2_mul(a.p[i], sn));
+                }
+                *reinterpret_cast<Vec<T, W>*>(dst) = narrow2<T, W>(ya);
+                *reinterpret_cast<Vec<T, W>*>(dst + c1) = narrow2<T, W>(yb);
+            } else {              // fp32 pairs: (a, b) of one rotation
+                const Pairs<W> x = widen2<T, W>(lo[j]);
+                Pairs<W> y;
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                y[2 * p] = fmaf(a[2 * p], cs[p], -(a[2 * p + 1] * sn[p]));
-                y[2 * p + 1] = fmaf(a[2 * p + 1], cs[p], a[2 * p] * sn[p]);
+                for (int p = 0; p < P; ++p) {
+                    float a, bb;
+                    f2_unpack(x.p[p], a, bb);
+                    y.p[p] = f2_fma(x.p[p], f2_pack(cs[p].x, cs[p].x), f2_mul(f2_pack(bb, a), f2_pack(-cs[p].y, cs[p].y)));
+                }
+                *reinterpret_cast<Vec<T, W>*>(dst) = narrow2<T, W>(y);
             }
-            *reinterpret_cast<Vec<T, W>*>(dst[j] + c0) = narrow<T, W>(y);
+            dst += side.yh;
         }
     }
 }
@@ -174,25 +188,33 @@ inline int rope_access(const RopeSide* side, int sides, int D, int rot, bool hal
     return 1;
 }
 
+template <typename T, bool HALVES, int W, int HEADS>
+static void launch_rope_heads(RopeArgs A, int64_t tokens, int items, cudaStream_t st) {
+    A.q_groups = (A.q.heads + HEADS - 1) / HEADS;
+    const int groups = A.q_groups + (A.k.heads + HEADS - 1) / HEADS;
+    const int64_t per_token = (int64_t)groups * items;
+    A.per_token = FastDiv((uint32_t)per_token);
+    A.items = FastDiv((uint32_t)items);
+    A.small = tokens < ((int64_t)1 << 31);
+    A.seq = FastDiv((uint32_t)A.S);
+    const int64_t most = (((int64_t)1 << 31) - kRopeThreads) / per_token;  // a launch's thread index fits 31 bits
+    for (int64_t t = 0; t < tokens; t += most) {
+        A.token0 = t;
+        A.threads = (uint32_t)((tokens - t < most ? tokens - t : most) * per_token);
+        rope_kernel<T, HALVES, W, HEADS><<<(unsigned)ceil_div(A.threads, kRopeThreads), kRopeThreads, 0, st>>>(A);
+    }
+}
+
 template <typename T, bool HALVES, int W>
 static cudaError_t launch_rope_w(RopeArgs A, int64_t tokens, cudaStream_t st) {
     constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);
-    const int heads = A.q.heads + A.k.heads;
     A.rot_items = A.rot / 2 / P;
-    A.items = A.rot_items + (A.head_dim - A.rot) / W;
+    const int items = A.rot_items + (A.head_dim - A.rot) / W;
     // Few tokens: one head per thread, the shortest chain.  Many: four, which share the table's values
     // and keep four loads (eight in halves) in flight.
-    const bool many = tokens * heads * A.items >= (int64_t)148 * 2048 * 2;
-    A.groups = many ? (heads + 3) / 4 : heads;
-    const int64_t per_token = (int64_t)A.groups * A.items;
-    const int64_t most = (((int64_t)1 << 31) - kRopeThreads) / per_token;  // the thread index is 32 bits wide
-    for (int64_t t = 0; t < tokens; t += most) {
-        A.token0 = t;
-        A.tokens = (int)(tokens - t < most ? tokens - t : most);
-        const unsigned grid = (unsigned)ceil_div((int64_t)A.tokens * per_token, kRopeThreads);
-        if (many) rope_kernel<T, HALVES, W, 4><<<grid, kRopeThreads, 0, st>>>(A);
-        else rope_kernel<T, HALVES, W, 1><<<grid, kRopeThreads, 0, st>>>(A);
-    }
+    const bool many = tokens * (A.q.heads + A.k.heads) * items >= (int64_t)148 * 2048 * 2;
+    if (many) launch_rope_heads<T, HALVES, W, 4>(A, tokens, items, st);
+    else launch_rope_heads<T, HALVES, W, 1>(A, tokens, items, st);
     return cudaGetLastError();
 }
 

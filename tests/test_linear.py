@@ -66,7 +66,7 @@ def status_ok():
 
 # sizes: one token; tiles and their edges (256 x 256 x 64); sizes that are no multiple of 8; one column;
 # long contractions (cut into pieces); many tiles
-FORWARD = [(1, 256, 256), (1, 1541, 1030), (7, 8, 8), (3, 1, 1), (16, 40, 64), (17, 255, 63), (33, 257, 65), (128, 512, 4100),
+FORWARD = [(1, 256, 256), (1, 1541, 1030), (7, 8, 8), (3, 1, 1), (16, 40, 64), (2, 100, 1537), (9, 33, 3000), (16, 9000, 40), (17, 255, 63), (33, 257, 65), (128, 512, 4100),
            (256, 256, 64), (257, 264, 200), (300, 1000, 136), (129, 768, 3000), (1021, 1541, 515), (2500, 2300, 72)]
 
 
@@ -153,7 +153,7 @@ def test_the_same_bits_every_time_and_on_another_stream():
     assert torch.equal(y, y2)
 
 
-BACKWARD = [(1, 64, 72), (1, 1541, 1030), (5, 8, 8), (2, 1, 3), (64, 256, 256), (65, 255, 130), (300, 264, 200), (1021, 515, 258), (4100, 72, 64),
+BACKWARD = [(1, 64, 72), (1, 1541, 1030), (5, 8, 8), (2, 1, 3), (3, 700, 1100), (16, 90, 2500), (17, 129, 65), (64, 256, 256), (65, 255, 130), (300, 264, 200), (1021, 515, 258), (4100, 72, 64),
             (700, 2100, 1100)]
 
 
@@ -248,8 +248,8 @@ def backward(**k):
     (dict(ldx=63), B.ERR_SHAPE), (dict(ldw=60), B.ERR_SHAPE), (dict(ldx=65), B.ERR_ALIGN), (dict(ldy=36), B.ERR_ALIGN),
     (dict(X=P + 2), B.ERR_ALIGN), (dict(Y=P + 8), B.ERR_ALIGN), (dict(bias=P + 1), B.ERR_ALIGN), (dict(R=P, ldr=31), B.ERR_SHAPE),
     (dict(R=P, ldr=33), B.ERR_ALIGN), (dict(Z=P, ldz=8), B.ERR_SHAPE), (dict(Z=P + 4, ldz=32), B.ERR_ALIGN),
-    (dict(K=6400, ldx=6400, ldw=6400), B.ERR_NULL), (dict(K=6400, ldx=6400, ldw=6400, ws=P, n=16), B.ERR_WORKSPACE),
-    (dict(K=6400, ldx=6400, ldw=6400, ws=P + 16, n=1 << 30), B.ERR_ALIGN), (dict(M=0, X=None, Y=None, W=None), B.OK)])
+    (dict(M=20, K=6400, ldx=6400, ldw=6400), B.ERR_NULL), (dict(M=20, K=6400, ldx=6400, ldw=6400, ws=P, n=16), B.ERR_WORKSPACE),
+    (dict(M=20, K=6400, ldx=6400, ldw=6400, ws=P + 16, n=1 << 30), B.ERR_ALIGN), (dict(M=0, X=None, Y=None, W=None), B.OK)])
 def test_linear_refuses(change, status):
     assert linear(**change) == status
 
@@ -266,7 +266,7 @@ def test_backward_refuses(change, status):
 def test_sizes_of_workspaces():
     assert B.dvdq_linear_workspace_bytes(0, 64, 64) == 0 and B.dvdq_linear_workspace_bytes(-1, 64, 64) == 0
     assert B.dvdq_linear_workspace_bytes(32760, 1536, 1536) == 0          # more tiles than CTA pairs: nothing is cut
-    n = B.dvdq_linear_workspace_bytes(10, 32, 6400)
+    n = B.dvdq_linear_workspace_bytes(20, 32, 6400)
     assert n > 0 and n % 256 == 0
     a, b = (B.dvdq_linear_backward_workspace_bytes(1000, 512, 512, k) for k in (0, 1))
     assert b >= a + 1000 * 512 * 2
