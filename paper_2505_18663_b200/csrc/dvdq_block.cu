@@ -89,9 +89,9 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
         auto k = act == DVDQ_ACT_GELU_TANH ? linear_dz_kernel<T, DVDQ_ACT_GELU_TANH>
                  : act == DVDQ_ACT_SILU    ? linear_dz_kernel<T, DVDQ_ACT_SILU>
                                            : linear_dz_kernel<T, DVDQ_ACT_NONE>;
-        k<<<grid, kStreamThreads, 0, st>>>(static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p), z.ld, M, (int)N, p.rows,
-                                          static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, sums);
-        if ((s = cuda_status(cudaGetLastError())) != DVDQ_OK) return s;
+        if ((s = cuda_status(launch_after(k, grid, dim3(kStreamThreads), 0, st, static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p),
+                                          z.ld, M, (int)N, p.rows, static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, sums))) != DVDQ_OK)
+            return s;
         if (db && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
                                                 (int)N, db))) != DVDQ_OK)
             return s;

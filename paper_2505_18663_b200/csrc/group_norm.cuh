@@ -155,6 +155,8 @@ constexpr int kGnDepth = 8, kGnGradDepth = 5;  // slots: 32 KB a CTA, 40 KB for 
 template <typename T, int V>
 __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
+    release_successor();
+    wait_predecessor();
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
     Pairs<V> s1, s2;
@@ -183,7 +185,6 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_co
     }
     __syncthreads();  // the ring's memory becomes the sums'
     gn_reduce_block<V, false>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
-    release_successor();
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -203,6 +204,7 @@ template <bool BACKWARD>
 __global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_constant__ GnArgs A, int group_ctas) {
     constexpr int kWarps = kGnThreads / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    release_successor();
     wait_predecessor();
     if ((int)blockIdx.x < group_ctas) {
         const int64_t ng = (int64_t)blockIdx.x * kWarps + warp;
@@ -294,6 +296,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
     extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
+    release_successor();
     wait_predecessor();
     if (!P.on) return;
     float mu[V], ga[V], be[V];
@@ -355,6 +358,8 @@ __device__ __forceinline__ GnGrad<T, V> gn_constants(const GnArgs& A, int n, int
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 4) gn_grad_stats_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
+    release_successor();
+    wait_predecessor();
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
     Pairs<V> s1, s2;
@@ -379,7 +384,6 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_grad_stats_kernel(const __gr
     }
     __syncthreads();  // the ring's memory becomes the sums'
     gn_reduce_block<V, true>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
-    release_successor();
 }
 
 // dx = rstd (gamma dz - m1 - h m2) = dz (rstd gamma) + (h (-rstd m2) + (-rstd m1))
@@ -406,6 +410,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __gr
     extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
+    release_successor();
     wait_predecessor();
     if (!P.on) return;
     float rs[V], ga[V], m1[V], m2[V];
@@ -470,6 +475,7 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     const float inv = 1.0f / ((float)S * A.per);
     const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
     float s1[V], pv[V];
+    release_successor();
     wait_predecessor();
     if (on) {
 #pragma unroll
@@ -547,6 +553,7 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
     float2* gsum = sums + width;            // per group
     double dgamma = 0.0, dbeta = 0.0;       // of channel cbase + threadIdx.x
     const float inv = 1.0f / ((float)S * A.per);
+    release_successor();
     wait_predecessor();
     for (int n = 0; n < A.N; ++n) {
         float rs[V], ga[V];
@@ -756,13 +763,11 @@ static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
     static_assert(one <= 48 * 1024 && two <= 48 * 1024 && sums <= 48 * 1024, "more than a kernel has without asking");
     cudaError_t e;
     if (!backward) {
-        gn_stats_kernel<T, V><<<grid, kGnThreads, sums > one ? sums : one, st>>>(A);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if ((e = launch_after(gn_stats_kernel<T, V>, grid, dim3(kGnThreads), sums > one ? sums : one, st, A)) != cudaSuccess) return e;
         if ((e = launch_after(gn_join_kernel<false>, dim3(group_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess) return e;
         return launch_after(gn_apply_kernel<T, V, ACT>, grid, dim3(kGnThreads), one, st, A);
     }
-    gn_grad_stats_kernel<T, V, ACT><<<grid, kGnThreads, sums > two ? sums : two, st>>>(A);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_after(gn_grad_stats_kernel<T, V, ACT>, grid, dim3(kGnThreads), sums > two ? sums : two, st, A)) != cudaSuccess) return e;
     const unsigned channel_ctas = A.dgamma || A.dbeta ? (unsigned)ceil_div(A.C, 32) : 0;
     if ((e = launch_after(gn_join_kernel<true>, dim3(group_ctas + channel_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess)
         return e;

@@ -35,7 +35,8 @@ enum LinOut { kLinFinal = 0, kLinFinalZ = 1, kLinPartial = 2 };
 
 template <int OUT>
 struct LinSmem {
-    // storing z as well takes a third output block per epilogue warp, and a stage less
+    // storing z as well takes a third output block per epilogue warp, and a stage less.  (More stages
+    // for narrow tiles, whose stages are smaller, changed nothing.)
     static constexpr int kStages = OUT == kLinFinalZ ? 5 : 6;
     static constexpr int kBufs = OUT == kLinFinalZ ? 3 : 2;
     static constexpr int kOperand = 128 * kLinBK * 2;       // one CTA's half of an operand's stage
@@ -57,7 +58,7 @@ struct LinArgs {
     int kblocks, splits;    // k-blocks of the contraction, pieces it is cut into
     int panel;              // column tiles walked together
     int part_rows;          // rows of one piece in the partial buffer
-    int act, has_residual, has_z;
+    int act, has_residual;
     const void* bias;
 };
 
@@ -116,7 +117,7 @@ __device__ __forceinline__ void lin_load(uint32_t dst, const CUtensorMap* m, uin
     }
 }
 template <bool MN>
-__device__ __forceinline__ uint32_t lin_bytes(int width) { return (uint32_t)(MN ? (width + 63) / 64 * (kLinBK * 128) : width * kLinBK * 2); }
+__host__ __device__ constexpr uint32_t lin_bytes(int width) { return (uint32_t)(MN ? (width + 63) / 64 * (kLinBK * 128) : width * kLinBK * 2); }
 
 template <typename T, bool AMN, bool BMN, int OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
@@ -159,6 +160,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem_base = misc[0];
+    release_successor();
     wait_predecessor();
 
     if (warp == 0) {
@@ -368,7 +370,6 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 
     tc_fence_before();
     __syncthreads();
-    release_successor();
     cluster_sync_all();
     if (warp == 1) tmem_dealloc(tmem_base, 512);
 }
@@ -380,6 +381,7 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pitch, int splits, int64_t Md, int Nd, const T* __restrict__ bias,
                    const T* residual, int64_t ldr, int act, T* y, int64_t ldy, T* z, int64_t ldz) {
+    release_successor();
     wait_predecessor();
     const int quads = (Nd + 3) >> 2;
     const int64_t total = Md * quads;
@@ -434,6 +436,8 @@ __global__ void __launch_bounds__(kStreamThreads, 4)
 linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, int64_t M, int N, int64_t rows,
                  T* __restrict__ dz, int64_t lddz, float* __restrict__ sums) {
     constexpr bool kAct = ACT != DVDQ_ACT_NONE;
+    release_successor();
+    wait_predecessor();
     __shared__ __align__(16) uint8_t raw[kStreamThreads * 16 * kLinDzDepth * (kAct ? 2 : 1)];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
     const int n = blockIdx.x * kLinDzCols + tx * 8;
@@ -494,10 +498,10 @@ linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z
             sums[(int64_t)blockIdx.y * N + c] = t;
         }
     }
-    release_successor();
 }
 
 __global__ void __launch_bounds__(256) linear_colsum_kernel(const float* __restrict__ sums, int chunks, int N, float* __restrict__ out) {
+    release_successor();
     wait_predecessor();
     __shared__ double sh[8][33];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -512,7 +516,6 @@ __global__ void __launch_bounds__(256) linear_colsum_kernel(const float* __restr
         for (int y = 1; y < 8; ++y) t += sh[y][lane];
         out[c] = (float)t;
     }
-    release_successor();
 }
 
 // ------------------------------------------------------------------ host side
@@ -522,11 +525,13 @@ struct LinPlan {
     int64_t part_rows, part_pitch, part_bytes;
 };
 
-// Tile width and pieces along k, from the sizes alone, by an estimate in microseconds fitted to measurements: a k-block of a
-// 256-row tile takes a pair 0.37 us per 256 columns of products, but at least the time to bring its operands from L2 (about
-// 240 GB/s per pair); a tile's epilogue 0.5 + 2 us per 256 columns, hidden under the next tile's products if there is one; 2 us
-// to fill the ring.  Pieces cost a second launch (3.5 us) and writing and reading their fp32 sums (about 5 TB/s).
-// `step`: 32, or 64 where B is MN-major (its shared-memory tiles are 64 columns wide).
+// Tile width and pieces along k, from the sizes alone, by an estimate in microseconds fitted to measurements
+// (M x N x K = 509 x 5120 x 4096, 32760 x 1536 x 1536, 4096^3, 200 x 3072 x 3072, every width, 1 to 4 pieces): a
+// k-block of a 256-row tile takes a pair 0.345 us per 256 columns of products, but at least 0.21 us + 0.37 ns per column to
+// bring its operands from L2 (about 50 bytes a clock per SM); a tile's epilogue 0.5 + 2 us per 256 columns, hidden under
+// the next tile's products if there is one; 2 us to fill the ring.  Pieces cost a second launch (2.5 us) and writing and
+// reading their fp32 sums in L2 (about 8 TB/s).  `step`: 32, or 64 where B is MN-major (its shared-memory tiles
+// are 64 columns wide).
 inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
     const int64_t kb = ceil_div(Kc, kLinBK), num_m = ceil_div(Md, kLinTile);
     LinPlan p;
@@ -537,13 +542,13 @@ inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
     double best = 1e300;
     for (int bn = kLinTile; bn >= 32 && bn % step == 0; bn -= step) {
         const int64_t tiles = num_m * ceil_div(Nd, bn);
-        const double products = 0.37 * bn / 256.0, feed = (256.0 + bn) * 128.0 / 240e3;
+        const double products = 0.345 * bn / 256.0, feed = 0.21 + 0.00037 * bn;
         const double t_kb = products > feed ? products : feed, t_epi = 0.5 + 2.0 * bn / 256.0;
         for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
             if (s > 1 && (tiles * s > 4 * kLinPairs || s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20))) break;
             const double item = (double)ceil_div(kb, s) * t_kb;
             double cost = (double)ceil_div(tiles * s, kLinPairs) * (item > t_epi ? item : t_epi) + 2.0 + t_epi;
-            if (s > 1) cost += 3.5 + (double)s * Md * Nd * 8.0 / 5.0e6;
+            if (s > 1) cost += 2.5 + (double)s * Md * Nd * 8.0 / 8.0e6;
             if (cost < best * 0.97) { best = cost; p.bn = bn; p.splits = (int)s; }  // a wider tile reads less: prefer it when near
         }
     }
@@ -615,7 +620,6 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
     A.part_rows = (int)plan.part_rows;
     A.act = e.act;
     A.has_residual = fin && e.residual.p != nullptr;
-    A.has_z = OUT == kLinFinalZ;
     A.bias = fin ? e.bias : nullptr;
     auto kern = linear_kernel<T, AMN, BMN, OUT>;
     static PerDevice<int> cache;

@@ -48,6 +48,7 @@ linear_few_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ W,
     __shared__ float sh[WARPS][MT * 8][16];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int n0 = blockIdx.x * 16;
+    release_successor();
     wait_predecessor();
     // rows past N repeat the last one: their results are not stored
     const T* w0 = W + (int64_t)min(n0 + g, N - 1) * ldw;
@@ -132,6 +133,7 @@ linear_few_dx_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[m].p[i] = 0ull;
+    release_successor();
     wait_predecessor();
     for (int nb = n0; nb < n1; nb += kFewRows) {
         __syncthreads();
@@ -179,6 +181,7 @@ __global__ void __launch_bounds__(256) linear_few_join_kernel(const float* __res
     __shared__ float sh[8][33];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, k = blockIdx.x * 32 + lane, m = blockIdx.y;
     const int64_t pitch = align_up(K, 8), step = (int64_t)M * pitch;
+    release_successor();
     wait_predecessor();
     float t = 0.f;
     if (k < K) {
@@ -202,6 +205,7 @@ linear_few_dw_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict
                      int M, int N, int K, T* __restrict__ dW, int64_t lddw, float* __restrict__ db) {
     __shared__ float dz[kFewRows][MT];
     const int k = blockIdx.y * kFewCols + threadIdx.x * 8, n0 = blockIdx.x * kFewRows, here = min(kFewRows, N - n0);
+    release_successor();
     wait_predecessor();
     for (int i = threadIdx.x; i < kFewRows * MT; i += 128) {
         const int n = n0 + i / MT, m = i % MT;

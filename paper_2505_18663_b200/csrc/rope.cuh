@@ -78,6 +78,8 @@ template <typename T, bool HALVES, int W, int HEADS>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs A) {
     constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);
     constexpr bool TWO = HALVES || W == 1;  // a rotating item is two accesses
+    release_successor();
+    wait_predecessor();
     const uint32_t idx = blockIdx.x * (uint32_t)kRopeThreads + threadIdx.x;
     if (idx >= A.threads) return;
     const uint32_t lt = A.per_token(idx), rem = idx - lt * A.per_token.d;
@@ -189,7 +191,7 @@ inline int rope_access(const RopeSide* side, int sides, int D, int rot, bool hal
 }
 
 template <typename T, bool HALVES, int W, int HEADS>
-static void launch_rope_heads(RopeArgs A, int64_t tokens, int items, cudaStream_t st) {
+static cudaError_t launch_rope_heads(RopeArgs A, int64_t tokens, int items, cudaStream_t st) {
     A.q_groups = (A.q.heads + HEADS - 1) / HEADS;
     const int groups = A.q_groups + (A.k.heads + HEADS - 1) / HEADS;
     const int64_t per_token = (int64_t)groups * items;
@@ -201,8 +203,10 @@ static void launch_rope_heads(RopeArgs A, int64_t tokens, int items, cudaStream_
     for (int64_t t = 0; t < tokens; t += most) {
         A.token0 = t;
         A.threads = (uint32_t)((tokens - t < most ? tokens - t : most) * per_token);
-        rope_kernel<T, HALVES, W, HEADS><<<(unsigned)ceil_div(A.threads, kRopeThreads), kRopeThreads, 0, st>>>(A);
+        const cudaError_t e = launch_after(rope_kernel<T, HALVES, W, HEADS>, dim3((unsigned)ceil_div(A.threads, kRopeThreads)), dim3(kRopeThreads), 0, st, A);
+        if (e != cudaSuccess) return e;
     }
+    return cudaSuccess;
 }
 
 template <typename T, bool HALVES, int W>
@@ -213,9 +217,7 @@ static cudaError_t launch_rope_w(RopeArgs A, int64_t tokens, cudaStream_t st) {
     // Few tokens: one head per thread, the shortest chain.  Many: four, which share the table's values
     // and keep four loads (eight in halves) in flight.
     const bool many = tokens * (A.q.heads + A.k.heads) * items >= (int64_t)148 * 2048 * 2;
-    if (many) launch_rope_heads<T, HALVES, W, 4>(A, tokens, items, st);
-    else launch_rope_heads<T, HALVES, W, 1>(A, tokens, items, st);
-    return cudaGetLastError();
+    return many ? launch_rope_heads<T, HALVES, W, 4>(A, tokens, items, st) : launch_rope_heads<T, HALVES, W, 1>(A, tokens, items, st);
 }
 
 template <typename T, bool HALVES>
