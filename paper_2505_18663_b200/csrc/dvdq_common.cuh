@@ -69,7 +69,7 @@ static __device__ uint32_t g_device_status[2] = {0u, 0u};
 
 enum WaitId : uint32_t {
     kWaitPackedEmpty = 1, kWaitPackedFull = 2, kWaitWideEmpty = 3, kWaitWideFull = 4,
-    kWaitAccEmpty = 5, kWaitAccFull = 6, kWaitDrain = 7, kWaitDebug = 8
+    kWaitAccEmpty = 5, kWaitAccFull = 6, kWaitDrain = 7, kWaitDebug = 8, kWaitMeet = 9
 };
 constexpr uint32_t kDetailRopeRow = 16;  // DVDQ_ERR_SHAPE: a position's row is outside the table
 

@@ -8,13 +8,15 @@
 // before its first output, so a tensor larger than the chip's shared memory is read twice; the
 // second pass walks every chunk backwards, so that it begins with what the L2 cache still holds.
 //
-// Large tensors, three launches.  Pass 1: a CTA sums one chunk of places of one sample over all channels (a
-// thread keeps its 16 bytes of channels, so its loads are whole sectors) and writes two numbers per
-// group.  Join: a warp per group adds up its chunks in a fixed order (no atomics: the same bits every
-// time); backward, the channels' sums over samples and chunks as well.  Pass 2 streams the chunks.
-// Join and pass 2 are launched while their predecessor drains.  Sums are of x minus a value of the
-// group itself (the first place's first channel), so that a mean far from zero costs no digits, in
-// fp32 within a chunk and in fp64 across chunks.
+// Large tensors, one cooperative launch of one CTA per SM: pass 1 sums a chunk of places of one sample over
+// all channels (a thread keeps its 16 bytes of channels, so its loads are whole sectors) and writes two
+// numbers per group; all CTAs meet once; every CTA adds up its sample's numbers in a fixed order (no
+// atomics on data: the same bits every time); pass 2 walks the chunk backwards, first the pieces that pass 1
+// left in shared memory (about 20 MB over the chip), then what the L2 cache still holds.  Sums
+// are of x minus a value of the group itself (the first place's first channel), so that a mean far from
+// zero costs no digits, in fp32 within a chunk and in fp64 across chunks.
+// Where that does not fit (channels that 16 bytes do not divide, more than 4096 of them, sample counts that
+// leave SMs idle): three launches, pass 1, join, pass 2, each started while its predecessor drains.
 // Small tensors, one launch: where a slice of whole groups of one sample fits a CTA's shared memory,
 // the CTA reads it once, and does both passes on it.
 #pragma once
@@ -40,6 +42,7 @@ struct GnArgs {
     float* pivot;            // [N, G]: what pass 1 subtracted (y may be x: pass 2 cannot read it there)
     float2* part_c;          // backward: [N, chunks, C]
     float2* stat;            // [N, G]: (mean, rstd) forward, (<dh>, <dh h>) backward
+    uint32_t* arrived;       // one-launch kernels: CTAs that have written their numbers
     int64_t xn, xs, dn, ds, yn, ys;  // pitches of samples and places, elements
     int64_t S;
     int N, C, G, per;        // per = C / G
@@ -273,6 +276,27 @@ __global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_consta
     }
 }
 
+// Calls get(i, group of channel c0 + i) for V channels; where they all lie in one group, once, and copy(i) for the rest.
+template <int V, typename Get, typename Copy>
+__device__ __forceinline__ void gn_by_channel(int per, int c0, Get get, Copy copy) {
+    if (per % V == 0) {
+        get(0, c0 / per);
+#pragma unroll
+        for (int i = 1; i < V; ++i) copy(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) get(i, (c0 + i) / per);
+    }
+}
+template <int V>
+__device__ __forceinline__ void gn_params(const GnArgs& A, int c0, float (&ga)[V], float (&be)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        ga[i] = gn_param(A.gamma, A.params_f32, A.params_bf16, c0 + i, 1.0f);
+        be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, c0 + i, 0.0f);
+    }
+}
+
 // z = (x - mean) a + beta with a = gamma rstd.  For 16-bit x the mean goes into the constant (x a + (beta -
 // mean a): the constant's rounding, 2^-24 |mean| a, is far below x's own step); fp32 x subtracts first.
 template <typename T, int V>
@@ -291,6 +315,18 @@ struct GnScale {
     }
 };
 
+// ... from the groups' (mean, rstd)
+template <typename T, int V>
+__device__ __forceinline__ GnScale<T, V> gn_scale(const GnArgs& A, int c0, const float2* stat) {
+    float mu[V], rs[V], ga[V], be[V];
+    gn_by_channel<V>(A.per, c0, [&](int i, int g) { const float2 t = stat[g]; mu[i] = t.x; rs[i] = t.y; },
+                     [&](int i) { mu[i] = mu[0]; rs[i] = rs[0]; });
+    gn_params<V>(A, c0, ga, be);
+#pragma unroll
+    for (int i = 0; i < V; ++i) ga[i] *= rs[i];
+    return GnScale<T, V>(mu, ga, be);
+}
+
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
@@ -299,15 +335,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
     release_successor();
     wait_predecessor();
     if (!P.on) return;
-    float mu[V], ga[V], be[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 t = A.stat[(int64_t)n * A.G + (P.c0 + i) / A.per];
-        mu[i] = t.x;
-        ga[i] = t.y * gn_param(A.gamma, A.params_f32, A.params_bf16, P.c0 + i, 1.0f);
-        be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, P.c0 + i, 0.0f);
-    }
-    const GnScale<T, V> scale(mu, ga, be);
+    const float2* stat = A.stat + (int64_t)n * A.G;
+    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, stat);
     // backwards: from the place pass 1 read last
     const int count = P.count(A.lanes);
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
@@ -340,15 +369,11 @@ struct GnGrad {
 template <typename T, int V>
 __device__ __forceinline__ GnGrad<T, V> gn_constants(const GnArgs& A, int n, int c0, float (&rs)[V], float (&ga)[V]) {
     float mu[V], be[V], none[V];
+    gn_by_channel<V>(A.per, c0, [&](int i, int g) { mu[i] = A.mean[(int64_t)n * A.G + g]; rs[i] = A.rstd[(int64_t)n * A.G + g]; },
+                     [&](int i) { mu[i] = mu[0]; rs[i] = rs[0]; });
+    gn_params<V>(A, c0, ga, be);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int64_t g = (int64_t)n * A.G + (c0 + i) / A.per;
-        mu[i] = A.mean[g];
-        rs[i] = A.rstd[g];
-        ga[i] = gn_param(A.gamma, A.params_f32, A.params_bf16, c0 + i, 1.0f);
-        be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, c0 + i, 0.0f);
-        none[i] = 0.f;
-    }
+    for (int i = 0; i < V; ++i) none[i] = 0.f;
     GnGrad<T, V> r{GnScale<T, V>(mu, rs, none), {}, {}};
     r.gamma.set(ga);
     r.beta.set(be);
@@ -405,6 +430,15 @@ struct GnDx {
     __device__ __forceinline__ uint64_t operator()(uint64_t dz, uint64_t h, int i) const { return f2_fma(dz, c1.p[i], f2_fma(h, c2.p[i], c3.p[i])); }
 };
 
+// ... from the groups' (<dh>, <dh h>)
+template <int V>
+__device__ __forceinline__ GnDx<V> gn_dx(const GnArgs& A, int c0, const float2* stat, const float (&rs)[V], const float (&ga)[V]) {
+    float m1[V], m2[V];
+    gn_by_channel<V>(A.per, c0, [&](int i, int g) { const float2 t = stat[g]; m1[i] = t.x; m2[i] = t.y; },
+                     [&](int i) { m1[i] = m1[0]; m2[i] = m2[0]; });
+    return GnDx<V>(rs, ga, m1, m2);
+}
+
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
@@ -413,15 +447,9 @@ __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __gr
     release_successor();
     wait_predecessor();
     if (!P.on) return;
-    float rs[V], ga[V], m1[V], m2[V];
+    float rs[V], ga[V];
     const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 t = A.stat[(int64_t)n * A.G + (P.c0 + i) / A.per];
-        m1[i] = t.x;
-        m2[i] = t.y;
-    }
-    const GnDx<V> dx(rs, ga, m1, m2);
+    const GnDx<V> dx = gn_dx<V>(A, P.c0, A.stat + (int64_t)n * A.G, rs, ga);
     const int count = P.count(A.lanes);
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
     T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + P.c0 + last * A.ys;
@@ -440,6 +468,325 @@ __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __gr
         store_streaming<T, V>(q, narrow2<T, V>(o));
         q += back;
     });
+}
+
+// ------------------------------------------------------------------ large tensors: one cooperative launch
+
+// Threads, and slots of the ring: it and the sums fill the shared memory of an SM.
+constexpr int kGnFusedThreads = 1024, kGnFusedDepth = 9, kGnFusedGradThreads = 512, kGnFusedGradDepth = 10, kGnFusedGroups = 1024;
+
+// Both passes of one thread over its pieces.  forward(): as thread_stream, and the last D pieces stay in the ring;
+// backward(): from the last piece to the first, those D from where they are, the rest through the ring again.
+template <int D, int STREAMS, int THREADS, typename T, int V>
+struct TwoWay {
+    static constexpr uint32_t kSlot = THREADS * 16, kPiece = STREAMS * kSlot;
+    uint32_t ring, zero;
+    int count;
+    const T *at0, *at1;      // next piece to fetch
+    int64_t step0, step1;
+    __device__ __forceinline__ void fill(uint32_t slot, uint32_t dep) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + dep), "l"(at0) : "memory");
+        if constexpr (STREAMS == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + kSlot + dep), "l"(at1) : "memory");
+    }
+    __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory"); }
+    // hands the slot's pieces to use(); the value returned is zero, but known only when they have been delivered
+    template <typename Use>
+    __device__ __forceinline__ uint32_t take(uint32_t slot, Use& use) {
+        union { uint4 w; Vec<T, V> v; } in[STREAMS];
+        uint32_t dep = 0u;
+#pragma unroll
+        for (int j = 0; j < STREAMS; ++j) {
+            in[j].w = lds128(ring + slot * kPiece + j * kSlot);
+            dep ^= in[j].w.w;
+        }
+        if constexpr (STREAMS == 1) use(in[0].v);
+        else use(in[0].v, in[1].v);
+        return dep & zero;
+    }
+    __device__ __forceinline__ TwoWay(const uint8_t* raw, int n, const T* from0, int64_t s0, const T* from1, int64_t s1)
+        : ring(smem_u32(raw) + threadIdx.x * 16), count(n), at0(from0), at1(from1), step0(s0), step1(s1) {
+        asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
+        zero -= 1u;
+    }
+    template <typename Use>
+    __device__ __forceinline__ void forward(Use use) {
+        auto next = [&](uint32_t slot, int k, uint32_t dep) {
+            if (k < count) {
+                fill(slot, dep);
+                at0 += step0;
+                if (STREAMS == 2) at1 += step1;
+            }
+            commit();
+        };
+#pragma unroll
+        for (int k = 0; k < D - 1; ++k) next((uint32_t)k, k, 0u);
+        uint32_t slot = 0, behind = D - 1, dep = 0u;
+        for (int k = 0; k < count; ++k) {
+            next(behind, k + D - 1, dep);
+            wait();
+            dep = take(slot, use);
+            behind = slot;
+            slot = slot + 1 == D ? 0u : slot + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    template <typename Use>
+    __device__ __forceinline__ void backward(Use use) {
+        if (count == 0) return;
+        // piece k is in slot k % D; at0 stands one past the last piece
+        uint32_t slot = (uint32_t)((count - 1) % D);
+        at0 -= (int64_t)(D + 1) * step0;  // piece count - 1 - D
+        if (STREAMS == 2) at1 -= (int64_t)(D + 1) * step1;
+        for (int k = count - 1; k >= 0; --k) {
+            wait();
+            const uint32_t dep = take(slot, use);
+            if (k >= D) {
+                fill(slot, dep);
+                at0 -= step0;
+                if (STREAMS == 2) at1 -= step1;
+            }
+            commit();
+            slot = slot == 0 ? D - 1 : slot - 1;
+        }
+    }
+};
+
+// The CTA's place: sample n, chunk j of `chunks`.
+template <int V, int THREADS>
+struct GnTeam {
+    int n, j, v, c0, r, lanes, count;
+    int64_t s0;
+    bool on;
+    __device__ __forceinline__ GnTeam(const GnArgs& A) {
+        n = blockIdx.x / A.chunks;
+        j = blockIdx.x - n * A.chunks;
+        lanes = THREADS / A.vecs;
+        v = threadIdx.x % A.vecs;
+        r = threadIdx.x / A.vecs;
+        c0 = v * V;
+        on = r < lanes;
+        s0 = (int64_t)j * A.rows + r;
+        const int64_t s1 = min((int64_t)(j + 1) * A.rows, A.S);
+        count = on && s0 < s1 ? (int)((s1 - s0 + lanes - 1) / lanes) : 0;
+    }
+};
+
+// Adds the threads' sums over the lanes, then over each group's channels, and writes the CTA's numbers.
+// Channel i of vector v of lane r lies at [r][i][v]: neighbouring threads write neighbouring words.
+template <int V, int THREADS, bool PER_CHANNEL>
+__device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, THREADS>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
+    if (P.on) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) sh[(P.r * V + i) * A.vecs + P.v] = make_float2(s1.get(i), s2.get(i));
+    }
+    __syncthreads();
+    for (int o = threadIdx.x; o < A.C; o += THREADS) {  // o = i * vecs + v
+        float2 t = sh[o];
+        for (int l = 1; l < P.lanes; ++l) {
+            const float2 u = sh[l * A.C + o];
+            t.x += u.x;
+            t.y += u.y;
+        }
+        if (PER_CHANNEL) {
+            const int i = o / A.vecs, c = (o - i * A.vecs) * V + i;
+            A.part_c[(int64_t)blockIdx.x * A.C + c] = t;
+            const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
+            t.x *= g;
+            t.y *= g;
+        }
+        sh[o] = t;
+    }
+    __syncthreads();
+    float2* out = A.part + (int64_t)blockIdx.x * A.G;
+    auto channel = [&](int c) { return sh[(c % V) * A.vecs + c / V]; };
+    if (A.per <= 8) {
+        for (int g = threadIdx.x; g < A.G; g += THREADS) {
+            float2 t = channel(g * A.per);
+            for (int i = 1; i < A.per; ++i) {
+                const float2 u = channel(g * A.per + i);
+                t.x += u.x;
+                t.y += u.y;
+            }
+            out[g] = t;
+        }
+    } else {
+        for (int g = threadIdx.x >> 5; g < A.G; g += THREADS / 32) {
+            float2 t = make_float2(0.f, 0.f);
+            for (int i = threadIdx.x & 31; i < A.per; i += 32) {
+                const float2 u = channel(g * A.per + i);
+                t.x += u.x;
+                t.y += u.y;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
+                t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
+            }
+            if ((threadIdx.x & 31) == 0) out[g] = t;
+        }
+    }
+}
+
+// All CTAs of the (cooperative, hence co-resident) launch meet: what each wrote before is seen by all after.
+// A wait that runs out is reported and left, as every wait of the library.
+__device__ __forceinline__ void gn_meet(uint32_t* arrived) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
+        uint64_t t0 = 0;
+        for (uint32_t it = 1;; ++it) {
+            uint32_t v;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(arrived) : "memory");
+            if (v >= gridDim.x) break;
+            if ((it & 0x3FFu) == 0u) {
+                const uint64_t now = global_timer_ns();
+                if (t0 == 0) t0 = now;
+                if (now - t0 > kWaitLimitNs) {
+                    report_timeout(kWaitMeet);
+                    break;
+                }
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// The sample's numbers, a warp per group: stat[g] = finish(g, mean of the first, mean of the second).
+template <int THREADS, typename Finish>
+__device__ __forceinline__ void gn_team_join(const GnArgs& A, int n, float2* stat, Finish finish) {
+    const int lane = threadIdx.x & 31;
+    const double count = (double)A.S * A.per;
+    for (int g = threadIdx.x >> 5; g < A.G; g += THREADS / 32) {
+        const float2* base = A.part + (int64_t)n * A.chunks * A.G + g;
+        double a = 0.0, b = 0.0;
+#pragma unroll 5
+        for (int i = lane; i < A.chunks; i += 32) {
+            const float2 t = __ldcg(base + (int64_t)i * A.G);
+            a += t.x;
+            b += t.y;
+        }
+        a = warp_sum(a) / count;
+        b = warp_sum(b) / count;
+        if (lane == 0) stat[g] = finish(g, a, b);
+    }
+    __syncthreads();
+}
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __grid_constant__ GnArgs A) {
+    constexpr int THREADS = kGnFusedThreads, D = kGnFusedDepth;
+    extern __shared__ __align__(16) uint8_t raw[];
+    float2* sums = reinterpret_cast<float2*>(raw + THREADS * 16 * D);
+    __shared__ float pivots[kGnFusedGroups];  // y may be x: what was subtracted is kept
+    const GnTeam<V, THREADS> P(A);
+    const T* x = static_cast<const T*>(A.x) + (int64_t)P.n * A.xn;
+    for (int g = threadIdx.x; g < A.G; g += THREADS) pivots[g] = to_f32(x[g * A.per]);
+    __syncthreads();
+    TwoWay<D, 1, THREADS, T, V> walk(raw, P.count, x + P.c0 + P.s0 * A.xs, P.lanes * A.xs, nullptr, 0);
+    {
+        Pairs<V> s1, s2, pivot;
+        float pv[V];
+        gn_by_channel<V>(A.per, P.c0, [&](int i, int g) { pv[i] = pivots[g]; }, [&](int i) { pv[i] = pv[0]; });
+        pivot.set(pv);
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
+        walk.forward([&](const Vec<T, V>& in) {
+            const Pairs<V> f = widen2<T, V>(in);
+#pragma unroll
+            for (int i = 0; i < Pairs<V>::N; ++i) {
+                const uint64_t d = f2_sub(f.p[i], pivot.p[i]);
+                s1.p[i] = f2_add(s1.p[i], d);
+                s2.p[i] = f2_fma(d, d, s2.p[i]);
+            }
+        });
+        gn_team_sums<V, THREADS, false>(A, P, s1, s2, sums);
+    }
+    gn_meet(A.arrived);
+    gn_team_join<THREADS>(A, P.n, sums, [&](int g, double m1, double m2) {
+        const float2 t = gn_mean_rstd((double)pivots[g], m1, m2, A.eps);
+        if (P.j == 0 && A.mean) A.mean[(int64_t)P.n * A.G + g] = t.x;
+        if (P.j == 0 && A.rstd) A.rstd[(int64_t)P.n * A.G + g] = t.y;
+        return t;
+    });
+    if (!P.on) return;
+    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, sums);
+    T* q = static_cast<T*>(A.y) + (int64_t)P.n * A.yn + P.c0 + (P.s0 + (int64_t)(P.count - 1) * P.lanes) * A.ys;
+    const int64_t back = -(int64_t)P.lanes * A.ys;
+    walk.backward([&](const Vec<T, V>& in) {
+        const Pairs<V> f = widen2<T, V>(in);
+        Pairs<V> o;
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT>(scale(f.p[i], i));
+        store_streaming<T, V>(q, narrow2<T, V>(o));
+        q += back;
+    });
+}
+
+template <typename T, int V, int ACT>
+__global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(const __grid_constant__ GnArgs A) {
+    constexpr int THREADS = kGnFusedGradThreads, D = kGnFusedGradDepth;
+    extern __shared__ __align__(16) uint8_t raw[];
+    float2* sums = reinterpret_cast<float2*>(raw + THREADS * 32 * D);
+    const GnTeam<V, THREADS> P(A);
+    float rs[V], ga[V];
+    const GnGrad<T, V> K = gn_constants<T, V>(A, P.n, P.c0, rs, ga);
+    TwoWay<D, 2, THREADS, T, V> walk(raw, P.count, static_cast<const T*>(A.x) + (int64_t)P.n * A.xn + P.c0 + P.s0 * A.xs, P.lanes * A.xs,
+                                     static_cast<const T*>(A.dy) + (int64_t)P.n * A.dn + P.c0 + P.s0 * A.ds, P.lanes * A.ds);
+    {
+        Pairs<V> s1, s2;
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
+        walk.forward([&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
+            const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
+#pragma unroll
+            for (int i = 0; i < Pairs<V>::N; ++i) {
+                uint64_t dz, h;
+                K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+                s1.p[i] = f2_add(s1.p[i], dz);
+                s2.p[i] = f2_fma(dz, h, s2.p[i]);
+            }
+        });
+        gn_team_sums<V, THREADS, true>(A, P, s1, s2, sums);
+    }
+    gn_meet(A.arrived);
+    gn_team_join<THREADS>(A, P.n, sums, [](int, double m1, double m2) { return make_float2((float)m1, (float)m2); });
+    if (P.on && A.y) {
+        const GnDx<V> dx = gn_dx<V>(A, P.c0, sums, rs, ga);
+        T* q = static_cast<T*>(A.y) + (int64_t)P.n * A.yn + P.c0 + (P.s0 + (int64_t)(P.count - 1) * P.lanes) * A.ys;
+        const int64_t back = -(int64_t)P.lanes * A.ys;
+        walk.backward([&](const Vec<T, V>& xv, const Vec<T, V>& dv) {
+            const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
+            Pairs<V> o;
+#pragma unroll
+            for (int i = 0; i < Pairs<V>::N; ++i) {
+                uint64_t dz, h;
+                K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+                o.p[i] = dx(dz, h, i);
+            }
+            store_streaming<T, V>(q, narrow2<T, V>(o));
+            q += back;
+        });
+    }
+    if (!A.dgamma && !A.dbeta) return;
+    // the parameters' gradients: a warp per channel, the channels dealt out over the CTAs
+    const int lane = threadIdx.x & 31, ctas = (int)gridDim.x;
+    for (int c = (threadIdx.x >> 5) * ctas + blockIdx.x; c < A.C; c += ctas * (THREADS / 32)) {
+        double a = 0.0, b = 0.0;
+#pragma unroll 5
+        for (int i = lane; i < ctas; i += 32) {
+            const float2 t = __ldcg(A.part_c + (int64_t)i * A.C + c);
+            a += t.x;
+            b += t.y;
+        }
+        a = warp_sum(a);
+        b = warp_sum(b);
+        if (lane == 0) {
+            if (A.dbeta) A.dbeta[c] = (float)a;
+            if (A.dgamma) A.dgamma[c] = (float)b;
+        }
+    }
 }
 
 // ------------------------------------------------------------------ small tensors: one launch
@@ -671,18 +1018,21 @@ inline GnPlan gn_plan(int64_t N, int64_t S) {
     p.chunks = (int)ceil_div(S, p.rows);
     return p;
 }
+constexpr int kGnFusedCtas = 148;  // SMs of a B200: the most CTAs of a one-launch kernel
 // Pieces that a group wider than a CTA's vectors is cut into, at most (single-element accesses).
 inline int64_t gn_pieces(int64_t per) { return ceil_div(per, kGnMaxVecs); }
 struct GnRoom {
-    int64_t pivot_off, stat_off, part_c_off, total;
+    int64_t pivot_off, stat_off, part_c_off, arrived_off, total;
 };
 inline GnRoom gn_room(int64_t N, int64_t S, int64_t C, int64_t G) {
     const GnPlan p = gn_plan(N, S);
+    const int64_t slots = N * p.chunks > kGnFusedCtas ? N * p.chunks : kGnFusedCtas;  // CTAs that write sums, either way
     GnRoom r;
-    r.pivot_off = align_up(N * p.chunks * G * gn_pieces(C / G) * 8, 256);
+    r.pivot_off = align_up(slots * G * gn_pieces(C / G) * 8, 256);
     r.stat_off = r.pivot_off + align_up(N * G * 4, 256);
     r.part_c_off = r.stat_off + align_up(N * G * 8, 256);
-    r.total = r.part_c_off + N * p.chunks * C * 8;
+    r.arrived_off = r.part_c_off + align_up(slots * C * 8, 256);
+    r.total = r.arrived_off + 256;
     return r;
 }
 
@@ -742,6 +1092,44 @@ static bool gn_small_ready(PerDevice<int>& cache, Kern kern) {
     }) != nullptr;
 }
 
+// One CTA per SM, shared evenly among the samples; taken where that keeps at least four SMs in five busy.
+// Returns whether the call was made; *e says how it went.
+template <typename Kern>
+static bool launch_gn_fused(PerDevice<int>& cache, Kern kern, GnArgs A, int V, int threads, size_t smem, int64_t most_channels, cudaStream_t st,
+                            cudaError_t* e) {
+    if (A.C % V != 0 || A.C > most_channels || A.G > kGnFusedGroups) return false;
+    const int* sms = cache.get([&](int& n, int dev) {
+        int per_sm = 0, coop = 0;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, smem) != cudaSuccess ||
+            cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev) != cudaSuccess)
+            return false;
+        if (per_sm < 1 || !coop) n = 0;
+        if (n > kGnFusedCtas) n = kGnFusedCtas;
+        return true;
+    });
+    if (!sms || *sms == 0) return false;
+    int chunks = *sms / A.N;
+    if (chunks < 1 || (int64_t)chunks * A.N * 5 < (int64_t)*sms * 4) return false;
+    A.rows = ceil_div(A.S, chunks);
+    A.chunks = (int)ceil_div(A.S, A.rows);
+    A.vecs = A.C / V;
+    if ((*e = cudaMemsetAsync(A.arrived, 0, sizeof(uint32_t), st)) != cudaSuccess) return true;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(A.chunks * A.N));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    *e = cudaLaunchKernelEx(&cfg, kern, A);
+    return true;
+}
+
 template <typename T, int V, int ACT>
 static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
     size_t smem = 0;
@@ -754,6 +1142,17 @@ static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
         if (!gn_small_ready(ready_grad, gn_small_grad_kernel<T, V, ACT>)) return cudaErrorInvalidValue;
         return launch_after(gn_small_grad_kernel<T, V, ACT>, dim3((unsigned)A.blocks), dim3(kGnThreads), smem, st, A);
     }
+    cudaError_t e = cudaSuccess;
+    if constexpr (WholePieces<T, V>::value) {
+        static PerDevice<int> fused, fused_grad;
+        constexpr size_t sums = (size_t)kGnFusedThreads * V * sizeof(float2), grad_sums = (size_t)kGnFusedGradThreads * V * sizeof(float2);
+        constexpr size_t ring = (size_t)kGnFusedThreads * 16 * kGnFusedDepth, grad_ring = (size_t)kGnFusedGradThreads * 32 * kGnFusedGradDepth;
+        static_assert(ring + sums + kGnFusedGroups * 4 <= 232448 && grad_ring + grad_sums <= 232448, "more than the 227 KB of shared memory a CTA can have");
+        if (!backward ? launch_gn_fused(fused, gn_fused_kernel<T, V, ACT>, A, V, kGnFusedThreads, ring + sums, kGnFusedThreads * V, st, &e)
+                      : launch_gn_fused(fused_grad, gn_fused_grad_kernel<T, V, ACT>, A, V, kGnFusedGradThreads, grad_ring + grad_sums,
+                                        kGnFusedGradThreads * V, st, &e))
+            return e;
+    }
     const dim3 grid((unsigned)A.chunks, (unsigned)A.N, (unsigned)A.blocks);
     const unsigned group_ctas = (unsigned)ceil_div((int64_t)A.N * A.G, kGnThreads / 32);
     // the rings; the sums of pass 1 (V pairs per thread) take their place
@@ -761,7 +1160,6 @@ static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
     constexpr size_t sums = (size_t)kGnThreads * V * sizeof(float2);
     constexpr size_t one = ring ? (size_t)kGnThreads * 16 * kGnDepth : 0, two = ring ? (size_t)kGnThreads * 16 * 2 * kGnGradDepth : 0;
     static_assert(one <= 48 * 1024 && two <= 48 * 1024 && sums <= 48 * 1024, "more than a kernel has without asking");
-    cudaError_t e;
     if (!backward) {
         if ((e = launch_after(gn_stats_kernel<T, V>, grid, dim3(kGnThreads), sums > one ? sums : one, st, A)) != cudaSuccess) return e;
         if ((e = launch_after(gn_join_kernel<false>, dim3(group_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess) return e;
