@@ -154,30 +154,42 @@ __device__ __forceinline__ Vec<T, V> narrow2(const Pairs<V>& r) {
     return v;
 }
 __device__ __forceinline__ uint64_t f2_splat(float v) { return f2_pack(v, v); }
-// logistic(u) of a pair, given -log2(e) u
+// logistic(u) of a pair, given -log2(e) u.  SHARED: one reciprocal for both, 1/a = b / (ab), for kernels that the
+// special-function unit (16 a clock per SM; two per value otherwise) would bound.  The exponents are then held at
+// 60, so that ab stays finite: logistic(u) is 2^-60 for all u below -41.6.
+template <bool SHARED>
 __device__ __forceinline__ uint64_t logistic2_scaled(uint64_t e) {
     float a, b;
     f2_unpack(e, a, b);
+    if (SHARED) {  // NaN stays NaN
+        asm("min.NaN.f32 %0, %0, 0f42700000;" : "+f"(a));
+        asm("min.NaN.f32 %0, %0, 0f42700000;" : "+f"(b));
+    }
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
     f2_unpack(f2_add(f2_pack(a, b), f2_splat(1.0f)), a, b);
+    if (SHARED) {
+        float r = a * b;
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
+        return f2_mul(f2_splat(r), f2_pack(b, a));
+    }
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
     return f2_pack(a, b);
 }
 constexpr float kMinusLog2e = -1.4426950408889634f;
-template <int ACT>
+template <int ACT, bool SHARED = false>
 __device__ __forceinline__ uint64_t act_value2(uint64_t z) {
     if (ACT == DVDQ_ACT_NONE) return z;
     const uint64_t e = ACT == DVDQ_ACT_SILU ? f2_mul(z, f2_splat(kMinusLog2e))
                                             : f2_mul(z, f2_fma(f2_splat(kGeluB * kMinusLog2e), f2_mul(z, z), f2_splat(kGeluA * kMinusLog2e)));
-    return f2_mul(z, logistic2_scaled(e));
+    return f2_mul(z, logistic2_scaled<SHARED>(e));
 }
 // act_slope of a pair.  SiLU needs no bound on z: f (1 + z (1 - f)) has no power of z to overflow.
-template <int ACT>
+template <int ACT, bool SHARED = false>
 __device__ __forceinline__ uint64_t act_slope2(uint64_t z) {
     if (ACT == DVDQ_ACT_SILU) {
-        const uint64_t f = logistic2_scaled(f2_mul(z, f2_splat(kMinusLog2e)));
+        const uint64_t f = logistic2_scaled<SHARED>(f2_mul(z, f2_splat(kMinusLog2e)));
         return f2_fma(f, f2_sub(z, f2_mul(z, f)), f);
     }
     if (ACT == DVDQ_ACT_GELU_TANH) {
@@ -186,7 +198,7 @@ __device__ __forceinline__ uint64_t act_slope2(uint64_t z) {
         asm("{\n\tmax.NaN.f32 %0, %0, 0fC1A00000;\n\tmin.NaN.f32 %0, %0, 0f41A00000;\n\t}" : "+f"(a));
         asm("{\n\tmax.NaN.f32 %0, %0, 0fC1A00000;\n\tmin.NaN.f32 %0, %0, 0f41A00000;\n\t}" : "+f"(b));
         const uint64_t c = f2_pack(a, b), s = f2_mul(c, c);
-        const uint64_t f = logistic2_scaled(f2_mul(c, f2_fma(f2_splat(kGeluB * kMinusLog2e), s, f2_splat(kGeluA * kMinusLog2e))));
+        const uint64_t f = logistic2_scaled<SHARED>(f2_mul(c, f2_fma(f2_splat(kGeluB * kMinusLog2e), s, f2_splat(kGeluA * kMinusLog2e))));
         const uint64_t w = f2_mul(f2_mul(c, f2_fma(f2_splat(3.0f * kGeluB), s, f2_splat(kGeluA))), f);  // c u'(c) f
         return f2_add(f, f2_sub(w, f2_mul(w, f)));
     }

@@ -325,6 +325,7 @@ static dvdq_status group_norm_run(const GnArgs& A0, int64_t N, int64_t S, int32_
     const GnPlan p = gn_plan(N, S);
     A.N = (int)N;
     A.S = S;
+    A.inv = 1.0 / ((double)S * A.per);
     A.chunks = p.chunks;
     A.rows = p.rows;
     A.params_f32 = param_dtype == DVDQ_F32;

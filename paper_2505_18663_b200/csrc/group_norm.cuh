@@ -52,6 +52,7 @@ struct GnArgs {
     int blocks;              // channel blocks: each some whole groups, or (bpg > 1) a piece of one group
     int bpg;                 // blocks per group
     int params_f32, params_bf16;
+    double inv;              // 1 / (S per)
     float eps;
 };
 
@@ -199,7 +200,7 @@ __device__ __forceinline__ double warp_sum(double v) {
 // mean and rstd from the group's mean and mean square about its pivot
 __device__ __forceinline__ float2 gn_mean_rstd(double pivot, double m1, double m2, float eps) {
     const double var = m2 - m1 * m1;
-    return make_float2((float)(pivot + m1), (float)(1.0 / sqrt((var > 0.0 || var != var ? var : 0.0) + (double)eps)));
+    return make_float2((float)(pivot + m1), (float)rsqrt((var > 0.0 || var != var ? var : 0.0) + (double)eps));
 }
 
 // Adds up the chunks: the first `group_ctas` CTAs a warp per group, the rest (backward) 32 channels each.
@@ -230,9 +231,8 @@ __global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_consta
             a += t.x;
             b += t.y;
         }
-        const double count = (double)A.S * A.per;
-        a = warp_sum(a) / count;
-        b = warp_sum(b) / count;
+        a = warp_sum(a) * A.inv;
+        b = warp_sum(b) * A.inv;
         if (lane == 0) {
             if (BACKWARD) {
                 A.stat[ng] = make_float2((float)a, (float)b);
@@ -317,14 +317,13 @@ struct GnScale {
 
 // ... from the groups' (mean, rstd)
 template <typename T, int V>
-__device__ __forceinline__ GnScale<T, V> gn_scale(const GnArgs& A, int c0, const float2* stat) {
-    float mu[V], rs[V], ga[V], be[V];
-    gn_by_channel<V>(A.per, c0, [&](int i, int g) { const float2 t = stat[g]; mu[i] = t.x; rs[i] = t.y; },
-                     [&](int i) { mu[i] = mu[0]; rs[i] = rs[0]; });
-    gn_params<V>(A, c0, ga, be);
+__device__ __forceinline__ GnScale<T, V> gn_scale(const GnArgs& A, int c0, const float2* stat, const float (&ga)[V], const float (&be)[V]) {
+    float mu[V], sc[V];
+    gn_by_channel<V>(A.per, c0, [&](int i, int g) { const float2 t = stat[g]; mu[i] = t.x; sc[i] = t.y; },
+                     [&](int i) { mu[i] = mu[0]; sc[i] = sc[0]; });
 #pragma unroll
-    for (int i = 0; i < V; ++i) ga[i] *= rs[i];
-    return GnScale<T, V>(mu, ga, be);
+    for (int i = 0; i < V; ++i) sc[i] *= ga[i];
+    return GnScale<T, V>(mu, sc, be);
 }
 
 template <typename T, int V, int ACT>
@@ -335,8 +334,9 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
     release_successor();
     wait_predecessor();
     if (!P.on) return;
-    const float2* stat = A.stat + (int64_t)n * A.G;
-    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, stat);
+    float ga[V], be[V];
+    gn_params<V>(A, P.c0, ga, be);
+    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, A.stat + (int64_t)n * A.G, ga, be);
     // backwards: from the place pass 1 read last
     const int count = P.count(A.lanes);
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
         const Pairs<V> x = widen2<T, V>(v);
         Pairs<V> o;
 #pragma unroll
-        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT>(scale(x.p[i], i));
+        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT, true>(scale(x.p[i], i));
         store_streaming<T, V>(q, narrow2<T, V>(o));
         q += back;
     });
@@ -355,7 +355,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
 
 // ------------------------------------------------------------------ backward
 
-// What the backward passes hold per channel: h = (x - mean) rstd, z = gamma h + beta.
+// What the backward passes hold per channel: h = (x - mean) rstd, z = gamma h + beta.  |h| is at most the
+// root of the group's size, so the shared reciprocal's 2^-60 in place of a smaller number is far below any rounding.
 template <typename T, int V>
 struct GnGrad {
     GnScale<T, V> h;
@@ -363,7 +364,7 @@ struct GnGrad {
     template <int ACT>
     __device__ __forceinline__ void dz(uint64_t x, uint64_t dy, int i, uint64_t& out_dz, uint64_t& out_h) const {
         out_h = h(x, i);
-        out_dz = ACT == DVDQ_ACT_NONE ? dy : f2_mul(dy, act_slope2<ACT>(f2_fma(gamma.p[i], out_h, beta.p[i])));
+        out_dz = ACT == DVDQ_ACT_NONE ? dy : f2_mul(dy, act_slope2<ACT, true>(f2_fma(gamma.p[i], out_h, beta.p[i])));
     }
 };
 template <typename T, int V>
@@ -508,19 +509,19 @@ struct TwoWay {
         : ring(smem_u32(raw) + threadIdx.x * 16), count(n), at0(from0), at1(from1), step0(s0), step1(s1) {
         asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
         zero -= 1u;
-    }
-    template <typename Use>
-    __device__ __forceinline__ void forward(Use use) {
-        auto next = [&](uint32_t slot, int k, uint32_t dep) {
-            if (k < count) {
-                fill(slot, dep);
-                at0 += step0;
-                if (STREAMS == 2) at1 += step1;
-            }
-            commit();
-        };
 #pragma unroll
         for (int k = 0; k < D - 1; ++k) next((uint32_t)k, k, 0u);
+    }
+    __device__ __forceinline__ void next(uint32_t slot, int k, uint32_t dep) {
+        if (k < count) {
+            fill(slot, dep);
+            at0 += step0;
+            if (STREAMS == 2) at1 += step1;
+        }
+        commit();
+    }
+    template <typename Use>
+    __device__ __forceinline__ void forward(Use use) {  // the constructor has asked for the first D - 1 pieces
         uint32_t slot = 0, behind = D - 1, dep = 0u;
         for (int k = 0; k < count; ++k) {
             next(behind, k + D - 1, dep);
@@ -590,7 +591,7 @@ __device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, TH
         }
         if (PER_CHANNEL) {
             const int i = o / A.vecs, c = (o - i * A.vecs) * V + i;
-            A.part_c[(int64_t)blockIdx.x * A.C + c] = t;
+            A.part_c[(int64_t)c * gridDim.x + blockIdx.x] = t;
             const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
             t.x *= g;
             t.y *= g;
@@ -598,7 +599,7 @@ __device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, TH
         sh[o] = t;
     }
     __syncthreads();
-    float2* out = A.part + (int64_t)blockIdx.x * A.G;
+    float2* out = A.part + (int64_t)P.n * A.G * A.chunks + P.j;
     auto channel = [&](int c) { return sh[(c % V) * A.vecs + c / V]; };
     if (A.per <= 8) {
         for (int g = threadIdx.x; g < A.G; g += THREADS) {
@@ -608,7 +609,7 @@ __device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, TH
                 t.x += u.x;
                 t.y += u.y;
             }
-            out[g] = t;
+            out[(int64_t)g * A.chunks] = t;
         }
     } else {
         for (int g = threadIdx.x >> 5; g < A.G; g += THREADS / 32) {
@@ -623,7 +624,7 @@ __device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, TH
                 t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
                 t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
             }
-            if ((threadIdx.x & 31) == 0) out[g] = t;
+            if ((threadIdx.x & 31) == 0) out[(int64_t)g * A.chunks] = t;
         }
     }
 }
@@ -653,22 +654,25 @@ __device__ __forceinline__ void gn_meet(uint32_t* arrived) {
     __syncthreads();
 }
 
-// The sample's numbers, a warp per group: stat[g] = finish(g, mean of the first, mean of the second).
+// The sample's numbers ([N, G, chunks]: a group's are neighbours), a warp per group: stat[g] = finish(g, mean of the first, mean of the second).
 template <int THREADS, typename Finish>
 __device__ __forceinline__ void gn_team_join(const GnArgs& A, int n, float2* stat, Finish finish) {
     const int lane = threadIdx.x & 31;
-    const double count = (double)A.S * A.per;
     for (int g = threadIdx.x >> 5; g < A.G; g += THREADS / 32) {
-        const float2* base = A.part + (int64_t)n * A.chunks * A.G + g;
+        const float2* base = A.part + ((int64_t)n * A.G + g) * A.chunks;
         double a = 0.0, b = 0.0;
-#pragma unroll 5
-        for (int i = lane; i < A.chunks; i += 32) {
-            const float2 t = __ldcg(base + (int64_t)i * A.G);
-            a += t.x;
-            b += t.y;
+        float2 t[5];
+        for (int i = lane; i < A.chunks; i += 5 * 32) {  // at most 148 chunks: once
+#pragma unroll
+            for (int u = 0; u < 5; ++u) t[u] = i + 32 * u < A.chunks ? __ldcg(base + i + 32 * u) : make_float2(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < 5; ++u) {
+                a += t[u].x;
+                b += t[u].y;
+            }
         }
-        a = warp_sum(a) / count;
-        b = warp_sum(b) / count;
+        a = warp_sum(a) * A.inv;
+        b = warp_sum(b) * A.inv;
         if (lane == 0) stat[g] = finish(g, a, b);
     }
     __syncthreads();
@@ -682,9 +686,9 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
     __shared__ float pivots[kGnFusedGroups];  // y may be x: what was subtracted is kept
     const GnTeam<V, THREADS> P(A);
     const T* x = static_cast<const T*>(A.x) + (int64_t)P.n * A.xn;
+    TwoWay<D, 1, THREADS, T, V> walk(raw, P.count, x + P.c0 + P.s0 * A.xs, P.lanes * A.xs, nullptr, 0);
     for (int g = threadIdx.x; g < A.G; g += THREADS) pivots[g] = to_f32(x[g * A.per]);
     __syncthreads();
-    TwoWay<D, 1, THREADS, T, V> walk(raw, P.count, x + P.c0 + P.s0 * A.xs, P.lanes * A.xs, nullptr, 0);
     {
         Pairs<V> s1, s2, pivot;
         float pv[V];
@@ -703,6 +707,8 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
         });
         gn_team_sums<V, THREADS, false>(A, P, s1, s2, sums);
     }
+    float ga[V], be[V];
+    gn_params<V>(A, P.c0, ga, be);  // asked for before the wait
     gn_meet(A.arrived);
     gn_team_join<THREADS>(A, P.n, sums, [&](int g, double m1, double m2) {
         const float2 t = gn_mean_rstd((double)pivots[g], m1, m2, A.eps);
@@ -711,14 +717,14 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
         return t;
     });
     if (!P.on) return;
-    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, sums);
+    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, sums, ga, be);
     T* q = static_cast<T*>(A.y) + (int64_t)P.n * A.yn + P.c0 + (P.s0 + (int64_t)(P.count - 1) * P.lanes) * A.ys;
     const int64_t back = -(int64_t)P.lanes * A.ys;
     walk.backward([&](const Vec<T, V>& in) {
         const Pairs<V> f = widen2<T, V>(in);
         Pairs<V> o;
 #pragma unroll
-        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT>(scale(f.p[i], i));
+        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT, true>(scale(f.p[i], i));
         store_streaming<T, V>(q, narrow2<T, V>(o));
         q += back;
     });
@@ -730,10 +736,10 @@ __global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(c
     extern __shared__ __align__(16) uint8_t raw[];
     float2* sums = reinterpret_cast<float2*>(raw + THREADS * 32 * D);
     const GnTeam<V, THREADS> P(A);
-    float rs[V], ga[V];
-    const GnGrad<T, V> K = gn_constants<T, V>(A, P.n, P.c0, rs, ga);
     TwoWay<D, 2, THREADS, T, V> walk(raw, P.count, static_cast<const T*>(A.x) + (int64_t)P.n * A.xn + P.c0 + P.s0 * A.xs, P.lanes * A.xs,
                                      static_cast<const T*>(A.dy) + (int64_t)P.n * A.dn + P.c0 + P.s0 * A.ds, P.lanes * A.ds);
+    float rs[V], ga[V];
+    const GnGrad<T, V> K = gn_constants<T, V>(A, P.n, P.c0, rs, ga);
     {
         Pairs<V> s1, s2;
 #pragma unroll
@@ -776,7 +782,7 @@ __global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(c
         double a = 0.0, b = 0.0;
 #pragma unroll 5
         for (int i = lane; i < ctas; i += 32) {
-            const float2 t = __ldcg(A.part_c + (int64_t)i * A.C + c);
+            const float2 t = __ldcg(A.part_c + (int64_t)c * ctas + i);
             a += t.x;
             b += t.y;
         }
