@@ -280,21 +280,21 @@ def dvdq_qlinear_static(X: torch.Tensor, q: ActQuant, w: Weights, bias: Optional
 
 # ------------------------------------------------------------------ around the quantized layers
 
-def _address(t: Optional[torch.Tensor], dtype, name: str, shape=None) -> Optional[int]:
-    """Device address of a tensor whose dtype (and shape) are as required; None for None."""
+def _address(t: Optional[torch.Tensor], dtype, name: str) -> Optional[int]:
+    """Device address of a tensor whose dtype is as required; None for None."""
     if t is None:
         return None
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and t.shape != shape:
-        raise TypeError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _vector(t: Optional[torch.Tensor], dtype, n: int, name: str) -> Optional[int]:
-    if t is not None and (t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1)):
+    if t is None:
+        return None
+    if t.dim() != 1 or len(t) != n or (n > 1 and t.stride(0) != 1):
         raise TypeError(f"{name} must be a dense vector of {n} values")
     return _address(t, dtype, name)
 
@@ -303,11 +303,16 @@ def _matrix(t: Optional[torch.Tensor], dtype, rows: int, cols: int, name: str):
     """(address, row pitch) of a [rows, cols] matrix with unit inner stride."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise TypeError(f"{name} must have shape {(rows, cols)}, got {tuple(t.shape)}")
-    if cols > 1 and t.stride(1) != 1:
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise TypeError(f"{name} must have shape {(rows, cols)}, got {tuple(shape)}")
+    pitch, inner = t.stride()
+    if cols > 1 and inner != 1:
         raise TypeError(f"{name} must have unit inner stride")
-    return _address(t, dtype, name), t.stride(0)
+    return _address(t, dtype, name), pitch
+
+
+_ANY_FLOAT, _HALF_FLOAT = (BF16, F16, F32), (BF16, F16)
 
 
 def _element_type(t: torch.Tensor, name: str, allowed) -> int:
@@ -339,7 +344,7 @@ def dvdq_linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], 
     pre-activation for dvdq_linear_backward.  residual may be Y itself.  Rows start on 16 bytes (pitches
     are multiples of 8 elements); workspace: dvdq_linear_workspace_bytes(M, N, K) bytes, None where that is 0."""
     dt = X.dtype
-    code = _element_type(X, "X", (BF16, F16))
+    code = _element_type(X, "X", _HALF_FLOAT)
     if X.dim() != 2 or W.dim() != 2:
         raise TypeError("X and W must be 2-D")
     (M, K), N = X.shape, W.shape[0]
@@ -363,7 +368,7 @@ def dvdq_linear_backward(dY: torch.Tensor, Z: Optional[torch.Tensor], X: Optiona
     """Gradients of dvdq_linear: dX [M, K], dW [N, K] (dY's type), dbias fp32 [N], each written if given.  Z is
     the pre-activation (not read without an activation); X is needed for dW, W for dX.  The residual's gradient is dY."""
     dt = dY.dtype
-    code = _element_type(dY, "dY", (BF16, F16))
+    code = _element_type(dY, "dY", _HALF_FLOAT)
     if dY.dim() != 2:
         raise TypeError("dY must be 2-D")
     M, N = dY.shape
@@ -409,14 +414,17 @@ def dvdq_rope_table(freqs, positions: Optional[torch.Tensor], table: torch.Tenso
                                   amplitude, _address(table, torch.float32, "table"), _raw_stream(stream, table)), "dvdq_rope_table")
 
 
-def _rope_tensor(x: torch.Tensor, y: torch.Tensor, shape, dtype, name: str) -> RopeTensor:
-    if x.dim() != 4 or x.shape[0] != shape[0] or x.shape[1] != shape[1] or x.shape[3] != shape[3]:
+def _rope_tensor(x: torch.Tensor, y: torch.Tensor, B: int, S: int, D: int, dtype, name: str) -> RopeTensor:
+    shape = x.shape
+    if len(shape) != 4 or shape[0] != B or shape[1] != S or shape[3] != D:
         raise TypeError(f"{name} must be [B, S, heads, head_dim] like q")
-    xs, ys = x.stride(), y.stride()
-    if shape[3] > 1 and (xs[3] != 1 or ys[3] != 1):
+    if y.shape != shape:
+        raise TypeError(f"{name}_out must have shape {tuple(shape)}, got {tuple(y.shape)}")
+    xb, xs, xh, xd = x.stride()
+    yb, ys, yh, yd = y.stride()
+    if D > 1 and (xd != 1 or yd != 1):
         raise TypeError(f"{name} must have unit stride inside a head")
-    return RopeTensor(_address(x, dtype, name), _address(y, dtype, name + "_out", x.shape), x.shape[2], xs[0], xs[1], xs[2],
-                      ys[0], ys[1], ys[2])
+    return RopeTensor(_address(x, dtype, name), _address(y, dtype, name + "_out"), shape[2], xb, xs, xh, yb, ys, yh)
 
 
 def dvdq_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: torch.Tensor, rows: Optional[torch.Tensor], layout: int,
@@ -425,25 +433,27 @@ def dvdq_rope(q: torch.Tensor, k: Optional[torch.Tensor], table: torch.Tensor, r
     may be q and k themselves.  table [rows, rot_dim / 2, 2] of dvdq_rope_table; rows: int32 [B, S] or [S], the table
     row of each token (None: token s takes row s).  inverse=True: the gradient."""
     dt = q.dtype
-    code = _element_type(q, "q", (BF16, F16, F32))
+    code = _element_type(q, "q", _ANY_FLOAT)
     if q.dim() != 4:
         raise TypeError("q must be [B, S, heads, head_dim]")
     B, S, _, D = q.shape
     if (k is None) != (k_out is None):
         raise TypeError("k and k_out come together")
-    if table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+    table_rows, pairs, two = table.shape if table.dim() == 3 else (0, 0, 0)
+    if two != 2 or not table.is_contiguous():
         raise TypeError("table must be dense [rows, rot_dim / 2, 2]")
-    batch = 0
+    batch, index = 0, None
     if rows is not None:
-        if rows.shape != (B, S) and rows.shape != (S,):
+        shape, strides = rows.shape, rows.stride()
+        if shape != (B, S) and shape != (S,):
             raise TypeError("rows must be [B, S] or [S]")
-        if S > 1 and rows.stride(-1) != 1:
+        if S > 1 and strides[-1] != 1:
             raise TypeError("rows must have unit stride along the tokens")
-        batch = rows.stride(0) if rows.dim() == 2 else 0
-    qt = _rope_tensor(q, q_out, q.shape, dt, "q")
-    kt = _rope_tensor(k, k_out, q.shape, dt, "k") if k is not None else None
-    _check(load().dvdq_rope(qt, kt, B, S, D, 2 * table.shape[1], _address(table, torch.float32, "table"), table.shape[0],
-                            _address(rows, torch.int32, "rows"), batch, layout, 1 if inverse else 0, code, _raw_stream(stream, q)), "dvdq_rope")
+        batch = strides[0] if len(shape) == 2 else 0
+        index = _address(rows, torch.int32, "rows")
+    _check(load().dvdq_rope(_rope_tensor(q, q_out, B, S, D, dt, "q"), None if k is None else _rope_tensor(k, k_out, B, S, D, dt, "k"),
+                            B, S, D, 2 * pairs, _address(table, torch.float32, "table"), table_rows, index, batch, layout,
+                            1 if inverse else 0, code, _raw_stream(stream, q)), "dvdq_rope")
 
 
 def dvdq_group_norm_workspace_bytes(N: int, S: int, C_: int, G: int) -> int:
@@ -482,7 +492,7 @@ def dvdq_group_norm(X: torch.Tensor, G: int, gamma: Optional[torch.Tensor], beta
     """Y = act(group norm of X [N, S, C]) over G groups of neighbouring channels, channels last (places of a feature map
     flattened to S); mean and rstd, if given, receive fp32 [N, G] for dvdq_group_norm_backward."""
     dt = X.dtype
-    code = _element_type(X, "X", (BF16, F16, F32))
+    code = _element_type(X, "X", _ANY_FLOAT)
     if X.dim() != 3:
         raise TypeError("X must be [N, S, C]")
     N, S, channels = X.shape
@@ -500,7 +510,7 @@ def dvdq_group_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tens
                              stream=None) -> None:
     """Gradients of dvdq_group_norm: dX (X's type), dgamma and dbeta (fp32 [C]), each written if given."""
     dt = X.dtype
-    code = _element_type(X, "X", (BF16, F16, F32))
+    code = _element_type(X, "X", _ANY_FLOAT)
     if X.dim() != 3:
         raise TypeError("X must be [N, S, C]")
     N, S, channels = X.shape
