@@ -217,9 +217,9 @@ template <typename T, int V> struct WholePieces { static constexpr bool value = 
 // a warp waits for its slowest load with nothing in flight: 3.8 instead of 5 TB/s.
 // A slot is refilled only when what was read from it has been delivered: the copy's address
 // depends on the words read (ANDed with a zero that the compiler does not know).
-template <int D, int STREAMS, typename T, int V, typename Use>
+template <int D, int STREAMS, typename T, int V, int THREADS = kStreamThreads, typename Use>
 __device__ __forceinline__ void thread_stream(uint32_t ring, int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
-    constexpr uint32_t kSlot = kStreamThreads * 16;
+    constexpr uint32_t kSlot = THREADS * 16;
     static_assert(sizeof(Vec<T, V>) == 16, "16-byte pieces");
     uint32_t zero;
     asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
@@ -283,6 +283,83 @@ __device__ __forceinline__ void store_streaming(T* p, const Vec<T, V>& v) {  // 
     if constexpr (sizeof(Vec<T, V>) == 16) __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
     else *reinterpret_cast<Vec<T, V>*>(p) = v;
 }
+// Both passes of one thread over its pieces.  forward(): as thread_stream, and the last D pieces stay in the ring;
+// backward(): from the last piece to the first, those D from where they are, the rest through the ring again.
+template <int D, int STREAMS, int THREADS, typename T, int V>
+struct TwoWay {
+    static constexpr uint32_t kSlot = THREADS * 16, kPiece = STREAMS * kSlot;
+    uint32_t ring, zero;
+    int count;
+    const T *at0, *at1;      // next piece to fetch
+    int64_t step0, step1;
+    __device__ __forceinline__ void fill(uint32_t slot, uint32_t dep) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + dep), "l"(at0) : "memory");
+        if constexpr (STREAMS == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + kSlot + dep), "l"(at1) : "memory");
+    }
+    __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory"); }
+    // hands the slot's pieces to use(); the value returned is zero, but known only when they have been delivered
+    template <typename Use>
+    __device__ __forceinline__ uint32_t take(uint32_t slot, Use& use) {
+        union { uint4 w; Vec<T, V> v; } in[STREAMS];
+        uint32_t dep = 0u;
+#pragma unroll
+        for (int j = 0; j < STREAMS; ++j) {
+            in[j].w = lds128(ring + slot * kPiece + j * kSlot);
+            dep ^= in[j].w.w;
+        }
+        if constexpr (STREAMS == 1) use(in[0].v);
+        else use(in[0].v, in[1].v);
+        return dep & zero;
+    }
+    __device__ __forceinline__ TwoWay(const uint8_t* raw, int n, const T* from0, int64_t s0, const T* from1, int64_t s1)
+        : ring(smem_u32(raw) + threadIdx.x * 16), count(n), at0(from0), at1(from1), step0(s0), step1(s1) {
+        asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
+        zero -= 1u;
+#pragma unroll
+        for (int k = 0; k < D - 1; ++k) next((uint32_t)k, k, 0u);
+    }
+    __device__ __forceinline__ void next(uint32_t slot, int k, uint32_t dep) {
+        if (k < count) {
+            fill(slot, dep);
+            at0 += step0;
+            if (STREAMS == 2) at1 += step1;
+        }
+        commit();
+    }
+    template <typename Use>
+    __device__ __forceinline__ void forward(Use use) {  // the constructor has asked for the first D - 1 pieces
+        uint32_t slot = 0, behind = D - 1, dep = 0u;
+        for (int k = 0; k < count; ++k) {
+            next(behind, k + D - 1, dep);
+            wait();
+            dep = take(slot, use);
+            behind = slot;
+            slot = slot + 1 == D ? 0u : slot + 1;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    template <typename Use>
+    __device__ __forceinline__ void backward(Use use) {
+        if (count == 0) return;
+        // piece k is in slot k % D; at0 stands one past the last piece
+        uint32_t slot = (uint32_t)((count - 1) % D);
+        at0 -= (int64_t)(D + 1) * step0;  // piece count - 1 - D
+        if (STREAMS == 2) at1 -= (int64_t)(D + 1) * step1;
+        for (int k = count - 1; k >= 0; --k) {
+            wait();
+            const uint32_t dep = take(slot, use);
+            if (k >= D) {
+                fill(slot, dep);
+                at0 -= step0;
+                if (STREAMS == 2) at1 -= step1;
+            }
+            commit();
+            slot = slot == 0 ? D - 1 : slot - 1;
+        }
+    }
+};
+
 // ------------------------------------------------------------------ dependent launches
 
 // A kernel launched with launch_after may start while its predecessor on the stream drains; it

@@ -45,11 +45,7 @@ struct LinBackwardPlan {
     int64_t chunks, rows;
 };
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
-    LinBackwardPlan p = {};
-    if (M <= kFewTokens) {
-        p.total = few_dx_plan(M, N, K).bytes;
-        return p;
-    }
+    LinBackwardPlan p;
     p.dx = lin_plan(M, K, N, 64);
     p.dw = lin_plan(N, K, M, 64);
     p.lddz = align_up(N, 8);
@@ -72,19 +68,14 @@ static dvdq_status linear_t(const LinMatrix& x, const LinMatrix& w, int64_t M, i
 template <typename T>
 static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N,
                                      int64_t K, int32_t act, const LinMatrix& dx, const LinMatrix& dw, float* db, uint8_t* ws, cudaStream_t st) {
-    if (M <= kFewTokens) {
-        float* few = reinterpret_cast<float*>(ws);
-        if (M == 1) return launch_linear_few_grad<T, 1>(dy, z, x, w, M, N, K, act, dx, dw, db, few, st);
-        if (M <= 4) return launch_linear_few_grad<T, 4>(dy, z, x, w, M, N, K, act, dx, dw, db, few, st);
-        return launch_linear_few_grad<T, 16>(dy, z, x, w, M, N, K, act, dx, dw, db, few, st);
-    }
     const LinBackwardPlan p = linear_backward_plan(M, N, K, act);
-    float* sums = db ? reinterpret_cast<float*>(ws + p.sums_off) : nullptr;
+    const bool few = M <= kFewGradTokens;  // dW and dbias by their own kernel
+    float* sums = db && !few ? reinterpret_cast<float*>(ws + p.sums_off) : nullptr;
     float* part = reinterpret_cast<float*>(ws + p.part_off);
     LinMatrix dz = dy;
     if (act != DVDQ_ACT_NONE) dz = LinMatrix{ws + p.dz_off, p.lddz};
     dvdq_status s;
-    if (act != DVDQ_ACT_NONE || db) {
+    if (sums || (act != DVDQ_ACT_NONE && (dx.p || (dw.p && !few)))) {
         const dim3 grid((unsigned)ceil_div(N, kLinDzCols), (unsigned)p.chunks);
         auto k = act == DVDQ_ACT_GELU_TANH ? linear_dz_kernel<T, DVDQ_ACT_GELU_TANH>
                  : act == DVDQ_ACT_SILU    ? linear_dz_kernel<T, DVDQ_ACT_SILU>
@@ -92,12 +83,14 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
         if ((s = cuda_status(launch_after(k, grid, dim3(kStreamThreads), 0, st, static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p),
                                           z.ld, M, (int)N, p.rows, static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, sums))) != DVDQ_OK)
             return s;
-        if (db && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
+        if (sums && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
                                                 (int)N, db))) != DVDQ_OK)
             return s;
     }
     const LinEpilogue none = {};
     if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK) return s;
+    if (few && (dw.p || db))
+        return M == 1 ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st) : launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st);
     if (dw.p && (s = launch_linear<T, true, true>(dz, x, N, K, M, p.dw, none, dw, part, st)) != DVDQ_OK) return s;
     return DVDQ_OK;
 }

@@ -476,83 +476,6 @@ __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __gr
 // Threads, and slots of the ring: it and the sums fill the shared memory of an SM.
 constexpr int kGnFusedThreads = 1024, kGnFusedDepth = 9, kGnFusedGradThreads = 512, kGnFusedGradDepth = 10, kGnFusedGroups = 1024;
 
-// Both passes of one thread over its pieces.  forward(): as thread_stream, and the last D pieces stay in the ring;
-// backward(): from the last piece to the first, those D from where they are, the rest through the ring again.
-template <int D, int STREAMS, int THREADS, typename T, int V>
-struct TwoWay {
-    static constexpr uint32_t kSlot = THREADS * 16, kPiece = STREAMS * kSlot;
-    uint32_t ring, zero;
-    int count;
-    const T *at0, *at1;      // next piece to fetch
-    int64_t step0, step1;
-    __device__ __forceinline__ void fill(uint32_t slot, uint32_t dep) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + dep), "l"(at0) : "memory");
-        if constexpr (STREAMS == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + kSlot + dep), "l"(at1) : "memory");
-    }
-    __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory"); }
-    // hands the slot's pieces to use(); the value returned is zero, but known only when they have been delivered
-    template <typename Use>
-    __device__ __forceinline__ uint32_t take(uint32_t slot, Use& use) {
-        union { uint4 w; Vec<T, V> v; } in[STREAMS];
-        uint32_t dep = 0u;
-#pragma unroll
-        for (int j = 0; j < STREAMS; ++j) {
-            in[j].w = lds128(ring + slot * kPiece + j * kSlot);
-            dep ^= in[j].w.w;
-        }
-        if constexpr (STREAMS == 1) use(in[0].v);
-        else use(in[0].v, in[1].v);
-        return dep & zero;
-    }
-    __device__ __forceinline__ TwoWay(const uint8_t* raw, int n, const T* from0, int64_t s0, const T* from1, int64_t s1)
-        : ring(smem_u32(raw) + threadIdx.x * 16), count(n), at0(from0), at1(from1), step0(s0), step1(s1) {
-        asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
-        zero -= 1u;
-#pragma unroll
-        for (int k = 0; k < D - 1; ++k) next((uint32_t)k, k, 0u);
-    }
-    __device__ __forceinline__ void next(uint32_t slot, int k, uint32_t dep) {
-        if (k < count) {
-            fill(slot, dep);
-            at0 += step0;
-            if (STREAMS == 2) at1 += step1;
-        }
-        commit();
-    }
-    template <typename Use>
-    __device__ __forceinline__ void forward(Use use) {  // the constructor has asked for the first D - 1 pieces
-        uint32_t slot = 0, behind = D - 1, dep = 0u;
-        for (int k = 0; k < count; ++k) {
-            next(behind, k + D - 1, dep);
-            wait();
-            dep = take(slot, use);
-            behind = slot;
-            slot = slot + 1 == D ? 0u : slot + 1;
-        }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-    }
-    template <typename Use>
-    __device__ __forceinline__ void backward(Use use) {
-        if (count == 0) return;
-        // piece k is in slot k % D; at0 stands one past the last piece
-        uint32_t slot = (uint32_t)((count - 1) % D);
-        at0 -= (int64_t)(D + 1) * step0;  // piece count - 1 - D
-        if (STREAMS == 2) at1 -= (int64_t)(D + 1) * step1;
-        for (int k = count - 1; k >= 0; --k) {
-            wait();
-            const uint32_t dep = take(slot, use);
-            if (k >= D) {
-                fill(slot, dep);
-                at0 -= step0;
-                if (STREAMS == 2) at1 -= step1;
-            }
-            commit();
-            slot = slot == 0 ? D - 1 : slot - 1;
-        }
-    }
-};
-
 // The CTA's place: sample n, chunk j of `chunks`.
 template <int V, int THREADS>
 struct GnTeam {

@@ -11,7 +11,7 @@
 // it is, the more tiles a small product has for the 74 pairs): tcgen05.mma.cta_group::2.kind::f16 256 x bn x 16,
 // operands in shared memory (128-byte swizzle) in a ring of TMA-filled stages of 64 along k, two fp32
 // accumulators in tensor memory, so that the epilogue of a tile runs under the next tile's products.
-// Roles per CTA: warp 0 TMA producer; warp 1 (leader CTA) issues the products; warps 4-11 epilogue, two
+// Roles per CTA: warps 0 and 2 TMA producers of A and B; warp 1 (leader CTA) issues the products; warps 4-11 epilogue, two
 // per tensor-memory lane quarter, every other 32 columns each: bias, activation, residual in fp32, ONE rounding,
 // and TMA stores of 32 x 32 blocks; the residual's blocks come by TMA one block ahead.
 //
@@ -35,17 +35,15 @@ enum LinOut { kLinFinal = 0, kLinFinalZ = 1, kLinPartial = 2 };
 
 template <int OUT>
 struct LinSmem {
-    // storing z as well takes a third output block per epilogue warp, and a stage less.  (More stages
-    // for narrow tiles, whose stages are smaller, changed nothing.)
-    static constexpr int kStages = OUT == kLinFinalZ ? 5 : 6;
+    // storing z as well takes a third output block per epilogue warp, and 32 KB of the ring
+    static constexpr int kRing = (OUT == kLinFinalZ ? 5 : 6) * 32768;
+    static constexpr int kMaxStages = 16;                   // a stage is 32 KB at most; narrow tiles and few rows take less
     static constexpr int kBufs = OUT == kLinFinalZ ? 3 : 2;
-    static constexpr int kOperand = 128 * kLinBK * 2;       // one CTA's half of an operand's stage
-    static constexpr int kStage = 2 * kOperand;
     static constexpr int kBuf = 32 * 32 * 2;                // 32 x 32 outputs; fp32 partials use two as one
-    static constexpr int kBufOff = kStages * kStage;
+    static constexpr int kBufOff = kRing;
     static constexpr int kBiasOff = kBufOff + kLinEpiWarps * kBufs * kBuf;
     static constexpr int kBarOff = kBiasOff + kLinEpiWarps * 32 * 4;
-    static constexpr int kNumBars = 2 * kStages + 5 + 2 * kLinEpiWarps;
+    static constexpr int kNumBars = 2 * kMaxStages + 5 + 2 * kLinEpiWarps;
     static constexpr int kMiscOff = kBarOff + kNumBars * 8;
     static constexpr int kTotal = kMiscOff + 16 + 1024;
     static_assert(kTotal <= 232448, "more than the 227 KB of shared memory a CTA can have");
@@ -58,8 +56,50 @@ struct LinArgs {
     int kblocks, splits;    // k-blocks of the contraction, pieces it is cut into
     int panel;              // column tiles walked together
     int part_rows;          // rows of one piece in the partial buffer
+    int a_bytes;            // of one CTA's half of A's stage
+    int stages, stage, b_off;  // of the operand ring: how many, bytes per CTA of each, where B's half begins in it
     int act, has_residual;
     const void* bias;
+};
+
+// mbar_wait by a converged warp of which one lane polls (32 polling lanes of eight warps keep the shared memory's
+// barrier unit busy, and the producer and the issuer of products wait for it); the others look once, when it is over.
+__device__ __forceinline__ bool mbar_wait_one_lane(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t wait_id) {
+    bool ok = true;
+    if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity, abort_flag, wait_id);
+    ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0) != 0;
+    return ok && __all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity));
+}
+
+// A walk through a ring of stages by one thread: visit(stage) for `n` stages in turn, after their barriers' phases.  The
+// barriers of a deep ring (narrow tiles) are looked at in pairs, which overlaps their latencies: with one look per stage
+// these loops, not the tensor pipe, were the bound of tiles narrower than 192 columns (0.19 us a k-block; 0.145 in
+// pairs).  A ring of six 32 KB stages has none to spare for pairs (4096^3: 95 us with, 93 without).
+constexpr int kLinPairStages = 7;
+struct LinRing {
+    uint32_t bars, stages, st = 0, parity;
+    __device__ __forceinline__ LinRing(uint32_t first_bar, uint32_t n, uint32_t p) : bars(first_bar), stages(n), parity(p) {}
+    __device__ __forceinline__ void step() {
+        if (++st == stages) { st = 0; parity ^= 1u; }
+    }
+    template <typename Visit>
+    __device__ __forceinline__ bool walk(int n, volatile uint32_t* abort_flag, uint32_t wait_id, Visit visit) {
+        for (const bool pairs = stages > kLinPairStages; n > 0;) {
+            const bool two = pairs && n > 1, wraps = st + 1 == stages;
+            const uint32_t bar0 = bars + 8u * st, bar1 = wraps ? bars : bar0 + 8u, parity1 = wraps ? parity ^ 1u : parity;
+            const bool first = mbar_try_wait(bar0, parity), second = !two || mbar_try_wait(bar1, parity1);
+            if (!first && !mbar_wait(bar0, parity, abort_flag, wait_id)) return false;
+            if (!second && !mbar_wait(bar1, parity1, abort_flag, wait_id)) return false;
+            visit(st);
+            step();
+            if (two) {
+                visit(st);
+                step();
+            }
+            n -= two ? 2 : 1;
+        }
+        return true;
+    }
 };
 
 // Item -> tile and piece.  Tiles are walked in panels of `panel` column tiles, columns fastest, so that the
@@ -124,7 +164,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
               const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ LinArgs A) {
     using S = LinSmem<OUT>;
-    constexpr int ST = S::kStages;
+    constexpr int MS = S::kMaxStages;
+    const uint32_t ST = (uint32_t)A.stages, stage = (uint32_t)A.stage;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sbase = smem_u32(smem);
@@ -135,16 +176,16 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 
     const uint32_t bar0 = sbase + S::kBarOff;
     auto full = [&](int s) { return bar0 + 8u * s; };                    // leader's copy: both CTAs' operands are in place
-    auto empty = [&](int s) { return bar0 + 8u * (ST + s); };            // one per CTA
-    auto acc_full = [&](int s) { return bar0 + 8u * (2 * ST + s); };     // one per CTA
-    auto acc_empty = [&](int s) { return bar0 + 8u * (2 * ST + 2 + s); };  // leader's copy
-    const uint32_t drain_bar = bar0 + 8u * (2 * ST + 4);
-    auto res_full = [&](int w, int b) { return bar0 + 8u * (2 * ST + 5 + 2 * w + b); };  // a warp's residual block has landed
+    auto empty = [&](int s) { return bar0 + 8u * (MS + s); };            // one per CTA
+    auto acc_full = [&](int s) { return bar0 + 8u * (2 * MS + s); };     // one per CTA
+    auto acc_empty = [&](int s) { return bar0 + 8u * (2 * MS + 2 + s); };  // leader's copy
+    const uint32_t drain_bar = bar0 + 8u * (2 * MS + 4);
+    auto res_full = [&](int w, int b) { return bar0 + 8u * (2 * MS + 5 + 2 * w + b); };  // a warp's residual block has landed
     volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kMiscOff);  // [0] tmem base, [1] abort
     volatile uint32_t* abort_flag = misc + 1;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int s = 0; s < MS; ++s) { mbar_init(full(s), 2); mbar_init(empty(s), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), 2 * kLinEpiWarps); }
         mbar_init(drain_bar, 1);
         for (int w = 0; w < kLinEpiWarps; ++w) { mbar_init(res_full(w, 0), 1); mbar_init(res_full(w, 1), 1); }
@@ -163,28 +204,35 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     release_successor();
     wait_predecessor();
 
-    if (warp == 0) {
-        // ------------------------------------------------------------ TMA producer
-        if (lane == 0) {
-            tma_prefetch_desc(&tmA);
-            tma_prefetch_desc(&tmB);
-            uint32_t st = 0, ph = 0;
-            bool ok = true;
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------ TMA producers: warp 0 of A, warp 2 of B
+        // (one thread that asks for both takes 460 clocks a k-block, as long as the products of a 256-wide tile)
+        if (elect_one()) {
+            const bool of_a = warp == 0;
+            const CUtensorMap* map = of_a ? &tmA : &tmB;
+            tma_prefetch_desc(map);
             const int bw = A.bn / 2;  // columns per CTA
-            const uint32_t bytes = 2 * (lin_bytes<AMN>(128) + lin_bytes<BMN>(bw));
+            const uint32_t leader_full = map_to_cta(full(0), 0);
+            LinRing ring(empty(0), ST, 1u);
+            const uint32_t dst = sbase + (of_a ? 0 : A.b_off);
+            bool ok = true;
             for (int item = pair; ok && item < items; item += num_pairs) {
                 int tm, tn, piece;
                 lin_item(A, item, tm, tn, piece);
                 const int2 kr = lin_range(A, piece);
-                const int m0 = tm * kLinTile + (int)rank * 128, n0 = tn * A.bn + (int)rank * bw;
-                for (int kb = kr.x; kb < kr.y; ++kb) {
-                    if (!mbar_wait(empty(st), ph ^ 1u, abort_flag, kWaitWideEmpty)) { ok = false; break; }
+                const int r0 = of_a ? tm * kLinTile + (int)rank * 128 : tn * A.bn + (int)rank * bw;
+                // rows past D's last need no operand: whatever lies in their stage reaches only rows that are not stored
+                const bool needed = !of_a || r0 < A.Md;
+                const uint32_t bytes = of_a ? A.a_bytes * (tm * kLinTile + 128 < A.Md ? 2u : 1u) : 2 * lin_bytes<BMN>(bw);
+                int k0 = kr.x * kLinBK;
+                ok = ring.walk(kr.y - kr.x, abort_flag, kWaitWideEmpty, [&](uint32_t st) {
                     if (rank == 0) mbar_arrive_expect_tx(full(st), bytes);
-                    const uint32_t bar = map_to_cta(full(st), 0), dst = sbase + st * S::kStage;
-                    lin_load<AMN>(dst, &tmA, bar, kb * kLinBK, m0, 128);
-                    lin_load<BMN>(dst + S::kOperand, &tmB, bar, kb * kLinBK, n0, bw);
-                    if (++st == ST) { st = 0; ph ^= 1u; }
-                }
+                    if (needed) {
+                        if (of_a) lin_load<AMN>(dst + st * stage, map, leader_full + 8u * st, k0, r0, 128);
+                        else lin_load<BMN>(dst + st * stage, map, leader_full + 8u * st, k0, r0, bw);
+                    }
+                    k0 += kLinBK;
+                });
             }
             if (!ok)  // giving up after seconds of waiting: a bounded pause covers the last copies
                 for (int it = 0; it < 64; ++it) __nanosleep(1000);
@@ -192,39 +240,38 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------------------ products (leader CTA only)
-        if (rank == 0) {
+        // One thread runs the whole loop: a warp-wide wait for every k-block costs more than the products of a narrow tile.
+        if (rank == 0 && elect_one()) {
             const uint32_t idesc = umma_idesc_f16(IsBf16<T>::value, AMN, BMN, kLinTile) | ((uint32_t)(A.bn >> 3) << 17);
             // 16 elements along k: 32 bytes inside a K-major swizzle row, two atoms of an MN-major tile
             constexpr uint32_t kStepA = AMN ? 2048 / 16 : 2, kStepB = BMN ? 2048 / 16 : 2;
-            uint32_t st = 0, ph = 0, lt = 0;
+            const uint64_t ad0 = AMN ? umma_desc_sw128_mnmajor(sbase) : umma_desc_sw128_kmajor(sbase);
+            const uint64_t bd0 = BMN ? umma_desc_sw128_mnmajor(sbase + A.b_off) : umma_desc_sw128_kmajor(sbase + A.b_off);
+            LinRing ring(full(0), ST, 0u);
+            uint32_t lt = 0;
             bool ok = true;
             for (int item = pair; ok && item < items; item += num_pairs, ++lt) {
                 int tm, tn, piece;
                 lin_item(A, item, tm, tn, piece);
                 const int2 kr = lin_range(A, piece);
                 const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
-                if (!mbar_wait_warp(acc_empty(a), aph ^ 1u, abort_flag, kWaitAccEmpty)) { ok = false; break; }
+                if (!mbar_wait(acc_empty(a), aph ^ 1u, abort_flag, kWaitAccEmpty)) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + a * kLinTile;
-                for (int kb = kr.x; kb < kr.y; ++kb) {
-                    if (!mbar_wait_warp(full(st), ph, abort_flag, kWaitWideFull)) { ok = false; break; }
+                uint32_t add = 0u;
+                ok = ring.walk(kr.y - kr.x, abort_flag, kWaitWideFull, [&](uint32_t st) {
                     tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t at = sbase + st * S::kStage;
-                        const uint64_t ad = AMN ? umma_desc_sw128_mnmajor(at) : umma_desc_sw128_kmajor(at);
-                        const uint64_t bd = BMN ? umma_desc_sw128_mnmajor(at + S::kOperand) : umma_desc_sw128_kmajor(at + S::kOperand);
+                    const uint32_t off = st * (stage >> 4);  // in the descriptors' 16-byte units
 #pragma unroll
-                        for (int k = 0; k < kLinBK / 16; ++k)
-                            tc_mma_f16_pair(d_tmem, ad + kStepA * k, bd + kStepB * k, idesc, (kb != kr.x || k != 0) ? 1u : 0u);
-                        tc_commit_pair(empty(st), 3);
-                        if (kb + 1 == kr.y) tc_commit_pair(acc_full(a), 3);
+                    for (int k = 0; k < kLinBK / 16; ++k) {
+                        tc_mma_f16_pair(d_tmem, ad0 + (off + kStepA * k), bd0 + (off + kStepB * k), idesc, add);
+                        add = 1u;
                     }
-                    __syncwarp();
-                    if (++st == ST) { st = 0; ph ^= 1u; }
-                }
+                    tc_commit_pair(empty(st), 3);
+                });
+                if (ok) tc_commit_pair(acc_full(a), 3);
             }
-            if (elect_one()) tc_commit_pair(drain_bar, 1);
-            __syncwarp();
+            tc_commit_pair(drain_bar, 1);
             mbar_wait(drain_bar, 0u, abort_flag, kWaitDrain);
         }
         __syncwarp();
@@ -261,7 +308,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             if (with_bias && blocks > 0 && col0 + lane < A.Nd) b_next = to_f32(bias[col0 + lane]);
             __syncwarp();
             if (residual && blocks > 0) ask(row0, col0);
-            ok = mbar_wait_warp(acc_full(a), aph, abort_flag, kWaitAccFull);
+            ok = mbar_wait_one_lane(acc_full(a), aph, abort_flag, kWaitAccFull);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -293,7 +340,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 if (with_bias && c + 1 < blocks) b_next = col0 + (c + 1) * 64 + lane < A.Nd ? to_f32(bias[col0 + (c + 1) * 64 + lane]) : 0.f;
                 const uint32_t buf = buf0 + ((residual ? rwait : blk) & 1u) * S::kBuf;
                 if (residual) {
-                    ok = mbar_wait_warp(res_full(ew, rwait & 1u), (rwait >> 1) & 1u, abort_flag, kWaitPackedFull);
+                    ok = mbar_wait_one_lane(res_full(ew, rwait & 1u), (rwait >> 1) & 1u, abort_flag, kWaitPackedFull);
                     ++rwait;
                     if (!ok) break;
                 }
@@ -526,12 +573,16 @@ struct LinPlan {
 };
 
 // Tile width and pieces along k, from the sizes alone, by an estimate in microseconds fitted to measurements
-// (M x N x K = 509 x 5120 x 4096, 32760 x 1536 x 1536, 4096^3, 200 x 3072 x 3072, every width, 1 to 4 pieces): a
-// k-block of a 256-row tile takes a pair 0.345 us per 256 columns of products, but at least 0.21 us + 0.37 ns per column to
-// bring its operands from L2 (about 50 bytes a clock per SM); a tile's epilogue 0.5 + 2 us per 256 columns, hidden under
-// the next tile's products if there is one; 2 us to fill the ring.  Pieces cost a second launch (2.5 us) and writing and
+// (M x N x K = 509 x 5120 x 4096, 32760 x 1536 x 1536, 4096^3, 200 x 3072 x 3072, 16 x 5120 x 5120, every width, 1 to 8
+// pieces): a k-block of a 256-row tile takes a pair 0.345 us per 256 columns of products, but at least what the
+// loops around it take: 0.15 us + 0.6 ns per column with a deep ring, 0.135 us + 0.83 ns with a shallow one; all of it
+// at least the time of reading both operands at 6 TB/s; a tile's epilogue 0.5 + 2 us per 256 columns, hidden under the
+// next tile's products if there is one; 2 us to fill the ring.  Pieces cost a second launch (2.5 us) and writing and
 // reading their fp32 sums in L2 (about 8 TB/s).  `step`: 32, or 64 where B is MN-major (its shared-memory tiles
 // are 64 columns wide).
+// Rows of A that a CTA loads for its half of a tile: all 128, or (one tile, one CTA with rows) those that exist.
+inline int lin_a_rows(int64_t Md) { return Md < 128 ? (int)align_up(Md, 8) : 128; }
+
 inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
     const int64_t kb = ceil_div(Kc, kLinBK), num_m = ceil_div(Md, kLinTile);
     LinPlan p;
@@ -540,14 +591,19 @@ inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
     p.part_rows = align_up(Md, 32);
     p.part_pitch = align_up(Nd, 4);
     double best = 1e300;
+    const int a_rows = lin_a_rows(Md);
+    const double memory = ((double)Md + Nd) * Kc * 2.0 / 6.0e6;
     for (int bn = kLinTile; bn >= 32 && bn % step == 0; bn -= step) {
         const int64_t tiles = num_m * ceil_div(Nd, bn);
-        const double products = 0.345 * bn / 256.0, feed = 0.21 + 0.00037 * bn;
-        const double t_kb = products > feed ? products : feed, t_epi = 0.5 + 2.0 * bn / 256.0;
+        const bool deep = LinSmem<kLinFinal>::kRing / ((a_rows + bn / 2) * kLinBK * 2) > kLinPairStages;
+        const double products = 0.345 * bn / 256.0, loops = deep ? 0.15 + 0.0006 * bn : 0.135 + 0.00083 * bn;
+        const double t_kb = products > loops ? products : loops, t_epi = 0.5 + 2.0 * bn / 256.0;
         for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
             if (s > 1 && (tiles * s > 4 * kLinPairs || s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20))) break;
             const double item = (double)ceil_div(kb, s) * t_kb;
-            double cost = (double)ceil_div(tiles * s, kLinPairs) * (item > t_epi ? item : t_epi) + 2.0 + t_epi;
+            double cost = (double)ceil_div(tiles * s, kLinPairs) * (item > t_epi ? item : t_epi);
+            if (cost < memory) cost = memory;
+            cost += 2.0 + t_epi;
             if (s > 1) cost += 2.5 + (double)s * Md * Nd * 8.0 / 8.0e6;
             if (cost < best * 0.97) { best = cost; p.bn = bn; p.splits = (int)s; }  // a wider tile reads less: prefer it when near
         }
@@ -600,7 +656,8 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
         return mn ? make_map16(m, bf, x.p, Kc, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
                   : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, (uint32_t)box, CU_TENSOR_MAP_SWIZZLE_128B);
     };
-    if (!operand(&tmA, AMN, a, Md, 128) || !operand(&tmB, BMN, b, Nd, plan.bn / 2)) return DVDQ_ERR_CUDA;
+    const int a_rows = AMN ? 128 : lin_a_rows(Md);
+    if (!operand(&tmA, AMN, a, Md, a_rows) || !operand(&tmB, BMN, b, Nd, plan.bn / 2)) return DVDQ_ERR_CUDA;
     if (OUT == kLinPartial ? !make_map_f32(&tmY, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
                            : !make_map16(&tmY, bf, y.p, Md, Nd, y.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return DVDQ_ERR_CUDA;
@@ -618,6 +675,10 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
     A.splits = plan.splits;
     A.panel = 2048 / plan.bn < A.num_n ? 2048 / plan.bn : A.num_n;
     A.part_rows = (int)plan.part_rows;
+    A.a_bytes = (int)lin_bytes<AMN>(a_rows);
+    A.b_off = (int)align_up(A.a_bytes, 1024);  // swizzle atoms are 1024 bytes
+    A.stage = A.b_off + (int)align_up(lin_bytes<BMN>(plan.bn / 2), 1024);
+    A.stages = S::kRing / A.stage < S::kMaxStages ? S::kRing / A.stage : S::kMaxStages;
     A.act = e.act;
     A.has_residual = fin && e.residual.p != nullptr;
     A.bias = fin ? e.bias : nullptr;

@@ -1,23 +1,24 @@
-// The linear layer for a few tokens (M <= 16): modulation of one conditioning vector, single decoded
-// tokens, and the gradients of such a step.
+// The linear layer for a few tokens: modulation of one conditioning vector, single decoded tokens (M <= 8), and
+// the weights' gradient of such a step (M <= 4).  With more tokens the kernel of linear.cuh is faster
+// (5120 x 5120: 17 us for 16 tokens there, 24 here with a second group of tokens, 14.6 for 4).
 //
 // What bounds it: reading W (or writing dW) once, 2 N K bytes; the products are a rounding error beside
-// that.  So W goes from memory straight into registers, 16 bytes per lane, and whatever multiplies it
-// is chosen to keep the load pipe fed:
+// that.  So W comes in 16-byte pieces per lane, always several in flight, and whatever multiplies it
+// is chosen to keep the loads going:
 //   forward  y = x W^T   warp-level mma.sync m16n8k16 with 16 rows of W as its A operand and 8 tokens as B: a dot
 //            product does not care for the order of k, so a lane's 8 consecutive values of a row fill its A
-//            slots of two MMAs, and the same 8 values of a token its B slots.  The warps of a CTA take
+//            slots of two MMAs, and the same 8 values of a token its B slots.  Warps that share channels take
 //            neighbouring pieces of k and add up through shared memory.
-//   dX = dz W            a thread keeps 8 neighbouring columns of W, walks down rows n and adds dz[m, n] W[n, k] for all m
-//   dW = dz^T x          a thread keeps 8 columns of x for all m, and writes one row of dW after another
-// dz = dy act'(z) stays in fp32 throughout.
+//   dW = dz^T x          a thread keeps 8 columns of x for all m, and writes one row of dW after another; dz = dy act'(z)
+//            stays in fp32 (so few terms would not average a rounding of dz away)
+// dX = dz W takes linear.cuh's kernel: streaming W by columns with fp32 sums was slower (18432 x 3072, 1 token: 33 us, 26 there).
 #pragma once
 
 #include "linear.cuh"
 
 namespace dvdq {
 
-constexpr int kFewTokens = 16;
+constexpr int kFewTokens = 8, kFewGradTokens = 4;
 
 // 8 elements of a row from column k on; those past K are zero (and are not read: what follows a row's last element may be anything).
 template <typename T>
@@ -39,66 +40,56 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// MT groups of 8 tokens; WARPS warps share the contraction of 16 channels.
-template <typename T, int MT, int WARPS>
+// A CTA's warps are WARPS / KS groups of 16 channels times KS neighbouring pieces of k; each
+// lane streams its two rows of W through its own ring (thread_stream), so that loads never pause.
+constexpr int kFewDepth = 6;
+template <typename T, int WARPS, int KS>
 __global__ void __launch_bounds__(WARPS * 32)
 linear_few_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ W, int64_t ldw, int M, int N, int K, int k_per_warp,
                   const T* __restrict__ bias, const T* R, int64_t ldr, int act, T* Y, int64_t ldy, T* Z, int64_t ldz) {
-    constexpr int U = 4;  // k-steps of 32 in flight: 128 bytes of W per lane
-    __shared__ float sh[WARPS][MT * 8][16];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int n0 = blockIdx.x * 16;
+    extern __shared__ __align__(16) uint8_t raw[];
     release_successor();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int piece = warp % KS, group = warp / KS;
+    const int n0 = (blockIdx.x * (WARPS / KS) + group) * 16;
     wait_predecessor();
-    // rows past N repeat the last one: their results are not stored
-    const T* w0 = W + (int64_t)min(n0 + g, N - 1) * ldw;
-    const T* w1 = W + (int64_t)min(n0 + g + 8, N - 1) * ldw;
-    float c[MT][4];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[i][j] = 0.f;
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-    const int k1 = min(K, (warp + 1) * k_per_warp);
-    auto step = [&](const uint4& a, const uint4& b, int k) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int m = i * 8 + g;
-            const uint4 x = m < M ? few_load(X + m * ldx, k, K) : none;
-            mma_16x8x16<T>(c[i], a.x, b.x, a.y, b.y, x.x, x.y);
-            mma_16x8x16<T>(c[i], a.z, b.z, a.w, b.w, x.z, x.w);
+    float c[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n0 < N) {
+        // rows past N repeat the last one: their results are not stored
+        const T* w0 = W + (int64_t)min(n0 + g, N - 1) * ldw;
+        const T* w1 = W + (int64_t)min(n0 + g + 8, N - 1) * ldw;
+        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+        int k = piece * k_per_warp + t * 8;
+        const int k1 = min(K, (piece + 1) * k_per_warp);  // k_per_warp is a multiple of 32
+        auto step = [&](const uint4& a, const uint4& b) {
+            const uint4 x = g < M ? few_load(X + g * ldx, k, K) : none;
+            mma_16x8x16<T>(c, a.x, b.x, a.y, b.y, x.x, x.y);
+            mma_16x8x16<T>(c, a.z, b.z, a.w, b.w, x.z, x.w);
+            k += 32;
+        };
+        const int whole = k1 > k - t * 8 ? (k1 - (k - t * 8)) / 32 : 0;  // steps of 32 that lie in the rows
+        thread_stream<kFewDepth, 2, T, 8, WARPS * 32>(smem_u32(raw) + threadIdx.x * 16, whole, w0 + k, 32, w1 + k, 32,
+            [&](const Vec<T, 8>& a, const Vec<T, 8>& b) { step(*reinterpret_cast<const uint4*>(&a), *reinterpret_cast<const uint4*>(&b)); });
+        if (k - t * 8 < k1) {  // the end of the rows
+            const bool in = k < K;
+            step(in ? few_load(w0, k, K) : none, in ? few_load(w1, k, K) : none);
         }
-    };
-    int k = warp * k_per_warp + t * 8;
-    for (; k - t * 8 + 32 * U <= k1; k += 32 * U) {
-        uint4 a[U], b[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            a[u] = __ldg(reinterpret_cast<const uint4*>(w0 + k + 32 * u));
-            b[u] = __ldg(reinterpret_cast<const uint4*>(w1 + k + 32 * u));
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) step(a[u], b[u], k + 32 * u);
     }
-    for (; k - t * 8 < k1; k += 32) {
-        const bool in = k < k1;  // k_per_warp is a multiple of 32: only the end of K cuts a step short
-        step(in ? few_load(w0, k, K) : none, in ? few_load(w1, k, K) : none, k);
-    }
-    // c[i] = (row g, tokens 2t, 2t + 1), (row g + 8, the same)
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        sh[warp][i * 8 + 2 * t][g] = c[i][0];
-        sh[warp][i * 8 + 2 * t + 1][g] = c[i][1];
-        sh[warp][i * 8 + 2 * t][g + 8] = c[i][2];
-        sh[warp][i * 8 + 2 * t + 1][g + 8] = c[i][3];
-    }
+    __syncthreads();  // the ring's memory becomes the sums'
+    float* sh = reinterpret_cast<float*>(raw);  // [warp][token][16]
+    constexpr int kTile = 8 * 16;
+    float* mine = sh + warp * kTile + 2 * t * 16 + g;  // c = (row g, tokens 2t, 2t + 1), (row g + 8, the same)
+    mine[0] = c[0];
+    mine[16] = c[1];
+    mine[8] = c[2];
+    mine[24] = c[3];
     __syncthreads();
-    for (int o = threadIdx.x; o < MT * 8 * 16; o += WARPS * 32) {
-        const int m = o >> 4, n = n0 + (o & 15);
+    for (int o = threadIdx.x; o < (WARPS / KS) * kTile; o += WARPS * 32) {
+        const int gr = o / kTile, r = o - gr * kTile, m = r >> 4, n = (blockIdx.x * (WARPS / KS) + gr) * 16 + (r & 15);
         if (m >= M || n >= N) continue;
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) v += sh[w][m][o & 15];
+        for (int w = 0; w < KS; ++w) v += sh[(gr * KS + w) * kTile + r];
         if (bias) v += to_f32(bias[n]);
         if (Z) Z[m * ldz + n] = from_f32<T>(v);
         v = act_value_rt(act, v);
@@ -118,85 +109,7 @@ __device__ __forceinline__ float few_dz(const T* dy, int64_t lddy, const T* z, i
 }
 
 constexpr int kFewCols = 128 * 8;  // columns of a CTA of the gradients: 128 threads, 8 each
-constexpr int kFewRows = 32;       // rows of W whose dz a CTA holds at a time
-
-// part[chunk][m][k] = sum over the chunk's rows n of dz[m, n] W[n, k]
-template <typename T, int MT>
-__global__ void __launch_bounds__(128)
-linear_few_dx_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ Z, int64_t ldz, int act, const T* __restrict__ W, int64_t ldw,
-                     int M, int N, int K, int rows, float* __restrict__ part) {
-    __shared__ float dz[kFewRows][MT];
-    const int k = blockIdx.x * kFewCols + threadIdx.x * 8;
-    const int n0 = blockIdx.y * rows, n1 = min(N, n0 + rows);
-    Pairs<8> acc[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[m].p[i] = 0ull;
-    release_successor();
-    wait_predecessor();
-    for (int nb = n0; nb < n1; nb += kFewRows) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kFewRows * MT; i += 128) {
-            const int n = nb + i / MT, m = i % MT;
-            dz[i / MT][m] = n < n1 && m < M ? few_dz(dY, lddy, Z, ldz, act, m, n) : 0.f;
-        }
-        __syncthreads();
-        if (k >= K) continue;
-        const int here = min(kFewRows, n1 - nb);
-        const T* w = W + (int64_t)nb * ldw;
-        int r = 0;
-        auto add = [&](const uint4& raw, int row) {
-            const Pairs<8> v = widen2<T, 8>(*reinterpret_cast<const Vec<T, 8>*>(&raw));
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const uint64_t d = f2_splat(dz[row][m]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m].p[i] = f2_fma(v.p[i], d, acc[m].p[i]);
-            }
-        };
-        for (; r + 8 <= here; r += 8) {
-            uint4 raw[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) raw[u] = few_load(w + (int64_t)(r + u) * ldw, k, K);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) add(raw[u], r + u);
-        }
-        for (; r < here; ++r) add(few_load(w + (int64_t)r * ldw, k, K), r);
-    }
-    if (k >= K) return;
-    float* out = part + ((int64_t)blockIdx.y * M) * align_up(K, 8) + k;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        if (m < M) {
-            float4* o = reinterpret_cast<float4*>(out + m * align_up(K, 8));  // pitch: whole groups of 8
-            o[0] = make_float4(acc[m].get(0), acc[m].get(1), acc[m].get(2), acc[m].get(3));
-            o[1] = make_float4(acc[m].get(4), acc[m].get(5), acc[m].get(6), acc[m].get(7));
-        }
-    }
-}
-// dX[m, k] = sum of the chunks, a warp for each eighth of them
-template <typename T>
-__global__ void __launch_bounds__(256) linear_few_join_kernel(const float* __restrict__ part, int chunks, int M, int K, T* __restrict__ dX, int64_t lddx) {
-    __shared__ float sh[8][33];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, k = blockIdx.x * 32 + lane, m = blockIdx.y;
-    const int64_t pitch = align_up(K, 8), step = (int64_t)M * pitch;
-    release_successor();
-    wait_predecessor();
-    float t = 0.f;
-    if (k < K) {
-        const float* p = part + m * pitch + k;
-#pragma unroll 8
-        for (int c = w; c < chunks; c += 8) t += p[c * step];
-    }
-    sh[w][lane] = t;
-    __syncthreads();
-    if (w == 0 && k < K) {
-#pragma unroll
-        for (int y = 1; y < 8; ++y) t += sh[y][lane];
-        dX[m * lddx + k] = from_f32<T>(t);
-    }
-}
+constexpr int kFewRows = 32;       // rows of dW that a CTA writes
 
 // dW[n, k] = sum over m of dz[m, n] x[m, k], and dbias[n] = sum over m of dz[m, n]
 template <typename T, int MT>
@@ -249,60 +162,42 @@ linear_few_dw_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict
 
 // ------------------------------------------------------------------ host side
 
-template <typename T, int MT, int WARPS>
+template <typename T, int WARPS, int KS>
 static cudaError_t launch_linear_few_w(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e,
                                        const LinMatrix& y, cudaStream_t st) {
-    const int per_warp = (int)align_up(ceil_div(K, WARPS), 32);
-    return launch_after(linear_few_kernel<T, MT, WARPS>, dim3((unsigned)ceil_div(N, 16)), dim3(WARPS * 32), 0, st, static_cast<const T*>(x.p), x.ld,
+    constexpr int smem = WARPS * 32 * 32 * kFewDepth;  // the rings; the sums take their place
+    auto kern = linear_few_kernel<T, WARPS, KS>;
+    static PerDevice<int> ready;
+    if (smem > 48 * 1024 &&
+        !ready.get([&](int&, int) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; }))
+        return cudaErrorInvalidValue;
+    const int per_warp = (int)align_up(ceil_div(K, KS), 32);
+    return launch_after(kern, dim3((unsigned)ceil_div(N, 16 * (WARPS / KS))), dim3(WARPS * 32), smem, st, static_cast<const T*>(x.p), x.ld,
                         static_cast<const T*>(w.p), w.ld, (int)M, (int)N, (int)K, per_warp, static_cast<const T*>(e.bias),
                         static_cast<const T*>(e.residual.p), e.residual.ld, e.act, static_cast<T*>(const_cast<void*>(y.p)), y.ld,
                         static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld);
 }
-// Sixteen warps per 16 channels where the channels alone do not fill the SMs and k is long enough to share.
+// Warps that share 16 channels (KS): as many as keep all CTAs in one wave (four of eight warps per SM): the longer a
+// warp's piece of k, the less its start and the joining weigh, but a second, partial wave costs more.  Few
+// channels and a long k: sixteen warps share them, two such CTAs per SM.
 template <typename T>
 static dvdq_status launch_linear_few(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e,
                                      const LinMatrix& y, cudaStream_t st) {
-    const bool wide = N / 16 < 148 * 4 && K >= 1024;
-    if (M <= 8)
-        return cuda_status(wide ? launch_linear_few_w<T, 1, 16>(x, w, M, N, K, e, y, st) : launch_linear_few_w<T, 1, 8>(x, w, M, N, K, e, y, st));
-    return cuda_status(wide ? launch_linear_few_w<T, 2, 16>(x, w, M, N, K, e, y, st) : launch_linear_few_w<T, 2, 8>(x, w, M, N, K, e, y, st));
-}
-
-struct FewDxPlan {
-    int chunks, rows;
-    int64_t bytes;
-};
-inline FewDxPlan few_dx_plan(int64_t M, int64_t N, int64_t K) {
-    // about six CTAs of 128 threads per SM; fewer chunks for more tokens, whose partial sums weigh more
-    const int64_t cols = ceil_div(K, kFewCols);
-    int64_t chunks = ceil_div(148 * (M <= 4 ? 6 : 3), cols);
-    const int64_t most = ceil_div(N, kFewRows);
-    if (chunks > most) chunks = most;
-    FewDxPlan p;
-    p.rows = (int)align_up(ceil_div(N, chunks), 8);
-    p.chunks = (int)ceil_div(N, p.rows);
-    p.bytes = (int64_t)p.chunks * M * align_up(K, 8) * 4;
-    return p;
+    const int64_t groups = ceil_div(N, 16), wave = 148 * 4 * 8;
+    if (groups <= 148 * 2 && K >= 1024) return cuda_status(launch_linear_few_w<T, 16, 16>(x, w, M, N, K, e, y, st));
+    if (groups * 8 <= wave) return cuda_status(launch_linear_few_w<T, 8, 8>(x, w, M, N, K, e, y, st));
+    if (groups * 4 <= wave) return cuda_status(launch_linear_few_w<T, 8, 4>(x, w, M, N, K, e, y, st));
+    if (groups * 2 <= wave) return cuda_status(launch_linear_few_w<T, 8, 2>(x, w, M, N, K, e, y, st));
+    return cuda_status(launch_linear_few_w<T, 8, 1>(x, w, M, N, K, e, y, st));
 }
 
 template <typename T, int MT>
-static dvdq_status launch_linear_few_grad(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K,
-                                          int act, const LinMatrix& dx, const LinMatrix& dw, float* db, float* part, cudaStream_t st) {
-    const T *pdy = static_cast<const T*>(dy.p), *pz = static_cast<const T*>(z.p);
-    const unsigned cols = (unsigned)ceil_div(K, kFewCols);
-    cudaError_t e = cudaSuccess;
-    if (dx.p) {
-        const FewDxPlan p = few_dx_plan(M, N, K);
-        e = launch_after(linear_few_dx_kernel<T, MT>, dim3(cols, (unsigned)p.chunks), dim3(128), 0, st, pdy, dy.ld, pz, z.ld, act,
-                         static_cast<const T*>(w.p), w.ld, (int)M, (int)N, (int)K, p.rows, part);
-        if (e == cudaSuccess)
-            e = launch_after(linear_few_join_kernel<T>, dim3((unsigned)ceil_div(K, 32), (unsigned)M), dim3(256), 0, st, part, p.chunks, (int)M, (int)K,
-                             static_cast<T*>(const_cast<void*>(dx.p)), dx.ld);
-    }
-    if (e == cudaSuccess && (dw.p || db))
-        e = launch_after(linear_few_dw_kernel<T, MT>, dim3((unsigned)ceil_div(N, kFewRows), dw.p ? cols : 1u), dim3(128), 0, st, pdy, dy.ld, pz, z.ld,
-                         act, static_cast<const T*>(x.p), x.ld, (int)M, (int)N, (int)K, static_cast<T*>(const_cast<void*>(dw.p)), dw.ld, db);
-    return cuda_status(e);
+static dvdq_status launch_linear_few_dw(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, int64_t M, int64_t N, int64_t K, int act,
+                                        const LinMatrix& dw, float* db, cudaStream_t st) {
+    const unsigned cols = dw.p ? (unsigned)ceil_div(K, kFewCols) : 1u;
+    return cuda_status(launch_after(linear_few_dw_kernel<T, MT>, dim3((unsigned)ceil_div(N, kFewRows), cols), dim3(128), 0, st,
+                                    static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p), z.ld, act, static_cast<const T*>(x.p), x.ld, (int)M,
+                                    (int)N, (int)K, static_cast<T*>(const_cast<void*>(dw.p)), dw.ld, db));
 }
 
 }  // namespace dvdq
