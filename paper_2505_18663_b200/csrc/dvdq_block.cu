@@ -34,6 +34,7 @@ static bool linear_sizes_ok(int64_t M, int64_t N, int64_t K) {
 }
 
 static int64_t dz_chunks(int64_t M, int64_t N) {
+    if (M <= 256) return 1;  // one chunk: its sums are the result, no second kernel
     int64_t c = ceil_div(148 * 6, ceil_div(N, kLinDzCols));
     const int64_t most = ceil_div(M, 32);
     c = c > most ? most : c;
@@ -43,11 +44,11 @@ struct LinBackwardPlan {
     LinPlan dx, dw;
     int64_t lddz, dz_off, sums_off, part_off, total;
     int64_t chunks, rows;
+    bool two;  // dX and dW in one launch
 };
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
     LinBackwardPlan p;
-    p.dx = lin_plan(M, K, N, 64);
-    p.dw = lin_plan(N, K, M, 64);
+    p.two = lin_plan_two(M, N, K, &p.dx, &p.dw);
     p.lddz = align_up(N, 8);
     p.rows = ceil_div(M, dz_chunks(M, N));
     p.chunks = ceil_div(M, p.rows);
@@ -59,18 +60,18 @@ static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int
 }
 
 template <typename T>
-static dvdq_status linear_t(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e, const LinMatrix& y,
-                            void* ws, cudaStream_t st) {
+static dvdq_status linear_t(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinPlan& plan, const LinEpilogue& e,
+                            const LinMatrix& y, void* ws, cudaStream_t st) {
     if (M <= kFewTokens) return launch_linear_few<T>(x, w, M, N, K, e, y, st);
-    return launch_linear<T, false, false>(x, w, M, N, K, lin_plan(M, N, K, 32), e, y, static_cast<float*>(ws), st);
+    return launch_linear<T, false, false>(x, w, M, N, K, plan, e, y, static_cast<float*>(ws), st);
 }
 
 template <typename T>
 static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N,
-                                     int64_t K, int32_t act, const LinMatrix& dx, const LinMatrix& dw, float* db, uint8_t* ws, cudaStream_t st) {
-    const LinBackwardPlan p = linear_backward_plan(M, N, K, act);
+                                     int64_t K, int32_t act, const LinBackwardPlan& p, const LinMatrix& dx, const LinMatrix& dw, float* db,
+                                     uint8_t* ws, cudaStream_t st) {
     const bool few = M <= kFewGradTokens;  // dW and dbias by their own kernel
-    float* sums = db && !few ? reinterpret_cast<float*>(ws + p.sums_off) : nullptr;
+    float* sums = !db || few ? nullptr : p.chunks == 1 ? db : reinterpret_cast<float*>(ws + p.sums_off);
     float* part = reinterpret_cast<float*>(ws + p.part_off);
     LinMatrix dz = dy;
     if (act != DVDQ_ACT_NONE) dz = LinMatrix{ws + p.dz_off, p.lddz};
@@ -83,11 +84,12 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
         if ((s = cuda_status(launch_after(k, grid, dim3(kStreamThreads), 0, st, static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p),
                                           z.ld, M, (int)N, p.rows, static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, sums))) != DVDQ_OK)
             return s;
-        if (sums && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
+        if (sums && sums != db && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
                                                 (int)N, db))) != DVDQ_OK)
             return s;
     }
     const LinEpilogue none = {};
+    if (p.two && !few && dx.p && dw.p) return launch_linear_two<T>(dz, x, w, M, N, K, p.dx, p.dw, dx, dw, st);
     if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK) return s;
     if (few && (dw.p || db))
         return M == 1 ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st) : launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st);
@@ -120,17 +122,17 @@ dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, in
         (s = check_matrix(Z, M, N, &ldz, false)) != DVDQ_OK)
         return s;
     if (bias && !aligned_to(bias, 2)) return DVDQ_ERR_ALIGN;
-    const size_t need = dvdq_linear_workspace_bytes(M, N, K);
-    if (need > 0) {
+    const LinPlan plan = M <= kFewTokens ? LinPlan{} : lin_plan(M, N, K, 32);
+    if (plan.part_bytes > 0) {
         if (!workspace) return DVDQ_ERR_NULL;
         if (!aligned_to(workspace, 256)) return DVDQ_ERR_ALIGN;
-        if (workspace_bytes < need) return DVDQ_ERR_WORKSPACE;
+        if (workspace_bytes < (size_t)plan.part_bytes) return DVDQ_ERR_WORKSPACE;
     }
     if ((s = check_device_arch()) != DVDQ_OK) return s;
     const LinMatrix x{X, ldx}, w{W, ldw}, y{Y, ldy};
     const LinEpilogue e{bias, {R, ldr}, {Z, ldz}, act};
-    return dtype == DVDQ_BF16 ? linear_t<__nv_bfloat16>(x, w, M, N, K, e, y, workspace, (cudaStream_t)stream)
-                              : linear_t<__half>(x, w, M, N, K, e, y, workspace, (cudaStream_t)stream);
+    return dtype == DVDQ_BF16 ? linear_t<__nv_bfloat16>(x, w, M, N, K, plan, e, y, workspace, (cudaStream_t)stream)
+                              : linear_t<__half>(x, w, M, N, K, plan, e, y, workspace, (cudaStream_t)stream);
 }
 
 size_t dvdq_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t act) {
@@ -160,12 +162,13 @@ dvdq_status dvdq_linear_backward(const void* dY, int64_t lddy, const void* Z, in
     }
     if (!workspace) return DVDQ_ERR_NULL;
     if (!aligned_to(workspace, 256)) return DVDQ_ERR_ALIGN;
-    if (workspace_bytes < dvdq_linear_backward_workspace_bytes(M, N, K, act)) return DVDQ_ERR_WORKSPACE;
+    const LinBackwardPlan plan = linear_backward_plan(M, N, K, act);
+    if (workspace_bytes < (size_t)plan.total) return DVDQ_ERR_WORKSPACE;
     if ((s = check_device_arch()) != DVDQ_OK) return s;
     const LinMatrix dy{dY, lddy}, z{act == DVDQ_ACT_NONE ? nullptr : Z, ldz}, x{X, ldx}, w{W, ldw}, dx{dX, lddx}, dw{dW, lddw};
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    return dtype == DVDQ_BF16 ? linear_backward_t<__nv_bfloat16>(dy, z, x, w, M, N, K, act, dx, dw, dbias, ws, (cudaStream_t)stream)
-                              : linear_backward_t<__half>(dy, z, x, w, M, N, K, act, dx, dw, dbias, ws, (cudaStream_t)stream);
+    return dtype == DVDQ_BF16 ? linear_backward_t<__nv_bfloat16>(dy, z, x, w, M, N, K, act, plan, dx, dw, dbias, ws, (cudaStream_t)stream)
+                              : linear_backward_t<__half>(dy, z, x, w, M, N, K, act, plan, dx, dw, dbias, ws, (cudaStream_t)stream);
 }
 
 // ---- rotary positions ---------------------------------------------------------------------------

@@ -147,22 +147,35 @@ __device__ __forceinline__ void tc_mma_f16_pair(uint32_t d_tmem, uint64_t a_desc
 
 // This CTA's `width` rows (or columns) of an operand's stage: one box of 64 x width, or boxes of 64 columns x 64
 // rows of k (the last one may be wider than needed); all count their bytes on the leader's barrier.
-template <bool MN>
-__device__ __forceinline__ void lin_load(uint32_t dst, const CUtensorMap* m, uint32_t bar, int k0, int r0, int width) {
-    if (!MN) {
+__device__ __forceinline__ void lin_load(bool mn, uint32_t dst, const CUtensorMap* m, uint32_t bar, int k0, int r0, int width) {
+    if (!mn) {
         tma_load_2d_pair(dst, m, bar, k0, r0);
     } else {
         tma_load_2d_pair(dst, m, bar, r0, k0);
         if (width > 64) tma_load_2d_pair(dst + kLinBK * 128, m, bar, r0 + 64, k0);
     }
 }
-template <bool MN>
-__host__ __device__ constexpr uint32_t lin_bytes(int width) { return (uint32_t)(MN ? (width + 63) / 64 * (kLinBK * 128) : width * kLinBK * 2); }
+__host__ __device__ constexpr uint32_t lin_bytes(bool mn, int width) { return (uint32_t)(mn ? (width + 63) / 64 * (kLinBK * 128) : width * kLinBK * 2); }
 
-template <typename T, bool AMN, bool BMN, int OUT>
+// One product's operands and where it goes.
+struct LinMaps {
+    CUtensorMap a, b, y;
+};
+
+// TWO: dX and dW of a small layer in one launch: neither fills the pairs, so the first items of the grid are the tiles of
+// one, the rest those of the other (each pair has one tile).  The first product's A is then K-major, the second's MN-major.
+template <typename T, bool AMN_, bool BMN, int OUT, bool TWO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
-linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
-              const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ LinArgs A) {
+linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmZ,
+              const __grid_constant__ LinArgs args1, const __grid_constant__ LinMaps maps2, const __grid_constant__ LinArgs args2) {
+    const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+    const int items1 = args1.num_m * args1.num_n * args1.splits;
+    const bool second = TWO && pair >= items1;
+    const LinMaps& maps = second ? maps2 : maps1;
+    const LinArgs& A = second ? args2 : args1;
+    const bool AMN = TWO ? second : AMN_;
+    const int items = second ? args2.num_m * args2.num_n : items1;
+    const int first_item = second ? pair - items1 : pair, item_step = TWO ? 1 << 30 : num_pairs;
     using S = LinSmem<OUT>;
     constexpr int MS = S::kMaxStages;
     const uint32_t ST = (uint32_t)A.stages, stage = (uint32_t)A.stage;
@@ -171,8 +184,6 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const uint32_t sbase = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
-    const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-    const int items = A.num_m * A.num_n * A.splits;
 
     const uint32_t bar0 = sbase + S::kBarOff;
     auto full = [&](int s) { return bar0 + 8u * s; };                    // leader's copy: both CTAs' operands are in place
@@ -209,27 +220,26 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         // (one thread that asks for both takes 460 clocks a k-block, as long as the products of a 256-wide tile)
         if (elect_one()) {
             const bool of_a = warp == 0;
-            const CUtensorMap* map = of_a ? &tmA : &tmB;
+            const CUtensorMap* map = of_a ? &maps.a : &maps.b;
             tma_prefetch_desc(map);
             const int bw = A.bn / 2;  // columns per CTA
             const uint32_t leader_full = map_to_cta(full(0), 0);
             LinRing ring(empty(0), ST, 1u);
             const uint32_t dst = sbase + (of_a ? 0 : A.b_off);
             bool ok = true;
-            for (int item = pair; ok && item < items; item += num_pairs) {
+            for (int item = first_item; ok && item < items; item += item_step) {
                 int tm, tn, piece;
                 lin_item(A, item, tm, tn, piece);
                 const int2 kr = lin_range(A, piece);
                 const int r0 = of_a ? tm * kLinTile + (int)rank * 128 : tn * A.bn + (int)rank * bw;
                 // rows past D's last need no operand: whatever lies in their stage reaches only rows that are not stored
                 const bool needed = !of_a || r0 < A.Md;
-                const uint32_t bytes = of_a ? A.a_bytes * (tm * kLinTile + 128 < A.Md ? 2u : 1u) : 2 * lin_bytes<BMN>(bw);
+                const uint32_t bytes = of_a ? A.a_bytes * (tm * kLinTile + 128 < A.Md ? 2u : 1u) : 2 * lin_bytes(BMN, bw);
                 int k0 = kr.x * kLinBK;
                 ok = ring.walk(kr.y - kr.x, abort_flag, kWaitWideEmpty, [&](uint32_t st) {
                     if (rank == 0) mbar_arrive_expect_tx(full(st), bytes);
                     if (needed) {
-                        if (of_a) lin_load<AMN>(dst + st * stage, map, leader_full + 8u * st, k0, r0, 128);
-                        else lin_load<BMN>(dst + st * stage, map, leader_full + 8u * st, k0, r0, bw);
+                        lin_load(of_a ? AMN : BMN, dst + st * stage, map, leader_full + 8u * st, k0, r0, of_a ? 128 : bw);
                     }
                     k0 += kLinBK;
                 });
@@ -244,13 +254,14 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         if (rank == 0 && elect_one()) {
             const uint32_t idesc = umma_idesc_f16(IsBf16<T>::value, AMN, BMN, kLinTile) | ((uint32_t)(A.bn >> 3) << 17);
             // 16 elements along k: 32 bytes inside a K-major swizzle row, two atoms of an MN-major tile
-            constexpr uint32_t kStepA = AMN ? 2048 / 16 : 2, kStepB = BMN ? 2048 / 16 : 2;
+            const uint32_t step_a = AMN ? 2048 / 16 : 2;
+            constexpr uint32_t kStepB = BMN ? 2048 / 16 : 2;
             const uint64_t ad0 = AMN ? umma_desc_sw128_mnmajor(sbase) : umma_desc_sw128_kmajor(sbase);
             const uint64_t bd0 = BMN ? umma_desc_sw128_mnmajor(sbase + A.b_off) : umma_desc_sw128_kmajor(sbase + A.b_off);
             LinRing ring(full(0), ST, 0u);
             uint32_t lt = 0;
             bool ok = true;
-            for (int item = pair; ok && item < items; item += num_pairs, ++lt) {
+            for (int item = first_item; ok && item < items; item += item_step, ++lt) {
                 int tm, tn, piece;
                 lin_item(A, item, tm, tn, piece);
                 const int2 kr = lin_range(A, piece);
@@ -264,7 +275,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     const uint32_t off = st * (stage >> 4);  // in the descriptors' 16-byte units
 #pragma unroll
                     for (int k = 0; k < kLinBK / 16; ++k) {
-                        tc_mma_f16_pair(d_tmem, ad0 + (off + kStepA * k), bd0 + (off + kStepB * k), idesc, add);
+                        tc_mma_f16_pair(d_tmem, ad0 + (off + step_a * k), bd0 + (off + kStepB * k), idesc, add);
                         add = 1u;
                     }
                     tc_commit_pair(empty(st), 3);
@@ -284,7 +295,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const bool residual = OUT != kLinPartial && A.has_residual;
         const bool with_bias = OUT != kLinPartial && A.bias != nullptr;
         const T* bias = static_cast<const T*>(A.bias);
-        if (lane == 0) tma_prefetch_desc(&tmY);
+        if (lane == 0) tma_prefetch_desc(&maps.y);
         uint32_t lt = 0, blk = 0, rload = 0, rwait = 0;  // output blocks so far; residual blocks asked for / taken
         bool ok = true;
         // asks for the residual of the block at (row, col) into output buffer `rload & 1`
@@ -296,7 +307,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             }
             ++rload;
         };
-        for (int item = pair; ok && item < items; item += num_pairs, ++lt) {
+        for (int item = first_item; ok && item < items; item += item_step, ++lt) {
             int tm, tn, piece;
             lin_item(A, item, tm, tn, piece);
             const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
@@ -326,7 +337,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(&tmY, buf0, col0 + c * 64, piece * A.part_rows + row0);
+                        tma_store_2d(&maps.y, buf0, col0 + c * 64, piece * A.part_rows + row0);
                         tma_store_commit();
                     }
                     continue;
@@ -398,7 +409,7 @@ linear_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    tma_store_2d(&tmY, buf, col0 + c * 64, row0);
+                    tma_store_2d(&maps.y, buf, col0 + c * 64, row0);
                     tma_store_commit();
                 }
             }
@@ -583,7 +594,17 @@ struct LinPlan {
 // Rows of A that a CTA loads for its half of a tile: all 128, or (one tile, one CTA with rows) those that exist.
 inline int lin_a_rows(int64_t Md) { return Md < 128 ? (int)align_up(Md, 8) : 128; }
 
-inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
+// The estimate for one wave (or `waves`) of pieces of `kblocks`.
+inline double lin_cost(int64_t Md, int bn, int64_t kblocks, int64_t waves, double memory) {
+    const bool deep = LinSmem<kLinFinal>::kRing / ((lin_a_rows(Md) + bn / 2) * kLinBK * 2) > kLinPairStages;
+    const double products = 0.345 * bn / 256.0, loops = deep ? 0.15 + 0.0006 * bn : 0.135 + 0.00083 * bn;
+    const double t_epi = 0.5 + 2.0 * bn / 256.0, item = (double)kblocks * (products > loops ? products : loops);
+    const double cost = (double)waves * (item > t_epi ? item : t_epi);
+    return (cost < memory ? memory : cost) + 2.0 + t_epi;
+}
+inline double lin_memory_time(int64_t Md, int64_t Nd, int64_t Kc) { return ((double)Md + Nd) * Kc * 2.0 / 6.0e6; }
+
+inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* estimate = nullptr) {
     const int64_t kb = ceil_div(Kc, kLinBK), num_m = ceil_div(Md, kLinTile);
     LinPlan p;
     p.bn = kLinTile;
@@ -591,25 +612,42 @@ inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step) {
     p.part_rows = align_up(Md, 32);
     p.part_pitch = align_up(Nd, 4);
     double best = 1e300;
-    const int a_rows = lin_a_rows(Md);
-    const double memory = ((double)Md + Nd) * Kc * 2.0 / 6.0e6;
     for (int bn = kLinTile; bn >= 32 && bn % step == 0; bn -= step) {
         const int64_t tiles = num_m * ceil_div(Nd, bn);
-        const bool deep = LinSmem<kLinFinal>::kRing / ((a_rows + bn / 2) * kLinBK * 2) > kLinPairStages;
-        const double products = 0.345 * bn / 256.0, loops = deep ? 0.15 + 0.0006 * bn : 0.135 + 0.00083 * bn;
-        const double t_kb = products > loops ? products : loops, t_epi = 0.5 + 2.0 * bn / 256.0;
         for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
             if (s > 1 && (tiles * s > 4 * kLinPairs || s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20))) break;
-            const double item = (double)ceil_div(kb, s) * t_kb;
-            double cost = (double)ceil_div(tiles * s, kLinPairs) * (item > t_epi ? item : t_epi);
-            if (cost < memory) cost = memory;
-            cost += 2.0 + t_epi;
+            double cost = lin_cost(Md, bn, ceil_div(kb, s), ceil_div(tiles * s, kLinPairs), lin_memory_time(Md, Nd, Kc));
             if (s > 1) cost += 2.5 + (double)s * Md * Nd * 8.0 / 8.0e6;
             if (cost < best * 0.97) { best = cost; p.bn = bn; p.splits = (int)s; }  // a wider tile reads less: prefer it when near
         }
     }
+    if (estimate) *estimate = best;
     p.part_bytes = p.splits > 1 ? align_up(p.splits * p.part_rows * p.part_pitch * 4, 256) : 0;
     return p;
+}
+
+// dX [M, K] (contraction N) and dW [N, K] (contraction M) side by side: the widths, or false where their tiles do not fit the
+// pairs together or one after the other is estimated to be as fast (a launch of its own: 2 us).
+inline bool lin_plan_two(int64_t M, int64_t N, int64_t K, LinPlan* dx, LinPlan* dw) {
+    double e1, e2, best = 1e300;
+    const LinPlan p1 = lin_plan(M, K, N, 64, &e1), p2 = lin_plan(N, K, M, 64, &e2);
+    *dx = p1;
+    *dw = p2;
+    for (int b1 = kLinTile; b1 >= 64; b1 -= 64)
+        for (int b2 = kLinTile; b2 >= 64; b2 -= 64) {
+            if (ceil_div(M, kLinTile) * ceil_div(K, b1) + ceil_div(N, kLinTile) * ceil_div(K, b2) > kLinPairs) continue;
+            const double c1 = lin_cost(M, b1, ceil_div(N, kLinBK), 1, lin_memory_time(M, K, N)), c2 = lin_cost(N, b2, ceil_div(M, kLinBK), 1, lin_memory_time(N, K, M));
+            const double cost = c1 > c2 ? c1 : c2;
+            if (cost < best) { best = cost; dx->bn = b1; dw->bn = b2; }
+        }
+    if (best >= e1 + e2 + 2.0) {
+        *dx = p1;
+        *dw = p2;
+        return false;
+    }
+    dx->splits = dw->splits = 1;
+    dx->part_bytes = dw->part_bytes = 0;
+    return true;
 }
 
 // A 16-bit matrix [rows, cols] with row pitch ld elements, tiles of box_rows x box_cols.
@@ -646,49 +684,59 @@ struct LinEpilogue {
     int act;
 };
 
+// Tensor maps and arguments of one product; false if a map cannot be made.
 template <typename T, bool AMN, bool BMN, int OUT>
-static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
-                                     const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
+static bool make_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan, const LinEpilogue& e,
+                        const LinMatrix& y, float* part, LinMaps* maps, LinArgs* A) {
     constexpr bool bf = IsBf16<T>::value != 0;
     using S = LinSmem<OUT>;
-    CUtensorMap tmA, tmB, tmY, tmR, tmZ;
     auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows, int box) {
         return mn ? make_map16(m, bf, x.p, Kc, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
                   : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, (uint32_t)box, CU_TENSOR_MAP_SWIZZLE_128B);
     };
     const int a_rows = AMN ? 128 : lin_a_rows(Md);
-    if (!operand(&tmA, AMN, a, Md, a_rows) || !operand(&tmB, BMN, b, Nd, plan.bn / 2)) return DVDQ_ERR_CUDA;
-    if (OUT == kLinPartial ? !make_map_f32(&tmY, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
-                           : !make_map16(&tmY, bf, y.p, Md, Nd, y.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
-        return DVDQ_ERR_CUDA;
-    tmR = tmZ = tmY;  // where unused
+    if (!operand(&maps->a, AMN, a, Md, a_rows) || !operand(&maps->b, BMN, b, Nd, plan.bn / 2)) return false;
+    if (OUT == kLinPartial ? !make_map_f32(&maps->y, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
+                           : !make_map16(&maps->y, bf, y.p, Md, Nd, y.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+        return false;
+    A->Md = (int)Md;
+    A->Nd = (int)Nd;
+    A->num_m = (int)ceil_div(Md, kLinTile);
+    A->bn = plan.bn;
+    A->num_n = (int)ceil_div(Nd, plan.bn);
+    A->kblocks = (int)ceil_div(Kc, kLinBK);
+    A->splits = plan.splits;
+    A->panel = 2048 / plan.bn < A->num_n ? 2048 / plan.bn : A->num_n;
+    A->part_rows = (int)plan.part_rows;
+    A->a_bytes = (int)lin_bytes(AMN, a_rows);
+    A->b_off = (int)align_up(A->a_bytes, 1024);  // swizzle atoms are 1024 bytes
+    A->stage = A->b_off + (int)align_up(lin_bytes(BMN, plan.bn / 2), 1024);
+    A->stages = S::kRing / A->stage < S::kMaxStages ? S::kRing / A->stage : S::kMaxStages;
+    A->act = e.act;
+    A->has_residual = OUT != kLinPartial && e.residual.p != nullptr;
+    A->bias = OUT != kLinPartial ? e.bias : nullptr;
+    return true;
+}
+
+template <typename T, bool AMN, bool BMN, int OUT>
+static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
+                                     const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
+    constexpr bool bf = IsBf16<T>::value != 0;
+    using S = LinSmem<OUT>;
+    LinMaps maps;
+    LinArgs A;
+    if (!make_linear<T, AMN, BMN, OUT>(a, b, Md, Nd, Kc, plan, e, y, part, &maps, &A)) return DVDQ_ERR_CUDA;
+    CUtensorMap tmR = maps.y, tmZ = maps.y;  // where unused
     const bool fin = OUT != kLinPartial;
     if (fin && e.residual.p && !make_map16(&tmR, bf, e.residual.p, Md, Nd, e.residual.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
     if (fin && e.z.p && !make_map16(&tmZ, bf, e.z.p, Md, Nd, e.z.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
-    LinArgs A;
-    A.Md = (int)Md;
-    A.Nd = (int)Nd;
-    A.num_m = (int)ceil_div(Md, kLinTile);
-    A.bn = plan.bn;
-    A.num_n = (int)ceil_div(Nd, plan.bn);
-    A.kblocks = (int)ceil_div(Kc, kLinBK);
-    A.splits = plan.splits;
-    A.panel = 2048 / plan.bn < A.num_n ? 2048 / plan.bn : A.num_n;
-    A.part_rows = (int)plan.part_rows;
-    A.a_bytes = (int)lin_bytes<AMN>(a_rows);
-    A.b_off = (int)align_up(A.a_bytes, 1024);  // swizzle atoms are 1024 bytes
-    A.stage = A.b_off + (int)align_up(lin_bytes<BMN>(plan.bn / 2), 1024);
-    A.stages = S::kRing / A.stage < S::kMaxStages ? S::kRing / A.stage : S::kMaxStages;
-    A.act = e.act;
-    A.has_residual = fin && e.residual.p != nullptr;
-    A.bias = fin ? e.bias : nullptr;
-    auto kern = linear_kernel<T, AMN, BMN, OUT>;
+    auto kern = linear_kernel<T, AMN, BMN, OUT, false>;
     static PerDevice<int> cache;
     const int max_pairs = resident_pairs(cache, kern, kLinThreads, S::kTotal);
     if (max_pairs == 0) return DVDQ_ERR_CUDA;
     const int64_t items = (int64_t)A.num_m * A.num_n * A.splits;
     const unsigned pairs = (unsigned)(items < max_pairs ? items : max_pairs);
-    return cuda_status(launch_after(kern, dim3(2 * pairs), dim3(kLinThreads), S::kTotal, st, tmA, tmB, tmY, tmR, tmZ, A));
+    return cuda_status(launch_after(kern, dim3(2 * pairs), dim3(kLinThreads), S::kTotal, st, maps, tmR, tmZ, A, maps, A));
 }
 
 // D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.
@@ -710,6 +758,25 @@ static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t
                                     plan.part_rows * plan.part_pitch, (int)plan.part_pitch, plan.splits, Md, (int)Nd,
                                     static_cast<const T*>(e.bias), static_cast<const T*>(e.residual.p), e.residual.ld, e.act,
                                     static_cast<T*>(const_cast<void*>(y.p)), y.ld, static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld));
+}
+
+// dX = dZ W and dW = dZ^T X of a small layer in one launch.
+template <typename T>
+static dvdq_status launch_linear_two(const LinMatrix& dz, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinPlan& p1,
+                                     const LinPlan& p2, const LinMatrix& dx, const LinMatrix& dw, cudaStream_t st) {
+    using S = LinSmem<kLinFinal>;
+    LinMaps m1, m2;
+    LinArgs a1, a2;
+    const LinEpilogue none = {};
+    if (!make_linear<T, false, true, kLinFinal>(dz, w, M, K, N, p1, none, dx, nullptr, &m1, &a1) ||
+        !make_linear<T, true, true, kLinFinal>(dz, x, N, K, M, p2, none, dw, nullptr, &m2, &a2))
+        return DVDQ_ERR_CUDA;
+    auto kern = linear_kernel<T, false, true, kLinFinal, true>;
+    static PerDevice<int> cache;
+    if (resident_pairs(cache, kern, kLinThreads, S::kTotal) == 0) return DVDQ_ERR_CUDA;
+    // each pair of the grid has one tile; pairs need not be resident together
+    const unsigned pairs = (unsigned)(a1.num_m * a1.num_n + a2.num_m * a2.num_n);
+    return cuda_status(launch_after(kern, dim3(2 * pairs), dim3(kLinThreads), S::kTotal, st, m1, m1.y, m1.y, a1, m2, a2));
 }
 
 }  // namespace dvdq
