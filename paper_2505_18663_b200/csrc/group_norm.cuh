@@ -284,8 +284,15 @@ __device__ __forceinline__ void gn_by_channel(int per, int c0, Get get, Copy cop
 #pragma unroll
         for (int i = 1; i < V; ++i) copy(i);
     } else {
+        int g = c0 / per, left = (g + 1) * per - c0;  // channels of this group still to come
 #pragma unroll
-        for (int i = 0; i < V; ++i) get(i, (c0 + i) / per);
+        for (int i = 0; i < V; ++i) {
+            get(i, g);
+            if (--left == 0) {
+                ++g;
+                left = per;
+            }
+        }
     }
 }
 template <int V>
@@ -631,7 +638,7 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
         gn_team_sums<V, THREADS, false>(A, P, s1, s2, sums);
     }
     float ga[V], be[V];
-    gn_params<V>(A, P.c0, ga, be);  // asked for before the wait
+    gn_params<V>(A, P.c0, ga, be);  // before the wait; at the start, next to the streams, 148 CTAs' reads of one line took 4 us
     gn_meet(A.arrived);
     gn_team_join<THREADS>(A, P.n, sums, [&](int g, double m1, double m2) {
         const float2 t = gn_mean_rstd((double)pivots[g], m1, m2, A.eps);
