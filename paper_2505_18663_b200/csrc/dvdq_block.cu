@@ -45,15 +45,22 @@ struct LinBackwardPlan {
     int64_t lddz, dz_off, sums_off, part_off, total;
     int64_t chunks, rows;
     bool two;  // dX and dW in one launch
+    int low;   // dz in two parts: rows M .. 2 M hold what rounding left over
 };
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
     LinBackwardPlan p;
-    p.two = lin_plan_two(M, N, K, &p.dx, &p.dw);
+    p.low = act != DVDQ_ACT_NONE && M <= kLowTokens ? (int)M : 0;
+    p.two = !p.low && lin_plan_two(M, N, K, &p.dx, &p.dw);
+    if (p.low) {
+        p.dx = lin_plan(2 * M, K, N, 64);
+        p.dx.part_bytes = lin_part_bytes(p.dx);  // fp32 sums even of one piece: two rows of them make one of dX
+        p.dw = lin_plan(N, K, M, 64);
+    }
     p.lddz = align_up(N, 8);
     p.rows = ceil_div(M, dz_chunks(M, N));
     p.chunks = ceil_div(M, p.rows);
     p.dz_off = 0;
-    p.sums_off = act == DVDQ_ACT_NONE ? 0 : align_up(M * p.lddz * 2, 256);
+    p.sums_off = act == DVDQ_ACT_NONE ? 0 : align_up((M + p.low) * p.lddz * 2, 256);
     p.part_off = p.sums_off + align_up(p.chunks * N * 4, 256);
     p.total = p.part_off + (p.dx.part_bytes > p.dw.part_bytes ? p.dx.part_bytes : p.dw.part_bytes);
     return p;
@@ -70,7 +77,7 @@ template <typename T>
 static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N,
                                      int64_t K, int32_t act, const LinBackwardPlan& p, const LinMatrix& dx, const LinMatrix& dw, float* db,
                                      uint8_t* ws, cudaStream_t st) {
-    const bool few = M <= kFewGradTokens;  // dW and dbias by their own kernel
+    const bool few = few_weight_gradient(M, N);  // dW and dbias by their own kernel
     float* sums = !db || few ? nullptr : p.chunks == 1 ? db : reinterpret_cast<float*>(ws + p.sums_off);
     float* part = reinterpret_cast<float*>(ws + p.part_off);
     LinMatrix dz = dy;
@@ -82,7 +89,7 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
                  : act == DVDQ_ACT_SILU    ? linear_dz_kernel<T, DVDQ_ACT_SILU>
                                            : linear_dz_kernel<T, DVDQ_ACT_NONE>;
         if ((s = cuda_status(launch_after(k, grid, dim3(kStreamThreads), 0, st, static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p),
-                                          z.ld, M, (int)N, p.rows, static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, sums))) != DVDQ_OK)
+                                          z.ld, M, (int)N, p.rows, static_cast<T*>(const_cast<void*>(dz.p)), dz.ld, p.low, sums))) != DVDQ_OK)
             return s;
         if (sums && sums != db && (s = cuda_status(launch_after(linear_colsum_kernel, dim3((unsigned)ceil_div(N, 32)), dim3(256), 0, st, sums, (int)p.chunks,
                                                 (int)N, db))) != DVDQ_OK)
@@ -90,9 +97,15 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
     }
     const LinEpilogue none = {};
     if (p.two && !few && dx.p && dw.p) return launch_linear_two<T>(dz, x, w, M, N, K, p.dx, p.dw, dx, dw, st);
-    if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK) return s;
+    if (p.low && dx.p) {
+        if ((s = launch_linear_out<T, false, true, kLinPartial>(dz, w, 2 * M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK ||
+            (s = launch_linear_join<T>(p.dx, p.low, M, K, none, dx, part, st)) != DVDQ_OK)
+            return s;
+    } else if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK) return s;
     if (few && (dw.p || db))
-        return M == 1 ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st) : launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st);
+        return M == 1   ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st)
+               : M <= 4 ? launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st)
+                        : launch_linear_few_dw<T, 16>(dy, z, x, M, N, K, act, dw, db, st);
     if (dw.p && (s = launch_linear<T, true, true>(dz, x, N, K, M, p.dw, none, dw, part, st)) != DVDQ_OK) return s;
     return DVDQ_OK;
 }

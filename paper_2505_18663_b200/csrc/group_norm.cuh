@@ -62,6 +62,34 @@ __device__ __forceinline__ float gn_param(const void* p, int f32, int bf16, int 
     return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[c]) : __half2float(static_cast<const __half*>(p)[c]);
 }
 
+// Sums of d and d^2 of a thread's pieces.  Squares below half a unit in the last place of a long sum are lost, and small
+// squares are the many: 250 normal values summed one after another are 2e-6 low.  So every 16 pieces the short sum moves on.
+template <int V>
+struct GnMoments {
+    Pairs<V> s1, s2, outer;
+    int n = 0;
+    __device__ __forceinline__ GnMoments() {
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = outer.p[i] = 0ull;
+    }
+    __device__ __forceinline__ void add(const Pairs<V>& x, const Pairs<V>& pivot) {
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            const uint64_t d = f2_sub(x.p[i], pivot.p[i]);
+            s1.p[i] = f2_add(s1.p[i], d);
+            s2.p[i] = f2_fma(d, d, s2.p[i]);
+        }
+        if ((++n & 15) == 0) flush();
+    }
+    __device__ __forceinline__ void flush() {
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            outer.p[i] = f2_add(outer.p[i], s2.p[i]);
+            s2.p[i] = 0ull;
+        }
+    }
+};
+
 // Where this thread works: channel vector v of its CTA's channel block, row r of `lanes` side by side.
 template <int V>
 struct GnPlace {
@@ -99,41 +127,55 @@ struct GnPlace {
     }
 };
 
-// Adds up [lanes][vecs * V] pairs in shared memory over the lanes, then over the channels of each group
-// in this block, and writes one pair per group (and per channel).
+// Adds the threads' sums over the lanes, pairwise (a long sum of equal terms loses digits, and a serial walk over a thousand
+// lanes takes 16 us).  Thread r * vecs + v of `on` threads holds channels v V ..; sum i of vector v ends in sh[i * threads + v].
+template <int V>
+__device__ __forceinline__ void gn_sum_lanes(bool on, int r, int lanes, int vecs, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
+    const int threads = lanes * vecs, t = threadIdx.x;
+    if (on) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) sh[i * threads + t] = make_float2(s1.get(i), s2.get(i));
+    }
+    __syncthreads();
+    for (int left = lanes; left > 1;) {
+        const int half = (left + 1) >> 1;
+        if (on && r < left - half) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float2 a = sh[i * threads + t], b = sh[i * threads + t + half * vecs];
+                sh[i * threads + t] = make_float2(a.x + b.x, a.y + b.y);
+            }
+        }
+        left = half;
+        __syncthreads();
+    }
+}
+
+// ... then over the channels of each group in this block, and writes one pair per group (and per channel).
 template <int V, bool PER_CHANNEL>
 __device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
-    const int width = A.vecs * V;
-    if (P.on) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) sh[P.r * width + P.v * V + i] = make_float2(s1.get(i), s2.get(i));
-    }
-    __syncthreads();
+    const int threads = A.lanes * A.vecs;
+    gn_sum_lanes<V>(P.r < A.lanes, P.r, A.lanes, A.vecs, s1, s2, sh);  // vectors past the block's end carry zeros
     const int64_t slot = (int64_t)blockIdx.y * A.chunks + blockIdx.x;
-    for (int c = threadIdx.x; c < P.here; c += kGnThreads) {
-        float2 t = sh[c];
-        for (int l = 1; l < A.lanes; ++l) {
-            const float2 u = sh[l * width + c];
-            t.x += u.x;
-            t.y += u.y;
-        }
-        if (PER_CHANNEL) {
+    auto place = [&](int c) { return (c % V) * threads + c / V; };  // of the block's channel c
+    if (PER_CHANNEL) {
+        for (int c = threadIdx.x; c < P.here; c += kGnThreads) {
+            float2 t = sh[place(c)];
             A.part_c[slot * A.C + P.cbase + c] = t;
             const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, P.cbase + c, 1.0f);
-            t.x *= g;
-            t.y *= g;
+            sh[place(c)] = make_float2(t.x * g, t.y * g);
         }
-        sh[c] = t;
+        __syncthreads();
     }
-    __syncthreads();
     const int groups = P.g1 - P.g0, span = A.bpg == 1 ? A.per : P.here;
     float2* out = A.part + slot * (A.G * A.bpg) + (A.bpg == 1 ? P.g0 : (int)blockIdx.z);
     if (span <= 8) {
         for (int g = threadIdx.x; g < groups; g += kGnThreads) {
-            float2 t = sh[g * span];
+            float2 t = sh[place(g * span)];
             for (int i = 1; i < span; ++i) {
-                t.x += sh[g * span + i].x;
-                t.y += sh[g * span + i].y;
+                const float2 u = sh[place(g * span + i)];
+                t.x += u.x;
+                t.y += u.y;
             }
             out[g] = t;
         }
@@ -141,8 +183,9 @@ __device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V
         for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
             float2 t = make_float2(0.f, 0.f);
             for (int i = threadIdx.x & 31; i < span; i += 32) {
-                t.x += sh[g * span + i].x;
-                t.y += sh[g * span + i].y;
+                const float2 u = sh[place(g * span + i)];
+                t.x += u.x;
+                t.y += u.y;
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) {
@@ -163,9 +206,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_co
     wait_predecessor();
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
-    Pairs<V> s1, s2;
-#pragma unroll
-    for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
+    GnMoments<V> sums;
     if (P.on) {
         const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
         float pv[V];
@@ -177,18 +218,12 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_co
         }
         Pairs<V> pivot;
         pivot.set(pv);
-        walk<kGnDepth, 1, T, V>(raw, P.count(A.lanes), base + P.c0 + (P.s0 + P.r) * A.xs, A.lanes * A.xs, nullptr, 0, [&](const Vec<T, V>& v) {
-            const Pairs<V> x = widen2<T, V>(v);
-#pragma unroll
-            for (int i = 0; i < Pairs<V>::N; ++i) {
-                const uint64_t d = f2_sub(x.p[i], pivot.p[i]);
-                s1.p[i] = f2_add(s1.p[i], d);
-                s2.p[i] = f2_fma(d, d, s2.p[i]);
-            }
-        });
+        walk<kGnDepth, 1, T, V>(raw, P.count(A.lanes), base + P.c0 + (P.s0 + P.r) * A.xs, A.lanes * A.xs, nullptr, 0,
+                                 [&](const Vec<T, V>& v) { sums.add(widen2<T, V>(v), pivot); });
+        sums.flush();
     }
     __syncthreads();  // the ring's memory becomes the sums'
-    gn_reduce_block<V, false>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
+    gn_reduce_block<V, false>(A, P, sums.s1, sums.outer, reinterpret_cast<float2*>(raw));
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -504,33 +539,21 @@ struct GnTeam {
 };
 
 // Adds the threads' sums over the lanes, then over each group's channels, and writes the CTA's numbers.
-// Channel i of vector v of lane r lies at [r][i][v]: neighbouring threads write neighbouring words.
 template <int V, int THREADS, bool PER_CHANNEL>
 __device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, THREADS>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
-    if (P.on) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) sh[(P.r * V + i) * A.vecs + P.v] = make_float2(s1.get(i), s2.get(i));
-    }
-    __syncthreads();
-    for (int o = threadIdx.x; o < A.C; o += THREADS) {  // o = i * vecs + v
-        float2 t = sh[o];
-        for (int l = 1; l < P.lanes; ++l) {
-            const float2 u = sh[l * A.C + o];
-            t.x += u.x;
-            t.y += u.y;
-        }
-        if (PER_CHANNEL) {
-            const int i = o / A.vecs, c = (o - i * A.vecs) * V + i;
+    const int threads = P.lanes * A.vecs;
+    gn_sum_lanes<V>(P.on, P.r, P.lanes, A.vecs, s1, s2, sh);
+    auto channel = [&](int c) -> float2& { return sh[(c % V) * threads + c / V]; };
+    if (PER_CHANNEL) {
+        for (int c = threadIdx.x; c < A.C; c += THREADS) {
+            const float2 t = channel(c);
             A.part_c[(int64_t)c * gridDim.x + blockIdx.x] = t;
             const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
-            t.x *= g;
-            t.y *= g;
+            channel(c) = make_float2(t.x * g, t.y * g);
         }
-        sh[o] = t;
+        __syncthreads();
     }
-    __syncthreads();
     float2* out = A.part + (int64_t)P.n * A.G * A.chunks + P.j;
-    auto channel = [&](int c) { return sh[(c % V) * A.vecs + c / V]; };
     if (A.per <= 8) {
         for (int g = threadIdx.x; g < A.G; g += THREADS) {
             float2 t = channel(g * A.per);
@@ -620,22 +643,14 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
     for (int g = threadIdx.x; g < A.G; g += THREADS) pivots[g] = to_f32(x[g * A.per]);
     __syncthreads();
     {
-        Pairs<V> s1, s2, pivot;
+        GnMoments<V> moments;
+        Pairs<V> pivot;
         float pv[V];
         gn_by_channel<V>(A.per, P.c0, [&](int i, int g) { pv[i] = pivots[g]; }, [&](int i) { pv[i] = pv[0]; });
         pivot.set(pv);
-#pragma unroll
-        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
-        walk.forward([&](const Vec<T, V>& in) {
-            const Pairs<V> f = widen2<T, V>(in);
-#pragma unroll
-            for (int i = 0; i < Pairs<V>::N; ++i) {
-                const uint64_t d = f2_sub(f.p[i], pivot.p[i]);
-                s1.p[i] = f2_add(s1.p[i], d);
-                s2.p[i] = f2_fma(d, d, s2.p[i]);
-            }
-        });
-        gn_team_sums<V, THREADS, false>(A, P, s1, s2, sums);
+        walk.forward([&](const Vec<T, V>& in) { moments.add(widen2<T, V>(in), pivot); });
+        moments.flush();
+        gn_team_sums<V, THREADS, false>(A, P, moments.s1, moments.outer, sums);
     }
     float ga[V], be[V];
     gn_params<V>(A, P.c0, ga, be);  // before the wait; at the start, next to the streams, 148 CTAs' reads of one line took 4 us
@@ -727,24 +742,27 @@ __global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(c
 
 // ------------------------------------------------------------------ small tensors: one launch
 
-// Sums of one float per (lane, channel) over the lanes and the channels of each group: out[g].
-__device__ __forceinline__ void gn_small_groups(const float* red, int lanes, int width, int per, int groups, float scale, float* out) {
+// Sums of one pair per (lane, channel) over the lanes and the channels of each group, in fp64: out[g].
+__device__ __forceinline__ void gn_small_groups(const float2* red, int lanes, int width, int per, int groups, double2* out) {
     __syncthreads();
     for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
-        float t = 0.f;
+        double a = 0.0, b = 0.0;
         for (int i = threadIdx.x & 31; i < lanes * per; i += 32) {
             const int l = i / per;
-            t += red[l * width + g * per + (i - l * per)];
+            const float2 u = red[l * width + g * per + (i - l * per)];
+            a += u.x;
+            b += u.y;
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-        if ((threadIdx.x & 31) == 0) out[g] = t * scale;
+        a = warp_sum(a);
+        b = warp_sum(b);
+        if ((threadIdx.x & 31) == 0) out[g] = make_double2(a, b);
     }
     __syncthreads();
 }
 
 // A CTA: `vecs` vectors of whole groups, all places of sample blockIdx.y.  Every thread keeps to the places it
-// loaded itself, so only the sums go through barriers.  Mean first, then squares about it.
+// loaded itself, so only the sums go through barriers.  The mean first, from sums about the first place's first
+// channel; then the squares about that mean.
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
@@ -753,69 +771,67 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     const bool on = r < A.lanes && v * V < here;
     const int S = (int)A.S;
     Vec<T, V>* data = reinterpret_cast<Vec<T, V>*>(raw);
-    float* red = reinterpret_cast<float*>(raw + align_up((int64_t)S * width * sizeof(T), 16));
-    float *mean = red + A.lanes * width, *rstd = mean + width;
-    const float inv = 1.0f / ((float)S * A.per);
+    float2* red = reinterpret_cast<float2*>(raw + align_up((int64_t)S * width * sizeof(T), 16));
+    double2* totals = reinterpret_cast<double2*>(red + align_up(A.lanes * width, 2));
     const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
-    float s1[V], pv[V];
     release_successor();
     wait_predecessor();
+    Pairs<V> mu, s1;
     if (on) {
+        float pv[V];
+        gn_by_channel<V>(A.per, c0, [&](int i, int g) { pv[i] = to_f32(base[g * A.per]); }, [&](int i) { pv[i] = pv[0]; });
+        mu.set(pv);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            pv[i] = to_f32(base[(c0 + i) / A.per * A.per]);
-            s1[i] = 0.f;
-        }
+        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = 0ull;
 #pragma unroll 4
         for (int s = r; s < S; s += A.lanes) {
-            const Vec<T, V> x = *reinterpret_cast<const Vec<T, V>*>(base + s * A.xs + c0);
-            data[s * A.vecs + v] = x;
+            const Vec<T, V> in = *reinterpret_cast<const Vec<T, V>*>(base + s * A.xs + c0);
+            data[s * A.vecs + v] = in;
+            const Pairs<V> x = widen2<T, V>(in);
 #pragma unroll
-            for (int i = 0; i < V; ++i) s1[i] += to_f32(x.e[i]) - pv[i];
+            for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = f2_add(s1.p[i], f2_sub(x.p[i], mu.p[i]));
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) red[r * width + v * V + i] = s1[i];
+        for (int i = 0; i < V; ++i) red[r * width + v * V + i] = make_float2(s1.get(i), 0.f);
     }
-    gn_small_groups(red, A.lanes, width, A.per, groups, inv, mean);  // about the pivot
-    float mu[V];
+    gn_small_groups(red, A.lanes, width, A.per, groups, totals);  // about the pivot
+    float mean[V], rs[V];
     if (on) {
+        const int g0 = cbase / A.per;
+        gn_by_channel<V>(A.per, c0, [&](int i, int g) { mean[i] = (float)((double)mu.get(i) + totals[g - g0].x * A.inv); },
+                         [&](int i) { mean[i] = mean[0]; });
+        mu.set(mean);
+        GnMoments<V> m;
+        for (int s = r; s < S; s += A.lanes) m.add(widen2<T, V>(data[s * A.vecs + v]), mu);
+        m.flush();
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            mu[i] = pv[i] + mean[(c0 + i) / A.per - cbase / A.per];
-            s1[i] = 0.f;
-        }
-        for (int s = r; s < S; s += A.lanes) {
-            const Vec<T, V> x = data[s * A.vecs + v];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = to_f32(x.e[i]) - mu[i];
-                s1[i] = fmaf(d, d, s1[i]);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) red[r * width + v * V + i] = s1[i];
+        for (int i = 0; i < V; ++i) red[r * width + v * V + i] = make_float2(m.s1.get(i), m.outer.get(i));
     }
-    gn_small_groups(red, A.lanes, width, A.per, groups, inv, rstd);
+    gn_small_groups(red, A.lanes, width, A.per, groups, totals);
     if (!on) return;
-    float ga[V], be[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int c = c0 + i, g = c / A.per;
-        const float rs = 1.0f / sqrtf(rstd[g - cbase / A.per] + A.eps);
-        ga[i] = rs * gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
-        be[i] = gn_param(A.beta, A.params_f32, A.params_bf16, c, 0.0f);
-        if (r == 0 && c == g * A.per) {
-            if (A.mean) A.mean[(int64_t)n * A.G + g] = mu[i];
-            if (A.rstd) A.rstd[(int64_t)n * A.G + g] = rs;
-        }
+    {
+        const int g0 = cbase / A.per;
+        gn_by_channel<V>(A.per, c0, [&](int i, int g) {
+            const double m1 = totals[g - g0].x * A.inv;  // what the mean's rounding left
+            rs[i] = gn_mean_rstd(0.0, m1, totals[g - g0].y * A.inv, A.eps).y;
+            if (r == 0 && c0 + i == g * A.per) {
+                if (A.mean) A.mean[(int64_t)n * A.G + g] = mean[i];
+                if (A.rstd) A.rstd[(int64_t)n * A.G + g] = rs[i];
+            }
+        }, [&](int i) { rs[i] = rs[0]; });
     }
+    float ga[V], be[V];
+    gn_params<V>(A, c0, ga, be);
+#pragma unroll
+    for (int i = 0; i < V; ++i) ga[i] *= rs[i];
+    const GnScale<T, V> scale(mean, ga, be);
     T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + c0;
     for (int s = r; s < S; s += A.lanes) {
-        const Vec<T, V> x = data[s * A.vecs + v];
-        float o[V];
+        const Pairs<V> x = widen2<T, V>(data[s * A.vecs + v]);
+        Pairs<V> o;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = act_value<ACT>(fmaf(to_f32(x.e[i]) - mu[i], ga[i], be[i]));
-        *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow<T, V>(o);
+        for (int i = 0; i < Pairs<V>::N; ++i) o.p[i] = act_value2<ACT, true>(scale(x.p[i], i));
+        *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow2<T, V>(o);
     }
 }
 
@@ -841,12 +857,12 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
     for (int n = 0; n < A.N; ++n) {
         float rs[V], ga[V];
         const GnGrad<T, V> K = gn_constants<T, V>(A, n, on ? c0 : cbase, rs, ga);
+        Pairs<V> s1, s2;
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
         if (on) {
-            Pairs<V> s1, s2;
             const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + c0;
             const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + c0;
-#pragma unroll
-            for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
 #pragma unroll 2
             for (int s = r; s < S; s += A.lanes) {
                 const Vec<T, V> xv = *reinterpret_cast<const Vec<T, V>*>(p + s * A.xs), dv = *reinterpret_cast<const Vec<T, V>*>(d + s * A.ds);
@@ -861,16 +877,10 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
                     s2.p[i] = f2_fma(dz, h, s2.p[i]);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) red[r * width + v * V + i] = make_float2(s1.get(i), s2.get(i));
         }
-        __syncthreads();
+        gn_sum_lanes<V>(r < A.lanes, r, A.lanes, A.vecs, s1, s2, red);
         for (int c = threadIdx.x; c < here; c += kGnThreads) {
-            float2 t = red[c];
-            for (int l = 1; l < A.lanes; ++l) {
-                t.x += red[l * width + c].x;
-                t.y += red[l * width + c].y;
-            }
+            const float2 t = red[(c % V) * (A.lanes * A.vecs) + c / V];
             // the host keeps a CTA's channels within its threads: one channel per thread
             dbeta += t.x;
             dgamma += t.y;
@@ -1016,7 +1026,7 @@ static bool gn_small_cut(GnArgs& A, bool backward, size_t* smem) {
     if (A.lanes > A.S) A.lanes = (int)A.S;
     A.blocks = (int)ceil_div(A.C, width);
     const int64_t slice = align_up(bytes, 16), red = (int64_t)A.lanes * width;
-    *smem = (size_t)(backward ? 2 * slice + (red + 2 * width) * 8 : slice + (red + 2 * width) * 4);
+    *smem = (size_t)((backward ? 2 : 1) * slice + (align_up(red, 2) + 2 * width) * 8);
     return true;
 }
 

@@ -434,10 +434,11 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
 
 // ------------------------------------------------------------------ joining the pieces
 
-// y = act(sum of the pieces + bias) + residual, four columns per thread; pieces are added in order.
+// y = act(sum of the pieces + bias) + residual, four columns per thread; pieces are added in order.  fold > 0: row m's sum is
+// that of rows m and m + fold of the pieces.
 template <typename T>
 __global__ void __launch_bounds__(256)
-linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pitch, int splits, int64_t Md, int Nd, const T* __restrict__ bias,
+linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pitch, int splits, int fold, int64_t Md, int Nd, const T* __restrict__ bias,
                    const T* residual, int64_t ldr, int act, T* y, int64_t ldy, T* z, int64_t ldz) {
     release_successor();
     wait_predecessor();
@@ -452,6 +453,12 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
         for (int k = 1; k < splits; ++k) {
             const float4 t = *reinterpret_cast<const float4*>(p + k * piece_floats);
             s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+        }
+        if (fold > 0) {
+            for (int k = 0; k < splits; ++k) {
+                const float4 t = *reinterpret_cast<const float4*>(p + (int64_t)fold * pitch + k * piece_floats);
+                s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+            }
         }
         float v[4] = {s.x, s.y, s.z, s.w};
         const int here = Nd - n < 4 ? Nd - n : 4;
@@ -485,6 +492,8 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
 
 // dz = dy act'(z) in fp32, rounded once to the operands' type for the tensor cores (an fp32 dz would cost
 // the two products half of their rate or more); the bias's gradient sums the unrounded values.
+// low > 0 (few tokens, whose roundings would not average out in dX): what the rounding left over, itself rounded, goes
+// to row m + low, and dX is formed from both.
 // A CTA takes 256 columns (8 per thread, 32 threads side by side, 8 rows at a time) of one chunk of
 // rows and writes their sums; linear_colsum_kernel adds the chunks.  act = none: dz is dy itself, only sums.
 constexpr int kLinDzCols = 256, kLinDzDepth = 5;
@@ -492,7 +501,7 @@ constexpr int kLinDzCols = 256, kLinDzDepth = 5;
 template <typename T, int ACT>
 __global__ void __launch_bounds__(kStreamThreads, 4)
 linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, int64_t M, int N, int64_t rows,
-                 T* __restrict__ dz, int64_t lddz, float* __restrict__ sums) {
+                 T* __restrict__ dz, int64_t lddz, int low, float* __restrict__ sums) {
     constexpr bool kAct = ACT != DVDQ_ACT_NONE;
     release_successor();
     wait_predecessor();
@@ -517,7 +526,14 @@ linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z
                 s.p[i] = f2_add(s.p[i], d.p[i]);
             }
             if (kAct) {
-                *reinterpret_cast<Vec<T, 8>*>(out) = narrow2<T, 8>(d);
+                const Vec<T, 8> high = narrow2<T, 8>(d);
+                *reinterpret_cast<Vec<T, 8>*>(out) = high;
+                if (low > 0) {
+                    const Pairs<8> h = widen2<T, 8>(high);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d.p[i] = f2_sub(d.p[i], h.p[i]);
+                    *reinterpret_cast<Vec<T, 8>*>(out + low * lddz) = narrow2<T, 8>(d);
+                }
                 out += 8 * lddz;
             }
         };
@@ -602,6 +618,7 @@ inline double lin_cost(int64_t Md, int bn, int64_t kblocks, int64_t waves, doubl
     const double cost = (double)waves * (item > t_epi ? item : t_epi);
     return (cost < memory ? memory : cost) + 2.0 + t_epi;
 }
+inline int64_t lin_part_bytes(const LinPlan& p) { return align_up(p.splits * p.part_rows * p.part_pitch * 4, 256); }
 inline double lin_memory_time(int64_t Md, int64_t Nd, int64_t Kc) { return ((double)Md + Nd) * Kc * 2.0 / 6.0e6; }
 
 inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* estimate = nullptr) {
@@ -622,7 +639,7 @@ inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* es
         }
     }
     if (estimate) *estimate = best;
-    p.part_bytes = p.splits > 1 ? align_up(p.splits * p.part_rows * p.part_pitch * 4, 256) : 0;
+    p.part_bytes = p.splits > 1 ? lin_part_bytes(p) : 0;
     return p;
 }
 
@@ -739,6 +756,16 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
     return cuda_status(launch_after(kern, dim3(2 * pairs), dim3(kLinThreads), S::kTotal, st, maps, tmR, tmZ, A, maps, A));
 }
 
+template <typename T>
+static dvdq_status launch_linear_join(const LinPlan& plan, int fold, int64_t Md, int64_t Nd, const LinEpilogue& e, const LinMatrix& y,
+                                      const float* part, cudaStream_t st) {
+    const int64_t ctas = ceil_div(Md * ((Nd + 3) / 4), 256);
+    return cuda_status(launch_after(linear_join_kernel<T>, dim3((unsigned)(ctas < 148 * 8 ? ctas : 148 * 8)), dim3(256), 0, st, part,
+                                    plan.part_rows * plan.part_pitch, (int)plan.part_pitch, plan.splits, fold, Md, (int)Nd,
+                                    static_cast<const T*>(e.bias), static_cast<const T*>(e.residual.p), e.residual.ld, e.act,
+                                    static_cast<T*>(const_cast<void*>(y.p)), y.ld, static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld));
+}
+
 // D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.
 template <typename T, bool AMN, bool BMN>
 static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
@@ -750,14 +777,8 @@ static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t
         }
         return launch_linear_out<T, AMN, BMN, kLinFinal>(a, b, Md, Nd, Kc, plan, e, y, part, st);
     }
-    dvdq_status s = launch_linear_out<T, AMN, BMN, kLinPartial>(a, b, Md, Nd, Kc, plan, e, y, part, st);
-    if (s != DVDQ_OK) return s;
-    const int64_t quads = Md * ((Nd + 3) / 4);
-    const int64_t ctas = ceil_div(quads, 256);
-    return cuda_status(launch_after(linear_join_kernel<T>, dim3((unsigned)(ctas < 148 * 8 ? ctas : 148 * 8)), dim3(256), 0, st, part,
-                                    plan.part_rows * plan.part_pitch, (int)plan.part_pitch, plan.splits, Md, (int)Nd,
-                                    static_cast<const T*>(e.bias), static_cast<const T*>(e.residual.p), e.residual.ld, e.act,
-                                    static_cast<T*>(const_cast<void*>(y.p)), y.ld, static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld));
+    const dvdq_status s = launch_linear_out<T, AMN, BMN, kLinPartial>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+    return s != DVDQ_OK ? s : launch_linear_join<T>(plan, 0, Md, Nd, e, y, part, st);
 }
 
 // dX = dZ W and dW = dZ^T X of a small layer in one launch.

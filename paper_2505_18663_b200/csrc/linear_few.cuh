@@ -1,5 +1,5 @@
 // The linear layer for a few tokens: modulation of one conditioning vector, single decoded tokens (M <= 8), and
-// the weights' gradient of such a step (M <= 4).  With more tokens the kernel of linear.cuh is faster
+// the weights' gradient of such a step (M <= 4, or 16 if the layer is small).  With more tokens the kernel of linear.cuh is faster
 // (5120 x 5120: 17 us for 16 tokens there, 24 here with a second group of tokens, 14.6 for 4).
 //
 // What bounds it: reading W (or writing dW) once, 2 N K bytes; the products are a rounding error beside
@@ -11,14 +11,15 @@
 //            neighbouring pieces of k and add up through shared memory.
 //   dW = dz^T x          a thread keeps 8 columns of x for all m, and writes one row of dW after another; dz = dy act'(z)
 //            stays in fp32 (so few terms would not average a rounding of dz away)
-// dX = dz W takes linear.cuh's kernel: streaming W by columns with fp32 sums was slower (18432 x 3072, 1 token: 33 us, 26 there).
+// dX = dz W takes linear.cuh's kernel, with dz in two 16-bit parts, one below the other: streaming W by columns with fp32 sums was slower (18432 x 3072, 1 token: 33 us, 26 there).
 #pragma once
 
 #include "linear.cuh"
 
 namespace dvdq {
 
-constexpr int kFewTokens = 8, kFewGradTokens = 4;
+constexpr int kFewTokens = 8;
+constexpr int kLowTokens = 32;  // dX is formed from dz in two parts up to here: the tile's 256 rows have room for both
 
 // 8 elements of a row from column k on; those past K are zero (and are not read: what follows a row's last element may be anything).
 template <typename T>
@@ -161,6 +162,10 @@ linear_few_dw_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict
 }
 
 // ------------------------------------------------------------------ host side
+
+// dW by linear_few_dw_kernel: up to 4 tokens because it is faster (5120 x 5120, 4 tokens: 13.5 us, 18.4 in linear.cuh), up to 16
+// where so few values of dz would not average their rounding out (and the matrix is small).
+inline bool few_weight_gradient(int64_t M, int64_t N) { return M <= 4 || (M <= 16 && M * N < 4096); }
 
 template <typename T, int WARPS, int KS>
 static cudaError_t launch_linear_few_w(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e,

@@ -275,3 +275,18 @@ def test_workspace_sizes():
     assert B.dvdq_group_norm_workspace_bytes(0, 10, 8, 2) == 0 and B.dvdq_group_norm_workspace_bytes(1, 10, 8, 3) == 0
     assert B.dvdq_group_norm_workspace_bytes(1, 10, 8, 2) > 0
     assert B.dvdq_group_norm_workspace_bytes(1, 499200, 128, 32) < 8 << 20
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(1, 162285, 8, 4), (2, 60000, 12, 4), (1, 3000, 8, 1), (1, 40000, 3, 1)])
+def test_small_squares_are_not_lost_in_long_sums(shape):
+    """bf16 values near the mean have squares below half a unit of a sum of some hundred terms, and they are the many: a
+    plain running fp32 sum of 1000 squares is 7e-6 low.  Sums of at most 16 terms, then pairwise, stay within 16 + 10
+    roundings of 2^-24 that partly cancel: 1e-6 for the variance, half of that for rstd."""
+    N, S, C, G = shape
+    x = (0.4 + torch.randn(N, S, C, device=DEV, generator=torch.Generator(device=DEV).manual_seed(7))).bfloat16()
+    y, mean, rstd = torch.empty_like(x), torch.empty(N, G, device=DEV), torch.empty(N, G, device=DEV)
+    B.dvdq_group_norm(x, G, None, None, EPS, 0, y, mean, rstd, workspace(*shape))
+    _, m6, r6, _, _ = norm64(x.double(), G, None, None, 0)
+    assert ((rstd - r6) / r6).abs().max() <= 5e-7
+    assert (mean - m6).abs().max() <= 2.0 ** -23
