@@ -255,19 +255,29 @@ __device__ __forceinline__ void thread_stream(uint32_t ring, int count, const T*
         slot = slot + 1 == D ? 0u : slot + 1;
     }
 }
-// The same sequence with plain loads, for accesses narrower than 16 bytes.
+// The same sequence with plain loads, sixteen (or twice eight) in flight, for accesses narrower than 16 bytes.
 template <int STREAMS, typename T, int V, typename Use>
 __device__ __forceinline__ void plain_stream(int count, const T* from0, int64_t step0, const T* from1, int64_t step1, Use use) {
-#pragma unroll 4
-    for (int k = 0; k < count; ++k) {
-        const Vec<T, V> a = *reinterpret_cast<const Vec<T, V>*>(from0);
-        from0 += step0;
-        if constexpr (STREAMS == 1) {
-            use(a);
-        } else {
-            const Vec<T, V> b = *reinterpret_cast<const Vec<T, V>*>(from1);
-            from1 += step1;
-            use(a, b);
+    constexpr int U = STREAMS == 1 ? 16 : 8;
+    for (; count > 0; count -= U) {
+        Vec<T, V> a[U], b[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u < count) {
+                a[u] = *reinterpret_cast<const Vec<T, V>*>(from0);
+                from0 += step0;
+                if (STREAMS == 2) {
+                    b[u] = *reinterpret_cast<const Vec<T, V>*>(from1);
+                    from1 += step1;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u < count) {
+                if constexpr (STREAMS == 1) use(a[u]);
+                else use(a[u], b[u]);
+            }
         }
     }
 }
@@ -287,33 +297,49 @@ __device__ __forceinline__ void store_streaming(T* p, const Vec<T, V>& v) {  // 
 // backward(): from the last piece to the first, those D from where they are, the rest through the ring again.
 template <int D, int STREAMS, int THREADS, typename T, int V>
 struct TwoWay {
-    static constexpr uint32_t kSlot = THREADS * 16, kPiece = STREAMS * kSlot;
+    static constexpr int kBytes = sizeof(Vec<T, V>);
+    static_assert(kBytes == 4 || kBytes == 8 || kBytes == 16, "what cp.async copies");
+    static constexpr uint32_t kSlot = THREADS * kBytes, kPiece = STREAMS * kSlot;
+    static constexpr size_t kRingBytes = (size_t)kPiece * D;
     uint32_t ring, zero;
     int count;
     const T *at0, *at1;      // next piece to fetch
     int64_t step0, step1;
+    __device__ __forceinline__ static void copy(uint32_t to, const T* from) {
+        if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(kBytes) : "memory");
+    }
     __device__ __forceinline__ void fill(uint32_t slot, uint32_t dep) {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + dep), "l"(at0) : "memory");
-        if constexpr (STREAMS == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + slot * kPiece + kSlot + dep), "l"(at1) : "memory");
+        copy(ring + slot * kPiece + dep, at0);
+        if constexpr (STREAMS == 2) copy(ring + slot * kPiece + kSlot + dep, at1);
     }
     __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
     __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory"); }
     // hands the slot's pieces to use(); the value returned is zero, but known only when they have been delivered
     template <typename Use>
     __device__ __forceinline__ uint32_t take(uint32_t slot, Use& use) {
-        union { uint4 w; Vec<T, V> v; } in[STREAMS];
+        union Piece { uint32_t w[kBytes / 4]; Vec<T, V> v; __device__ Piece() {} } in[STREAMS];
         uint32_t dep = 0u;
 #pragma unroll
         for (int j = 0; j < STREAMS; ++j) {
-            in[j].w = lds128(ring + slot * kPiece + j * kSlot);
-            dep ^= in[j].w.w;
+            const uint32_t at = ring + slot * kPiece + j * kSlot;
+            if constexpr (kBytes == 16) {
+                const uint4 w = lds128(at);
+                in[j].w[0] = w.x; in[j].w[1] = w.y; in[j].w[2] = w.z; in[j].w[3] = w.w;
+            } else if constexpr (kBytes == 8) {
+                const uint2 w = lds64(at);
+                in[j].w[0] = w.x; in[j].w[1] = w.y;
+            } else {
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(in[j].w[0]) : "r"(at));
+            }
+            dep ^= in[j].w[kBytes / 4 - 1];
         }
         if constexpr (STREAMS == 1) use(in[0].v);
         else use(in[0].v, in[1].v);
         return dep & zero;
     }
     __device__ __forceinline__ TwoWay(const uint8_t* raw, int n, const T* from0, int64_t s0, const T* from1, int64_t s1)
-        : ring(smem_u32(raw) + threadIdx.x * 16), count(n), at0(from0), at1(from1), step0(s0), step1(s1) {
+        : ring(smem_u32(raw) + threadIdx.x * kBytes), count(n), at0(from0), at1(from1), step0(s0), step1(s1) {
         asm volatile("mov.u32 %0, %%ntid.z;" : "=r"(zero));  // the CTAs here are one-dimensional: ntid.z == 1
         zero -= 1u;
 #pragma unroll

@@ -331,7 +331,7 @@ static dvdq_status group_norm_run(const GnArgs& A0, int64_t N, int64_t S, int32_
     if (workspace_bytes < (size_t)room.total) return DVDQ_ERR_WORKSPACE;
     dvdq_status s = check_device_arch();
     if (s != DVDQ_OK) return s;
-    const GnPlan p = gn_plan(N, S);
+    const GnPlan p = gn_plan(N, S, backward ? 2 : 4);
     A.N = (int)N;
     A.S = S;
     A.inv = 1.0 / ((double)S * A.per);

@@ -424,7 +424,7 @@ __device__ __forceinline__ GnGrad<T, V> gn_constants(const GnArgs& A, int n, int
 }
 
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads, 4) gn_grad_stats_kernel(const __grid_constant__ GnArgs A) {
+__global__ void __launch_bounds__(kGnThreads, 2) gn_grad_stats_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
     release_successor();
     wait_predecessor();
@@ -483,7 +483,7 @@ __device__ __forceinline__ GnDx<V> gn_dx(const GnArgs& A, int c0, const float2* 
 }
 
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __grid_constant__ GnArgs A) {
+__global__ void __launch_bounds__(kGnThreads, 2) gn_grad_apply_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
@@ -515,8 +515,12 @@ __global__ void __launch_bounds__(kGnThreads, 3) gn_grad_apply_kernel(const __gr
 
 // ------------------------------------------------------------------ large tensors: one cooperative launch
 
-// Threads, and slots of the ring: it and the sums fill the shared memory of an SM.
-constexpr int kGnFusedThreads = 1024, kGnFusedDepth = 9, kGnFusedGradThreads = 512, kGnFusedGradDepth = 10, kGnFusedGroups = 1024;
+// Threads, and slots of the ring: it and the sums fill the shared memory of an SM.  Channel counts that 16 bytes do not divide
+// go in pieces of 8 or 4 bytes, more of them.
+constexpr int kGnFusedThreads = 1024, kGnFusedGradThreads = 512, kGnFusedGroups = 1024;
+template <typename T, int V> struct GnDepth {
+    static constexpr int fused = 9 * 16 / (int)sizeof(Vec<T, V>), fused_grad = 10 * 16 / (int)sizeof(Vec<T, V>);
+};
 
 // The CTA's place: sample n, chunk j of `chunks`.
 template <int V, int THREADS>
@@ -633,9 +637,9 @@ __device__ __forceinline__ void gn_team_join(const GnArgs& A, int n, float2* sta
 
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __grid_constant__ GnArgs A) {
-    constexpr int THREADS = kGnFusedThreads, D = kGnFusedDepth;
+    constexpr int THREADS = kGnFusedThreads, D = GnDepth<T, V>::fused;
     extern __shared__ __align__(16) uint8_t raw[];
-    float2* sums = reinterpret_cast<float2*>(raw + THREADS * 16 * D);
+    float2* sums = reinterpret_cast<float2*>(raw + TwoWay<D, 1, THREADS, T, V>::kRingBytes);
     __shared__ float pivots[kGnFusedGroups];  // y may be x: what was subtracted is kept
     const GnTeam<V, THREADS> P(A);
     const T* x = static_cast<const T*>(A.x) + (int64_t)P.n * A.xn;
@@ -677,9 +681,9 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
 
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(const __grid_constant__ GnArgs A) {
-    constexpr int THREADS = kGnFusedGradThreads, D = kGnFusedGradDepth;
+    constexpr int THREADS = kGnFusedGradThreads, D = GnDepth<T, V>::fused_grad;
     extern __shared__ __align__(16) uint8_t raw[];
-    float2* sums = reinterpret_cast<float2*>(raw + THREADS * 32 * D);
+    float2* sums = reinterpret_cast<float2*>(raw + TwoWay<D, 2, THREADS, T, V>::kRingBytes);
     const GnTeam<V, THREADS> P(A);
     TwoWay<D, 2, THREADS, T, V> walk(raw, P.count, static_cast<const T*>(A.x) + (int64_t)P.n * A.xn + P.c0 + P.s0 * A.xs, P.lanes * A.xs,
                                      static_cast<const T*>(A.dy) + (int64_t)P.n * A.dn + P.c0 + P.s0 * A.ds, P.lanes * A.ds);
@@ -947,15 +951,15 @@ __global__ void gn_empty_kernel(float* mean, float* rstd, int64_t ng, float* dga
 // ------------------------------------------------------------------ host side
 
 // How the places and channels are cut, from the shape alone (so that the workspace can be asked for
-// without the tensors): V is decided at the call, and both widths use the same chunks.
+// without the tensors): V is decided at the call, and all widths use the same chunks.
 struct GnPlan {
     int chunks;
     int64_t rows;
 };
-inline GnPlan gn_plan(int64_t N, int64_t S) {
-    // One wave of CTAs, four per SM, over all samples; a chunk has at least 32 places, so that a small
+inline GnPlan gn_plan(int64_t N, int64_t S, int per_sm) {
+    // One wave of CTAs (four per SM forward, two backward) over all samples; a chunk has at least 32 places, so that a small
     // tensor's second pass has few partial sums to add up.
-    int64_t chunks = (148 * 4 + N - 1) / N;
+    int64_t chunks = (148 * per_sm + N - 1) / N;
     const int64_t most = ceil_div(S, 32);
     if (chunks > most) chunks = most;
     if (chunks < 1) chunks = 1;
@@ -971,7 +975,7 @@ struct GnRoom {
     int64_t pivot_off, stat_off, part_c_off, arrived_off, total;
 };
 inline GnRoom gn_room(int64_t N, int64_t S, int64_t C, int64_t G) {
-    const GnPlan p = gn_plan(N, S);
+    const GnPlan p = gn_plan(N, S, 4);
     const int64_t slots = N * p.chunks > kGnFusedCtas ? N * p.chunks : kGnFusedCtas;  // CTAs that write sums, either way
     GnRoom r;
     r.pivot_off = align_up(slots * G * gn_pieces(C / G) * 8, 256);
@@ -1077,29 +1081,37 @@ static bool launch_gn_fused(PerDevice<int>& cache, Kern kern, GnArgs A, int V, i
 }
 
 template <typename T, int V, int ACT>
-static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
+static bool launch_gn_small(GnArgs A, bool backward, cudaStream_t st, cudaError_t* e) {
     size_t smem = 0;
-    if (gn_small_cut<T, V>(A, backward, &smem)) {
-        static PerDevice<int> ready, ready_grad;
-        if (!backward) {
-            if (!gn_small_ready(ready, gn_small_kernel<T, V, ACT>)) return cudaErrorInvalidValue;
-            return launch_after(gn_small_kernel<T, V, ACT>, dim3((unsigned)A.blocks, (unsigned)A.N), dim3(kGnThreads), smem, st, A);
-        }
-        if (!gn_small_ready(ready_grad, gn_small_grad_kernel<T, V, ACT>)) return cudaErrorInvalidValue;
-        return launch_after(gn_small_grad_kernel<T, V, ACT>, dim3((unsigned)A.blocks), dim3(kGnThreads), smem, st, A);
+    if (!gn_small_cut<T, V>(A, backward, &smem)) return false;
+    static PerDevice<int> ready, ready_grad;
+    const dim3 block(kGnThreads);
+    *e = cudaErrorInvalidValue;
+    if (!backward) {
+        if (gn_small_ready(ready, gn_small_kernel<T, V, ACT>))
+            *e = launch_after(gn_small_kernel<T, V, ACT>, dim3((unsigned)A.blocks, (unsigned)A.N), block, smem, st, A);
+    } else if (gn_small_ready(ready_grad, gn_small_grad_kernel<T, V, ACT>)) {
+        *e = launch_after(gn_small_grad_kernel<T, V, ACT>, dim3((unsigned)A.blocks), block, smem, st, A);
     }
-    cudaError_t e = cudaSuccess;
-    if constexpr (WholePieces<T, V>::value) {
-        static PerDevice<int> fused, fused_grad;
-        constexpr size_t sums = (size_t)kGnFusedThreads * V * sizeof(float2), grad_sums = (size_t)kGnFusedGradThreads * V * sizeof(float2);
-        constexpr size_t ring = (size_t)kGnFusedThreads * 16 * kGnFusedDepth, grad_ring = (size_t)kGnFusedGradThreads * 32 * kGnFusedGradDepth;
-        static_assert(ring + sums + kGnFusedGroups * 4 <= 232448 && grad_ring + grad_sums <= 232448, "more than the 227 KB of shared memory a CTA can have");
-        if (!backward ? launch_gn_fused(fused, gn_fused_kernel<T, V, ACT>, A, V, kGnFusedThreads, ring + sums, kGnFusedThreads * V, st, &e)
-                      : launch_gn_fused(fused_grad, gn_fused_grad_kernel<T, V, ACT>, A, V, kGnFusedGradThreads, grad_ring + grad_sums,
-                                        kGnFusedGradThreads * V, st, &e))
-            return e;
-    }
-    const dim3 grid((unsigned)A.chunks, (unsigned)A.N, (unsigned)A.blocks);
+    return true;
+}
+
+template <typename T, int V, int ACT>
+static bool launch_gn_one(const GnArgs& A, bool backward, cudaStream_t st, cudaError_t* e) {
+    static PerDevice<int> fused, fused_grad;
+    constexpr size_t sums = (size_t)kGnFusedThreads * V * sizeof(float2), grad_sums = (size_t)kGnFusedGradThreads * V * sizeof(float2);
+    constexpr size_t ring = TwoWay<GnDepth<T, V>::fused, 1, kGnFusedThreads, T, V>::kRingBytes;
+    constexpr size_t grad_ring = TwoWay<GnDepth<T, V>::fused_grad, 2, kGnFusedGradThreads, T, V>::kRingBytes;
+    static_assert(ring + sums + kGnFusedGroups * 4 <= 232448 && grad_ring + grad_sums <= 232448, "more than the 227 KB of shared memory a CTA can have");
+    return !backward ? launch_gn_fused(fused, gn_fused_kernel<T, V, ACT>, A, V, kGnFusedThreads, ring + sums, kGnFusedThreads * V, st, e)
+                     : launch_gn_fused(fused_grad, gn_fused_grad_kernel<T, V, ACT>, A, V, kGnFusedGradThreads, grad_ring + grad_sums,
+                                       kGnFusedGradThreads * V, st, e);
+}
+
+template <typename T, int V, int ACT>
+static bool launch_gn_three(GnArgs A, bool backward, cudaStream_t st, cudaError_t* e) {
+    if (!gn_cut(A, V)) return false;
+    const dim3 grid((unsigned)A.chunks, (unsigned)A.N, (unsigned)A.blocks), block(kGnThreads);
     const unsigned group_ctas = (unsigned)ceil_div((int64_t)A.N * A.G, kGnThreads / 32);
     // the rings; the sums of pass 1 (V pairs per thread) take their place
     constexpr bool ring = WholePieces<T, V>::value;
@@ -1107,32 +1119,47 @@ static cudaError_t launch_gn_act(GnArgs A, bool backward, cudaStream_t st) {
     constexpr size_t one = ring ? (size_t)kGnThreads * 16 * kGnDepth : 0, two = ring ? (size_t)kGnThreads * 16 * 2 * kGnGradDepth : 0;
     static_assert(one <= 48 * 1024 && two <= 48 * 1024 && sums <= 48 * 1024, "more than a kernel has without asking");
     if (!backward) {
-        if ((e = launch_after(gn_stats_kernel<T, V>, grid, dim3(kGnThreads), sums > one ? sums : one, st, A)) != cudaSuccess) return e;
-        if ((e = launch_after(gn_join_kernel<false>, dim3(group_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess) return e;
-        return launch_after(gn_apply_kernel<T, V, ACT>, grid, dim3(kGnThreads), one, st, A);
+        if ((*e = launch_after(gn_stats_kernel<T, V>, grid, block, sums > one ? sums : one, st, A)) != cudaSuccess) return true;
+        if ((*e = launch_after(gn_join_kernel<false>, dim3(group_ctas), block, 0, st, A, (int)group_ctas)) != cudaSuccess) return true;
+        *e = launch_after(gn_apply_kernel<T, V, ACT>, grid, block, one, st, A);
+        return true;
     }
-    if ((e = launch_after(gn_grad_stats_kernel<T, V, ACT>, grid, dim3(kGnThreads), sums > two ? sums : two, st, A)) != cudaSuccess) return e;
+    if ((*e = launch_after(gn_grad_stats_kernel<T, V, ACT>, grid, block, sums > two ? sums : two, st, A)) != cudaSuccess) return true;
     const unsigned channel_ctas = A.dgamma || A.dbeta ? (unsigned)ceil_div(A.C, 32) : 0;
-    if ((e = launch_after(gn_join_kernel<true>, dim3(group_ctas + channel_ctas), dim3(kGnThreads), 0, st, A, (int)group_ctas)) != cudaSuccess)
-        return e;
-    return A.y ? launch_after(gn_grad_apply_kernel<T, V, ACT>, grid, dim3(kGnThreads), two, st, A) : cudaSuccess;
+    *e = launch_after(gn_join_kernel<true>, dim3(group_ctas + channel_ctas), block, 0, st, A, (int)group_ctas);
+    if (*e == cudaSuccess && A.y) *e = launch_after(gn_grad_apply_kernel<T, V, ACT>, grid, block, two, st, A);
+    return true;
 }
 
-template <typename T, int V>
-static cudaError_t launch_gn_v(const GnArgs& A, bool backward, int act, cudaStream_t st) {
-    if (act == DVDQ_ACT_GELU_TANH) return launch_gn_act<T, V, DVDQ_ACT_GELU_TANH>(A, backward, st);
-    if (act == DVDQ_ACT_SILU) return launch_gn_act<T, V, DVDQ_ACT_SILU>(A, backward, st);
-    return launch_gn_act<T, V, DVDQ_ACT_NONE>(A, backward, st);
+// `wide`: channels per access that the channel count, pitches and pointers allow.
+template <typename T, int ACT>
+static cudaError_t launch_gn_act(const GnArgs& A, int wide, bool backward, cudaStream_t st) {
+    constexpr int FULL = 16 / (int)sizeof(T);
+    cudaError_t e = cudaErrorInvalidValue;
+    if (wide == FULL) {
+        if (launch_gn_small<T, FULL, ACT>(A, backward, st, &e) || launch_gn_one<T, FULL, ACT>(A, backward, st, &e) ||
+            launch_gn_three<T, FULL, ACT>(A, backward, st, &e))
+            return e;
+    }
+    if (launch_gn_small<T, 1, ACT>(A, backward, st, &e)) return e;
+    if (wide == FULL / 2 && launch_gn_one<T, FULL / 2, ACT>(A, backward, st, &e)) return e;
+    if (wide == FULL / 4 && launch_gn_one<T, FULL / 4, ACT>(A, backward, st, &e)) return e;
+    launch_gn_three<T, 1, ACT>(A, backward, st, &e);
+    return e;
 }
 
-// Whole 16-byte accesses where channels, pitches and pointers allow it, single elements otherwise.
 template <typename T>
-static cudaError_t launch_gn_t(GnArgs A, bool backward, int act, cudaStream_t st) {
-    constexpr int V = 16 / (int)sizeof(T);
-    bool wide = A.C % V == 0 && aligned_to(A.x, 16) && aligned_to(A.y, 16) && aligned_to(A.dy, 16);
-    for (int64_t p : {A.xn, A.xs, A.yn, A.ys, A.dn, A.ds}) wide = wide && p % V == 0;
-    if (wide && gn_cut(A, V)) return launch_gn_v<T, V>(A, backward, act, st);
-    return gn_cut(A, 1) ? launch_gn_v<T, 1>(A, backward, act, st) : cudaErrorInvalidValue;
+static cudaError_t launch_gn_t(const GnArgs& A, bool backward, int act, cudaStream_t st) {
+    int wide = 16 / (int)sizeof(T);
+    for (; wide > 1; wide /= 2) {
+        const uintptr_t bytes = (uintptr_t)wide * sizeof(T);
+        bool ok = A.C % wide == 0 && aligned_to(A.x, bytes) && aligned_to(A.y, bytes) && aligned_to(A.dy, bytes);
+        for (int64_t p : {A.xn, A.xs, A.yn, A.ys, A.dn, A.ds}) ok = ok && p % wide == 0;
+        if (ok) break;
+    }
+    if (act == DVDQ_ACT_GELU_TANH) return launch_gn_act<T, DVDQ_ACT_GELU_TANH>(A, wide, backward, st);
+    if (act == DVDQ_ACT_SILU) return launch_gn_act<T, DVDQ_ACT_SILU>(A, wide, backward, st);
+    return launch_gn_act<T, DVDQ_ACT_NONE>(A, wide, backward, st);
 }
 
 }  // namespace dvdq

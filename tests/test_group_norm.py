@@ -19,10 +19,12 @@ E = 64 * 2.0 ** -24
 
 # (N, S, C, G): one place; one channel per group; groups inside a 16-byte access and across several; channel counts that
 # 16 bytes do not divide; wide rows (channel blocks); one group of many channels (cut into pieces); long samples;
-# sample counts that share the SMs evenly (one launch), leave SMs idle and exceed them (three launches)
+# sample counts that share the SMs evenly (one launch), leave SMs idle and exceed them (three launches);
+# large samples whose channels go in pieces of 8, 4 and 2 bytes
 SHAPES = [(1, 1, 32, 2), (2, 1, 24, 1), (1, 70, 8, 8), (3, 77, 180, 12), (2, 50, 64, 32), (1, 333, 30, 3), (2, 64, 7, 7), (1, 40, 2304, 32),
           (1, 9, 4160, 1), (2, 17, 600, 2), (1, 33, 5000, 8), (1, 20000, 128, 32), (4, 1000, 96, 4), (1, 3000, 5, 1),
-          (40, 1500, 64, 4), (100, 1200, 64, 4), (200, 40, 64, 8), (1, 70, 9000, 9)]
+          (40, 1500, 64, 4), (100, 1200, 64, 4), (200, 40, 64, 8), (1, 70, 9000, 9),
+          (1, 9000, 36, 4), (2, 7000, 34, 2), (1, 5000, 35, 5)]
 
 
 def act64(z, act):
