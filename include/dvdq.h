@@ -337,7 +337,7 @@ typedef enum {
  *   Z [M, N] or NULL               the pre-activation z = x W^T + bias, for the backward pass (pitch ldz)
  * fp32 accumulation on the tensor cores; bias, activation and residual in fp32, one rounding each for y and z.
  * Matrices start on 16 bytes and pitches are multiples of 8 elements (DVDQ_ERR_ALIGN); M, N and K
- * themselves are arbitrary (N, K <= 2^25), and what lies between a row's last element and the pitch is neither read nor
+ * themselves are arbitrary (N, K <= 2^25), and what lies between a row's last element and the pitch is not used and not
  * written.  The pitch of a single row is not read.  M == 0 is a no-op.  Few tokens: the contraction is
  * cut into pieces, whose fp32 sums live in the workspace (dvdq_linear_workspace_bytes, often 0; 256-byte aligned). */
 size_t dvdq_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);

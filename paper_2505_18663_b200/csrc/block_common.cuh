@@ -205,6 +205,18 @@ __device__ __forceinline__ uint64_t act_slope2(uint64_t z) {
     return f2_splat(1.0f);
 }
 
+// n / d for 32-bit n by a multiplication: m = ceil(2^(32 + s) / d) with 2^s >= d, n < 2^31.
+struct FastDiv {
+    uint32_t d, m, s;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t div) : d(div), m(0), s(0) {
+        while ((1u << s) < div) ++s;
+        const uint64_t full = (((uint64_t)1 << (32 + s)) + div - 1) / div;  // in (2^32, 2^33]: keep the low word
+        m = (uint32_t)(full - ((uint64_t)1 << 32));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)__umulhi(n, m) + n) >> s); }
+};
+
 // ------------------------------------------------------------------ streams
 
 constexpr int kStreamThreads = 256;  // threads of the CTAs that stream

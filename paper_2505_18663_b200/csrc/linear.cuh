@@ -31,19 +31,20 @@ constexpr int kLinEpiWarps = 8, kLinFirstEpi = 4;
 constexpr int kLinThreads = (kLinFirstEpi + kLinEpiWarps) * 32;
 constexpr int kLinPairs = 74;                 // CTA pairs of a B200 (148 SMs): what the split along k is planned for
 
-enum LinOut { kLinFinal = 0, kLinFinalZ = 1, kLinPartial = 2 };
+// What the kernel writes: the output; the output from a residual, or z as well; fp32 pieces.
+enum LinOut { kLinFinal = 0, kLinFinalMore = 1, kLinPartial = 2 };
 
 template <int OUT>
 struct LinSmem {
-    // storing z as well takes a third output block per epilogue warp, and 32 KB of the ring
-    static constexpr int kRing = (OUT == kLinFinalZ ? 5 : 6) * 32768;
+    // a residual that comes early, and z, take two more blocks per epilogue warp, and 32 KB of the ring
+    static constexpr int kRing = (OUT == kLinFinalMore ? 5 : 6) * 32768;
     static constexpr int kMaxStages = 16;                   // a stage is 32 KB at most; narrow tiles and few rows take less
-    static constexpr int kBufs = OUT == kLinFinalZ ? 3 : 2;
+    static constexpr int kBufs = OUT == kLinFinalMore ? 4 : 2;
     static constexpr int kBuf = 32 * 32 * 2;                // 32 x 32 outputs; fp32 partials use two as one
     static constexpr int kBufOff = kRing;
     static constexpr int kBiasOff = kBufOff + kLinEpiWarps * kBufs * kBuf;
     static constexpr int kBarOff = kBiasOff + kLinEpiWarps * 32 * 4;
-    static constexpr int kNumBars = 2 * kMaxStages + 5 + 2 * kLinEpiWarps;
+    static constexpr int kNumBars = 2 * kMaxStages + 5 + 4 * kLinEpiWarps;
     static constexpr int kMiscOff = kBarOff + kNumBars * 8;
     static constexpr int kTotal = kMiscOff + 16 + 1024;
     static_assert(kTotal <= 232448, "more than the 227 KB of shared memory a CTA can have");
@@ -55,10 +56,11 @@ struct LinArgs {
     int num_m, num_n;       // tiles
     int kblocks, splits;    // k-blocks of the contraction, pieces it is cut into
     int panel;              // column tiles walked together
+    FastDiv by_splits, by_panel_tiles, by_panel, by_last;  // pieces; tiles of a panel; columns of a panel, of the last one
     int part_rows;          // rows of one piece in the partial buffer
     int a_bytes;            // of one CTA's half of A's stage
     int stages, stage, b_off;  // of the operand ring: how many, bytes per CTA of each, where B's half begins in it
-    int act, has_residual;
+    int act, has_residual, has_z;
     const void* bias;
 };
 
@@ -105,12 +107,12 @@ struct LinRing {
 // Item -> tile and piece.  Tiles are walked in panels of `panel` column tiles, columns fastest, so that the
 // tiles in flight together share rows and columns of the operands in L2; the pieces of a tile are neighbours.
 __device__ __forceinline__ void lin_item(const LinArgs& A, int item, int& tm, int& tn, int& piece) {
-    const int tile = item / A.splits;
+    const int tile = (int)A.by_splits((uint32_t)item);
     piece = item - tile * A.splits;
-    const int per_panel = A.num_m * A.panel;
-    const int p = tile / per_panel, r = tile - p * per_panel;
-    const int w = min(A.panel, A.num_n - p * A.panel);
-    tm = r / w;
+    const int p = (int)A.by_panel_tiles((uint32_t)tile), r = tile - p * A.num_m * A.panel;
+    const bool last = (p + 1) * A.panel >= A.num_n;
+    const int w = last ? A.num_n - p * A.panel : A.panel;
+    tm = (int)(last ? A.by_last((uint32_t)r) : A.by_panel((uint32_t)r));
     tn = p * A.panel + (r - tm * w);
 }
 __device__ __forceinline__ int2 lin_range(const LinArgs& A, int piece) {  // k-blocks of a piece: never empty
@@ -162,6 +164,32 @@ struct LinMaps {
     CUtensorMap a, b, y;
 };
 
+// Walks the 32 x 32 blocks of one epilogue warp, tile after tile.
+struct LinBlocks {
+    int item, c = -1, blocks = 0, row0 = 0, col0 = 0, piece = 0;
+    bool more = true;
+    __device__ __forceinline__ void tile(const LinArgs& A, int rows_from, int half) {
+        int tm, tn;
+        lin_item(A, item, tm, tn, piece);
+        row0 = tm * kLinTile + rows_from;
+        col0 = tn * A.bn + half * 32;
+        const int width = min(A.bn, A.Nd - tn * A.bn) - half * 32;
+        blocks = row0 < A.Md && width > 0 ? (width + 63) >> 6 : 0;  // those that lie in D: columns col0, col0 + 64, ...
+    }
+    // to the next block that lies in D
+    __device__ __forceinline__ void next(const LinArgs& A, int items, int step, int rows_from, int half) {
+        if (!more || (c >= 0 && ++c < blocks)) return;
+        if (c < 0) c = 0;
+        else item += step;
+        for (; item < items; item += step) {
+            tile(A, rows_from, half);
+            c = 0;
+            if (blocks > 0) return;
+        }
+        more = false;
+    }
+};
+
 // TWO: dX and dW of a small layer in one launch: neither fills the pairs, so the first items of the grid are the tiles of
 // one, the rest those of the other (each pair has one tile).  The first product's A is then K-major, the second's MN-major.
 template <typename T, bool AMN_, bool BMN, int OUT, bool TWO>
@@ -191,7 +219,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
     auto acc_full = [&](int s) { return bar0 + 8u * (2 * MS + s); };     // one per CTA
     auto acc_empty = [&](int s) { return bar0 + 8u * (2 * MS + 2 + s); };  // leader's copy
     const uint32_t drain_bar = bar0 + 8u * (2 * MS + 4);
-    auto res_full = [&](int w, int b) { return bar0 + 8u * (2 * MS + 5 + 2 * w + b); };  // a warp's residual block has landed
+    auto res_full = [&](int w, int b) { return bar0 + 8u * (2 * MS + 5 + 4 * w + b); };  // a warp's residual block has landed
     volatile uint32_t* misc = reinterpret_cast<volatile uint32_t*>(smem + S::kMiscOff);  // [0] tmem base, [1] abort
     volatile uint32_t* abort_flag = misc + 1;
 
@@ -199,7 +227,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
         for (int s = 0; s < MS; ++s) { mbar_init(full(s), 2); mbar_init(empty(s), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(acc_full(s), 1); mbar_init(acc_empty(s), 2 * kLinEpiWarps); }
         mbar_init(drain_bar, 1);
-        for (int w = 0; w < kLinEpiWarps; ++w) { mbar_init(res_full(w, 0), 1); mbar_init(res_full(w, 1), 1); }
+        for (int w = 0; w < 4 * kLinEpiWarps; ++w) mbar_init(res_full(0, w), 1);
         misc[1] = 0u;
         fence_mbar_init();
     }
@@ -292,33 +320,44 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
         const int q = warp & 3, half = ew >> 2;  // tensor-memory lane quarter; which of every two 32-column blocks
         const uint32_t buf0 = sbase + S::kBufOff + ew * (S::kBufs * S::kBuf);
         const uint32_t c_bias = sbase + S::kBiasOff + ew * 128;
-        const bool residual = OUT != kLinPartial && A.has_residual;
+        const bool residual = OUT == kLinFinalMore && A.has_residual, with_z = OUT == kLinFinalMore && A.has_z;
         const bool with_bias = OUT != kLinPartial && A.bias != nullptr;
         const T* bias = static_cast<const T*>(A.bias);
+        // output blocks take turns in `turns` buffers; z has the last one to itself
+        const uint32_t turns = OUT == kLinFinalMore ? (with_z ? 3u : 4u) : 2u;
         if (lane == 0) tma_prefetch_desc(&maps.y);
-        uint32_t lt = 0, blk = 0, rload = 0, rwait = 0;  // output blocks so far; residual blocks asked for / taken
+        const int rows_from = (int)rank * 128 + q * 32;
+        uint32_t lt = 0;
+        uint32_t buf_i = 0;               // the next block's buffer
+        uint32_t rask = 0, rphase = 0;    // the next residual's buffer; the parity to wait for, a bit per buffer
+        uint32_t pending = 0;             // residual blocks asked for and not taken
         bool ok = true;
-        // asks for the residual of the block at (row, col) into output buffer `rload & 1`
-        auto ask = [&](int row, int col) {
+        // Asks for the residual of the next block ahead, into the buffer whose turn it is: at the start all but one, then one after
+        // each block, when that block's store is the newest and the store that used the buffer is the one before it.
+        LinBlocks ahead;
+        ahead.item = first_item;
+        auto ask = [&]() {
+            ahead.next(A, items, item_step, rows_from, half);
+            if (!ahead.more) return;
             if (lane == 0) {
-                tma_store_wait_read<0>();
-                mbar_arrive_expect_tx(res_full(ew, rload & 1u), S::kBuf);
-                tma_load_2d(buf0 + (rload & 1u) * S::kBuf, &tmR, res_full(ew, rload & 1u), col, row);
+                if (with_z) tma_store_wait_read<2>();
+                else tma_store_wait_read<1>();
+                mbar_arrive_expect_tx(res_full(ew, rask), S::kBuf);
+                tma_load_2d(buf0 + rask * S::kBuf, &tmR, res_full(ew, rask), ahead.col0 + ahead.c * 64, ahead.row0);
             }
-            ++rload;
+            rask = rask + 1 == turns ? 0u : rask + 1;
+            ++pending;
         };
-        for (int item = first_item; ok && item < items; item += item_step, ++lt) {
-            int tm, tn, piece;
-            lin_item(A, item, tm, tn, piece);
+        if (residual)
+            for (uint32_t i = 1; i < turns; ++i) ask();
+        LinBlocks b;
+        for (b.item = first_item; ok && b.item < items; b.item += item_step, ++lt) {
+            b.tile(A, rows_from, half);
             const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
-            const int row0 = tm * kLinTile + (int)rank * 128 + q * 32, col0 = tn * A.bn + half * 32;
-            // 32 x 32 blocks of this warp that lie in D: columns col0, col0 + 64, ...
-            const int width = min(A.bn, A.Nd - tn * A.bn) - half * 32;
-            const int blocks = row0 < A.Md && width > 0 ? (width + 63) >> 6 : 0;
+            const int row0 = b.row0, col0 = b.col0, blocks = b.blocks, piece = b.piece;
             float b_next = 0.f;
             if (with_bias && blocks > 0 && col0 + lane < A.Nd) b_next = to_f32(bias[col0 + lane]);
             __syncwarp();
-            if (residual && blocks > 0) ask(row0, col0);
             ok = mbar_wait_one_lane(acc_full(a), aph, abort_flag, kWaitAccFull);
             if (!ok) break;
             tc_fence_after();
@@ -342,41 +381,48 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                     }
                     continue;
                 }
-                // the block's output buffer: free once all but the newest store have been read
-                // (with a residual, ask() has waited for it)
-                if (residual && c + 1 < blocks) ask(row0, col0 + (c + 1) * 64);
-                if (!residual && lane == 0) tma_store_wait_read<1>();
+                // the block's output buffer (without a residual: else ask() has waited for it) and z's: free once all but the
+                // newest store have been read
+                if ((!residual || with_z) && lane == 0) tma_store_wait_read<1>();
                 if (with_bias) sts32f(c_bias + 4 * lane, b_next);
                 __syncwarp();
                 if (with_bias && c + 1 < blocks) b_next = col0 + (c + 1) * 64 + lane < A.Nd ? to_f32(bias[col0 + (c + 1) * 64 + lane]) : 0.f;
-                const uint32_t buf = buf0 + ((residual ? rwait : blk) & 1u) * S::kBuf;
+                const uint32_t buf = buf0 + buf_i * S::kBuf;
                 if (residual) {
-                    ok = mbar_wait_one_lane(res_full(ew, rwait & 1u), (rwait >> 1) & 1u, abort_flag, kWaitPackedFull);
-                    ++rwait;
+                    ok = mbar_wait_one_lane(res_full(ew, buf_i), (rphase >> buf_i) & 1u, abort_flag, kWaitPackedFull);
                     if (!ok) break;
+                    rphase ^= 1u << buf_i;
+                    --pending;
                 }
-                ++blk;
+                buf_i = buf_i + 1 == turns ? 0u : buf_i + 1;
                 tmem_ld_wait();
-                float v[32];
+                uint64_t v[16];  // pairs of columns
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+                for (int j = 0; j < 16; ++j) v[j] = f2_pack(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
                 if (with_bias) {
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 b = lds128f(c_bias + 4 * j);
-                        v[j] += b.x; v[j + 1] += b.y; v[j + 2] += b.z; v[j + 3] += b.w;
+                    for (int j = 0; j < 16; j += 2) {
+                        const float4 f = lds128f(c_bias + 8 * j);
+                        v[j] = f2_add(v[j], f2_pack(f.x, f.y));
+                        v[j + 1] = f2_add(v[j + 1], f2_pack(f.z, f.w));
                     }
                 }
                 // rows of 64 bytes, 16-byte chunk index XORed with (row / 2) % 4: what the swizzled TMA copies use
-                auto at = [&](uint32_t base, int j) { return base + lane * 64 + (((j >> 3) ^ ((lane >> 1) & 3)) << 4); };
-                if (OUT == kLinFinalZ) {
-                    const uint32_t zb = buf0 + 2 * S::kBuf;
-                    if (residual && lane == 0) tma_store_wait_read<0>();  // z's own buffer
-                    __syncwarp();
+                auto at = [&](uint32_t base, int j) { return base + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4); };
+                auto put = [&](uint32_t base, int j) {  // columns 8 j .. 8 j + 7
+                    uint32_t w[4];
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8)
-                        sts128(at(zb, j), pack2<T>(v[j], v[j + 1]), pack2<T>(v[j + 2], v[j + 3]), pack2<T>(v[j + 4], v[j + 5]),
-                               pack2<T>(v[j + 6], v[j + 7]));
+                    for (int t = 0; t < 4; ++t) {
+                        float lo, hi;
+                        f2_unpack(v[4 * j + t], lo, hi);
+                        w[t] = pack2<T>(lo, hi);
+                    }
+                    sts128(at(base, j), w[0], w[1], w[2], w[3]);
+                };
+                if (with_z) {
+                    const uint32_t zb = buf0 + 3 * S::kBuf;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) put(zb, j);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
@@ -386,25 +432,20 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                 }
                 if (A.act == DVDQ_ACT_GELU_TANH) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = act_value<DVDQ_ACT_GELU_TANH>(v[j]);
+                    for (int j = 0; j < 16; ++j) v[j] = act_value2<DVDQ_ACT_GELU_TANH>(v[j]);
                 } else if (A.act == DVDQ_ACT_SILU) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = act_value<DVDQ_ACT_SILU>(v[j]);
+                    for (int j = 0; j < 16; ++j) v[j] = act_value2<DVDQ_ACT_SILU>(v[j]);
                 }
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
+                for (int j = 0; j < 4; ++j) {
                     if (residual) {
                         const uint4 w = lds128(at(buf, j));
-                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+                        const Pairs<8> f = widen2<T, 8>(*reinterpret_cast<const Vec<T, 8>*>(&w));
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) {
-                            const float2 f = unpack2<T>(ws[t]);
-                            v[j + 2 * t] += f.x;
-                            v[j + 2 * t + 1] += f.y;
-                        }
+                        for (int t = 0; t < 4; ++t) v[4 * j + t] = f2_add(v[4 * j + t], f.p[t]);
                     }
-                    sts128(at(buf, j), pack2<T>(v[j], v[j + 1]), pack2<T>(v[j + 2], v[j + 3]), pack2<T>(v[j + 4], v[j + 5]),
-                           pack2<T>(v[j + 6], v[j + 7]));
+                    put(buf, j);
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -412,6 +453,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                     tma_store_2d(&maps.y, buf, col0 + c * 64, row0);
                     tma_store_commit();
                 }
+                if (residual) ask();
             }
             tc_fence_before();
             __syncwarp();
@@ -419,9 +461,11 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
         }
         if (lane == 0) {
             tma_store_wait_all();
-            // gave up with a residual block in flight: let it land (bounded) before the CTA exits
-            for (; rwait < rload; ++rwait)
-                for (int it = 0; it < (1 << 16) && !mbar_try_wait(res_full(ew, rwait & 1u), (rwait >> 1) & 1u); ++it) {}
+            // gave up with residual blocks in flight: let them land (bounded) before the CTA exits
+            for (; pending > 0; --pending) {
+                for (int it = 0; it < (1 << 16) && !mbar_try_wait(res_full(ew, buf_i), (rphase >> buf_i) & 1u); ++it) {}
+                buf_i = buf_i + 1 == turns ? 0u : buf_i + 1;
+            }
         }
         __syncwarp();
     }
@@ -537,25 +581,20 @@ linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z
                 out += 8 * lddz;
             }
         };
-        if (here == 8) {
-            const T *pd = dy + mt * lddy + n, *pz = z + mt * ldz + n;
-            if constexpr (kAct) walk<kLinDzDepth, 2, T, 8>(raw, count, pd, 8 * lddy, pz, 8 * ldz, row);
-            else walk<kLinDzDepth, 1, T, 8>(raw, count, pd, 8 * lddy, pd, 0, [&](const Vec<T, 8>& dv) { row(dv, dv); });
-        } else {
-            // only the first N values of a row are the caller's: the last group goes element by element
-            // (dz is the workspace's: whole groups may be written)
-            for (int64_t m = mt; m < m1; m += 8) {
-                Vec<T, 8> d, zz;
-                for (int j = 0; j < 8; ++j) {
-                    d.e[j] = from_f32<T>(0.f);
-                    zz.e[j] = from_f32<T>(0.f);
-                    if (j < here) {
-                        d.e[j] = dy[m * lddy + n + j];
-                        if (kAct) zz.e[j] = z[m * ldz + n + j];
-                    }
-                }
-                row(d, zz);
+        const T *pd = dy + mt * lddy + n, *pz = z + mt * ldz + n;
+        // Past the last column a row's 16 bytes hold what lies between it and the next row: read, but used by nobody (dz
+        // is the workspace's, whole groups may be written).  The matrix's very last row has no next row: element by element.
+        const int streamed = here < 8 && mt + (int64_t)(count - 1) * 8 == M - 1 ? count - 1 : count;
+        if constexpr (kAct) walk<kLinDzDepth, 2, T, 8>(raw, streamed, pd, 8 * lddy, pz, 8 * ldz, row);
+        else walk<kLinDzDepth, 1, T, 8>(raw, streamed, pd, 8 * lddy, pd, 0, [&](const Vec<T, 8>& dv) { row(dv, dv); });
+        if (streamed < count) {
+            Vec<T, 8> d, zz;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                d.e[j] = j < here ? dy[(M - 1) * lddy + n + j] : from_f32<T>(0.f);
+                zz.e[j] = kAct && j < here ? z[(M - 1) * ldz + n + j] : from_f32<T>(0.f);
             }
+            row(d, zz);
         }
     }
     if (sums) {
@@ -724,13 +763,18 @@ static bool make_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int6
     A->kblocks = (int)ceil_div(Kc, kLinBK);
     A->splits = plan.splits;
     A->panel = 2048 / plan.bn < A->num_n ? 2048 / plan.bn : A->num_n;
+    A->by_splits = FastDiv((uint32_t)A->splits);
+    A->by_panel_tiles = FastDiv((uint32_t)(A->num_m * A->panel));
+    A->by_panel = FastDiv((uint32_t)A->panel);
+    A->by_last = FastDiv((uint32_t)(A->num_n - (A->num_n - 1) / A->panel * A->panel));
     A->part_rows = (int)plan.part_rows;
     A->a_bytes = (int)lin_bytes(AMN, a_rows);
     A->b_off = (int)align_up(A->a_bytes, 1024);  // swizzle atoms are 1024 bytes
     A->stage = A->b_off + (int)align_up(lin_bytes(BMN, plan.bn / 2), 1024);
     A->stages = S::kRing / A->stage < S::kMaxStages ? S::kRing / A->stage : S::kMaxStages;
     A->act = e.act;
-    A->has_residual = OUT != kLinPartial && e.residual.p != nullptr;
+    A->has_residual = OUT == kLinFinalMore && e.residual.p != nullptr;
+    A->has_z = OUT == kLinFinalMore && e.z.p != nullptr;
     A->bias = OUT != kLinPartial ? e.bias : nullptr;
     return true;
 }
@@ -744,7 +788,7 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
     LinArgs A;
     if (!make_linear<T, AMN, BMN, OUT>(a, b, Md, Nd, Kc, plan, e, y, part, &maps, &A)) return DVDQ_ERR_CUDA;
     CUtensorMap tmR = maps.y, tmZ = maps.y;  // where unused
-    const bool fin = OUT != kLinPartial;
+    const bool fin = OUT == kLinFinalMore;
     if (fin && e.residual.p && !make_map16(&tmR, bf, e.residual.p, Md, Nd, e.residual.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
     if (fin && e.z.p && !make_map16(&tmZ, bf, e.z.p, Md, Nd, e.z.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
     auto kern = linear_kernel<T, AMN, BMN, OUT, false>;
@@ -771,9 +815,9 @@ template <typename T, bool AMN, bool BMN>
 static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
                                  const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
     if (plan.splits == 1) {
-        // only the forward product stores its pre-activation
+        // only the forward product has a residual or stores its pre-activation
         if constexpr (!AMN && !BMN) {
-            if (e.z.p) return launch_linear_out<T, AMN, BMN, kLinFinalZ>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+            if (e.z.p || e.residual.p) return launch_linear_out<T, AMN, BMN, kLinFinalMore>(a, b, Md, Nd, Kc, plan, e, y, part, st);
         }
         return launch_linear_out<T, AMN, BMN, kLinFinal>(a, b, Md, Nd, Kc, plan, e, y, part, st);
     }
