@@ -764,6 +764,34 @@ __device__ __forceinline__ void gn_small_groups(const float2* red, int lanes, in
     __syncthreads();
 }
 
+// Brings a thread's pieces (places r, r + lanes, ...) into shared memory, all in flight together; gn_small_brought() waits for them.
+template <typename T, int V>
+__device__ __forceinline__ void gn_small_bring(bool on, int r, int lanes, int S, const T* from, int64_t pitch, Vec<T, V>* to, int vecs) {
+    if (!on) return;
+    if constexpr (sizeof(Vec<T, V>) >= 4) {
+        for (int s = r; s < S; s += lanes) {
+            const uint32_t at = smem_u32(to + s * vecs);
+            if constexpr (sizeof(Vec<T, V>) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from + s * pitch) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at), "l"(from + s * pitch) : "memory");
+        }
+    } else {
+        constexpr int U = 16;
+        for (int s = r; s < S; s += U * lanes) {
+            Vec<T, V> in[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u * lanes < S) in[u] = *reinterpret_cast<const Vec<T, V>*>(from + (s + u * lanes) * pitch);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u * lanes < S) to[(s + u * lanes) * vecs] = in[u];
+        }
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void gn_small_brought() {
+    if constexpr (sizeof(Vec<T, V>) >= 4) asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
 // A CTA: `vecs` vectors of whole groups, all places of sample blockIdx.y.  Every thread keeps to the places it
 // loaded itself, so only the sums go through barriers.  The mean first, from sums about the first place's first
 // channel; then the squares about that mean.
@@ -781,17 +809,16 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     release_successor();
     wait_predecessor();
     Pairs<V> mu, s1;
+    gn_small_bring<T, V>(on, r, A.lanes, S, base + c0, A.xs, data + v, A.vecs);
     if (on) {
         float pv[V];
         gn_by_channel<V>(A.per, c0, [&](int i, int g) { pv[i] = to_f32(base[g * A.per]); }, [&](int i) { pv[i] = pv[0]; });
         mu.set(pv);
 #pragma unroll
         for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = 0ull;
-#pragma unroll 4
+        gn_small_brought<T, V>();
         for (int s = r; s < S; s += A.lanes) {
-            const Vec<T, V> in = *reinterpret_cast<const Vec<T, V>*>(base + s * A.xs + c0);
-            data[s * A.vecs + v] = in;
-            const Pairs<V> x = widen2<T, V>(in);
+            const Pairs<V> x = widen2<T, V>(data[s * A.vecs + v]);
 #pragma unroll
             for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = f2_add(s1.p[i], f2_sub(x.p[i], mu.p[i]));
         }
@@ -839,12 +866,11 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     }
 }
 
-// Its gradients: the CTA takes its channels of every sample in turn, so that the parameters' gradients
-// need no second kernel.
+// Its gradients; the parameters' are final where there is one sample, and otherwise left in part_c [N, C] for gn_small_join_kernel.
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
-    const int width = A.vecs * V, v = threadIdx.x % A.vecs, r = threadIdx.x / A.vecs;
+    const int width = A.vecs * V, v = threadIdx.x % A.vecs, r = threadIdx.x / A.vecs, n = blockIdx.y;
     const int cbase = blockIdx.x * width, here = min(A.C - cbase, width), groups = here / A.per, c0 = cbase + v * V;
     const bool on = r < A.lanes && v * V < here;
     const int S = (int)A.S;
@@ -854,85 +880,89 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
     float2* red = reinterpret_cast<float2*>(raw + 2 * slice);
     float2* sums = red + A.lanes * width;   // per channel
     float2* gsum = sums + width;            // per group
-    double dgamma = 0.0, dbeta = 0.0;       // of channel cbase + threadIdx.x
-    const float inv = 1.0f / ((float)S * A.per);
     release_successor();
     wait_predecessor();
+    const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + c0;
+    const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + c0;
+    // everything of this thread at once; it reads only what it brought itself
+    gn_small_bring<T, V>(on, r, A.lanes, S, p, A.xs, xd + v, A.vecs);
+    gn_small_bring<T, V>(on, r, A.lanes, S, d, A.ds, dd + v, A.vecs);
+    float rs[V], ga[V];
+    const GnGrad<T, V> K = gn_constants<T, V>(A, n, on ? c0 : cbase, rs, ga);
+    gn_small_brought<T, V>();
+    Pairs<V> s1, s2;
+#pragma unroll
+    for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
+    if (on) {
+        for (int s = r; s < S; s += A.lanes) {
+            const Pairs<V> x = widen2<T, V>(xd[s * A.vecs + v]), dy = widen2<T, V>(dd[s * A.vecs + v]);
+#pragma unroll
+            for (int i = 0; i < Pairs<V>::N; ++i) {
+                uint64_t dz, h;
+                K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+                s1.p[i] = f2_add(s1.p[i], dz);
+                s2.p[i] = f2_fma(dz, h, s2.p[i]);
+            }
+        }
+    }
+    gn_sum_lanes<V>(r < A.lanes, r, A.lanes, A.vecs, s1, s2, red);
+    for (int c = threadIdx.x; c < here; c += kGnThreads) {
+        const float2 t = red[(c % V) * (A.lanes * A.vecs) + c / V];
+        if (A.N > 1) {
+            A.part_c[(int64_t)n * A.C + cbase + c] = t;
+        } else {
+            if (A.dbeta) A.dbeta[cbase + c] = t.x;
+            if (A.dgamma) A.dgamma[cbase + c] = t.y;
+        }
+        const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, cbase + c, 1.0f);
+        sums[c] = make_float2(t.x * g, t.y * g);
+    }
+    __syncthreads();
+    const float inv = (float)A.inv;
+    for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
+        float2 t = make_float2(0.f, 0.f);
+        for (int i = threadIdx.x & 31; i < A.per; i += 32) {
+            t.x += sums[g * A.per + i].x;
+            t.y += sums[g * A.per + i].y;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
+            t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
+        }
+        if ((threadIdx.x & 31) == 0) gsum[g] = make_float2(t.x * inv, t.y * inv);
+    }
+    __syncthreads();
+    if (!on || !A.y) return;
+    T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + c0;
+    const GnDx<V> dx = gn_dx<V>(A, c0, gsum - cbase / A.per, rs, ga);
+    for (int s = r; s < S; s += A.lanes) {
+        const Pairs<V> x = widen2<T, V>(xd[s * A.vecs + v]), dy = widen2<T, V>(dd[s * A.vecs + v]);
+        Pairs<V> o;
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            uint64_t dz, h;
+            K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
+            o.p[i] = dx(dz, h, i);
+        }
+        *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow2<T, V>(o);
+    }
+}
+
+__global__ void __launch_bounds__(kGnThreads) gn_small_join_kernel(const __grid_constant__ GnArgs A) {
+    const int c = blockIdx.x * kGnThreads + threadIdx.x;
+    release_successor();
+    wait_predecessor();
+    if (c >= A.C) return;
+    double a = 0.0, b = 0.0;
+#pragma unroll 8
     for (int n = 0; n < A.N; ++n) {
-        float rs[V], ga[V];
-        const GnGrad<T, V> K = gn_constants<T, V>(A, n, on ? c0 : cbase, rs, ga);
-        Pairs<V> s1, s2;
-#pragma unroll
-        for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
-        if (on) {
-            const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + c0;
-            const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + c0;
-#pragma unroll 2
-            for (int s = r; s < S; s += A.lanes) {
-                const Vec<T, V> xv = *reinterpret_cast<const Vec<T, V>*>(p + s * A.xs), dv = *reinterpret_cast<const Vec<T, V>*>(d + s * A.ds);
-                xd[s * A.vecs + v] = xv;
-                dd[s * A.vecs + v] = dv;
-                const Pairs<V> x = widen2<T, V>(xv), dy = widen2<T, V>(dv);
-#pragma unroll
-                for (int i = 0; i < Pairs<V>::N; ++i) {
-                    uint64_t dz, h;
-                    K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
-                    s1.p[i] = f2_add(s1.p[i], dz);
-                    s2.p[i] = f2_fma(dz, h, s2.p[i]);
-                }
-            }
-        }
-        gn_sum_lanes<V>(r < A.lanes, r, A.lanes, A.vecs, s1, s2, red);
-        for (int c = threadIdx.x; c < here; c += kGnThreads) {
-            const float2 t = red[(c % V) * (A.lanes * A.vecs) + c / V];
-            // the host keeps a CTA's channels within its threads: one channel per thread
-            dbeta += t.x;
-            dgamma += t.y;
-            const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, cbase + c, 1.0f);
-            sums[c] = make_float2(t.x * g, t.y * g);
-        }
-        __syncthreads();
-        for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
-            float2 t = make_float2(0.f, 0.f);
-            for (int i = threadIdx.x & 31; i < A.per; i += 32) {
-                t.x += sums[g * A.per + i].x;
-                t.y += sums[g * A.per + i].y;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
-                t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
-            }
-            if ((threadIdx.x & 31) == 0) gsum[g] = make_float2(t.x * inv, t.y * inv);
-        }
-        __syncthreads();
-        if (on && A.y) {
-            T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + c0;
-            float m1[V], m2[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 t = gsum[(c0 + i) / A.per - cbase / A.per];
-                m1[i] = t.x;
-                m2[i] = t.y;
-            }
-            const GnDx<V> dx(rs, ga, m1, m2);
-            for (int s = r; s < S; s += A.lanes) {
-                const Pairs<V> x = widen2<T, V>(xd[s * A.vecs + v]), dy = widen2<T, V>(dd[s * A.vecs + v]);
-                Pairs<V> o;
-#pragma unroll
-                for (int i = 0; i < Pairs<V>::N; ++i) {
-                    uint64_t dz, h;
-                    K.template dz<ACT>(x.p[i], dy.p[i], i, dz, h);
-                    o.p[i] = dx(dz, h, i);
-                }
-                *reinterpret_cast<Vec<T, V>*>(q + s * A.ys) = narrow2<T, V>(o);
-            }
-        }
+        const float2 t = A.part_c[(int64_t)n * A.C + c];
+        a += t.x;
+        b += t.y;
     }
-    if ((int)threadIdx.x < here) {
-        if (A.dbeta) A.dbeta[cbase + threadIdx.x] = (float)dbeta;
-        if (A.dgamma) A.dgamma[cbase + threadIdx.x] = (float)dgamma;
-    }
+    if (A.dbeta) A.dbeta[c] = (float)a;
+    if (A.dgamma) A.dgamma[c] = (float)b;
 }
 
 // An empty sample: nothing to normalise; its statistics are (0, 1 / sqrt(eps)), its gradients zero.
@@ -1021,10 +1051,9 @@ static bool gn_small_cut(GnArgs& A, bool backward, size_t* smem) {
     int64_t width = A.per;
     while (width % V != 0 || (width * (int64_t)sizeof(T) < 64 && width < A.C)) width += A.per;
     if (width > A.C) width = A.C;
-    if (width % V != 0 || width > kGnThreads) return false;  // a channel per thread in the last sums
+    if (width % V != 0 || width / V > kGnThreads) return false;
     const int64_t bytes = A.S * width * (int64_t)sizeof(T);
     if (bytes * (backward ? 2 : 1) > kGnSmallSmem || (int64_t)A.N * A.S * A.C * (int64_t)sizeof(T) > kGnSmallBytes) return false;
-    if (backward && A.N > 8) return false;                    // samples in turn
     A.vecs = (int)(width / V);
     A.lanes = kGnThreads / A.vecs;
     if (A.lanes > A.S) A.lanes = (int)A.S;
@@ -1037,8 +1066,8 @@ static bool gn_small_cut(GnArgs& A, bool backward, size_t* smem) {
 template <typename Kern>
 static bool gn_small_ready(PerDevice<int>& cache, Kern kern) {
     return cache.get([&](int&, int) {
-        // 64 KB of data, at most 256 x 8 sums of 8 bytes, statistics
-        return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnSmallSmem + 24 * 1024) == cudaSuccess;
+        // 64 KB of data, at most 256 x 8 sums of 8 bytes, two numbers of 8 bytes for each of at most 2048 channels
+        return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnSmallSmem + 52 * 1024) == cudaSuccess;
     }) != nullptr;
 }
 
@@ -1091,7 +1120,9 @@ static bool launch_gn_small(GnArgs A, bool backward, cudaStream_t st, cudaError_
         if (gn_small_ready(ready, gn_small_kernel<T, V, ACT>))
             *e = launch_after(gn_small_kernel<T, V, ACT>, dim3((unsigned)A.blocks, (unsigned)A.N), block, smem, st, A);
     } else if (gn_small_ready(ready_grad, gn_small_grad_kernel<T, V, ACT>)) {
-        *e = launch_after(gn_small_grad_kernel<T, V, ACT>, dim3((unsigned)A.blocks), block, smem, st, A);
+        *e = launch_after(gn_small_grad_kernel<T, V, ACT>, dim3((unsigned)A.blocks, (unsigned)A.N), block, smem, st, A);
+        if (*e == cudaSuccess && A.N > 1 && (A.dgamma || A.dbeta))
+            *e = launch_after(gn_small_join_kernel, dim3((unsigned)ceil_div(A.C, kGnThreads)), block, 0, st, A);
     }
     return true;
 }

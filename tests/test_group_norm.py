@@ -24,7 +24,7 @@ E = 64 * 2.0 ** -24
 SHAPES = [(1, 1, 32, 2), (2, 1, 24, 1), (1, 70, 8, 8), (3, 77, 180, 12), (2, 50, 64, 32), (1, 333, 30, 3), (2, 64, 7, 7), (1, 40, 2304, 32),
           (1, 9, 4160, 1), (2, 17, 600, 2), (1, 33, 5000, 8), (1, 20000, 128, 32), (4, 1000, 96, 4), (1, 3000, 5, 1),
           (40, 1500, 64, 4), (100, 1200, 64, 4), (200, 40, 64, 8), (1, 70, 9000, 9),
-          (1, 9000, 36, 4), (2, 7000, 34, 2), (1, 5000, 35, 5)]
+          (1, 9000, 36, 4), (2, 7000, 34, 2), (1, 5000, 35, 5), (3, 7, 2048, 1)]
 
 
 def act64(z, act):
