@@ -333,7 +333,7 @@ typedef enum {
 /* ---- linear layer in 16-bit floating point: y = act(x W^T + bias) + residual -----------
  *
  *   X [M, K], W [N, K], Y [M, N]   dtype DVDQ_BF16 or DVDQ_F16, all the same; row pitches ldx, ldw, ldy
- *   bias [N] or NULL, R [M, N] or NULL (the residual, pitch ldr; R may be Y itself), same type
+ *   bias [N] or NULL, R [M, N] or NULL (the residual, pitch ldr; R may be Y itself, same pitch), same type
  *   Z [M, N] or NULL               the pre-activation z = x W^T + bias, for the backward pass (pitch ldz)
  * fp32 accumulation on the tensor cores; bias, activation and residual in fp32, one rounding each for y and z.
  * Matrices start on 16 bytes and pitches are multiples of 8 elements (DVDQ_ERR_ALIGN); M, N and K
@@ -349,7 +349,7 @@ dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, in
  * gradient is dy itself).  dY, Z, X, W, dX, dW as above in one dtype; dbias fp32 [N].  dX, dW and dbias may each be
  * NULL: not computed.  Z is not read for DVDQ_ACT_NONE; X only for dW, W only for dX.  dz is rounded to dtype for
  * the tensor cores; dbias sums it unrounded.  M == 0 writes zeros to dW and dbias.
- * The outputs are written, not added to.  Workspace: 256-byte aligned. */
+ * The outputs are written, not added to, and overlap no input.  Workspace: 256-byte aligned. */
 size_t dvdq_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t act);
 dvdq_status dvdq_linear_backward(const void* dY, int64_t lddy, const void* Z, int64_t ldz, const void* X, int64_t ldx,
                                  const void* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t act,
@@ -370,7 +370,7 @@ dvdq_status dvdq_linear_backward(const void* dY, int64_t lddy, const void* Z, in
  *     DVDQ_ROPE_BY_PARTS   pairs that turn more than beta_fast times over original_length stay, those that turn less than
  *                          beta_slow times are / factor, in between a ramp over the pair index; amplitude
  *                          0.1 ln(factor) + 1
- *   rot_dim even, <= 512. */
+ *   rot_dim even, <= 512; theta > 0 (> 1 for BY_PARTS), factor >= 1. */
 typedef enum { DVDQ_ROPE_PAIRS = 0, DVDQ_ROPE_HALVES = 1 } dvdq_rope_layout;
 typedef enum { DVDQ_ROPE_PLAIN = 0, DVDQ_ROPE_LINEAR = 1, DVDQ_ROPE_BASE = 2, DVDQ_ROPE_BY_PARTS = 3 } dvdq_rope_scaling;
 dvdq_status dvdq_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double original_length,
@@ -453,7 +453,8 @@ dvdq_status dvdq_debug_wait_timeout(uint64_t limit_ns, void* cuda_stream);
 
 /* Reads (and clears) the device-side status word of the current device; synchronizes
  * the device.  DVDQ_OK, or DVDQ_ERR_DEVICE_TIMEOUT with `detail` (host, may be NULL)
- * set to a code identifying the wait that gave up. */
+ * set to a code identifying the wait that gave up, or DVDQ_ERR_SHAPE with detail 16 (dvdq_rope met a row
+ * outside its table). */
 dvdq_status dvdq_last_device_status(uint32_t* detail /* host */);
 
 /* Library version, for the Python binding's sanity check. */

@@ -401,7 +401,9 @@ struct TwoWay {
 // ------------------------------------------------------------------ dependent launches
 
 // A kernel launched with launch_after may start while its predecessor on the stream drains; it
-// must not touch the predecessor's results before wait_predecessor.
+// must not touch the predecessor's results before wait_predecessor.  It releases its own successor after that wait, not before:
+// released at its start, a chain of kernels piles up on the SMs, and waiting CTAs with a whole SM's shared memory keep those in
+// front of them from it (gradients of 1 token, 1536 -> 1536: 25 us, 11 this way; of 4: 20 and 12.7).
 __device__ __forceinline__ void wait_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void release_successor() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -34,14 +34,17 @@ static bool linear_sizes_ok(int64_t M, int64_t N, int64_t K) {
 }
 
 static int64_t dz_chunks(int64_t M, int64_t N) {
-    if (M <= 256) return 1;  // one chunk: its sums are the result, no second kernel
+    // One chunk: its sums are the result, no second kernel.  Both ways with 1536 -> 1536: 64 tokens 9.7 and 9.9 us, 128 12.5 and 11.5,
+    // 256 16.6 and 12.7.
+    if (M <= 64) return 1;
     int64_t c = ceil_div(148 * 6, ceil_div(N, kLinDzCols));
     const int64_t most = ceil_div(M, 32);
     c = c > most ? most : c;
     return c < 1 ? 1 : c;
 }
 struct LinBackwardPlan {
-    LinPlan dx, dw;
+    LinPlan dx, dw;          // a launch each
+    LinPlan dx_two, dw_two;  // in one launch, where `two`
     int64_t lddz, dz_off, sums_off, part_off, total;
     int64_t chunks, rows;
     bool two;  // dX and dW in one launch
@@ -50,12 +53,10 @@ struct LinBackwardPlan {
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
     LinBackwardPlan p;
     p.low = act != DVDQ_ACT_NONE && M <= kLowTokens ? (int)M : 0;
-    p.two = !p.low && lin_plan_two(M, N, K, &p.dx, &p.dw);
-    if (p.low) {
-        p.dx = lin_plan(2 * M, K, N, 64);
-        p.dx.part_bytes = lin_part_bytes(p.dx);  // fp32 sums even of one piece: two rows of them make one of dX
-        p.dw = lin_plan(N, K, M, 64);
-    }
+    double e_dx, e_dw;
+    p.dx = lin_plan(M, K, N, 64, &e_dx);
+    p.dw = lin_plan(N, K, M, 64, &e_dw);
+    p.two = !few_weight_gradient(M, N) && lin_plan_two(M, N, K, e_dx, e_dw, &p.dx_two, &p.dw_two);
     p.lddz = align_up(N, 8);
     p.rows = ceil_div(M, dz_chunks(M, N));
     p.chunks = ceil_div(M, p.rows);
@@ -70,7 +71,7 @@ template <typename T>
 static dvdq_status linear_t(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinPlan& plan, const LinEpilogue& e,
                             const LinMatrix& y, void* ws, cudaStream_t st) {
     if (M <= kFewTokens) return launch_linear_few<T>(x, w, M, N, K, e, y, st);
-    return launch_linear<T, false, false>(x, w, M, N, K, plan, e, y, static_cast<float*>(ws), st);
+    return launch_linear<T, false, false>(x, w, M, N, K, plan, e, y, static_cast<float*>(ws), 0, st);
 }
 
 template <typename T>
@@ -96,17 +97,13 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
             return s;
     }
     const LinEpilogue none = {};
-    if (p.two && !few && dx.p && dw.p) return launch_linear_two<T>(dz, x, w, M, N, K, p.dx, p.dw, dx, dw, st);
-    if (p.low && dx.p) {
-        if ((s = launch_linear_out<T, false, true, kLinPartial>(dz, w, 2 * M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK ||
-            (s = launch_linear_join<T>(p.dx, p.low, M, K, none, dx, part, st)) != DVDQ_OK)
-            return s;
-    } else if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, st)) != DVDQ_OK) return s;
+    if (p.two && dx.p && dw.p) return launch_linear_two<T>(dz, x, w, M, N, K, p.dx_two, p.dw_two, dx, dw, p.low, st);
+    if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, p.low, st)) != DVDQ_OK) return s;
     if (few && (dw.p || db))
         return M == 1   ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st)
                : M <= 4 ? launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st)
                         : launch_linear_few_dw<T, 16>(dy, z, x, M, N, K, act, dw, db, st);
-    if (dw.p && (s = launch_linear<T, true, true>(dz, x, N, K, M, p.dw, none, dw, part, st)) != DVDQ_OK) return s;
+    if (dw.p && (s = launch_linear<T, true, true>(dz, x, N, K, M, p.dw, none, dw, part, 0, st)) != DVDQ_OK) return s;
     return DVDQ_OK;
 }
 
@@ -134,6 +131,7 @@ dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, in
         (s = check_matrix(R, M, N, &ldr, false)) != DVDQ_OK || (s = check_matrix(Y, M, N, &ldy, true)) != DVDQ_OK ||
         (s = check_matrix(Z, M, N, &ldz, false)) != DVDQ_OK)
         return s;
+    if (R == Y && ldr != ldy) return DVDQ_ERR_SHAPE;  // in place: an output may not land on a residual still to be read
     if (bias && !aligned_to(bias, 2)) return DVDQ_ERR_ALIGN;
     const LinPlan plan = M <= kFewTokens ? LinPlan{} : lin_plan(M, N, K, 32);
     if (plan.part_bytes > 0) {
@@ -193,7 +191,8 @@ dvdq_status dvdq_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling
     if (scaling < DVDQ_ROPE_PLAIN || scaling > DVDQ_ROPE_BY_PARTS) return DVDQ_ERR_UNSUPPORTED;
     if (scaling != DVDQ_ROPE_PLAIN && !(factor >= 1.0)) return DVDQ_ERR_SHAPE;
     if (scaling == DVDQ_ROPE_BASE && rot_dim == 2) return DVDQ_ERR_SHAPE;  // the one frequency is 1 whatever the base
-    if (scaling == DVDQ_ROPE_BY_PARTS && (!(original_length > 0.0) || !(beta_fast > beta_slow) || !(beta_slow > 0.0))) return DVDQ_ERR_SHAPE;
+    // (theta <= 1: no pair turns slower than the one before it, and there is no ramp over the pairs)
+    if (scaling == DVDQ_ROPE_BY_PARTS && (!(theta > 1.0) || !(original_length > 0.0) || !isfinite(original_length) || !(beta_fast > beta_slow) || !(beta_slow > 0.0))) return DVDQ_ERR_SHAPE;
     const int pairs = rot_dim / 2;
     const double two_pi = 6.283185307179586476925286766559;
     // base: theta' so that the lowest frequency is divided by factor and the highest stays
@@ -322,6 +321,11 @@ static dvdq_status check_gn_tensor(const void* p, int64_t N, int64_t S, int64_t 
     return aligned_to(p, bytes) ? DVDQ_OK : DVDQ_ERR_ALIGN;
 }
 
+// A tensor written over the one it is made from has the same pitches (after check_gn_tensor).
+static bool gn_in_place_ok(const void* from, int64_t fn, int64_t fs, const void* to, int64_t tn, int64_t ts) {
+    return from != to || (fn == tn && fs == ts);
+}
+
 static dvdq_status group_norm_run(const GnArgs& A0, int64_t N, int64_t S, int32_t act, int32_t dtype, int32_t param_dtype, bool backward,
                                   void* workspace, size_t workspace_bytes, cudaStream_t st) {
     GnArgs A = A0;
@@ -362,6 +366,7 @@ dvdq_status dvdq_group_norm(const void* X, int64_t x_sample, int64_t x_place, in
     if ((s = check_gn_tensor(X, N, S, C, &x_sample, &x_place, bytes, false)) != DVDQ_OK ||
         (s = check_gn_tensor(Y, N, S, C, &y_sample, &y_place, bytes, true)) != DVDQ_OK)
         return s;
+    if (S > 0 && !gn_in_place_ok(X, x_sample, x_place, Y, y_sample, y_place)) return DVDQ_ERR_SHAPE;
     if ((gamma && !aligned_to(gamma, pb)) || (beta && !aligned_to(beta, pb)) || (mean_out && !aligned_to(mean_out, 4)) ||
         (rstd_out && !aligned_to(rstd_out, 4)))
         return DVDQ_ERR_ALIGN;
@@ -411,6 +416,8 @@ dvdq_status dvdq_group_norm_backward(const void* dY, int64_t dy_sample, int64_t 
         (s = check_gn_tensor(X, N, S, C, &x_sample, &x_place, bytes, false)) != DVDQ_OK ||
         (s = check_gn_tensor(dX, N, S, C, &dx_sample, &dx_place, bytes, true)) != DVDQ_OK)
         return s;
+    if (!gn_in_place_ok(dY, dy_sample, dy_place, dX, dx_sample, dx_place) || !gn_in_place_ok(X, x_sample, x_place, dX, dx_sample, dx_place))
+        return DVDQ_ERR_SHAPE;
     GnArgs A = {};
     A.x = X;
     A.dy = dY;

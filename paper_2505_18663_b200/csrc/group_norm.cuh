@@ -202,8 +202,8 @@ constexpr int kGnDepth = 8, kGnGradDepth = 5;  // slots: 32 KB a CTA, 40 KB for 
 template <typename T, int V>
 __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
-    release_successor();
     wait_predecessor();
+    release_successor();
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
     GnMoments<V> sums;
@@ -243,8 +243,8 @@ template <bool BACKWARD>
 __global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_constant__ GnArgs A, int group_ctas) {
     constexpr int kWarps = kGnThreads / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    release_successor();
     wait_predecessor();
+    release_successor();
     if ((int)blockIdx.x < group_ctas) {
         const int64_t ng = (int64_t)blockIdx.x * kWarps + warp;
         if (ng >= (int64_t)A.N * A.G) return;
@@ -373,8 +373,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
     extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
-    release_successor();
     wait_predecessor();
+    release_successor();
     if (!P.on) return;
     float ga[V], be[V];
     gn_params<V>(A, P.c0, ga, be);
@@ -426,8 +426,8 @@ __device__ __forceinline__ GnGrad<T, V> gn_constants(const GnArgs& A, int n, int
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kGnThreads, 2) gn_grad_stats_kernel(const __grid_constant__ GnArgs A) {
     extern __shared__ __align__(16) uint8_t raw[];
-    release_successor();
     wait_predecessor();
+    release_successor();
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
     Pairs<V> s1, s2;
@@ -487,8 +487,8 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_grad_apply_kernel(const __gr
     extern __shared__ __align__(16) uint8_t raw[];
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
-    release_successor();
     wait_predecessor();
+    release_successor();
     if (!P.on) return;
     float rs[V], ga[V];
     const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
@@ -806,8 +806,8 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     float2* red = reinterpret_cast<float2*>(raw + align_up((int64_t)S * width * sizeof(T), 16));
     double2* totals = reinterpret_cast<double2*>(red + align_up(A.lanes * width, 2));
     const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
-    release_successor();
     wait_predecessor();
+    release_successor();
     Pairs<V> mu, s1;
     gn_small_bring<T, V>(on, r, A.lanes, S, base + c0, A.xs, data + v, A.vecs);
     if (on) {
@@ -880,8 +880,8 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
     float2* red = reinterpret_cast<float2*>(raw + 2 * slice);
     float2* sums = red + A.lanes * width;   // per channel
     float2* gsum = sums + width;            // per group
-    release_successor();
     wait_predecessor();
+    release_successor();
     const T* p = static_cast<const T*>(A.x) + (int64_t)n * A.xn + c0;
     const T* d = static_cast<const T*>(A.dy) + (int64_t)n * A.dn + c0;
     // everything of this thread at once; it reads only what it brought itself
@@ -951,8 +951,8 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
 
 __global__ void __launch_bounds__(kGnThreads) gn_small_join_kernel(const __grid_constant__ GnArgs A) {
     const int c = blockIdx.x * kGnThreads + threadIdx.x;
-    release_successor();
     wait_predecessor();
+    release_successor();
     if (c >= A.C) return;
     double a = 0.0, b = 0.0;
 #pragma unroll 8
@@ -1071,7 +1071,9 @@ static bool gn_small_ready(PerDevice<int>& cache, Kern kern) {
     }) != nullptr;
 }
 
-// One CTA per SM, shared evenly among the samples; taken where that keeps at least four SMs in five busy.
+// One CTA per SM, shared evenly among the samples; taken where that keeps at least two SMs in three busy.  Samples of 2000 places
+// of 512 channels, this and three launches: 100 samples (100 SMs) 121 and 121 us forward, 189 and 223 backward; 80 samples 109 and
+// 103, 187 and 175.
 // Returns whether the call was made; *e says how it went.
 template <typename Kern>
 static bool launch_gn_fused(PerDevice<int>& cache, Kern kern, GnArgs A, int V, int threads, size_t smem, int64_t most_channels, cudaStream_t st,
@@ -1090,7 +1092,7 @@ static bool launch_gn_fused(PerDevice<int>& cache, Kern kern, GnArgs A, int V, i
     });
     if (!sms || *sms == 0) return false;
     int chunks = *sms / A.N;
-    if (chunks < 1 || (int64_t)chunks * A.N * 5 < (int64_t)*sms * 4) return false;
+    if (chunks < 1 || (int64_t)chunks * A.N * 3 < (int64_t)*sms * 2) return false;
     A.rows = ceil_div(A.S, chunks);
     A.chunks = (int)ceil_div(A.S, A.rows);
     A.vecs = A.C / V;

@@ -12,10 +12,13 @@
 // operands in shared memory (128-byte swizzle) in a ring of TMA-filled stages of 64 along k, two fp32
 // accumulators in tensor memory, so that the epilogue of a tile runs under the next tile's products.
 // Roles per CTA: warps 0 and 2 TMA producers of A and B; warp 1 (leader CTA) issues the products; warps 4-11 epilogue, two
-// per tensor-memory lane quarter, every other 32 columns each: bias, activation, residual in fp32, ONE rounding,
-// and TMA stores of 32 x 32 blocks; the residual's blocks come by TMA one block ahead.
+// per tensor-memory lane quarter, every other block of 32 (or 64) columns each: bias, activation, residual in fp32, ONE
+// rounding (fp32 outputs would double what is written), and TMA stores; the residual's blocks come by TMA, up to three ahead.
 //
-// What bounds it: the tensor pipe on layers of thousands of tokens; with few tokens, streaming W.
+// What bounds it: the tensor pipe on layers of thousands of tokens (32760 x 5120 -> 13824 with GELU: 3.2-3.4 ms, 1.36-1.45
+// PFLOP/s under the power cap, the bare product of the vendor's library 3.3 ms; tensor pipe 98 % active in the gradients, 88 %
+// at 32760 x 1536 -> 1536, where it takes 105-139 us with the clock); with few tokens, streaming W; with a contraction of a few
+// k-blocks, the copies of outputs and residuals (32760 x 64 -> 1536: 27 us, with a residual 50 for 205 MB).
 // Products with fewer tiles than CTA pairs are cut along k (`splits`): each piece writes its fp32 sums,
 // and a second kernel adds the pieces in a fixed order and does the epilogue (no atomics).
 #pragma once
@@ -34,13 +37,14 @@ constexpr int kLinPairs = 74;                 // CTA pairs of a B200 (148 SMs): 
 // What the kernel writes: the output; the output from a residual, or z as well; fp32 pieces.
 enum LinOut { kLinFinal = 0, kLinFinalMore = 1, kLinPartial = 2 };
 
-template <int OUT>
+template <int OUT, bool WIDE>
 struct LinSmem {
     // a residual that comes early, and z, take two more blocks per epilogue warp, and 32 KB of the ring
-    static constexpr int kRing = (OUT == kLinFinalMore ? 5 : 6) * 32768;
+    static constexpr int kRing = (OUT == kLinFinalMore ? (WIDE ? 3 : 5) : (WIDE ? 5 : 6)) * 32768;
     static constexpr int kMaxStages = 16;                   // a stage is 32 KB at most; narrow tiles and few rows take less
     static constexpr int kBufs = OUT == kLinFinalMore ? 4 : 2;
-    static constexpr int kBuf = 32 * 32 * 2;                // 32 x 32 outputs; fp32 partials use two as one
+    static constexpr int kCols = WIDE ? 64 : 32;            // of an epilogue block
+    static constexpr int kBuf = 32 * kCols * 2;             // 32 x kCols outputs; fp32 partials use two as one
     static constexpr int kBufOff = kRing;
     static constexpr int kBiasOff = kBufOff + kLinEpiWarps * kBufs * kBuf;
     static constexpr int kBarOff = kBiasOff + kLinEpiWarps * 32 * 4;
@@ -59,6 +63,7 @@ struct LinArgs {
     FastDiv by_splits, by_panel_tiles, by_panel, by_last;  // pieces; tiles of a panel; columns of a panel, of the last one
     int part_rows;          // rows of one piece in the partial buffer
     int a_bytes;            // of one CTA's half of A's stage
+    int low;                // A in two parts that add up: row m + low is the second part of row m (0: one part)
     int stages, stage, b_off;  // of the operand ring: how many, bytes per CTA of each, where B's half begins in it
     int act, has_residual, has_z;
     const void* bias;
@@ -164,7 +169,8 @@ struct LinMaps {
     CUtensorMap a, b, y;
 };
 
-// Walks the 32 x 32 blocks of one epilogue warp, tile after tile.
+// Walks the 32 x COLS blocks of one epilogue warp, tile after tile.
+template <int COLS>
 struct LinBlocks {
     int item, c = -1, blocks = 0, row0 = 0, col0 = 0, piece = 0;
     bool more = true;
@@ -172,9 +178,9 @@ struct LinBlocks {
         int tm, tn;
         lin_item(A, item, tm, tn, piece);
         row0 = tm * kLinTile + rows_from;
-        col0 = tn * A.bn + half * 32;
-        const int width = min(A.bn, A.Nd - tn * A.bn) - half * 32;
-        blocks = row0 < A.Md && width > 0 ? (width + 63) >> 6 : 0;  // those that lie in D: columns col0, col0 + 64, ...
+        col0 = tn * A.bn + half * COLS;
+        const int width = min(A.bn, A.Nd - tn * A.bn) - half * COLS;
+        blocks = row0 < A.Md && width > 0 ? (width + 2 * COLS - 1) / (2 * COLS) : 0;  // those that lie in D: columns col0, col0 + 2 COLS, ...
     }
     // to the next block that lies in D
     __device__ __forceinline__ void next(const LinArgs& A, int items, int step, int rows_from, int half) {
@@ -192,7 +198,7 @@ struct LinBlocks {
 
 // TWO: dX and dW of a small layer in one launch: neither fills the pairs, so the first items of the grid are the tiles of
 // one, the rest those of the other (each pair has one tile).  The first product's A is then K-major, the second's MN-major.
-template <typename T, bool AMN_, bool BMN, int OUT, bool TWO>
+template <typename T, bool AMN_, bool BMN, int OUT, bool TWO, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmZ,
               const __grid_constant__ LinArgs args1, const __grid_constant__ LinMaps maps2, const __grid_constant__ LinArgs args2) {
@@ -204,7 +210,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
     const bool AMN = TWO ? second : AMN_;
     const int items = second ? args2.num_m * args2.num_n : items1;
     const int first_item = second ? pair - items1 : pair, item_step = TWO ? 1 << 30 : num_pairs;
-    using S = LinSmem<OUT>;
+    using S = LinSmem<OUT, WIDE>;
     constexpr int MS = S::kMaxStages;
     const uint32_t ST = (uint32_t)A.stages, stage = (uint32_t)A.stage;
     extern __shared__ uint8_t smem_raw[];
@@ -240,8 +246,8 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem_base = misc[0];
-    release_successor();
     wait_predecessor();
+    release_successor();
 
     if (warp == 0 || warp == 2) {
         // ------------------------------------------------------------ TMA producers: warp 0 of A, warp 2 of B
@@ -268,6 +274,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                     if (rank == 0) mbar_arrive_expect_tx(full(st), bytes);
                     if (needed) {
                         lin_load(of_a ? AMN : BMN, dst + st * stage, map, leader_full + 8u * st, k0, r0, of_a ? 128 : bw);
+                        if (BMN && of_a && A.low > 0) tma_load_2d_pair(dst + st * stage + A.a_bytes / 2, map, leader_full + 8u * st, k0, r0 + A.low);
                     }
                     k0 += kLinBK;
                 });
@@ -285,6 +292,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
             const uint32_t step_a = AMN ? 2048 / 16 : 2;
             constexpr uint32_t kStepB = BMN ? 2048 / 16 : 2;
             const uint64_t ad0 = AMN ? umma_desc_sw128_mnmajor(sbase) : umma_desc_sw128_kmajor(sbase);
+            const uint64_t ad1 = ad0 + (uint32_t)(A.a_bytes / 2 >> 4);  // the second part
             const uint64_t bd0 = BMN ? umma_desc_sw128_mnmajor(sbase + A.b_off) : umma_desc_sw128_kmajor(sbase + A.b_off);
             LinRing ring(full(0), ST, 0u);
             uint32_t lt = 0;
@@ -305,6 +313,11 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                     for (int k = 0; k < kLinBK / 16; ++k) {
                         tc_mma_f16_pair(d_tmem, ad0 + (off + step_a * k), bd0 + (off + kStepB * k), idesc, add);
                         add = 1u;
+                    }
+                    if (BMN && A.low > 0) {
+#pragma unroll
+                        for (int k = 0; k < kLinBK / 16; ++k)
+                            tc_mma_f16_pair(d_tmem, ad1 + (off + step_a * k), bd0 + (off + kStepB * k), idesc, 1u);
                     }
                     tc_commit_pair(empty(st), 3);
                 });
@@ -334,7 +347,7 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
         bool ok = true;
         // Asks for the residual of the next block ahead, into the buffer whose turn it is: at the start all but one, then one after
         // each block, when that block's store is the newest and the store that used the buffer is the one before it.
-        LinBlocks ahead;
+        LinBlocks<S::kCols> ahead;
         ahead.item = first_item;
         auto ask = [&]() {
             ahead.next(A, items, item_step, rows_from, half);
@@ -343,14 +356,14 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                 if (with_z) tma_store_wait_read<2>();
                 else tma_store_wait_read<1>();
                 mbar_arrive_expect_tx(res_full(ew, rask), S::kBuf);
-                tma_load_2d(buf0 + rask * S::kBuf, &tmR, res_full(ew, rask), ahead.col0 + ahead.c * 64, ahead.row0);
+                tma_load_2d(buf0 + rask * S::kBuf, &tmR, res_full(ew, rask), ahead.col0 + ahead.c * (2 * S::kCols), ahead.row0);
             }
             rask = rask + 1 == turns ? 0u : rask + 1;
             ++pending;
         };
         if (residual)
             for (uint32_t i = 1; i < turns; ++i) ask();
-        LinBlocks b;
+        LinBlocks<S::kCols> b;
         for (b.item = first_item; ok && b.item < items; b.item += item_step, ++lt) {
             b.tile(A, rows_from, half);
             const uint32_t a = lt & 1u, aph = (lt >> 1) & 1u;
@@ -363,10 +376,10 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < blocks; ++c) {
-                uint32_t r[32];
-                __syncwarp();
-                tmem_ld_32x32(tmem_base + a * kLinTile + half * 32 + c * 64 + ((uint32_t)(q * 32) << 16), r);
-                if (OUT == kLinPartial) {
+                if constexpr (OUT == kLinPartial) {
+                    uint32_t r[32];
+                    __syncwarp();
+                    tmem_ld_32x32(tmem_base + a * kLinTile + half * 32 + c * 64 + ((uint32_t)(q * 32) << 16), r);
                     if (lane == 0) tma_store_wait_read<0>();
                     __syncwarp();
                     tmem_ld_wait();
@@ -379,81 +392,96 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                         tma_store_2d(&maps.y, buf0, col0 + c * 64, piece * A.part_rows + row0);
                         tma_store_commit();
                     }
-                    continue;
-                }
-                // the block's output buffer (without a residual: else ask() has waited for it) and z's: free once all but the
-                // newest store have been read
-                if ((!residual || with_z) && lane == 0) tma_store_wait_read<1>();
-                if (with_bias) sts32f(c_bias + 4 * lane, b_next);
-                __syncwarp();
-                if (with_bias && c + 1 < blocks) b_next = col0 + (c + 1) * 64 + lane < A.Nd ? to_f32(bias[col0 + (c + 1) * 64 + lane]) : 0.f;
-                const uint32_t buf = buf0 + buf_i * S::kBuf;
-                if (residual) {
-                    ok = mbar_wait_one_lane(res_full(ew, buf_i), (rphase >> buf_i) & 1u, abort_flag, kWaitPackedFull);
+                } else {
+                    const uint32_t buf = buf0 + buf_i * S::kBuf, zb = buf0 + 3 * S::kBuf;
+                    const int block_col = col0 + c * (2 * S::kCols);
+#pragma unroll
+                    for (int h = 0; h < S::kCols / 32; ++h) {  // 32 columns at a time
+                        uint32_t r[32];
+                        __syncwarp();
+                        tmem_ld_32x32(tmem_base + a * kLinTile + half * S::kCols + c * (2 * S::kCols) + h * 32 + ((uint32_t)(q * 32) << 16), r);
+                        // the block's output buffer (without a residual: else ask() has waited for it) and z's: free once all but the
+                        // newest store have been read
+                        if (h == 0 && (!residual || with_z) && lane == 0) tma_store_wait_read<1>();
+                        if (with_bias) sts32f(c_bias + 4 * lane, b_next);
+                        __syncwarp();
+                        if (with_bias) {
+                            const int next = h + 1 < S::kCols / 32 ? block_col + (h + 1) * 32 : c + 1 < blocks ? block_col + 2 * S::kCols : A.Nd;
+                            b_next = next + lane < A.Nd ? to_f32(bias[next + lane]) : 0.f;
+                        }
+                        if (residual && h == 0) {
+                            ok = mbar_wait_one_lane(res_full(ew, buf_i), (rphase >> buf_i) & 1u, abort_flag, kWaitPackedFull);
+                            if (!ok) break;
+                            rphase ^= 1u << buf_i;
+                            --pending;
+                        }
+                        tmem_ld_wait();
+                        uint64_t v[16];  // pairs of columns
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) v[j] = f2_pack(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                        if (with_bias) {
+#pragma unroll
+                            for (int j = 0; j < 16; j += 2) {
+                                const float4 f = lds128f(c_bias + 8 * j);
+                                v[j] = f2_add(v[j], f2_pack(f.x, f.y));
+                                v[j + 1] = f2_add(v[j + 1], f2_pack(f.z, f.w));
+                            }
+                        }
+                        // what the swizzled TMA copies use: rows of 64 bytes, 16-byte chunk index XORed with (row / 2) % 4, or of
+                        // 128 bytes, with row % 8
+                        auto at = [&](uint32_t base, int j) {
+                            return WIDE ? base + lane * 128 + (((h * 4 + j) ^ (lane & 7)) << 4) : base + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4);
+                        };
+                        auto put = [&](uint32_t base, int j) {  // columns 8 j .. 8 j + 7
+                            uint32_t w[4];
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) {
+                                float lo, hi;
+                                f2_unpack(v[4 * j + t], lo, hi);
+                                w[t] = pack2<T>(lo, hi);
+                            }
+                            sts128(at(base, j), w[0], w[1], w[2], w[3]);
+                        };
+                        if (with_z) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) put(zb, j);
+                            if (h + 1 == S::kCols / 32) {
+                                fence_proxy_async_smem();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    tma_store_2d(&tmZ, zb, block_col, row0);
+                                    tma_store_commit();
+                                }
+                            }
+                        }
+                        if (A.act == DVDQ_ACT_GELU_TANH) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = act_value2<DVDQ_ACT_GELU_TANH>(v[j]);
+                        } else if (A.act == DVDQ_ACT_SILU) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = act_value2<DVDQ_ACT_SILU>(v[j]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (residual) {
+                                const uint4 w = lds128(at(buf, j));
+                                const Pairs<8> f = widen2<T, 8>(*reinterpret_cast<const Vec<T, 8>*>(&w));
+#pragma unroll
+                                for (int t = 0; t < 4; ++t) v[4 * j + t] = f2_add(v[4 * j + t], f.p[t]);
+                            }
+                            put(buf, j);
+                        }
+                    }
                     if (!ok) break;
-                    rphase ^= 1u << buf_i;
-                    --pending;
-                }
-                buf_i = buf_i + 1 == turns ? 0u : buf_i + 1;
-                tmem_ld_wait();
-                uint64_t v[16];  // pairs of columns
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = f2_pack(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-                if (with_bias) {
-#pragma unroll
-                    for (int j = 0; j < 16; j += 2) {
-                        const float4 f = lds128f(c_bias + 8 * j);
-                        v[j] = f2_add(v[j], f2_pack(f.x, f.y));
-                        v[j + 1] = f2_add(v[j + 1], f2_pack(f.z, f.w));
-                    }
-                }
-                // rows of 64 bytes, 16-byte chunk index XORed with (row / 2) % 4: what the swizzled TMA copies use
-                auto at = [&](uint32_t base, int j) { return base + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4); };
-                auto put = [&](uint32_t base, int j) {  // columns 8 j .. 8 j + 7
-                    uint32_t w[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        float lo, hi;
-                        f2_unpack(v[4 * j + t], lo, hi);
-                        w[t] = pack2<T>(lo, hi);
-                    }
-                    sts128(at(base, j), w[0], w[1], w[2], w[3]);
-                };
-                if (with_z) {
-                    const uint32_t zb = buf0 + 3 * S::kBuf;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) put(zb, j);
+                    buf_i = buf_i + 1 == turns ? 0u : buf_i + 1;
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_2d(&tmZ, zb, col0 + c * 64, row0);
+                        tma_store_2d(&maps.y, buf, block_col, row0);
                         tma_store_commit();
                     }
+                    if (residual) ask();
                 }
-                if (A.act == DVDQ_ACT_GELU_TANH) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = act_value2<DVDQ_ACT_GELU_TANH>(v[j]);
-                } else if (A.act == DVDQ_ACT_SILU) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = act_value2<DVDQ_ACT_SILU>(v[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (residual) {
-                        const uint4 w = lds128(at(buf, j));
-                        const Pairs<8> f = widen2<T, 8>(*reinterpret_cast<const Vec<T, 8>*>(&w));
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) v[4 * j + t] = f2_add(v[4 * j + t], f.p[t]);
-                    }
-                    put(buf, j);
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    tma_store_2d(&maps.y, buf, col0 + c * 64, row0);
-                    tma_store_commit();
-                }
-                if (residual) ask();
             }
             tc_fence_before();
             __syncwarp();
@@ -478,14 +506,13 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
 
 // ------------------------------------------------------------------ joining the pieces
 
-// y = act(sum of the pieces + bias) + residual, four columns per thread; pieces are added in order.  fold > 0: row m's sum is
-// that of rows m and m + fold of the pieces.
+// y = act(sum of the pieces + bias) + residual, four columns per thread; pieces are added in order.
 template <typename T>
 __global__ void __launch_bounds__(256)
-linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pitch, int splits, int fold, int64_t Md, int Nd, const T* __restrict__ bias,
+linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pitch, int splits, int64_t Md, int Nd, const T* __restrict__ bias,
                    const T* residual, int64_t ldr, int act, T* y, int64_t ldy, T* z, int64_t ldz) {
-    release_successor();
     wait_predecessor();
+    release_successor();
     const int quads = (Nd + 3) >> 2;
     const int64_t total = Md * quads;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -497,12 +524,6 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
         for (int k = 1; k < splits; ++k) {
             const float4 t = *reinterpret_cast<const float4*>(p + k * piece_floats);
             s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
-        }
-        if (fold > 0) {
-            for (int k = 0; k < splits; ++k) {
-                const float4 t = *reinterpret_cast<const float4*>(p + (int64_t)fold * pitch + k * piece_floats);
-                s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
-            }
         }
         float v[4] = {s.x, s.y, s.z, s.w};
         const int here = Nd - n < 4 ? Nd - n : 4;
@@ -537,7 +558,7 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
 // dz = dy act'(z) in fp32, rounded once to the operands' type for the tensor cores (an fp32 dz would cost
 // the two products half of their rate or more); the bias's gradient sums the unrounded values.
 // low > 0 (few tokens, whose roundings would not average out in dX): what the rounding left over, itself rounded, goes
-// to row m + low, and dX is formed from both.
+// to row m + low, and dX is formed from both, in one accumulator.
 // A CTA takes 256 columns (8 per thread, 32 threads side by side, 8 rows at a time) of one chunk of
 // rows and writes their sums; linear_colsum_kernel adds the chunks.  act = none: dz is dy itself, only sums.
 constexpr int kLinDzCols = 256, kLinDzDepth = 5;
@@ -547,8 +568,8 @@ __global__ void __launch_bounds__(kStreamThreads, 4)
 linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z, int64_t ldz, int64_t M, int N, int64_t rows,
                  T* __restrict__ dz, int64_t lddz, int low, float* __restrict__ sums) {
     constexpr bool kAct = ACT != DVDQ_ACT_NONE;
-    release_successor();
     wait_predecessor();
+    release_successor();
     __shared__ __align__(16) uint8_t raw[kStreamThreads * 16 * kLinDzDepth * (kAct ? 2 : 1)];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
     const int n = blockIdx.x * kLinDzCols + tx * 8;
@@ -614,8 +635,8 @@ linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z
 }
 
 __global__ void __launch_bounds__(256) linear_colsum_kernel(const float* __restrict__ sums, int chunks, int N, float* __restrict__ out) {
-    release_successor();
     wait_predecessor();
+    release_successor();
     __shared__ double sh[8][33];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
@@ -632,6 +653,11 @@ __global__ void __launch_bounds__(256) linear_colsum_kernel(const float* __restr
 }
 
 // ------------------------------------------------------------------ host side
+
+// Epilogue blocks of 32 x 64 instead of 32 x 32 outputs: half as many TMA copies, at the price of operand stages.  Worth it where
+// a tile has few products to hide its copies under: up to 4 k-blocks (32760 x 256 -> 1536: 30.9 us, 32.5 in narrow blocks; 512:
+// 46.5 and 44.5), and 8 with a residual or z (512 -> 1536 with residual: 63 us, 72 in narrow blocks; 256: 54 and 66; 768: 82 and 80).
+constexpr int kLinWide = 4, kLinWideMore = 8;
 
 struct LinPlan {
     int bn, splits;
@@ -651,13 +677,12 @@ inline int lin_a_rows(int64_t Md) { return Md < 128 ? (int)align_up(Md, 8) : 128
 
 // The estimate for one wave (or `waves`) of pieces of `kblocks`.
 inline double lin_cost(int64_t Md, int bn, int64_t kblocks, int64_t waves, double memory) {
-    const bool deep = LinSmem<kLinFinal>::kRing / ((lin_a_rows(Md) + bn / 2) * kLinBK * 2) > kLinPairStages;
+    const bool deep = LinSmem<kLinFinal, false>::kRing / ((lin_a_rows(Md) + bn / 2) * kLinBK * 2) > kLinPairStages;
     const double products = 0.345 * bn / 256.0, loops = deep ? 0.15 + 0.0006 * bn : 0.135 + 0.00083 * bn;
     const double t_epi = 0.5 + 2.0 * bn / 256.0, item = (double)kblocks * (products > loops ? products : loops);
     const double cost = (double)waves * (item > t_epi ? item : t_epi);
     return (cost < memory ? memory : cost) + 2.0 + t_epi;
 }
-inline int64_t lin_part_bytes(const LinPlan& p) { return align_up(p.splits * p.part_rows * p.part_pitch * 4, 256); }
 inline double lin_memory_time(int64_t Md, int64_t Nd, int64_t Kc) { return ((double)Md + Nd) * Kc * 2.0 / 6.0e6; }
 
 inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* estimate = nullptr) {
@@ -678,17 +703,14 @@ inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* es
         }
     }
     if (estimate) *estimate = best;
-    p.part_bytes = p.splits > 1 ? lin_part_bytes(p) : 0;
+    p.part_bytes = p.splits > 1 ? align_up(p.splits * p.part_rows * p.part_pitch * 4, 256) : 0;
     return p;
 }
 
-// dX [M, K] (contraction N) and dW [N, K] (contraction M) side by side: the widths, or false where their tiles do not fit the
-// pairs together or one after the other is estimated to be as fast (a launch of its own: 2 us).
-inline bool lin_plan_two(int64_t M, int64_t N, int64_t K, LinPlan* dx, LinPlan* dw) {
-    double e1, e2, best = 1e300;
-    const LinPlan p1 = lin_plan(M, K, N, 64, &e1), p2 = lin_plan(N, K, M, 64, &e2);
-    *dx = p1;
-    *dw = p2;
+// dX [M, K] (contraction N) and dW [N, K] (contraction M) side by side: the plans, or false where their tiles do not fit the
+// pairs together or one after the other (estimates e1 and e2) is estimated to be as fast (a launch of its own: 2 us).
+inline bool lin_plan_two(int64_t M, int64_t N, int64_t K, double e1, double e2, LinPlan* dx, LinPlan* dw) {
+    double best = 1e300;
     for (int b1 = kLinTile; b1 >= 64; b1 -= 64)
         for (int b2 = kLinTile; b2 >= 64; b2 -= 64) {
             if (ceil_div(M, kLinTile) * ceil_div(K, b1) + ceil_div(N, kLinTile) * ceil_div(K, b2) > kLinPairs) continue;
@@ -696,14 +718,9 @@ inline bool lin_plan_two(int64_t M, int64_t N, int64_t K, LinPlan* dx, LinPlan* 
             const double cost = c1 > c2 ? c1 : c2;
             if (cost < best) { best = cost; dx->bn = b1; dw->bn = b2; }
         }
-    if (best >= e1 + e2 + 2.0) {
-        *dx = p1;
-        *dw = p2;
-        return false;
-    }
     dx->splits = dw->splits = 1;
-    dx->part_bytes = dw->part_bytes = 0;
-    return true;
+    dx->part_rows = dx->part_pitch = dx->part_bytes = dw->part_rows = dw->part_pitch = dw->part_bytes = 0;  // no pieces
+    return best < e1 + e2 + 2.0;
 }
 
 // A 16-bit matrix [rows, cols] with row pitch ld elements, tiles of box_rows x box_cols.
@@ -734,6 +751,11 @@ struct LinMatrix {
     const void* p;
     int64_t ld;
 };
+// The blocks in which the epilogue writes an output or reads the residual.
+template <bool WIDE>
+inline bool make_map_out(CUtensorMap* tm, bool bf16, const LinMatrix& y, int64_t rows, int64_t cols) {
+    return make_map16(tm, bf16, y.p, rows, cols, y.ld, WIDE ? 64 : 32, 32, WIDE ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
 struct LinEpilogue {
     const void* bias;
     LinMatrix residual, z;
@@ -741,19 +763,19 @@ struct LinEpilogue {
 };
 
 // Tensor maps and arguments of one product; false if a map cannot be made.
-template <typename T, bool AMN, bool BMN, int OUT>
+template <typename T, bool AMN, bool BMN, int OUT, bool WIDE = false>
 static bool make_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan, const LinEpilogue& e,
-                        const LinMatrix& y, float* part, LinMaps* maps, LinArgs* A) {
+                        const LinMatrix& y, float* part, int low, LinMaps* maps, LinArgs* A) {
     constexpr bool bf = IsBf16<T>::value != 0;
-    using S = LinSmem<OUT>;
+    using S = LinSmem<OUT, WIDE>;
     auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows, int box) {
         return mn ? make_map16(m, bf, x.p, Kc, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
                   : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, (uint32_t)box, CU_TENSOR_MAP_SWIZZLE_128B);
     };
     const int a_rows = AMN ? 128 : lin_a_rows(Md);
-    if (!operand(&maps->a, AMN, a, Md, a_rows) || !operand(&maps->b, BMN, b, Nd, plan.bn / 2)) return false;
+    if (!operand(&maps->a, AMN, a, Md + low, a_rows) || !operand(&maps->b, BMN, b, Nd, plan.bn / 2)) return false;
     if (OUT == kLinPartial ? !make_map_f32(&maps->y, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
-                           : !make_map16(&maps->y, bf, y.p, Md, Nd, y.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+                           : !make_map_out<WIDE>(&maps->y, bf, y, Md, Nd))
         return false;
     A->Md = (int)Md;
     A->Nd = (int)Nd;
@@ -768,7 +790,8 @@ static bool make_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int6
     A->by_panel = FastDiv((uint32_t)A->panel);
     A->by_last = FastDiv((uint32_t)(A->num_n - (A->num_n - 1) / A->panel * A->panel));
     A->part_rows = (int)plan.part_rows;
-    A->a_bytes = (int)lin_bytes(AMN, a_rows);
+    A->low = low;
+    A->a_bytes = (int)lin_bytes(AMN, a_rows) * (low > 0 ? 2 : 1);
     A->b_off = (int)align_up(A->a_bytes, 1024);  // swizzle atoms are 1024 bytes
     A->stage = A->b_off + (int)align_up(lin_bytes(BMN, plan.bn / 2), 1024);
     A->stages = S::kRing / A->stage < S::kMaxStages ? S::kRing / A->stage : S::kMaxStages;
@@ -779,19 +802,19 @@ static bool make_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int6
     return true;
 }
 
-template <typename T, bool AMN, bool BMN, int OUT>
+template <typename T, bool AMN, bool BMN, int OUT, bool WIDE = false>
 static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
-                                     const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
+                                     const LinEpilogue& e, const LinMatrix& y, float* part, int low, cudaStream_t st) {
     constexpr bool bf = IsBf16<T>::value != 0;
-    using S = LinSmem<OUT>;
+    using S = LinSmem<OUT, WIDE>;
     LinMaps maps;
     LinArgs A;
-    if (!make_linear<T, AMN, BMN, OUT>(a, b, Md, Nd, Kc, plan, e, y, part, &maps, &A)) return DVDQ_ERR_CUDA;
+    if (!make_linear<T, AMN, BMN, OUT, WIDE>(a, b, Md, Nd, Kc, plan, e, y, part, low, &maps, &A)) return DVDQ_ERR_CUDA;
     CUtensorMap tmR = maps.y, tmZ = maps.y;  // where unused
     const bool fin = OUT == kLinFinalMore;
-    if (fin && e.residual.p && !make_map16(&tmR, bf, e.residual.p, Md, Nd, e.residual.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
-    if (fin && e.z.p && !make_map16(&tmZ, bf, e.z.p, Md, Nd, e.z.ld, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DVDQ_ERR_CUDA;
-    auto kern = linear_kernel<T, AMN, BMN, OUT, false>;
+    if (fin && e.residual.p && !make_map_out<WIDE>(&tmR, bf, e.residual, Md, Nd)) return DVDQ_ERR_CUDA;
+    if (fin && e.z.p && !make_map_out<WIDE>(&tmZ, bf, e.z, Md, Nd)) return DVDQ_ERR_CUDA;
+    auto kern = linear_kernel<T, AMN, BMN, OUT, false, WIDE>;
     static PerDevice<int> cache;
     const int max_pairs = resident_pairs(cache, kern, kLinThreads, S::kTotal);
     if (max_pairs == 0) return DVDQ_ERR_CUDA;
@@ -801,42 +824,47 @@ static dvdq_status launch_linear_out(const LinMatrix& a, const LinMatrix& b, int
 }
 
 template <typename T>
-static dvdq_status launch_linear_join(const LinPlan& plan, int fold, int64_t Md, int64_t Nd, const LinEpilogue& e, const LinMatrix& y,
+static dvdq_status launch_linear_join(const LinPlan& plan, int64_t Md, int64_t Nd, const LinEpilogue& e, const LinMatrix& y,
                                       const float* part, cudaStream_t st) {
     const int64_t ctas = ceil_div(Md * ((Nd + 3) / 4), 256);
     return cuda_status(launch_after(linear_join_kernel<T>, dim3((unsigned)(ctas < 148 * 8 ? ctas : 148 * 8)), dim3(256), 0, st, part,
-                                    plan.part_rows * plan.part_pitch, (int)plan.part_pitch, plan.splits, fold, Md, (int)Nd,
+                                    plan.part_rows * plan.part_pitch, (int)plan.part_pitch, plan.splits, Md, (int)Nd,
                                     static_cast<const T*>(e.bias), static_cast<const T*>(e.residual.p), e.residual.ld, e.act,
                                     static_cast<T*>(const_cast<void*>(y.p)), y.ld, static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld));
 }
 
-// D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.
+// D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.  low > 0 (dX of at most kLowTokens rows): A is the sum of its
+// rows m and m + low.
 template <typename T, bool AMN, bool BMN>
 static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
-                                 const LinEpilogue& e, const LinMatrix& y, float* part, cudaStream_t st) {
+                                 const LinEpilogue& e, const LinMatrix& y, float* part, int low, cudaStream_t st) {
     if (plan.splits == 1) {
         // only the forward product has a residual or stores its pre-activation
+        const int64_t wide_kb = plan.bn % 128 == 0 ? ceil_div(Kc, kLinBK) : kLinWideMore + 1;  // a tile is whole blocks for both warps
         if constexpr (!AMN && !BMN) {
-            if (e.z.p || e.residual.p) return launch_linear_out<T, AMN, BMN, kLinFinalMore>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+            if (e.z.p || e.residual.p)
+                return wide_kb <= kLinWideMore ? launch_linear_out<T, AMN, BMN, kLinFinalMore, true>(a, b, Md, Nd, Kc, plan, e, y, part, low, st)
+                                               : launch_linear_out<T, AMN, BMN, kLinFinalMore>(a, b, Md, Nd, Kc, plan, e, y, part, low, st);
         }
-        return launch_linear_out<T, AMN, BMN, kLinFinal>(a, b, Md, Nd, Kc, plan, e, y, part, st);
+        if (wide_kb <= kLinWide) return launch_linear_out<T, AMN, BMN, kLinFinal, true>(a, b, Md, Nd, Kc, plan, e, y, part, low, st);
+        return launch_linear_out<T, AMN, BMN, kLinFinal>(a, b, Md, Nd, Kc, plan, e, y, part, low, st);
     }
-    const dvdq_status s = launch_linear_out<T, AMN, BMN, kLinPartial>(a, b, Md, Nd, Kc, plan, e, y, part, st);
-    return s != DVDQ_OK ? s : launch_linear_join<T>(plan, 0, Md, Nd, e, y, part, st);
+    const dvdq_status s = launch_linear_out<T, AMN, BMN, kLinPartial>(a, b, Md, Nd, Kc, plan, e, y, part, low, st);
+    return s != DVDQ_OK ? s : launch_linear_join<T>(plan, Md, Nd, e, y, part, st);
 }
 
 // dX = dZ W and dW = dZ^T X of a small layer in one launch.
 template <typename T>
 static dvdq_status launch_linear_two(const LinMatrix& dz, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinPlan& p1,
-                                     const LinPlan& p2, const LinMatrix& dx, const LinMatrix& dw, cudaStream_t st) {
-    using S = LinSmem<kLinFinal>;
+                                     const LinPlan& p2, const LinMatrix& dx, const LinMatrix& dw, int low, cudaStream_t st) {
+    using S = LinSmem<kLinFinal, false>;
     LinMaps m1, m2;
     LinArgs a1, a2;
     const LinEpilogue none = {};
-    if (!make_linear<T, false, true, kLinFinal>(dz, w, M, K, N, p1, none, dx, nullptr, &m1, &a1) ||
-        !make_linear<T, true, true, kLinFinal>(dz, x, N, K, M, p2, none, dw, nullptr, &m2, &a2))
+    if (!make_linear<T, false, true, kLinFinal>(dz, w, M, K, N, p1, none, dx, nullptr, low, &m1, &a1) ||
+        !make_linear<T, true, true, kLinFinal>(dz, x, N, K, M, p2, none, dw, nullptr, 0, &m2, &a2))
         return DVDQ_ERR_CUDA;
-    auto kern = linear_kernel<T, false, true, kLinFinal, true>;
+    auto kern = linear_kernel<T, false, true, kLinFinal, true, false>;
     static PerDevice<int> cache;
     if (resident_pairs(cache, kern, kLinThreads, S::kTotal) == 0) return DVDQ_ERR_CUDA;
     // each pair of the grid has one tile; pairs need not be resident together

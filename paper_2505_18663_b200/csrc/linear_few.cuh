@@ -49,11 +49,11 @@ __global__ void __launch_bounds__(WARPS * 32)
 linear_few_kernel(const T* __restrict__ X, int64_t ldx, const T* __restrict__ W, int64_t ldw, int M, int N, int K, int k_per_warp,
                   const T* __restrict__ bias, const T* R, int64_t ldr, int act, T* Y, int64_t ldy, T* Z, int64_t ldz) {
     extern __shared__ __align__(16) uint8_t raw[];
-    release_successor();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int piece = warp % KS, group = warp / KS;
     const int n0 = (blockIdx.x * (WARPS / KS) + group) * 16;
     wait_predecessor();
+    release_successor();
     float c[4] = {0.f, 0.f, 0.f, 0.f};
     if (n0 < N) {
         // rows past N repeat the last one: their results are not stored
@@ -110,20 +110,20 @@ __device__ __forceinline__ float few_dz(const T* dy, int64_t lddy, const T* z, i
 }
 
 constexpr int kFewCols = 128 * 8;  // columns of a CTA of the gradients: 128 threads, 8 each
-constexpr int kFewRows = 32;       // rows of dW that a CTA writes
+constexpr int kFewRows = 16;       // rows of dW that a CTA writes, at most
 
 // dW[n, k] = sum over m of dz[m, n] x[m, k], and dbias[n] = sum over m of dz[m, n]
 template <typename T, int MT>
 __global__ void __launch_bounds__(128)
 linear_few_dw_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict__ Z, int64_t ldz, int act, const T* __restrict__ X, int64_t ldx,
-                     int M, int N, int K, T* __restrict__ dW, int64_t lddw, float* __restrict__ db) {
+                     int M, int N, int K, int rows, T* __restrict__ dW, int64_t lddw, float* __restrict__ db) {
     __shared__ float dz[kFewRows][MT];
-    const int k = blockIdx.y * kFewCols + threadIdx.x * 8, n0 = blockIdx.x * kFewRows, here = min(kFewRows, N - n0);
-    release_successor();
+    const int k = blockIdx.y * kFewCols + threadIdx.x * 8, n0 = blockIdx.x * rows, here = min(rows, N - n0);
     wait_predecessor();
-    for (int i = threadIdx.x; i < kFewRows * MT; i += 128) {
+    release_successor();
+    for (int i = threadIdx.x; i < here * MT; i += 128) {
         const int n = n0 + i / MT, m = i % MT;
-        dz[i / MT][m] = n < N && m < M ? few_dz(dY, lddy, Z, ldz, act, m, n) : 0.f;
+        dz[i / MT][m] = m < M ? few_dz(dY, lddy, Z, ldz, act, m, n) : 0.f;
     }
     Pairs<8> x[MT];
     if (dW && k < K) {
@@ -163,7 +163,7 @@ linear_few_dw_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict
 
 // ------------------------------------------------------------------ host side
 
-// dW by linear_few_dw_kernel: up to 4 tokens because it is faster (5120 x 5120, 4 tokens: 13.5 us, 18.4 in linear.cuh), up to 16
+// dW by linear_few_dw_kernel: up to 4 tokens because it is faster (5120 x 5120, 4 tokens: 10.0 us, 13.7 in linear.cuh), up to 16
 // where so few values of dz would not average their rounding out (and the matrix is small).
 inline bool few_weight_gradient(int64_t M, int64_t N) { return M <= 4 || (M <= 16 && M * N < 4096); }
 
@@ -184,7 +184,8 @@ static cudaError_t launch_linear_few_w(const LinMatrix& x, const LinMatrix& w, i
 }
 // Warps that share 16 channels (KS): as many as keep all CTAs in one wave (four of eight warps per SM): the longer a
 // warp's piece of k, the less its start and the joining weigh, but a second, partial wave costs more.  Few
-// channels and a long k: sixteen warps share them, two such CTAs per SM.
+// channels and a long k: sixteen warps share them, two such CTAs per SM.  One token, KS = 1, 2, 4, 8, 16, in us: 3072 -> 18432 40.8, 26.1,
+// 21.2, 22.9, 23.4; 5120 -> 5120 66, 37, 21.8, 14.2, 16.9; 8960 -> 1536 122, 63, 36, 19.2, 11.8; 512 -> 40000 10.9, 12.3, 10.2, 11.4, 17.5.
 template <typename T>
 static dvdq_status launch_linear_few(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e,
                                      const LinMatrix& y, cudaStream_t st) {
@@ -196,13 +197,21 @@ static dvdq_status launch_linear_few(const LinMatrix& x, const LinMatrix& w, int
     return cuda_status(launch_linear_few_w<T, 8, 1>(x, w, M, N, K, e, y, st));
 }
 
+// Rows of a CTA: 16, fewer where that leaves SMs with little to do.  32, 16, 8, 4, 2 rows: 4 tokens 5120 -> 5120 14.5, 10.0, 10.9, 12.7,
+// 17.9 us, 1536 -> 1536 5.0, 3.8, 3.2, 3.6, 3.8; 16 tokens 300 -> 200 12.2, 8.4, 6.5, 5.7, 5.2.
+inline int few_rows(int64_t N, int64_t cols) {
+    int rows = kFewRows;
+    while (rows > 4 && ceil_div(N, rows) * cols < 148 * 4) rows /= 2;
+    return rows;
+}
 template <typename T, int MT>
 static dvdq_status launch_linear_few_dw(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, int64_t M, int64_t N, int64_t K, int act,
                                         const LinMatrix& dw, float* db, cudaStream_t st) {
     const unsigned cols = dw.p ? (unsigned)ceil_div(K, kFewCols) : 1u;
-    return cuda_status(launch_after(linear_few_dw_kernel<T, MT>, dim3((unsigned)ceil_div(N, kFewRows), cols), dim3(128), 0, st,
+    const int rows = few_rows(N, cols);
+    return cuda_status(launch_after(linear_few_dw_kernel<T, MT>, dim3((unsigned)ceil_div(N, rows), cols), dim3(128), 0, st,
                                     static_cast<const T*>(dy.p), dy.ld, static_cast<const T*>(z.p), z.ld, act, static_cast<const T*>(x.p), x.ld, (int)M,
-                                    (int)N, (int)K, static_cast<T*>(const_cast<void*>(dw.p)), dw.ld, db));
+                                    (int)N, (int)K, rows, static_cast<T*>(const_cast<void*>(dw.p)), dw.ld, db));
 }
 
 }  // namespace dvdq

@@ -66,8 +66,8 @@ template <typename T, bool HALVES, int W, int HEADS>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs A) {
     constexpr int P = HALVES ? W : (W > 1 ? W / 2 : 1);
     constexpr bool TWO = HALVES || W == 1;  // a rotating item is two accesses
-    release_successor();
     wait_predecessor();
+    release_successor();
     const uint32_t idx = blockIdx.x * (uint32_t)kRopeThreads + threadIdx.x;
     if (idx >= A.threads) return;
     const uint32_t lt = A.per_token(idx), rem = idx - lt * A.per_token.d;
@@ -203,8 +203,9 @@ static cudaError_t launch_rope_w(RopeArgs A, int64_t tokens, cudaStream_t st) {
     A.rot_items = A.rot / 2 / P;
     const int items = A.rot_items + (A.head_dim - A.rot) / W;
     // Few tokens: one head per thread, the shortest chain.  Many: four, which share the table's values
-    // and keep four loads (eight in halves) in flight.
-    const bool many = tokens * (A.q.heads + A.k.heads) * items >= (int64_t)148 * 2048 * 2;
+    // and keep four loads (eight in halves) in flight.  24 heads of 128 channels, one and four heads per thread: 100 tokens 1.6
+    // and 1.8 us, 400 2.8 and 2.5, 1600 5.3 and 3.9, 32760 81 and 63 (6.4 TB/s); 32 heads of 96, halves, 65536: 148 and 121 (6.7 TB/s).
+    const bool many = tokens * (A.q.heads + A.k.heads) * items >= (int64_t)148 * 1024;
     return many ? launch_rope_heads<T, HALVES, W, 4>(A, tokens, items, st) : launch_rope_heads<T, HALVES, W, 1>(A, tokens, items, st);
 }
 

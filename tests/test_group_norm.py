@@ -260,7 +260,7 @@ def backward(**k):
     (dict(dtype=3), B.ERR_UNSUPPORTED), (dict(pt=1), B.ERR_UNSUPPORTED), (dict(dtype=2, pt=0), B.ERR_UNSUPPORTED), (dict(X=None), B.ERR_NULL),
     (dict(Y=None), B.ERR_NULL), (dict(ws=None), B.ERR_NULL), (dict(n=10), B.ERR_WORKSPACE), (dict(ws=P + 8), B.ERR_ALIGN),
     (dict(X=P + 1), B.ERR_ALIGN), (dict(gamma=P + 2), B.ERR_ALIGN), (dict(mean=P + 2), B.ERR_ALIGN), (dict(ys=31), B.ERR_SHAPE),
-    (dict(xs=-32), B.ERR_SHAPE), (dict(yn=0), B.ERR_SHAPE), (dict(N=0), B.OK), (dict(S=0), B.OK)])
+    (dict(xs=-32), B.ERR_SHAPE), (dict(yn=0), B.ERR_SHAPE), (dict(xs=40, xn=400), B.ERR_SHAPE), (dict(xn=640), B.ERR_SHAPE), (dict(N=0), B.OK), (dict(S=0), B.OK)])
 def test_forward_refuses(change, status):
     assert forward(**change) == status
 
@@ -268,7 +268,7 @@ def test_forward_refuses(change, status):
 @pytest.mark.parametrize("change,status", [
     (dict(G=3), B.ERR_SHAPE), (dict(act=-1), B.ERR_UNSUPPORTED), (dict(dY=None), B.ERR_NULL), (dict(X=None), B.ERR_NULL),
     (dict(mean=None), B.ERR_NULL), (dict(rstd=None), B.ERR_NULL), (dict(ws=None), B.ERR_NULL), (dict(n=10), B.ERR_WORKSPACE),
-    (dict(es=16), B.ERR_SHAPE), (dict(dX=P + 1), B.ERR_ALIGN), (dict(dg=P + 2), B.ERR_ALIGN), (dict(N=0, dg=None, db=None), B.OK)])
+    (dict(es=16), B.ERR_SHAPE), (dict(en=640), B.ERR_SHAPE), (dict(dY=2 * P, es=40, en=400), B.ERR_SHAPE), (dict(dX=P + 1), B.ERR_ALIGN), (dict(dg=P + 2), B.ERR_ALIGN), (dict(N=0, dg=None, db=None), B.OK)])
 def test_backward_refuses(change, status):
     assert backward(**change) == status
 

@@ -67,7 +67,8 @@ def status_ok():
 # sizes: one token; tiles and their edges (256 x 256 x 64); sizes that are no multiple of 8; one column;
 # long contractions (cut into pieces); many tiles
 FORWARD = [(1, 256, 256), (1, 1541, 1030), (7, 8, 8), (3, 1, 1), (16, 40, 64), (2, 100, 1537), (8, 300, 700), (9, 33, 3000), (5, 12000, 96), (16, 9000, 40), (17, 255, 63), (33, 257, 65), (128, 512, 4100),
-           (256, 256, 64), (257, 264, 200), (300, 1000, 136), (129, 768, 3000), (1021, 1541, 515), (2500, 2300, 72)]
+           (256, 256, 64), (257, 264, 200), (300, 1000, 136), (129, 768, 3000), (1021, 1541, 515), (2500, 2300, 72),
+           (6000, 1130, 130), (6000, 1130, 450)]
 
 
 @gpu
@@ -154,7 +155,7 @@ def test_the_same_bits_every_time_and_on_another_stream():
 
 
 BACKWARD = [(1, 64, 72), (1, 1541, 1030), (5, 8, 8), (2, 1, 3), (3, 700, 1100), (4, 257, 130), (16, 90, 2500), (17, 129, 65), (64, 256, 256), (65, 255, 130), (300, 264, 200), (1021, 515, 258), (4100, 72, 64),
-            (700, 2100, 1100)]
+            (700, 2100, 1100), (4200, 130, 1200), (200, 2600, 1100)]
 
 
 @gpu
@@ -247,7 +248,7 @@ def backward(**k):
     (dict(X=None), B.ERR_NULL), (dict(W=None), B.ERR_NULL), (dict(Y=None), B.ERR_NULL),
     (dict(ldx=63), B.ERR_SHAPE), (dict(ldw=60), B.ERR_SHAPE), (dict(ldx=65), B.ERR_ALIGN), (dict(ldy=36), B.ERR_ALIGN),
     (dict(X=P + 2), B.ERR_ALIGN), (dict(Y=P + 8), B.ERR_ALIGN), (dict(bias=P + 1), B.ERR_ALIGN), (dict(R=P, ldr=31), B.ERR_SHAPE),
-    (dict(R=P, ldr=33), B.ERR_ALIGN), (dict(Z=P, ldz=8), B.ERR_SHAPE), (dict(Z=P + 4, ldz=32), B.ERR_ALIGN),
+    (dict(R=P, ldr=33), B.ERR_ALIGN), (dict(R=P, ldr=40), B.ERR_SHAPE), (dict(Z=P, ldz=8), B.ERR_SHAPE), (dict(Z=P + 4, ldz=32), B.ERR_ALIGN),
     (dict(M=20, K=6400, ldx=6400, ldw=6400), B.ERR_NULL), (dict(M=20, K=6400, ldx=6400, ldw=6400, ws=P, n=16), B.ERR_WORKSPACE),
     (dict(M=20, K=6400, ldx=6400, ldw=6400, ws=P + 16, n=1 << 30), B.ERR_ALIGN), (dict(M=0, X=None, Y=None, W=None), B.OK)])
 def test_linear_refuses(change, status):

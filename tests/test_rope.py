@@ -188,7 +188,9 @@ def test_frequencies():
             assert f[i] / 8 * 0.999999 <= g[i] <= f[i]
     assert g[0] == f[0] and sorted(g, reverse=True) == g
     for bad in (dict(rot_dim=3), dict(rot_dim=0), dict(rot_dim=514), dict(rot_dim=8, theta=0.0), dict(rot_dim=8, scaling=9),
-                dict(rot_dim=8, scaling=1, factor=0.5), dict(rot_dim=8, scaling=3, factor=2.0), dict(rot_dim=2, scaling=2, factor=2.0)):
+                dict(rot_dim=8, scaling=1, factor=0.5), dict(rot_dim=8, scaling=3, factor=2.0), dict(rot_dim=2, scaling=2, factor=2.0),
+                dict(rot_dim=8, theta=1.0, scaling=3, factor=2.0, original_length=4096.0, beta_fast=32.0, beta_slow=1.0),
+                dict(rot_dim=8, theta=100.0, scaling=3, factor=2.0, original_length=float("inf"), beta_fast=32.0, beta_slow=1.0)):
         with pytest.raises(B.DvdqError):
             B.dvdq_rope_frequencies(**bad)
 
