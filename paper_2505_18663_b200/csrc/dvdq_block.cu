@@ -48,15 +48,15 @@ struct LinBackwardPlan {
     int64_t lddz, dz_off, sums_off, part_off, total;
     int64_t chunks, rows;
     bool two;  // dX and dW in one launch
-    int low;   // dz in two parts: rows M .. 2 M hold what rounding left over
+    int low;   // M where dz comes in two parts: rows M .. 2 M hold what rounding left over; or 0
 };
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
     LinBackwardPlan p;
-    p.low = act != DVDQ_ACT_NONE && M <= kLowTokens ? (int)M : 0;
+    p.low = act != DVDQ_ACT_NONE && dz_in_two_parts(M, N) ? (int)M : 0;
     double e_dx, e_dw;
     p.dx = lin_plan(M, K, N, 64, &e_dx);
     p.dw = lin_plan(N, K, M, 64, &e_dw);
-    p.two = !few_weight_gradient(M, N) && lin_plan_two(M, N, K, e_dx, e_dw, &p.dx_two, &p.dw_two);
+    p.two = !few_weight_gradient(M) && lin_plan_two(M, N, K, e_dx, e_dw, &p.dx_two, &p.dw_two);
     p.lddz = align_up(N, 8);
     p.rows = ceil_div(M, dz_chunks(M, N));
     p.chunks = ceil_div(M, p.rows);
@@ -78,7 +78,7 @@ template <typename T>
 static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N,
                                      int64_t K, int32_t act, const LinBackwardPlan& p, const LinMatrix& dx, const LinMatrix& dw, float* db,
                                      uint8_t* ws, cudaStream_t st) {
-    const bool few = few_weight_gradient(M, N);  // dW and dbias by their own kernel
+    const bool few = few_weight_gradient(M);  // dW and dbias by their own kernel
     float* sums = !db || few ? nullptr : p.chunks == 1 ? db : reinterpret_cast<float*>(ws + p.sums_off);
     float* part = reinterpret_cast<float*>(ws + p.part_off);
     LinMatrix dz = dy;
@@ -100,10 +100,8 @@ static dvdq_status linear_backward_t(const LinMatrix& dy, const LinMatrix& z, co
     if (p.two && dx.p && dw.p) return launch_linear_two<T>(dz, x, w, M, N, K, p.dx_two, p.dw_two, dx, dw, p.low, st);
     if (dx.p && (s = launch_linear<T, false, true>(dz, w, M, K, N, p.dx, none, dx, part, p.low, st)) != DVDQ_OK) return s;
     if (few && (dw.p || db))
-        return M == 1   ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st)
-               : M <= 4 ? launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st)
-                        : launch_linear_few_dw<T, 16>(dy, z, x, M, N, K, act, dw, db, st);
-    if (dw.p && (s = launch_linear<T, true, true>(dz, x, N, K, M, p.dw, none, dw, part, 0, st)) != DVDQ_OK) return s;
+        return M == 1 ? launch_linear_few_dw<T, 1>(dy, z, x, M, N, K, act, dw, db, st) : launch_linear_few_dw<T, 4>(dy, z, x, M, N, K, act, dw, db, st);
+    if (dw.p && (s = launch_linear<T, true, true>(dz, x, N, K, M, p.dw, none, dw, part, p.low, st)) != DVDQ_OK) return s;
     return DVDQ_OK;
 }
 

@@ -63,7 +63,7 @@ struct LinArgs {
     FastDiv by_splits, by_panel_tiles, by_panel, by_last;  // pieces; tiles of a panel; columns of a panel, of the last one
     int part_rows;          // rows of one piece in the partial buffer
     int a_bytes;            // of one CTA's half of A's stage
-    int low;                // A in two parts that add up: row m + low is the second part of row m (0: one part)
+    int low;                // dz as A in two parts that add up: row m + low of dz is the second part of row m (0: one part)
     int stages, stage, b_off;  // of the operand ring: how many, bytes per CTA of each, where B's half begins in it
     int act, has_residual, has_z;
     const void* bias;
@@ -274,7 +274,8 @@ linear_kernel(const __grid_constant__ LinMaps maps1, const __grid_constant__ CUt
                     if (rank == 0) mbar_arrive_expect_tx(full(st), bytes);
                     if (needed) {
                         lin_load(of_a ? AMN : BMN, dst + st * stage, map, leader_full + 8u * st, k0, r0, of_a ? 128 : bw);
-                        if (BMN && of_a && A.low > 0) tma_load_2d_pair(dst + st * stage + A.a_bytes / 2, map, leader_full + 8u * st, k0, r0 + A.low);
+                        if (BMN && of_a && A.low > 0)
+                            lin_load(AMN, dst + st * stage + A.a_bytes / 2, map, leader_full + 8u * st, AMN ? k0 + A.low : k0, AMN ? r0 : r0 + A.low, 128);
                     }
                     k0 += kLinBK;
                 });
@@ -557,8 +558,9 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
 
 // dz = dy act'(z) in fp32, rounded once to the operands' type for the tensor cores (an fp32 dz would cost
 // the two products half of their rate or more); the bias's gradient sums the unrounded values.
-// low > 0 (few tokens, whose roundings would not average out in dX): what the rounding left over, itself rounded, goes
-// to row m + low, and dX is formed from both, in one accumulator.
+// low > 0 (so few values that their roundings would not average out): what the rounding left over, itself rounded, goes
+// to row m + low, and dX and dW are formed from both, in one accumulator (where dW's last k-block reaches past row M it meets rows
+// of the second part, but x has zeros there).  Beside an infinity nothing is left over.
 // A CTA takes 256 columns (8 per thread, 32 threads side by side, 8 rows at a time) of one chunk of
 // rows and writes their sums; linear_colsum_kernel adds the chunks.  act = none: dz is dy itself, only sums.
 constexpr int kLinDzCols = 256, kLinDzDepth = 5;
@@ -596,7 +598,12 @@ linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z
                 if (low > 0) {
                     const Pairs<8> h = widen2<T, 8>(high);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) d.p[i] = f2_sub(d.p[i], h.p[i]);
+                    for (int i = 0; i < 4; ++i) {
+                        float a, b, ha, hb;
+                        f2_unpack(d.p[i], a, b);
+                        f2_unpack(h.p[i], ha, hb);
+                        d.p[i] = f2_pack(isfinite(ha) ? a - ha : 0.f, isfinite(hb) ? b - hb : 0.f);
+                    }
                     *reinterpret_cast<Vec<T, 8>*>(out + low * lddz) = narrow2<T, 8>(d);
                 }
                 out += 8 * lddz;
@@ -768,12 +775,12 @@ static bool make_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int6
                         const LinMatrix& y, float* part, int low, LinMaps* maps, LinArgs* A) {
     constexpr bool bf = IsBf16<T>::value != 0;
     using S = LinSmem<OUT, WIDE>;
-    auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows, int box) {
-        return mn ? make_map16(m, bf, x.p, Kc, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
-                  : make_map16(m, bf, x.p, rows, Kc, x.ld, kLinBK, (uint32_t)box, CU_TENSOR_MAP_SWIZZLE_128B);
+    auto operand = [&](CUtensorMap* m, bool mn, const LinMatrix& x, int64_t rows, int64_t k, int more, int box) {  // `more` rows in memory
+        return mn ? make_map16(m, bf, x.p, k + more, rows, x.ld, 64, kLinBK, CU_TENSOR_MAP_SWIZZLE_128B)
+                  : make_map16(m, bf, x.p, rows + more, k, x.ld, kLinBK, (uint32_t)box, CU_TENSOR_MAP_SWIZZLE_128B);
     };
     const int a_rows = AMN ? 128 : lin_a_rows(Md);
-    if (!operand(&maps->a, AMN, a, Md + low, a_rows) || !operand(&maps->b, BMN, b, Nd, plan.bn / 2)) return false;
+    if (!operand(&maps->a, AMN, a, Md, Kc, low, a_rows) || !operand(&maps->b, BMN, b, Nd, Kc, 0, plan.bn / 2)) return false;
     if (OUT == kLinPartial ? !make_map_f32(&maps->y, part, plan.splits * plan.part_rows, Nd, plan.part_pitch)
                            : !make_map_out<WIDE>(&maps->y, bf, y, Md, Nd))
         return false;
@@ -833,8 +840,7 @@ static dvdq_status launch_linear_join(const LinPlan& plan, int64_t Md, int64_t N
                                     static_cast<T*>(const_cast<void*>(y.p)), y.ld, static_cast<T*>(const_cast<void*>(e.z.p)), e.z.ld));
 }
 
-// D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.  low > 0 (dX of at most kLowTokens rows): A is the sum of its
-// rows m and m + low.
+// D = A B^T with the epilogue e, into y; `part` holds plan.part_bytes.  low > 0: dz, which is A, comes in two parts.
 template <typename T, bool AMN, bool BMN>
 static dvdq_status launch_linear(const LinMatrix& a, const LinMatrix& b, int64_t Md, int64_t Nd, int64_t Kc, const LinPlan& plan,
                                  const LinEpilogue& e, const LinMatrix& y, float* part, int low, cudaStream_t st) {
@@ -862,7 +868,7 @@ static dvdq_status launch_linear_two(const LinMatrix& dz, const LinMatrix& x, co
     LinArgs a1, a2;
     const LinEpilogue none = {};
     if (!make_linear<T, false, true, kLinFinal>(dz, w, M, K, N, p1, none, dx, nullptr, low, &m1, &a1) ||
-        !make_linear<T, true, true, kLinFinal>(dz, x, N, K, M, p2, none, dw, nullptr, 0, &m2, &a2))
+        !make_linear<T, true, true, kLinFinal>(dz, x, N, K, M, p2, none, dw, nullptr, low, &m2, &a2))
         return DVDQ_ERR_CUDA;
     auto kern = linear_kernel<T, false, true, kLinFinal, true, false>;
     static PerDevice<int> cache;

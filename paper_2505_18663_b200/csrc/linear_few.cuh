@@ -1,5 +1,5 @@
 // The linear layer for a few tokens: modulation of one conditioning vector, single decoded tokens (M <= 8), and
-// the weights' gradient of such a step (M <= 4, or 16 if the layer is small).  With more tokens the kernel of linear.cuh is faster
+// the weights' gradient of such a step (M <= 4).  With more tokens the kernel of linear.cuh is faster
 // (5120 x 5120: 17 us for 16 tokens there, 24 here with a second group of tokens, 14.6 for 4).
 //
 // What bounds it: reading W (or writing dW) once, 2 N K bytes; the products are a rounding error beside
@@ -19,7 +19,9 @@
 namespace dvdq {
 
 constexpr int kFewTokens = 8;
-constexpr int kLowTokens = 32;  // dX is formed from dz in two parts up to here: the tile's 256 rows have room for both
+// The gradients are formed from dz in two parts where its values are so few that their roundings do not average out.  Both ways with
+// 1536 -> 1536: 32 tokens 10.4 and 8.5 us.
+inline bool dz_in_two_parts(int64_t M, int64_t N) { return M <= 32 || M * N < 4096; }
 
 // 8 elements of a row from column k on; those past K are zero (and are not read: what follows a row's last element may be anything).
 template <typename T>
@@ -163,9 +165,8 @@ linear_few_dw_kernel(const T* __restrict__ dY, int64_t lddy, const T* __restrict
 
 // ------------------------------------------------------------------ host side
 
-// dW by linear_few_dw_kernel: up to 4 tokens because it is faster (5120 x 5120, 4 tokens: 10.0 us, 13.7 in linear.cuh), up to 16
-// where so few values of dz would not average their rounding out (and the matrix is small).
-inline bool few_weight_gradient(int64_t M, int64_t N) { return M <= 4 || (M <= 16 && M * N < 4096); }
+// dW by linear_few_dw_kernel (5120 x 5120, 4 tokens: 10.0 us, 13.7 in linear.cuh).
+inline bool few_weight_gradient(int64_t M) { return M <= 4; }
 
 template <typename T, int WARPS, int KS>
 static cudaError_t launch_linear_few_w(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinEpilogue& e,
@@ -198,7 +199,7 @@ static dvdq_status launch_linear_few(const LinMatrix& x, const LinMatrix& w, int
 }
 
 // Rows of a CTA: 16, fewer where that leaves SMs with little to do.  32, 16, 8, 4, 2 rows: 4 tokens 5120 -> 5120 14.5, 10.0, 10.9, 12.7,
-// 17.9 us, 1536 -> 1536 5.0, 3.8, 3.2, 3.6, 3.8; 16 tokens 300 -> 200 12.2, 8.4, 6.5, 5.7, 5.2.
+// 17.9 us, 1536 -> 1536 5.0, 3.8, 3.2, 3.6, 3.8.
 inline int few_rows(int64_t N, int64_t cols) {
     int rows = kFewRows;
     while (rows > 4 && ceil_div(N, rows) * cols < 148 * 4) rows /= 2;

@@ -285,19 +285,18 @@ def test_the_binding_refuses_what_is_no_cuda_matrix():
 
 @gpu
 @pytest.mark.parametrize("dt", DTYPES)
-@pytest.mark.parametrize("M,N,K", [(1, 70, 300), (3, 151, 1090), (16, 64, 90), (17, 130, 72), (32, 600, 200)])
+@pytest.mark.parametrize("M,N,K", [(1, 70, 300), (3, 151, 1090), (16, 64, 90), (17, 130, 72), (32, 600, 200), (17, 73, 79), (63, 64, 300), (300, 13, 40)])
 def test_gradients_of_few_tokens_do_not_round_dz(dt, M, N, K):
-    """Up to 32 tokens dX is formed from dz in two parts (what is left after both is below u^2 |dz|, or half the smallest fp16
-    step); up to 4, and 16 in small layers, dW from fp32: one rounding of the result, as if dz were exact."""
+    """Up to 32 tokens, and in small layers, the gradients are formed from dz in two parts (what is left after both is below
+    u^2 |dz|, or half the smallest fp16 step), or from fp32: one rounding of the result, as if dz were exact."""
     g = gen(N)
     dy, x, w, z = rows(M, N, dt, g), rows(M, K, dt, g), rows(N, K, dt, g), rows(M, N, dt, g, 2.0)
     dx, dw = rows(M, K, dt), rows(N, K, dt)
     B.dvdq_linear_backward(dy, z, x, w, B.ACT_SILU, dx, dw, None, workspace(B.dvdq_linear_backward_workspace_bytes(M, N, K, B.ACT_SILU)))
     dz = dy.double() * slope64(z.double(), B.ACT_SILU)
     fine = 2.0 ** -18 * dy.double().abs() * (1 + z.double().abs()) * 1.2 + U[dt] ** 2 * dz.abs() + TINY[dt]
-    outs = [(dx, dz @ w.double(), fine @ w.double().abs(), 2 * N, dz.abs() @ w.double().abs())]
-    if M <= 4 or M * N < 4096 and M <= 16:
-        outs.append((dw, dz.T @ x.double(), fine.T @ x.double().abs(), M, dz.abs().T @ x.double().abs()))
+    outs = [(dx, dz @ w.double(), fine @ w.double().abs(), 2 * N, dz.abs() @ w.double().abs()),
+            (dw, dz.T @ x.double(), fine.T @ x.double().abs(), 2 * M, dz.abs().T @ x.double().abs())]
     for got, want, spread, terms, mag in outs:
         inner = spread + (terms + 8) * 2.0 ** -23 * mag
         check(got, want, inner + U[dt] * (want.abs() + inner) + TINY[dt], "gradient")
