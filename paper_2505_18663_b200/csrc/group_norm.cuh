@@ -19,6 +19,10 @@
 // leave SMs idle): three launches, pass 1, join, pass 2, each started while its predecessor drains.
 // Small tensors, one launch: where a slice of whole groups of one sample fits a CTA's shared memory,
 // the CTA reads it once, and does both passes on it.
+//
+// Measured: 499200 places of 128 channels, bf16 with SiLU, 73 us (3.5 TB/s of x once and y once, 39 us at the copy rate); gradients
+// of 2 x 18720 places of 512 channels 41 us (115 MB, 2.8 TB/s); 3 x 77 places of 180 fp32 channels 6.3 us in a graph.
+// One launch and three: 2 MB (small kernel aside) 15.7 and 11.9 us, 8 MB 18.5 and 20.1, 61 MB 40 and 41, gradients 57 and 59.
 #pragma once
 
 #include "block_common.cuh"
@@ -1042,8 +1046,8 @@ inline bool gn_cut(GnArgs& A, int V) {
 
 // The one-launch kernels: the fewest whole groups that fill 64 bytes of a place (or all channels, if
 // those are fewer), so that a warp's loads are whole sectors; used where their places fit kGnSmallSmem, which
-// leaves room for three CTAs per SM.  A tensor of more than kGnSmallBytes is left to the three launches,
-// whose loads are whole rows.
+// leaves room for three CTAs per SM.  A tensor of more than kGnSmallBytes is left to the kernels above, whose loads are whole rows:
+// samples of 1000 places of 512 channels, small kernel and those: 8 MB 14.6 and 18.4 us, 16 MB 15.2 and 20.6, but 16 MB in 64 samples 25 and 21.
 constexpr int64_t kGnSmallSmem = 64 << 10, kGnSmallBytes = 8 << 20;
 template <typename T, int V>
 static bool gn_small_cut(GnArgs& A, bool backward, size_t* smem) {

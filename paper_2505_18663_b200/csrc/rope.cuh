@@ -9,7 +9,7 @@
 // shared by all heads).  So the angles' cosines and sines come from a table that is made once
 // (rope_table_kernel, in fp64: at position 10^5 an fp32 angle is off by 0.004), q and k go in one
 // launch, and a thread keeps the table's values of its channels in registers while it walks over
-// kRopeHeads heads of the token, all their loads in flight at once.
+// up to four heads of the token, all their loads in flight at once.
 #pragma once
 
 #include "block_common.cuh"

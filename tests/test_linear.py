@@ -300,3 +300,19 @@ def test_gradients_of_few_tokens_do_not_round_dz(dt, M, N, K):
     for got, want, spread, terms, mag in outs:
         inner = spread + (terms + 8) * 2.0 ** -23 * mag
         check(got, want, inner + U[dt] * (want.abs() + inner) + TINY[dt], "gradient")
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("M,N,K", [(5, 40, 72), (20, 130, 96)])
+def test_an_infinite_gradient_stays_in_its_token_and_channel(dt, M, N, K):
+    """Nothing is left of an infinity to round, and no row of dz's second part reaches a sum that it does not belong to."""
+    g = gen(N + 1)
+    dy, x, w, z = rows(M, N, dt, g), rows(M, K, dt, g), rows(N, K, dt, g), rows(M, N, dt, g)
+    dy[2, 3], z[2, 3] = float("inf"), 1.0
+    dx, dw, db = rows(M, K, dt), rows(N, K, dt), torch.empty(N, device=DEV)
+    B.dvdq_linear_backward(dy, z, x, w, B.ACT_SILU, dx, dw, db, workspace(B.dvdq_linear_backward_workspace_bytes(M, N, K, B.ACT_SILU)))
+    status_ok()
+    assert torch.equal(dx[2].float(), torch.sign(w[3].float()) * math.inf) and torch.equal(dw[3].float(), torch.sign(x[2].float()) * math.inf)
+    assert dx[[i for i in range(M) if i != 2]].isfinite().all() and dw[[i for i in range(N) if i != 3]].isfinite().all()
+    assert db[3] == math.inf and db[[i for i in range(N) if i != 3]].isfinite().all()
