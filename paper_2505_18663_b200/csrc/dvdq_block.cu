@@ -342,6 +342,7 @@ static dvdq_status group_norm_run(const GnArgs& A0, int64_t N, int64_t S, int32_
     A.params_f32 = param_dtype == DVDQ_F32;
     A.params_bf16 = param_dtype == DVDQ_BF16;
     A.part = static_cast<float2*>(workspace);
+    A.part64 = static_cast<double2*>(workspace);
     A.pivot = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + room.pivot_off);
     A.arrived = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(workspace) + room.arrived_off);
     A.stat = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + room.stat_off);

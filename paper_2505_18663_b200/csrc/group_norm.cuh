@@ -12,9 +12,9 @@
 // all channels (a thread keeps its 16 bytes of channels, so its loads are whole sectors) and writes two
 // numbers per group; all CTAs meet once; every CTA adds up its sample's numbers in a fixed order (no
 // atomics on data: the same bits every time); pass 2 walks the chunk backwards, first the pieces that pass 1
-// left in shared memory (about 20 MB over the chip), then what the L2 cache still holds.  Sums
-// are of x minus a value of the group itself (the first place's first channel), so that a mean far from
-// zero costs no digits, in fp32 within a chunk and in fp64 across chunks.
+// left in shared memory (about 20 MB over the chip), then what the L2 cache still holds.  A thread sums in fp32, about a centre that
+// follows its own mean (GnMoments), everything beyond in fp64: neither a mean far from zero nor a value far from the mean costs
+// digits.
 // Where that does not fit (channels that 16 bytes do not divide, more than 4096 of them, sample counts that
 // leave SMs idle): three launches, pass 1, join, pass 2, each started while its predecessor drains.
 // Small tensors, one launch: where a slice of whole groups of one sample fits a CTA's shared memory,
@@ -24,6 +24,8 @@
 // of 2 x 18720 places of 512 channels 41 us (115 MB, 2.8 TB/s); 3 x 77 places of 180 fp32 channels 6.3 us in a graph.
 // One launch and three: 2 MB (small kernel aside) 15.7 and 11.9 us, 8 MB 18.5 and 20.1, 61 MB 40 and 41, gradients 57 and 59.
 #pragma once
+
+#include <type_traits>
 
 #include "block_common.cuh"
 
@@ -42,7 +44,8 @@ struct GnArgs {
     float* rstd;
     float* dgamma;
     float* dbeta;
-    float2* part;            // [N, chunks, G]
+    float2* part;            // [N, chunks, G]: sums of the backward pass
+    double2* part64;         // the same room: moments of the forward pass
     float* pivot;            // [N, G]: what pass 1 subtracted (y may be x: pass 2 cannot read it there)
     float2* part_c;          // backward: [N, chunks, C]
     float2* stat;            // [N, G]: (mean, rstd) forward, (<dh>, <dh h>) backward
@@ -66,20 +69,21 @@ __device__ __forceinline__ float gn_param(const void* p, int f32, int bf16, int 
     return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[c]) : __half2float(static_cast<const __half*>(p)[c]);
 }
 
-// Sums of d and d^2 of a thread's pieces.  Squares below half a unit in the last place of a long sum are lost, and small
-// squares are the many: 250 normal values summed one after another are 2e-6 low.  So every 16 pieces the short sum moves on.
+// Sums of d and d^2 of a thread's pieces, d = x - centre, where the centre is the group's mean already (small tensors).  Squares
+// below half a unit in the last place of a long sum are lost, and small squares are the many: 250 normal values summed one after
+// another are 2e-6 low.  So every 16 pieces the short sum moves on.
 template <int V>
-struct GnMoments {
+struct GnCentred {
     Pairs<V> s1, s2, outer;
     int n = 0;
-    __device__ __forceinline__ GnMoments() {
+    __device__ __forceinline__ GnCentred() {
 #pragma unroll
         for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = outer.p[i] = 0ull;
     }
-    __device__ __forceinline__ void add(const Pairs<V>& x, const Pairs<V>& pivot) {
+    __device__ __forceinline__ void add(const Pairs<V>& x, const Pairs<V>& centre) {
 #pragma unroll
         for (int i = 0; i < Pairs<V>::N; ++i) {
-            const uint64_t d = f2_sub(x.p[i], pivot.p[i]);
+            const uint64_t d = f2_sub(x.p[i], centre.p[i]);
             s1.p[i] = f2_add(s1.p[i], d);
             s2.p[i] = f2_fma(d, d, s2.p[i]);
         }
@@ -93,6 +97,78 @@ struct GnMoments {
         }
     }
 };
+
+// The same where the mean is not known yet: d = x - k with a centre k of the thread's own, channel by channel.  k is the first
+// piece, and whenever the number of pieces has doubled it moves to their mean: by e, which takes n e from the sum and
+// e (s1 + s1') from the squares.  So the squares about k are never more than about twice those about the mean, and no single value,
+// the group's first or any other, decides how many digits are left.  (About one fixed value, -1000 among normal values: rstd off by 2e-3.)
+template <int V>
+struct GnMoments {
+    Pairs<V> k, s1, s2, q;
+    int n = 0, next = 0;  // pieces so far; how many there are when the short sum moves on: 0, 2, 4, 8, 16, then every 16
+    __device__ __forceinline__ GnMoments() {
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) k.p[i] = s1.p[i] = s2.p[i] = q.p[i] = 0ull;
+    }
+    __device__ __forceinline__ void add(const Pairs<V>& x) {
+        if (n == next) {
+            if (n == 0) k = x;
+            else flush();
+            if ((n & (n - 1)) == 0 && n > 0) move();
+            next = n == 0 ? 2 : n < 16 ? 2 * n : n + 16;
+        }
+        ++n;
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            const uint64_t d = f2_sub(x.p[i], k.p[i]);
+            s1.p[i] = f2_add(s1.p[i], d);
+            s2.p[i] = f2_fma(d, d, s2.p[i]);
+        }
+    }
+    __device__ __forceinline__ void flush() {
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            q.p[i] = f2_add(q.p[i], s2.p[i]);
+            s2.p[i] = 0ull;
+        }
+    }
+    __device__ __forceinline__ void move() {  // n is a power of two
+        const float count = (float)n;
+        const uint64_t minus_n = f2_splat(-count), one_nth = f2_splat(__int_as_float(0x7F000000 - __float_as_int(count)));
+#pragma unroll
+        for (int i = 0; i < Pairs<V>::N; ++i) {
+            const uint64_t to = f2_fma(s1.p[i], one_nth, k.p[i]), e = f2_sub(to, k.p[i]), s = f2_fma(minus_n, e, s1.p[i]);
+            q.p[i] = f2_sub(q.p[i], f2_mul(e, f2_add(s1.p[i], s)));
+            s1.p[i] = s;
+            k.p[i] = to;
+        }
+    }
+    // use(u, sums of x - pivot and its square over unit u) after the last flush(); a unit is 1 << log channels of one group.  Within it
+    // the sums are brought to its first channel's centre in fp32 (a value that lies far out there, and so moves that centre, has its
+    // own square among them), then to the group's pivot in fp64, in which they stay.
+    template <typename Use>
+    __device__ __forceinline__ void by_unit(int log, const float (&pivot)[V], Use use) const {
+        const int last = (1 << log) - 1;
+        const float count = (float)n;
+        float k0 = 0.f, a = 0.f, b = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if ((i & last) == 0) {
+                k0 = k.get(i);
+                a = b = 0.f;
+            }
+            const float e = k.get(i) - k0, s = s1.get(i), moved = fmaf(count, e, s);
+            a += moved;
+            b += fmaf(e, s + moved, q.get(i));
+            if ((i & last) == last) {
+                const double shift = (double)k0 - (double)pivot[i], all = (double)(n << log), to = a + all * shift;
+                use(i >> log, make_double2(to, b + shift * (a + to)));
+            }
+        }
+    }
+};
+// log2 of the channels of a unit: as many as divide both a thread's vector and the group
+__device__ __forceinline__ int gn_unit(int per, int V) { return __ffs(per | V) - 1; }
 
 // Where this thread works: channel vector v of its CTA's channel block, row r of `lanes` side by side.
 template <int V>
@@ -132,22 +208,22 @@ struct GnPlace {
 };
 
 // Adds the threads' sums over the lanes, pairwise (a long sum of equal terms loses digits, and a serial walk over a thousand
-// lanes takes 16 us).  Thread r * vecs + v of `on` threads holds channels v V ..; sum i of vector v ends in sh[i * threads + v].
-template <int V>
-__device__ __forceinline__ void gn_sum_lanes(bool on, int r, int lanes, int vecs, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
+// lanes takes 16 us).  Thread r * vecs + v of `on` threads has put its `sums` sums of vector v at sh[i * threads + thread]; the total
+// of sum i ends in sh[i * threads + v].
+template <typename Pair>
+__device__ __forceinline__ void gn_sum_lanes(bool on, int r, int lanes, int vecs, int sums, Pair* sh) {
     const int threads = lanes * vecs, t = threadIdx.x;
-    if (on) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) sh[i * threads + t] = make_float2(s1.get(i), s2.get(i));
-    }
     __syncthreads();
     for (int left = lanes; left > 1;) {
         const int half = (left + 1) >> 1;
         if (on && r < left - half) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float2 a = sh[i * threads + t], b = sh[i * threads + t + half * vecs];
-                sh[i * threads + t] = make_float2(a.x + b.x, a.y + b.y);
+#pragma unroll 4
+            for (int i = 0; i < sums; ++i) {
+                Pair a = sh[i * threads + t];
+                const Pair b = sh[i * threads + t + half * vecs];
+                a.x += b.x;
+                a.y += b.y;
+                sh[i * threads + t] = a;
             }
         }
         left = half;
@@ -155,39 +231,30 @@ __device__ __forceinline__ void gn_sum_lanes(bool on, int r, int lanes, int vecs
     }
 }
 
-// ... then over the channels of each group in this block, and writes one pair per group (and per channel).
-template <int V, bool PER_CHANNEL>
-__device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
-    const int threads = A.lanes * A.vecs;
-    gn_sum_lanes<V>(P.r < A.lanes, P.r, A.lanes, A.vecs, s1, s2, sh);  // vectors past the block's end carry zeros
-    const int64_t slot = (int64_t)blockIdx.y * A.chunks + blockIdx.x;
-    auto place = [&](int c) { return (c % V) * threads + c / V; };  // of the block's channel c
-    if (PER_CHANNEL) {
-        for (int c = threadIdx.x; c < P.here; c += kGnThreads) {
-            float2 t = sh[place(c)];
-            A.part_c[slot * A.C + P.cbase + c] = t;
-            const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, P.cbase + c, 1.0f);
-            sh[place(c)] = make_float2(t.x * g, t.y * g);
-        }
-        __syncthreads();
-    }
-    const int groups = P.g1 - P.g0, span = A.bpg == 1 ? A.per : P.here;
-    float2* out = A.part + slot * (A.G * A.bpg) + (A.bpg == 1 ? P.g0 : (int)blockIdx.z);
+template <int V>
+__device__ __forceinline__ void gn_put_sums(int threads, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) sh[i * threads + threadIdx.x] = make_float2(s1.get(i), s2.get(i));
+}
+
+// ... then over the `span` channels (or units) of each group: put(g, the sum of channel(g span) .. channel(g span + span - 1)).
+template <int THREADS, typename Pair, typename Channel, typename Put>
+__device__ __forceinline__ void gn_sum_groups(int groups, int span, Channel channel, Put put) {
     if (span <= 8) {
-        for (int g = threadIdx.x; g < groups; g += kGnThreads) {
-            float2 t = sh[place(g * span)];
+        for (int g = threadIdx.x; g < groups; g += THREADS) {
+            Pair t = channel(g * span);
             for (int i = 1; i < span; ++i) {
-                const float2 u = sh[place(g * span + i)];
+                const Pair u = channel(g * span + i);
                 t.x += u.x;
                 t.y += u.y;
             }
-            out[g] = t;
+            put(g, t);
         }
     } else {  // wide groups: a warp each
-        for (int g = threadIdx.x >> 5; g < groups; g += kGnThreads / 32) {
-            float2 t = make_float2(0.f, 0.f);
+        for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {
+            Pair t = {};
             for (int i = threadIdx.x & 31; i < span; i += 32) {
-                const float2 u = sh[place(g * span + i)];
+                const Pair u = channel(g * span + i);
                 t.x += u.x;
                 t.y += u.y;
             }
@@ -196,9 +263,41 @@ __device__ __forceinline__ void gn_reduce_block(const GnArgs& A, const GnPlace<V
                 t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
                 t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
             }
-            if ((threadIdx.x & 31) == 0) out[g] = t;
+            if ((threadIdx.x & 31) == 0) put(g, t);
         }
     }
+}
+
+// A block's moments about the groups' pivots, a pair per group, in fp64 from the threads on.
+template <int V>
+__device__ __forceinline__ void gn_block_moments(const GnArgs& A, const GnPlace<V>& P, const GnMoments<V>& m, const float (&pivot)[V], double2* sh) {
+    const int threads = A.lanes * A.vecs, log = gn_unit(A.per, V), units = V >> log, wide = 31 - __clz(units);
+    const bool on = P.r < A.lanes;  // vectors past the block's end carry zeros
+    if (on) m.by_unit(log, pivot, [&](int u, const double2& t) { sh[u * threads + threadIdx.x] = t; });
+    gn_sum_lanes(on, P.r, A.lanes, A.vecs, units, sh);
+    double2* out = A.part64 + ((int64_t)blockIdx.y * A.chunks + blockIdx.x) * (A.G * A.bpg) + (A.bpg == 1 ? P.g0 : (int)blockIdx.z);
+    gn_sum_groups<kGnThreads, double2>(P.g1 - P.g0, (A.bpg == 1 ? A.per : P.here) >> log,
+                                       [&](int u) { return sh[(u & (units - 1)) * threads + (u >> wide)]; },
+                                       [&](int g, const double2& t) { out[g] = t; });
+}
+// A block's sums of the backward pass, a pair per channel and, gamma in them, per group.
+template <int V>
+__device__ __forceinline__ void gn_block_sums(const GnArgs& A, const GnPlace<V>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
+    const int threads = A.lanes * A.vecs;
+    if (P.r < A.lanes) gn_put_sums<V>(threads, s1, s2, sh);  // vectors past the block's end carry zeros
+    gn_sum_lanes(P.r < A.lanes, P.r, A.lanes, A.vecs, V, sh);
+    const int64_t slot = (int64_t)blockIdx.y * A.chunks + blockIdx.x;
+    auto place = [&](int c) { return (c % V) * threads + c / V; };  // of the block's channel c
+    for (int c = threadIdx.x; c < P.here; c += kGnThreads) {
+        float2 t = sh[place(c)];
+        A.part_c[slot * A.C + P.cbase + c] = t;
+        const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, P.cbase + c, 1.0f);
+        sh[place(c)] = make_float2(t.x * g, t.y * g);
+    }
+    __syncthreads();
+    float2* out = A.part + slot * (A.G * A.bpg) + (A.bpg == 1 ? P.g0 : (int)blockIdx.z);
+    gn_sum_groups<kGnThreads, float2>(P.g1 - P.g0, A.bpg == 1 ? A.per : P.here, [&](int c) { return sh[place(c)]; },
+                                      [&](int g, const float2& t) { out[g] = t; });
 }
 
 constexpr int kGnDepth = 8, kGnGradDepth = 5;  // slots: 32 KB a CTA, 40 KB for two tensors; four CTAs per SM
@@ -211,23 +310,21 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_stats_kernel(const __grid_co
     const GnPlace<V> P(A);
     const int n = blockIdx.y;
     GnMoments<V> sums;
+    float pivot[V] = {};
     if (P.on) {
         const T* base = static_cast<const T*>(A.x) + (int64_t)n * A.xn;
-        float pv[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int g = (P.c0 + i) / A.per;
-            pv[i] = to_f32(base[g * A.per]);
-            if (blockIdx.x == 0 && P.r == 0 && P.c0 + i == g * A.per) A.pivot[(int64_t)n * A.G + g] = pv[i];
+            pivot[i] = to_f32(base[g * A.per]);
+            if (blockIdx.x == 0 && P.r == 0 && P.c0 + i == g * A.per) A.pivot[(int64_t)n * A.G + g] = pivot[i];
         }
-        Pairs<V> pivot;
-        pivot.set(pv);
         walk<kGnDepth, 1, T, V>(raw, P.count(A.lanes), base + P.c0 + (P.s0 + P.r) * A.xs, A.lanes * A.xs, nullptr, 0,
-                                 [&](const Vec<T, V>& v) { sums.add(widen2<T, V>(v), pivot); });
+                                 [&](const Vec<T, V>& v) { sums.add(widen2<T, V>(v)); });
         sums.flush();
     }
     __syncthreads();  // the ring's memory becomes the sums'
-    gn_reduce_block<V, false>(A, P, sums.s1, sums.outer, reinterpret_cast<float2*>(raw));
+    gn_block_moments<V>(A, P, sums, pivot, reinterpret_cast<double2*>(raw));
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -244,6 +341,13 @@ __device__ __forceinline__ float2 gn_mean_rstd(double pivot, double m1, double m
 
 // Adds up the chunks: the first `group_ctas` CTAs a warp per group, the rest (backward) 32 channels each.
 template <bool BACKWARD>
+using GnPart = typename std::conditional<BACKWARD, float2, double2>::type;
+template <bool BACKWARD>
+__device__ __forceinline__ const GnPart<BACKWARD>* gn_part(const GnArgs& A) {
+    if constexpr (BACKWARD) return A.part;
+    else return A.part64;
+}
+template <bool BACKWARD>
 __global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_constant__ GnArgs A, int group_ctas) {
     constexpr int kWarps = kGnThreads / 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -254,19 +358,20 @@ __global__ void __launch_bounds__(kGnThreads) gn_join_kernel(const __grid_consta
         if (ng >= (int64_t)A.N * A.G) return;
         const int n = (int)(ng / A.G), g = (int)(ng - (int64_t)n * A.G);
         const int entries = A.chunks * A.bpg, pitch = A.G * A.bpg;
-        const float2* base = A.part + (int64_t)n * A.chunks * pitch + (int64_t)g * A.bpg;
+        using Part = GnPart<BACKWARD>;
+        const Part* base = gn_part<BACKWARD>(A) + (int64_t)n * A.chunks * pitch + (int64_t)g * A.bpg;
         double a = 0.0, b = 0.0;
         auto entry = [&](int i) { return A.bpg == 1 ? base[(int64_t)i * pitch] : base[(int64_t)(i / A.bpg) * pitch + i % A.bpg]; };
         int i = lane;
         for (; i + 7 * 32 < entries; i += 8 * 32) {
-            float2 t[8];
+            Part t[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) t[u] = entry(i + 32 * u);
 #pragma unroll
             for (int u = 0; u < 8; ++u) { a += t[u].x; b += t[u].y; }
         }
         for (; i < entries; i += 32) {
-            const float2 t = entry(i);
+            const Part t = entry(i);
             a += t.x;
             b += t.y;
         }
@@ -455,7 +560,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_grad_stats_kernel(const __gr
         });
     }
     __syncthreads();  // the ring's memory becomes the sums'
-    gn_reduce_block<V, true>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
+    gn_block_sums<V>(A, P, s1, s2, reinterpret_cast<float2*>(raw));
 }
 
 // dx = rstd (gamma dz - m1 - h m2) = dz (rstd gamma) + (h (-rstd m2) + (-rstd m1))
@@ -546,48 +651,53 @@ struct GnTeam {
     }
 };
 
-// Adds the threads' sums over the lanes, then over each group's channels, and writes the CTA's numbers.
-template <int V, int THREADS, bool PER_CHANNEL>
+// The CTA's moments about the groups' pivots, a pair per group, in fp64 from the threads on; four units of each vector at a
+// time, since the ring keeps the rest of the shared memory (eight only where a group has an odd number of 16-bit channels).
+template <int V> struct GnRound { static constexpr int units = V < 4 ? V : 4; };
+template <int V, int THREADS>
+__device__ __forceinline__ void gn_team_moments(const GnArgs& A, const GnTeam<V, THREADS>& P, const GnMoments<V>& m, const float (&pivot)[V], double2* sh) {
+    const int threads = P.lanes * A.vecs, log = gn_unit(A.per, V), units = V >> log, wide = 31 - __clz(units), w = min(units, GnRound<V>::units);
+    double2* out = A.part64 + (int64_t)P.n * A.G * A.chunks + P.j;
+#pragma unroll 1
+    for (int first = 0; first < units; first += w) {
+        if (first > 0) __syncthreads();
+        auto here = [&](int u) { return (uint32_t)(u - first) < (uint32_t)w; };
+        if (P.on)
+            m.by_unit(log, pivot, [&](int u, const double2& t) {
+                if (here(u)) sh[(u - first) * threads + threadIdx.x] = t;
+            });
+        gn_sum_lanes(P.on, P.r, P.lanes, A.vecs, w, sh);
+        gn_sum_groups<THREADS, double2>(A.G, A.per >> log,
+            [&](int u) {
+                const int i = u & (units - 1);
+                return here(i) ? sh[(i - first) * threads + (u >> wide)] : make_double2(0.0, 0.0);
+            },
+            [&](int g, double2 t) {
+                double2* to = out + (int64_t)g * A.chunks;
+                if (first > 0) {  // this thread's own number of the round before
+                    t.x += to->x;
+                    t.y += to->y;
+                }
+                *to = t;
+            });
+    }
+}
+// The CTA's sums of the backward pass, a pair per channel and, gamma in them, per group.
+template <int V, int THREADS>
 __device__ __forceinline__ void gn_team_sums(const GnArgs& A, const GnTeam<V, THREADS>& P, const Pairs<V>& s1, const Pairs<V>& s2, float2* sh) {
     const int threads = P.lanes * A.vecs;
-    gn_sum_lanes<V>(P.on, P.r, P.lanes, A.vecs, s1, s2, sh);
+    if (P.on) gn_put_sums<V>(threads, s1, s2, sh);
+    gn_sum_lanes(P.on, P.r, P.lanes, A.vecs, V, sh);
     auto channel = [&](int c) -> float2& { return sh[(c % V) * threads + c / V]; };
-    if (PER_CHANNEL) {
-        for (int c = threadIdx.x; c < A.C; c += THREADS) {
-            const float2 t = channel(c);
-            A.part_c[(int64_t)c * gridDim.x + blockIdx.x] = t;
-            const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
-            channel(c) = make_float2(t.x * g, t.y * g);
-        }
-        __syncthreads();
+    for (int c = threadIdx.x; c < A.C; c += THREADS) {
+        const float2 t = channel(c);
+        A.part_c[(int64_t)c * gridDim.x + blockIdx.x] = t;
+        const float g = gn_param(A.gamma, A.params_f32, A.params_bf16, c, 1.0f);
+        channel(c) = make_float2(t.x * g, t.y * g);
     }
+    __syncthreads();
     float2* out = A.part + (int64_t)P.n * A.G * A.chunks + P.j;
-    if (A.per <= 8) {
-        for (int g = threadIdx.x; g < A.G; g += THREADS) {
-            float2 t = channel(g * A.per);
-            for (int i = 1; i < A.per; ++i) {
-                const float2 u = channel(g * A.per + i);
-                t.x += u.x;
-                t.y += u.y;
-            }
-            out[(int64_t)g * A.chunks] = t;
-        }
-    } else {
-        for (int g = threadIdx.x >> 5; g < A.G; g += THREADS / 32) {
-            float2 t = make_float2(0.f, 0.f);
-            for (int i = threadIdx.x & 31; i < A.per; i += 32) {
-                const float2 u = channel(g * A.per + i);
-                t.x += u.x;
-                t.y += u.y;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                t.x += __shfl_xor_sync(0xFFFFFFFFu, t.x, o);
-                t.y += __shfl_xor_sync(0xFFFFFFFFu, t.y, o);
-            }
-            if ((threadIdx.x & 31) == 0) out[(int64_t)g * A.chunks] = t;
-        }
-    }
+    gn_sum_groups<THREADS, float2>(A.G, A.per, channel, [&](int g, const float2& t) { out[(int64_t)g * A.chunks] = t; });
 }
 
 // All CTAs of the (cooperative, hence co-resident) launch meet: what each wrote before is seen by all after.
@@ -616,16 +726,16 @@ __device__ __forceinline__ void gn_meet(uint32_t* arrived) {
 }
 
 // The sample's numbers ([N, G, chunks]: a group's are neighbours), a warp per group: stat[g] = finish(g, mean of the first, mean of the second).
-template <int THREADS, typename Finish>
-__device__ __forceinline__ void gn_team_join(const GnArgs& A, int n, float2* stat, Finish finish) {
+template <int THREADS, typename Part, typename Finish>
+__device__ __forceinline__ void gn_team_join(const GnArgs& A, int n, const Part* part, float2* stat, Finish finish) {
     const int lane = threadIdx.x & 31;
     for (int g = threadIdx.x >> 5; g < A.G; g += THREADS / 32) {
-        const float2* base = A.part + ((int64_t)n * A.G + g) * A.chunks;
+        const Part* base = part + ((int64_t)n * A.G + g) * A.chunks;
         double a = 0.0, b = 0.0;
-        float2 t[5];
+        Part t[5];
         for (int i = lane; i < A.chunks; i += 5 * 32) {  // at most 148 chunks: once
 #pragma unroll
-            for (int u = 0; u < 5; ++u) t[u] = i + 32 * u < A.chunks ? __ldcg(base + i + 32 * u) : make_float2(0.f, 0.f);
+            for (int u = 0; u < 5; ++u) t[u] = i + 32 * u < A.chunks ? __ldcg(base + i + 32 * u) : Part{};
 #pragma unroll
             for (int u = 0; u < 5; ++u) {
                 a += t[u].x;
@@ -652,18 +762,16 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
     __syncthreads();
     {
         GnMoments<V> moments;
-        Pairs<V> pivot;
-        float pv[V];
-        gn_by_channel<V>(A.per, P.c0, [&](int i, int g) { pv[i] = pivots[g]; }, [&](int i) { pv[i] = pv[0]; });
-        pivot.set(pv);
-        walk.forward([&](const Vec<T, V>& in) { moments.add(widen2<T, V>(in), pivot); });
+        walk.forward([&](const Vec<T, V>& in) { moments.add(widen2<T, V>(in)); });
         moments.flush();
-        gn_team_sums<V, THREADS, false>(A, P, moments.s1, moments.outer, sums);
+        float pivot[V];
+        gn_by_channel<V>(A.per, P.c0, [&](int i, int g) { pivot[i] = pivots[g]; }, [&](int i) { pivot[i] = pivot[0]; });
+        gn_team_moments<V, THREADS>(A, P, moments, pivot, reinterpret_cast<double2*>(sums));
     }
     float ga[V], be[V];
     gn_params<V>(A, P.c0, ga, be);  // before the wait; at the start, next to the streams, 148 CTAs' reads of one line took 4 us
     gn_meet(A.arrived);
-    gn_team_join<THREADS>(A, P.n, sums, [&](int g, double m1, double m2) {
+    gn_team_join<THREADS>(A, P.n, A.part64, sums, [&](int g, double m1, double m2) {
         const float2 t = gn_mean_rstd((double)pivots[g], m1, m2, A.eps);
         if (P.j == 0 && A.mean) A.mean[(int64_t)P.n * A.G + g] = t.x;
         if (P.j == 0 && A.rstd) A.rstd[(int64_t)P.n * A.G + g] = t.y;
@@ -707,10 +815,10 @@ __global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(c
                 s2.p[i] = f2_fma(dz, h, s2.p[i]);
             }
         });
-        gn_team_sums<V, THREADS, true>(A, P, s1, s2, sums);
+        gn_team_sums<V, THREADS>(A, P, s1, s2, sums);
     }
     gn_meet(A.arrived);
-    gn_team_join<THREADS>(A, P.n, sums, [](int, double m1, double m2) { return make_float2((float)m1, (float)m2); });
+    gn_team_join<THREADS>(A, P.n, A.part, sums, [](int, double m1, double m2) { return make_float2((float)m1, (float)m2); });
     if (P.on && A.y) {
         const GnDx<V> dx = gn_dx<V>(A, P.c0, sums, rs, ga);
         T* q = static_cast<T*>(A.y) + (int64_t)P.n * A.yn + P.c0 + (P.s0 + (int64_t)(P.count - 1) * P.lanes) * A.ys;
@@ -836,7 +944,7 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
         gn_by_channel<V>(A.per, c0, [&](int i, int g) { mean[i] = (float)((double)mu.get(i) + totals[g - g0].x * A.inv); },
                          [&](int i) { mean[i] = mean[0]; });
         mu.set(mean);
-        GnMoments<V> m;
+        GnCentred<V> m;
         for (int s = r; s < S; s += A.lanes) m.add(widen2<T, V>(data[s * A.vecs + v]), mu);
         m.flush();
 #pragma unroll
@@ -909,7 +1017,8 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
             }
         }
     }
-    gn_sum_lanes<V>(r < A.lanes, r, A.lanes, A.vecs, s1, s2, red);
+    if (r < A.lanes) gn_put_sums<V>(A.lanes * A.vecs, s1, s2, red);
+    gn_sum_lanes(r < A.lanes, r, A.lanes, A.vecs, V, red);
     for (int c = threadIdx.x; c < here; c += kGnThreads) {
         const float2 t = red[(c % V) * (A.lanes * A.vecs) + c / V];
         if (A.N > 1) {
@@ -1012,7 +1121,7 @@ inline GnRoom gn_room(int64_t N, int64_t S, int64_t C, int64_t G) {
     const GnPlan p = gn_plan(N, S, 4);
     const int64_t slots = N * p.chunks > kGnFusedCtas ? N * p.chunks : kGnFusedCtas;  // CTAs that write sums, either way
     GnRoom r;
-    r.pivot_off = align_up(slots * G * gn_pieces(C / G) * 8, 256);
+    r.pivot_off = align_up(slots * G * gn_pieces(C / G) * 16, 256);  // two fp64 numbers
     r.stat_off = r.pivot_off + align_up(N * G * 4, 256);
     r.part_c_off = r.stat_off + align_up(N * G * 8, 256);
     r.arrived_off = r.part_c_off + align_up(slots * C * 8, 256);
@@ -1136,7 +1245,7 @@ static bool launch_gn_small(GnArgs A, bool backward, cudaStream_t st, cudaError_
 template <typename T, int V, int ACT>
 static bool launch_gn_one(const GnArgs& A, bool backward, cudaStream_t st, cudaError_t* e) {
     static PerDevice<int> fused, fused_grad;
-    constexpr size_t sums = (size_t)kGnFusedThreads * V * sizeof(float2), grad_sums = (size_t)kGnFusedGradThreads * V * sizeof(float2);
+    constexpr size_t sums = (size_t)kGnFusedThreads * GnRound<V>::units * sizeof(double2), grad_sums = (size_t)kGnFusedGradThreads * V * sizeof(float2);
     constexpr size_t ring = TwoWay<GnDepth<T, V>::fused, 1, kGnFusedThreads, T, V>::kRingBytes;
     constexpr size_t grad_ring = TwoWay<GnDepth<T, V>::fused_grad, 2, kGnFusedGradThreads, T, V>::kRingBytes;
     static_assert(ring + sums + kGnFusedGroups * 4 <= 232448 && grad_ring + grad_sums <= 232448, "more than the 227 KB of shared memory a CTA can have");
@@ -1152,7 +1261,7 @@ static bool launch_gn_three(GnArgs A, bool backward, cudaStream_t st, cudaError_
     const unsigned group_ctas = (unsigned)ceil_div((int64_t)A.N * A.G, kGnThreads / 32);
     // the rings; the sums of pass 1 (V pairs per thread) take their place
     constexpr bool ring = WholePieces<T, V>::value;
-    constexpr size_t sums = (size_t)kGnThreads * V * sizeof(float2);
+    constexpr size_t sums = (size_t)kGnThreads * V * sizeof(double2), grad_sums = (size_t)kGnThreads * V * sizeof(float2);
     constexpr size_t one = ring ? (size_t)kGnThreads * 16 * kGnDepth : 0, two = ring ? (size_t)kGnThreads * 16 * 2 * kGnGradDepth : 0;
     static_assert(one <= 48 * 1024 && two <= 48 * 1024 && sums <= 48 * 1024, "more than a kernel has without asking");
     if (!backward) {
@@ -1161,7 +1270,7 @@ static bool launch_gn_three(GnArgs A, bool backward, cudaStream_t st, cudaError_
         *e = launch_after(gn_apply_kernel<T, V, ACT>, grid, block, one, st, A);
         return true;
     }
-    if ((*e = launch_after(gn_grad_stats_kernel<T, V, ACT>, grid, block, sums > two ? sums : two, st, A)) != cudaSuccess) return true;
+    if ((*e = launch_after(gn_grad_stats_kernel<T, V, ACT>, grid, block, grad_sums > two ? grad_sums : two, st, A)) != cudaSuccess) return true;
     const unsigned channel_ctas = A.dgamma || A.dbeta ? (unsigned)ceil_div(A.C, 32) : 0;
     *e = launch_after(gn_join_kernel<true>, dim3(group_ctas + channel_ctas), block, 0, st, A, (int)group_ctas);
     if (*e == cudaSuccess && A.y) *e = launch_after(gn_grad_apply_kernel<T, V, ACT>, grid, block, two, st, A);

@@ -292,3 +292,45 @@ def test_small_squares_are_not_lost_in_long_sums(shape):
     _, m6, r6, _, _ = norm64(x.double(), G, None, None, 0)
     assert ((rstd - r6) / r6).abs().max() <= 5e-7
     assert (mean - m6).abs().max() <= 2.0 ** -23
+
+
+# ------------------------------------------------------------------ values that are far out
+
+# one launch in shared memory; one launch over all SMs; three launches (80 samples leave SMs idle; single elements)
+PATHS = {"small": (2, 40), "one": (1, 20000), "three": (80, 3000)}
+
+
+def run_forward(x, G, gamma, beta, act, eps=EPS):
+    N, S, C = x.shape
+    y, mean, rstd = torch.full_like(x, float("nan")), torch.empty(N, G, device=DEV), torch.empty(N, G, device=DEV)
+    B.dvdq_group_norm(x, G, gamma, beta, eps, act, y, mean, rstd, workspace(N, S, C, G))
+    return y, mean, rstd
+
+
+def run_backward(dy, x, mean, rstd, G, gamma, beta, act):
+    N, S, C = x.shape
+    dx, dg, db = torch.full_like(x, float("nan")), torch.empty(C, device=DEV), torch.empty(C, device=DEV)
+    B.dvdq_group_norm_backward(dy, x, mean, rstd, G, gamma, beta, act, dx, dg, db, workspace(N, S, C, G))
+    return dx, dg, db
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 162285, 8, 4), (1, 20000, 128, 32), (4, 1000, 96, 4), (80, 3000, 64, 4), (1, 40000, 35, 5), (2, 64, 64, 4),
+                                   (1, 30000, 36, 4), (1, 9000, 34, 2), (1, 70, 9000, 9), (1, 30000, 1, 1)])
+@pytest.mark.parametrize("first", [-50.0, -1000.0, -10000.0, 0.0])
+def test_an_outlying_first_value_costs_no_digits(dt, shape, first):
+    """Whatever the first value of each group is (far from the rest, or 0 where the rest is near 300), the variance keeps the accuracy
+    of its own size, not of the spread about that value.  Per thread: short sums of 16 squares, 8 channels brought to one centre,
+    each of at most twice the squares about the mean, 2^-24 a rounding: 2 (16 + 8) 2^-24 = 2.9e-6 if none cancelled, half of
+    that for rstd; most do: 1e-6.  The mean: the same roundings of at most the deviations' sizes."""
+    N, S, C, G = shape
+    g = torch.Generator(device=DEV).manual_seed(S)
+    x = (0.3 + torch.randn(N, S, C, generator=g, device=DEV)).to(dt)
+    if first == 0.0:
+        x = (x.float() + 300.0).to(dt)
+    x[:, 0, ::C // G] = first
+    _, mean, rstd = run_forward(x, G, None, None, 0)
+    _, m6, r6, _, _ = norm64(x.double(), G, None, None, 0)
+    assert ((rstd - r6) / r6).abs().max() <= 1e-6
+    assert (((mean - m6).abs() - 2.0 ** -24 * m6.abs()) * r6).max() <= 1e-6   # 2^-24: its own rounding
