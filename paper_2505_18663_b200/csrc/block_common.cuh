@@ -161,9 +161,9 @@ template <bool SHARED>
 __device__ __forceinline__ uint64_t logistic2_scaled(uint64_t e) {
     float a, b;
     f2_unpack(e, a, b);
-    if (SHARED) {  // NaN stays NaN
-        asm("min.NaN.f32 %0, %0, 0f42700000;" : "+f"(a));
-        asm("min.NaN.f32 %0, %0, 0f42700000;" : "+f"(b));
+    if (SHARED) {  // of NaN this makes 60: it must not reach the other value (maybe another group's); its own result is NaN by z
+        asm("min.f32 %0, %0, 0f42700000;" : "+f"(a));
+        asm("min.f32 %0, %0, 0f42700000;" : "+f"(b));
     }
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));

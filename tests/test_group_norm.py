@@ -334,3 +334,54 @@ def test_an_outlying_first_value_costs_no_digits(dt, shape, first):
     _, m6, r6, _, _ = norm64(x.double(), G, None, None, 0)
     assert ((rstd - r6) / r6).abs().max() <= 1e-6
     assert (((mean - m6).abs() - 2.0 ** -24 * m6.abs()) * r6).max() <= 1e-6   # 2^-24: its own rounding
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("C,G", [(24, 8), (16, 16), (40, 8), (64, 16)])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_not_finite_stays_in_its_group(dt, path, C, G, act, bad):
+    (N, S), per = PATHS[path], C // G
+    g = torch.Generator(device=DEV).manual_seed(C)
+    x, dy = torch.randn(N, S, C, generator=g, device=DEV).to(dt), torch.randn(N, S, C, generator=g, device=DEV).to(dt)
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g, device=DEV), 0.3 * torch.randn(C, generator=g, device=DEV)
+    clean = run_forward(x, G, gamma, beta, act)
+    clean_back = run_backward(dy, x, clean[1], clean[2], G, gamma, beta, act)
+    xb = x.clone()
+    xb[:, S // 2, 2 * per - 1] = bad
+    y, mean, rstd = run_forward(xb, G, gamma, beta, act)
+    dx, dg, db = run_backward(dy, xb, mean, rstd, G, gamma, beta, act)
+    rest = [c for c in range(C) if c // per != 1]
+    inside = [c for c in range(C) if c // per == 1]
+    assert y[..., inside].isnan().all() and dx[..., inside].isnan().all()
+    # what shares an access with a value that is not a number has its logistic function formed in another way: both runs are
+    # within 2^-18 (1 + |z|) of the slope (1.2 at most times as much), of 2^-18 |z| of the value
+    groups = lambda t: t.view(N, S, G, per).mean((1, 3), keepdim=True).expand(N, S, G, per).reshape(N, S, C)  # noqa: E731
+    r = clean[2].double().repeat_interleave(per, 1)[:, None]
+    h = (x.double() - clean[1].double().repeat_interleave(per, 1)[:, None]) * r
+    z, g6 = h * gamma.double() + beta.double(), gamma.double().abs()
+    ez = 2 * 2.0 ** -18 * 1.2 * dy.double().abs() * (1 + z.abs()) if act else torch.zeros_like(z)
+    dz, h = 1.2 * dy.double().abs(), h.abs()
+    rx = r * (ez * g6 + groups(ez * g6) + h * groups(ez * g6 * h) + 2.0 ** -20 * (dz * g6 + groups(dz * g6) + h * groups(dz * g6 * h)))
+    for got, want, rough, u in ((y, clean[0], 2 * 2.0 ** -18 * z.abs(), U[dt]), (dx, clean_back[0], rx, U[dt]),
+                                (dg, clean_back[1], (ez * h + E * dz * h).sum((0, 1)), 0.0), (db, clean_back[2], (ez + E * dz).sum((0, 1)), 0.0)):
+        got, want, rough = got[..., rest].double(), want[..., rest].double(), rough[..., rest]
+        assert ((got - want).abs() <= rough + 2 * u * (want.abs() + rough) + (2.0 ** -24 if dt == torch.float16 else 0.0)).all()
+
+
+@gpu
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("act", [1, 2])
+def test_a_parameter_that_is_not_a_number_stays_in_its_channel(path, act):
+    (N, S), C, G, dt = PATHS[path], 32, 4, torch.bfloat16
+    g = torch.Generator(device=DEV).manual_seed(C)
+    x = torch.randn(N, S, C, generator=g, device=DEV).to(dt)
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g, device=DEV), 0.3 * torch.randn(C, generator=g, device=DEV)
+    clean, _, _ = run_forward(x, G, gamma, beta, act)
+    gamma[9], beta[20] = float("nan"), float("nan")
+    y, _, _ = run_forward(x, G, gamma, beta, act)
+    rest = [c for c in range(C) if c not in (9, 20)]
+    got, want = y[..., rest].double(), clean[..., rest].double()
+    assert y[..., [9, 20]].isnan().all() and ((got - want).abs() <= 2 * U[dt] * want.abs() + 2.0 ** -18).all()
