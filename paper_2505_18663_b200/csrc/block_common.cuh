@@ -156,11 +156,12 @@ __device__ __forceinline__ Vec<T, V> narrow2(const Pairs<V>& r) {
 __device__ __forceinline__ uint64_t f2_splat(float v) { return f2_pack(v, v); }
 // logistic(u) of a pair, given -log2(e) u.  SHARED: one reciprocal for both, 1/a = b / (ab), for kernels that the
 // special-function unit (16 a clock per SM; two per value otherwise) would bound.  The exponents are then held at
-// 60, so that ab stays finite: logistic(u) is 2^-60 for all u below -41.6.
+// 60, so that ab stays finite, and past that logistic(u), below 2^-60, is 0: z times 2^-60 would not be small for z = -1e20.
 template <bool SHARED>
 __device__ __forceinline__ uint64_t logistic2_scaled(uint64_t e) {
     float a, b;
     f2_unpack(e, a, b);
+    const bool a_gone = a > 60.0f, b_gone = b > 60.0f;
     if (SHARED) {  // of NaN this makes 60: it must not reach the other value (maybe another group's); its own result is NaN by z
         asm("min.f32 %0, %0, 0f42700000;" : "+f"(a));
         asm("min.f32 %0, %0, 0f42700000;" : "+f"(b));
@@ -171,7 +172,7 @@ __device__ __forceinline__ uint64_t logistic2_scaled(uint64_t e) {
     if (SHARED) {
         float r = a * b;
         asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
-        return f2_mul(f2_splat(r), f2_pack(b, a));
+        return f2_mul(f2_splat(r), f2_pack(a_gone ? 0.0f : b, b_gone ? 0.0f : a));
     }
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));

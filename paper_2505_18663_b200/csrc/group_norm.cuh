@@ -506,8 +506,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
 
 // ------------------------------------------------------------------ backward
 
-// What the backward passes hold per channel: h = (x - mean) rstd, z = gamma h + beta.  |h| is at most the
-// root of the group's size, so the shared reciprocal's 2^-60 in place of a smaller number is far below any rounding.
+// What the backward passes hold per channel: h = (x - mean) rstd, z = gamma h + beta.
 template <typename T, int V>
 struct GnGrad {
     GnScale<T, V> h;

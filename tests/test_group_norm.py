@@ -385,3 +385,30 @@ def test_a_parameter_that_is_not_a_number_stays_in_its_channel(path, act):
     rest = [c for c in range(C) if c not in (9, 20)]
     got, want = y[..., rest].double(), clean[..., rest].double()
     assert y[..., [9, 20]].isnan().all() and ((got - want).abs() <= 2 * U[dt] * want.abs() + 2.0 ** -18).all()
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("act", [1, 2])
+def test_activations_of_the_lowest_values(dt, path, act):
+    """A channel whose beta is the lowest value (a mask) is 0 after the activation, and its slope is 0; z = -inf gives NaN, as
+    z / (1 + exp(-z)) does.  2e-5: 2^-18 of |z| < 5, twice for the statistics' roundings in z."""
+    (N, S), C, G = PATHS[path], 32, 2
+    x = torch.randn(N, S, C, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3)).to(dt)
+    lowest = torch.finfo(torch.float32).min
+    beta = torch.zeros(C, device=DEV)
+    special = torch.tensor([-45.0, -60.0, -100.0, -1e4, -1e20, lowest, 1e20 if dt != torch.float16 else 6e4, float("-inf")], device=DEV)
+    beta[5:13] = special
+    beta[20] = -1e20
+    y, mean, rstd = run_forward(x, G, None, beta, act)
+    y6, _, _, _, _ = norm64(x.double(), G, None, beta.double(), act)
+    assert torch.equal(y.isnan(), y6.isnan())
+    ok = ~y6.isnan()
+    assert ((y.double() - y6)[ok].abs() <= (U[dt] + 2.0 ** -18) * 2 * y6[ok].abs() + 2e-5).all()
+    beta[12] = 0.0
+    dy = torch.randn(N, S, C, device=DEV).to(dt)
+    dx, dg, db = run_backward(dy, x, mean, rstd, G, None, beta, act)
+    assert dx.isfinite().all()
+    far = [6, 7, 8, 9, 10, 20]    # slopes below 1e-24: nothing reaches the parameters' gradients
+    assert (dg[far].abs() <= 1e-15).all() and (db[far].abs() <= 1e-15).all()
