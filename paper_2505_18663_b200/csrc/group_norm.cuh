@@ -448,33 +448,30 @@ __device__ __forceinline__ void gn_params(const GnArgs& A, int c0, float (&ga)[V
     }
 }
 
-// z = (x - mean) a + beta with a = gamma rstd.  For 16-bit x the mean goes into the constant (x a + (beta -
-// mean a): the constant's rounding, 2^-24 |mean| a, is far below x's own step); fp32 x subtracts first.
-template <typename T, int V>
+// z = (x - mean) a + beta with a = gamma rstd.  The mean is taken off first: inside the constant (x a + (beta - mean a)) its
+// rounding, 2^-24 |mean| a, is all that is left of a group whose values are equal, or nearly all.
+template <int V>
 struct GnScale {
     Pairs<V> mean, a, b;
     __device__ __forceinline__ GnScale(const float (&mu)[V], const float (&sc)[V], const float (&sh)[V]) {
-        float t[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) t[i] = sizeof(T) == 2 ? fmaf(-mu[i], sc[i], sh[i]) : sh[i];
         mean.set(mu);
         a.set(sc);
-        b.set(t);
+        b.set(sh);
     }
     __device__ __forceinline__ uint64_t operator()(uint64_t x, int i) const {
-        return f2_fma(sizeof(T) == 2 ? x : f2_sub(x, mean.p[i]), a.p[i], b.p[i]);
+        return f2_fma(f2_sub(x, mean.p[i]), a.p[i], b.p[i]);
     }
 };
 
 // ... from the groups' (mean, rstd)
-template <typename T, int V>
-__device__ __forceinline__ GnScale<T, V> gn_scale(const GnArgs& A, int c0, const float2* stat, const float (&ga)[V], const float (&be)[V]) {
+template <int V>
+__device__ __forceinline__ GnScale<V> gn_scale(const GnArgs& A, int c0, const float2* stat, const float (&ga)[V], const float (&be)[V]) {
     float mu[V], sc[V];
     gn_by_channel<V>(A.per, c0, [&](int i, int g) { const float2 t = stat[g]; mu[i] = t.x; sc[i] = t.y; },
                      [&](int i) { mu[i] = mu[0]; sc[i] = sc[0]; });
 #pragma unroll
     for (int i = 0; i < V; ++i) sc[i] *= ga[i];
-    return GnScale<T, V>(mu, sc, be);
+    return GnScale<V>(mu, sc, be);
 }
 
 template <typename T, int V, int ACT>
@@ -487,7 +484,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
     if (!P.on) return;
     float ga[V], be[V];
     gn_params<V>(A, P.c0, ga, be);
-    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, A.stat + (int64_t)n * A.G, ga, be);
+    const GnScale<V> scale = gn_scale<V>(A, P.c0, A.stat + (int64_t)n * A.G, ga, be);
     // backwards: from the place pass 1 read last
     const int count = P.count(A.lanes);
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
@@ -507,9 +504,9 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_apply_kernel(const __grid_co
 // ------------------------------------------------------------------ backward
 
 // What the backward passes hold per channel: h = (x - mean) rstd, z = gamma h + beta.
-template <typename T, int V>
+template <int V>
 struct GnGrad {
-    GnScale<T, V> h;
+    GnScale<V> h;
     Pairs<V> gamma, beta;
     template <int ACT>
     __device__ __forceinline__ void dz(uint64_t x, uint64_t dy, int i, uint64_t& out_dz, uint64_t& out_h) const {
@@ -517,15 +514,15 @@ struct GnGrad {
         out_dz = ACT == DVDQ_ACT_NONE ? dy : f2_mul(dy, act_slope2<ACT, true>(f2_fma(gamma.p[i], out_h, beta.p[i])));
     }
 };
-template <typename T, int V>
-__device__ __forceinline__ GnGrad<T, V> gn_constants(const GnArgs& A, int n, int c0, float (&rs)[V], float (&ga)[V]) {
+template <int V>
+__device__ __forceinline__ GnGrad<V> gn_constants(const GnArgs& A, int n, int c0, float (&rs)[V], float (&ga)[V]) {
     float mu[V], be[V], none[V];
     gn_by_channel<V>(A.per, c0, [&](int i, int g) { mu[i] = A.mean[(int64_t)n * A.G + g]; rs[i] = A.rstd[(int64_t)n * A.G + g]; },
                      [&](int i) { mu[i] = mu[0]; rs[i] = rs[0]; });
     gn_params<V>(A, c0, ga, be);
 #pragma unroll
     for (int i = 0; i < V; ++i) none[i] = 0.f;
-    GnGrad<T, V> r{GnScale<T, V>(mu, rs, none), {}, {}};
+    GnGrad<V> r{GnScale<V>(mu, rs, none), {}, {}};
     r.gamma.set(ga);
     r.beta.set(be);
     return r;
@@ -543,7 +540,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_grad_stats_kernel(const __gr
     for (int i = 0; i < Pairs<V>::N; ++i) s1.p[i] = s2.p[i] = 0ull;
     if (P.on) {
         float rs[V], ga[V];
-        const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
+        const GnGrad<V> K = gn_constants<V>(A, n, P.c0, rs, ga);
         const int64_t s0 = P.s0 + P.r;
         walk<kGnGradDepth, 2, T, V>(raw, P.count(A.lanes), static_cast<const T*>(A.x) + (int64_t)n * A.xn + P.c0 + s0 * A.xs, A.lanes * A.xs,
                                        static_cast<const T*>(A.dy) + (int64_t)n * A.dn + P.c0 + s0 * A.ds, A.lanes * A.ds,
@@ -599,7 +596,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_grad_apply_kernel(const __gr
     release_successor();
     if (!P.on) return;
     float rs[V], ga[V];
-    const GnGrad<T, V> K = gn_constants<T, V>(A, n, P.c0, rs, ga);
+    const GnGrad<V> K = gn_constants<V>(A, n, P.c0, rs, ga);
     const GnDx<V> dx = gn_dx<V>(A, P.c0, A.stat + (int64_t)n * A.G, rs, ga);
     const int count = P.count(A.lanes);
     const int64_t last = P.s0 + P.r + (int64_t)(count - 1) * A.lanes;
@@ -777,7 +774,7 @@ __global__ void __launch_bounds__(kGnFusedThreads, 1) gn_fused_kernel(const __gr
         return t;
     });
     if (!P.on) return;
-    const GnScale<T, V> scale = gn_scale<T, V>(A, P.c0, sums, ga, be);
+    const GnScale<V> scale = gn_scale<V>(A, P.c0, sums, ga, be);
     T* q = static_cast<T*>(A.y) + (int64_t)P.n * A.yn + P.c0 + (P.s0 + (int64_t)(P.count - 1) * P.lanes) * A.ys;
     const int64_t back = -(int64_t)P.lanes * A.ys;
     walk.backward([&](const Vec<T, V>& in) {
@@ -799,7 +796,7 @@ __global__ void __launch_bounds__(kGnFusedGradThreads, 1) gn_fused_grad_kernel(c
     TwoWay<D, 2, THREADS, T, V> walk(raw, P.count, static_cast<const T*>(A.x) + (int64_t)P.n * A.xn + P.c0 + P.s0 * A.xs, P.lanes * A.xs,
                                      static_cast<const T*>(A.dy) + (int64_t)P.n * A.dn + P.c0 + P.s0 * A.ds, P.lanes * A.ds);
     float rs[V], ga[V];
-    const GnGrad<T, V> K = gn_constants<T, V>(A, P.n, P.c0, rs, ga);
+    const GnGrad<V> K = gn_constants<V>(A, P.n, P.c0, rs, ga);
     {
         Pairs<V> s1, s2;
 #pragma unroll
@@ -966,7 +963,7 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     gn_params<V>(A, c0, ga, be);
 #pragma unroll
     for (int i = 0; i < V; ++i) ga[i] *= rs[i];
-    const GnScale<T, V> scale(mean, ga, be);
+    const GnScale<V> scale(mean, ga, be);
     T* q = static_cast<T*>(A.y) + (int64_t)n * A.yn + c0;
     for (int s = r; s < S; s += A.lanes) {
         const Pairs<V> x = widen2<T, V>(data[s * A.vecs + v]);
@@ -999,7 +996,7 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_grad_kernel(const __grid_
     gn_small_bring<T, V>(on, r, A.lanes, S, p, A.xs, xd + v, A.vecs);
     gn_small_bring<T, V>(on, r, A.lanes, S, d, A.ds, dd + v, A.vecs);
     float rs[V], ga[V];
-    const GnGrad<T, V> K = gn_constants<T, V>(A, n, on ? c0 : cbase, rs, ga);
+    const GnGrad<V> K = gn_constants<V>(A, n, on ? c0 : cbase, rs, ga);
     gn_small_brought<T, V>();
     Pairs<V> s1, s2;
 #pragma unroll

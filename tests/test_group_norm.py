@@ -412,3 +412,19 @@ def test_activations_of_the_lowest_values(dt, path, act):
     assert dx.isfinite().all()
     far = [6, 7, 8, 9, 10, 20]    # slopes below 1e-24: nothing reaches the parameters' gradients
     assert (dg[far].abs() <= 1e-15).all() and (db[far].abs() <= 1e-15).all()
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("C,G", [(32, 4), (35, 5)])
+def test_a_constant_group_far_from_zero_gives_beta(dt, path, C, G):
+    """x - mean is 0, whatever 1000 / sqrt(eps) rounds to: y is beta itself, and h is 0 in the gradients."""
+    N, S = PATHS[path]
+    x = torch.full((N, S, C), 1000.0, device=DEV).to(dt)
+    beta = (torch.arange(C, device=DEV) / 8.0).to(dt)
+    y, mean, rstd = run_forward(x, G, None, beta, 0, eps=EPS)
+    assert torch.equal(y, beta.expand_as(x))
+    dy = torch.ones_like(x)
+    _, dg, db = run_backward(dy, x, mean, rstd, G, None, beta, 0)
+    assert (dg == 0).all() and (db == N * S).all()
