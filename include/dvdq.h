@@ -349,7 +349,8 @@ dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, in
  * gradient is dy itself).  dY, Z, X, W, dX, dW as above in one dtype; dbias fp32 [N].  dX, dW and dbias may each be
  * NULL: not computed.  Z is not read for DVDQ_ACT_NONE; X only for dW, W only for dX.  dz is rounded to dtype for
  * the tensor cores; dbias sums it unrounded.  M == 0 writes zeros to dW and dbias.
- * The outputs are written, not added to, and overlap no input.  Workspace: 256-byte aligned. */
+ * The outputs are written, not added to, and overlap no input.  Workspace: 256-byte aligned; the layer's size is enough
+ * for any choice of outputs (with dX and dW both NULL no K is read: any valid value will do). */
 size_t dvdq_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t act);
 dvdq_status dvdq_linear_backward(const void* dY, int64_t lddy, const void* Z, int64_t ldz, const void* X, int64_t ldx,
                                  const void* W, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t act,

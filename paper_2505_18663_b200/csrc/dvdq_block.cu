@@ -49,6 +49,14 @@ struct LinBackwardPlan {
     int64_t chunks, rows;
     bool two;  // dX and dW in one launch
     int low;   // M where dz comes in two parts: rows M .. 2 M hold what rounding left over; or 0
+    // What a call needs of it: pieces only of the products it asks for.  (K matters to those alone: a call for the
+    // bias's gradient need not know it.)
+    int64_t room(bool with_dx, bool with_dw, bool few) const {
+        int64_t part = 0;
+        if (with_dx && !(two && with_dw)) part = dx.part_bytes;
+        if (with_dw && !few && !(two && with_dx) && part < dw.part_bytes) part = dw.part_bytes;
+        return part_off + part;
+    }
 };
 static LinBackwardPlan linear_backward_plan(int64_t M, int64_t N, int64_t K, int32_t act) {
     LinBackwardPlan p;
@@ -172,7 +180,7 @@ dvdq_status dvdq_linear_backward(const void* dY, int64_t lddy, const void* Z, in
     if (!workspace) return DVDQ_ERR_NULL;
     if (!aligned_to(workspace, 256)) return DVDQ_ERR_ALIGN;
     const LinBackwardPlan plan = linear_backward_plan(M, N, K, act);
-    if (workspace_bytes < (size_t)plan.total) return DVDQ_ERR_WORKSPACE;
+    if (workspace_bytes < (size_t)plan.room(dX != nullptr, dW != nullptr, few_weight_gradient(M))) return DVDQ_ERR_WORKSPACE;
     if ((s = check_device_arch()) != DVDQ_OK) return s;
     const LinMatrix dy{dY, lddy}, z{act == DVDQ_ACT_NONE ? nullptr : Z, ldz}, x{X, ldx}, w{W, ldw}, dx{dX, lddx}, dw{dW, lddw};
     uint8_t* ws = static_cast<uint8_t*>(workspace);

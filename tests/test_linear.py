@@ -316,3 +316,30 @@ def test_an_infinite_gradient_stays_in_its_token_and_channel(dt, M, N, K):
     assert torch.equal(dx[2].float(), torch.sign(w[3].float()) * math.inf) and torch.equal(dw[3].float(), torch.sign(x[2].float()) * math.inf)
     assert dx[[i for i in range(M) if i != 2]].isfinite().all() and dw[[i for i in range(N) if i != 3]].isfinite().all()
     assert db[3] == math.inf and db[[i for i in range(N) if i != 3]].isfinite().all()
+
+
+# layers whose own workspace is smaller than the one of the same tokens and channels with a K of 8
+LAYERS = [(1021, 1541, 1030, 0), (4096, 4096, 4096, 0), (4096, 4096, 4096, 1), (8192, 5120, 5120, 0), (100, 300, 5000, 2)]
+
+
+@pytest.mark.parametrize("M,N,K,act", LAYERS)
+def test_a_bias_gradient_alone_needs_no_more_than_the_layer(M, N, K, act):
+    """Sized for the layer, with a K of 8 in the call: refused here for want of a GPU, not for want of room."""
+    n = B.dvdq_linear_backward_workspace_bytes(M, N, K, act)
+    need = dict(M=M, N=N, K=8, lddy=-(-N // 8) * 8, ldz=-(-N // 8) * 8, act=act, X=None, W=None, dX=None, dW=None, n=n)
+    if not torch.cuda.is_available():  # (these addresses are for no GPU)
+        assert backward(**need) not in (B.OK, B.ERR_WORKSPACE)
+    assert backward(**dict(need, n=M)) == B.ERR_WORKSPACE
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K,act", LAYERS)
+def test_a_bias_gradient_alone(M, N, K, act):
+    g = gen(M)
+    dt = torch.bfloat16
+    dy, z = rows(M, N, dt, g), rows(M, N, dt, g) if act else None
+    db = torch.empty(N, device=DEV)
+    B.dvdq_linear_backward(dy, z, None, None, act, None, None, db, workspace(B.dvdq_linear_backward_workspace_bytes(M, N, K, act)))
+    dz = dy.double() * (slope64(z.double(), act) if act else 1.0)
+    rough = 2.0 ** -18 * dy.double().abs() * (1 + z.double().abs()) * 1.2 if act else torch.zeros_like(dz)
+    check(db, dz.sum(0), rough.sum(0) + (M + 8) * 2.0 ** -24 * dz.abs().sum(0), "db")
