@@ -455,7 +455,8 @@ dvdq_status dvdq_debug_wait_timeout(uint64_t limit_ns, void* cuda_stream);
 /* Reads (and clears) the device-side status word of the current device; synchronizes
  * the device.  DVDQ_OK, or DVDQ_ERR_DEVICE_TIMEOUT with `detail` (host, may be NULL)
  * set to a code identifying the wait that gave up, or DVDQ_ERR_SHAPE with detail 16 (dvdq_rope met a row
- * outside its table). */
+ * outside its table).  One failure a call: the quantized layers' and that of the operators around them are kept
+ * apart, and where both have one the next call gives the other. */
 dvdq_status dvdq_last_device_status(uint32_t* detail /* host */);
 
 /* Library version, for the Python binding's sanity check. */

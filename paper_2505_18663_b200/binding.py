@@ -642,7 +642,8 @@ def dvdq_gbs_observe(g: GbsState, l1_change: float, l1_prev: float) -> None:
 
 
 def dvdq_last_device_status():
-    """(status, detail) of the device-side status word; synchronizes the device and clears it."""
+    """(status, detail) of a device-side failure, (OK, 0) where there is none; synchronizes the device and clears what it
+    reports.  One failure a call: the quantized layers' and that of the operators around them are kept apart."""
     d = C.c_uint32(0)
     s = load().dvdq_last_device_status(C.byref(d))
     return int(s), int(d.value)

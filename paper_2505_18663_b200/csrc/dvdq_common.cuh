@@ -64,7 +64,7 @@ __host__ __device__ inline int hi_field_shift(int a, int i) { return 2 * (4 * (i
 // ------------------------------------------------------------------ device status word
 
 // [0] = status (0 ok, else dvdq_status), [1] = detail of the first failure.  One copy per translation
-// unit; dvdq_last_device_status reads them all.
+// unit; dvdq_last_device_status reads them in turn, up to the first that holds a failure.
 static __device__ uint32_t g_device_status[2] = {0u, 0u};
 
 enum WaitId : uint32_t {

@@ -539,12 +539,12 @@ dvdq_status dvdq_debug_wait_timeout(uint64_t limit_ns, void* stream) {
 }
 
 dvdq_status dvdq_last_device_status(uint32_t* detail) {
-    uint32_t h[2], other[2];
+    uint32_t h[2];
     if (cudaDeviceSynchronize() != cudaSuccess) return DVDQ_ERR_CUDA;
-    if (read_status_word(g_device_status, h) != DVDQ_OK || read_block_status(other) != DVDQ_OK) return DVDQ_ERR_CUDA;
-    const uint32_t* first = h[0] != 0u ? h : other;
-    if (detail) *detail = first[1];
-    return (dvdq_status)first[0];
+    if (read_status_word(g_device_status, h) != DVDQ_OK) return DVDQ_ERR_CUDA;
+    if (h[0] == 0u && read_block_status(h) != DVDQ_OK) return DVDQ_ERR_CUDA;  // else the other word stays for the next call
+    if (detail) *detail = h[1];
+    return (dvdq_status)h[0];
 }
 
 }  // extern "C"

@@ -113,3 +113,15 @@ def test_two_host_threads_share_the_library():
     # both layouts give the same output; every thread got it
     for i in range(1, 4):
         assert torch.equal(results[0], results[i])
+
+
+def test_two_failures_are_both_reported():
+    """One of the quantized layers' side (a wait that runs out), one of the operators' around them (a row outside the table of
+    rotary positions): each read clears what it reports and no more."""
+    assert B.dvdq_last_device_status() == (B.OK, 0)
+    q, table = torch.randn(1, 3, 2, 8, device=DEV), torch.zeros(4, 4, 2, device=DEV)
+    rows = torch.tensor([0, 9, 1], dtype=torch.int32, device=DEV)
+    B.dvdq_rope(q, None, table, rows, B.ROPE_PAIRS, False, torch.empty_like(q))
+    B.dvdq_debug_wait_timeout(3_000_000)
+    seen = [B.dvdq_last_device_status() for _ in range(3)]
+    assert sorted(seen[:2]) == sorted([(B.ERR_DEVICE_TIMEOUT, 8), (B.ERR_SHAPE, 16)]) and seen[2] == (B.OK, 0)
