@@ -88,16 +88,18 @@ __device__ __forceinline__ float act_value(float z) {
     const float u = ACT == DVDQ_ACT_SILU ? z : z * fmaf(kGeluB, z * z, kGeluA);
     return z * logistic(u);
 }
-// d/dz of it: f + z u'(z) f (1 - f).  Past |z| = 20 the second term is below the smallest float
-// (u > 30, and z u' f (1 - f) < 1e-9 for SiLU, 0 for GELU), so z is held there: no overflow of z^3.
+// d/dz of it: f + z u'(z) f (1 - f).  GELU's z is held at 20, where u is 600 and f 0 or 1: no overflow of z^3.  SiLU's is not: its
+// u is z, the slope still 4e-8 at -20, and f (1 + z (1 - f)) has no power of z to overflow.
 template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
     if (ACT == DVDQ_ACT_NONE) return 1.0f;
+    if (ACT == DVDQ_ACT_SILU) {
+        const float f = logistic(z);
+        return fmaf(f, fmaf(-z, f, z), f);
+    }
     const float c = z != z ? z : fminf(fmaxf(z, -20.0f), 20.0f);
-    const float u = ACT == DVDQ_ACT_SILU ? c : c * fmaf(kGeluB, c * c, kGeluA);
-    const float du = ACT == DVDQ_ACT_SILU ? 1.0f : fmaf(3.0f * kGeluB, c * c, kGeluA);
-    const float f = logistic(u);
-    return fmaf(c * du * f, 1.0f - f, f);
+    const float f = logistic(c * fmaf(kGeluB, c * c, kGeluA));
+    return fmaf(c * fmaf(3.0f * kGeluB, c * c, kGeluA) * f, 1.0f - f, f);
 }
 __device__ __forceinline__ float act_value_rt(int act, float z) {
     return act == DVDQ_ACT_GELU_TANH ? act_value<DVDQ_ACT_GELU_TANH>(z) : act == DVDQ_ACT_SILU ? act_value<DVDQ_ACT_SILU>(z) : z;
@@ -186,7 +188,7 @@ __device__ __forceinline__ uint64_t act_value2(uint64_t z) {
                                             : f2_mul(z, f2_fma(f2_splat(kGeluB * kMinusLog2e), f2_mul(z, z), f2_splat(kGeluA * kMinusLog2e)));
     return f2_mul(z, logistic2_scaled<SHARED>(e));
 }
-// act_slope of a pair.  SiLU needs no bound on z: f (1 + z (1 - f)) has no power of z to overflow.
+// act_slope of a pair.
 template <int ACT, bool SHARED = false>
 __device__ __forceinline__ uint64_t act_slope2(uint64_t z) {
     if (ACT == DVDQ_ACT_SILU) {

@@ -343,3 +343,28 @@ def test_a_bias_gradient_alone(M, N, K, act):
     dz = dy.double() * (slope64(z.double(), act) if act else 1.0)
     rough = 2.0 ** -18 * dy.double().abs() * (1 + z.double().abs()) * 1.2 if act else torch.zeros_like(dz)
     check(db, dz.sum(0), rough.sum(0) + (M + 8) * 2.0 ** -24 * dz.abs().sum(0), "db")
+
+
+@gpu
+@pytest.mark.parametrize("M", [1, 4, 5, 20])
+@pytest.mark.parametrize("act", [1, 2])
+def test_slopes_far_below_zero(M, act):
+    """Where the slope of the activation is small but a large dy still makes something of it (in bf16; fp16 has no such range).
+    The slope is right to |z| 2^-22 of itself, what two parts of dz leave to 2^-15, the output to 2^-8: 2^-7 of sum |dz||x| holds
+    them all."""
+    dt, N, K = torch.bfloat16, 72, 40
+    g = gen(M)
+    x, w, dy, z = rows(M, K, dt, g), rows(N, K, dt, g), rows(M, N, dt), rows(M, N, dt)
+    dy.fill_(2.0 ** 15)
+    far = 6.0 if act == 1 else 60.0
+    z.copy_(-torch.linspace(far / 6, far, N, device=DEV).expand(M, N))
+    dw, db = rows(N, K, dt), torch.empty(N, device=DEV)
+    B.dvdq_linear_backward(dy, z, x, w, act, None, dw, db, workspace(B.dvdq_linear_backward_workspace_bytes(M, N, K, act)))
+    z6 = z.double()
+    u, du = (z6, torch.ones_like(z6)) if act == 2 else (2 * math.sqrt(2 / math.pi) * (z6 + 0.044715 * z6 ** 3),
+                                                       2 * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * z6 ** 2))
+    f = torch.sigmoid(u)   # 1 + tanh would cancel here
+    dz = dy.double() * (f + z6 * du * f * (1 - f))
+    mag = dz.abs().T @ x.double().abs()
+    check(dw, dz.T @ x.double(), 2.0 ** -7 * mag, "dw")
+    check(db, dz.sum(0), 2.0 ** -14 * dz.abs().sum(0), "db")
