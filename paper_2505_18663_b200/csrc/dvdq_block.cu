@@ -48,7 +48,7 @@ struct LinBackwardPlan {
     int64_t lddz, dz_off, sums_off, part_off, total;
     int64_t chunks, rows;
     bool two;  // dX and dW in one launch
-    int low;   // M where dz comes in two parts: rows M .. 2 M hold what rounding left over; or 0
+    int low;   // M where dz comes in two parts: rows M .. 2 M hold the second; or 0
     // What a call needs of it: pieces only of the products it asks for.  (K matters to those alone: a call for the
     // bias's gradient need not know it.)
     int64_t room(bool with_dx, bool with_dw, bool few) const {

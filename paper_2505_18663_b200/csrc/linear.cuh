@@ -558,12 +558,30 @@ linear_join_kernel(const float* __restrict__ part, int64_t piece_floats, int pit
 
 // dz = dy act'(z) in fp32, rounded once to the operands' type for the tensor cores (an fp32 dz would cost
 // the two products half of their rate or more); the bias's gradient sums the unrounded values.
-// low > 0 (so few values that their roundings would not average out): what the rounding left over, itself rounded, goes
-// to row m + low, and dX and dW are formed from both, in one accumulator (where dW's last k-block reaches past row M it meets rows
-// of the second part, but x has zeros there).  Beside an infinity nothing is left over.
+// low > 0 (so few values that their roundings would not average out): dz goes into two parts (split_in_two), the second to row
+// m + low, and dX and dW are formed from both, in one accumulator.  Where dW's last k-block reaches past row M it meets rows
+// of the second part, but x has zeros there and a second part is finite.
 // A CTA takes 256 columns (8 per thread, 32 threads side by side, 8 rows at a time) of one chunk of
 // rows and writes their sums; linear_colsum_kernel adds the chunks.  Bound by its bytes: 32760 x 8960 with GELU 276 us, 6.4 TB/s.  act = none: dz is dy itself, only sums.
 constexpr int kLinDzCols = 256, kLinDzDepth = 5;
+
+__device__ __forceinline__ __nv_bfloat16 toward_zero(float d, __nv_bfloat16) { return __float2bfloat16_rz(d); }
+__device__ __forceinline__ __half toward_zero(float d, __half) { return __float2half_rz(d); }
+// d = first + second up to the rounding of `second`.  Both have d's sign and neither is zero (unless d is zero, or the type's smallest
+// number or less), so that beside an infinity in the other operand the two products are the same infinity, not NaN: `first` is d
+// toward zero, and one step further where that is d itself.  An infinite d: the second part is 1 of its sign.
+template <typename T>
+__device__ __forceinline__ void split_in_two(float d, T& first, T& second) {
+    first = toward_zero(d, T());
+    second = from_f32<T>(isfinite(d) ? d - to_f32(first) : d != d ? 0.0f : copysignf(1.0f, d));
+    uint16_t bits;
+    memcpy(&bits, &first, 2);
+    if (to_f32(second) == 0.0f && (bits & 0x7FFF) > 1 && isfinite(d)) {
+        --bits;
+        memcpy(&first, &bits, 2);
+        second = from_f32<T>(d - to_f32(first));
+    }
+}
 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(kStreamThreads, 4)
@@ -593,18 +611,14 @@ linear_dz_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ z
                 s.p[i] = f2_add(s.p[i], d.p[i]);
             }
             if (kAct) {
-                const Vec<T, 8> high = narrow2<T, 8>(d);
-                *reinterpret_cast<Vec<T, 8>*>(out) = high;
                 if (low > 0) {
-                    const Pairs<8> h = widen2<T, 8>(high);
+                    Vec<T, 8> first, second;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float a, b, ha, hb;
-                        f2_unpack(d.p[i], a, b);
-                        f2_unpack(h.p[i], ha, hb);
-                        d.p[i] = f2_pack(isfinite(ha) ? a - ha : 0.f, isfinite(hb) ? b - hb : 0.f);
-                    }
-                    *reinterpret_cast<Vec<T, 8>*>(out + low * lddz) = narrow2<T, 8>(d);
+                    for (int i = 0; i < 8; ++i) split_in_two(d.get(i), first.e[i], second.e[i]);
+                    *reinterpret_cast<Vec<T, 8>*>(out) = first;
+                    *reinterpret_cast<Vec<T, 8>*>(out + low * lddz) = second;
+                } else {
+                    *reinterpret_cast<Vec<T, 8>*>(out) = narrow2<T, 8>(d);
                 }
                 out += 8 * lddz;
             }

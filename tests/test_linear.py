@@ -368,3 +368,22 @@ def test_slopes_far_below_zero(M, act):
     mag = dz.abs().T @ x.double().abs()
     check(dw, dz.T @ x.double(), 2.0 ** -7 * mag, "dw")
     check(db, dz.sum(0), 2.0 ** -14 * dz.abs().sum(0), "db")
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 40, 72), (3, 40, 72), (5, 40, 72), (20, 130, 96), (63, 64, 300), (300, 13, 40)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_infinities_in_the_other_operand_of_the_gradients(dt, M, N, K, sign):
+    """w and x with an infinity each: what it is multiplied with decides its sign, whether dz comes whole or in two parts (one dz
+    here is a power of two, which is its own first part)."""
+    g = gen(N + 1)
+    dy, x, w, z = rows(M, N, dt, g), rows(M, K, dt, g), rows(N, K, dt, g), rows(M, N, dt, g)
+    dy[0, 3], z[0, 3] = 0.5, 0.0    # dz = 0.25
+    w[3, 5], x[M // 2, 7] = sign * math.inf, sign * math.inf
+    dx, dw = rows(M, K, dt), rows(N, K, dt)
+    B.dvdq_linear_backward(dy, z, x, w, B.ACT_SILU, dx, dw, None, workspace(B.dvdq_linear_backward_workspace_bytes(M, N, K, B.ACT_SILU)))
+    dz = dy.double() * slope64(z.double(), B.ACT_SILU)
+    assert torch.equal(dx[:, 5].double(), torch.sign(dz[:, 3]) * sign * math.inf)
+    assert torch.equal(dw[:, 7].double(), torch.sign(dz[M // 2]) * sign * math.inf)
+    assert dx[:, [c for c in range(K) if c != 5]].isfinite().all() and dw[:, [c for c in range(K) if c != 7]].isfinite().all()
