@@ -19,9 +19,10 @@
 namespace dvdq {
 
 constexpr int kFewTokens = 8;
-// The gradients are formed from dz in two parts where its values are so few that their roundings do not average out.  Both ways with
-// 1536 -> 1536: 32 tokens 10.4 and 8.5 us.
-inline bool dz_in_two_parts(int64_t M, int64_t N) { return M <= 32 || M * N < 4096; }
+// The gradients are formed from dz in two parts where a sum over tokens (dW) or over channels (dX) has so few terms that their roundings
+// do not average out, or dz is small altogether.  Both ways with 1536 -> 1536: 32 tokens 10.4 and 8.5 us; 32760 tokens, 1536 ->
+// 16, cold: 90 and 74.  (Rows of the second part begin at M, and a tile's coordinate is 32 bits.)
+inline bool dz_in_two_parts(int64_t M, int64_t N) { return M <= 32 || (N <= 32 && M < ((int64_t)1 << 30)) || M * N < 4096; }
 
 // 8 elements of a row from column k on; those past K are zero (and are not read: what follows a row's last element may be anything).
 template <typename T>

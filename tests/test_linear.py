@@ -387,3 +387,22 @@ def test_infinities_in_the_other_operand_of_the_gradients(dt, M, N, K, sign):
     assert torch.equal(dx[:, 5].double(), torch.sign(dz[:, 3]) * sign * math.inf)
     assert torch.equal(dw[:, 7].double(), torch.sign(dz[M // 2]) * sign * math.inf)
     assert dx[:, [c for c in range(K) if c != 5]].isfinite().all() and dw[:, [c for c in range(K) if c != 7]].isfinite().all()
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("M,N,K", [(1024, 4, 200), (5000, 16, 130), (2000, 1, 64), (700, 32, 300)])
+def test_gradients_of_few_channels_do_not_round_dz(dt, M, N, K):
+    """dX sums over channels: with up to 32 of them it has one rounding of the result too, however many tokens there are, and so has dW."""
+    g = gen(N)
+    dy, x, w, z = rows(M, N, dt, g), rows(M, K, dt, g), rows(N, K, dt, g), rows(M, N, dt, g, 2.0)
+    dx, dw = rows(M, K, dt), rows(N, K, dt)
+    B.dvdq_linear_backward(dy, z, x, w, B.ACT_SILU, dx, dw, None, workspace(B.dvdq_linear_backward_workspace_bytes(M, N, K, B.ACT_SILU)))
+    dz = dy.double() * slope64(z.double(), B.ACT_SILU)
+    fine = 2.0 ** -18 * dy.double().abs() * (1 + z.double().abs()) * 1.2 + U[dt] ** 2 * dz.abs() + TINY[dt]
+    outs = [(dx, dz @ w.double(), fine @ w.double().abs(), 2 * N, dz.abs() @ w.double().abs()),
+            (dw, dz.T @ x.double(), fine.T @ x.double().abs(), 2 * M, dz.abs().T @ x.double().abs())]
+    for got, want, spread, terms, mag in outs:
+        inner = spread + (terms + 8) * 2.0 ** -23 * mag
+        check(got, want, inner + U[dt] * (want.abs() + inner) + TINY[dt], "gradient")
+    status_ok()
