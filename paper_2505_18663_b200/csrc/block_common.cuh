@@ -49,24 +49,10 @@ struct alignas(sizeof(T) * V) Vec {
     T e[V];
 };
 template <typename T, int V>
-__device__ __forceinline__ void load_f32(const T* p, float (&f)[V]) {
-    const Vec<T, V> v = *reinterpret_cast<const Vec<T, V>*>(p);
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
-}
-template <typename T, int V>
 __device__ __forceinline__ void widen(const Vec<T, V>& v, float (&f)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
 }
-template <typename T, int V>
-__device__ __forceinline__ Vec<T, V> narrow(const float (&f)[V]) {
-    Vec<T, V> v;
-#pragma unroll
-    for (int i = 0; i < V; ++i) v.e[i] = from_f32<T>(f[i]);
-    return v;
-}
-
 // ------------------------------------------------------------------ activations
 
 // 1 / (1 + exp(-u)): one ex2.approx and one rcp.approx, about 1e-6 relative for |u| < 10.
