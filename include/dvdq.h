@@ -394,8 +394,8 @@ typedef struct {
 } dvdq_rope_tensor;
 /* Rotates q and (if not NULL) k.  Token (b, s) takes table row rows[b * rows_batch + s] (device, int32; rows_batch 0: the
  * same for all sequences), or row s if rows is NULL.  A row outside [0, table_rows) gives NaN in the rotated channels and DVDQ_ERR_SHAPE
- * in dvdq_last_device_status (detail 16).  inverse != 0 turns the other way: the gradient.  dtype: any.
- * B == 0 or S == 0 is a no-op. */
+ * in dvdq_last_device_status (detail 16); a table without rows is refused.  inverse != 0 turns the other way: the gradient.  dtype:
+ * any.  heads <= 65536, head_dim <= 4096, rot_dim <= 512.  B == 0 or S == 0 is a no-op. */
 dvdq_status dvdq_rope(const dvdq_rope_tensor* q /* host */, const dvdq_rope_tensor* k /* host */, int64_t B, int64_t S,
                       int32_t head_dim, int32_t rot_dim, const float* table, int64_t table_rows, const int32_t* rows,
                       int64_t rows_batch, int32_t layout, int32_t inverse, int32_t dtype, void* cuda_stream);

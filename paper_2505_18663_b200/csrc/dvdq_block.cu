@@ -277,6 +277,7 @@ dvdq_status dvdq_rope(const dvdq_rope_tensor* q, const dvdq_rope_tensor* k, int6
     if (B == 0 || S == 0) return DVDQ_OK;
     if (!table) return DVDQ_ERR_NULL;
     if (!rows && table_rows < S) return DVDQ_ERR_SHAPE;  // without rows, token s takes row s
+    if (table_rows == 0) return DVDQ_ERR_SHAPE;          // a row outside the table is read as row 0 before its NaN is written
     if (!aligned_to(table, 16) || (rows && !aligned_to(rows, 4))) return DVDQ_ERR_ALIGN;
     RopeSide side[2] = {};
     const int bytes = dtype_bytes(dtype);

@@ -215,6 +215,11 @@ def test_rope_refuses(q, kw, status):
     assert rope(q, **kw) == status
 
 
+def test_a_table_without_rows_is_refused():
+    """A token whose row lies outside the table loads row 0 (and gets NaN): there has to be one."""
+    assert rope({}, index=4096, rows=0) == B.ERR_SHAPE
+
+
 def test_rope_table_refuses():
     f = (C.c_double * 4)(1, 1, 1, 1)
     call = B.load().dvdq_rope_table
