@@ -144,24 +144,31 @@ struct GnMoments {
         }
     }
     // use(u, sums of x - pivot and its square over unit u) after the last flush(); a unit is 1 << log channels of one group.  Within it
-    // the sums are brought to its first channel's centre in fp32 (a value that lies far out there, and so moves that centre, has its
-    // own square among them), then to the group's pivot in fp64, in which they stay.
+    // the sums are brought to the mean of the channels' centres in fp32 (to one of them, a centre that lies far out would have its
+    // square counted for each of the others), then to the group's pivot in fp64, in which they stay.
     template <typename Use>
     __device__ __forceinline__ void by_unit(int log, const float (&pivot)[V], Use use) const {
         const int last = (1 << log) - 1;
-        const float count = (float)n;
-        float k0 = 0.f, a = 0.f, b = 0.f;
+        const float count = (float)n, part = __int_as_float((127 - log) << 23);  // 1 / (channels of a unit)
+        float c[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) c[i] = k.get(i) * part;
+#pragma unroll
+        for (int step = 1; step < V; step <<= 1) {
+            if (step > last) continue;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if ((i & step) == 0) c[i] = c[i + step] = c[i] + c[i + step];
+        }
+        float a = 0.f, b = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if ((i & last) == 0) {
-                k0 = k.get(i);
-                a = b = 0.f;
-            }
-            const float e = k.get(i) - k0, s = s1.get(i), moved = fmaf(count, e, s);
+            if ((i & last) == 0) a = b = 0.f;
+            const float e = k.get(i) - c[i], s = s1.get(i), moved = fmaf(count, e, s);
             a += moved;
             b += fmaf(e, s + moved, q.get(i));
             if ((i & last) == last) {
-                const double shift = (double)k0 - (double)pivot[i], all = (double)(n << log), to = a + all * shift;
+                const double shift = (double)c[i] - (double)pivot[i], all = (double)(n << log), to = a + all * shift;
                 use(i >> log, make_double2(to, b + shift * (a + to)));
             }
         }
@@ -951,13 +958,14 @@ __global__ void __launch_bounds__(kGnThreads) gn_small_kernel(const __grid_const
     {
         const int g0 = cbase / A.per;
         gn_by_channel<V>(A.per, c0, [&](int i, int g) {
-            const double m1 = totals[g - g0].x * A.inv;  // what the mean's rounding left
+            const double m1 = totals[g - g0].x * A.inv;  // what the first pass's fp32 sums, and the mean's rounding, left
             rs[i] = gn_mean_rstd(0.0, m1, totals[g - g0].y * A.inv, A.eps).y;
+            mean[i] = (float)((double)mean[i] + m1);
             if (r == 0 && c0 + i == g * A.per) {
                 if (A.mean) A.mean[(int64_t)n * A.G + g] = mean[i];
                 if (A.rstd) A.rstd[(int64_t)n * A.G + g] = rs[i];
             }
-        }, [&](int i) { rs[i] = rs[0]; });
+        }, [&](int i) { rs[i] = rs[0]; mean[i] = mean[0]; });
     }
     float ga[V], be[V];
     gn_params<V>(A, c0, ga, be);

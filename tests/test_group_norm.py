@@ -428,3 +428,18 @@ def test_a_constant_group_far_from_zero_gives_beta(dt, path, C, G):
     dy = torch.ones_like(x)
     _, dg, db = run_backward(dy, x, mean, rstd, G, None, beta, 0)
     assert (dg == 0).all() and (db == N * S).all()
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 30000, 1, 1), (1, 16000, 2, 1), (1, 100, 128, 16), (1, 700, 1024, 4), (80, 3000, 64, 4)])
+def test_an_outlier_in_few_pieces(dt, shape):
+    """-60000 at the first place, where a thread has a piece or two, or one channel's sums are long: no channel's square counts for its
+    neighbours too, and the mean is as good as the variance.  Bounds as above."""
+    N, S, C, G = shape
+    x = (0.3 + torch.randn(N, S, C, generator=torch.Generator(device=DEV).manual_seed(S), device=DEV)).to(dt)
+    x[:, 0, ::C // G] = -60000.0
+    _, mean, rstd = run_forward(x, G, None, None, 0)
+    _, m6, r6, _, _ = norm64(x.double(), G, None, None, 0)
+    assert ((rstd - r6) / r6).abs().max() <= 1e-6
+    assert (((mean - m6).abs() - 2.0 ** -24 * m6.abs()) * r6).max() <= 1e-6
