@@ -8,21 +8,20 @@
 // before its first output, so a tensor larger than the chip's shared memory is read twice; the
 // second pass walks every chunk backwards, so that it begins with what the L2 cache still holds.
 //
-// Large tensors, one cooperative launch of one CTA per SM: pass 1 sums a chunk of places of one sample over
+// Large tensors, in one of two ways.  One cooperative launch of one CTA per SM: pass 1 sums a chunk of places of one sample over
 // all channels (a thread keeps its 16 bytes of channels, so its loads are whole sectors) and writes two
 // numbers per group; all CTAs meet once; every CTA adds up its sample's numbers in a fixed order (no
 // atomics on data: the same bits every time); pass 2 walks the chunk backwards, first the pieces that pass 1
 // left in shared memory (about 20 MB over the chip), then what the L2 cache still holds.  A thread sums in fp32, about a centre that
 // follows its own mean (GnMoments), everything beyond in fp64: neither a mean far from zero nor a value far from the mean costs
 // digits.
-// Where that does not fit (channels that 16 bytes do not divide, more than 4096 of them, sample counts that
-// leave SMs idle): three launches, pass 1, join, pass 2, each started while its predecessor drains.
+// Where that does not fit (places not made of 4-byte pieces, more than 512 or 1024 pieces in one, sample counts that leave SMs idle) or
+// is the slower (kGnOneFrom): three launches, pass 1, join, pass 2, each started while its predecessor drains.
 // Small tensors, one launch: where a slice of whole groups of one sample fits a CTA's shared memory,
 // the CTA reads it once, and does both passes on it.
 //
-// Measured: 499200 places of 128 channels, bf16 with SiLU, 73 us (3.5 TB/s of x once and y once, 39 us at the copy rate); gradients
-// of 2 x 18720 places of 512 channels 41 us (115 MB, 2.8 TB/s); 3 x 77 places of 180 fp32 channels 6.3 us in a graph.
-// One launch and three: 2 MB (small kernel aside) 15.7 and 11.9 us, 8 MB 18.5 and 20.1, 61 MB 40 and 41, gradients 57 and 59.
+// Measured: 499200 places of 128 channels, bf16 with SiLU, 77 us (3.3 TB/s of x once and y once, 39 us at the copy rate); gradients
+// of 2 x 18720 places of 512 channels 43 us (115 MB, 2.7 TB/s); 3 x 77 places of 180 fp32 channels 6.3 us in a graph.
 #pragma once
 
 #include <type_traits>
@@ -1160,7 +1159,7 @@ inline bool gn_cut(GnArgs& A, int V) {
 // The one-launch kernels: the fewest whole groups that fill 64 bytes of a place (or all channels, if
 // those are fewer), so that a warp's loads are whole sectors; used where their places fit kGnSmallSmem, which
 // leaves room for three CTAs per SM.  A tensor of more than kGnSmallBytes is left to the kernels above, whose loads are whole rows:
-// samples of 1000 places of 512 channels, small kernel and those: 8 MB 14.6 and 18.4 us, 16 MB 15.2 and 20.6, but 16 MB in 64 samples 25 and 21.
+// samples of 1000 places of 512 channels, small kernel and those: 8 MB 13.4 and 15.8 us, 16 MB 19.0 and 22.2, but 16 MB in 64 samples 26.6 and 22.1.
 constexpr int64_t kGnSmallSmem = 64 << 10, kGnSmallBytes = 8 << 20;
 template <typename T, int V>
 static bool gn_small_cut(GnArgs& A, bool backward, size_t* smem) {
@@ -1189,8 +1188,8 @@ static bool gn_small_ready(PerDevice<int>& cache, Kern kern) {
 }
 
 // One CTA per SM, shared evenly among the samples; taken where that keeps at least two SMs in three busy.  Samples of 2000 places
-// of 512 channels, this and three launches: 100 samples (100 SMs) 121 and 121 us forward, 189 and 223 backward; 80 samples 109 and
-// 103, 187 and 175.
+// of 512 channels, this and three launches: 100 samples (100 SMs) 126 and 121 us forward, 206 and 230 backward; 80 samples 127 and
+// 108, 205 and 179.
 // Returns whether the call was made; *e says how it went.
 template <typename Kern>
 static bool launch_gn_fused(PerDevice<int>& cache, Kern kern, GnArgs A, int V, int threads, size_t smem, int64_t most_channels, cudaStream_t st,
@@ -1281,15 +1280,22 @@ static bool launch_gn_three(GnArgs A, bool backward, cudaStream_t st, cudaError_
     return true;
 }
 
+// Forward, 16-byte pieces: bytes of x for which one launch is the faster.  One and three launches, us: 8 MB 20.6 and 16.3, 32 MB 32.8 and
+// 30.6, 61 MB 44.4 and 44.2, 98 MB 60.9 and 62.8, 128 MB 77.1 and 78.2, 205 MB in 100 samples 125.6 and 121.1, 256 MB 145.5 and 143.5.
+// Backward the two lie within 13 % of each other either way (8 MB 24.2 and 21.1, 61 MB 61.9 and 63.5, 128 MB 120 and 112): one launch always.
+constexpr int64_t kGnOneFrom = 64 << 20, kGnOneTo = 192 << 20;
+
 // `wide`: channels per access that the channel count, pitches and pointers allow.
 template <typename T, int ACT>
 static cudaError_t launch_gn_act(const GnArgs& A, int wide, bool backward, cudaStream_t st) {
     constexpr int FULL = 16 / (int)sizeof(T);
     cudaError_t e = cudaErrorInvalidValue;
     if (wide == FULL) {
-        if (launch_gn_small<T, FULL, ACT>(A, backward, st, &e) || launch_gn_one<T, FULL, ACT>(A, backward, st, &e) ||
-            launch_gn_three<T, FULL, ACT>(A, backward, st, &e))
-            return e;
+        const int64_t bytes = (int64_t)A.N * A.S * A.C * (int64_t)sizeof(T);
+        const bool one = backward || (bytes >= kGnOneFrom && bytes < kGnOneTo);
+        if (launch_gn_small<T, FULL, ACT>(A, backward, st, &e) || (one && launch_gn_one<T, FULL, ACT>(A, backward, st, &e)) ||
+            launch_gn_three<T, FULL, ACT>(A, backward, st, &e) || (!one && launch_gn_one<T, FULL, ACT>(A, backward, st, &e)))
+            return e;  // (three launches do not cut wide groups of an odd number of channels)
     }
     if (launch_gn_small<T, 1, ACT>(A, backward, st, &e)) return e;
     if (wide == FULL / 2 && launch_gn_one<T, FULL / 2, ACT>(A, backward, st, &e)) return e;

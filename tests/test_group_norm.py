@@ -296,7 +296,7 @@ def test_small_squares_are_not_lost_in_long_sums(shape):
 
 # ------------------------------------------------------------------ values that are far out
 
-# one launch in shared memory; one launch over all SMs; three launches (80 samples leave SMs idle; single elements)
+# one launch in shared memory; gradients in one launch over all SMs (forward three: the tensor is small); three launches (80 samples leave SMs idle)
 PATHS = {"small": (2, 40), "one": (1, 20000), "three": (80, 3000)}
 
 
@@ -443,3 +443,31 @@ def test_an_outlier_in_few_pieces(dt, shape):
     _, m6, r6, _, _ = norm64(x.double(), G, None, None, 0)
     assert ((rstd - r6) / r6).abs().max() <= 1e-6
     assert (((mean - m6).abs() - 2.0 ** -24 * m6.abs()) * r6).max() <= 1e-6
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("C,G", [(128, 32), (56, 8), (64, 64)])
+@pytest.mark.parametrize("act", [1, 2])
+def test_large_tensors_in_one_launch(dt, C, G, act):
+    """70 MB of whole 16-byte pieces, groups of 4, 7 and 1 channels (an odd number goes through the sums in two rounds), each of the far
+    values in a group of its own: an outlier first, a masked channel, equal values, NaN.
+    h is off by the statistics' 1e-6 and its own roundings, 2^-22 (|h| + |mean| rstd); the activation by 2^-18 |z|."""
+    S, per = 70_000_000 // (C * torch.empty(0, dtype=dt).element_size()), C // G
+    g = torch.Generator(device=DEV).manual_seed(C)
+    x = (0.3 + torch.randn(1, S, C, generator=g, device=DEV)).to(dt)
+    gamma, beta = 1 + 0.3 * torch.randn(C, generator=g, device=DEV), 0.3 * torch.randn(C, generator=g, device=DEV)
+    x[:, 0, 0] = -10000.0
+    beta[per] = -1e20
+    x[..., 2 * per:3 * per] = 1000.0
+    x[:, S // 2, 4 * per - 1] = float("nan")
+    y, mean, rstd = run_forward(x, G, gamma, beta, act)
+    y6, m6, r6, h6, z6 = norm64(x.double(), G, gamma.double(), beta.double(), act)
+    assert y[..., 3 * per:4 * per].isnan().all() and mean[:, 3].isnan().all() and rstd[:, 3].isnan().all()
+    keep, groups = [c for c in range(C) if c // per != 3], [k for k in range(G) if k != 3]
+    assert ((rstd - r6) / r6)[:, groups].abs().max() <= 1e-6
+    assert (((mean - m6).abs() - 2.0 ** -24 * m6.abs()) * r6)[:, groups].max() <= 1e-6
+    h6, z6, y6, y = h6[..., keep].abs(), z6[..., keep].abs(), y6[..., keep], y[..., keep].double()
+    far = (m6.abs() * r6).repeat_interleave(per, 1)[0, keep] * (h6.amax((0, 1)) > 0)   # equal values leave no rounding
+    inner = 1.2 * gamma.double().abs()[keep] * ((1e-6 + 2.0 ** -22) * (1 + h6) + 2.0 ** -22 * far) + 2.0 ** -18 * z6 * (z6 < 1e10)
+    assert ((y - y6).abs() <= inner + U[dt] * (y6.abs() + inner) + 2.0 ** -24).all()
