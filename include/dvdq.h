@@ -335,6 +335,7 @@ typedef enum {
  *   X [M, K], W [N, K], Y [M, N]   dtype DVDQ_BF16 or DVDQ_F16, all the same; row pitches ldx, ldw, ldy
  *   bias [N] or NULL, R [M, N] or NULL (the residual, pitch ldr; R may be Y itself, same pitch), same type
  *   Z [M, N] or NULL               the pre-activation z = x W^T + bias, for the backward pass (pitch ldz)
+ * Apart from R = Y, the outputs overlap nothing that the call reads or writes.
  * fp32 accumulation on the tensor cores; bias, activation and residual in fp32, one rounding each for y and z.
  * Matrices start on 16 bytes and pitches are multiples of 8 elements (DVDQ_ERR_ALIGN); M, N and K
  * themselves are arbitrary (N, K <= 2^25), and what lies between a row's last element and the pitch is not used and not
@@ -348,7 +349,8 @@ dvdq_status dvdq_linear(const void* X, int64_t M, int64_t ldx, const void* W, in
 /* Its gradients:  dz = dy act'(z),  dX = dz W,  dW = dz^T X,  dbias = sum over tokens of dz  (the residual's
  * gradient is dy itself).  dY, Z, X, W, dX, dW as above in one dtype; dbias fp32 [N].  dX, dW and dbias may each be
  * NULL: not computed.  Z is not read for DVDQ_ACT_NONE; X only for dW, W only for dX.  dz is rounded to dtype for
- * the tensor cores; dbias sums it unrounded.  M == 0 writes zeros to dW and dbias.
+ * the tensor cores (in fp16 a dz beyond 65504 becomes an infinity); with up to 32 tokens, up to 32 channels N, or fewer than 4096 values
+ * dX and dW are formed from dz in two parts, or in fp32, instead.  dbias sums dz unrounded.  M == 0 writes zeros to dW and dbias.
  * The outputs are written, not added to, and overlap no input.  Workspace: 256-byte aligned; the layer's size is enough
  * for any choice of outputs (with dX and dW both NULL no K is read: any valid value will do). */
 size_t dvdq_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t act);
@@ -407,7 +409,9 @@ dvdq_status dvdq_rope(const dvdq_rope_tensor* q /* host */, const dvdq_rope_tens
  * rstd = 1 / sqrt(variance + eps);  y = act(gamma_c h + beta_c).
  *   gamma, beta [C] or NULL (1 and 0), of type param_dtype: X's, or DVDQ_F32
  *   mean_out, rstd_out [N, G] fp32 or NULL: what the backward pass reads
- * Y may be X itself (same pitches).  N <= 65535, S < 2^31, C <= 2^20.  S == 0: statistics (0, 1 / sqrt(eps)). */
+ * Y may be X itself (same pitches).  N <= 65535, S < 2^31, C <= 2^20, G times ceil(C / G / 256) <= 65535.  S == 0: statistics (0, 1 / sqrt(eps)).
+ * Sums are about the data's own mean and in fp64 beyond a thread: what is far from zero, or far from the rest, costs no digits.  What is not
+ * finite reaches its group (x) or channel (gamma, beta) only. */
 size_t dvdq_group_norm_workspace_bytes(int64_t N, int64_t S, int64_t C, int64_t G);
 dvdq_status dvdq_group_norm(const void* X, int64_t x_sample, int64_t x_place, int64_t N, int64_t S, int64_t C, int64_t G,
                             const void* gamma, const void* beta, int32_t param_dtype, float eps, int32_t act,

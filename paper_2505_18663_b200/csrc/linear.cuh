@@ -691,8 +691,9 @@ struct LinPlan {
 // loops around it take: 0.15 us + 0.6 ns per column with a deep ring, 0.135 us + 0.83 ns with a shallow one; all of it
 // at least the time of reading both operands at 6 TB/s; a tile's epilogue 0.5 + 2 us per 256 columns, hidden under the
 // next tile's products if there is one; 2 us to fill the ring.  Pieces cost a second launch (2.5 us) and writing and
-// reading their fp32 sums in L2 (about 8 TB/s).  `step`: 32, or 64 where B is MN-major (its shared-memory tiles
-// are 64 columns wide).
+// reading their fp32 sums in L2 (about 8 TB/s).  The estimate knows nothing of the row pitch or of L2's traffic; it compares plans
+// and does not predict: 509 x 5120 x 4096 is 18 us to it and 24-27 in fact, 34 with rows of 8208 bytes.
+// `step`: 32, or 64 where B is MN-major (its shared-memory tiles are 64 columns wide).
 // Rows of A that a CTA loads for its half of a tile: all 128, or (one tile, one CTA with rows) those that exist.
 inline int lin_a_rows(int64_t Md) { return Md < 128 ? (int)align_up(Md, 8) : 128; }
 
