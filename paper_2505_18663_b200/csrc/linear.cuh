@@ -15,10 +15,10 @@
 // per tensor-memory lane quarter, every other block of 32 (or 64) columns each: bias, activation, residual in fp32, ONE
 // rounding (fp32 outputs would double what is written), and TMA stores; the residual's blocks come by TMA, up to three ahead.
 //
-// What bounds it: the tensor pipe on layers of thousands of tokens (32760 x 5120 -> 13824 with GELU: 3.2-3.4 ms, 1.36-1.45
-// PFLOP/s under the power cap, the bare product of the vendor's library 3.3 ms; tensor pipe 98 % active in the gradients, 88 %
-// at 32760 x 1536 -> 1536, where it takes 105-139 us with the clock); with few tokens, streaming W; with a contraction of a few
-// k-blocks, the copies of outputs and residuals (32760 x 64 -> 1536: 27 us, with a residual 50 for 205 MB).
+// What bounds it: the tensor pipe on layers of thousands of tokens (32760 x 5120 -> 13824 with GELU: 3.1-3.5 ms, 1.32-1.5
+// PFLOP/s under the power cap; cold 3.3-3.8 ms, 2.9-4.3 the bare product of the vendor's library in the same run; tensor pipe
+// 98 % active in the gradients, 84 % at 32760 x 1536 -> 1536, where it takes 105-145 us with the clock); with few tokens, streaming
+// W; with a contraction of a few k-blocks, the copies of outputs and residuals (32760 x 64 -> 1536: 27 us, with a residual 50 for 205 MB).
 // Products with fewer tiles than CTA pairs are cut along k (`splits`): each piece writes its fp32 sums,
 // and a second kernel adds the pieces in a fixed order and does the epilogue (no atomics).
 #pragma once
