@@ -426,6 +426,60 @@ dvdq_status dvdq_group_norm_backward(const void* dY, int64_t dy_sample, int64_t 
                                      void* dX, int64_t dx_sample, int64_t dx_place, float* dgamma, float* dbeta,
                                      int32_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ---- RMS norm of rows, with the residual's addition and an output in 8 bits ------------------
+ *
+ * Rows of C values in an [N, S, C] tensor (pitches x_outer and x_row in elements, unit stride inside a row): the tokens of a
+ * batch, or N tokens' S heads inside a fused projection's output.
+ *   h = x + r (r: the residual R, or nothing),  rstd = 1 / sqrt(mean h^2 + eps),  y = h rstd gamma
+ *   s = max |y| / 127,  c = round_half_even(y / s): codes in [-127, 127] that stand for c s
+ *   gamma [C] or NULL (ones), of type param_dtype: X's, or DVDQ_F32
+ *   H, Y      of X's type, codes int8 (pitches like X's, in elements), scales and rstd_out fp32, dense [N, S]; each may be NULL, but
+ *             codes and scales come together, and something is asked for
+ * h, y and c are computed in fp32 and rounded once each: y and c come from the h that is not yet rounded.  Rows of values whose squares
+ * leave fp32's range are scaled by a power of two first.  A row of zeros has scale 0 and codes 0; a row whose y holds a value that
+ * is not finite has scale NaN and codes 0.
+ * H may be X or R itself, Y may be X or R itself (same pitches, not both the same one); apart from that outputs overlap nothing.
+ * N * S < 2^31, C <= 2^20, eps >= 0.  Any alignment of rows; 16 bytes (and codes on 8) are the fastest. */
+dvdq_status dvdq_rms_norm(const void* X, int64_t x_outer, int64_t x_row, const void* R, int64_t r_outer, int64_t r_row,
+                          int64_t N, int64_t S, int64_t C, const void* gamma, int32_t param_dtype, float eps,
+                          void* H, int64_t h_outer, int64_t h_row, void* Y, int64_t y_outer, int64_t y_row,
+                          int8_t* codes, int64_t c_outer, int64_t c_row, float* scales, float* rstd_out, int32_t dtype,
+                          void* cuda_stream);
+/* Its gradients, with H the h of the forward call (X itself where there was no residual) and hh = h rstd:
+ *   dX = rstd (gamma dy - hh <gamma dy hh>) + dH, <.> the mean over the row: the gradient of x and of r alike.  dH (or NULL): the gradient
+ *        that reaches h by another way, along the residual stream
+ *   dgamma = sum over rows of dy hh (fp32 [C]), in a fixed order
+ * dX and dgamma may each be NULL, not both.  dX may be dY, H or dH itself (same pitches).  The workspace (256-byte aligned) is needed for dgamma
+ * only.  N * S == 0: dgamma is zeros.  The codes' rounding has no gradient: through it, dy is taken as that of y. */
+size_t dvdq_rms_norm_backward_workspace_bytes(int64_t N, int64_t S, int64_t C);
+dvdq_status dvdq_rms_norm_backward(const void* dY, int64_t dy_outer, int64_t dy_row, const void* H, int64_t h_outer, int64_t h_row,
+                                   const float* rstd, const void* dH, int64_t dh_outer, int64_t dh_row, int64_t N, int64_t S,
+                                   int64_t C, const void* gamma, int32_t param_dtype, void* dX, int64_t dx_outer, int64_t dx_row,
+                                   float* dgamma, int32_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---- rows in 8 bits: the operands of dvdq_linear_int8 -----------------------------------------
+ *
+ * s_m = max |x_m| / 127, c = round_half_even(x / s) as above, in natural order: codes [M, K] int8, row pitch ldc (a multiple of
+ * 16 for dvdq_linear_int8), scales [M] fp32.  X [M, K] of any dtype, row pitch ldx: tokens, or a layer's weights (a scale for each
+ * output channel).  M < 2^31, K <= 2^20. */
+dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx, int8_t* codes, int64_t ldc, float* scales,
+                               int32_t dtype, void* cuda_stream);
+
+/* ---- linear layer in 8-bit integers: y = act(s_m t_n sum_k a_mk w_nk + bias_n) + residual ------
+ *
+ *   A [M, K] int8 codes with a_scales s [M], W [N, K] int8 codes with w_scales t [N] (fp32): of dvdq_rms_norm or
+ *   dvdq_quantize_rows, or any codes in [-128, 127]; row pitches lda, ldw
+ *   bias [N] or NULL, R [M, N] or NULL (the residual, pitch ldr; may be Y itself, same pitch), Y [M, N]: all DVDQ_BF16 or all DVDQ_F16
+ * The sums over k are exact (int32: K < 131072); scales, bias, activation and residual in fp32, one rounding.  A row's result does not
+ * depend on the rows beside it.  Matrices start on 16 bytes and pitches are multiples of 16 bytes (DVDQ_ERR_ALIGN); M, N and K themselves
+ * are arbitrary, and what lies between a row's last element and the pitch is not used and not written.  The pitch of a single row is
+ * not read.  M == 0 is a no-op.  Apart from R = Y, the output overlaps nothing that the call reads.  Workspace: 256-byte aligned, often 0. */
+size_t dvdq_linear_int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+dvdq_status dvdq_linear_int8(const int8_t* A, const float* a_scales, int64_t M, int64_t lda, const int8_t* W,
+                             const float* w_scales, int64_t N, int64_t K, int64_t ldw, const void* bias, const void* R,
+                             int64_t ldr, int32_t act, void* Y, int64_t ldy, int32_t dtype, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+
 /* ---- test / debug entry points (so that no caller depends on the packed layouts) ---- */
 
 /* The raw accumulators of dvdq_qgemm: acc_out [M, N] int32, row pitch ldacc elements. */
@@ -459,8 +513,8 @@ dvdq_status dvdq_debug_wait_timeout(uint64_t limit_ns, void* cuda_stream);
 /* Reads (and clears) the device-side status word of the current device; synchronizes
  * the device.  DVDQ_OK, or DVDQ_ERR_DEVICE_TIMEOUT with `detail` (host, may be NULL)
  * set to a code identifying the wait that gave up, or DVDQ_ERR_SHAPE with detail 16 (dvdq_rope met a row
- * outside its table).  One failure a call: the quantized layers' and that of the operators around them are kept
- * apart, and where both have one the next call gives the other. */
+ * outside its table).  One failure a call: the quantized layers', that of dvdq_linear_int8 and that of the
+ * other operators around them are kept apart, and where several have one the next call gives another. */
 dvdq_status dvdq_last_device_status(uint32_t* detail /* host */);
 
 /* Library version, for the Python binding's sanity check. */

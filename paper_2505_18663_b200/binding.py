@@ -30,6 +30,8 @@ EXPORTS = [
     "dvdq_linear_workspace_bytes", "dvdq_linear", "dvdq_linear_backward_workspace_bytes", "dvdq_linear_backward",
     "dvdq_rope_frequencies", "dvdq_rope_table", "dvdq_rope",
     "dvdq_group_norm_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_backward",
+    "dvdq_rms_norm", "dvdq_rms_norm_backward_workspace_bytes", "dvdq_rms_norm_backward", "dvdq_quantize_rows",
+    "dvdq_linear_int8_workspace_bytes", "dvdq_linear_int8",
 ]
 
 # element types, activations and rotary options of include/dvdq.h
@@ -137,6 +139,13 @@ def load():
         "dvdq_group_norm": (C.c_int, [p, i64, i64, i64, i64, i64, i64, p, p, i32, C.c_float, i32, p, i64, i64, p, p, i32, p, sz, p]),
         "dvdq_group_norm_backward": (C.c_int, [p, i64, i64, p, i64, i64, p, p, i64, i64, i64, i64, p, p, i32, i32, p, i64, i64, p, p,
                                                i32, p, sz, p]),
+        "dvdq_rms_norm": (C.c_int, [p, i64, i64, p, i64, i64, i64, i64, i64, p, i32, C.c_float, p, i64, i64, p, i64, i64, p, i64, i64, p, p,
+                                    i32, p]),
+        "dvdq_rms_norm_backward_workspace_bytes": (sz, [i64, i64, i64]),
+        "dvdq_rms_norm_backward": (C.c_int, [p, i64, i64, p, i64, i64, p, p, i64, i64, i64, i64, i64, p, i32, p, i64, i64, p, i32, p, sz, p]),
+        "dvdq_quantize_rows": (C.c_int, [p, i64, i64, i64, p, i64, p, i32, p]),
+        "dvdq_linear_int8_workspace_bytes": (sz, [i64, i64, i64]),
+        "dvdq_linear_int8": (C.c_int, [p, p, i64, i64, p, p, i64, i64, i64, p, p, i64, i32, p, i64, i32, p, sz, p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -523,6 +532,137 @@ def dvdq_group_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tens
                                            channels, G, ga, be, param_code, act, y, yn, ys, _vector(dgamma, torch.float32, channels, "dgamma"),
                                            _vector(dbeta, torch.float32, channels, "dbeta"), code, ws, room, _raw_stream(stream, X)),
            "dvdq_group_norm_backward")
+
+
+def _on_current_device(t: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """The calls run on the current device: tensors of another one are refused, not read from there."""
+    device = t.device
+    if device.type != "cuda":
+        raise TypeError("tensors must be CUDA tensors")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    for o in others:
+        if o is not None and o.device != device:
+            raise ValueError(f"tensors must all be on {device}, got one on {o.device}")
+
+
+def _rows3(t: Optional[torch.Tensor], dtype, shape, name: str):
+    """(address, outer pitch, row pitch) of rows in an [N, S, C] tensor, or (N = 1) in an [S, C] one."""
+    if t is None:
+        return None, 0, 0
+    if t.shape != shape:
+        raise TypeError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    st = t.stride()
+    if shape[-1] > 1 and st[-1] != 1:
+        raise TypeError(f"{name} must have unit stride inside a row")
+    return _address(t, dtype, name), st[0] if len(st) == 3 else 0, st[-2]
+
+
+def _row_values(t: Optional[torch.Tensor], shape, name: str):
+    """A dense fp32 value for each row."""
+    if t is not None and (t.shape != shape[:-1] or not t.is_contiguous()):
+        raise TypeError(f"{name} must be dense {tuple(shape[:-1])}")
+    return _address(t, torch.float32, name)
+
+
+def _rows_shape(t: torch.Tensor, name: str):
+    shape = t.shape
+    if len(shape) == 3:
+        return shape, shape[0], shape[1], shape[2]
+    if len(shape) == 2:
+        return shape, 1, shape[0], shape[1]
+    raise TypeError(f"{name} must be [S, C] or [N, S, C]")
+
+
+def _gamma(t: Optional[torch.Tensor], dt, code: int, channels: int):
+    if t is None:
+        return None, code
+    if t.dtype is not dt and t.dtype is not torch.float32:
+        raise TypeError(f"gamma must be {dt} or torch.float32, got {t.dtype}")
+    return _vector(t, t.dtype, channels, "gamma"), code if t.dtype is dt else F32
+
+
+def dvdq_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], gamma: Optional[torch.Tensor], eps: float,
+                  H: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
+                  scales: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None) -> None:
+    """h = X + residual and y = h / sqrt(mean h^2 + eps) * gamma, row by row, for X [S, C] or [N, S, C] (any strides of rows: heads inside a
+    fused projection's output).  Written where given: H (h), Y (y), codes int8 with scales fp32 (y in 8 bits, a scale for each row), rstd
+    fp32 for dvdq_rms_norm_backward.  H and Y may each be X or residual itself."""
+    dt = X.dtype
+    code = _element_type(X, "X", _ANY_FLOAT)
+    shape, N, S, channels = _rows_shape(X, "X")
+    _on_current_device(X, residual, gamma, H, Y, codes, scales, rstd)
+    x, xo, xr = _rows3(X, dt, shape, "X")
+    r, ro, rr = _rows3(residual, dt, shape, "residual")
+    h, ho, hr = _rows3(H, dt, shape, "H")
+    y, yo, yr = _rows3(Y, dt, shape, "Y")
+    c, co, cr = _rows3(codes, torch.int8, shape, "codes")
+    ga, param_code = _gamma(gamma, dt, code, channels)
+    _check(load().dvdq_rms_norm(x, xo, xr, r, ro, rr, N, S, channels, ga, param_code, eps, h, ho, hr, y, yo, yr, c, co, cr,
+                                _row_values(scales, shape, "scales"), _row_values(rstd, shape, "rstd"), code, _raw_stream(stream, X)),
+           "dvdq_rms_norm")
+
+
+def dvdq_rms_norm_backward_workspace_bytes(N: int, S: int, C_: int) -> int:
+    return int(load().dvdq_rms_norm_backward_workspace_bytes(N, S, C_))
+
+
+def dvdq_rms_norm_backward(dY: torch.Tensor, H: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor], dH: Optional[torch.Tensor],
+                           dX: Optional[torch.Tensor], dgamma: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None,
+                           stream=None) -> None:
+    """Gradients of dvdq_rms_norm: dX (of X and of the residual alike; dH, if given, is added: the gradient that reaches h along the residual stream)
+    and dgamma (fp32 [C]), each written if given.  H: the h of the forward call.  dX may be dY, H or dH itself.  The workspace is needed for dgamma."""
+    dt = H.dtype
+    code = _element_type(H, "H", _ANY_FLOAT)
+    shape, N, S, channels = _rows_shape(H, "H")
+    _on_current_device(H, dY, rstd, gamma, dH, dX, dgamma, workspace)
+    d, do, dr = _rows3(dY, dt, shape, "dY")
+    h, ho, hr = _rows3(H, dt, shape, "H")
+    e, eo, er = _rows3(dH, dt, shape, "dH")
+    x, xo, xr = _rows3(dX, dt, shape, "dX")
+    ga, param_code = _gamma(gamma, dt, code, channels)
+    ws, room = _room(workspace)
+    _check(load().dvdq_rms_norm_backward(d, do, dr, h, ho, hr, _row_values(rstd, shape, "rstd"), e, eo, er, N, S, channels, ga, param_code,
+                                         x, xo, xr, _vector(dgamma, torch.float32, channels, "dgamma"), code, ws, room,
+                                         _raw_stream(stream, H)), "dvdq_rms_norm_backward")
+
+
+def dvdq_quantize_rows(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """codes int8 [M, K] = round(X / scale) with scale = max |row| / 127 (scales fp32 [M]): operands of dvdq_linear_int8."""
+    code = _element_type(X, "X", _ANY_FLOAT)
+    if X.dim() != 2:
+        raise TypeError("X must be 2-D")
+    M, K = X.shape
+    _on_current_device(X, codes, scales)
+    x, ldx = _matrix(X, X.dtype, M, K, "X")
+    c, ldc = _matrix(codes, torch.int8, M, K, "codes")
+    _check(load().dvdq_quantize_rows(x, M, K, ldx, c, ldc, _row_values(scales, X.shape, "scales"), code, _raw_stream(stream, X)),
+           "dvdq_quantize_rows")
+
+
+def dvdq_linear_int8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(load().dvdq_linear_int8_workspace_bytes(M, N, K))
+
+
+def dvdq_linear_int8(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, bias: Optional[torch.Tensor],
+                     residual: Optional[torch.Tensor], act: int, Y: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Y = act(a_scales w_scales^T * (A W^T) + bias) + residual for int8 codes A [M, K] and W [N, K] with a scale for each row; Y, bias and residual
+    in bf16 or fp16.  residual may be Y itself.  Rows start on 16 bytes; workspace: dvdq_linear_int8_workspace_bytes(M, N, K) bytes, None
+    where that is 0."""
+    dt = Y.dtype
+    code = _element_type(Y, "Y", _HALF_FLOAT)
+    if A.dim() != 2 or W.dim() != 2:
+        raise TypeError("A and W must be 2-D")
+    (M, K), N = A.shape, W.shape[0]
+    _on_current_device(A, a_scales, W, w_scales, bias, residual, Y, workspace)
+    a, lda = _matrix(A, torch.int8, M, K, "A")
+    w, ldw = _matrix(W, torch.int8, N, K, "W")
+    r, ldr = _matrix(residual, dt, M, N, "residual")
+    y, ldy = _matrix(Y, dt, M, N, "Y")
+    ws, room = _room(workspace)
+    _check(load().dvdq_linear_int8(a, _vector(a_scales, torch.float32, M, "a_scales"), M, lda, w, _vector(w_scales, torch.float32, N, "w_scales"),
+                                   N, K, ldw, _vector(bias, dt, N, "bias"), r, ldr, act, y, ldy, code, ws, room, _raw_stream(stream, A)),
+           "dvdq_linear_int8")
 
 
 # ------------------------------------------------------------------ test / debug entry points

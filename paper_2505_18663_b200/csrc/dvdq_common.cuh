@@ -328,6 +328,16 @@ __device__ __forceinline__ void tc_mma_i8_ts_pair(uint32_t d_tmem, uint32_t a_tm
         ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// D[tmem] (+)= A[smem] * B[smem]^T for a CTA pair, int8 operands, int32 accumulators: each CTA
+// holds its 128 rows of A and half of B's rows at the same shared-memory offsets.
+__device__ __forceinline__ void tc_mma_i8_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // Arrives once on the mbarrier at this shared-memory offset in EVERY CTA of cta_mask when all
 // tcgen05.mma issued so far by this thread have finished (a signal, not a data copy).
 __device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint16_t cta_mask) {
@@ -436,6 +446,7 @@ inline dvdq_status read_status_word(const void* symbol, uint32_t (&h)[2]) {
     if (h[0] != 0u && cudaMemcpyToSymbol(symbol, zero, sizeof zero) != cudaSuccess) return DVDQ_ERR_CUDA;
     return DVDQ_OK;
 }
-dvdq_status read_block_status(uint32_t (&h)[2]);  // dvdq_block.cu
+dvdq_status read_block_status(uint32_t (&h)[2]);        // dvdq_block.cu
+dvdq_status read_linear_int8_status(uint32_t (&h)[2]);  // dvdq_linear_int8.cu
 
 }  // namespace dvdq

@@ -542,7 +542,9 @@ dvdq_status dvdq_last_device_status(uint32_t* detail) {
     uint32_t h[2];
     if (cudaDeviceSynchronize() != cudaSuccess) return DVDQ_ERR_CUDA;
     if (read_status_word(g_device_status, h) != DVDQ_OK) return DVDQ_ERR_CUDA;
-    if (h[0] == 0u && read_block_status(h) != DVDQ_OK) return DVDQ_ERR_CUDA;  // else the other word stays for the next call
+    // else the other words stay for the next calls
+    if (h[0] == 0u && read_block_status(h) != DVDQ_OK) return DVDQ_ERR_CUDA;
+    if (h[0] == 0u && read_linear_int8_status(h) != DVDQ_OK) return DVDQ_ERR_CUDA;
     if (detail) *detail = h[1];
     return (dvdq_status)h[0];
 }

@@ -95,17 +95,6 @@ struct SsSmem {
     static_assert(kTotal <= 232448, "more than the 227 KB of shared memory a CTA can have");
 };
 
-// D[tmem] (+)= A[smem] * B[smem]^T for a CTA pair, int8 operands, int32 accumulators: each CTA
-// holds its 128 rows of A and half of B's rows at the same shared-memory offsets.
-__device__ __forceinline__ void tc_mma_i8_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
 template <int ABITS>
 constexpr int ss_warps(int ew) { return ew == 8 ? kSsFirstEpilogueWarp2 + 4 : (ABITS != 8 ? kSsFirstAWarp + kSsAWarps : kSsFirstEpilogueWarp2); }
 
