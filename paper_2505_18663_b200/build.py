@@ -8,7 +8,8 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libdvdq.so")
-SOURCES = ["dvdq_lib.cu", "dvdq_block.cu", "dvdq_rows.cu", "dvdq_rows_backward.cu", "dvdq_linear_int8.cu"]
+SOURCES = ["dvdq_lib.cu", "dvdq_block.cu", "dvdq_rows.cu", "dvdq_rows_bf16.cu", "dvdq_rows_f16.cu", "dvdq_rows_f32.cu",
+           "dvdq_linear_int8.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

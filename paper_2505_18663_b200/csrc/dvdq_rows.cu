@@ -1,17 +1,22 @@
-// C ABI (see include/dvdq.h) of the operators on rows that feed the 8-bit linear layer: RMS norm with the residual's addition,
-// quantization of rows (rms_norm.cuh).  Argument validation, launches.
+// C ABI (see include/dvdq.h) of the operators on rows that feed the 8-bit linear layer: RMS norm with the residual's addition
+// (rms_norm.cuh), its gradients (rms_norm_backward.cuh), quantization of rows.  Argument validation, size queries, launches.
 #include <math.h>
 
 #include "rms_norm.cuh"
+#include "rms_norm_backward.cuh"
 
 namespace dvdq {
 
-template <bool NORM>
-static dvdq_status rms_run(const RmsArgs& A, int32_t dtype, int access, cudaStream_t st) {
-    return cuda_status(dtype == DVDQ_BF16  ? launch_rms_t<__nv_bfloat16, NORM>(A, access, st)
-                       : dtype == DVDQ_F16 ? launch_rms_t<__half, NORM>(A, access, st)
-                                           : launch_rms_t<float, NORM>(A, access, st));
-}
+// dvdq_rows_{bf16,f16,f32}.cu
+cudaError_t launch_rms_norm_bf16(const RmsArgs& A, int access, cudaStream_t st);
+cudaError_t launch_rms_norm_f16(const RmsArgs& A, int access, cudaStream_t st);
+cudaError_t launch_rms_norm_f32(const RmsArgs& A, int access, cudaStream_t st);
+cudaError_t launch_quantize_rows_bf16(const RmsArgs& A, int access, cudaStream_t st);
+cudaError_t launch_quantize_rows_f16(const RmsArgs& A, int access, cudaStream_t st);
+cudaError_t launch_quantize_rows_f32(const RmsArgs& A, int access, cudaStream_t st);
+cudaError_t launch_rms_norm_backward_bf16(const RmsBackwardArgs& A, int access, int64_t parts, int* ctas, cudaStream_t st);
+cudaError_t launch_rms_norm_backward_f16(const RmsBackwardArgs& A, int access, int64_t parts, int* ctas, cudaStream_t st);
+cudaError_t launch_rms_norm_backward_f32(const RmsBackwardArgs& A, int access, int64_t parts, int* ctas, cudaStream_t st);
 
 }  // namespace dvdq
 
@@ -50,7 +55,9 @@ dvdq_status dvdq_rms_norm(const void* X, int64_t x_outer, int64_t x_row, const v
     A.eps = eps;
     A.inv_c = 1.0f / (float)C;
     const RowsOf* all[] = {&A.x, &A.r, &A.h, &A.y};
-    return rms_run<true>(A, dtype, rows_access(all, 4, &A.codes, gamma, bytes, pb), (cudaStream_t)stream);
+    const int access = rows_access(all, 4, &A.codes, gamma, bytes, pb);
+    const cudaStream_t st = (cudaStream_t)stream;
+    return cuda_status(dtype == DVDQ_BF16 ? launch_rms_norm_bf16(A, access, st) : dtype == DVDQ_F16 ? launch_rms_norm_f16(A, access, st) : launch_rms_norm_f32(A, access, st));
 }
 
 dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx, int8_t* codes, int64_t ldc, float* scales, int32_t dtype,
@@ -70,7 +77,64 @@ dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx,
     A.shape = rows_shape(1, M, K);
     A.scales = scales;
     const RowsOf* all[] = {&A.x};
-    return rms_run<false>(A, dtype, rows_access(all, 1, &A.codes, nullptr, bytes, 0), (cudaStream_t)stream);
+    const int access = rows_access(all, 1, &A.codes, nullptr, bytes, 0);
+    const cudaStream_t st = (cudaStream_t)stream;
+    return cuda_status(dtype == DVDQ_BF16  ? launch_quantize_rows_bf16(A, access, st)
+                       : dtype == DVDQ_F16 ? launch_quantize_rows_f16(A, access, st)
+                                           : launch_quantize_rows_f32(A, access, st));
+}
+
+size_t dvdq_rms_norm_backward_workspace_bytes(int64_t N, int64_t S, int64_t C) {
+    if (!rows_sizes_ok(N, S, C) || N == 0 || S == 0) return 0;
+    return (size_t)align_up(rms_parts(N * S, C) * C * 4, 256);
+}
+
+dvdq_status dvdq_rms_norm_backward(const void* dY, int64_t dy_outer, int64_t dy_row, const void* H, int64_t h_outer, int64_t h_row,
+                                   const float* rstd, const void* dH, int64_t dh_outer, int64_t dh_row, int64_t N, int64_t S, int64_t C,
+                                   const void* gamma, int32_t param_dtype, void* dX, int64_t dx_outer, int64_t dx_row, float* dgamma,
+                                   int32_t dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!rows_sizes_ok(N, S, C)) return DVDQ_ERR_SHAPE;
+    if (!rows_dtype_ok(dtype) || (param_dtype != dtype && param_dtype != DVDQ_F32)) return DVDQ_ERR_UNSUPPORTED;
+    const int bytes = dtype_bytes(dtype), pb = dtype_bytes(param_dtype);
+    if ((gamma && !aligned_to(gamma, pb)) || (dgamma && !aligned_to(dgamma, 4)) || (rstd && !aligned_to(rstd, 4))) return DVDQ_ERR_ALIGN;
+    dvdq_status s;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (N == 0 || S == 0) {  // sums over nothing
+        if (!dgamma) return DVDQ_OK;
+        if ((s = check_device_arch()) != DVDQ_OK) return s;
+        return cuda_status(launch_after(rms_norm_no_rows_kernel, dim3((unsigned)ceil_div(C, 256)), dim3(256), 0, st, dgamma, (int)C));
+    }
+    if (!dY || !H || !rstd || (!dX && !dgamma)) return DVDQ_ERR_NULL;
+    RmsBackwardArgs A = {};
+    A.dy = RowsOf{const_cast<void*>(dY), dy_outer, dy_row};
+    A.h = RowsOf{const_cast<void*>(H), h_outer, h_row};
+    A.dh = RowsOf{const_cast<void*>(dH), dh_outer, dh_row};
+    A.dx = RowsOf{dX, dx_outer, dx_row};
+    if ((s = check_rows(&A.dy, N, S, C, bytes, false)) != DVDQ_OK || (s = check_rows(&A.h, N, S, C, bytes, false)) != DVDQ_OK ||
+        (s = check_rows(&A.dh, N, S, C, bytes, false)) != DVDQ_OK || (s = check_rows(&A.dx, N, S, C, bytes, true)) != DVDQ_OK)
+        return s;
+    if (!in_place_ok(A.dy, A.dx) || !in_place_ok(A.h, A.dx) || !in_place_ok(A.dh, A.dx)) return DVDQ_ERR_SHAPE;
+    const int64_t parts = rms_parts(N * S, C);
+    if (dgamma) {
+        if (!workspace) return DVDQ_ERR_NULL;
+        if (!aligned_to(workspace, 256)) return DVDQ_ERR_ALIGN;
+        if (workspace_bytes < (size_t)(parts * C * 4)) return DVDQ_ERR_WORKSPACE;
+    }
+    if ((s = check_device_arch()) != DVDQ_OK) return s;
+    A.shape = rows_shape(N, S, C);
+    A.gamma = gamma;
+    A.rstd = rstd;
+    A.part = dgamma ? static_cast<float*>(workspace) : nullptr;
+    A.params_f32 = param_dtype == DVDQ_F32;
+    A.inv_c = 1.0f / (float)C;
+    const RowsOf* all[] = {&A.dy, &A.h, &A.dh, &A.dx};
+    const int access = rows_access(all, 4, nullptr, gamma, bytes, pb);
+    int ctas = 0;
+    const cudaError_t e = dtype == DVDQ_BF16  ? launch_rms_norm_backward_bf16(A, access, parts, &ctas, st)
+                          : dtype == DVDQ_F16 ? launch_rms_norm_backward_f16(A, access, parts, &ctas, st)
+                                              : launch_rms_norm_backward_f32(A, access, parts, &ctas, st);
+    if (e != cudaSuccess || !dgamma) return cuda_status(e);
+    return cuda_status(launch_after(rms_norm_join_kernel, dim3((unsigned)ceil_div(C, 32)), dim3(kRmsJoinWarps * 32), 0, st, A.part, ctas, (int)C, dgamma));
 }
 
 }  // extern "C"

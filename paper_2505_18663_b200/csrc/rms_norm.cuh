@@ -38,9 +38,10 @@ __device__ __forceinline__ float bring_to_one(float v) {
 }
 
 // A row in registers (P > 0), or loaded from memory at each visit (P = 0).
-template <typename T, int V, int P>
+template <typename T, int V, int P, bool FULL>
 struct RowValues {
     static constexpr int K = P > 0 ? P : 1;
+    using Lanes = RowLanes<V, P, FULL>;
     Pairs<V> v[K], end;
     const T *x, *r;
     template <bool WHOLE>
@@ -49,24 +50,22 @@ struct RowValues {
         if (r) add_to<V>(h, row_load<T, V, WHOLE>(r, c, C).wide());
         return h;
     }
-    // f(piece, channel, values, Whole or Part)
+    // f(piece, channel, values, Whole or Part, whether the piece is there: its values are zero otherwise)
     template <typename F>
-    __device__ __forceinline__ void visit(const RowLanes& L, F f) {
+    __device__ __forceinline__ void visit(const Lanes& L, F f) {
         if constexpr (P > 0) {
 #pragma unroll
-            for (int i = 0; i < P; ++i)
-                if (L.has(i)) f(i, (L.lane + i * L.lanes) * V, v[i], Whole());
-            if (V > 1 && L.tail) f(P, L.whole * V, end, Part());
+            for (int i = 0; i < P; ++i) f(i, L.channel(i), v[i], Whole(), L.has(i));
+            if (!FULL && V > 1 && L.tail) f(P, L.end(), end, Part(), true);
         } else {
-            int p = L.lane;
-            for (; p < L.whole; p += L.lanes) f(0, p * V, get<true>(p * V, L.C), Whole());
-            if (V > 1 && L.tail) f(0, L.whole * V, get<false>(L.whole * V, L.C), Part());
+            for (int p = L.lane; p < L.whole; p += L.lanes) f(0, p * V, get<true>(p * V, L.C), Whole(), true);
+            if (V > 1 && L.tail) f(0, L.end(), get<false>(L.end(), L.C), Part(), true);
         }
     }
 };
 // U rows' loads, all of them before the first is used.
-template <typename T, int V, int P, int U>
-__device__ __forceinline__ void rows_load(const RowLanes& L, RowValues<T, V, P> (&rows)[U], const bool (&active)[U]) {
+template <typename T, int V, int P, bool FULL, int U>
+__device__ __forceinline__ void rows_load(const RowLanes<V, P, FULL>& L, RowValues<T, V, P, FULL> (&rows)[U], const bool (&active)[U], bool both) {
     if constexpr (P > 0) {
         Piece<T, V> a[U][P], b[U][P];
 #pragma unroll
@@ -74,27 +73,33 @@ __device__ __forceinline__ void rows_load(const RowLanes& L, RowValues<T, V, P> 
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 a[u][i].clear();
-                b[u][i].clear();
-                if (active[u] && L.has(i)) {
-                    a[u][i].load(rows[u].x + (L.lane + i * L.lanes) * V);
-                    if (rows[u].r) b[u][i].load(rows[u].r + (L.lane + i * L.lanes) * V);
-                }
+                if (active[u] && L.has(i)) a[u][i].load(rows[u].x + L.channel(i));
             }
+        if (both) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    b[u][i].clear();
+                    if (active[u] && L.has(i)) b[u][i].load(rows[u].r + L.channel(i));
+                }
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (V > 1 && L.tail) rows[u].end = rows[u].template get<false>(L.whole * V, active[u] ? L.C : 0);
+            if (!FULL && V > 1 && L.tail) rows[u].end = rows[u].template get<false>(L.end(), active[u] ? L.C : 0);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 rows[u].v[i] = a[u][i].wide();
-                if (rows[u].r) add_to<V>(rows[u].v[i], b[u][i].wide());
+                if (both) add_to<V>(rows[u].v[i], b[u][i].wide());
             }
         }
     }
 }
+
 // Codes of V channels: y * inv, rounded to a whole number in the one rounding of its addition to 1.5 * 2^23, whose last byte then is the
 // code.  |y| inv is at most 127 (1 + 2^-22).
 template <int V, bool WHOLE>
-__device__ __forceinline__ void codes_store(int8_t* p, int c, int C, const Pairs<V>& y, float inv) {
+__device__ __forceinline__ void codes_store(int8_t* p, int c, int C, const Pairs<V>& y, float inv, bool there) {
     constexpr int N = Pairs<V>::N;
     uint32_t w[2 * N];
 #pragma unroll
@@ -108,15 +113,16 @@ __device__ __forceinline__ void codes_store(int8_t* p, int c, int C, const Pairs
         uint2 o;
         o.x = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
         o.y = __byte_perm(__byte_perm(w[4], w[5], 0x0040), __byte_perm(w[6], w[7], 0x0040), 0x5410);
-        *reinterpret_cast<uint2*>(p + c) = o;
+        if (there) *reinterpret_cast<uint2*>(p + c) = o;
     } else if constexpr (WHOLE && V == 4) {
-        *reinterpret_cast<uint32_t*>(p + c) = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+        const uint32_t o = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+        if (there) *reinterpret_cast<uint32_t*>(p + c) = o;
     } else if constexpr (WHOLE && V == 2) {
-        *reinterpret_cast<uint16_t*>(p + c) = (uint16_t)__byte_perm(w[0], w[1], 0x0040);
+        if (there) *reinterpret_cast<uint16_t*>(p + c) = (uint16_t)__byte_perm(w[0], w[1], 0x0040);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (c + j < C) p[c + j] = (int8_t)(w[j] & 0xFFu);
+            if (there && c + j < C) p[c + j] = (int8_t)(w[j] & 0xFFu);
     }
 }
 
@@ -127,18 +133,48 @@ __device__ __forceinline__ float root(float m) {
     return r;
 }
 
-// The row's q and top.
-template <typename T, int V, int P, bool NORM, bool KEEP>
-__device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes& L, RowValues<T, V, P>& row, const RowGamma<T, V, P, KEEP>& gamma, RowMeet& meet) {
+// Squares that left fp32's range, or an h gamma that did: the row once more, from memory, with f h, f a power of two that brings the largest
+// |h| (or sqrt(eps), where that is larger) to 1.
+template <typename T, typename Lanes, typename Meet>
+__device__ __forceinline__ RowScale row_far(const RmsArgs& A, const Lanes& L, const T* x, const T* r, Meet& meet) {
+    float f = 1.0f, q = 1.0f, a = 0.f;
+#pragma unroll 1
+    for (int turn = 0; turn < 3; ++turn) {  // largest |h|; sum of squares; largest |y|
+        a = 0.f;
+#pragma unroll 1
+        for (int c = L.lane; c < L.C; c += L.lanes) {
+            float h = to_f32(x[c]);
+            if (r) h += to_f32(r[c]);
+            h *= f;
+            if (turn == 0) a = max_nan(a, fabsf(h));
+            else if (turn == 1) a = fmaf(h, h, a);
+            else a = max_nan(a, fabsf(h * q * gamma_at<T>(A.gamma, A.params_f32, c)));
+        }
+        const float2 all = meet(a, a, turn != 1);
+        if (turn == 0) {
+            const float largest = fmaxf(all.y, sqrtf(A.eps));
+            f = largest <= 3.4028235e38f && largest > 0.f ? bring_to_one(largest) : 1.0f;
+        } else if (turn == 1) {
+            q = 1.0f / sqrtf(fmaf(all.x, A.inv_c, A.eps * f * f));
+        }
+        a = all.y;
+    }
+    return RowScale{q, f, a};
+}
+
+// The row's q and top.  CODES: whether the output in 8 bits is asked for.
+template <bool NORM, bool WIDE, typename T, int V, int P, bool FULL, bool KEEP>
+__device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes<V, P, FULL>& L, RowValues<T, V, P, FULL>& row,
+                                               const RowGamma<T, V, P, FULL, KEEP>& gamma, RowMeet<WIDE>& meet, bool codes) {
     constexpr int N = Pairs<V>::N;
     uint64_t sum = 0ull;
     float top = 0.f;
-    row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole) {
+    row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole, bool) {
         if (NORM) {
 #pragma unroll
             for (int j = 0; j < N; ++j) sum = f2_fma(h.p[j], h.p[j], sum);
         }
-        if (A.scales) {
+        if (codes) {
             const Pairs<V> g = NORM ? gamma.template get<decltype(whole)::value>(i, c) : h;
 #pragma unroll
             for (int j = 0; j < N; ++j) top = max_abs2(top, NORM ? f2_mul(h.p[j], g.p[j]) : h.p[j]);
@@ -146,54 +182,30 @@ __device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes&
     });
     float s0, s1;
     f2_unpack(sum, s0, s1);
-    const float2 all = meet(s0 + s1, top, A.scales != nullptr);
+    const float2 all = meet(s0 + s1, top, codes);
     RowScale o{1.0f, 1.0f, all.y};
     if (!NORM) return o;
     const float m = fmaf(all.x, A.inv_c, A.eps);
     o.q = root(m);
     o.top *= o.q;
-    // Squares that left fp32's range, or an h gamma that did: once more with f h, f a power of two that brings the largest |h|
-    // (or sqrt(eps), where that is larger) to 1.  The rows of a warp take the turn together and keep what is theirs.
+    // The rows of a warp take the turn together and keep what is theirs.
     const bool far = !(m > 1e-30f && m < 1e30f && o.top < 3e38f);
-    if (meet.lanes > 32 ? far : __any_sync(0xFFFFFFFFu, far)) {
-        float largest = 0.f;
-        row.visit(L, [&](int, int, const Pairs<V>& h, auto) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) largest = max_abs2(largest, h.p[j]);
-        });
-        largest = fmaxf(meet(0.f, largest, true).y, sqrtf(A.eps));
-        const float f = largest <= 3.4028235e38f && largest > 0.f ? bring_to_one(largest) : 1.0f;
-        uint64_t ss = 0ull;
-        row.visit(L, [&](int, int, const Pairs<V>& h, auto) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const uint64_t t = f2_mul(h.p[j], f2_splat(f));
-                ss = f2_fma(t, t, ss);
-            }
-        });
-        f2_unpack(ss, s0, s1);
-        const float q = 1.0f / sqrtf(fmaf(meet(s0 + s1, 0.f, false).x, A.inv_c, A.eps * f * f));
-        top = 0.f;
-        row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole) {
-            const Pairs<V> g = gamma.template get<decltype(whole)::value>(i, c);
-#pragma unroll
-            for (int j = 0; j < N; ++j) top = max_abs2(top, f2_mul(f2_mul(f2_mul(h.p[j], f2_splat(f)), f2_splat(q)), g.p[j]));
-        });
-        top = meet(0.f, top, true).y;
-        if (far) o = RowScale{q, f, top};
+    if (WIDE ? far : __any_sync(0xFFFFFFFFu, far)) {
+        const RowScale again = row_far<T>(A, L, row.x, row.r, meet);
+        if (far) o = again;
     }
     return o;
 }
 
-template <typename T, int V, int P, bool NORM, bool KEEP>
-__device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes& L, RowValues<T, V, P>& row, const RowGamma<T, V, P, KEEP>& gamma, const RowScale& o,
-                                          uint32_t index, uint32_t n, uint32_t s) {
+template <bool NORM, typename T, int V, int P, bool FULL, bool KEEP>
+__device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P, FULL>& L, RowValues<T, V, P, FULL>& row,
+                                          const RowGamma<T, V, P, FULL, KEEP>& gamma, const RowScale& o, uint32_t index, uint32_t n, uint32_t s, bool codes) {
     constexpr int N = Pairs<V>::N;
     const int C = A.shape.C;
-    if (A.rstd && L.lane == 0) A.rstd[index] = o.q * o.f;
+    if (NORM && A.rstd && L.lane == 0) A.rstd[index] = o.q * o.f;
     // codes are y lift inv; a row near the smallest numbers is lifted first, so that 127 / top stays finite
     float lift = 0.f, inv = 0.f;
-    if (A.scales) {
+    if (codes) {
         const bool finite = o.top <= 3.4028235e38f;  // not NaN, not infinite
         if (finite && o.top > 0.f) {
             lift = o.top < 1e-30f ? 18446744073709551616.0f : 1.0f;
@@ -201,14 +213,14 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes& L, R
         }
         if (L.lane == 0) A.scales[index] = finite ? o.top / 127.0f : __uint_as_float(0x7FC00000u);
     }
-    T* to_h = A.h.p ? static_cast<T*>(A.h.p) + row_at(A.h, n, s) : nullptr;
-    T* to_y = A.y.p ? static_cast<T*>(A.y.p) + row_at(A.y, n, s) : nullptr;
-    int8_t* to_c = A.codes.p ? static_cast<int8_t*>(A.codes.p) + row_at(A.codes, n, s) : nullptr;
-    if (!to_h && !to_y && !to_c) return;
-    row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole) {
+    T* to_h = NORM && A.h.p ? static_cast<T*>(A.h.p) + row_at(A.h, n, s) : nullptr;
+    T* to_y = NORM && A.y.p ? static_cast<T*>(A.y.p) + row_at(A.y, n, s) : nullptr;
+    int8_t* to_c = codes ? static_cast<int8_t*>(A.codes.p) + row_at(A.codes, n, s) : nullptr;
+    if (to_h) row.visit(L, [&](int, int c, const Pairs<V>& h, auto whole, bool there) { row_store<T, V, decltype(whole)::value>(to_h, c, C, h, there); });
+    if (!to_y && !codes) return;
+    const bool plain = o.f == 1.0f && lift == 1.0f;  // else: far from one, near the smallest numbers, zeros or not finite
+    row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole, bool there) {
         constexpr bool W = decltype(whole)::value;
-        if (to_h) row_store<T, V, W>(to_h, c, C, h);
-        if (!to_y && !to_c) return;
         Pairs<V> y = h;
         if (NORM) {
             if (o.f != 1.0f) {
@@ -219,13 +231,13 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes& L, R
 #pragma unroll
             for (int j = 0; j < N; ++j) y.p[j] = f2_mul(f2_mul(y.p[j], f2_splat(o.q)), g.p[j]);
         }
-        if (to_y) row_store<T, V, W>(to_y, c, C, y);
-        if (to_c) {
-            if (lift != 1.0f) {  // near the smallest numbers; or 0: zeros, or not finite: codes 0
+        if (to_y) row_store<T, V, W>(to_y, c, C, y, there);
+        if (codes) {
+            if (!plain) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) y.p[j] = lift == 0.f ? 0ull : f2_mul(y.p[j], f2_splat(lift));
             }
-            codes_store<V, W>(to_c, c, C, y, inv);
+            codes_store<V, W>(to_c, c, C, y, inv, there);
         }
     });
 }
@@ -234,74 +246,103 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes& L, R
 __host__ __device__ constexpr int rows_at_once(int P) { return P == 1 ? 4 : P == 2 ? 2 : 1; }
 __host__ __device__ constexpr int rows_threads(int V, int P) { return P * V > 24 ? 256 : P * V > 8 ? 512 : kRowThreads; }
 
+// What a call asks for, as far as kernels are built for it (each branch of an inner loop costs as much as a piece's arithmetic): a
+// residual, codes; else all is looked up at run time.
+enum RowsAsk { kAskAny = 0, kAskPlain = 1, kAskResidual = 2, kAskCodes = 3, kAskBoth = 4 };
+
 // WIDE: a row has the CTA to itself.
-template <typename T, int V, int P, bool NORM, bool WIDE>
+template <typename T, int V, int P, bool NORM, bool WIDE, bool FULL, int ASK>
 __global__ void __launch_bounds__(WIDE ? rows_threads(V, P) : kSmallThreads)
 rms_norm_kernel(const __grid_constant__ RmsArgs A) {
     constexpr int U = WIDE ? 1 : rows_at_once(P);
     constexpr bool KEEP = NORM && P > 0 && P * V <= 40;
+    const bool both = ASK == kAskAny ? A.r.p != nullptr : ASK == kAskResidual || ASK == kAskBoth;
+    const bool codes = !NORM || (ASK == kAskAny ? A.scales != nullptr : ASK == kAskCodes || ASK == kAskBoth);
     __shared__ float2 slots[64];
     const int lanes = WIDE ? (int)blockDim.x : A.lanes, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
     const int groups = WIDE ? 1 : kSmallThreads >> A.lanes_log2, group = WIDE ? 0 : (int)threadIdx.x >> A.lanes_log2;
-    const RowLanes L(A.shape.C, lanes, lane, V);
-    RowMeet meet(slots, lanes);
+    const RowLanes<V, P, FULL> L(A.shape.C, lanes, lane);
+    RowMeet<WIDE> meet(slots, lanes);
     wait_predecessor();
     release_successor();
-    RowGamma<T, V, P, KEEP> gamma;
+    RowGamma<T, V, P, FULL, KEEP> gamma;
     if (NORM) gamma.init(L, A.gamma, A.params_f32);
     for (int64_t at = (int64_t)blockIdx.x * (groups * U); at < A.shape.rows; at += (int64_t)gridDim.x * (groups * U)) {
-        RowValues<T, V, P> rows[U];
+        RowValues<T, V, P, FULL> rows[U];
         uint32_t index[U], n[U], s[U];
         bool active[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = at + u * groups + group;
-            active[u] = row < A.shape.rows;
+            active[u] = WIDE || row < A.shape.rows;
             index[u] = (uint32_t)(active[u] ? row : at);  // threads without a row of their own take part in the exchanges
             n[u] = A.shape.by_s(index[u]);
             s[u] = index[u] - n[u] * (uint32_t)A.shape.S;
             rows[u].x = static_cast<const T*>(A.x.p) + row_at(A.x, n[u], s[u]);
-            rows[u].r = A.r.p ? static_cast<const T*>(A.r.p) + row_at(A.r, n[u], s[u]) : nullptr;
+            rows[u].r = both ? static_cast<const T*>(A.r.p) + row_at(A.r, n[u], s[u]) : nullptr;
         }
-        rows_load<T, V, P, U>(L, rows, active);
+        rows_load<T, V, P, FULL, U>(L, rows, active, both);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const RowScale o = row_decide<T, V, P, NORM, KEEP>(A, L, rows[u], gamma, meet);
-            if (active[u]) row_write<T, V, P, NORM, KEEP>(A, L, rows[u], gamma, o, index[u], n[u], s[u]);
+            const RowScale o = row_decide<NORM>(A, L, rows[u], gamma, meet, codes);
+            if (active[u]) row_write<NORM>(A, L, rows[u], gamma, o, index[u], n[u], s[u], codes);
         }
     }
 }
 
 // ------------------------------------------------------------------ launches
 
-template <typename T, int V, int P, bool NORM, bool WIDE>
+template <typename T, int V, int P, bool NORM, bool WIDE, bool FULL, int ASK>
 static cudaError_t launch_rms_p(const RmsArgs& A0, const RowsPlan& p, cudaStream_t st) {
     RmsArgs A = A0;
     A.lanes = p.lanes;
     A.lanes_log2 = p.lanes_log2;
-    auto kern = rms_norm_kernel<T, V, P, NORM, WIDE>;
+    auto kern = rms_norm_kernel<T, V, P, NORM, WIDE, FULL, ASK>;
     static PerDevice<RowsHeld> cache;
     const int held = rows_held(cache, kern, p.threads);
     if (held == 0) return cudaErrorInvalidValue;
     const int64_t at_once = WIDE ? 1 : (int64_t)(kSmallThreads / p.lanes) * rows_at_once(P), ctas = ceil_div(A.shape.rows, at_once);
     return launch_after(kern, dim3((unsigned)(ctas < 148 * held ? ctas : 148 * held)), dim3(p.threads), 0, st, A);
 }
-template <typename T, int V, int P, bool NORM>
+template <typename T, int V, int P, bool NORM, bool FULL, int ASK>
 static cudaError_t launch_rms_w(const RmsArgs& A, const RowsPlan& p, cudaStream_t st) {
-    return p.wide ? launch_rms_p<T, V, P, NORM, true>(A, p, st) : launch_rms_p<T, V, P, NORM, false>(A, p, st);
+    return p.wide ? launch_rms_p<T, V, P, NORM, true, FULL, ASK>(A, p, st) : launch_rms_p<T, V, P, NORM, false, FULL, ASK>(A, p, st);
+}
+template <typename T, int V, int P, bool NORM>
+static cudaError_t launch_rms_full(const RmsArgs& A, const RowsPlan& p, cudaStream_t st) {
+    if constexpr (NORM) {
+        if (A.r.p && A.scales) return launch_rms_w<T, V, P, NORM, true, kAskBoth>(A, p, st);
+        if (A.r.p) return launch_rms_w<T, V, P, NORM, true, kAskResidual>(A, p, st);
+        if (A.scales) return launch_rms_w<T, V, P, NORM, true, kAskCodes>(A, p, st);
+        return launch_rms_w<T, V, P, NORM, true, kAskPlain>(A, p, st);
+    }
+    return launch_rms_w<T, V, P, NORM, true, kAskCodes>(A, p, st);
 }
 template <typename T, int V, bool NORM>
 static cudaError_t launch_rms_v(const RmsArgs& A, cudaStream_t st) {
-    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), 8, [](int k) { return rows_threads(V, k); });
+    constexpr bool kPieces16 = V * sizeof(T) == 16;
+    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0, 8, [](int k) { return rows_threads(V, k); });
+    if constexpr (kPieces16) {
+        if (p.full) {
+            switch (p.pieces) {
+                case 1: return launch_rms_full<T, V, 1, NORM>(A, p, st);
+                case 2: return launch_rms_full<T, V, 2, NORM>(A, p, st);
+                case 3: return launch_rms_full<T, V, 3, NORM>(A, p, st);
+                case 4: return launch_rms_full<T, V, 4, NORM>(A, p, st);
+                case 5: return launch_rms_full<T, V, 5, NORM>(A, p, st);
+                case 6: return launch_rms_full<T, V, 6, NORM>(A, p, st);
+                case 7: return launch_rms_full<T, V, 7, NORM>(A, p, st);
+                default: return launch_rms_full<T, V, 8, NORM>(A, p, st);
+            }
+        }
+    }
+    constexpr int ask = NORM ? kAskAny : kAskCodes;
     switch (p.pieces) {
-        case 0: return launch_rms_p<T, V, 0, NORM, true>(A, p, st);
-        case 1: return launch_rms_w<T, V, 1, NORM>(A, p, st);
-        case 2: return launch_rms_w<T, V, 2, NORM>(A, p, st);
-        case 3: return launch_rms_w<T, V, 3, NORM>(A, p, st);
-        case 4: return launch_rms_w<T, V, 4, NORM>(A, p, st);
-        case 5: return launch_rms_w<T, V, 5, NORM>(A, p, st);
-        case 6: return launch_rms_w<T, V, 6, NORM>(A, p, st);
-        default: return launch_rms_w<T, V, 8, NORM>(A, p, st);
+        case 0: return launch_rms_p<T, V, 0, NORM, true, false, ask>(A, p, st);
+        case 1: return launch_rms_w<T, V, 1, NORM, false, ask>(A, p, st);
+        case 2: return launch_rms_w<T, V, 2, NORM, false, ask>(A, p, st);
+        case 4: return launch_rms_w<T, V, 4, NORM, false, ask>(A, p, st);
+        default: return launch_rms_w<T, V, 8, NORM, false, ask>(A, p, st);
     }
 }
 // `access`: bytes of a piece that every tensor's alignment allows: 16, 4 or the element's

@@ -21,15 +21,13 @@ struct RmsBackwardArgs {
     int lanes, lanes_log2;
 };
 
-// q (gamma dy - hh mean) + more
+// q (gamma dy - h (q mean))
 template <int V>
 __device__ __forceinline__ Pairs<V> row_gradient(const Pairs<V>& d, const Pairs<V>& h, const Pairs<V>& g, float q, float mean) {
     Pairs<V> o;
+    const uint64_t along = f2_splat(-q * mean);
 #pragma unroll
-    for (int j = 0; j < Pairs<V>::N; ++j) {
-        const uint64_t along = f2_mul(f2_mul(h.p[j], f2_splat(q)), f2_splat(mean));
-        o.p[j] = f2_mul(f2_sub(f2_mul(d.p[j], g.p[j]), along), f2_splat(q));
-    }
+    for (int j = 0; j < Pairs<V>::N; ++j) o.p[j] = f2_mul(f2_fma(h.p[j], along, f2_mul(d.p[j], g.p[j])), f2_splat(q));
     return o;
 }
 // What one piece adds to dgamma, and to the row's <dh hh>.
@@ -46,19 +44,20 @@ __device__ __forceinline__ Pairs<V> row_terms(const Pairs<V>& d, const Pairs<V>&
 __host__ __device__ constexpr int rows_threads_backward(int V, int P) { return P * V > 16 ? 256 : P * V > 4 ? 512 : kRowThreads; }
 
 // A thread's channels are the same in every row that it meets, so dgamma's sums stay with it (P > 0: in registers; P = 0: in the CTA's own
-// row of `part`) until the CTA has been through its rows.
-template <typename T, int V, int P, bool WIDE>
+// row of `part`) until the CTA has been through its rows.  FULL: dX is asked for, and every thread has P whole pieces.
+template <typename T, int V, int P, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(WIDE ? rows_threads_backward(V, P) : kSmallThreads)
 rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     constexpr int N = Pairs<V>::N, K = P > 0 ? P : 1, U = !WIDE && P > 0 && P <= 2 ? 2 : 1;
-    constexpr bool KEEP = P > 0 && P * V <= 24;
+    constexpr bool KEEP = P > 0 && P * V <= 16;
     __shared__ float2 slots[64];
     extern __shared__ float joined[];
     const int lanes = WIDE ? (int)blockDim.x : A.lanes, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
     const int groups = WIDE ? 1 : kSmallThreads >> A.lanes_log2, group = WIDE ? 0 : (int)threadIdx.x >> A.lanes_log2;
     const int C = A.shape.C;
-    const RowLanes L(C, lanes, lane, V);
-    RowMeet meet(slots, lanes);
+    const bool with_dx = FULL || A.dx.p != nullptr, with_dh = with_dx && A.dh.p != nullptr;
+    const RowLanes<V, P, FULL> L(C, lanes, lane);
+    RowMeet<WIDE> meet(slots, lanes);
     Pairs<V> acc[K + 1];
 #pragma unroll
     for (int i = 0; i <= K; ++i)
@@ -67,7 +66,7 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     float* mine = A.part ? A.part + (int64_t)blockIdx.x * C : nullptr;
     wait_predecessor();
     release_successor();
-    RowGamma<T, V, P, KEEP> gamma;
+    RowGamma<T, V, P, FULL, KEEP> gamma;
     gamma.init(L, A.gamma, A.params_f32);
     bool first = true;
     for (int64_t at = (int64_t)blockIdx.x * (groups * U); at < A.shape.rows; at += (int64_t)gridDim.x * (groups * U)) {
@@ -79,48 +78,55 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = at + u * groups + group;
-            active[u] = row < A.shape.rows;
+            active[u] = WIDE || row < A.shape.rows;
             const uint32_t index = (uint32_t)(active[u] ? row : at), n = A.shape.by_s(index), s = index - n * (uint32_t)A.shape.S;
             dy[u] = static_cast<const T*>(A.dy.p) + row_at(A.dy, n, s);
             h[u] = static_cast<const T*>(A.h.p) + row_at(A.h, n, s);
-            dh[u] = A.dh.p && A.dx.p ? static_cast<const T*>(A.dh.p) + row_at(A.dh, n, s) : nullptr;
-            dx[u] = A.dx.p ? static_cast<T*>(A.dx.p) + row_at(A.dx, n, s) : nullptr;
+            if (with_dh) dh[u] = static_cast<const T*>(A.dh.p) + row_at(A.dh, n, s);
+            if (with_dx) dx[u] = static_cast<T*>(A.dx.p) + row_at(A.dx, n, s);
             q[u] = A.rstd[index];
         }
-        auto ask = [&](int u, int i, int c, auto whole) {
+        auto ask = [&](int u, int i, int c, auto whole, bool there) {
             constexpr bool W = decltype(whole)::value;
+            if (W && !there) {
+                a[u][i].clear();
+                b[u][i].clear();
+                return;
+            }
             a[u][i] = row_load<T, V, W>(dy[u], c, C);
             b[u][i] = row_load<T, V, W>(h[u], c, C);
-            if (dh[u]) e[u][i] = row_load<T, V, W>(dh[u], c, C);
         };
-        // f(u, piece, channel, Whole or Part)
+        auto ask_more = [&](int u, int i, int c, auto whole, bool there) {
+            if (there) e[u][i] = row_load<T, V, decltype(whole)::value>(dh[u], c, C);
+        };
+        // f(u, piece, channel, Whole or Part, whether the piece is there)
         auto visit = [&](int u, auto f) {
-            if (!active[u]) return;
             if constexpr (P > 0) {
 #pragma unroll
-                for (int i = 0; i < P; ++i)
-                    if (L.has(i)) f(u, i, (L.lane + i * L.lanes) * V, Whole());
-                if (V > 1 && L.tail) f(u, P, L.whole * V, Part());
+                for (int i = 0; i < P; ++i) f(u, i, L.channel(i), Whole(), active[u] && L.has(i));
+                if (!FULL && V > 1 && L.tail && active[u]) f(u, P, L.end(), Part(), true);
             } else {
-                int p = L.lane;
-                for (; p < L.whole; p += L.lanes) {
-                    ask(u, 0, p * V, Whole());
-                    f(u, 0, p * V, Whole());
+                for (int p = L.lane; p < L.whole; p += L.lanes) {
+                    ask(u, 0, p * V, Whole(), true);
+                    f(u, 0, p * V, Whole(), true);
                 }
                 if (V > 1 && L.tail) {
-                    ask(u, 0, L.whole * V, Part());
-                    f(u, 0, L.whole * V, Part());
+                    ask(u, 0, L.end(), Part(), true);
+                    f(u, 0, L.end(), Part(), true);
                 }
             }
         };
         if constexpr (P > 0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) visit(u, ask);
+            for (int u = 0; u < U; ++u) {
+                visit(u, ask);
+                if (with_dh) visit(u, ask_more);
+            }
         }
 #pragma unroll
         for (int v = 0; v < U; ++v) {
             uint64_t sum = 0ull;
-            visit(v, [&](int u, int i, int c, auto whole) {
+            visit(v, [&](int u, int i, int c, auto whole, bool) {
                 const Pairs<V> t = row_terms<V>(a[u][i].wide(), b[u][i].wide(), gamma.template get<decltype(whole)::value>(i, c), q[u], sum);
                 if constexpr (P > 0) {
                     add_to<V>(acc[i], t);
@@ -131,15 +137,18 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
                 }
             });
             first = false;
-            if (!A.dx.p) continue;
+            if (!with_dx) continue;
             float s0, s1;
             f2_unpack(sum, s0, s1);
             const float mean = meet(s0 + s1, 0.f, false).x * A.inv_c;
-            visit(v, [&](int u, int i, int c, auto whole) {
+            visit(v, [&](int u, int i, int c, auto whole, bool there) {
                 constexpr bool W = decltype(whole)::value;
                 Pairs<V> o = row_gradient<V>(a[u][i].wide(), b[u][i].wide(), gamma.template get<W>(i, c), q[u], mean);
-                if (dh[u]) add_to<V>(o, e[u][i].wide());
-                row_store<T, V, W>(dx[u], c, C, o);
+                if (with_dh) {
+                    if constexpr (P == 0) ask_more(u, i, c, whole, there);
+                    add_to<V>(o, e[u][i].wide());
+                }
+                row_store<T, V, W>(dx[u], c, C, o, there);
             });
         }
     }
@@ -151,12 +160,12 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
         for (int i = 0; i < P; ++i)
             if (L.has(i)) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) to[(L.lane + i * L.lanes) * V + j] = acc[i].get(j);
+                for (int j = 0; j < V; ++j) to[L.channel(i) + j] = acc[i].get(j);
             }
-        if (V > 1 && L.tail) {
+        if (!FULL && V > 1 && L.tail) {
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (L.whole * V + j < C) to[L.whole * V + j] = acc[P].get(j);
+                if (L.end() + j < C) to[L.end() + j] = acc[P].get(j);
         }
         if (groups == 1) return;
         __syncthreads();
@@ -207,12 +216,12 @@ inline int64_t rms_parts(int64_t rows, int64_t C) {
 
 // ------------------------------------------------------------------ launches
 
-template <typename T, int V, int P, bool WIDE>
+template <typename T, int V, int P, bool WIDE, bool FULL>
 static cudaError_t launch_rms_backward_p(const RmsBackwardArgs& A0, const RowsPlan& p, int64_t parts, int* ctas_out, cudaStream_t st) {
     RmsBackwardArgs A = A0;
     A.lanes = p.lanes;
     A.lanes_log2 = p.lanes_log2;
-    auto kern = rms_norm_backward_kernel<T, V, P, WIDE>;
+    auto kern = rms_norm_backward_kernel<T, V, P, WIDE, FULL>;
     static PerDevice<RowsHeld> cache;
     const int held = rows_held(cache, kern, p.threads);
     if (held == 0) return cudaErrorInvalidValue;
@@ -224,24 +233,34 @@ static cudaError_t launch_rms_backward_p(const RmsBackwardArgs& A0, const RowsPl
     const size_t sums = A.part && groups > 1 ? (size_t)groups * A.shape.C * 4 : 0;  // of 128 threads with 8 pieces at most: 32 KB
     return launch_after(kern, dim3((unsigned)ctas), dim3(p.threads), sums, st, A);
 }
-template <typename T, int V, int P>
+template <typename T, int V, int P, bool FULL>
 static cudaError_t launch_rms_backward_w(const RmsBackwardArgs& A, const RowsPlan& p, int64_t parts, int* ctas, cudaStream_t st) {
-    return p.wide ? launch_rms_backward_p<T, V, P, true>(A, p, parts, ctas, st) : launch_rms_backward_p<T, V, P, false>(A, p, parts, ctas, st);
+    return p.wide ? launch_rms_backward_p<T, V, P, true, FULL>(A, p, parts, ctas, st) : launch_rms_backward_p<T, V, P, false, FULL>(A, p, parts, ctas, st);
 }
 template <typename T, int V>
 static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts, int* ctas, cudaStream_t st) {
-    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), V == 8 ? 6 : 8, [](int k) { return rows_threads_backward(V, k); });
+    constexpr bool kPieces16 = V * sizeof(T) == 16;
+    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0 && A.dx.p, 8, [](int k) { return rows_threads_backward(V, k); });
+    if constexpr (kPieces16) {
+        if (p.full) {
+            switch (p.pieces) {
+                case 1: return launch_rms_backward_w<T, V, 1, true>(A, p, parts, ctas, st);
+                case 2: return launch_rms_backward_w<T, V, 2, true>(A, p, parts, ctas, st);
+                case 3: return launch_rms_backward_w<T, V, 3, true>(A, p, parts, ctas, st);
+                case 4: return launch_rms_backward_w<T, V, 4, true>(A, p, parts, ctas, st);
+                case 5: return launch_rms_backward_w<T, V, 5, true>(A, p, parts, ctas, st);
+                case 6: return launch_rms_backward_w<T, V, 6, true>(A, p, parts, ctas, st);
+                case 7: return launch_rms_backward_w<T, V, 7, true>(A, p, parts, ctas, st);
+                default: return launch_rms_backward_w<T, V, 8, true>(A, p, parts, ctas, st);
+            }
+        }
+    }
     switch (p.pieces) {
-        case 0: return launch_rms_backward_p<T, V, 0, true>(A, p, parts, ctas, st);
-        case 1: return launch_rms_backward_w<T, V, 1>(A, p, parts, ctas, st);
-        case 2: return launch_rms_backward_w<T, V, 2>(A, p, parts, ctas, st);
-        case 3: return launch_rms_backward_w<T, V, 3>(A, p, parts, ctas, st);
-        case 4: return launch_rms_backward_w<T, V, 4>(A, p, parts, ctas, st);
-        case 5: return launch_rms_backward_w<T, V, 5>(A, p, parts, ctas, st);
-        case 6: return launch_rms_backward_w<T, V, 6>(A, p, parts, ctas, st);
-        default:
-            if constexpr (V < 8) return launch_rms_backward_w<T, V, 8>(A, p, parts, ctas, st);
-            return cudaErrorInvalidValue;  // not reached: `most` is 6
+        case 0: return launch_rms_backward_p<T, V, 0, true, false>(A, p, parts, ctas, st);
+        case 1: return launch_rms_backward_w<T, V, 1, false>(A, p, parts, ctas, st);
+        case 2: return launch_rms_backward_w<T, V, 2, false>(A, p, parts, ctas, st);
+        case 4: return launch_rms_backward_w<T, V, 4, false>(A, p, parts, ctas, st);
+        default: return launch_rms_backward_w<T, V, 8, false>(A, p, parts, ctas, st);
     }
 }
 template <typename T>

@@ -124,15 +124,19 @@ __device__ __forceinline__ Piece<T, V> row_load(const T* p, int c, int C) {
     return v;
 }
 template <typename T, int V, bool WHOLE>
-__device__ __forceinline__ void row_store(T* p, int c, int C, const Pairs<V>& f) {
+__device__ __forceinline__ void row_store(T* p, int c, int C, const Pairs<V>& f, bool there) {
     const Piece<T, V> v = Piece<T, V>::narrow(f);
     if constexpr (WHOLE) {
-        v.store(p + c);
+        if (there) v.store(p + c);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (c + j < C) p[c + j] = v.take(j);
+            if (there && c + j < C) p[c + j] = v.take(j);
     }
+}
+template <typename T>
+__device__ __forceinline__ float gamma_at(const void* gamma, int params_f32, int c) {
+    return !gamma ? 1.0f : params_f32 ? static_cast<const float*>(gamma)[c] : to_f32(static_cast<const T*>(gamma)[c]);
 }
 template <typename T, int V, bool WHOLE>
 __device__ __forceinline__ Pairs<V> gamma_load(const void* gamma, int params_f32, int c, int C) {  // NULL: ones
@@ -174,18 +178,22 @@ __device__ __forceinline__ int64_t row_at(const RowsOf& t, uint32_t n, uint32_t 
 
 // ------------------------------------------------------------------ what a whole row decides
 
-// Sum of a and max of b over the threads of a row, the same bits in each of them.  A CTA's warps meet through shared memory;
+// Sum of a and max of b over the threads of a row, the same bits in each of them.  WIDE: a CTA's warps meet through shared memory;
 // `turn` alternates between two sets of slots, so that one barrier a row is enough.
+template <bool WIDE>
 struct RowMeet {
-    float2* slots;   // [2][32], where the row has the CTA to itself
+    float2* slots;   // [2][32]
     int lanes, turn = 0;
     __device__ __forceinline__ RowMeet(float2* s, int l) : slots(s), lanes(l) {}
     __device__ __forceinline__ float2 operator()(float a, float b, bool with_max) {
-        for (int o = (lanes < 32 ? lanes : 32) >> 1; o > 0; o >>= 1) {
-            a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-            if (with_max) b = max_nan(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            if (WIDE || o < lanes) {
+                a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+                if (with_max) b = max_nan(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
+            }
         }
-        if (lanes > 32) {
+        if constexpr (WIDE) {
             float2* at = slots + 32 * turn;
             turn ^= 1;
             if ((threadIdx.x & 31) == 0) at[threadIdx.x >> 5] = make_float2(a, b);
@@ -213,35 +221,43 @@ struct RowMeet {
 };
 
 // The pieces of a row that a thread has: whole ones (lane + i lanes, i < P), and behind the last of them, where V does not divide C, the row's end.
+// FULL: every thread has P whole pieces, and that is the row.
+template <int V, int P, bool FULL>
 struct RowLanes {
-    int C, lanes, lane, whole, tail;  // whole pieces of the row; whether this thread has its end
-    __device__ __forceinline__ RowLanes(int channels, int n, int l, int V) : C(channels), lanes(n), lane(l) {
+    int C, lanes, lane, whole;  // whole pieces of the row
+    bool tail;                  // whether this thread has its end
+    __device__ __forceinline__ RowLanes(int channels, int n, int l) : C(channels), lanes(n), lane(l) {
         whole = channels / V;
-        tail = channels % V != 0 && whole % n == l;
+        tail = !FULL && V > 1 && channels % V != 0 && whole % n == l;
     }
-    __device__ __forceinline__ bool has(int i) const { return lane + i * lanes < whole; }
+    __device__ __forceinline__ bool has(int i) const { return FULL || lane + i * lanes < whole; }
+    __device__ __forceinline__ int channel(int i) const { return (lane + i * lanes) * V; }
+    __device__ __forceinline__ int end() const { return whole * V; }
 };
-
 // gamma of a thread's channels: kept (KEEP), or loaded where it is needed
-template <typename T, int V, int P, bool KEEP>
+template <typename T, int V, int P, bool FULL, bool KEEP>
 struct RowGamma {
     static constexpr int K = KEEP ? P : 0;
+    using Lanes = RowLanes<V, P, FULL>;
     Pairs<V> g[K + 1], end;
     const void* p;
     int f32, C;
-    __device__ __forceinline__ void init(const RowLanes& L, const void* gamma, int params_f32) {
+    __device__ __forceinline__ void init(const Lanes& L, const void* gamma, int params_f32) {
         p = gamma;
         f32 = params_f32;
         C = L.C;
 #pragma unroll
-        for (int i = 0; i < K; ++i)
-            if (L.has(i)) g[i] = gamma_load<T, V, true>(p, f32, (L.lane + i * L.lanes) * V, C);
-        if (KEEP && V > 1 && L.tail) end = gamma_load<T, V, false>(p, f32, L.whole * V, C);
+        for (int i = 0; i < K; ++i) {
+#pragma unroll
+            for (int j = 0; j < Pairs<V>::N; ++j) g[i].p[j] = 0ull;
+            if (L.has(i)) g[i] = gamma_load<T, V, true>(p, f32, L.channel(i), C);
+        }
+        if (KEEP && L.tail) end = gamma_load<T, V, false>(p, f32, L.end(), C);
     }
     template <bool WHOLE>
     __device__ __forceinline__ Pairs<V> get(int i, int c) const {
         if constexpr (KEEP) return WHOLE ? g[i] : end;
-        else return gamma_load<T, V, WHOLE>(p, f32, c, C);
+        else return gamma_load<T, V, WHOLE>(p, f32, WHOLE && c + V > C ? 0 : c, C);  // a piece that is not there: any
     }
 };
 
@@ -249,36 +265,43 @@ struct RowGamma {
 
 struct RowsPlan {
     int lanes, lanes_log2, threads, pieces;  // pieces 0: the row is read again instead of kept
-    bool wide;
+    bool wide, full;
 };
-// How `rows` rows of nv pieces are laid over threads that keep up to `most` pieces each, in CTAs of up to limit(pieces) threads.
+// Pieces a thread that the kernels are built for, in CTAs (wide) or in lanes of a warp: 1, 2, 4, 8, and where they fill the threads 3, 5, 6, 7 too.
+constexpr int rows_pieces(int64_t k) { return k <= 2 ? (int)k : k <= 4 ? 4 : 8; }
+// How `rows` rows of nv pieces are laid over threads that keep up to `most` pieces each, in CTAs of up to limit(pieces) threads.  `whole`: nothing is left
+// of the row behind its pieces.
 template <typename Limit>
-inline RowsPlan rows_plan(int64_t rows, int64_t nv, int most, Limit limit) {
+inline RowsPlan rows_plan(int64_t rows, int64_t nv, bool whole, int most, Limit limit) {
     RowsPlan p = {};
-    if (nv <= 64 || (nv <= 32 * most && rows >= 148 * 8)) {  // a warp or part of it
+    const bool few = rows < 148 * 2;
+    if (nv <= 64 || (nv <= 32 * most && !few && rows >= 148 * 8)) {  // a warp or part of it
         p.lanes_log2 = 5;
         while (p.lanes_log2 > 0 && nv <= 1 << p.lanes_log2) --p.lanes_log2;  // two pieces a thread, where there are two
         p.lanes = 1 << p.lanes_log2;
         p.threads = kSmallThreads;
         p.pieces = (int)ceil_div(nv, p.lanes);
+        p.full = whole && nv == (int64_t)p.pieces * p.lanes;
+        if (!p.full) p.pieces = rows_pieces(p.pieces);
         return p;
     }
-    // a CTA: few rows take as many threads as there are pieces, many rows fewer threads with several pieces each
     p.wide = true;
-    const bool few = rows < 148 * 2;
-    int64_t best = 0;
-    for (int k = few ? 1 : most < 4 ? most : 4; k <= most; ++k) {
+    // a CTA whose threads all have as many pieces: four to `most` (few rows: as few as there can be)
+    for (int k = few ? 1 : most < 4 ? most : 4; whole && k <= most; ++k)
+        if (nv % (32 * k) == 0 && nv / k >= 64 && nv / k <= limit(k)) {
+            p.pieces = k;
+            p.lanes = p.threads = (int)(nv / k);
+            p.full = true;
+            return p;
+        }
+    for (int k = few ? 1 : most < 4 ? most : 4; k <= most; k *= 2) {
         const int64_t threads = align_up(ceil_div(nv, k), 32);
         if (threads > limit(k)) continue;
-        if (p.pieces == 0 || threads * k < best) {
-            best = threads * k;
-            p.pieces = k;
-            p.threads = (int)(threads < 64 ? 64 : threads);
-            if (few) break;
-        }
+        p.pieces = k;
+        p.lanes = p.threads = (int)(threads < 64 ? 64 : threads);
+        return p;
     }
-    if (p.pieces == 0) p.threads = kRowThreads;
-    p.lanes = p.threads;
+    p.lanes = p.threads = kRowThreads;
     return p;
 }
 // CTAs of a kernel that an SM holds, for each number of warps (asked once).
