@@ -534,52 +534,78 @@ def dvdq_group_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tens
            "dvdq_group_norm_backward")
 
 
-def _on_current_device(t: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-    """The calls run on the current device: tensors of another one are refused, not read from there."""
-    device = t.device
-    if device.type != "cuda":
-        raise TypeError("tensors must be CUDA tensors")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    for o in others:
-        if o is not None and o.device != device:
-            raise ValueError(f"tensors must all be on {device}, got one on {o.device}")
+def _current(t: torch.Tensor, name: str) -> int:
+    """The current device, which the calls run on; a tensor that is elsewhere is refused."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
 
 
-def _rows3(t: Optional[torch.Tensor], dtype, shape, name: str):
-    """(address, outer pitch, row pitch) of rows in an [N, S, C] tensor, or (N = 1) in an [S, C] one."""
-    if t is None:
-        return None, 0, 0
+def _refuse(t: torch.Tensor, dtype, shape, dev: int, name: str, inner: str):
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on cuda:{dev} as the others are, got {t.device}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise TypeError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    st = t.stride()
-    if shape[-1] > 1 and st[-1] != 1:
-        raise TypeError(f"{name} must have unit stride inside a row")
-    return _address(t, dtype, name), st[0] if len(st) == 3 else 0, st[-2]
+    raise TypeError(f"{name} must {inner}")
 
 
-def _row_values(t: Optional[torch.Tensor], shape, name: str):
-    """A dense fp32 value for each row."""
-    if t is not None and (t.shape != shape[:-1] or not t.is_contiguous()):
-        raise TypeError(f"{name} must be dense {tuple(shape[:-1])}")
-    return _address(t, torch.float32, name)
+# The checks below look at a tensor once, in the order of what is cheap, and say what is wrong afterwards: a call of the smallest
+# rows takes longer here than on the GPU.
+def _rows3(t: torch.Tensor, dtype, shape, dev: int, name: str):
+    """(address, outer pitch, row pitch) of rows in an [N, S, C] tensor, or (N = 1) in an [S, C] one."""
+    if t.get_device() == dev and t.dtype is dtype and t.shape == shape:
+        st = t.stride()
+        if st[-1] == 1 or shape[-1] == 1:
+            return (t.data_ptr(), st[0], st[1]) if len(st) == 3 else (t.data_ptr(), 0, st[0])
+    _refuse(t, dtype, shape, dev, name, "have unit stride inside a row")
+
+
+def _dense(t: torch.Tensor, dtype, shape, dev: int, name: str) -> int:
+    if t.get_device() == dev and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(t, dtype, shape, dev, name, "be dense")
+
+
+def _pitched(t: torch.Tensor, dtype, shape, dev: int, name: str):
+    """(address, row pitch) of a matrix with unit inner stride."""
+    if t.get_device() == dev and t.dtype is dtype and t.shape == shape:
+        pitch, inner = t.stride()
+        if inner == 1 or shape[1] == 1:
+            return t.data_ptr(), pitch
+    _refuse(t, dtype, shape, dev, name, "have unit inner stride")
+
+
+def _scratch(t: Optional[torch.Tensor], dev: int):
+    if t is None:
+        return None, 0
+    if t.get_device() != dev or t.dtype is not torch.uint8:
+        _refuse(t, torch.uint8, t.shape, dev, "workspace", "be bytes")
+    return t.data_ptr(), t.numel()
+
+
+def _stream_of(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _rows_shape(t: torch.Tensor, name: str):
     shape = t.shape
     if len(shape) == 3:
-        return shape, shape[0], shape[1], shape[2]
+        return shape, *shape
     if len(shape) == 2:
-        return shape, 1, shape[0], shape[1]
+        return shape, 1, *shape
     raise TypeError(f"{name} must be [S, C] or [N, S, C]")
 
 
-def _gamma(t: Optional[torch.Tensor], dt, code: int, channels: int):
+def _gamma(t: Optional[torch.Tensor], dt, code: int, channels: int, dev: int):
     if t is None:
         return None, code
-    if t.dtype is not dt and t.dtype is not torch.float32:
-        raise TypeError(f"gamma must be {dt} or torch.float32, got {t.dtype}")
-    return _vector(t, t.dtype, channels, "gamma"), code if t.dtype is dt else F32
+    pt = t.dtype
+    if pt is not dt and pt is not torch.float32:
+        raise TypeError(f"gamma must be {dt} or torch.float32, got {pt}")
+    return _dense(t, pt, (channels,), dev, "gamma"), code if pt is dt else F32
 
 
 def dvdq_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], gamma: Optional[torch.Tensor], eps: float,
@@ -591,16 +617,17 @@ def dvdq_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], gamma: Opti
     dt = X.dtype
     code = _element_type(X, "X", _ANY_FLOAT)
     shape, N, S, channels = _rows_shape(X, "X")
-    _on_current_device(X, residual, gamma, H, Y, codes, scales, rstd)
-    x, xo, xr = _rows3(X, dt, shape, "X")
-    r, ro, rr = _rows3(residual, dt, shape, "residual")
-    h, ho, hr = _rows3(H, dt, shape, "H")
-    y, yo, yr = _rows3(Y, dt, shape, "Y")
-    c, co, cr = _rows3(codes, torch.int8, shape, "codes")
-    ga, param_code = _gamma(gamma, dt, code, channels)
-    _check(load().dvdq_rms_norm(x, xo, xr, r, ro, rr, N, S, channels, ga, param_code, eps, h, ho, hr, y, yo, yr, c, co, cr,
-                                _row_values(scales, shape, "scales"), _row_values(rstd, shape, "rstd"), code, _raw_stream(stream, X)),
-           "dvdq_rms_norm")
+    dev = _current(X, "X")
+    x, xo, xr = _rows3(X, dt, shape, dev, "X")
+    r, ro, rr = _rows3(residual, dt, shape, dev, "residual") if residual is not None else (None, 0, 0)
+    h, ho, hr = _rows3(H, dt, shape, dev, "H") if H is not None else (None, 0, 0)
+    y, yo, yr = _rows3(Y, dt, shape, dev, "Y") if Y is not None else (None, 0, 0)
+    c, co, cr = _rows3(codes, torch.int8, shape, dev, "codes") if codes is not None else (None, 0, 0)
+    s = _dense(scales, torch.float32, shape[:-1], dev, "scales") if scales is not None else None
+    q = _dense(rstd, torch.float32, shape[:-1], dev, "rstd") if rstd is not None else None
+    ga, param_code = _gamma(gamma, dt, code, channels, dev)
+    _check(load().dvdq_rms_norm(x, xo, xr, r, ro, rr, N, S, channels, ga, param_code, eps, h, ho, hr, y, yo, yr, c, co, cr, s, q, code,
+                                _stream_of(stream, dev)), "dvdq_rms_norm")
 
 
 def dvdq_rms_norm_backward_workspace_bytes(N: int, S: int, C_: int) -> int:
@@ -615,28 +642,30 @@ def dvdq_rms_norm_backward(dY: torch.Tensor, H: torch.Tensor, rstd: torch.Tensor
     dt = H.dtype
     code = _element_type(H, "H", _ANY_FLOAT)
     shape, N, S, channels = _rows_shape(H, "H")
-    _on_current_device(H, dY, rstd, gamma, dH, dX, dgamma, workspace)
-    d, do, dr = _rows3(dY, dt, shape, "dY")
-    h, ho, hr = _rows3(H, dt, shape, "H")
-    e, eo, er = _rows3(dH, dt, shape, "dH")
-    x, xo, xr = _rows3(dX, dt, shape, "dX")
-    ga, param_code = _gamma(gamma, dt, code, channels)
-    ws, room = _room(workspace)
-    _check(load().dvdq_rms_norm_backward(d, do, dr, h, ho, hr, _row_values(rstd, shape, "rstd"), e, eo, er, N, S, channels, ga, param_code,
-                                         x, xo, xr, _vector(dgamma, torch.float32, channels, "dgamma"), code, ws, room,
-                                         _raw_stream(stream, H)), "dvdq_rms_norm_backward")
+    dev = _current(H, "H")
+    h, ho, hr = _rows3(H, dt, shape, dev, "H")
+    d, do, dr = _rows3(dY, dt, shape, dev, "dY")
+    e, eo, er = _rows3(dH, dt, shape, dev, "dH") if dH is not None else (None, 0, 0)
+    x, xo, xr = _rows3(dX, dt, shape, dev, "dX") if dX is not None else (None, 0, 0)
+    q = _dense(rstd, torch.float32, shape[:-1], dev, "rstd")
+    ga, param_code = _gamma(gamma, dt, code, channels, dev)
+    dg = _dense(dgamma, torch.float32, (channels,), dev, "dgamma") if dgamma is not None else None
+    ws, room = _scratch(workspace, dev)
+    _check(load().dvdq_rms_norm_backward(d, do, dr, h, ho, hr, q, e, eo, er, N, S, channels, ga, param_code, x, xo, xr, dg, code, ws, room,
+                                         _stream_of(stream, dev)), "dvdq_rms_norm_backward")
 
 
 def dvdq_quantize_rows(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
     """codes int8 [M, K] = round(X / scale) with scale = max |row| / 127 (scales fp32 [M]): operands of dvdq_linear_int8."""
     code = _element_type(X, "X", _ANY_FLOAT)
-    if X.dim() != 2:
+    shape = X.shape
+    if len(shape) != 2:
         raise TypeError("X must be 2-D")
-    M, K = X.shape
-    _on_current_device(X, codes, scales)
-    x, ldx = _matrix(X, X.dtype, M, K, "X")
-    c, ldc = _matrix(codes, torch.int8, M, K, "codes")
-    _check(load().dvdq_quantize_rows(x, M, K, ldx, c, ldc, _row_values(scales, X.shape, "scales"), code, _raw_stream(stream, X)),
+    dev = _current(X, "X")
+    x, ldx = _pitched(X, X.dtype, shape, dev, "X")
+    c, ldc = _pitched(codes, torch.int8, shape, dev, "codes")
+    M, K = shape
+    _check(load().dvdq_quantize_rows(x, M, K, ldx, c, ldc, _dense(scales, torch.float32, (M,), dev, "scales"), code, _stream_of(stream, dev)),
            "dvdq_quantize_rows")
 
 
@@ -651,18 +680,20 @@ def dvdq_linear_int8(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w
     where that is 0."""
     dt = Y.dtype
     code = _element_type(Y, "Y", _HALF_FLOAT)
-    if A.dim() != 2 or W.dim() != 2:
-        raise TypeError("A and W must be 2-D")
-    (M, K), N = A.shape, W.shape[0]
-    _on_current_device(A, a_scales, W, w_scales, bias, residual, Y, workspace)
-    a, lda = _matrix(A, torch.int8, M, K, "A")
-    w, ldw = _matrix(W, torch.int8, N, K, "W")
-    r, ldr = _matrix(residual, dt, M, N, "residual")
-    y, ldy = _matrix(Y, dt, M, N, "Y")
-    ws, room = _room(workspace)
-    _check(load().dvdq_linear_int8(a, _vector(a_scales, torch.float32, M, "a_scales"), M, lda, w, _vector(w_scales, torch.float32, N, "w_scales"),
-                                   N, K, ldw, _vector(bias, dt, N, "bias"), r, ldr, act, y, ldy, code, ws, room, _raw_stream(stream, A)),
-           "dvdq_linear_int8")
+    a_shape, w_shape = A.shape, W.shape
+    if len(a_shape) != 2 or len(w_shape) != 2 or a_shape[1] != w_shape[1]:
+        raise TypeError(f"A and W must be [M, K] and [N, K], got {tuple(a_shape)} and {tuple(w_shape)}")
+    (M, K), N = a_shape, w_shape[0]
+    dev = _current(A, "A")
+    a, lda = _pitched(A, torch.int8, a_shape, dev, "A")
+    w, ldw = _pitched(W, torch.int8, w_shape, dev, "W")
+    y, ldy = _pitched(Y, dt, (M, N), dev, "Y")
+    r, ldr = _pitched(residual, dt, (M, N), dev, "residual") if residual is not None else (None, 0)
+    b = _dense(bias, dt, (N,), dev, "bias") if bias is not None else None
+    ws, room = _scratch(workspace, dev)
+    _check(load().dvdq_linear_int8(a, _dense(a_scales, torch.float32, (M,), dev, "a_scales"), M, lda, w,
+                                   _dense(w_scales, torch.float32, (N,), dev, "w_scales"), N, K, ldw, b, r, ldr, act, y, ldy, code, ws, room,
+                                   _stream_of(stream, dev)), "dvdq_linear_int8")
 
 
 # ------------------------------------------------------------------ test / debug entry points

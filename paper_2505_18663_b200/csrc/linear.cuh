@@ -707,7 +707,8 @@ inline double lin_cost(int64_t Md, int bn, int64_t kblocks, int64_t waves, doubl
 }
 inline double lin_memory_time(int64_t Md, int64_t Nd, int64_t Kc) { return ((double)Md + Nd) * Kc * 2.0 / 6.0e6; }
 
-inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* estimate = nullptr) {
+// per_piece: what each piece costs beyond that.
+inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* estimate = nullptr, double per_piece = 0.0) {
     const int64_t kb = ceil_div(Kc, kLinBK), num_m = ceil_div(Md, kLinTile);
     LinPlan p;
     p.bn = kLinTile;
@@ -720,7 +721,7 @@ inline LinPlan lin_plan(int64_t Md, int64_t Nd, int64_t Kc, int step, double* es
         for (int64_t s = 1; s <= 32 && s <= kb; ++s) {
             if (s > 1 && (tiles * s > 4 * kLinPairs || s * p.part_rows * p.part_pitch * 4 > ((int64_t)256 << 20))) break;
             double cost = lin_cost(Md, bn, ceil_div(kb, s), ceil_div(tiles * s, kLinPairs), lin_memory_time(Md, Nd, Kc));
-            if (s > 1) cost += 2.5 + (double)s * Md * Nd * 8.0 / 8.0e6;
+            if (s > 1) cost += 2.5 + s * per_piece + (double)s * Md * Nd * 8.0 / 8.0e6;
             if (cost < best * 0.97) { best = cost; p.bn = bn; p.splits = (int)s; }  // a wider tile reads less: prefer it when near
         }
     }

@@ -453,12 +453,19 @@ linear_int8_few_kernel(const int8_t* __restrict__ X, int64_t ldx, const int8_t* 
 
 // ------------------------------------------------------------------ host side
 
+// Epilogue blocks of 32 x 64 instead of 32 x 32 outputs with a residual, up to this many k-blocks (fewer copies, fewer operand stages): 32760 x K ->
+// 1536, K = 128, 512, 1024, 1536: 48.4, 55.4, 66.7, 90.7 us, in narrow blocks 57.4, 59.8, 74.7, 85.7.  Without a residual narrow ones are the faster from
+// 512 on (35 us, 38), and even below.
+constexpr int kL8WideMore = 8;
+
 struct L8Scales {
     const float *a, *w;
 };
 
-// Tile width and pieces along k: lin_plan's estimate, with k-blocks of 128 codes that take as long as its 64 16-bit values.
-inline LinPlan l8_plan(int64_t M, int64_t N, int64_t K) { return lin_plan(M, N, ceil_div(K, 2), 32); }
+// Tile width and pieces along k: lin_plan's estimate, with k-blocks of 128 codes that take as long as its 64 16-bit values.  Joining integer pieces
+// costs more than it says by about 0.3 us a piece (16 x 5120 -> 5120: 12.8 us in 3 pieces of 224-column tiles, 10.0 whole in 96-column ones; 100 x 8960 -> 1536:
+// 12.4 in 7 pieces, 10.4 in 3 or 4).
+inline LinPlan l8_plan(int64_t M, int64_t N, int64_t K) { return lin_plan(M, N, ceil_div(K, 2), 32, nullptr, 0.3); }
 
 inline bool l8_map(CUtensorMap* tm, CUtensorMapDataType type, const void* base, int64_t rows, int64_t cols, int64_t pitch_bytes, uint32_t box_cols,
                    uint32_t box_rows) {
@@ -535,11 +542,13 @@ static cudaError_t launch_linear_int8_few_w(const LinMatrix& x, const LinMatrix&
                         static_cast<const int8_t*>(w.p), w.ld, (int)M, (int)N, (int)K, per_warp, sc.a, sc.w, static_cast<const T*>(e.bias),
                         static_cast<const T*>(e.residual.p), e.residual.ld, e.act, static_cast<T*>(const_cast<void*>(y.p)), y.ld);
 }
+// Warps that share 16 channels, as launch_linear_few chooses them.  In us, KS = 2, 4, 8, 16: 1 token 5120 -> 13824 22.9, 16.0, 18.3, 17.8 (71 MB: 10.8 at the copy
+// rate); 5120 -> 5120 20.5, 12.0, 9.0, 10.2; 8960 -> 1536 34.6, 18.7, 10.8, 6.9; 3 tokens 1536 -> 1536 7.5, 4.3, 3.2, 3.0.
 template <typename T>
 static dvdq_status launch_linear_int8_few(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const L8Scales& sc,
                                           const LinEpilogue& e, const LinMatrix& y, cudaStream_t st) {
     const int64_t groups = ceil_div(N, 16), wave = 148 * 4 * 8;
-    if (groups <= 148 * 2 && K >= 2048) return cuda_status(launch_linear_int8_few_w<T, 16, 16>(x, w, M, N, K, sc, e, y, st));
+    if (groups <= 148 * 2 && K >= 1024) return cuda_status(launch_linear_int8_few_w<T, 16, 16>(x, w, M, N, K, sc, e, y, st));
     if (groups * 8 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 8>(x, w, M, N, K, sc, e, y, st));
     if (groups * 4 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 4>(x, w, M, N, K, sc, e, y, st));
     if (groups * 2 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 2>(x, w, M, N, K, sc, e, y, st));
@@ -551,6 +560,8 @@ static dvdq_status launch_linear_int8(const LinMatrix& a, const LinMatrix& w, in
                                       const L8Scales& sc, const LinEpilogue& e, const LinMatrix& y, int32_t* part, cudaStream_t st) {
     if (M <= kL8FewTokens) return launch_linear_int8_few<T>(a, w, M, N, K, sc, e, y, st);
     if (plan.splits == 1) {
+        // a tile is whole blocks for both warps
+        if (e.residual.p && plan.bn % 128 == 0 && ceil_div(K, kL8BK) <= kL8WideMore) return launch_linear_int8_out<T, kLinFinalMore, true>(a, w, M, N, K, plan, sc, e, y, part, st);
         if (e.residual.p) return launch_linear_int8_out<T, kLinFinalMore, false>(a, w, M, N, K, plan, sc, e, y, part, st);
         return launch_linear_int8_out<T, kLinFinal, false>(a, w, M, N, K, plan, sc, e, y, part, st);
     }
