@@ -134,7 +134,7 @@ dvdq_status dvdq_rms_norm_backward(const void* dY, int64_t dy_outer, int64_t dy_
                           : dtype == DVDQ_F16 ? launch_rms_norm_backward_f16(A, access, parts, &ctas, st)
                                               : launch_rms_norm_backward_f32(A, access, parts, &ctas, st);
     if (e != cudaSuccess || !dgamma) return cuda_status(e);
-    return cuda_status(launch_after(rms_norm_join_kernel, dim3((unsigned)ceil_div(C, 32)), dim3(kRmsJoinWarps * 32), 0, st, A.part, ctas, (int)C, dgamma));
+    return cuda_status(launch_after(rms_norm_join_kernel, dim3((unsigned)ceil_div(C, kJoinCols)), dim3(kJoinThreads), 0, st, A.part, ctas, (int)C, dgamma));
 }
 
 }  // extern "C"

@@ -58,6 +58,7 @@ struct RowValues {
             for (int i = 0; i < P; ++i) f(i, L.channel(i), v[i], Whole(), L.has(i));
             if (!FULL && V > 1 && L.tail) f(P, L.end(), end, Part(), true);
         } else {
+#pragma unroll 4
             for (int p = L.lane; p < L.whole; p += L.lanes) f(0, p * V, get<true>(p * V, L.C), Whole(), true);
             if (V > 1 && L.tail) f(0, L.end(), get<false>(L.end(), L.C), Part(), true);
         }
@@ -308,31 +309,35 @@ template <typename T, int V, int P, bool NORM, bool FULL, int ASK>
 static cudaError_t launch_rms_w(const RmsArgs& A, const RowsPlan& p, cudaStream_t st) {
     return p.wide ? launch_rms_p<T, V, P, NORM, true, FULL, ASK>(A, p, st) : launch_rms_p<T, V, P, NORM, false, FULL, ASK>(A, p, st);
 }
-template <typename T, int V, int P, bool NORM>
-static cudaError_t launch_rms_full(const RmsArgs& A, const RowsPlan& p, cudaStream_t st) {
+template <typename T, int V, int P, bool NORM, bool FULL>
+static cudaError_t launch_rms_ask(const RmsArgs& A, const RowsPlan& p, cudaStream_t st) {
     if constexpr (NORM) {
-        if (A.r.p && A.scales) return launch_rms_w<T, V, P, NORM, true, kAskBoth>(A, p, st);
-        if (A.r.p) return launch_rms_w<T, V, P, NORM, true, kAskResidual>(A, p, st);
-        if (A.scales) return launch_rms_w<T, V, P, NORM, true, kAskCodes>(A, p, st);
-        return launch_rms_w<T, V, P, NORM, true, kAskPlain>(A, p, st);
+        if (A.r.p && A.scales) return launch_rms_w<T, V, P, NORM, FULL, kAskBoth>(A, p, st);
+        if (A.r.p) return launch_rms_w<T, V, P, NORM, FULL, kAskResidual>(A, p, st);
+        if (A.scales) return launch_rms_w<T, V, P, NORM, FULL, kAskCodes>(A, p, st);
+        return launch_rms_w<T, V, P, NORM, FULL, kAskPlain>(A, p, st);
     }
-    return launch_rms_w<T, V, P, NORM, true, kAskCodes>(A, p, st);
+    return launch_rms_w<T, V, P, NORM, FULL, kAskCodes>(A, p, st);
 }
 template <typename T, int V, bool NORM>
 static cudaError_t launch_rms_v(const RmsArgs& A, cudaStream_t st) {
     constexpr bool kPieces16 = V * sizeof(T) == 16;
-    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0, 8, [](int k) { return rows_threads(V, k); });
+    // Pieces a thread, 4 and 5, 32760 x 5120: residual and codes 190 and 181 us, residual and y 209 and 225, y alone 144 and 118; 6 and more leave too few warps
+    // (267).  Rows whose pieces do not fill the threads: 8 (20000 x 1541, odd: 1, 2, 4, 8, 16 pieces 389, 183, 119, 94, 91 us).
+    static const int five[] = {5, 4, 6, 7, 8, 3, 2, 1, 0}, four[] = {4, 5, 6, 7, 8, 3, 2, 1, 0};
+    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0, 8, 8, 8, [](int k) { return rows_threads(V, k); },
+                                 A.r.p && !A.scales ? four : five);
     if constexpr (kPieces16) {
         if (p.full) {
             switch (p.pieces) {
-                case 1: return launch_rms_full<T, V, 1, NORM>(A, p, st);
-                case 2: return launch_rms_full<T, V, 2, NORM>(A, p, st);
-                case 3: return launch_rms_full<T, V, 3, NORM>(A, p, st);
-                case 4: return launch_rms_full<T, V, 4, NORM>(A, p, st);
-                case 5: return launch_rms_full<T, V, 5, NORM>(A, p, st);
-                case 6: return launch_rms_full<T, V, 6, NORM>(A, p, st);
-                case 7: return launch_rms_full<T, V, 7, NORM>(A, p, st);
-                default: return launch_rms_full<T, V, 8, NORM>(A, p, st);
+                case 1: return launch_rms_ask<T, V, 1, NORM, true>(A, p, st);
+                case 2: return launch_rms_ask<T, V, 2, NORM, true>(A, p, st);
+                case 3: return launch_rms_ask<T, V, 3, NORM, true>(A, p, st);
+                case 4: return launch_rms_ask<T, V, 4, NORM, true>(A, p, st);
+                case 5: return launch_rms_ask<T, V, 5, NORM, true>(A, p, st);
+                case 6: return launch_rms_ask<T, V, 6, NORM, true>(A, p, st);
+                case 7: return launch_rms_ask<T, V, 7, NORM, true>(A, p, st);
+                default: return launch_rms_ask<T, V, 8, NORM, true>(A, p, st);
             }
         }
     }
@@ -341,8 +346,8 @@ static cudaError_t launch_rms_v(const RmsArgs& A, cudaStream_t st) {
         case 0: return launch_rms_p<T, V, 0, NORM, true, false, ask>(A, p, st);
         case 1: return launch_rms_w<T, V, 1, NORM, false, ask>(A, p, st);
         case 2: return launch_rms_w<T, V, 2, NORM, false, ask>(A, p, st);
-        case 4: return launch_rms_w<T, V, 4, NORM, false, ask>(A, p, st);
-        default: return launch_rms_w<T, V, 8, NORM, false, ask>(A, p, st);
+        case 4: return launch_rms_ask<T, V, 4, NORM, false>(A, p, st);
+        default: return launch_rms_ask<T, V, 8, NORM, false>(A, p, st);
     }
 }
 // `access`: bytes of a piece that every tensor's alignment allows: 16, 4 or the element's

@@ -41,12 +41,14 @@ __device__ __forceinline__ Pairs<V> row_terms(const Pairs<V>& d, const Pairs<V>&
     }
     return t;
 }
-__host__ __device__ constexpr int rows_threads_backward(int V, int P) { return P * V > 16 ? 256 : P * V > 4 ? 512 : kRowThreads; }
+// Registers of a thread, and with them threads of a CTA at most.
+__host__ __device__ constexpr int rows_registers_backward(int V, int P) { return P * V > 40 ? 255 : P * V > 24 ? 168 : P * V > 8 ? 128 : 64; }
+__host__ __device__ constexpr int rows_threads_backward(int V, int P) { return 65536 / rows_registers_backward(V, P) / 32 * 32; }
 
 // A thread's channels are the same in every row that it meets, so dgamma's sums stay with it (P > 0: in registers; P = 0: in the CTA's own
 // row of `part`) until the CTA has been through its rows.  FULL: dX is asked for, and every thread has P whole pieces.
 template <typename T, int V, int P, bool WIDE, bool FULL>
-__global__ void __launch_bounds__(WIDE ? rows_threads_backward(V, P) : kSmallThreads)
+__global__ void __maxnreg__(rows_registers_backward(V, P))
 rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     constexpr int N = Pairs<V>::N, K = P > 0 ? P : 1, U = !WIDE && P > 0 && P <= 2 ? 2 : 1;
     constexpr bool KEEP = P > 0 && P * V <= 16;
@@ -106,6 +108,7 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
                 for (int i = 0; i < P; ++i) f(u, i, L.channel(i), Whole(), active[u] && L.has(i));
                 if (!FULL && V > 1 && L.tail && active[u]) f(u, P, L.end(), Part(), true);
             } else {
+#pragma unroll 2
                 for (int p = L.lane; p < L.whole; p += L.lanes) {
                     ask(u, 0, p * V, Whole(), true);
                     f(u, 0, p * V, Whole(), true);
@@ -177,24 +180,116 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     }
 }
 
-// dgamma from the CTAs' sums, in fp64 and in a fixed order: 32 channels a CTA, 16 warps share its rows.
-constexpr int kRmsJoinWarps = 16;
-static __global__ void __launch_bounds__(kRmsJoinWarps * 32) rms_norm_join_kernel(const float* __restrict__ part, int parts, int C, float* __restrict__ out) {
-    __shared__ double sh[kRmsJoinWarps][33];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+// Many rows of whole pieces, a CTA each: the next row's pieces are on their way (cp.async, into slots of shared memory that are a thread's own: no
+// barrier) while this one's two passes read theirs from there.  Held in registers instead, inputs and sums leave an SM 10 warps, with nothing
+// in flight while they compute: 32760 x 5120 266 us.
+// A slot is asked for again only after both passes' stores, whose values came from it, have been issued.
+__host__ __device__ constexpr int ring_registers(int P) { return P <= 3 ? 96 : P == 4 ? 128 : 80 + 16 * P; }
+__host__ __device__ constexpr int ring_threads(int P) { return 65536 / ring_registers(P) / 32 * 32; }
+template <typename T, int V, int P>
+__global__ void __maxnreg__(ring_registers(P))
+rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
+    constexpr int N = Pairs<V>::N;
+    __shared__ float2 slots[64];
+    extern __shared__ __align__(16) uint8_t ring[];
+    const int lanes = (int)blockDim.x, lane = (int)threadIdx.x, C = A.shape.C;
+    const RowLanes<V, P, true> L(C, lanes, lane);
+    RowMeet<true> meet(slots, lanes);
+    Pairs<V> acc[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[i].p[j] = 0ull;
+    const bool with_dh = A.dh.p != nullptr;
+    const uint32_t step = (uint32_t)lanes * 16u, stage_bytes = (with_dh ? 3u : 2u) * P * step, mine = smem_u32(ring) + (uint32_t)lane * 16u;
+    auto ask = [&](int64_t row, uint32_t stage) {
+        if (row < A.shape.rows) {
+            const uint32_t n = A.shape.by_s((uint32_t)row), s = (uint32_t)row - n * (uint32_t)A.shape.S;
+            uint32_t to = mine + stage * stage_bytes;
+            auto copy = [&](const RowsOf& t) {
+                const T* from = static_cast<const T*>(t.p) + row_at(t, n, s) + L.channel(0);
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * step), "l"(from + (int64_t)i * lanes * V) : "memory");
+                to += P * step;
+            };
+            copy(A.dy);
+            copy(A.h);
+            if (with_dh) copy(A.dh);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    wait_predecessor();
+    release_successor();
+    RowGamma<T, V, P, true, true> gamma;
+    gamma.init(L, A.gamma, A.params_f32);
+    int64_t row = blockIdx.x;
+    uint32_t stage = 0;
+    ask(row, 0u);
+    float q_next = A.rstd[row];
+    for (; row < A.shape.rows; row += gridDim.x, stage ^= 1u) {
+        const float q = q_next;
+        ask(row + gridDim.x, stage ^ 1u);
+        if (row + gridDim.x < A.shape.rows) q_next = A.rstd[row + gridDim.x];
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        const uint32_t at = mine + stage * stage_bytes;
+        uint64_t sum = 0ull;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            Piece<T, V> d, h;
+            d.load_shared(at + i * step);
+            h.load_shared(at + (P + i) * step);
+            add_to<V>(acc[i], row_terms<V>(d.wide(), h.wide(), gamma.template get<true>(i, L.channel(i)), q, sum));
+        }
+        float s0, s1;
+        f2_unpack(sum, s0, s1);
+        const float mean = meet(s0 + s1, 0.f, false).x * A.inv_c;
+        const uint32_t n = A.shape.by_s((uint32_t)row), s = (uint32_t)row - n * (uint32_t)A.shape.S;
+        T* dx = static_cast<T*>(A.dx.p) + row_at(A.dx, n, s);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            Piece<T, V> d, h, e;
+            d.load_shared(at + i * step);
+            h.load_shared(at + (P + i) * step);
+            Pairs<V> o = row_gradient<V>(d.wide(), h.wide(), gamma.template get<true>(i, L.channel(i)), q, mean);
+            if (with_dh) {
+                e.load_shared(at + (2 * P + i) * step);
+                add_to<V>(o, e.wide());
+            }
+            row_store<T, V, true>(dx, L.channel(i), C, o, true);
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (!A.part) return;
+    float* to = A.part + (int64_t)blockIdx.x * C;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) to[L.channel(i) + j] = acc[i].get(j);
+}
+
+// dgamma from the CTAs' sums, in fp64 and in a fixed order: 8 channels a CTA, 128 threads share the rows of sums of each (with 16 warps for 32 channels,
+// 592 rows of 128 sums took 6 us longer: too few loads in flight).
+constexpr int kJoinThreads = 1024, kJoinCols = 8;
+static __global__ void __launch_bounds__(kJoinThreads) rms_norm_join_kernel(const float* __restrict__ part, int parts, int C, float* __restrict__ out) {
+    __shared__ double sh[kJoinThreads / 32][kJoinCols];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * kJoinCols + (lane & (kJoinCols - 1));
     wait_predecessor();
     release_successor();
     double t = 0.0;
     if (c < C) {
-#pragma unroll 8
-        for (int i = w; i < parts; i += kRmsJoinWarps) t += part[(int64_t)i * C + c];
+#pragma unroll 4
+        for (int i = threadIdx.x / kJoinCols; i < parts; i += kJoinThreads / kJoinCols) t += part[(int64_t)i * C + c];
     }
-    sh[w][lane] = t;
+    t += __shfl_xor_sync(0xFFFFFFFFu, t, 8);
+    t += __shfl_xor_sync(0xFFFFFFFFu, t, 16);
+    if (lane < kJoinCols) sh[w][lane] = t;
     __syncthreads();
-    if (w == 0 && c < C) {
+    if (w < kJoinCols) {  // a warp for each channel
+        t = sh[lane][w];
 #pragma unroll
-        for (int i = 1; i < kRmsJoinWarps; ++i) t += sh[i][lane];
-        out[c] = (float)t;
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+        if (lane == 0 && blockIdx.x * kJoinCols + w < C) out[blockIdx.x * kJoinCols + w] = (float)t;
     }
 }
 static __global__ void __launch_bounds__(256) rms_norm_no_rows_kernel(float* __restrict__ dgamma, int C) {
@@ -237,10 +332,52 @@ template <typename T, int V, int P, bool FULL>
 static cudaError_t launch_rms_backward_w(const RmsBackwardArgs& A, const RowsPlan& p, int64_t parts, int* ctas, cudaStream_t st) {
     return p.wide ? launch_rms_backward_p<T, V, P, true, FULL>(A, p, parts, ctas, st) : launch_rms_backward_p<T, V, P, false, FULL>(A, p, parts, ctas, st);
 }
+constexpr int kRingRoom = 216 * 1024;  // of an SM's shared memory, for its CTAs' rings
+// The ring's plan: a thread's pieces such that they fill a CTA, or 0.
+inline int ring_pieces(int64_t rows, int64_t nv, int tensors) {
+    if (rows < 148 * 4 || 2 * tensors * nv * 16 > kRingRoom) return 0;
+    static const int order[] = {2, 4, 3, 5, 6, 7, 8, 0};
+    for (const int* k = order; *k; ++k) {
+        if (nv % (32 * *k) == 0 && nv / *k >= 64 && nv / *k <= ring_threads(*k)) return *k;
+    }
+    return 0;
+}
+template <typename T, int V, int P>
+static cudaError_t launch_rms_backward_ring(const RmsBackwardArgs& A, int64_t parts, int* ctas_out, cudaStream_t st) {
+    const int threads = A.shape.C / (V * P), smem = 2 * (A.dh.p ? 3 : 2) * P * threads * 16;
+    auto kern = rms_norm_backward_ring_kernel<T, V, P>;
+    static PerDevice<int> ready;
+    if (!ready.get([&](int&, int) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingRoom) == cudaSuccess; }))
+        return cudaErrorInvalidValue;
+    int held = kRingRoom / (smem + 1536);                                   // 1 KB that the system takes, and the slots
+    const int by_registers = 65536 / (ring_registers(P) * threads);
+    if (held > by_registers) held = by_registers;
+    if (held < 1) held = 1;
+    int64_t ctas = A.shape.rows < 148 * held ? A.shape.rows : 148 * held;
+    if (A.part && ctas > parts) ctas = parts;
+    *ctas_out = (int)ctas;
+    return launch_after(kern, dim3((unsigned)ctas), dim3(threads), (size_t)smem, st, A);
+}
 template <typename T, int V>
 static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts, int* ctas, cudaStream_t st) {
     constexpr bool kPieces16 = V * sizeof(T) == 16;
-    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0 && A.dx.p, 8, [](int k) { return rows_threads_backward(V, k); });
+    if constexpr (kPieces16) {
+        const int pieces = A.dx.p && A.shape.C % V == 0 ? ring_pieces(A.shape.rows, A.shape.C / V, A.dh.p ? 3 : 2) : 0;
+        switch (pieces) {
+            case 0: break;
+            case 2: return launch_rms_backward_ring<T, V, 2>(A, parts, ctas, st);
+            case 3: return launch_rms_backward_ring<T, V, 3>(A, parts, ctas, st);
+            case 4: return launch_rms_backward_ring<T, V, 4>(A, parts, ctas, st);
+            case 5: return launch_rms_backward_ring<T, V, 5>(A, parts, ctas, st);
+            case 6: return launch_rms_backward_ring<T, V, 6>(A, parts, ctas, st);
+            case 7: return launch_rms_backward_ring<T, V, 7>(A, parts, ctas, st);
+            default: return launch_rms_backward_ring<T, V, 8>(A, parts, ctas, st);
+        }
+    }
+    // Rows whose pieces do not fill the threads: 4 (20000 x 1541, odd: 1, 2, 4, 8 pieces 478, 196, 119, 186 us; 30000 x 2049 fp32 666, 665, 333, 368).
+    static const int order[] = {5, 3, 4, 2, 6, 7, 8, 1, 0};
+    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0 && A.dx.p, 2, 8, 4,
+                                 [](int k) { return rows_threads_backward(V, k); }, order);
     if constexpr (kPieces16) {
         if (p.full) {
             switch (p.pieces) {
@@ -260,7 +397,7 @@ static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts
         case 1: return launch_rms_backward_w<T, V, 1, false>(A, p, parts, ctas, st);
         case 2: return launch_rms_backward_w<T, V, 2, false>(A, p, parts, ctas, st);
         case 4: return launch_rms_backward_w<T, V, 4, false>(A, p, parts, ctas, st);
-        default: return launch_rms_backward_w<T, V, 8, false>(A, p, parts, ctas, st);
+        default: return cudaErrorInvalidValue;  // not reached
     }
 }
 template <typename T>

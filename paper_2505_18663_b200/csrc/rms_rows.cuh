@@ -267,15 +267,16 @@ struct RowsPlan {
     int lanes, lanes_log2, threads, pieces;  // pieces 0: the row is read again instead of kept
     bool wide, full;
 };
-// Pieces a thread that the kernels are built for, in CTAs (wide) or in lanes of a warp: 1, 2, 4, 8, and where they fill the threads 3, 5, 6, 7 too.
+// Pieces a thread that the kernels are built for: 1, 2, 4, 8, and where they fill the threads 3, 5, 6, 7 too.
 constexpr int rows_pieces(int64_t k) { return k <= 2 ? (int)k : k <= 4 ? 4 : 8; }
-// How `rows` rows of nv pieces are laid over threads that keep up to `most` pieces each, in CTAs of up to limit(pieces) threads.  `whole`: nothing is left
-// of the row behind its pieces.
+// How `rows` rows of nv pieces are laid over threads that keep up to `most` pieces each (`warp_most` in rows of a warp, ragged_most where pieces do not
+// fill the threads), in CTAs of up to limit(pieces) threads.  `whole`: nothing is left of the row behind its pieces; `order`: which numbers of pieces to try
+// then.
 template <typename Limit>
-inline RowsPlan rows_plan(int64_t rows, int64_t nv, bool whole, int most, Limit limit) {
+inline RowsPlan rows_plan(int64_t rows, int64_t nv, bool whole, int warp_most, int most, int ragged_most, Limit limit, const int* order) {
     RowsPlan p = {};
     const bool few = rows < 148 * 2;
-    if (nv <= 64 || (nv <= 32 * most && !few && rows >= 148 * 8)) {  // a warp or part of it
+    if (nv <= 64 || (nv <= 32 * warp_most && !few && rows >= 148 * 8)) {  // a warp or part of it
         p.lanes_log2 = 5;
         while (p.lanes_log2 > 0 && nv <= 1 << p.lanes_log2) --p.lanes_log2;  // two pieces a thread, where there are two
         p.lanes = 1 << p.lanes_log2;
@@ -286,17 +287,20 @@ inline RowsPlan rows_plan(int64_t rows, int64_t nv, bool whole, int most, Limit 
         return p;
     }
     p.wide = true;
-    // a CTA whose threads all have as many pieces: four to `most` (few rows: as few as there can be)
-    for (int k = few ? 1 : most < 4 ? most : 4; whole && k <= most; ++k)
-        if (nv % (32 * k) == 0 && nv / k >= 64 && nv / k <= limit(k)) {
-            p.pieces = k;
-            p.lanes = p.threads = (int)(nv / k);
+    // a CTA whose threads all have as many pieces (few rows: as few as there can be)
+    static const int up[] = {1, 2, 3, 4, 5, 6, 7, 8, 0};
+    for (const int* k = few ? up : order; whole && *k; ++k) {
+        if (*k <= most && nv % (32 * *k) == 0 && nv / *k >= 64 && nv / *k <= limit(*k)) {
+            p.pieces = *k;
+            p.lanes = p.threads = (int)(nv / *k);
             p.full = true;
             return p;
         }
-    for (int k = few ? 1 : most < 4 ? most : 4; k <= most; k *= 2) {
+    }
+    // otherwise as many as leave two warps
+    for (int k = few ? 1 : ragged_most; k >= 1 && k <= ragged_most; k = few ? k * 2 : k / 2) {
         const int64_t threads = align_up(ceil_div(nv, k), 32);
-        if (threads > limit(k)) continue;
+        if (threads > limit(k) || (!few && threads < 64 && k > 1)) continue;
         p.pieces = k;
         p.lanes = p.threads = (int)(threads < 64 ? 64 : threads);
         return p;
