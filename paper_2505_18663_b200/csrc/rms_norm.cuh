@@ -38,10 +38,10 @@ __device__ __forceinline__ float bring_to_one(float v) {
 }
 
 // A row in registers (P > 0), or loaded from memory at each visit (P = 0).
-template <typename T, int V, int P, bool FULL>
+template <typename T, int V, int P, int KIND>
 struct RowValues {
     static constexpr int K = P > 0 ? P : 1;
-    using Lanes = RowLanes<V, P, FULL>;
+    using Lanes = RowLanes<V, P, KIND>;
     Pairs<V> v[K], end;
     const T *x, *r;
     template <bool WHOLE>
@@ -56,7 +56,7 @@ struct RowValues {
         if constexpr (P > 0) {
 #pragma unroll
             for (int i = 0; i < P; ++i) f(i, L.channel(i), v[i], Whole(), L.has(i));
-            if (!FULL && V > 1 && L.tail) f(P, L.end(), end, Part(), true);
+            if (!Lanes::FULL && V > 1 && L.tail) f(P, L.end(), end, Part(), true);
         } else {
 #pragma unroll 4
             for (int p = L.lane; p < L.whole; p += L.lanes) f(0, p * V, get<true>(p * V, L.C), Whole(), true);
@@ -65,8 +65,8 @@ struct RowValues {
     }
 };
 // U rows' loads, all of them before the first is used.
-template <typename T, int V, int P, bool FULL, int U>
-__device__ __forceinline__ void rows_load(const RowLanes<V, P, FULL>& L, RowValues<T, V, P, FULL> (&rows)[U], const bool (&active)[U], bool both) {
+template <typename T, int V, int P, int KIND, int U>
+__device__ __forceinline__ void rows_load(const RowLanes<V, P, KIND>& L, RowValues<T, V, P, KIND> (&rows)[U], const bool (&active)[U], bool both) {
     if constexpr (P > 0) {
         Piece<T, V> a[U][P], b[U][P];
 #pragma unroll
@@ -87,7 +87,7 @@ __device__ __forceinline__ void rows_load(const RowLanes<V, P, FULL>& L, RowValu
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!FULL && V > 1 && L.tail) rows[u].end = rows[u].template get<false>(L.end(), active[u] ? L.C : 0);
+            if (!L.FULL && V > 1 && L.tail) rows[u].end = rows[u].template get<false>(L.end(), active[u] ? L.C : 0);
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 rows[u].v[i] = a[u][i].wide();
@@ -164,9 +164,9 @@ __device__ __forceinline__ RowScale row_far(const RmsArgs& A, const Lanes& L, co
 }
 
 // The row's q and top.  CODES: whether the output in 8 bits is asked for.
-template <bool NORM, bool WIDE, typename T, int V, int P, bool FULL, bool KEEP>
-__device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes<V, P, FULL>& L, RowValues<T, V, P, FULL>& row,
-                                               const RowGamma<T, V, P, FULL, KEEP>& gamma, RowMeet<WIDE>& meet, bool codes) {
+template <bool NORM, bool WIDE, typename T, int V, int P, int KIND, bool KEEP>
+__device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes<V, P, KIND>& L, RowValues<T, V, P, KIND>& row,
+                                               const RowGamma<T, V, P, KIND, KEEP>& gamma, RowMeet<WIDE>& meet, bool codes) {
     constexpr int N = Pairs<V>::N;
     uint64_t sum = 0ull;
     float top = 0.f;
@@ -198,9 +198,9 @@ __device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes<
     return o;
 }
 
-template <bool NORM, typename T, int V, int P, bool FULL, bool KEEP>
-__device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P, FULL>& L, RowValues<T, V, P, FULL>& row,
-                                          const RowGamma<T, V, P, FULL, KEEP>& gamma, const RowScale& o, uint32_t index, uint32_t n, uint32_t s, bool codes) {
+template <bool NORM, typename T, int V, int P, int KIND, bool KEEP>
+__device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P, KIND>& L, RowValues<T, V, P, KIND>& row,
+                                          const RowGamma<T, V, P, KIND, KEEP>& gamma, const RowScale& o, uint32_t index, uint32_t n, uint32_t s, bool codes) {
     constexpr int N = Pairs<V>::N;
     const int C = A.shape.C;
     if (NORM && A.rstd && L.lane == 0) A.rstd[index] = o.q * o.f;
@@ -243,9 +243,12 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P,
     });
 }
 
-// Rows that a thread has in hand at once, and threads of a CTA at most: what its registers hold.
+// Rows that a thread has in hand at once.
 __host__ __device__ constexpr int rows_at_once(int P) { return P == 1 ? 4 : P == 2 ? 2 : 1; }
-__host__ __device__ constexpr int rows_threads(int V, int P) { return P * V > 24 ? 256 : P * V > 8 ? 512 : kRowThreads; }
+// Registers of a thread of a wide row, and with them threads of a CTA at most.  (Given a number of threads instead, the compiler spills to 80 registers for an occupancy
+// that is of no use: 32760 x 5120 with residual and y 228 us.)
+__host__ __device__ constexpr int rows_registers(int V, int P) { return P * V > 40 ? 128 : P * V > 24 ? 112 : P * V > 8 ? 96 : 64; }
+__host__ __device__ constexpr int rows_threads(int V, int P) { return 65536 / rows_registers(V, P) / 32 * 32; }
 
 // What a call asks for, as far as kernels are built for it (each branch of an inner loop costs as much as a piece's arithmetic): a
 // residual, codes; else all is looked up at run time.
@@ -253,23 +256,23 @@ enum RowsAsk { kAskAny = 0, kAskPlain = 1, kAskResidual = 2, kAskCodes = 3, kAsk
 
 // WIDE: a row has the CTA to itself.
 template <typename T, int V, int P, bool NORM, bool WIDE, bool FULL, int ASK>
-__global__ void __launch_bounds__(WIDE ? rows_threads(V, P) : kSmallThreads)
-rms_norm_kernel(const __grid_constant__ RmsArgs A) {
+__device__ __forceinline__ void rms_norm_rows(const RmsArgs& A) {
     constexpr int U = WIDE ? 1 : rows_at_once(P);
     constexpr bool KEEP = NORM && P > 0 && P * V <= 40;
+    constexpr int KIND = (FULL ? kFull : 0) | (WIDE ? kWide : 0);
     const bool both = ASK == kAskAny ? A.r.p != nullptr : ASK == kAskResidual || ASK == kAskBoth;
     const bool codes = !NORM || (ASK == kAskAny ? A.scales != nullptr : ASK == kAskCodes || ASK == kAskBoth);
     __shared__ float2 slots[64];
     const int lanes = WIDE ? (int)blockDim.x : A.lanes, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
     const int groups = WIDE ? 1 : kSmallThreads >> A.lanes_log2, group = WIDE ? 0 : (int)threadIdx.x >> A.lanes_log2;
-    const RowLanes<V, P, FULL> L(A.shape.C, lanes, lane);
+    const RowLanes<V, P, KIND> L(A.shape.C, lanes, lane);
     RowMeet<WIDE> meet(slots, lanes);
     wait_predecessor();
     release_successor();
-    RowGamma<T, V, P, FULL, KEEP> gamma;
+    RowGamma<T, V, P, KIND, KEEP> gamma;
     if (NORM) gamma.init(L, A.gamma, A.params_f32);
     for (int64_t at = (int64_t)blockIdx.x * (groups * U); at < A.shape.rows; at += (int64_t)gridDim.x * (groups * U)) {
-        RowValues<T, V, P, FULL> rows[U];
+        RowValues<T, V, P, KIND> rows[U];
         uint32_t index[U], n[U], s[U];
         bool active[U];
 #pragma unroll
@@ -282,13 +285,24 @@ rms_norm_kernel(const __grid_constant__ RmsArgs A) {
             rows[u].x = static_cast<const T*>(A.x.p) + row_at(A.x, n[u], s[u]);
             rows[u].r = both ? static_cast<const T*>(A.r.p) + row_at(A.r, n[u], s[u]) : nullptr;
         }
-        rows_load<T, V, P, FULL, U>(L, rows, active, both);
+        rows_load<T, V, P, KIND, U>(L, rows, active, both);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const RowScale o = row_decide<NORM>(A, L, rows[u], gamma, meet, codes);
             if (active[u]) row_write<NORM>(A, L, rows[u], gamma, o, index[u], n[u], s[u], codes);
         }
     }
+}
+
+template <typename T, int V, int P, bool NORM, bool FULL, int ASK>
+__global__ void __maxnreg__(rows_registers(V, P))
+rms_norm_wide_kernel(const __grid_constant__ RmsArgs A) {
+    rms_norm_rows<T, V, P, NORM, true, FULL, ASK>(A);
+}
+template <typename T, int V, int P, bool NORM, bool FULL, int ASK>
+__global__ void __launch_bounds__(kSmallThreads)
+rms_norm_kernel(const __grid_constant__ RmsArgs A) {
+    rms_norm_rows<T, V, P, NORM, false, FULL, ASK>(A);
 }
 
 // ------------------------------------------------------------------ launches
@@ -298,7 +312,9 @@ static cudaError_t launch_rms_p(const RmsArgs& A0, const RowsPlan& p, cudaStream
     RmsArgs A = A0;
     A.lanes = p.lanes;
     A.lanes_log2 = p.lanes_log2;
-    auto kern = rms_norm_kernel<T, V, P, NORM, WIDE, FULL, ASK>;
+    void (*kern)(RmsArgs);
+    if constexpr (WIDE) kern = rms_norm_wide_kernel<T, V, P, NORM, FULL, ASK>;
+    else kern = rms_norm_kernel<T, V, P, NORM, FULL, ASK>;
     static PerDevice<RowsHeld> cache;
     const int held = rows_held(cache, kern, p.threads);
     if (held == 0) return cudaErrorInvalidValue;

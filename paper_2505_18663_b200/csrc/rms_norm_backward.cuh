@@ -52,13 +52,14 @@ __global__ void __maxnreg__(rows_registers_backward(V, P))
 rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     constexpr int N = Pairs<V>::N, K = P > 0 ? P : 1, U = !WIDE && P > 0 && P <= 2 ? 2 : 1;
     constexpr bool KEEP = P > 0 && P * V <= 16;
+    constexpr int KIND = (FULL ? kFull : 0) | (WIDE ? kWide : 0);
     __shared__ float2 slots[64];
     extern __shared__ float joined[];
     const int lanes = WIDE ? (int)blockDim.x : A.lanes, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
     const int groups = WIDE ? 1 : kSmallThreads >> A.lanes_log2, group = WIDE ? 0 : (int)threadIdx.x >> A.lanes_log2;
     const int C = A.shape.C;
     const bool with_dx = FULL || A.dx.p != nullptr, with_dh = with_dx && A.dh.p != nullptr;
-    const RowLanes<V, P, FULL> L(C, lanes, lane);
+    const RowLanes<V, P, KIND> L(C, lanes, lane);
     RowMeet<WIDE> meet(slots, lanes);
     Pairs<V> acc[K + 1];
 #pragma unroll
@@ -68,7 +69,7 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     float* mine = A.part ? A.part + (int64_t)blockIdx.x * C : nullptr;
     wait_predecessor();
     release_successor();
-    RowGamma<T, V, P, FULL, KEEP> gamma;
+    RowGamma<T, V, P, KIND, KEEP> gamma;
     gamma.init(L, A.gamma, A.params_f32);
     bool first = true;
     for (int64_t at = (int64_t)blockIdx.x * (groups * U); at < A.shape.rows; at += (int64_t)gridDim.x * (groups * U)) {
@@ -193,7 +194,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
     __shared__ float2 slots[64];
     extern __shared__ __align__(16) uint8_t ring[];
     const int lanes = (int)blockDim.x, lane = (int)threadIdx.x, C = A.shape.C;
-    const RowLanes<V, P, true> L(C, lanes, lane);
+    const RowLanes<V, P, kFull | kWide> L(C, lanes, lane);
     RowMeet<true> meet(slots, lanes);
     Pairs<V> acc[P];
 #pragma unroll
@@ -201,7 +202,9 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[i].p[j] = 0ull;
     const bool with_dh = A.dh.p != nullptr;
-    const uint32_t step = (uint32_t)lanes * 16u, stage_bytes = (with_dh ? 3u : 2u) * P * step, mine = smem_u32(ring) + (uint32_t)lane * 16u;
+    // a tensor's pieces as they lie in the row: a thread's are 512 bytes apart
+    constexpr uint32_t step = 512u;
+    const uint32_t tensor = (uint32_t)(P * lanes) * 16u, stage_bytes = (with_dh ? 3u : 2u) * tensor, mine = smem_u32(ring) + (uint32_t)L.first * 16u;
     auto ask = [&](int64_t row, uint32_t stage) {
         if (row < A.shape.rows) {
             const uint32_t n = A.shape.by_s((uint32_t)row), s = (uint32_t)row - n * (uint32_t)A.shape.S;
@@ -210,8 +213,8 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
                 const T* from = static_cast<const T*>(t.p) + row_at(t, n, s) + L.channel(0);
 #pragma unroll
                 for (int i = 0; i < P; ++i)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * step), "l"(from + (int64_t)i * lanes * V) : "memory");
-                to += P * step;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * step), "l"(from + i * (32 * V)) : "memory");
+                to += tensor;
             };
             copy(A.dy);
             copy(A.h);
@@ -221,7 +224,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
     };
     wait_predecessor();
     release_successor();
-    RowGamma<T, V, P, true, true> gamma;
+    RowGamma<T, V, P, kFull | kWide, true> gamma;
     gamma.init(L, A.gamma, A.params_f32);
     int64_t row = blockIdx.x;
     uint32_t stage = 0;
@@ -238,7 +241,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
         for (int i = 0; i < P; ++i) {
             Piece<T, V> d, h;
             d.load_shared(at + i * step);
-            h.load_shared(at + (P + i) * step);
+            h.load_shared(at + tensor + i * step);
             add_to<V>(acc[i], row_terms<V>(d.wide(), h.wide(), gamma.template get<true>(i, L.channel(i)), q, sum));
         }
         float s0, s1;
@@ -250,10 +253,10 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
         for (int i = 0; i < P; ++i) {
             Piece<T, V> d, h, e;
             d.load_shared(at + i * step);
-            h.load_shared(at + (P + i) * step);
+            h.load_shared(at + tensor + i * step);
             Pairs<V> o = row_gradient<V>(d.wide(), h.wide(), gamma.template get<true>(i, L.channel(i)), q, mean);
             if (with_dh) {
-                e.load_shared(at + (2 * P + i) * step);
+                e.load_shared(at + 2 * tensor + i * step);
                 add_to<V>(o, e.wide());
             }
             row_store<T, V, true>(dx, L.channel(i), C, o, true);

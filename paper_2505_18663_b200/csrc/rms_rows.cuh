@@ -220,25 +220,31 @@ struct RowMeet {
     }
 };
 
-// The pieces of a row that a thread has: whole ones (lane + i lanes, i < P), and behind the last of them, where V does not divide C, the row's end.
-// FULL: every thread has P whole pieces, and that is the row.
-template <int V, int P, bool FULL>
+// The pieces of a row that a thread has: P whole ones, and, where V does not divide C, one thread the row's end.  KIND: kFull (every thread has P whole
+// pieces, and that is the row), kWide (a CTA's row: each warp has 32 P neighbouring pieces, so that a thread's addresses differ by constants; with
+// the CTA's width between them, odd rows of 1541 took 94 us instead of 71).
+enum RowKind { kRagged = 0, kFull = 1, kWide = 2 };
+template <int V, int P, int KIND>
 struct RowLanes {
+    static constexpr bool FULL = (KIND & kFull) != 0, WIDE = (KIND & kWide) != 0;
     int C, lanes, lane, whole;  // whole pieces of the row
+    int first;                  // this thread's first
     bool tail;                  // whether this thread has its end
     __device__ __forceinline__ RowLanes(int channels, int n, int l) : C(channels), lanes(n), lane(l) {
         whole = channels / V;
+        first = WIDE && P > 0 ? (l >> 5) * (32 * P) + (l & 31) : l;
         tail = !FULL && V > 1 && channels % V != 0 && whole % n == l;
     }
-    __device__ __forceinline__ bool has(int i) const { return FULL || lane + i * lanes < whole; }
-    __device__ __forceinline__ int channel(int i) const { return (lane + i * lanes) * V; }
+    __device__ __forceinline__ int piece(int i) const { return first + i * (WIDE ? 32 : lanes); }
+    __device__ __forceinline__ bool has(int i) const { return FULL || piece(i) < whole; }
+    __device__ __forceinline__ int channel(int i) const { return piece(i) * V; }
     __device__ __forceinline__ int end() const { return whole * V; }
 };
 // gamma of a thread's channels: kept (KEEP), or loaded where it is needed
-template <typename T, int V, int P, bool FULL, bool KEEP>
+template <typename T, int V, int P, int KIND, bool KEEP>
 struct RowGamma {
     static constexpr int K = KEEP ? P : 0;
-    using Lanes = RowLanes<V, P, FULL>;
+    using Lanes = RowLanes<V, P, KIND>;
     Pairs<V> g[K + 1], end;
     const void* p;
     int f32, C;
@@ -277,26 +283,36 @@ inline RowsPlan rows_plan(int64_t rows, int64_t nv, bool whole, int warp_most, i
     RowsPlan p = {};
     const bool few = rows < 148 * 2;
     if (nv <= 64 || (nv <= 32 * warp_most && !few && rows >= 148 * 8)) {  // a warp or part of it
+        p.threads = kSmallThreads;
+        // lanes that have as many pieces each, two to `warp_most` (12 pieces of 96 channels: four lanes with three; eight with up to two took 55 us for
+        // 32760 x 12 heads, 16 bytes of each)
+        for (p.lanes_log2 = 5; whole && p.lanes_log2 >= 0; --p.lanes_log2) {
+            const int64_t k = nv >> p.lanes_log2;
+            if (k << p.lanes_log2 == nv && (k >= 2 || nv == 1) && k <= (warp_most < 5 ? 5 : warp_most)) {
+                p.lanes = 1 << p.lanes_log2;
+                p.pieces = (int)k;
+                p.full = true;
+                return p;
+            }
+        }
         p.lanes_log2 = 5;
         while (p.lanes_log2 > 0 && nv <= 1 << p.lanes_log2) --p.lanes_log2;  // two pieces a thread, where there are two
         p.lanes = 1 << p.lanes_log2;
-        p.threads = kSmallThreads;
-        p.pieces = (int)ceil_div(nv, p.lanes);
-        p.full = whole && nv == (int64_t)p.pieces * p.lanes;
-        if (!p.full) p.pieces = rows_pieces(p.pieces);
+        p.pieces = rows_pieces(ceil_div(nv, p.lanes));
         return p;
     }
     p.wide = true;
-    // a CTA whose threads all have as many pieces (few rows: as few as there can be)
+    // a CTA whose threads all have as many pieces (few rows: as few as there can be; many: up to 256 threads if possible, so that the CTAs of an SM wait for
+    // their barriers by turns: 10000 rows of 16384 202 us in 256 threads, 217 in 512)
     static const int up[] = {1, 2, 3, 4, 5, 6, 7, 8, 0};
-    for (const int* k = few ? up : order; whole && *k; ++k) {
-        if (*k <= most && nv % (32 * *k) == 0 && nv / *k >= 64 && nv / *k <= limit(*k)) {
-            p.pieces = *k;
-            p.lanes = p.threads = (int)(nv / *k);
-            p.full = true;
-            return p;
-        }
-    }
+    for (int cap = few ? kRowThreads : 256; whole && cap <= kRowThreads; cap *= 4)
+        for (const int* k = few ? up : order; *k; ++k)
+            if (*k <= most && nv % (32 * *k) == 0 && nv / *k >= 64 && nv / *k <= cap && nv / *k <= limit(*k)) {
+                p.pieces = *k;
+                p.lanes = p.threads = (int)(nv / *k);
+                p.full = true;
+                return p;
+            }
     // otherwise as many as leave two warps
     for (int k = few ? 1 : ragged_most; k >= 1 && k <= ragged_most; k = few ? k * 2 : k / 2) {
         const int64_t threads = align_up(ceil_div(nv, k), 32);
