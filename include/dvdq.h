@@ -439,12 +439,22 @@ dvdq_status dvdq_group_norm_backward(const void* dY, int64_t dy_sample, int64_t 
  * leave fp32's range are scaled by a power of two first.  A row of zeros has scale 0 and codes 0; a row whose y holds a value that
  * is not finite has scale NaN and codes 0.
  * H may be X or R itself, Y may be X or R itself (same pitches, not both the same one); apart from that outputs overlap nothing.
- * N * S < 2^31, C <= 2^20, eps >= 0.  Any alignment of rows; 16 bytes (and codes on 8) are the fastest. */
-dvdq_status dvdq_rms_norm(const void* X, int64_t x_outer, int64_t x_row, const void* R, int64_t r_outer, int64_t r_row,
-                          int64_t N, int64_t S, int64_t C, const void* gamma, int32_t param_dtype, float eps,
-                          void* H, int64_t h_outer, int64_t h_row, void* Y, int64_t y_outer, int64_t y_row,
-                          int8_t* codes, int64_t c_outer, int64_t c_row, float* scales, float* rstd_out, int32_t dtype,
-                          void* cuda_stream);
+ * N * S < 2^31, C <= 2^20, eps >= 0.  Any alignment of rows; 16 bytes (and codes on 8) are the fastest.  The arguments come in a struct on the
+ * host, read during the call. */
+typedef struct {
+    const void* X;  int64_t x_outer, x_row;
+    const void* R;  int64_t r_outer, r_row;   /* NULL: no residual */
+    void* H;        int64_t h_outer, h_row;
+    void* Y;        int64_t y_outer, y_row;
+    int8_t* codes;  int64_t c_outer, c_row;
+    int64_t N, S, C;
+    const void* gamma;
+    float* scales;
+    float* rstd_out;
+    int32_t param_dtype, dtype;
+    float eps;
+} dvdq_rms_norm_args;
+dvdq_status dvdq_rms_norm(const dvdq_rms_norm_args* args /* host */, void* cuda_stream);
 /* Its gradients, with H the h of the forward call (X itself where there was no residual) and hh = h rstd:
  *   dX = rstd (gamma dy - hh <gamma dy hh>) + dH, <.> the mean over the row: the gradient of x and of r alike.  dH (or NULL): the gradient
  *        that reaches h by another way, along the residual stream
@@ -452,10 +462,20 @@ dvdq_status dvdq_rms_norm(const void* X, int64_t x_outer, int64_t x_row, const v
  * dX and dgamma may each be NULL, not both.  dX may be dY, H or dH itself (same pitches).  The workspace (256-byte aligned) is needed for dgamma
  * only.  N * S == 0: dgamma is zeros.  The codes' rounding has no gradient: through it, dy is taken as that of y. */
 size_t dvdq_rms_norm_backward_workspace_bytes(int64_t N, int64_t S, int64_t C);
-dvdq_status dvdq_rms_norm_backward(const void* dY, int64_t dy_outer, int64_t dy_row, const void* H, int64_t h_outer, int64_t h_row,
-                                   const float* rstd, const void* dH, int64_t dh_outer, int64_t dh_row, int64_t N, int64_t S,
-                                   int64_t C, const void* gamma, int32_t param_dtype, void* dX, int64_t dx_outer, int64_t dx_row,
-                                   float* dgamma, int32_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+typedef struct {
+    const void* dY; int64_t dy_outer, dy_row;
+    const void* H;  int64_t h_outer, h_row;
+    const void* dH; int64_t dh_outer, dh_row; /* NULL: none */
+    void* dX;       int64_t dx_outer, dx_row;
+    int64_t N, S, C;
+    const void* gamma;
+    const float* rstd;
+    float* dgamma;
+    void* workspace;
+    uint64_t workspace_bytes;
+    int32_t param_dtype, dtype;
+} dvdq_rms_norm_backward_args;
+dvdq_status dvdq_rms_norm_backward(const dvdq_rms_norm_backward_args* args /* host */, void* cuda_stream);
 
 /* ---- rows in 8 bits: the operands of dvdq_linear_int8 -----------------------------------------
  *
@@ -475,10 +495,20 @@ dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx,
  * are arbitrary, and what lies between a row's last element and the pitch is not used and not written.  The pitch of a single row is
  * not read.  M == 0 is a no-op.  Apart from R = Y, the output overlaps nothing that the call reads.  Workspace: 256-byte aligned, often 0. */
 size_t dvdq_linear_int8_workspace_bytes(int64_t M, int64_t N, int64_t K);
-dvdq_status dvdq_linear_int8(const int8_t* A, const float* a_scales, int64_t M, int64_t lda, const int8_t* W,
-                             const float* w_scales, int64_t N, int64_t K, int64_t ldw, const void* bias, const void* R,
-                             int64_t ldr, int32_t act, void* Y, int64_t ldy, int32_t dtype, void* workspace,
-                             size_t workspace_bytes, void* cuda_stream);
+typedef struct {
+    const int8_t* A;  int64_t lda;
+    const int8_t* W;  int64_t ldw;
+    const float* a_scales;
+    const float* w_scales;
+    const void* bias;
+    const void* R;    int64_t ldr;
+    void* Y;          int64_t ldy;
+    int64_t M, N, K;
+    void* workspace;
+    uint64_t workspace_bytes;
+    int32_t act, dtype;
+} dvdq_linear_int8_args;
+dvdq_status dvdq_linear_int8(const dvdq_linear_int8_args* args /* host */, void* cuda_stream);
 
 /* ---- test / debug entry points (so that no caller depends on the packed layouts) ---- */
 

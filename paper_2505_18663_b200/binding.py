@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -139,13 +140,12 @@ def load():
         "dvdq_group_norm": (C.c_int, [p, i64, i64, i64, i64, i64, i64, p, p, i32, C.c_float, i32, p, i64, i64, p, p, i32, p, sz, p]),
         "dvdq_group_norm_backward": (C.c_int, [p, i64, i64, p, i64, i64, p, p, i64, i64, i64, i64, p, p, i32, i32, p, i64, i64, p, p,
                                                i32, p, sz, p]),
-        "dvdq_rms_norm": (C.c_int, [p, i64, i64, p, i64, i64, i64, i64, i64, p, i32, C.c_float, p, i64, i64, p, i64, i64, p, i64, i64, p, p,
-                                    i32, p]),
+        "dvdq_rms_norm": (C.c_int, [C.c_char_p, p]),
         "dvdq_rms_norm_backward_workspace_bytes": (sz, [i64, i64, i64]),
-        "dvdq_rms_norm_backward": (C.c_int, [p, i64, i64, p, i64, i64, p, p, i64, i64, i64, i64, i64, p, i32, p, i64, i64, p, i32, p, sz, p]),
+        "dvdq_rms_norm_backward": (C.c_int, [C.c_char_p, p]),
         "dvdq_quantize_rows": (C.c_int, [p, i64, i64, i64, p, i64, p, i32, p]),
         "dvdq_linear_int8_workspace_bytes": (sz, [i64, i64, i64]),
-        "dvdq_linear_int8": (C.c_int, [p, p, i64, i64, p, p, i64, i64, i64, p, p, i64, i32, p, i64, i32, p, sz, p]),
+        "dvdq_linear_int8": (C.c_int, [C.c_char_p, p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -534,6 +534,12 @@ def dvdq_group_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tens
            "dvdq_group_norm_backward")
 
 
+# Argument structs of include/dvdq.h, packed in one go: ctypes converts arguments one by one, a tenth of a microsecond each.
+RMS_NORM_ARGS = struct.Struct("21qiif4x")
+RMS_NORM_BACKWARD_ARGS = struct.Struct("20qii")
+LINEAR_INT8_ARGS = struct.Struct("16qii")
+
+
 def _current(t: torch.Tensor, name: str) -> int:
     """The current device, which the calls run on; a tensor that is elsewhere is refused."""
     dev = t.get_device()
@@ -580,10 +586,13 @@ def _pitched(t: torch.Tensor, dtype, shape, dev: int, name: str):
 
 def _scratch(t: Optional[torch.Tensor], dev: int):
     if t is None:
-        return None, 0
+        return 0, 0
     if t.get_device() != dev or t.dtype is not torch.uint8:
         _refuse(t, torch.uint8, t.shape, dev, "workspace", "be bytes")
     return t.data_ptr(), t.numel()
+
+
+_NO_ROWS = (0, 0, 0)
 
 
 def _stream_of(stream, dev: int) -> int:
@@ -601,7 +610,7 @@ def _rows_shape(t: torch.Tensor, name: str):
 
 def _gamma(t: Optional[torch.Tensor], dt, code: int, channels: int, dev: int):
     if t is None:
-        return None, code
+        return 0, code
     pt = t.dtype
     if pt is not dt and pt is not torch.float32:
         raise TypeError(f"gamma must be {dt} or torch.float32, got {pt}")
@@ -618,16 +627,18 @@ def dvdq_rms_norm(X: torch.Tensor, residual: Optional[torch.Tensor], gamma: Opti
     code = _element_type(X, "X", _ANY_FLOAT)
     shape, N, S, channels = _rows_shape(X, "X")
     dev = _current(X, "X")
-    x, xo, xr = _rows3(X, dt, shape, dev, "X")
-    r, ro, rr = _rows3(residual, dt, shape, dev, "residual") if residual is not None else (None, 0, 0)
-    h, ho, hr = _rows3(H, dt, shape, dev, "H") if H is not None else (None, 0, 0)
-    y, yo, yr = _rows3(Y, dt, shape, dev, "Y") if Y is not None else (None, 0, 0)
-    c, co, cr = _rows3(codes, torch.int8, shape, dev, "codes") if codes is not None else (None, 0, 0)
-    s = _dense(scales, torch.float32, shape[:-1], dev, "scales") if scales is not None else None
-    q = _dense(rstd, torch.float32, shape[:-1], dev, "rstd") if rstd is not None else None
+    x = _rows3(X, dt, shape, dev, "X")
+    r = _rows3(residual, dt, shape, dev, "residual") if residual is not None else _NO_ROWS
+    h = _rows3(H, dt, shape, dev, "H") if H is not None else _NO_ROWS
+    y = _rows3(Y, dt, shape, dev, "Y") if Y is not None else _NO_ROWS
+    c = _rows3(codes, torch.int8, shape, dev, "codes") if codes is not None else _NO_ROWS
+    s = _dense(scales, torch.float32, shape[:-1], dev, "scales") if scales is not None else 0
+    q = _dense(rstd, torch.float32, shape[:-1], dev, "rstd") if rstd is not None else 0
     ga, param_code = _gamma(gamma, dt, code, channels, dev)
-    _check(load().dvdq_rms_norm(x, xo, xr, r, ro, rr, N, S, channels, ga, param_code, eps, h, ho, hr, y, yo, yr, c, co, cr, s, q, code,
-                                _stream_of(stream, dev)), "dvdq_rms_norm")
+    args = RMS_NORM_ARGS.pack(*x, *r, *h, *y, *c, N, S, channels, ga, s, q, param_code, code, eps)
+    status = load().dvdq_rms_norm(args, _stream_of(stream, dev))
+    if status:
+        raise DvdqError(status, "dvdq_rms_norm")
 
 
 def dvdq_rms_norm_backward_workspace_bytes(N: int, S: int, C_: int) -> int:
@@ -643,16 +654,17 @@ def dvdq_rms_norm_backward(dY: torch.Tensor, H: torch.Tensor, rstd: torch.Tensor
     code = _element_type(H, "H", _ANY_FLOAT)
     shape, N, S, channels = _rows_shape(H, "H")
     dev = _current(H, "H")
-    h, ho, hr = _rows3(H, dt, shape, dev, "H")
-    d, do, dr = _rows3(dY, dt, shape, dev, "dY")
-    e, eo, er = _rows3(dH, dt, shape, dev, "dH") if dH is not None else (None, 0, 0)
-    x, xo, xr = _rows3(dX, dt, shape, dev, "dX") if dX is not None else (None, 0, 0)
+    h = _rows3(H, dt, shape, dev, "H")
+    d = _rows3(dY, dt, shape, dev, "dY")
+    e = _rows3(dH, dt, shape, dev, "dH") if dH is not None else _NO_ROWS
+    x = _rows3(dX, dt, shape, dev, "dX") if dX is not None else _NO_ROWS
     q = _dense(rstd, torch.float32, shape[:-1], dev, "rstd")
     ga, param_code = _gamma(gamma, dt, code, channels, dev)
-    dg = _dense(dgamma, torch.float32, (channels,), dev, "dgamma") if dgamma is not None else None
-    ws, room = _scratch(workspace, dev)
-    _check(load().dvdq_rms_norm_backward(d, do, dr, h, ho, hr, q, e, eo, er, N, S, channels, ga, param_code, x, xo, xr, dg, code, ws, room,
-                                         _stream_of(stream, dev)), "dvdq_rms_norm_backward")
+    dg = _dense(dgamma, torch.float32, (channels,), dev, "dgamma") if dgamma is not None else 0
+    args = RMS_NORM_BACKWARD_ARGS.pack(*d, *h, *e, *x, N, S, channels, ga, q, dg, *_scratch(workspace, dev), param_code, code)
+    status = load().dvdq_rms_norm_backward(args, _stream_of(stream, dev))
+    if status:
+        raise DvdqError(status, "dvdq_rms_norm_backward")
 
 
 def dvdq_quantize_rows(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
@@ -685,15 +697,16 @@ def dvdq_linear_int8(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w
         raise TypeError(f"A and W must be [M, K] and [N, K], got {tuple(a_shape)} and {tuple(w_shape)}")
     (M, K), N = a_shape, w_shape[0]
     dev = _current(A, "A")
-    a, lda = _pitched(A, torch.int8, a_shape, dev, "A")
-    w, ldw = _pitched(W, torch.int8, w_shape, dev, "W")
-    y, ldy = _pitched(Y, dt, (M, N), dev, "Y")
-    r, ldr = _pitched(residual, dt, (M, N), dev, "residual") if residual is not None else (None, 0)
-    b = _dense(bias, dt, (N,), dev, "bias") if bias is not None else None
-    ws, room = _scratch(workspace, dev)
-    _check(load().dvdq_linear_int8(a, _dense(a_scales, torch.float32, (M,), dev, "a_scales"), M, lda, w,
-                                   _dense(w_scales, torch.float32, (N,), dev, "w_scales"), N, K, ldw, b, r, ldr, act, y, ldy, code, ws, room,
-                                   _stream_of(stream, dev)), "dvdq_linear_int8")
+    y_shape = (M, N)
+    args = LINEAR_INT8_ARGS.pack(
+        *_pitched(A, torch.int8, a_shape, dev, "A"), *_pitched(W, torch.int8, w_shape, dev, "W"),
+        _dense(a_scales, torch.float32, (M,), dev, "a_scales"), _dense(w_scales, torch.float32, (N,), dev, "w_scales"),
+        _dense(bias, dt, (N,), dev, "bias") if bias is not None else 0,
+        *(_pitched(residual, dt, y_shape, dev, "residual") if residual is not None else (0, 0)), *_pitched(Y, dt, y_shape, dev, "Y"),
+        M, N, K, *_scratch(workspace, dev), act, code)
+    status = load().dvdq_linear_int8(args, _stream_of(stream, dev))
+    if status:
+        raise DvdqError(status, "dvdq_linear_int8")
 
 
 # ------------------------------------------------------------------ test / debug entry points

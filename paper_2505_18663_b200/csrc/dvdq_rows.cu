@@ -24,40 +24,42 @@ using namespace dvdq;
 
 extern "C" {
 
-dvdq_status dvdq_rms_norm(const void* X, int64_t x_outer, int64_t x_row, const void* R, int64_t r_outer, int64_t r_row, int64_t N, int64_t S,
-                          int64_t C, const void* gamma, int32_t param_dtype, float eps, void* H, int64_t h_outer, int64_t h_row, void* Y,
-                          int64_t y_outer, int64_t y_row, int8_t* codes, int64_t c_outer, int64_t c_row, float* scales, float* rstd_out,
-                          int32_t dtype, void* stream) {
-    if (!rows_sizes_ok(N, S, C) || !(eps >= 0.0f) || !isfinite(eps)) return DVDQ_ERR_SHAPE;
-    if (!rows_dtype_ok(dtype) || (param_dtype != dtype && param_dtype != DVDQ_F32)) return DVDQ_ERR_UNSUPPORTED;
+dvdq_status dvdq_rms_norm(const dvdq_rms_norm_args* args, void* stream) {
+    if (!args) return DVDQ_ERR_NULL;
+    const dvdq_rms_norm_args& a = *args;
+    const int64_t N = a.N, S = a.S, C = a.C;
+    if (!rows_sizes_ok(N, S, C) || !(a.eps >= 0.0f) || !isfinite(a.eps)) return DVDQ_ERR_SHAPE;
+    if (!rows_dtype_ok(a.dtype) || (a.param_dtype != a.dtype && a.param_dtype != DVDQ_F32)) return DVDQ_ERR_UNSUPPORTED;
     if (N == 0 || S == 0) return DVDQ_OK;
-    if (!X || (!H && !Y && !codes && !rstd_out) || (codes == nullptr) != (scales == nullptr)) return DVDQ_ERR_NULL;
-    const int bytes = dtype_bytes(dtype), pb = dtype_bytes(param_dtype);
+    if (!a.X || (!a.H && !a.Y && !a.codes && !a.rstd_out) || (a.codes == nullptr) != (a.scales == nullptr)) return DVDQ_ERR_NULL;
+    const int bytes = dtype_bytes(a.dtype), pb = dtype_bytes(a.param_dtype);
     RmsArgs A = {};
-    A.x = RowsOf{const_cast<void*>(X), x_outer, x_row};
-    A.r = RowsOf{const_cast<void*>(R), r_outer, r_row};
-    A.h = RowsOf{H, h_outer, h_row};
-    A.y = RowsOf{Y, y_outer, y_row};
-    A.codes = RowsOf{codes, c_outer, c_row};
+    A.x = RowsOf{const_cast<void*>(a.X), a.x_outer, a.x_row};
+    A.r = RowsOf{const_cast<void*>(a.R), a.r_outer, a.r_row};
+    A.h = RowsOf{a.H, a.h_outer, a.h_row};
+    A.y = RowsOf{a.Y, a.y_outer, a.y_row};
+    A.codes = RowsOf{a.codes, a.c_outer, a.c_row};
     dvdq_status s;
     if ((s = check_rows(&A.x, N, S, C, bytes, false)) != DVDQ_OK || (s = check_rows(&A.r, N, S, C, bytes, false)) != DVDQ_OK ||
         (s = check_rows(&A.h, N, S, C, bytes, true)) != DVDQ_OK || (s = check_rows(&A.y, N, S, C, bytes, true)) != DVDQ_OK ||
         (s = check_rows(&A.codes, N, S, C, 1, true)) != DVDQ_OK)
         return s;
-    if (!in_place_ok(A.x, A.h) || !in_place_ok(A.r, A.h) || !in_place_ok(A.x, A.y) || !in_place_ok(A.r, A.y) || (H && H == Y)) return DVDQ_ERR_SHAPE;
-    if ((gamma && !aligned_to(gamma, pb)) || (scales && !aligned_to(scales, 4)) || (rstd_out && !aligned_to(rstd_out, 4))) return DVDQ_ERR_ALIGN;
+    if (!in_place_ok(A.x, A.h) || !in_place_ok(A.r, A.h) || !in_place_ok(A.x, A.y) || !in_place_ok(A.r, A.y) || (a.H && a.H == a.Y)) return DVDQ_ERR_SHAPE;
+    if ((a.gamma && !aligned_to(a.gamma, pb)) || (a.scales && !aligned_to(a.scales, 4)) || (a.rstd_out && !aligned_to(a.rstd_out, 4))) return DVDQ_ERR_ALIGN;
     if ((s = check_device_arch()) != DVDQ_OK) return s;
     A.shape = rows_shape(N, S, C);
-    A.gamma = gamma;
-    A.scales = scales;
-    A.rstd = rstd_out;
-    A.params_f32 = param_dtype == DVDQ_F32;
-    A.eps = eps;
+    A.gamma = a.gamma;
+    A.scales = a.scales;
+    A.rstd = a.rstd_out;
+    A.params_f32 = a.param_dtype == DVDQ_F32;
+    A.eps = a.eps;
     A.inv_c = 1.0f / (float)C;
     const RowsOf* all[] = {&A.x, &A.r, &A.h, &A.y};
-    const int access = rows_access(all, 4, &A.codes, gamma, bytes, pb);
+    const int access = rows_access(all, 4, &A.codes, a.gamma, bytes, pb);
     const cudaStream_t st = (cudaStream_t)stream;
-    return cuda_status(dtype == DVDQ_BF16 ? launch_rms_norm_bf16(A, access, st) : dtype == DVDQ_F16 ? launch_rms_norm_f16(A, access, st) : launch_rms_norm_f32(A, access, st));
+    return cuda_status(a.dtype == DVDQ_BF16  ? launch_rms_norm_bf16(A, access, st)
+                       : a.dtype == DVDQ_F16 ? launch_rms_norm_f16(A, access, st)
+                                             : launch_rms_norm_f32(A, access, st));
 }
 
 dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx, int8_t* codes, int64_t ldc, float* scales, int32_t dtype,
@@ -89,14 +91,17 @@ size_t dvdq_rms_norm_backward_workspace_bytes(int64_t N, int64_t S, int64_t C) {
     return (size_t)align_up(rms_parts(N * S, C) * C * 4, 256);
 }
 
-dvdq_status dvdq_rms_norm_backward(const void* dY, int64_t dy_outer, int64_t dy_row, const void* H, int64_t h_outer, int64_t h_row,
-                                   const float* rstd, const void* dH, int64_t dh_outer, int64_t dh_row, int64_t N, int64_t S, int64_t C,
-                                   const void* gamma, int32_t param_dtype, void* dX, int64_t dx_outer, int64_t dx_row, float* dgamma,
-                                   int32_t dtype, void* workspace, size_t workspace_bytes, void* stream) {
+dvdq_status dvdq_rms_norm_backward(const dvdq_rms_norm_backward_args* args, void* stream) {
+    if (!args) return DVDQ_ERR_NULL;
+    const dvdq_rms_norm_backward_args& a = *args;
+    const int64_t N = a.N, S = a.S, C = a.C;
+    const int32_t dtype = a.dtype, param_dtype = a.param_dtype;
+    const void* gamma = a.gamma;
+    float* dgamma = a.dgamma;
     if (!rows_sizes_ok(N, S, C)) return DVDQ_ERR_SHAPE;
     if (!rows_dtype_ok(dtype) || (param_dtype != dtype && param_dtype != DVDQ_F32)) return DVDQ_ERR_UNSUPPORTED;
     const int bytes = dtype_bytes(dtype), pb = dtype_bytes(param_dtype);
-    if ((gamma && !aligned_to(gamma, pb)) || (dgamma && !aligned_to(dgamma, 4)) || (rstd && !aligned_to(rstd, 4))) return DVDQ_ERR_ALIGN;
+    if ((gamma && !aligned_to(gamma, pb)) || (dgamma && !aligned_to(dgamma, 4)) || (a.rstd && !aligned_to(a.rstd, 4))) return DVDQ_ERR_ALIGN;
     dvdq_status s;
     const cudaStream_t st = (cudaStream_t)stream;
     if (N == 0 || S == 0) {  // sums over nothing
@@ -104,27 +109,27 @@ dvdq_status dvdq_rms_norm_backward(const void* dY, int64_t dy_outer, int64_t dy_
         if ((s = check_device_arch()) != DVDQ_OK) return s;
         return cuda_status(launch_after(rms_norm_no_rows_kernel, dim3((unsigned)ceil_div(C, 256)), dim3(256), 0, st, dgamma, (int)C));
     }
-    if (!dY || !H || !rstd || (!dX && !dgamma)) return DVDQ_ERR_NULL;
+    if (!a.dY || !a.H || !a.rstd || (!a.dX && !dgamma)) return DVDQ_ERR_NULL;
     RmsBackwardArgs A = {};
-    A.dy = RowsOf{const_cast<void*>(dY), dy_outer, dy_row};
-    A.h = RowsOf{const_cast<void*>(H), h_outer, h_row};
-    A.dh = RowsOf{const_cast<void*>(dH), dh_outer, dh_row};
-    A.dx = RowsOf{dX, dx_outer, dx_row};
+    A.dy = RowsOf{const_cast<void*>(a.dY), a.dy_outer, a.dy_row};
+    A.h = RowsOf{const_cast<void*>(a.H), a.h_outer, a.h_row};
+    A.dh = RowsOf{const_cast<void*>(a.dH), a.dh_outer, a.dh_row};
+    A.dx = RowsOf{a.dX, a.dx_outer, a.dx_row};
     if ((s = check_rows(&A.dy, N, S, C, bytes, false)) != DVDQ_OK || (s = check_rows(&A.h, N, S, C, bytes, false)) != DVDQ_OK ||
         (s = check_rows(&A.dh, N, S, C, bytes, false)) != DVDQ_OK || (s = check_rows(&A.dx, N, S, C, bytes, true)) != DVDQ_OK)
         return s;
     if (!in_place_ok(A.dy, A.dx) || !in_place_ok(A.h, A.dx) || !in_place_ok(A.dh, A.dx)) return DVDQ_ERR_SHAPE;
     const int64_t parts = rms_parts(N * S, C);
     if (dgamma) {
-        if (!workspace) return DVDQ_ERR_NULL;
-        if (!aligned_to(workspace, 256)) return DVDQ_ERR_ALIGN;
-        if (workspace_bytes < (size_t)(parts * C * 4)) return DVDQ_ERR_WORKSPACE;
+        if (!a.workspace) return DVDQ_ERR_NULL;
+        if (!aligned_to(a.workspace, 256)) return DVDQ_ERR_ALIGN;
+        if (a.workspace_bytes < (uint64_t)(parts * C * 4)) return DVDQ_ERR_WORKSPACE;
     }
     if ((s = check_device_arch()) != DVDQ_OK) return s;
     A.shape = rows_shape(N, S, C);
     A.gamma = gamma;
-    A.rstd = rstd;
-    A.part = dgamma ? static_cast<float*>(workspace) : nullptr;
+    A.rstd = a.rstd;
+    A.part = dgamma ? static_cast<float*>(a.workspace) : nullptr;
     A.params_f32 = param_dtype == DVDQ_F32;
     A.inv_c = 1.0f / (float)C;
     const RowsOf* all[] = {&A.dy, &A.h, &A.dh, &A.dx};

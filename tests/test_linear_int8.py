@@ -186,22 +186,21 @@ def test_no_tokens_and_refusals_of_the_binding():
 
 
 def test_refusals_before_any_cuda_call():
-    import ctypes as C
     lib = B.load()
-    p = C.c_void_p
-    one, two = p(256), p(512)   # never dereferenced: validation fails first
+    one, two = 256, 512   # never dereferenced: validation fails first
 
-    def call(M=20, N=16, K=32, a=one, s=one, lda=32, w=one, t=one, ldw=32, bias=None, r=None, ldr=16, act=0, y=two, ldy=16, dt=B.BF16, ws=None, room=0):
-        return lib.dvdq_linear_int8(a, s, M, lda, w, t, N, K, ldw, bias, r, ldr, act, y, ldy, dt, ws, room, None)
+    def call(M=20, N=16, K=32, a=one, s=one, lda=32, w=one, t=one, ldw=32, bias=0, r=0, ldr=16, act=0, y=two, ldy=16, dt=B.BF16, ws=0, room=0):
+        return lib.dvdq_linear_int8(B.LINEAR_INT8_ARGS.pack(a or 0, lda, w or 0, ldw, s or 0, t or 0, bias, r, ldr, y or 0, ldy, M, N, K, ws, room, act, dt), None)
 
+    assert lib.dvdq_linear_int8(None, None) == B.ERR_NULL
     assert call(M=-1) == call(N=0) == call(K=0) == call(K=131072, lda=131072, ldw=131072) == call(M=1 << 31) == call(N=(1 << 25) + 1, ldy=1 << 26) == B.ERR_SHAPE
     assert call(act=3) == call(dt=B.F32) == call(dt=-1) == B.ERR_UNSUPPORTED
     assert call(a=None) == call(w=None) == call(s=None) == call(t=None) == call(y=None) == B.ERR_NULL
     assert call(lda=16) == call(ldw=31) == call(ldy=8) == call(r=one, ldr=8) == call(r=two, ldr=24) == B.ERR_SHAPE
-    assert call(lda=40) == call(ldw=33) == call(ldy=20) == call(a=p(8)) == call(w=p(264)) == call(y=p(520)) == call(s=p(258)) == call(bias=p(257)) == B.ERR_ALIGN
+    assert call(lda=40) == call(ldw=33) == call(ldy=20) == call(a=8) == call(w=264) == call(y=520) == call(s=258) == call(bias=257) == B.ERR_ALIGN
     assert call(M=0, a=None, s=None, y=None) == B.OK
     need = B.dvdq_linear_int8_workspace_bytes(200, 256, 65536)
     assert need > 0 and need % 256 == 0
     long = dict(M=200, N=256, K=65536, lda=65536, ldw=65536, ldy=256)
-    assert call(**long) == B.ERR_NULL and call(**long, ws=p(384), room=need) == B.ERR_ALIGN and call(**long, ws=one, room=need - 1) == B.ERR_WORKSPACE
+    assert call(**long) == B.ERR_NULL and call(**long, ws=384, room=need) == B.ERR_ALIGN and call(**long, ws=one, room=need - 1) == B.ERR_WORKSPACE
     assert B.dvdq_linear_int8_workspace_bytes(4, 256, 65536) == 0 and B.dvdq_linear_int8_workspace_bytes(200, 256, 131072) == 0

@@ -338,32 +338,48 @@ def test_binding_refuses():
         assert e.value.status == status
 
 
+def test_argument_structs_are_packed_as_the_header_lays_them_out():
+    import ctypes as C
+    p, i64 = C.c_void_p, C.c_int64
+
+    def size(counts, tail):
+        fields = [(f"f{i}", i64) for i in range(counts)] + [(f"t{i}", t) for i, t in enumerate(tail)]
+        return C.sizeof(type("S", (C.Structure,), {"_fields_": fields}))
+
+    assert B.RMS_NORM_ARGS.size == size(21, [C.c_int32, C.c_int32, C.c_float])
+    assert B.RMS_NORM_BACKWARD_ARGS.size == size(20, [C.c_int32, C.c_int32])
+    assert B.LINEAR_INT8_ARGS.size == size(16, [C.c_int32, C.c_int32])
+
+
 def test_refusals_before_any_cuda_call():
     import ctypes as C
     lib = B.load()
-    one, two = C.c_void_p(256), C.c_void_p(512)   # never dereferenced: validation fails first
-    p = C.c_void_p
+    one, two = 256, 512   # never dereferenced: validation fails first
 
-    def norm(N=2, S=3, Ch=8, x=one, r=None, gamma=None, pt=B.F32, eps=1e-6, h=None, y=two, yo=24, yr=8, c=None, s=None, q=None, dt=B.F32, xo=24, xr=8):
-        return lib.dvdq_rms_norm(x, xo, xr, r, 24, 8, N, S, Ch, gamma, pt, eps, h, yo, yr, y, yo, yr, c, 24, 8, s, q, dt, None)
+    def norm(N=2, S=3, Ch=8, x=one, r=0, gamma=0, pt=B.F32, eps=1e-6, h=0, y=two, yo=24, yr=8, c=0, s=0, q=0, dt=B.F32, xo=24, xr=8):
+        return lib.dvdq_rms_norm(B.RMS_NORM_ARGS.pack(x or 0, xo, xr, r, 24, 8, h, yo, yr, y or 0, yo, yr, c, 24, 8, N, S, Ch, gamma, s, q, pt, dt, eps), None)
 
+    assert lib.dvdq_rms_norm(None, None) == lib.dvdq_rms_norm_backward(None, None) == B.ERR_NULL
     assert norm(Ch=0) == norm(Ch=(1 << 20) + 1, xo=1 << 24, yo=1 << 24) == norm(N=-1) == norm(N=1 << 20, S=1 << 20) == B.ERR_SHAPE
     assert norm(eps=-1e-6) == norm(eps=float("nan")) == norm(eps=float("inf")) == B.ERR_SHAPE
     assert norm(dt=3) == norm(pt=B.F16) == norm(pt=7) == B.ERR_UNSUPPORTED
     assert norm(x=None) == norm(y=None) == norm(c=one) == norm(s=one) == B.ERR_NULL
     assert norm(yr=7) == norm(yo=4) == norm(xr=-8) == B.ERR_SHAPE                      # outputs that overlap, a negative pitch
     assert norm(y=one, yo=48) == norm(r=two, yo=48) == norm(h=two) == B.ERR_SHAPE       # in place with other pitches; two outputs in one place
-    assert norm(y=p(514)) == norm(gamma=p(258)) == norm(q=p(514)) == norm(c=one, s=p(514)) == B.ERR_ALIGN
+    assert norm(y=514) == norm(gamma=258) == norm(q=514) == norm(c=one, s=514) == B.ERR_ALIGN
     assert norm(N=0) == norm(S=0, x=None) == B.OK
 
-    def back(N=2, S=3, Ch=8, dy=one, h=one, q=one, dh=None, gamma=None, pt=B.F32, dx=two, xr=8, dg=None, dt=B.F32, ws=None, room=0):
-        return lib.dvdq_rms_norm_backward(dy, 24, 8, h, 24, 8, q, dh, 24, 8, N, S, Ch, gamma, pt, dx, 24, xr, dg, dt, ws, room, None)
+    def back(N=2, S=3, Ch=8, dy=one, h=one, q=one, dh=0, gamma=0, pt=B.F32, dx=two, xr=8, dg=0, dt=B.F32, ws=0, room=0):
+        return lib.dvdq_rms_norm_backward(B.RMS_NORM_BACKWARD_ARGS.pack(dy or 0, 24, 8, h or 0, 24, 8, dh, 24, 8, dx or 0, 24, xr, N, S, Ch, gamma, q or 0, dg, ws, room,
+                                                                        pt, dt), None)
 
     assert back(dx=None) == back(dy=None) == back(h=None) == back(q=None) == B.ERR_NULL
-    assert back(dg=one) == B.ERR_NULL and back(dg=one, ws=p(128), room=1 << 20) == B.ERR_ALIGN and back(dg=one, ws=one, room=100) == B.ERR_WORKSPACE
+    assert back(dg=one) == B.ERR_NULL and back(dg=one, ws=128, room=1 << 20) == B.ERR_ALIGN and back(dg=one, ws=one, room=100) == B.ERR_WORKSPACE
     assert back(xr=4) == back(dx=one, xr=9) == back(Ch=0) == B.ERR_SHAPE
-    assert back(dt=5) == back(pt=B.BF16) == B.ERR_UNSUPPORTED and back(q=p(6)) == back(dx=p(6)) == B.ERR_ALIGN
+    assert back(dt=5) == back(pt=B.BF16) == B.ERR_UNSUPPORTED and back(q=6) == back(dx=6) == B.ERR_ALIGN
     assert back(N=0) == B.OK
+
+    p = C.c_void_p
 
     def rows(M=4, K=8, x=one, ldx=8, c=two, ldc=8, s=one, dt=B.F32):
         return lib.dvdq_quantize_rows(x, M, K, ldx, c, ldc, s, dt, None)
