@@ -16,10 +16,10 @@ constexpr int kL8BK = 128;  // elements of k per stage: one 128-byte swizzle row
 
 template <int OUT, bool WIDE>
 struct L8Smem {
-    // a residual that comes early takes two more blocks per epilogue warp, and 32 KB of the ring
-    static constexpr int kRing = (OUT == kLinFinalMore ? (WIDE ? 3 : 5) : (WIDE ? 5 : 6)) * 32768;
+    // a residual that comes early takes two more blocks per epilogue warp (one, where they are wide), and 32 KB of the ring
+    static constexpr int kRing = (OUT == kLinFinalMore ? (WIDE ? 4 : 5) : (WIDE ? 5 : 6)) * 32768;
     static constexpr int kMaxStages = OUT == kLinFinalMore ? 12 : 16;  // a stage is 32 KB at most; narrow tiles and few rows take less
-    static constexpr int kBufs = OUT == kLinFinalMore ? 4 : 2;
+    static constexpr int kBufs = OUT == kLinFinalMore ? (WIDE ? 3 : 4) : 2;
     static constexpr int kCols = WIDE ? 64 : 32;            // of an epilogue block
     static constexpr int kBuf = 32 * kCols * 2;             // 32 x kCols outputs; int32 pieces use two as one
     static constexpr int kBufOff = kRing;
@@ -453,10 +453,10 @@ linear_int8_few_kernel(const int8_t* __restrict__ X, int64_t ldx, const int8_t* 
 
 // ------------------------------------------------------------------ host side
 
-// Epilogue blocks of 32 x 64 instead of 32 x 32 outputs with a residual, up to this many k-blocks (fewer copies, fewer operand stages): 32760 x K ->
-// 1536, K = 128, 512, 1024, 1536: 48.4, 55.4, 66.7, 90.7 us, in narrow blocks 57.4, 59.8, 74.7, 85.7.  Without a residual narrow ones are the faster from
-// 512 on (35 us, 38), and even below.
-constexpr int kL8WideMore = 8;
+// Epilogue blocks of 32 x 64 instead of 32 x 32 outputs with a residual, up to this many k-blocks (half the copies, one operand stage less): 32760 x K ->
+// 1536, K = 512, 1024, 1536, 2048, 5120, 8960: 52-56, 58-70, 74-83, 90-102, 196-212, 360-365 us, in narrow blocks 60-66, 75-77, 86-88, 91-115, 198-224,
+// 292-355 (ranges: the power cap's).  Without a residual narrow ones are the faster from 512 on (35 us, 38).
+constexpr int kL8WideMore = 12;
 
 struct L8Scales {
     const float *a, *w;
