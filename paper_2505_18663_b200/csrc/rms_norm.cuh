@@ -217,11 +217,14 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P,
     T* to_h = NORM && A.h.p ? static_cast<T*>(A.h.p) + row_at(A.h, n, s) : nullptr;
     T* to_y = NORM && A.y.p ? static_cast<T*>(A.y.p) + row_at(A.y, n, s) : nullptr;
     int8_t* to_c = codes ? static_cast<int8_t*>(A.codes.p) + row_at(A.codes, n, s) : nullptr;
-    if (to_h) row.visit(L, [&](int, int c, const Pairs<V>& h, auto whole, bool there) { row_store<T, V, decltype(whole)::value>(to_h, c, C, h, there); });
-    if (!to_y && !codes) return;
+    if constexpr (P > 0) {  // a row in registers; one that is read again may lie where h goes, and is stored with y below
+        if (to_h) row.visit(L, [&](int, int c, const Pairs<V>& h, auto whole, bool there) { row_store<T, V, decltype(whole)::value>(to_h, c, C, h, there); });
+        if (!to_y && !codes) return;
+    }
     const bool plain = o.f == 1.0f && lift == 1.0f;  // else: far from one, near the smallest numbers, zeros or not finite
     row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole, bool there) {
         constexpr bool W = decltype(whole)::value;
+        if (P == 0 && to_h) row_store<T, V, W>(to_h, c, C, h, there);
         Pairs<V> y = h;
         if (NORM) {
             if (o.f != 1.0f) {

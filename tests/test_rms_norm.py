@@ -142,6 +142,20 @@ def test_in_place(dt):
 
 
 @gpu
+@pytest.mark.parametrize("C", [40000, 40008, 33333])
+@pytest.mark.parametrize("over", ["x", "r"])
+def test_long_rows_whose_sum_is_kept_in_place(C, over):
+    """Rows that are read again for y and codes, after h has gone over x or r."""
+    g = gen(8)
+    x, r = (torch.randn(3, C, device=DEV, generator=g).bfloat16() for _ in range(2))
+    want = [torch.empty_like(x), torch.empty_like(x), torch.empty(3, C, dtype=torch.int8, device=DEV), torch.empty(3, device=DEV)]
+    B.dvdq_rms_norm(x, r, None, 1e-6, *want)
+    got = [x if over == "x" else r, torch.empty_like(x), torch.empty(3, C, dtype=torch.int8, device=DEV), torch.empty(3, device=DEV)]
+    B.dvdq_rms_norm(x, r, None, 1e-6, *got)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
 @pytest.mark.parametrize("C", [12, 300, 4100, 50000])
 @pytest.mark.parametrize("dt,scale,eps", [(torch.float32, 1e25, 1e-6), (torch.float32, 3e38, 0.0), (torch.float32, 1e-30, 0.0), (torch.float32, 1e-30, 1e-6),
                                           (torch.float32, 1e-41, 0.0), (torch.bfloat16, 1e30, 1e-6), (torch.bfloat16, 1e-30, 0.0),
