@@ -139,7 +139,7 @@ dvdq_status dvdq_rms_norm_backward(const dvdq_rms_norm_backward_args* args, void
                           : dtype == DVDQ_F16 ? launch_rms_norm_backward_f16(A, access, parts, &ctas, st)
                                               : launch_rms_norm_backward_f32(A, access, parts, &ctas, st);
     if (e != cudaSuccess || !dgamma) return cuda_status(e);
-    return cuda_status(launch_after(rms_norm_join_kernel, dim3((unsigned)ceil_div(C, kJoinCols)), dim3(kJoinThreads), 0, st, A.part, ctas, (int)C, dgamma));
+    return cuda_status(launch_rms_join(A.part, ctas, (int)C, dgamma, st));
 }
 
 }  // extern "C"

@@ -41,6 +41,13 @@ __device__ __forceinline__ Pairs<V> row_terms(const Pairs<V>& d, const Pairs<V>&
     }
     return t;
 }
+// V sums on 16 bytes (whole rows: C is a multiple of V, which is 4 or 8)
+template <int V>
+__device__ __forceinline__ void sums_store(float* p, const Pairs<V>& f) {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(f.get(j), f.get(j + 1), f.get(j + 2), f.get(j + 3));
+}
+
 // Registers of a thread, and with them threads of a CTA at most.
 __host__ __device__ constexpr int rows_registers_backward(int V, int P) { return P * V > 40 ? 255 : P * V > 24 ? 168 : P * V > 8 ? 128 : 64; }
 __host__ __device__ constexpr int rows_threads_backward(int V, int P) { return 65536 / rows_registers_backward(V, P) / 32 * 32; }
@@ -163,8 +170,12 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
 #pragma unroll
         for (int i = 0; i < P; ++i)
             if (L.has(i)) {
+                if constexpr (FULL) {
+                    sums_store<V>(to + L.channel(i), acc[i]);
+                } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) to[L.channel(i) + j] = acc[i].get(j);
+                    for (int j = 0; j < V; ++j) to[L.channel(i) + j] = acc[i].get(j);
+                }
             }
         if (!FULL && V > 1 && L.tail) {
 #pragma unroll
@@ -181,20 +192,22 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     }
 }
 
-// Many rows of whole pieces, a CTA each: the next row's pieces are on their way (cp.async, into slots of shared memory that are a thread's own: no
+// Many rows of whole pieces (C a multiple of V), a CTA each: the next row's pieces are on their way (cp.async, into slots of shared memory that are a thread's own: no
 // barrier) while this one's two passes read theirs from there.  Held in registers instead, inputs and sums leave an SM 10 warps, with nothing
 // in flight while they compute: 32760 x 5120 266 us.
 // A slot is asked for again only after both passes' stores, whose values came from it, have been issued.
 __host__ __device__ constexpr int ring_registers(int P) { return P <= 3 ? 96 : P == 4 ? 128 : 80 + 16 * P; }
 __host__ __device__ constexpr int ring_threads(int P) { return 65536 / ring_registers(P) / 32 * 32; }
-template <typename T, int V, int P>
+// FULL: every thread has P pieces.
+template <typename T, int V, int P, bool FULL>
 __global__ void __maxnreg__(ring_registers(P))
 rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
     constexpr int N = Pairs<V>::N;
     __shared__ float2 slots[64];
     extern __shared__ __align__(16) uint8_t ring[];
     const int lanes = (int)blockDim.x, lane = (int)threadIdx.x, C = A.shape.C;
-    const RowLanes<V, P, kFull | kWide> L(C, lanes, lane);
+    constexpr int KIND = (FULL ? kFull : 0) | kWide;
+    const RowLanes<V, P, KIND> L(C, lanes, lane);
     RowMeet<true> meet(slots, lanes);
     Pairs<V> acc[P];
 #pragma unroll
@@ -213,7 +226,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
                 const T* from = static_cast<const T*>(t.p) + row_at(t, n, s) + L.channel(0);
 #pragma unroll
                 for (int i = 0; i < P; ++i)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * step), "l"(from + i * (32 * V)) : "memory");
+                    if (L.has(i)) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * step), "l"(from + i * (32 * V)) : "memory");
                 to += tensor;
             };
             copy(A.dy);
@@ -224,7 +237,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
     };
     wait_predecessor();
     release_successor();
-    RowGamma<T, V, P, kFull | kWide, true> gamma;
+    RowGamma<T, V, P, KIND, true> gamma;
     gamma.init(L, A.gamma, A.params_f32);
     int64_t row = blockIdx.x;
     uint32_t stage = 0;
@@ -239,6 +252,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
         uint64_t sum = 0ull;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
+            if (!L.has(i)) continue;
             Piece<T, V> d, h;
             d.load_shared(at + i * step);
             h.load_shared(at + tensor + i * step);
@@ -251,6 +265,7 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
         T* dx = static_cast<T*>(A.dx.p) + row_at(A.dx, n, s);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
+            if (!L.has(i)) continue;
             Piece<T, V> d, h, e;
             d.load_shared(at + i * step);
             h.load_shared(at + tensor + i * step);
@@ -267,33 +282,38 @@ rms_norm_backward_ring_kernel(const __grid_constant__ RmsBackwardArgs A) {
     float* to = A.part + (int64_t)blockIdx.x * C;
 #pragma unroll
     for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) to[L.channel(i) + j] = acc[i].get(j);
+        if (L.has(i)) sums_store<V>(to + L.channel(i), acc[i]);
 }
 
-// dgamma from the CTAs' sums, in fp64 and in a fixed order: 8 channels a CTA, 128 threads share the rows of sums of each (with 16 warps for 32 channels,
-// 592 rows of 128 sums took 6 us longer: too few loads in flight).
-constexpr int kJoinThreads = 1024, kJoinCols = 8;
+// dgamma from the CTAs' sums, in fp64 and in a fixed order: COLS channels a CTA, whose other threads share the rows of sums.  Eight channels, where that
+// is a wave or less (with 32 of them 592 rows of 128 sums took 6 us longer: too few loads in flight), otherwise 32.
+constexpr int kJoinThreads = 1024;
+template <int COLS>
 static __global__ void __launch_bounds__(kJoinThreads) rms_norm_join_kernel(const float* __restrict__ part, int parts, int C, float* __restrict__ out) {
-    __shared__ double sh[kJoinThreads / 32][kJoinCols];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * kJoinCols + (lane & (kJoinCols - 1));
+    constexpr int kRows = kJoinThreads / COLS;  // rows of sums side by side
+    __shared__ double sh[32][COLS];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = threadIdx.x % COLS, c = blockIdx.x * COLS + col;
     wait_predecessor();
     release_successor();
     double t = 0.0;
     if (c < C) {
-#pragma unroll 4
-        for (int i = threadIdx.x / kJoinCols; i < parts; i += kJoinThreads / kJoinCols) t += part[(int64_t)i * C + c];
+#pragma unroll 8
+        for (int i = threadIdx.x / COLS; i < parts; i += kRows) t += part[(int64_t)i * C + c];
     }
-    t += __shfl_xor_sync(0xFFFFFFFFu, t, 8);
-    t += __shfl_xor_sync(0xFFFFFFFFu, t, 16);
-    if (lane < kJoinCols) sh[w][lane] = t;
+#pragma unroll
+    for (int o = COLS; o < 32; o *= 2) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+    if (lane < COLS) sh[w][lane] = t;
     __syncthreads();
-    if (w < kJoinCols) {  // a warp for each channel
+    if (w < COLS) {  // a warp for each channel
         t = sh[lane][w];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-        if (lane == 0 && blockIdx.x * kJoinCols + w < C) out[blockIdx.x * kJoinCols + w] = (float)t;
+        if (lane == 0 && blockIdx.x * COLS + w < C) out[blockIdx.x * COLS + w] = (float)t;
     }
+}
+inline cudaError_t launch_rms_join(const float* part, int parts, int C, float* out, cudaStream_t st) {
+    return C <= 8 * 148 * 2 ? launch_after(rms_norm_join_kernel<8>, dim3((unsigned)ceil_div(C, 8)), dim3(kJoinThreads), 0, st, part, parts, C, out)
+                            : launch_after(rms_norm_join_kernel<32>, dim3((unsigned)ceil_div(C, 32)), dim3(kJoinThreads), 0, st, part, parts, C, out);
 }
 static __global__ void __launch_bounds__(256) rms_norm_no_rows_kernel(float* __restrict__ dgamma, int C) {
     wait_predecessor();
@@ -336,19 +356,32 @@ static cudaError_t launch_rms_backward_w(const RmsBackwardArgs& A, const RowsPla
     return p.wide ? launch_rms_backward_p<T, V, P, true, FULL>(A, p, parts, ctas, st) : launch_rms_backward_p<T, V, P, false, FULL>(A, p, parts, ctas, st);
 }
 constexpr int kRingRoom = 216 * 1024;  // of an SM's shared memory, for its CTAs' rings
-// The ring's plan: a thread's pieces such that they fill a CTA, or 0.
-inline int ring_pieces(int64_t rows, int64_t nv, int tensors) {
-    if (rows < 148 * 4 || 2 * tensors * nv * 16 > kRingRoom) return 0;
+// The ring's plan: pieces of a thread such that they fill a CTA; or 2 or 4 that do not; or none.  Two, where that is two warps or more, are the best (32760 x
+// 5120, 2, 4 pieces: 200, 206 us; 2048: 85, 91; 20000 x 2560: 68, 86), but not three warps, which leave one of an SM's four schedulers idle (1536: 91 us, 69 with 3 pieces
+// in two warps).
+struct BackwardRing {
+    int pieces, threads;
+    bool full;
+};
+inline BackwardRing backward_ring(int64_t rows, int64_t nv, int tensors) {
+    if (rows < 148 * 4 || 2 * tensors * (nv + 128) * 16 > kRingRoom) return {0, 0, false};  // threads beyond the row have slots too
     static const int order[] = {2, 4, 3, 5, 6, 7, 8, 0};
-    for (const int* k = order; *k; ++k) {
-        if (nv % (32 * *k) == 0 && nv / *k >= 64 && nv / *k <= ring_threads(*k)) return *k;
-    }
-    return 0;
+    for (const int* k = order; *k; ++k)
+        if (nv % (32 * *k) == 0 && nv / *k >= 64 && nv / *k != 96 && nv / *k <= ring_threads(*k)) return {*k, (int)(nv / *k), true};
+    // pieces that do not fill the threads: four in up to 224 threads if three quarters of the slots are used, else two (2, 4: 20000 x 1544 58.6, 51.4 us; 30000 x
+    // 2052 fp32 245, 171; 5000 x 8008 65.5, 73.0; 32760 x 1200, whose 150 pieces take 256 slots with four, 63.5 with two, 97 without a ring)
+    if (nv < 128) return {0, 0, false};
+    const int64_t four = align_up(ceil_div(nv, 4), 32), two = align_up(ceil_div(nv, 2), 32);
+    if (four >= 64 && four <= 224 && four * 3 <= nv) return {4, (int)four, false};
+    if (two <= ring_threads(2)) return {2, (int)two, false};
+    if (four <= ring_threads(4)) return {4, (int)four, false};
+    return {0, 0, false};
 }
-template <typename T, int V, int P>
-static cudaError_t launch_rms_backward_ring(const RmsBackwardArgs& A, int64_t parts, int* ctas_out, cudaStream_t st) {
-    const int threads = A.shape.C / (V * P), smem = 2 * (A.dh.p ? 3 : 2) * P * threads * 16;
-    auto kern = rms_norm_backward_ring_kernel<T, V, P>;
+template <typename T, int V, int P, bool FULL>
+static cudaError_t launch_rms_backward_ring(const RmsBackwardArgs& A, int threads, int64_t parts, int* ctas_out, cudaStream_t st) {
+    const int smem = 2 * (A.dh.p ? 3 : 2) * P * threads * 16;
+    if (smem > kRingRoom) return cudaErrorInvalidValue;  // not reached
+    auto kern = rms_norm_backward_ring_kernel<T, V, P, FULL>;
     static PerDevice<int> ready;
     if (!ready.get([&](int&, int) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingRoom) == cudaSuccess; }))
         return cudaErrorInvalidValue;
@@ -365,17 +398,20 @@ template <typename T, int V>
 static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts, int* ctas, cudaStream_t st) {
     constexpr bool kPieces16 = V * sizeof(T) == 16;
     if constexpr (kPieces16) {
-        const int pieces = A.dx.p && A.shape.C % V == 0 ? ring_pieces(A.shape.rows, A.shape.C / V, A.dh.p ? 3 : 2) : 0;
-        switch (pieces) {
-            case 0: break;
-            case 2: return launch_rms_backward_ring<T, V, 2>(A, parts, ctas, st);
-            case 3: return launch_rms_backward_ring<T, V, 3>(A, parts, ctas, st);
-            case 4: return launch_rms_backward_ring<T, V, 4>(A, parts, ctas, st);
-            case 5: return launch_rms_backward_ring<T, V, 5>(A, parts, ctas, st);
-            case 6: return launch_rms_backward_ring<T, V, 6>(A, parts, ctas, st);
-            case 7: return launch_rms_backward_ring<T, V, 7>(A, parts, ctas, st);
-            default: return launch_rms_backward_ring<T, V, 8>(A, parts, ctas, st);
+        const BackwardRing r = A.dx.p && A.shape.C % V == 0 ? backward_ring(A.shape.rows, A.shape.C / V, A.dh.p ? 3 : 2) : BackwardRing{0, 0, false};
+        if (r.full) {
+            switch (r.pieces) {
+                case 2: return launch_rms_backward_ring<T, V, 2, true>(A, r.threads, parts, ctas, st);
+                case 3: return launch_rms_backward_ring<T, V, 3, true>(A, r.threads, parts, ctas, st);
+                case 4: return launch_rms_backward_ring<T, V, 4, true>(A, r.threads, parts, ctas, st);
+                case 5: return launch_rms_backward_ring<T, V, 5, true>(A, r.threads, parts, ctas, st);
+                case 6: return launch_rms_backward_ring<T, V, 6, true>(A, r.threads, parts, ctas, st);
+                case 7: return launch_rms_backward_ring<T, V, 7, true>(A, r.threads, parts, ctas, st);
+                default: return launch_rms_backward_ring<T, V, 8, true>(A, r.threads, parts, ctas, st);
+            }
         }
+        if (r.pieces == 2) return launch_rms_backward_ring<T, V, 2, false>(A, r.threads, parts, ctas, st);
+        if (r.pieces == 4) return launch_rms_backward_ring<T, V, 4, false>(A, r.threads, parts, ctas, st);
     }
     // Rows whose pieces do not fill the threads: 4 (20000 x 1541, odd: 1, 2, 4, 8 pieces 478, 196, 119, 186 us; 30000 x 2049 fp32 666, 665, 333, 368).
     static const int order[] = {5, 3, 4, 2, 6, 7, 8, 1, 0};
