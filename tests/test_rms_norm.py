@@ -75,7 +75,7 @@ def reference(x, r, gamma, eps):
 
 @gpu
 @pytest.mark.parametrize("dt", DTYPES)
-@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("shape", SHAPES + [(700, 5, 96), (1, 700, 768), (3, 411, 1200), (1, 1300, 2048), (2, 300, 2560), (1, 300, 8960), (1, 200, 12288)])
 @pytest.mark.parametrize("layout,residual,params,outs", [("dense", True, "own", "hycr"), ("heads", False, "fp32", "y"), ("padded", True, "own", "hc"),
                                                          ("odd", False, None, "yc"), ("turned", True, "fp32", "hyr")])
 def test_forward(dt, shape, layout, residual, params, outs):
@@ -248,7 +248,8 @@ def gradient64(dy, h, rstd, gamma, dh):
 
 @gpu
 @pytest.mark.parametrize("dt", DTYPES)
-@pytest.mark.parametrize("shape", SHAPES + [(1, 5000, 320), (3000, 12, 128)])
+@pytest.mark.parametrize("shape", SHAPES + [(1, 5000, 320), (3000, 12, 128), (700, 5, 96), (1, 700, 768), (3, 211, 1200), (1, 1000, 1544), (2, 300, 2560), (1, 650, 8008),
+                                            (1, 620, 8960)])
 @pytest.mark.parametrize("layout,residual,params,outs", [("dense", True, "own", "xg"), ("heads", False, "fp32", "xg"), ("padded", True, None, "x"),
                                                          ("odd", False, "own", "g"), ("turned", True, "fp32", "xg")])
 def test_backward(dt, shape, layout, residual, params, outs):
