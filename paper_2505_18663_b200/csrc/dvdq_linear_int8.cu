@@ -27,7 +27,7 @@ using namespace dvdq;
 extern "C" {
 
 size_t dvdq_linear_int8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    if (!l8_sizes_ok(M, N, K) || M <= kL8FewTokens) return 0;
+    if (!l8_sizes_ok(M, N, K) || l8_few(M, N, K)) return 0;
     return (size_t)l8_plan(M, N, K).part_bytes;
 }
 
@@ -46,7 +46,7 @@ dvdq_status dvdq_linear_int8(const dvdq_linear_int8_args* args, void* stream) {
         return s;
     if (r.p == y.p && r.ld != y.ld) return DVDQ_ERR_SHAPE;  // in place: an output may not land on a residual still to be read
     if (!aligned_to(p.a_scales, 4) || !aligned_to(p.w_scales, 4) || (p.bias && !aligned_to(p.bias, 2))) return DVDQ_ERR_ALIGN;
-    const LinPlan plan = M <= kL8FewTokens ? LinPlan{} : l8_plan(M, N, K);
+    const LinPlan plan = l8_few(M, N, K) ? LinPlan{} : l8_plan(M, N, K);
     if (plan.part_bytes > 0) {
         if (!p.workspace) return DVDQ_ERR_NULL;
         if (!aligned_to(p.workspace, 256)) return DVDQ_ERR_ALIGN;

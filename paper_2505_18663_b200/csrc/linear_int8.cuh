@@ -10,7 +10,7 @@
 // What bounds it: the tensor pipe on layers of thousands of tokens, and with it the power cap: 32760 x 5120 -> 13824 with GELU takes 1037 us (4.47 PTOPS, the issue
 // loop's 4.43) when all codes are zero, and 1400-1840 (2.5-3.3 PTOPS) with codes of normal values, by the clock (the vendor library's bare product in the same
 // run 1670-1990).  8192 x 5120 -> 5120: tensor pipe 91 % active.  Short contractions: the epilogue (a tile of 256 x 256 outputs takes a pair 2.9 us, 4.6
-// with an activation, 4.3 with a residual in wide blocks; 12 k-blocks of products 3.4).  Few tokens: streaming W (1 token 5120 -> 13824 16.0 us, 4.4 TB/s).
+// with an activation, 4.3 with a residual in wide blocks; 12 k-blocks of products 3.4).  Few tokens: streaming W (1 token 5120 -> 13824 15.2 us, 4.7 TB/s).
 #pragma once
 
 #include "linear.cuh"
@@ -385,7 +385,19 @@ linear_int8_join_kernel(const int32_t* __restrict__ part, int64_t piece_ints, in
 
 // ------------------------------------------------------------------ a few tokens
 
-// M <= 8, as linear_few_kernel: mma.sync m16n8k32 with 16 rows of W as its A operand and 8 tokens as B.  A dot product does not care for the order
+// 16 warps to a group of 16 channels where an SM has two groups at most.
+inline bool l8_long_few(int64_t N, int64_t K) { return ceil_div(N, 16) <= 148 * 2 && K >= 1024; }
+
+// Which calls: up to 8 tokens all.  With 16 warps a group also up to 16 tokens, unless the rows are very long, and up to 32 where an SM has one group at
+// most (the kernel then takes its registers), unless they are long for so few groups: tiles cut them over all SMs.  Here and in tiles, in us: 16 tokens
+// 1536 -> 1536 2.7, 4.8; 2049 -> 4101 5.7, 6.2; 8192 -> 4096 11.0, 13.5; 13824 -> 512 7.7, 8.0; 20000 -> 1536 16.4, 13.5; other warps: 1024 -> 20000 10.8, 9.2,
+// 5120 -> 5120 11.0, 10.2.  32 tokens 1536 -> 1536 3.4, 4.9; 5120 -> 2304 6.6, 9.9; 8960 -> 1536 9.6, 10.7; 8960 -> 512 7.8, 7.1; two groups:
+// 3584 -> 3584 10.2, 7.8; fewer warps: 300 -> 300 4.8, 3.4.
+inline bool l8_few(int64_t M, int64_t N, int64_t K) {
+    return M <= 8 || (l8_long_few(N, K) && ((M <= 16 && K <= 16384) || (M <= 32 && N <= 148 * 16 && K <= 6 * N)));
+}
+
+// As linear_few_kernel: mma.sync m16n8k32 with 16 rows of W as its A operand and 8 tokens as B, NT times.  A dot product does not care for the order
 // of k, so a lane's 16 consecutive codes of a row fill its A slots of two MMAs, and the same 16 codes of a token its B slots.
 __device__ __forceinline__ void mma_16x8x32_i8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -410,10 +422,9 @@ __device__ __forceinline__ void l8_few_ahead(const int8_t* W, int64_t ldw, int n
         if (n0 + r < N && k < k1) asm volatile("prefetch.global.L2 [%0];" ::"l"(W + (int64_t)(n0 + r) * ldw + k));
 }
 
-constexpr int kL8FewTokens = 8;
 constexpr int kL8FewDepth = 6;
-template <typename T, int WARPS, int KS>
-__global__ void __launch_bounds__(WARPS * 32)
+template <typename T, int WARPS, int KS, int NT>
+__global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 32 / WARPS : 1)  // the CTAs that an SM holds where WARPS and KS are chosen
 linear_int8_few_kernel(const int8_t* __restrict__ X, int64_t ldx, const int8_t* __restrict__ W, int64_t ldw, int M, int N, int K, int k_per_warp,
                        const float* __restrict__ a_scales, const float* __restrict__ w_scales, const T* __restrict__ bias, const T* R, int64_t ldr,
                        int act, T* Y, int64_t ldy) {
@@ -424,7 +435,7 @@ linear_int8_few_kernel(const int8_t* __restrict__ X, int64_t ldx, const int8_t* 
     l8_few_ahead(W, ldw, n0, N, piece * k_per_warp, min(K, (piece + 1) * k_per_warp));
     wait_predecessor();
     release_successor();
-    int c[4] = {0, 0, 0, 0};
+    int c[NT][4] = {};
     if (n0 < N) {
         // rows past N repeat the last one: their results are not stored
         const int8_t* w0 = W + (int64_t)min(n0 + g, N - 1) * ldw;
@@ -432,11 +443,23 @@ linear_int8_few_kernel(const int8_t* __restrict__ X, int64_t ldx, const int8_t* 
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
         int k = piece * k_per_warp + t * 16;
         const int k1 = min(K, (piece + 1) * k_per_warp);  // k_per_warp is a multiple of 64
+        uint4 x[NT];  // the tokens' codes of the next step: asked for a step ahead (5120 -> 2304 8 tokens 4.8 -> 4.3 us, 8960 -> 1536 7.4 -> 6.5)
+        auto ask = [&]() {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) x[j] = 8 * j + g < M && k < k1 ? l8_few_load(X + (8 * j + g) * ldx, k, K) : none;
+        };
+        ask();
         auto step = [&](const uint4& a, const uint4& b) {
-            const uint4 x = g < M ? l8_few_load(X + g * ldx, k, K) : none;
-            mma_16x8x32_i8(c, a.x, b.x, a.y, b.y, x.x, x.y);
-            mma_16x8x32_i8(c, a.z, b.z, a.w, b.w, x.z, x.w);
+            uint4 now[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) now[j] = x[j];
             k += 64;
+            ask();
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                mma_16x8x32_i8(c[j], a.x, b.x, a.y, b.y, now[j].x, now[j].y);
+                mma_16x8x32_i8(c[j], a.z, b.z, a.w, b.w, now[j].z, now[j].w);
+            }
         };
         const int whole = k1 > k - t * 16 ? (k1 - (k - t * 16)) / 64 : 0;  // steps of 64 that lie in the rows
         thread_stream<kL8FewDepth, 2, int8_t, 16, WARPS * 32>(smem_u32(raw) + threadIdx.x * 16, whole, w0 + k, 64, w1 + k, 64,
@@ -448,12 +471,15 @@ linear_int8_few_kernel(const int8_t* __restrict__ X, int64_t ldx, const int8_t* 
     }
     __syncthreads();  // the ring's memory becomes the sums'
     int* sh = reinterpret_cast<int*>(raw);  // [warp][token][16]
-    constexpr int kTile = 8 * 16;
+    constexpr int kTile = NT * 8 * 16;
     int* mine = sh + warp * kTile + 2 * t * 16 + g;  // c = (row g, tokens 2t, 2t + 1), (row g + 8, the same)
-    mine[0] = c[0];
-    mine[16] = c[1];
-    mine[8] = c[2];
-    mine[24] = c[3];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        mine[j * 128] = c[j][0];
+        mine[j * 128 + 16] = c[j][1];
+        mine[j * 128 + 8] = c[j][2];
+        mine[j * 128 + 24] = c[j][3];
+    }
     __syncthreads();
     for (int o = threadIdx.x; o < (WARPS / KS) * kTile; o += WARPS * 32) {
         const int gr = o / kTile, r = o - gr * kTile, m = r >> 4, n = (blockIdx.x * (WARPS / KS) + gr) * 16 + (r & 15);
@@ -544,11 +570,12 @@ static dvdq_status launch_linear_int8_out(const LinMatrix& a, const LinMatrix& w
     return cuda_status(launch_after(kern, dim3(2 * pairs), dim3(kLinThreads), S::kTotal, st, maps, tmR, args));
 }
 
-template <typename T, int WARPS, int KS>
+template <typename T, int WARPS, int KS, int NT>
 static cudaError_t launch_linear_int8_few_w(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const L8Scales& sc,
                                             const LinEpilogue& e, const LinMatrix& y, cudaStream_t st) {
+    static_assert(NT * 8 * 16 * 4 <= 32 * 32 * kL8FewDepth, "the sums of a warp fit its rings");
     constexpr int smem = WARPS * 32 * 32 * kL8FewDepth;  // the rings; the sums take their place
-    auto kern = linear_int8_few_kernel<T, WARPS, KS>;
+    auto kern = linear_int8_few_kernel<T, WARPS, KS, NT>;
     static PerDevice<int> ready;
     if (smem > 48 * 1024 &&
         !ready.get([&](int&, int) { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess; }))
@@ -559,22 +586,25 @@ static cudaError_t launch_linear_int8_few_w(const LinMatrix& x, const LinMatrix&
                         static_cast<const T*>(e.residual.p), e.residual.ld, e.act, static_cast<T*>(const_cast<void*>(y.p)), y.ld);
 }
 // Warps that share 16 channels, as launch_linear_few chooses them.  In us, KS = 2, 4, 8, 16: 1 token 5120 -> 13824 22.9, 16.0, 18.3, 17.8 (71 MB: 10.8 at the copy
-// rate); 5120 -> 5120 20.5, 12.0, 9.0, 10.2; 8960 -> 1536 34.6, 18.7, 10.8, 6.9; 3 tokens 1536 -> 1536 7.5, 4.3, 3.2, 3.0.
+// rate); 5120 -> 5120 20.5, 12.0, 9.0, 10.2; 8960 -> 1536 34.6, 18.7, 10.8, 6.9; 3 tokens 1536 -> 1536 7.5, 4.3, 3.2, 3.0
+// (since then the tokens' codes are asked for a step ahead: 15.2, 8.8, 5.9 and 2.2 with the KS chosen).
 template <typename T>
 static dvdq_status launch_linear_int8_few(const LinMatrix& x, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const L8Scales& sc,
                                           const LinEpilogue& e, const LinMatrix& y, cudaStream_t st) {
     const int64_t groups = ceil_div(N, 16), wave = 148 * 4 * 8;
-    if (groups <= 148 * 2 && K >= 1024) return cuda_status(launch_linear_int8_few_w<T, 16, 16>(x, w, M, N, K, sc, e, y, st));
-    if (groups * 8 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 8>(x, w, M, N, K, sc, e, y, st));
-    if (groups * 4 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 4>(x, w, M, N, K, sc, e, y, st));
-    if (groups * 2 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 2>(x, w, M, N, K, sc, e, y, st));
-    return cuda_status(launch_linear_int8_few_w<T, 8, 1>(x, w, M, N, K, sc, e, y, st));
+    if (M > 16) return cuda_status(launch_linear_int8_few_w<T, 16, 16, 4>(x, w, M, N, K, sc, e, y, st));
+    if (M > 8) return cuda_status(launch_linear_int8_few_w<T, 16, 16, 2>(x, w, M, N, K, sc, e, y, st));
+    if (l8_long_few(N, K)) return cuda_status(launch_linear_int8_few_w<T, 16, 16, 1>(x, w, M, N, K, sc, e, y, st));
+    if (groups * 8 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 8, 1>(x, w, M, N, K, sc, e, y, st));
+    if (groups * 4 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 4, 1>(x, w, M, N, K, sc, e, y, st));
+    if (groups * 2 <= wave) return cuda_status(launch_linear_int8_few_w<T, 8, 2, 1>(x, w, M, N, K, sc, e, y, st));
+    return cuda_status(launch_linear_int8_few_w<T, 8, 1, 1>(x, w, M, N, K, sc, e, y, st));
 }
 
 template <typename T>
 static dvdq_status launch_linear_int8(const LinMatrix& a, const LinMatrix& w, int64_t M, int64_t N, int64_t K, const LinPlan& plan,
                                       const L8Scales& sc, const LinEpilogue& e, const LinMatrix& y, int32_t* part, cudaStream_t st) {
-    if (M <= kL8FewTokens) return launch_linear_int8_few<T>(a, w, M, N, K, sc, e, y, st);
+    if (l8_few(M, N, K)) return launch_linear_int8_few<T>(a, w, M, N, K, sc, e, y, st);
     if (plan.splits == 1) {
         // a tile is whole blocks for both warps
         if (e.residual.p && plan.bn % 128 == 0 && ceil_div(K, kL8BK) <= kL8WideMore) return launch_linear_int8_out<T, kLinFinalMore, true>(a, w, M, N, K, plan, sc, e, y, part, st);

@@ -98,6 +98,36 @@ def test_forward(dt, M, N, K, act, bias, residual):
     check(y, y6, inner + U[dt] * (y6.abs() + inner) + TINY[dt])
 
 
+# up to 16 and up to 32 tokens without tiles: whole and partial groups of 8 tokens and of 16 channels, rows that end in any warp; and in tiles: short rows,
+# many channels, rows too long for so few channels, 33 tokens
+FEW = [(9, 1, 1), (10, 17, 63), (12, 2368, 1024), (13, 40, 5003), (15, 4736, 1090), (16, 4737, 1500), (16, 100, 16384), (10, 40, 16385), (16, 5000, 200), (9, 9600, 333), (14, 19000, 70), (16, 38000, 130),
+       (17, 33, 65), (20, 2367, 1031), (24, 1540, 9237), (25, 171, 1024), (31, 1541, 515), (31, 1541, 1039), (32, 2368, 2100), (17, 2369, 1300), (32, 64, 9217), (33, 500, 1100)]
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("M,N,K", FEW)
+@pytest.mark.parametrize("act,bias,residual", [(0, False, False), (1, True, True), (2, False, True)])
+def test_nine_to_thirty_three_tokens(dt, M, N, K, act, bias, residual):
+    test_forward(dt, M, N, K, act, bias, residual)
+
+
+@gpu
+@pytest.mark.parametrize("N,K", [(520, 1100), (2304, 640), (6000, 300)])
+def test_a_token_among_nine_to_forty_has_the_bits_it_has_alone(N, K):
+    dt, g = torch.bfloat16, gen(N * 5 + K)
+    a, w = codes(40, K, g), codes(N, K, g)
+    s, t = torch.rand(40, device=DEV, generator=g) * 0.02, torch.rand(N, device=DEV, generator=g) / (100 * math.sqrt(K))
+    alone = padded(40, N, dt)
+    for m in range(40):
+        B.dvdq_linear_int8(a[m:m + 1], s[m:m + 1], w, t, None, None, 1, alone[m:m + 1], workspace(1, N, K))
+    for M in (9, 16, 17, 24, 32, 33, 40):
+        y = padded(M, N, dt)
+        B.dvdq_linear_int8(a[:M], s[:M], w, t, None, None, 1, y, workspace(M, N, K))
+        assert torch.equal(y, alone[:M]), M
+    status_ok()
+
+
 @gpu
 @pytest.mark.parametrize("M,N,K", [(1, 64, 131071), (5, 40, 131071), (40, 64, 131071), (300, 96, 131071)])
 def test_the_longest_sums_do_not_wrap(M, N, K):
