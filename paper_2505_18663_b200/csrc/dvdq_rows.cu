@@ -130,6 +130,7 @@ dvdq_status dvdq_rms_norm_backward(const dvdq_rms_norm_backward_args* args, void
     A.gamma = gamma;
     A.rstd = a.rstd;
     A.part = dgamma ? static_cast<float*>(a.workspace) : nullptr;
+    A.dgamma = dgamma;
     A.params_f32 = param_dtype == DVDQ_F32;
     A.inv_c = 1.0f / (float)C;
     const RowsOf* all[] = {&A.dy, &A.h, &A.dh, &A.dx};
@@ -138,7 +139,7 @@ dvdq_status dvdq_rms_norm_backward(const dvdq_rms_norm_backward_args* args, void
     const cudaError_t e = dtype == DVDQ_BF16  ? launch_rms_norm_backward_bf16(A, access, parts, &ctas, st)
                           : dtype == DVDQ_F16 ? launch_rms_norm_backward_f16(A, access, parts, &ctas, st)
                                               : launch_rms_norm_backward_f32(A, access, parts, &ctas, st);
-    if (e != cudaSuccess || !dgamma) return cuda_status(e);
+    if (e != cudaSuccess || !dgamma || ctas == 0) return cuda_status(e);  // no sums to add
     return cuda_status(launch_rms_join(A.part, ctas, (int)C, dgamma, st));
 }
 

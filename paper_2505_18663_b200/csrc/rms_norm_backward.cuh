@@ -3,7 +3,7 @@
 //   dh = gamma dy,  dx = q (dh - hh mean(dh hh)) + the residual stream's own gradient,  dgamma = sum over rows of dy hh,  hh = h q
 //
 // Laid out as the forward pass: a thread's channels are the same from row to row, so that dgamma's sums and gamma stay with it; each CTA
-// then writes one row of sums, and a second kernel adds those.  Bound by memory (dy, h, dh in, dx out): many rows come through a ring of cp.async, since
+// then writes one row of sums, and a second kernel adds those (few rows: dgamma by columns, below).  Bound by memory (dy, h, dh in, dx out): many rows come through a ring of cp.async, since
 // sums, gamma and inputs together leave too few warps to hide a row's latency.  Measured: 32760 x 5120 bf16 with dh 196 us (1342 MB, 6.8 TB/s),
 // 10000 x 16384 204 us (6.4 TB/s), 32760 x 12 heads of 128 53 us (5.7 TB/s), 20000 x 1541 (odd: single elements, no ring) 110 us (2.2 TB/s).
 #pragma once
@@ -18,6 +18,8 @@ struct RmsBackwardArgs {
     const void* gamma;
     const float* rstd;
     float* part;           // [CTAs, C]: each CTA's sums for dgamma; or NULL
+    float* dgamma;         // of the first column_ctas CTAs, which form it of columns; or NULL
+    int column_ctas;
     int params_f32;
     float inv_c;
     int lanes, lanes_log2;
@@ -50,20 +52,90 @@ __device__ __forceinline__ void sums_store(float* p, const Pairs<V>& f) {
     for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(f.get(j), f.get(j + 1), f.get(j + 2), f.get(j + 3));
 }
 
+// Few rows: no sums of CTAs and no second kernel. Given rstd, dgamma needs nothing of a row's other channels, so that CTAs of their own form it,
+// 32 or 64 bytes of each row, while the others form dx; dy and h are read twice, the second time from L2. In a graph, by columns and by sums of CTAs, in us:
+// 64 x 1536 bf16 1.8, 3.5; 509 x 1536 4.4, 8.1; 590 x 2560 5.0, 15.4; 512 x 5120 8.7, 17.4; 500 x 16384 30, 33; 509 x 1541 (single elements) 6.6, 6.7.
+template <typename T, int V>
+__host__ __device__ constexpr int column_lanes() { return V * sizeof(T) == 16 ? 4 : V * sizeof(T) == 2 ? 16 : 8; }
+constexpr int kColumnsBelow = 148 * 4;  // rows; from there on the ring
+constexpr int kColumnRows = 24;  // of a lane at most: its sum is one in fp32
+
+template <typename T, int V>
+__device__ __forceinline__ void rms_norm_columns(const RmsBackwardArgs& A, double* sums) {
+    constexpr int LN = column_lanes<T, V>(), COLS = LN * V, U = 4;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
+    const int C = A.shape.C, c = ((int)blockIdx.x * LN + lane % LN) * V;
+    const uint32_t rows = (uint32_t)A.shape.rows, step = (uint32_t)warps * (32 / LN);
+    Pairs<V> acc;
+#pragma unroll
+    for (int j = 0; j < Pairs<V>::N; ++j) acc.p[j] = 0ull;
+    auto run = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        for (uint32_t at = (uint32_t)(warp * (32 / LN) + lane / LN); at < rows; at += U * step) {
+            Piece<T, V> a[U], b[U];
+            float q[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t row = at + u * step;
+                q[u] = 0.f;
+                a[u].clear();
+                b[u].clear();
+                if (row < rows) {
+                    const uint32_t n = A.shape.by_s(row), s = row - n * (uint32_t)A.shape.S;
+                    a[u] = row_load<T, V, W>(static_cast<const T*>(A.dy.p) + row_at(A.dy, n, s), c, C);
+                    b[u] = row_load<T, V, W>(static_cast<const T*>(A.h.p) + row_at(A.h, n, s), c, C);
+                    q[u] = A.rstd[row];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Pairs<V> d = a[u].wide(), h = b[u].wide();
+#pragma unroll
+                for (int j = 0; j < Pairs<V>::N; ++j) acc.p[j] = f2_fma(d.p[j], f2_mul(h.p[j], f2_splat(q[u])), acc.p[j]);
+            }
+        }
+    };
+    if (c + V <= C) run(Whole());
+    else if (c < C) run(Part());
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        double t = acc.get(j);
+#pragma unroll
+        for (int o = LN; o < 32; o *= 2) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+        if (lane < LN) sums[warp * COLS + lane * V + j] = t;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < COLS; i += blockDim.x) {
+        double t = 0.0;
+        for (int w = 0; w < warps; ++w) t += sums[w * COLS + i];
+        if ((int)blockIdx.x * COLS + i < C) A.dgamma[blockIdx.x * COLS + i] = (float)t;
+    }
+}
+
 // Registers of a thread, and with them threads of a CTA at most.
 __host__ __device__ constexpr int rows_registers_backward(int V, int P) { return P * V > 40 ? 255 : P * V > 24 ? 168 : P * V > 8 ? 128 : 64; }
 __host__ __device__ constexpr int rows_threads_backward(int V, int P) { return 65536 / rows_registers_backward(V, P) / 32 * 32; }
 
 // A thread's channels are the same in every row that it meets, so dgamma's sums stay with it (P > 0: in registers; P = 0: in the CTA's own
 // row of `part`) until the CTA has been through its rows.  FULL: dX is asked for, and every thread has P whole pieces.
-template <typename T, int V, int P, bool WIDE, bool FULL>
+// COLUMNS: the first CTAs are those of dgamma's columns (their code in the others' kernel costs those 8 registers).
+template <typename T, int V, int P, bool WIDE, bool FULL, bool COLUMNS>
 __global__ void __maxnreg__(rows_registers_backward(V, P))
 rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     constexpr int N = Pairs<V>::N, K = P > 0 ? P : 1, U = !WIDE && P > 0 && P <= 2 ? 2 : 1;
     constexpr bool KEEP = P > 0 && P * V <= 16;
     constexpr int KIND = (FULL ? kFull : 0) | (WIDE ? kWide : 0);
     __shared__ float2 slots[64];
-    extern __shared__ float joined[];
+    extern __shared__ __align__(16) float joined[];
+    if constexpr (COLUMNS)
+        if ((int)blockIdx.x < A.column_ctas) {
+            wait_predecessor();
+            release_successor();
+            rms_norm_columns<T, V>(A, reinterpret_cast<double*>(joined));
+            return;
+        }
+    const int before = COLUMNS ? A.column_ctas : 0, cta = (int)blockIdx.x - before, ctas = (int)gridDim.x - before;
     const int lanes = WIDE ? (int)blockDim.x : A.lanes, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
     const int groups = WIDE ? 1 : kSmallThreads >> A.lanes_log2, group = WIDE ? 0 : (int)threadIdx.x >> A.lanes_log2;
     const int C = A.shape.C;
@@ -75,13 +147,13 @@ rms_norm_backward_kernel(const __grid_constant__ RmsBackwardArgs A) {
     for (int i = 0; i <= K; ++i)
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[i].p[j] = 0ull;
-    float* mine = A.part ? A.part + (int64_t)blockIdx.x * C : nullptr;
+    float* mine = !COLUMNS && A.part ? A.part + (int64_t)cta * C : nullptr;
     wait_predecessor();
     release_successor();
     RowGamma<T, V, P, KIND, KEEP> gamma;
     gamma.init(L, A.gamma, A.params_f32);
     bool first = true;
-    for (int64_t at = (int64_t)blockIdx.x * (groups * U); at < A.shape.rows; at += (int64_t)gridDim.x * (groups * U)) {
+    for (int64_t at = (int64_t)cta * (groups * U); at < A.shape.rows; at += (int64_t)ctas * (groups * U)) {
         Piece<T, V> a[U][K + 1], b[U][K + 1], e[U][K + 1];  // dy, h, dh; the last: the row's end
         const T *dy[U], *h[U], *dh[U];
         T* dx[U];
@@ -336,18 +408,41 @@ inline int64_t rms_parts(int64_t rows, int64_t C) {
 
 // ------------------------------------------------------------------ launches
 
+// dgamma by columns: few rows of a lane (at_once: rows that a CTA's lanes take side by side), and few enough bytes for their second reading. Above 16 MB, and 2 MB of
+// single elements, the sums of CTAs cost less: 590 x 8960 fp32 20 us, 27 by columns; 300 x 2049 fp32 7.3, 8.3; 500 x 5121 bf16 25, 32.
+inline bool rms_by_columns(int64_t rows, int64_t C, int bytes, int v, int at_once) {
+    return rows < kColumnsBelow && ceil_div(rows, at_once) <= kColumnRows && rows * C * bytes <= (int64_t)(v > 2 ? 16 : 2 * v) << 20;
+}
+
 template <typename T, int V, int P, bool WIDE, bool FULL>
 static cudaError_t launch_rms_backward_p(const RmsBackwardArgs& A0, const RowsPlan& p, int64_t parts, int* ctas_out, cudaStream_t st) {
     RmsBackwardArgs A = A0;
     A.lanes = p.lanes;
     A.lanes_log2 = p.lanes_log2;
-    auto kern = rms_norm_backward_kernel<T, V, P, WIDE, FULL>;
+    const int groups = WIDE ? 1 : kSmallThreads / p.lanes;
+    const int64_t all = ceil_div(A.shape.rows, groups);
+    if constexpr (P > 0) {
+        constexpr int LN = column_lanes<T, V>();
+        if (A.dgamma && rms_by_columns(A.shape.rows, A.shape.C, (int)sizeof(T), V, p.threads / LN)) {
+            auto kern = rms_norm_backward_kernel<T, V, P, WIDE, FULL, true>;
+            const int columns = (int)ceil_div(A.shape.C, LN * V);
+            const size_t sums = (size_t)(p.threads / 32) * LN * V * 8;
+            A.part = nullptr;
+            A.column_ctas = columns;
+            *ctas_out = 0;
+            if (!A.dx.p) return launch_after(kern, dim3((unsigned)columns), dim3(p.threads), sums, st, A);
+            if (A.dx.p != A.dy.p && A.dx.p != A.h.p) return launch_after(kern, dim3((unsigned)(columns + all)), dim3(p.threads), sums, st, A);
+            const cudaError_t e = launch_after(kern, dim3((unsigned)columns), dim3(p.threads), sums, st, A);  // in place the columns come first
+            if (e != cudaSuccess) return e;
+            A.column_ctas = 0;
+            return launch_after(kern, dim3((unsigned)all), dim3(p.threads), 0, st, A);
+        }
+    }
+    auto kern = rms_norm_backward_kernel<T, V, P, WIDE, FULL, false>;
     static PerDevice<RowsHeld> cache;
     const int held = rows_held(cache, kern, p.threads);
     if (held == 0) return cudaErrorInvalidValue;
-    const int groups = WIDE ? 1 : kSmallThreads / p.lanes;
-    int64_t ctas = ceil_div(A.shape.rows, groups);
-    ctas = ctas < 148 * held ? ctas : 148 * held;
+    int64_t ctas = all < 148 * held ? all : 148 * held;
     if (A.part && ctas > parts) ctas = parts;
     *ctas_out = (int)ctas;
     const size_t sums = A.part && groups > 1 ? (size_t)groups * A.shape.C * 4 : 0;  // of 128 threads with 8 pieces at most: 32 KB
@@ -417,9 +512,25 @@ static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts
     }
     // Rows whose pieces do not fill the threads: 4 (20000 x 1541, odd: 1, 2, 4, 8 pieces 478, 196, 119, 186 us; 30000 x 2049 fp32 666, 665, 333, 368).
     static const int order[] = {5, 3, 4, 2, 6, 7, 8, 1, 0};
-    const RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0 && A.dx.p, 2, 8, 4,
+    RowsPlan p = rows_plan(A.shape.rows, ceil_div(A.shape.C, V), kPieces16 && A.shape.C % V == 0 && A.dx.p, 2, 8, 4,
                                  [](int k) { return rows_threads_backward(V, k); }, order);
     if constexpr (kPieces16) {
+        // Few rows, dgamma by columns: the pieces with which the CTAs of rows and columns come in the fewest rounds, and of those the fewest
+        // (1, 2, 5 pieces: 509 x 1536 4.5, 8.4 (3 pieces), - us; 512 x 5120 11.1, 11.4, 9.3; 590 x 2560 5.4, 15.5 (5, which is too few threads for columns))
+        if (p.full && p.wide && A.dgamma && A.shape.rows < kColumnsBelow) {
+            const int64_t nv = A.shape.C / V, ctas = A.shape.rows + ceil_div(nv, column_lanes<T, V>());
+            int64_t least = INT64_MAX;
+            for (int k = 1; k <= 8; ++k) {
+                const int64_t threads = nv / k;
+                if (nv % (32 * k) != 0 || threads < 64 || threads > kRowThreads || threads > rows_threads_backward(V, k)) continue;
+                if (!rms_by_columns(A.shape.rows, A.shape.C, (int)sizeof(T), V, (int)threads / column_lanes<T, V>())) continue;
+                const int64_t rounds = ceil_div(ctas, 148 * (65536 / (rows_registers_backward(V, k) * threads)));
+                if (rounds >= least) continue;
+                least = rounds;
+                p.pieces = k;
+                p.lanes = p.threads = (int)threads;
+            }
+        }
         if (p.full) {
             switch (p.pieces) {
                 case 1: return launch_rms_backward_w<T, V, 1, true>(A, p, parts, ctas, st);

@@ -290,6 +290,57 @@ def test_backward_in_place_and_again_the_same_bits(dt):
         assert torch.equal(t[i], dx) and torch.equal(dg2, dg)
 
 
+# dgamma by columns: whole and partial groups of columns and of rows, single elements and pieces, every number of lanes to a row; and where sums of CTAs
+# take over (rows, rows a lane, bytes)
+FEW_ROWS = [(1, 2, 64), (1, 96, 33), (1, 512, 1536), (1, 591, 2560), (1, 592, 2560), (1, 577, 128), (49, 12, 72), (1, 590, 40), (1, 300, 5120), (1, 100, 16384), (1, 590, 1541),
+            (3, 130, 1542), (2, 256, 8192), (1, 591, 14336), (1, 60, 12001)]
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("shape", FEW_ROWS)
+@pytest.mark.parametrize("layout,residual,params,outs", [("dense", True, "own", "xg"), ("heads", False, "fp32", "xg"), ("odd", True, "own", "xg"), ("padded", False, None, "g")])
+def test_gradients_of_few_rows(dt, shape, layout, residual, params, outs):
+    """A lane adds 24 products at most in fp32, and doubles join the lanes: 26 E of the bound's 40."""
+    test_backward(dt, shape, layout, residual, params, outs)
+
+
+@gpu
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 509, 1536), (1, 70, 131), (30, 12, 64), (1, 128, 5120)])
+def test_few_rows_in_place_have_the_same_bits(dt, shape):
+    g, C = gen(8), shape[-1]
+    dy, h, dh = (torch.randn(shape, device=DEV, generator=g).to(dt) for _ in range(3))
+    rstd = (h.double().square().mean(-1) + 1e-6).rsqrt().float()
+    gamma = torch.randn(C, device=DEV, generator=g)
+    ws = torch.empty(B.dvdq_rms_norm_backward_workspace_bytes(*shape), dtype=torch.uint8, device=DEV)
+    dx, dg = torch.empty_like(h), torch.empty(C, device=DEV)
+    B.dvdq_rms_norm_backward(dy, h, rstd, gamma, dh, dx, dg, ws)
+    for i in range(3):
+        for _ in range(3):
+            t = [dy.clone(), h.clone(), dh.clone()]
+            dg2 = torch.empty(C, device=DEV)
+            B.dvdq_rms_norm_backward(t[0], t[1], rstd, gamma, t[2], t[i], dg2, ws.fill_(255))
+            assert torch.equal(t[i], dx) and torch.equal(dg2, dg)
+    status_ok()
+
+
+@gpu
+def test_a_row_that_is_not_finite_leaves_the_other_columns_of_dgamma():
+    g = gen(9)
+    for C in (1536, 131):
+        dy, h = (torch.randn(1, 200, C, device=DEV, generator=g) for _ in range(2))
+        rstd, ws = torch.ones(1, 200, device=DEV), torch.empty(B.dvdq_rms_norm_backward_workspace_bytes(1, 200, C), dtype=torch.uint8, device=DEV)
+        clean, dg, dx = torch.empty(C, device=DEV), torch.empty(C, device=DEV), torch.empty_like(h)
+        B.dvdq_rms_norm_backward(dy, h, rstd, None, None, dx, clean, ws)
+        h[0, 199, 7], dy[0, 3, 100] = float("inf"), float("nan")
+        B.dvdq_rms_norm_backward(dy, h, rstd, None, None, dx, dg, ws)
+        assert dg[7].isinf() and dg[100].isnan()
+        keep = torch.ones(C, dtype=torch.bool, device=DEV)
+        keep[[7, 100]] = False
+        assert torch.equal(dg[keep], clean[keep])
+
+
 @gpu
 def test_gradients_are_those_of_the_forward_pass_by_differences():
     g = gen(7)
