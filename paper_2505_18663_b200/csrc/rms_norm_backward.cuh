@@ -486,7 +486,10 @@ static cudaError_t launch_rms_backward_ring(const RmsBackwardArgs& A, int thread
     const int by_registers = 65536 / (ring_registers(P) * threads);
     if (held > by_registers) held = by_registers;
     if (held < 1) held = 1;
-    int64_t ctas = A.shape.rows < 148 * held ? A.shape.rows : 148 * held;
+    // with dgamma three rows a CTA at least: its sums, written and read, are as many bytes as a row (with up to 148 * held CTAs, three rows, eight, in us:
+    // 600 x 1536 9.4, 6.3, 7.3; 1000 x 1536 11.1, 8.7, 10.0; 2000 x 1536 14.9, 13.2, 12.5; 4000 x 1536 17.5, 16.9, 19.6)
+    const int64_t most = A.part ? ceil_div(A.shape.rows, 3) : A.shape.rows;
+    int64_t ctas = most < 148 * held ? most : 148 * held;
     if (A.part && ctas > parts) ctas = parts;
     *ctas_out = (int)ctas;
     return launch_after(kern, dim3((unsigned)ctas), dim3(threads), (size_t)smem, st, A);
