@@ -100,8 +100,51 @@ __device__ __forceinline__ void rows_load(const RowLanes<V, P, KIND>& L, RowValu
     }
 }
 
-// Codes of V channels: y * inv, rounded to a whole number in the one rounding of its addition to 1.5 * 2^23, whose last byte then is the
-// code.  |y| inv is at most 127 (1 + 2^-22).
+// What turns a row's values into codes, c = round_half_even(v / scale) with the scale that is written.
+//
+// Plain rows are multiplied by `inv`, 127 / top to 2^-23.  Of a row in 16 bits no value lies that near a border without lying on it (254 v and (2 n + 1) top are
+// multiples of one number), and on it, 254 v = (2 n + 1) top, only if it is half of the largest value, n = 63, or if top is a multiple of 127.  So inv is the
+// neighbour of 127 / top above it or below it, whichever gives top / 2 the code of its quotient in fp32 (127 / top rounded to nearest gave it the other code in
+// half of all rows), and rows whose top / 127 is exact, but not 127 / top, are divided, as are rows far from one or near the smallest numbers.
+// (All rows by a corrected reciprocal: 32760 x 8960 142 us, 134 this way.)
+struct RowCodes {
+    float scale, inv;   // as written; the factor of plain rows
+    bool plain;
+    __device__ __forceinline__ RowCodes(const RowScale& o) : inv(0.f), plain(false) {
+        const float top = o.top;
+        scale = __uint_as_float(0x7FC00000u);
+        if (top <= 3.4028235e38f) scale = top / 127.0f;  // not NaN, not infinite
+        if (!(o.f == 1.0f && top >= kLiftBelow && top <= 3.4028235e38f)) return;
+        const float rest = fmaf(-63.5f, scale, 0.5f * top);  // of top / 2 over 63.5 steps, exact
+        plain = rest != 0.f || (__float_as_uint(scale) & 0x7FFFFFu) == 0u;
+        inv = 127.0f / top;
+        const float over = fmaf(inv, top, -127.0f);
+        // (top / 2) / scale in fp32 is 63.5 or more down to half a unit of its last place, 2^-19, below
+        const bool up = rest >= scale * -0x1p-19f;
+        if (up ? over < 0.f : over > 0.f) inv = __uint_as_float(__float_as_uint(inv) + (up ? 1u : 0xFFFFFFFFu));
+    }
+    static constexpr float kLiftBelow = 1e-27f;
+};
+// Quotients of values by a row's scale, those of a division in fp32: from the reciprocal, corrected once by the remainder (Markstein 1990; for the mantissa of every scale
+// and the values around each of its borders the codes were compared with the division's).  Zeros where the row has no scale.  Values near the smallest numbers are
+// lifted first, so that the reciprocal stays finite and remainders have all their digits.
+struct RowDivide {
+    float lift, step, recip;
+    __device__ __forceinline__ RowDivide(float top) : lift(0.f), step(1.f), recip(0.f) {
+        if (!(top > 0.f && top <= 3.4028235e38f)) return;
+        lift = top < RowCodes::kLiftBelow ? 18446744073709551616.0f : 1.0f;
+        step = top * lift / 127.0f;
+        recip = 1.0f / step;
+    }
+    __device__ __forceinline__ uint64_t operator()(uint64_t v) const {
+        if (lift == 0.f) return 0ull;
+        const uint64_t y = f2_mul(v, f2_splat(lift)), q = f2_mul(y, f2_splat(recip));
+        return f2_fma(f2_fma(q, f2_splat(-step), y), f2_splat(recip), q);
+    }
+};
+
+// Codes of V channels: y * inv (inv = 1: y is a quotient), rounded to a whole number in the one rounding of its addition to 1.5 * 2^23, whose last byte
+// then is the code.  |y| inv is at most 127 (1 + 2^-22).
 template <int V, bool WHOLE>
 __device__ __forceinline__ void codes_store(int8_t* p, int c, int C, const Pairs<V>& y, float inv, bool there) {
     constexpr int N = Pairs<V>::N;
@@ -207,15 +250,13 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P,
     constexpr int N = Pairs<V>::N;
     const int C = A.shape.C;
     if (NORM && A.rstd && L.lane == 0) A.rstd[index] = o.q * o.f;
-    // codes are y lift inv; a row near the smallest numbers is lifted first, so that 127 / top stays finite
-    float lift = 0.f, inv = 0.f;
+    bool plain = o.f == 1.0f;
+    float inv = 0.f;
     if (codes) {
-        const bool finite = o.top <= 3.4028235e38f;  // not NaN, not infinite
-        if (finite && o.top > 0.f) {
-            lift = o.top < 1e-30f ? 18446744073709551616.0f : 1.0f;
-            inv = 127.0f / (o.top * lift);
-        }
-        if (L.lane == 0) A.scales[index] = finite ? o.top / 127.0f : __uint_as_float(0x7FC00000u);
+        const RowCodes k(o);
+        if (L.lane == 0) A.scales[index] = k.scale;
+        plain = k.plain;
+        inv = k.inv;
     }
     T* to_h = NORM && A.h.p ? static_cast<T*>(A.h.p) + row_at(A.h, n, s) : nullptr;
     T* to_y = NORM && A.y.p ? static_cast<T*>(A.y.p) + row_at(A.y, n, s) : nullptr;
@@ -224,29 +265,54 @@ __device__ __forceinline__ void row_write(const RmsArgs& A, const RowLanes<V, P,
         if (to_h) row.visit(L, [&](int, int c, const Pairs<V>& h, auto whole, bool there) { row_store<T, V, decltype(whole)::value>(to_h, c, C, h, there); });
         if (!to_y && !codes) return;
     }
-    const bool plain = o.f == 1.0f && lift == 1.0f;  // else: far from one, near the smallest numbers, zeros or not finite
-    row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole, bool there) {
-        constexpr bool W = decltype(whole)::value;
-        if (P == 0 && to_h) row_store<T, V, W>(to_h, c, C, h, there);
-        Pairs<V> y = h;
-        if (NORM) {
-            if (o.f != 1.0f) {
+    auto write = [&](auto is_plain, const auto& divide) {
+        constexpr bool PLAIN = decltype(is_plain)::value;
+        row.visit(L, [&](int i, int c, const Pairs<V>& h, auto whole, bool there) {
+            constexpr bool W = decltype(whole)::value;
+            if (P == 0 && to_h) row_store<T, V, W>(to_h, c, C, h, there);
+            Pairs<V> y = h;
+            if (NORM) {
+                if (!PLAIN) {
 #pragma unroll
-                for (int j = 0; j < N; ++j) y.p[j] = f2_mul(y.p[j], f2_splat(o.f));
+                    for (int j = 0; j < N; ++j) y.p[j] = f2_mul(y.p[j], f2_splat(o.f));
+                }
+                const Pairs<V> g = gamma.template get<W>(i, c);
+#pragma unroll
+                for (int j = 0; j < N; ++j) y.p[j] = f2_mul(f2_mul(y.p[j], f2_splat(o.q)), g.p[j]);
             }
-            const Pairs<V> g = gamma.template get<W>(i, c);
+            if (to_y) row_store<T, V, W>(to_y, c, C, y, there);
+            if (codes) {
+                if constexpr (!PLAIN) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) y.p[j] = f2_mul(f2_mul(y.p[j], f2_splat(o.q)), g.p[j]);
-        }
-        if (to_y) row_store<T, V, W>(to_y, c, C, y, there);
-        if (codes) {
-            if (!plain) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) y.p[j] = lift == 0.f ? 0ull : f2_mul(y.p[j], f2_splat(lift));
+                    for (int j = 0; j < N; ++j) y.p[j] = divide(y.p[j]);
+                }
+                codes_store<V, W>(to_c, c, C, y, PLAIN ? inv : 1.0f, there);
             }
-            codes_store<V, W>(to_c, c, C, y, inv, there);
+        });
+    };
+    if constexpr (!NORM && P > 0) {
+        if (plain) {
+            write(Whole(), 0);
+            return;
         }
-    });
+        // read again, piece by piece (from registers: up to 34 more of them, 32760 x 8960 190 us, for the values are kept in their own type until here)
+        const RowDivide divide(o.top);
+        auto again = [&](int c, auto whole) {
+            constexpr bool W = decltype(whole)::value;
+            Pairs<V> y = row.template get<W>(c, C);
+#pragma unroll
+            for (int j = 0; j < N; ++j) y.p[j] = divide(y.p[j]);
+            codes_store<V, W>(to_c, c, C, y, 1.0f, true);
+        };
+#pragma unroll 1
+        for (int i = 0; i < P; ++i)
+            if (L.has(i)) again(L.channel(i), Whole());
+        if (!L.FULL && V > 1 && L.tail) again(L.end(), Part());
+    } else if (plain) {
+        write(Whole(), 0);
+    } else {
+        write(Part(), RowDivide(o.top));
+    }
 }
 
 // Rows that a thread has in hand at once (more warps are worth more than more rows a warp: 32760 x 12 heads of 128 channels, two pieces a thread, 1, 2, 4 rows: 34.6, 38.8, 37.1 us).
