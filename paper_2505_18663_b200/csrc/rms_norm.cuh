@@ -114,6 +114,7 @@ struct RowCodes {
         const float top = o.top;
         scale = __uint_as_float(0x7FC00000u);
         if (top <= 3.4028235e38f) scale = top / 127.0f;  // not NaN, not infinite
+        plain = o.f == 1.0f && top == 0.f;               // zeros
         if (!(o.f == 1.0f && top >= kLiftBelow && top <= 3.4028235e38f)) return;
         const float rest = fmaf(-63.5f, scale, 0.5f * top);  // of top / 2 over 63.5 steps, exact
         plain = rest != 0.f || (__float_as_uint(scale) & 0x7FFFFFu) == 0u;
@@ -181,32 +182,36 @@ __device__ __forceinline__ float root(float m) {
 }
 
 // Squares that left fp32's range, or an h gamma that did: the row once more, from memory, with f h, f a power of two that brings the largest
-// |h| (or sqrt(eps), where that is larger) to 1.
-template <typename T, typename Lanes, typename Meet>
-__device__ __forceinline__ RowScale row_far(const RmsArgs& A, const Lanes& L, const T* x, const T* r, Meet& meet) {
-    float f = 1.0f, q = 1.0f, a = 0.f;
+// |h| (or sqrt(eps), where that is larger) to 1, and with y formed as it is written.  `top`: max |h gamma| as row_decide found it; `far`: whether this row needs it.
+template <bool WIDE, typename T, int V, int P, int KIND>
+__device__ __forceinline__ RowScale row_far(const RmsArgs& A, const RowLanes<V, P, KIND>& L, RowValues<T, V, P, KIND>& row, RowMeet<WIDE>& meet, float top, bool far) {
+    float largest = 0.f;
+    row.visit(L, [&](int, int, const Pairs<V>& h, auto, bool) {
+#pragma unroll
+        for (int j = 0; j < Pairs<V>::N; ++j) largest = max_abs2(largest, h.p[j]);
+    });
+    largest = meet(0.f, largest, true).y;
+    RowScale o{1.0f / sqrtf(A.eps), 1.0f, top};  // a row of zeros
+    const bool zeros = largest == 0.f && A.eps > 0.f;
+    if (WIDE ? zeros : __all_sync(0xFFFFFFFFu, zeros || !far)) return o;
+    largest = fmaxf(largest, sqrtf(A.eps));
+    o.f = largest <= 3.4028235e38f && largest > 0.f ? bring_to_one(largest) : 1.0f;
 #pragma unroll 1
-    for (int turn = 0; turn < 3; ++turn) {  // largest |h|; sum of squares; largest |y|
-        a = 0.f;
+    for (int turn = 0; turn < 2; ++turn) {  // sum of squares; largest |y|
+        float a = 0.f;
 #pragma unroll 1
         for (int c = L.lane; c < L.C; c += L.lanes) {
-            float h = to_f32(x[c]);
-            if (r) h += to_f32(r[c]);
-            h *= f;
-            if (turn == 0) a = max_nan(a, fabsf(h));
-            else if (turn == 1) a = fmaf(h, h, a);
-            else a = max_nan(a, fabsf(h * q * gamma_at<T>(A.gamma, A.params_f32, c)));
+            float h = to_f32(row.x[c]);
+            if (row.r) h += to_f32(row.r[c]);
+            h *= o.f;
+            if (turn == 0) a = fmaf(h, h, a);
+            else a = max_nan(a, fabsf(h * o.q * gamma_at<T>(A.gamma, A.params_f32, c)));
         }
-        const float2 all = meet(a, a, turn != 1);
-        if (turn == 0) {
-            const float largest = fmaxf(all.y, sqrtf(A.eps));
-            f = largest <= 3.4028235e38f && largest > 0.f ? bring_to_one(largest) : 1.0f;
-        } else if (turn == 1) {
-            q = 1.0f / sqrtf(fmaf(all.x, A.inv_c, A.eps * f * f));
-        }
-        a = all.y;
+        const float2 all = meet(a, a, turn == 1);
+        if (turn == 0) o.q = 1.0f / sqrtf(fmaf(all.x, A.inv_c, A.eps * o.f * o.f));
+        else o.top = all.y;
     }
-    return RowScale{q, f, a};
+    return o;
 }
 
 // The row's q and top.  CODES: whether the output in 8 bits is asked for.
@@ -235,10 +240,11 @@ __device__ __forceinline__ RowScale row_decide(const RmsArgs& A, const RowLanes<
     const float m = fmaf(all.x, A.inv_c, A.eps);
     o.q = root(m);
     o.top *= o.q;
+    // (An h gamma below 2^-126 has not all its digits: y, which is (h q) gamma, may be larger than q times the largest of them, or be there without one.)
     // The rows of a warp take the turn together and keep what is theirs.
-    const bool far = !(m > 1e-30f && m < 1e30f && o.top < 3e38f);
+    const bool far = !(m > 1e-30f && m < 1e30f && o.top < 3e38f) || (codes && all.y < 1e-30f);
     if (WIDE ? far : __any_sync(0xFFFFFFFFu, far)) {
-        const RowScale again = row_far<T>(A, L, row.x, row.r, meet);
+        const RowScale again = row_far<WIDE, T>(A, L, row, meet, all.y, far);
         if (far) o = again;
     }
     return o;
