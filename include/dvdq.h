@@ -437,7 +437,8 @@ dvdq_status dvdq_group_norm_backward(const void* dY, int64_t dy_sample, int64_t 
  *             codes and scales come together, and something is asked for
  * h, y and c are computed in fp32 and rounded once each: y and c come from the h that is not yet rounded.  c has the code of the fp32 quotient of y and the s
  * that is written wherever y is half of an odd number of max |y| / 127, and everywhere for rows of 16-bit values (dvdq_quantize_rows); elsewhere the quotient may
- * be off by 2^-22 of itself, and next to a border c is one of the two codes beside it.  Rows of values whose squares
+ * be off by 2^-22 of itself, and next to a border c is one of the two codes beside it.  (A scale below 2^-126 is
+ * a multiple of 2^-149 like any number there: codes count it as it is written, up to 127 of it, and a row whose scale is 0 has codes 0.)  Rows of values whose squares
  * leave fp32's range are scaled by a power of two first.  A row of zeros has scale 0 and codes 0; a row whose y holds a value that
  * is not finite has scale NaN and codes 0.
  * H may be X or R itself, Y may be X or R itself (same pitches, not both the same one); apart from that outputs overlap nothing.

@@ -128,19 +128,23 @@ struct RowCodes {
 };
 // Quotients of values by a row's scale, those of a division in fp32: from the reciprocal, corrected once by the remainder (Markstein 1990; for the mantissa of every scale
 // and the values around each of its borders the codes were compared with the division's).  Zeros where the row has no scale.  Values near the smallest numbers are
-// lifted first, so that the reciprocal stays finite and remainders have all their digits.
+// lifted first, so that the reciprocal stays finite and remainders have all their digits; a scale below 2^-126 has few digits itself, so that quotients by it may
+// pass 127, where codes end.
 struct RowDivide {
     float lift, step, recip;
     __device__ __forceinline__ RowDivide(float top) : lift(0.f), step(1.f), recip(0.f) {
-        if (!(top > 0.f && top <= 3.4028235e38f)) return;
+        const float scale = top <= 3.4028235e38f ? top / 127.0f : 0.f;
+        if (scale == 0.f) return;
         lift = top < RowCodes::kLiftBelow ? 18446744073709551616.0f : 1.0f;
-        step = top * lift / 127.0f;
+        step = scale * lift;
         recip = 1.0f / step;
     }
     __device__ __forceinline__ uint64_t operator()(uint64_t v) const {
         if (lift == 0.f) return 0ull;
         const uint64_t y = f2_mul(v, f2_splat(lift)), q = f2_mul(y, f2_splat(recip));
-        return f2_fma(f2_fma(q, f2_splat(-step), y), f2_splat(recip), q);
+        float a, b;
+        f2_unpack(f2_fma(f2_fma(q, f2_splat(-step), y), f2_splat(recip), q), a, b);
+        return f2_pack(fminf(fmaxf(a, -127.f), 127.f), fminf(fmaxf(b, -127.f), 127.f));
     }
 };
 

@@ -102,3 +102,26 @@ def test_codes_of_the_norm_are_those_of_its_output(shape, residual, gamma):
     B.dvdq_rms_norm(x, r if residual else None, w, 1e-6, None, y, c, s)
     assert gamma or tie(y).any()
     check_codes(c, y, s)
+
+
+@gpu
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("C", [5, 64, 1541])
+def test_scales_among_the_smallest_numbers(dt, C):
+    """A scale below 2^-126 is a multiple of 2^-149: codes count that scale, so that c s is within half of it of y, or, where y is more than 127 of it, as near as 127 steps come
+    (s is at most 2^-150 below max |y| / 127).  No scale, no codes."""
+    g = torch.Generator().manual_seed(C)
+    units = torch.cat([torch.arange(1, 400), torch.randint(400, 1 << 14, (400,), generator=g), torch.randint(1 << 14, 1 << 28, (400,), generator=g)]).double()
+    x = (torch.rand(units.numel(), C, generator=g, dtype=torch.float64) * 2 - 1) * units[:, None]
+    x[:, C // 2] = units
+    x = (torch.round(x) * 2.0 ** -149).to(dt).to(DEV)
+    c, s = torch.full(x.shape, 99, dtype=torch.int8, device=DEV), torch.empty(x.shape[0], device=DEV)
+    B.dvdq_quantize_rows(x, c, s)
+    top = x.double().abs().amax(-1)
+    assert torch.equal(s.cpu(), top.cpu().float() / torch.full_like(top, 127.0).cpu().float())
+    assert (s == 0).any() or dt is torch.bfloat16
+    want = quotient(x, s).clamp(-127, 127)
+    small = s.cpu() < 2.0 ** -126
+    assert small.any() and torch.equal(c.cpu()[small].float(), torch.round(want)[small])
+    off = (c.double() * s.double()[:, None] - x.double()).abs() - s.double()[:, None] / 2 * (1 + 2.0 ** -14) - 127 * 2.0 ** -150
+    assert float(off.max()) <= 0
