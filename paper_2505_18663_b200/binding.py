@@ -543,7 +543,9 @@ LINEAR_INT8_ARGS = struct.Struct("16qii")
 def _current(t: torch.Tensor, name: str) -> int:
     """The current device, which the calls run on; a tensor that is elsewhere is refused."""
     dev = t.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if dev != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     return dev
 
