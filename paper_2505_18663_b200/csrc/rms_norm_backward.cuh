@@ -414,6 +414,9 @@ inline bool rms_by_columns(int64_t rows, int64_t C, int bytes, int v, int at_onc
     return rows < kColumnsBelow && ceil_div(rows, at_once) <= kColumnRows && rows * C * bytes <= (int64_t)(v > 2 ? 16 : 2 * v) << 20;
 }
 
+// Whether that is built for P pieces that fill a CTA's threads: those that the fewest rounds (launch_rms_backward_v) ever choose.
+__host__ __device__ constexpr bool full_columns(int V, int P) { return V == 8 ? P != 2 && P != 6 : P != 4; }
+
 template <typename T, int V, int P, bool WIDE, bool FULL>
 static cudaError_t launch_rms_backward_p(const RmsBackwardArgs& A0, const RowsPlan& p, int64_t parts, int* ctas_out, cudaStream_t st) {
     RmsBackwardArgs A = A0;
@@ -421,7 +424,7 @@ static cudaError_t launch_rms_backward_p(const RmsBackwardArgs& A0, const RowsPl
     A.lanes_log2 = p.lanes_log2;
     const int groups = WIDE ? 1 : kSmallThreads / p.lanes;
     const int64_t all = ceil_div(A.shape.rows, groups);
-    if constexpr (P > 0) {
+    if constexpr (P > 0 && !(WIDE && FULL && !full_columns(V, P))) {
         constexpr int LN = column_lanes<T, V>();
         if (A.dgamma && rms_by_columns(A.shape.rows, A.shape.C, (int)sizeof(T), V, p.threads / LN)) {
             auto kern = rms_norm_backward_kernel<T, V, P, WIDE, FULL, true>;
@@ -525,7 +528,7 @@ static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts
             int64_t least = INT64_MAX;
             for (int k = 1; k <= 8; ++k) {
                 const int64_t threads = nv / k;
-                if (nv % (32 * k) != 0 || threads < 64 || threads > kRowThreads || threads > rows_threads_backward(V, k)) continue;
+                if (!full_columns(V, k) || nv % (32 * k) != 0 || threads < 64 || threads > kRowThreads || threads > rows_threads_backward(V, k)) continue;
                 if (!rms_by_columns(A.shape.rows, A.shape.C, (int)sizeof(T), V, (int)threads / column_lanes<T, V>())) continue;
                 const int64_t rounds = ceil_div(ctas, 148 * (65536 / (rows_registers_backward(V, k) * threads)));
                 if (rounds >= least) continue;
@@ -534,16 +537,16 @@ static cudaError_t launch_rms_backward_v(const RmsBackwardArgs& A, int64_t parts
                 p.lanes = p.threads = (int)threads;
             }
         }
-        if (p.full) {
+        if (p.full) {  // rows of a warp or less (at most 64 pieces) come in 1, 2, 3 or 5 a thread
             switch (p.pieces) {
                 case 1: return launch_rms_backward_w<T, V, 1, true>(A, p, parts, ctas, st);
                 case 2: return launch_rms_backward_w<T, V, 2, true>(A, p, parts, ctas, st);
                 case 3: return launch_rms_backward_w<T, V, 3, true>(A, p, parts, ctas, st);
-                case 4: return launch_rms_backward_w<T, V, 4, true>(A, p, parts, ctas, st);
+                case 4: return launch_rms_backward_p<T, V, 4, true, true>(A, p, parts, ctas, st);
                 case 5: return launch_rms_backward_w<T, V, 5, true>(A, p, parts, ctas, st);
-                case 6: return launch_rms_backward_w<T, V, 6, true>(A, p, parts, ctas, st);
-                case 7: return launch_rms_backward_w<T, V, 7, true>(A, p, parts, ctas, st);
-                default: return launch_rms_backward_w<T, V, 8, true>(A, p, parts, ctas, st);
+                case 6: return launch_rms_backward_p<T, V, 6, true, true>(A, p, parts, ctas, st);
+                case 7: return launch_rms_backward_p<T, V, 7, true, true>(A, p, parts, ctas, st);
+                default: return launch_rms_backward_p<T, V, 8, true, true>(A, p, parts, ctas, st);
             }
         }
     }
