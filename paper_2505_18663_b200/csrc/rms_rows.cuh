@@ -371,13 +371,26 @@ inline bool rows_sizes_ok(int64_t N, int64_t S, int64_t C) {
     const int64_t most = 0x7FFFFFFFll;
     return N >= 0 && S >= 0 && N <= most && S <= most && N * S <= most && C > 0 && C <= (1 << 20);
 }
+// Whether rows of C elements that start at n * outer + s * row lie over one another (both pitches C or more).
+inline bool rows_collide(int64_t N, int64_t S, int64_t C, int64_t outer, int64_t row) {
+    if (N <= 1 || S <= 1) return false;
+    const bool rows_inside = row <= outer;
+    const int64_t inner = rows_inside ? row : outer, wide = rows_inside ? outer : row, steps = (rows_inside ? S : N) - 1;
+    if (inner > ((int64_t)1 << 61) / steps) return false;  // no memory holds such rows
+    const int64_t last = steps * inner;
+    for (int64_t k = 1, at = wide; k < (rows_inside ? N : S) && at < last + C; ++k, at += wide) {  // at most the smaller extent's number of turns
+        const int64_t below = at - at / inner * inner;
+        if (at > last || below < C || inner - below < C) return true;
+    }
+    return false;
+}
 // An [N, S, C] tensor's pitches; those of an extent of one are not read.
 inline dvdq_status check_rows(RowsOf* t, int64_t N, int64_t S, int64_t C, int bytes, bool written) {
     if (!t->p) return DVDQ_OK;
     if (N == 1) t->outer = 0;
     if (S == 1) t->row = 0;
     if (t->outer < 0 || t->row < 0) return DVDQ_ERR_SHAPE;
-    if (written && ((S > 1 && t->row < C) || (N > 1 && t->outer < C))) return DVDQ_ERR_SHAPE;  // outputs may not overlap
+    if (written && ((S > 1 && t->row < C) || (N > 1 && t->outer < C) || rows_collide(N, S, C, t->outer, t->row))) return DVDQ_ERR_SHAPE;  // a row over another
     return aligned_to(t->p, bytes) ? DVDQ_OK : DVDQ_ERR_ALIGN;
 }
 // An output over the tensor that it is made from lies exactly over it (after check_rows).
