@@ -435,9 +435,9 @@ dvdq_status dvdq_group_norm_backward(const void* dY, int64_t dy_sample, int64_t 
  *   gamma [C] or NULL (ones), of type param_dtype: X's, or DVDQ_F32
  *   H, Y      of X's type, codes int8 (pitches like X's, in elements), scales and rstd_out fp32, dense [N, S]; each may be NULL, but
  *             codes and scales come together, and something is asked for
- * h, y and c are computed in fp32 and rounded once each: y and c come from the h that is not yet rounded.  c has the code of the fp32 quotient of y and the s
- * that is written wherever y is half of an odd number of max |y| / 127, and everywhere for rows of 16-bit values (dvdq_quantize_rows); elsewhere the quotient may
- * be off by 2^-22 of itself, and next to a border c is one of the two codes beside it.  (A scale below 2^-126 is
+ * h, y and c are computed in fp32 and rounded once each: y and c come from the h that is not yet rounded.  c is 127 y / max |y| rounded half to even:
+ * to the bit for rows of 16-bit values (dvdq_quantize_rows), and without gamma wherever that is half of an odd number (half of the largest value has code 64); else
+ * it may be off by 2^-21 of itself, and next to a border c is one of the two codes beside it.  (A scale below 2^-126 is
  * a multiple of 2^-149 like any number there: codes count it as it is written, up to 127 of it, and a row whose scale is 0 has codes 0.)  Rows of values whose squares
  * leave fp32's range are scaled by a power of two first.  A row of zeros has scale 0 and codes 0; a row whose y holds a value that
  * is not finite has scale NaN and codes 0.

@@ -100,13 +100,12 @@ __device__ __forceinline__ void rows_load(const RowLanes<V, P, KIND>& L, RowValu
     }
 }
 
-// What turns a row's values into codes, c = round_half_even(v / scale) with the scale that is written.
+// What turns a row's values into codes, c = round_half_even(v / (top / 127)).
 //
-// Plain rows are multiplied by `inv`, 127 / top to 2^-23.  Of a row in 16 bits no value lies that near a border without lying on it (254 v and (2 n + 1) top are
-// multiples of one number), and on it, 254 v = (2 n + 1) top, only if it is half of the largest value, n = 63, or if top is a multiple of 127.  So inv is the
-// neighbour of 127 / top above it or below it, whichever gives top / 2 the code of its quotient in fp32 (127 / top rounded to nearest gave it the other code in
-// half of all rows), and rows whose top / 127 is exact, but not 127 / top, are divided, as are rows far from one or near the smallest numbers.
-// (All rows by a corrected reciprocal: 32760 x 8960 142 us, 134 this way.)
+// Plain rows are multiplied by `inv`, 127 / top rounded up.  Of a row in 16 bits no value lies within 2^-19 of a border without lying on it (254 v and (2 n + 1) top
+// are multiples of one number), and on it, 254 v = (2 n + 1) top, only if it is half of the largest value, n = 63, or if top is a multiple of 127.  Half of the largest
+// value then lies above 63.5 steps or on them and has the even code, 64 (with 127 / top rounded to nearest it had 63 in half of all rows); rows whose top / 127 is
+// exact, but not 127 / top, are divided, as are rows far from one or near the smallest numbers.  (All rows by a corrected reciprocal: 32760 x 8960 142 us, 134 this way.)
 struct RowCodes {
     float scale, inv;   // as written; the factor of plain rows
     bool plain;
@@ -116,20 +115,16 @@ struct RowCodes {
         if (top <= 3.4028235e38f) scale = top / 127.0f;  // not NaN, not infinite
         plain = o.f == 1.0f && top == 0.f;               // zeros
         if (!(o.f == 1.0f && top >= kLiftBelow && top <= 3.4028235e38f)) return;
-        const float rest = fmaf(-63.5f, scale, 0.5f * top);  // of top / 2 over 63.5 steps, exact
-        plain = rest != 0.f || (__float_as_uint(scale) & 0x7FFFFFu) == 0u;
+        plain = fmaf(scale, -127.0f, top) != 0.f || (__float_as_uint(scale) & 0x7FFFFFu) == 0u;
         inv = 127.0f / top;
-        const float over = fmaf(inv, top, -127.0f);
-        // (top / 2) / scale in fp32 is 63.5 or more down to half a unit of its last place, 2^-19, below
-        const bool up = rest >= scale * -0x1p-19f;
-        if (up ? over < 0.f : over > 0.f) inv = __uint_as_float(__float_as_uint(inv) + (up ? 1u : 0xFFFFFFFFu));
+        if (fmaf(inv, top, -127.0f) < 0.f) inv = __uint_as_float(__float_as_uint(inv) + 1u);
     }
     static constexpr float kLiftBelow = 1e-27f;
 };
-// Quotients of values by a row's scale, those of a division in fp32: from the reciprocal, corrected once by the remainder (Markstein 1990; for the mantissa of every scale
-// and the values around each of its borders the codes were compared with the division's).  Zeros where the row has no scale.  Values near the smallest numbers are
-// lifted first, so that the reciprocal stays finite and remainders have all their digits; a scale below 2^-126 has few digits itself, so that quotients by it may
-// pass 127, where codes end.
+// Quotients of values by top / 127 rounded down, so that half of the largest value has code 64 here too; those of a division in fp32: from the reciprocal, corrected once
+// by the remainder (Markstein 1990; for the mantissa of every divisor and the values around each of its borders the codes were compared with the division's).  Zeros where
+// the row has no scale.  Values near the smallest numbers are lifted first, so that the reciprocal stays finite and remainders have all their digits.  A scale below
+// 2^-126 has few digits itself and is what is divided by, so that its codes count it as it is written; quotients by it may pass 127, where codes end.
 struct RowDivide {
     float lift, step, recip;
     __device__ __forceinline__ RowDivide(float top) : lift(0.f), step(1.f), recip(0.f) {
@@ -137,6 +132,7 @@ struct RowDivide {
         if (scale == 0.f) return;
         lift = top < RowCodes::kLiftBelow ? 18446744073709551616.0f : 1.0f;
         step = scale * lift;
+        if (scale >= 1.17549435e-38f && fmaf(step, 127.0f, -top * lift) > 0.f) step = __uint_as_float(__float_as_uint(step) - 1u);
         recip = 1.0f / step;
     }
     __device__ __forceinline__ uint64_t operator()(uint64_t v) const {
