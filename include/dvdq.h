@@ -461,7 +461,7 @@ dvdq_status dvdq_rms_norm(const dvdq_rms_norm_args* args /* host */, void* cuda_
 /* Its gradients, with H the h of the forward call (X itself where there was no residual) and hh = h rstd:
  *   dX = rstd (gamma dy - hh <gamma dy hh>) + dH, <.> the mean over the row: the gradient of x and of r alike.  dH (or NULL): the gradient
  *        that reaches h by another way, along the residual stream
- *   dgamma = sum over rows of dy hh (fp32 [C]), in a fixed order
+ *   dgamma = sum over rows of dy hh (fp32 [C]), in a fixed order: the rows that a CTA takes one after another in fp32, those sums in fp64
  * dX and dgamma may each be NULL, not both.  dX may be dY, H or dH itself (same pitches).  The workspace (256-byte aligned) is needed for dgamma
  * only.  N * S == 0: dgamma is zeros.  The codes' rounding has no gradient: through it, dy is taken as that of y. */
 size_t dvdq_rms_norm_backward_workspace_bytes(int64_t N, int64_t S, int64_t C);
@@ -493,7 +493,8 @@ dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx,
  *   A [M, K] int8 codes with a_scales s [M], W [N, K] int8 codes with w_scales t [N] (fp32): of dvdq_rms_norm or
  *   dvdq_quantize_rows, or any codes in [-128, 127]; row pitches lda, ldw
  *   bias [N] or NULL, R [M, N] or NULL (the residual, pitch ldr; may be Y itself, same pitch), Y [M, N]: all DVDQ_BF16 or all DVDQ_F16
- * The sums over k are exact (int32: K < 131072); scales, bias, activation and residual in fp32, one rounding.  A row's result does not
+ * The sums over k are exact (int32: K < 131072); scales, bias, activation and residual in fp32, one rounding.  s_m t_n is formed first: it is to stay
+ * within fp32's range itself (below 2^-126 it holds fewer digits).  A row's result does not
  * depend on the rows beside it.  Matrices start on 16 bytes and pitches are multiples of 16 bytes (DVDQ_ERR_ALIGN); M, N and K themselves
  * are arbitrary, and what lies between a row's last element and the pitch is not used and not written.  The pitch of a single row is
  * not read.  M == 0 is a no-op.  Apart from R = Y, the output overlaps nothing that the call reads.  Workspace: 256-byte aligned, often 0. */

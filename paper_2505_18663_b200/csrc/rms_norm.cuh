@@ -11,9 +11,9 @@
 // what a row costs beside its pieces (addresses, exchange, root, division) is paid by each of its threads.  CTAs go from row to row and their threads keep
 // their channels, so that gamma stays in registers.  Instructions, not latency, were the next bound at each step: elements of 16 bits kept in
 // words, no branch in the inner loops (kernels for what is asked for, for rows that fill the threads), addresses that differ by constants (32760 x 5120 with
-// residual and codes: 538, 250, 189, 182 us).  Rows beyond a CTA's registers (P = 0) are read again from L2.
-// Measured: 32760 x 5120 bf16, residual, codes 182 us (1174 MB, 6.5 TB/s); residual, y 210 us; rows of 8960 in 8 bits 135 us (6.5 TB/s); 32760 x 12 heads of
-// 128 in a fused projection 34.6 us (5.8 TB/s); 20000 x 1541 (odd: single elements) 77 us (3.2 TB/s); 30000 x 2049 fp32 176 us (5.6 TB/s).
+// residual and codes: 538, 250, 189, 182, and 179 us since rows that are far from one have a loop of their own).  Rows beyond a CTA's registers (P = 0) are read again from L2.
+// Measured: 32760 x 5120 bf16, residual, codes 179 us (1174 MB, 6.6 TB/s); residual, y 208 us; rows of 8960 in 8 bits 133 us (6.6 TB/s); 32760 x 12 heads of
+// 128 in a fused projection 34.3 us (5.8 TB/s); 20000 x 1541 (odd: single elements) with residual, y 75 us (3.3 TB/s); 30000 x 2049 fp32 173 us (5.7 TB/s).
 #pragma once
 
 #include "rms_rows.cuh"
