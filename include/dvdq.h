@@ -484,7 +484,7 @@ dvdq_status dvdq_rms_norm_backward(const dvdq_rms_norm_backward_args* args /* ho
  *
  * s_m = max |x_m| / 127, c = round_half_even(x / s) as above, in natural order: codes [M, K] int8, row pitch ldc (a multiple of
  * 16 for dvdq_linear_int8), scales [M] fp32.  X [M, K] of any dtype, row pitch ldx: tokens, or a layer's weights (a scale for each
- * output channel).  M < 2^31, K <= 2^20. */
+ * output channel).  The codes overlap nothing that is read.  M < 2^31, K <= 2^20. */
 dvdq_status dvdq_quantize_rows(const void* X, int64_t M, int64_t K, int64_t ldx, int8_t* codes, int64_t ldc, float* scales,
                                int32_t dtype, void* cuda_stream);
 
